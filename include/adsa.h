@@ -86,6 +86,9 @@ typedef enum {
 #define ADSA_DEV_RING_TIMEOUT 8u   /* bounded wait on a free-ring entry ran out */
 #define ADSA_DEV_BAD_EVICT 16u     /* hole/survivor pairing of the compaction did not balance */
 #define ADSA_DEV_COPY_TIMEOUT 32u  /* bounded wait on a bulk copy into shared memory ran out */
+/* ... and of the status words that the calls on a paged whole-token cache take (adsa_paged_append, adsa_shared_prefix_attn) */
+#define ADSA_DEV_BAD_PAGE 64u      /* a page table names a page outside the pool */
+#define ADSA_DEV_BAD_GROUPS 128u   /* group boundaries do not ascend */
 
 typedef struct {
     int32_t n_layers, batch, n_heads; /* multi-head attention: one KV head per query head */
@@ -410,6 +413,102 @@ ADSA_API int adsa_swiglu(const void *gate, const void *up, void *out, long long 
  * One block per image; sums are taken in fp32 in a fixed order, so a call is reproducible. */
 ADSA_API int adsa_cfg_sample(const void *logits, int n_images, int vocab, float scale, int top_k, float temperature,
                              const float *uniforms, int32_t *tokens, adsa_stream_t stream);
+
+/* ---- many images of one prompt: a cache of whole tokens with shared prefixes -------------------------------------
+ * The streams of a context are private to their image, which eviction needs.  Where nothing is evicted and several
+ * images continue the same rows (one prompt, one null condition, earlier frames), those rows are kept once and every
+ * decode step reads them once for all images.  The four calls below are one such step around the caller's GEMMs:
+ * rotary positions, the rotated append into the cache, the attention, the norms with the residual.  They are
+ * stateless, on caller-owned buffers, and need no context.
+ *
+ * Rules they share.  All pointers are [device] unless marked [host] and belong to the current device.  16-bit tensors
+ * are ADSA_BF16 or ADSA_F16, all tensors of a call the same; strides are in elements, the innermost dimension is
+ * dense; arithmetic is fp32 and each output is rounded once, to nearest even.  Calls only enqueue kernels on `stream`,
+ * may be captured into a graph, and read lengths, tables and positions when they run.  ADSA_EINVAL (null pointer,
+ * misaligned buffer, size outside the stated range) and ADSA_ENOMEM are found before anything is launched.  What only
+ * the device can see sets bits of *status (one word, only ever ORed into; NULL: not wanted) and skips the access. */
+typedef enum { ADSA_BF16 = 0, ADSA_F16 = 1, ADSA_F32 = 2 } adsa_dtype;
+
+#define ADSA_MAX_HEAD_DIM 256
+#define ADSA_MAX_NORM_DIM 16384
+
+/* A paged pool of whole tokens: k_pool, v_pool [n_pages][n_kv_heads][page_rows][row_stride], 16-byte aligned.  Logical
+ * row r of a sequence with page table t lies in page t[r / page_rows], row r % page_rows.  row_stride is a multiple of
+ * 8; elements past head_dim are padding, which the append writes as zero and the attention does not read.  Any
+ * page_rows works; the attention copies boxes of the largest power of two (up to 64 rows) that divides it. */
+typedef struct {
+    void *k_pool, *v_pool;
+    int32_t dtype;                    /* ADSA_BF16 or ADSA_F16 */
+    int32_t n_pages, n_kv_heads;
+    int32_t page_rows;                /* 1 .. 4096; n_pages * n_kv_heads * page_rows < 2^31 */
+    int32_t head_dim, row_stride;     /* head_dim even, 2 .. row_stride; row_stride a multiple of 8, <= 256 */
+} adsa_paged_kv;
+
+/* Rotary positions with up to four axes (time, height, width, ...).  Filled on the host by adsa_rotary_init. */
+typedef struct {
+    int32_t head_dim, n_axes, n_pairs, halves;
+    double turns[ADSA_MAX_HEAD_DIM / 2];   /* theta_i / (2 pi) */
+    uint8_t axis[ADSA_MAX_HEAD_DIM / 2];   /* the axis pair i turns with */
+} adsa_rotary;
+
+/* pairs: [host] [n_axes], how many pairs of elements turn with each axis, in order; n = their sum, 2 n <= head_dim;
+ * elements past 2 n do not turn.  Pair i is elements (2i, 2i+1), or (i, i + n) with halves.  Its angle is
+ * pos[axis] * theta_i; theta_i = base^(-j / pairs[axis]) with restart, j counting within the axis (two axes of
+ * head_dim / 4 pairs: the angles of adsa_rope_2d), else base^(-i / n).  base 0 => 10000.  No CUDA call is made. */
+ADSA_API int adsa_rotary_init(adsa_rotary *rot, int head_dim, int n_axes, const int32_t *pairs, int halves, int restart, double base);
+
+/* out = x turned.  x, out: 16-bit [n_tokens][n_heads][head_dim] with the given token and head strides; out may be x
+ * (same strides), and must not overlap it otherwise.  pos: int32 [n_tokens][n_axes], any value.  Angles are reduced
+ * in 64 bits, so far positions keep their fraction of a turn. */
+ADSA_API int adsa_rope_axes(const adsa_rotary *rot, int dtype, const void *x, long long x_token, long long x_head, const int32_t *pos,
+                            long long n_tokens, int n_heads, void *out, long long out_token, long long out_head, adsa_stream_t stream);
+
+/* New rows into the cache, k turned on the way (and q, in the same launch, if given).
+ *   page_table  int32 [batch][max_pages];  n_rows  int32 [batch]: rows of each batch row's sequence before the call
+ *   cu_tokens   int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 belong to batch row b; tokens before cu[0] and
+ *               from cu[batch] on are padding (nothing is read or written for them).  NULL: n_tokens / batch tokens each
+ *   k, v        [n_tokens][n_kv_heads][head_dim];  token j of batch row b becomes logical row n_rows[b] + j
+ *   rot, pos    as adsa_rope_axes, rot->head_dim == kv->head_dim; rot NULL: nothing turns and pos is not read
+ *   q, q_out    [n_tokens][n_heads][head_dim], turned like k; n_heads 0: none; q_out may be q (same strides)
+ * Rows past the page table set ADSA_DEV_ROW_OVERFLOW, pages outside the pool ADSA_DEV_BAD_PAGE; such a token's k and v
+ * are not written.  n_rows is not changed.  No two tokens of a call may fall on the same row of the same page. */
+ADSA_API int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_table, int batch, int max_pages, const int32_t *n_rows,
+                               const int32_t *cu_tokens, long long n_tokens, const void *k, long long k_token, long long k_head,
+                               const void *v, long long v_token, long long v_head, const adsa_rotary *rot, const int32_t *pos,
+                               const void *q, int n_heads, long long q_token, long long q_head, void *q_out, long long q_out_token,
+                               long long q_out_head, uint32_t *status, adsa_stream_t stream);
+
+/* Decode attention, one query token per batch row, over a prefix that each group of batch rows shares and the batch
+ * row's own rows:  out = softmax_j(q.k_j * scale) . v_j  over rows 0 .. prefix_rows[g]-1 of prefix_table[g] and rows
+ * 0 .. n_rows[b]-1 of page_table[b].  A prefix is swept once for all rows of its group.
+ *   q            16-bit [batch][n_heads][head_dim], 4-byte aligned, even strides; n_heads = g * n_kv_heads with g <= 64:
+ *                query head h reads key head h / g
+ *   n_rows, prefix_rows   int32, each clamped to 0 .. what its table holds; table entries past them are not read
+ *   group_start  int32 [n_groups + 1], ascending: batch rows group_start[g] .. group_start[g+1]-1 are group g; batch
+ *                rows of no group have no prefix.  n_groups may be 0.  Boundaries are clamped to 0 .. batch
+ *   out, out_f32 16-bit / float [batch][n_heads][head_dim], either may be NULL, not both
+ *   lse          float [batch][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
+ * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).
+ * batch + n_groups <= 8192.  workspace: [device] 256-byte aligned, adsa_shared_prefix_workspace_bytes of them, nothing
+ * kept in it from call to call: calls that may overlap on the GPU (other streams, graphs in flight) need one each. */
+ADSA_API int adsa_shared_prefix_workspace_bytes(int batch, int n_groups, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes);
+ADSA_API int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_row, long long q_head, int batch, int n_heads,
+                                     const int32_t *page_table, int max_pages, const int32_t *n_rows, const int32_t *prefix_table,
+                                     int max_prefix_pages, const int32_t *prefix_rows, const int32_t *group_start, int n_groups,
+                                     float softmax_scale, void *out, float *out_f32, float *lse, void *workspace, size_t workspace_bytes,
+                                     uint32_t *status, adsa_stream_t stream);
+
+/* The norms around a block, with its gate and residual scale, row by row:
+ *   z  = y / sqrt(mean_j y_j^2 + eps) * w_post     (w_post NULL: z = y)
+ *   x' = x + scale * gate * z                      (gate NULL: 1)
+ *   h  = x' / sqrt(mean_j x'_j^2 + eps) * w_pre    (h and w_pre NULL: only x' is wanted)
+ *   y, h         16-bit [rows][dim];  w_post, w_pre  16-bit [dim];  x, x_out  [rows][dim], 16-bit or ADSA_F32 (x_dtype)
+ *   gate         16-bit [n_gates][dim], rows a multiple of n_gates: row r takes gate r / (rows / n_gates)
+ * h is made from x' before x' is rounded.  x_out may be x, h may be y.  dim a multiple of 8, 8 .. 16384; all 16-byte
+ * aligned. */
+ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const void *x, const void *w_post, const void *gate,
+                                long long n_gates, const void *w_pre, void *x_out, void *h, long long rows, int dim, float scale, float eps,
+                                adsa_stream_t stream);
 
 ADSA_API const char *adsa_strerror(int status);
 

@@ -5,10 +5,16 @@ from .binding import (  # noqa: F401
     AdsaEngine,
     AdsaError,
     EXPORTS,
+    Rotary,
     cfg_sample,
     decode_attn_static,
     load,
+    norm_residual,
+    paged_append,
     rmsnorm,
+    rope_axes,
+    shared_prefix_attn,
+    shared_prefix_workspace,
     strerror,
     swiglu,
     workspace_bytes,

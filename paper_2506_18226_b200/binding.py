@@ -17,6 +17,9 @@ from .build import build_lib
 OK, EINVAL, ESTATE, ENOMEM, ECUDA = 0, -1, -2, -3, -4
 DEV_POOL_EXHAUSTED, DEV_BAD_POSITION, DEV_ROW_OVERFLOW, DEV_RING_TIMEOUT, DEV_BAD_EVICT, DEV_COPY_TIMEOUT = \
     1, 2, 4, 8, 16, 32
+DEV_BAD_PAGE, DEV_BAD_GROUPS = 64, 128
+BF16, F16, F32 = 0, 1, 2
+_DTYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 EXPORTS = [
     "adsa_workspace_bytes", "adsa_create", "adsa_destroy", "adsa_reset", "adsa_prefill_rows",
@@ -24,6 +27,8 @@ EXPORTS = [
     "adsa_layer_step", "adsa_layer_step_host", "adsa_token_step", "adsa_token_step_gated", "adsa_token_step_host", "adsa_plan_attn", "adsa_set_attn_chunk_rows", "adsa_set_staged", "adsa_set_ring_stages", "adsa_set_l2_lookahead", "adsa_set_next_layer_hint", "adsa_set_token_launch", "adsa_set_host_chunks", "adsa_set_stream_warps", "adsa_set_single_sweep",
     "adsa_layer_rows_bound", "adsa_get_status", "adsa_launch_count", "adsa_strerror", "adsa_decode_attn_static",
     "adsa_rmsnorm", "adsa_swiglu", "adsa_cfg_sample",
+    "adsa_rotary_init", "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn",
+    "adsa_norm_residual",
 ]
 
 
@@ -40,6 +45,16 @@ class AdsaBuffers(C.Structure):
                 ("free_state", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class AdsaPagedKv(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p)] + \
+        [(n, C.c_int32) for n in ("dtype", "n_pages", "n_kv_heads", "page_rows", "head_dim", "row_stride")]
+
+
+class AdsaRotary(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "n_axes", "n_pairs", "halves")] + \
+        [("turns", C.c_double * 128), ("axis", C.c_uint8 * 128)]
+
+
 class AdsaError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -54,7 +69,7 @@ def load(rebuild: bool = False) -> C.CDLL:
     global _lib
     if _lib is None or rebuild:
         lib = C.CDLL(build_lib(rebuild))
-        vp, i32, sz = C.c_void_p, C.c_int, C.c_size_t
+        vp, i32, sz, ll = C.c_void_p, C.c_int, C.c_size_t, C.c_longlong
         sig = {
             "adsa_workspace_bytes": [C.POINTER(AdsaConfig), C.POINTER(sz)],
             "adsa_create": [C.POINTER(AdsaConfig), C.POINTER(AdsaBuffers), C.POINTER(vp)],
@@ -89,6 +104,12 @@ def load(rebuild: bool = False) -> C.CDLL:
             "adsa_rmsnorm": [vp, vp, vp, C.c_longlong, i32, C.c_float, vp],
             "adsa_swiglu": [vp, vp, vp, C.c_longlong, i32, C.c_longlong, vp],
             "adsa_cfg_sample": [vp, i32, i32, C.c_float, i32, C.c_float, vp, vp, vp],
+            "adsa_rotary_init": [C.POINTER(AdsaRotary), i32, i32, C.POINTER(C.c_int32), i32, i32, C.c_double],
+            "adsa_rope_axes": [vp, i32, vp, ll, ll, vp, ll, i32, vp, ll, ll, vp],
+            "adsa_paged_append": [vp, vp, i32, i32, vp, vp, ll, vp, ll, ll, vp, ll, ll, vp, vp, vp, i32, ll, ll, vp, ll, ll, vp, vp],
+            "adsa_shared_prefix_workspace_bytes": [i32, i32, i32, i32, i32, C.POINTER(sz)],
+            "adsa_shared_prefix_attn": [vp, vp, ll, ll, i32, i32, vp, i32, vp, vp, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, sz, vp, vp],
+            "adsa_norm_residual": [i32, i32, vp, vp, vp, vp, ll, vp, vp, vp, ll, i32, C.c_float, C.c_float, vp],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
@@ -169,6 +190,210 @@ def cfg_sample(logits, scale, top_k, temperature, uniforms, tokens=None):
     if rc:
         raise AdsaError(rc, "adsa_cfg_sample")
     return tokens
+
+
+# ---- many images of one prompt: rotary positions, paged append, shared-prefix attention, norms with the residual ----
+
+def _launch(name, like, *args):
+    """Call a stateless function on the device of `like` and torch's current stream there."""
+    fn, dev = getattr(load(), name), like.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} takes CUDA tensors")
+    if dev == torch._C._cuda_getDevice():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        raise AdsaError(rc, name)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _same_device(like, **tensors):
+    dev = like.get_device()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{name} is on another device")
+
+
+def _index(t, name, *shape):
+    """Checks an int32 index tensor: dense, with the given sizes (None: any)."""
+    if t.dtype is not torch.int32 or t.dim() != len(shape) or not t.is_contiguous() or \
+            any(want is not None and got != want for got, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {list(shape)}, got {t.dtype} {list(t.shape)}")
+
+
+def _rows3(t, name, dtype, tokens=None, heads=None, dim=None):
+    """Checks [tokens][heads][dim] rows, dense along the innermost dimension; returns (address, token and head stride)."""
+    shape = t.shape
+    if len(shape) != 3 or t.dtype is not dtype or (tokens is not None and shape[0] != tokens) or \
+            (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim):
+        raise ValueError(f"{name} must be {dtype} [{tokens}, {heads}, {dim}], got {t.dtype} {list(shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        raise ValueError(f"{name} must be dense along its last dimension")
+    return t.data_ptr(), s0, s1
+
+
+def _dtype16(t, name):
+    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float16:
+        raise ValueError(f"{name} must be bfloat16 or float16, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _paged_kv(k_pool, v_pool, head_dim):
+    """The descriptor of a pool [n_pages, n_kv_heads, page_rows, row_stride]."""
+    if k_pool.dim() != 4 or v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype or \
+            not (k_pool.is_contiguous() and v_pool.is_contiguous()):
+        raise ValueError("k_pool and v_pool must be contiguous [n_pages, n_kv_heads, page_rows, row_stride] tensors of one type")
+    pages, heads, rows, stride = k_pool.shape
+    return AdsaPagedKv(k_pool.data_ptr(), v_pool.data_ptr(), _dtype16(k_pool, "k_pool"), pages, heads, rows, head_dim, stride)
+
+
+class Rotary:
+    """adsa_rotary_init: rotary positions with one to four axes.
+
+    pairs: how many pairs of elements turn with each axis; style "pairs" (elements 2i, 2i+1) or "halves" (i, i + n);
+    restart: each axis starts again at frequency 1 (False: the frequencies run through all pairs)."""
+
+    def __init__(self, head_dim, pairs, base=10000.0, style="pairs", restart=True):
+        if style not in ("pairs", "halves"):
+            raise ValueError(f"style must be 'pairs' or 'halves', got {style!r}")
+        self.c = AdsaRotary()
+        self.head_dim, self.n_axes = head_dim, len(pairs)
+        rc = load().adsa_rotary_init(C.byref(self.c), head_dim, len(pairs), (C.c_int32 * len(pairs))(*pairs), style == "halves",
+                                     bool(restart), float(base))
+        if rc:
+            raise AdsaError(rc, "adsa_rotary_init")
+        self.ref = C.addressof(self.c)
+
+
+def rope_axes(rotary, x, pos, out=None):
+    """adsa_rope_axes: x [n_tokens, n_heads, head_dim] (any token and head stride) turned by pos, int32
+    [n_tokens, n_axes].  out may be x; default: a new tensor."""
+    dt = _dtype16(x, "x")
+    tokens, heads, d = x.shape
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    src = _rows3(x, "x", x.dtype, dim=rotary.head_dim)
+    dst = _rows3(out, "out", x.dtype, tokens, heads, d)
+    _index(pos, "pos", tokens, rotary.n_axes)
+    _same_device(x, pos=pos, out=out)
+    _launch("adsa_rope_axes", x, rotary.ref, dt, *src, pos.data_ptr(), tokens, heads, *dst)
+    return out
+
+
+def paged_append(k, v, k_pool, v_pool, page_table, n_rows, *, cu_tokens=None, rotary=None, pos=None, q=None, q_out=None,
+                 status=None):
+    """adsa_paged_append: rows k, v [n_tokens, n_kv_heads, head_dim] into the pools
+    [n_pages, n_kv_heads, page_rows, row_stride], k turned by pos on the way, and q [n_tokens, n_heads, head_dim] with it.
+
+    page_table int32 [batch, max_pages]; n_rows int32 [batch], rows before the call (not changed); cu_tokens int32
+    [batch + 1] or None (the same number of tokens for every batch row).  status: int32 [1] that device-side errors are
+    ORed into.  Returns q_out (a new tensor by default, q itself to turn in place), None without q."""
+    tokens, kv_heads, d = k.shape
+    kv = _paged_kv(k_pool, v_pool, d)
+    dtype, batch = k_pool.dtype, page_table.shape[0]
+    _index(page_table, "page_table", None, None)
+    _index(n_rows, "n_rows", batch)
+    if cu_tokens is not None:
+        _index(cu_tokens, "cu_tokens", batch + 1)
+    if status is not None:
+        _index(status, "status", 1)
+    src_k, src_v = _rows3(k, "k", dtype, tokens, kv.n_kv_heads, d), _rows3(v, "v", dtype, tokens, kv.n_kv_heads, d)
+    rot = None
+    if rotary is not None:
+        if rotary.head_dim != d or pos is None:
+            raise ValueError("the rotary needs pos and the head dimension of k")
+        _index(pos, "pos", tokens, rotary.n_axes)
+        rot = rotary.ref
+    heads, src_q, dst_q = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        heads = q.shape[1]
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        src_q, dst_q = _rows3(q, "q", dtype, tokens, None, d), _rows3(q_out, "q_out", dtype, tokens, heads, d)
+    _same_device(k, v=v, k_pool=k_pool, v_pool=v_pool, page_table=page_table, n_rows=n_rows, cu_tokens=cu_tokens, pos=pos, q=q,
+                 q_out=q_out, status=status)
+    _launch("adsa_paged_append", k, C.addressof(kv), page_table.data_ptr(), batch, page_table.shape[1], n_rows.data_ptr(),
+            _addr(cu_tokens), tokens, *src_k, *src_v, rot, _addr(pos) if rot else None, src_q[0], heads, src_q[1], src_q[2], *dst_q,
+            _addr(status))
+    return q_out if q is not None else None
+
+
+def shared_prefix_workspace(q, k_pool, page_table, prefix_table=None):
+    """The workspace shared_prefix_attn needs for these shapes (one for every call that may be in flight at a time)."""
+    out = C.c_size_t(0)
+    groups = 0 if prefix_table is None else prefix_table.shape[0]
+    with torch.cuda.device(q.device):
+        rc = load().adsa_shared_prefix_workspace_bytes(q.shape[0], groups, q.shape[1], k_pool.shape[1], q.shape[2], C.byref(out))
+    if rc:
+        raise AdsaError(rc, "adsa_shared_prefix_workspace_bytes")
+    return torch.empty(out.value, dtype=torch.uint8, device=q.device)
+
+
+def shared_prefix_attn(q, k_pool, v_pool, page_table, n_rows, prefix_table=None, prefix_rows=None, group_start=None, *, scale=0.0,
+                       out=None, out_f32=None, lse=None, workspace=None, status=None):
+    """adsa_shared_prefix_attn: one query token per batch row, q [batch, n_heads, head_dim], over the prefix of its group
+    and its own rows.
+
+    page_table int32 [batch, max_pages], n_rows int32 [batch]; prefix_table int32 [n_groups, max_prefix_pages],
+    prefix_rows int32 [n_groups], group_start int32 [n_groups + 1] (all three None: no prefix).  out 16-bit or out_f32
+    float [batch, n_heads, head_dim] (default: a new tensor like q), lse float [batch, n_heads].  workspace: from
+    shared_prefix_workspace; None takes one from torch's allocator for this call."""
+    batch, heads, d = q.shape
+    kv = _paged_kv(k_pool, v_pool, d)
+    src = _rows3(q, "q", k_pool.dtype)
+    _index(page_table, "page_table", batch, None)
+    _index(n_rows, "n_rows", batch)
+    groups = max_pp = 0
+    if prefix_table is not None:
+        groups, max_pp = prefix_table.shape
+        _index(prefix_table, "prefix_table", groups, max_pp)
+        _index(prefix_rows, "prefix_rows", groups)
+        _index(group_start, "group_start", groups + 1)
+    if status is not None:
+        _index(status, "status", 1)
+    if out is None and out_f32 is None:
+        out = torch.empty((batch, heads, d), dtype=q.dtype, device=q.device)
+    for name, t, dtype, shape in (("out", out, q.dtype, (batch, heads, d)), ("out_f32", out_f32, torch.float32, (batch, heads, d)),
+                                  ("lse", lse, torch.float32, (batch, heads))):
+        if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
+    if workspace is None:
+        workspace = shared_prefix_workspace(q, k_pool, page_table, prefix_table) if batch else torch.empty(0, dtype=torch.uint8, device=q.device)
+    _same_device(q, k_pool=k_pool, v_pool=v_pool, page_table=page_table, n_rows=n_rows, prefix_table=prefix_table,
+                 prefix_rows=prefix_rows, group_start=group_start, out=out, out_f32=out_f32, lse=lse, workspace=workspace, status=status)
+    _launch("adsa_shared_prefix_attn", q, C.addressof(kv), *src, batch, heads, page_table.data_ptr(), page_table.shape[1],
+            n_rows.data_ptr(), _addr(prefix_table), max_pp, _addr(prefix_rows), _addr(group_start), groups, float(scale), _addr(out),
+            _addr(out_f32), _addr(lse), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _addr(status))
+    return out if out is not None else out_f32
+
+
+def norm_residual(y, x, w_pre=None, *, w_post=None, gate=None, scale=1.0, eps=1e-5, x_out=None, h=None):
+    """adsa_norm_residual: x_out = x + scale * gate * norm(y) and h = norm(x_out), row by row; returns (x_out, h).
+
+    y [rows, dim] 16-bit, x [rows, dim] of the same type or float32; w_post [dim] or None (no norm on y); gate
+    [n_gates, dim] (rows / n_gates rows take each) or None; w_pre [dim] or None (then h is None).  x_out may be x, h
+    may be y; by default both are new."""
+    dt = _dtype16(y, "y")
+    rows, dim = y.shape
+    if x.shape != y.shape or x.dtype not in _DTYPES:
+        raise ValueError("x must have the shape of y, and its type or float32")
+    x_out = torch.empty_like(x) if x_out is None else x_out
+    if w_pre is not None and h is None:
+        h = torch.empty_like(y)
+    for name, t, like in (("y", y, y), ("x", x, x), ("x_out", x_out, x), ("h", h, y)):
+        if t is not None and (t.dtype is not like.dtype or t.shape != like.shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {like.dtype} tensor of shape {[rows, dim]}")
+    for name, t in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
+        if t is not None and (t.dtype is not y.dtype or t.shape[-1] != dim or t.dim() != (2 if name == "gate" else 1) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {y.dtype} tensor of {dim}-element rows")
+    _same_device(y, x=x, w_post=w_post, gate=gate, w_pre=w_pre, x_out=x_out, h=h)
+    _launch("adsa_norm_residual", y, dt, _DTYPES[x.dtype], y.data_ptr(), x.data_ptr(), _addr(w_post), _addr(gate),
+            0 if gate is None else gate.shape[0], _addr(w_pre), x_out.data_ptr(), _addr(h), rows, dim, float(scale), float(eps))
+    return x_out, h
 
 
 class AdsaEngine:
