@@ -6,16 +6,21 @@
 // so the prefix is swept ONCE per group and key head, by all of the group's queries together (a real matrix product:
 // members x query heads per key head rows against the prefix), and each batch row's own rows by its queries alone.
 //
-// Work split.  The unit is a tile of 64 cached rows of one key head.  All units of a call (of every prefix, 64 query
-// rows at a time, then of every batch row) form one list; block c of C takes units c U / C .. (c + 1) U / C, whatever
-// they belong to, so long and short rows, prefixes and single rows balance without the host knowing a length.  Where a block's
-// range changes from one item to the next it leaves the item's partial state in the workspace; a second small kernel
-// merges the states of each output row.  Lengths, tables and group boundaries are read on the device: a captured graph follows them.
+// Work split.  The unit is a tile of 64 cached rows of one key head.  All units of a call (of every prefix, 32 query
+// rows at a time, then of every batch row) form one list; run c of C takes units c U / C .. (c + 1) U / C, whatever
+// they belong to, so long and short rows, prefixes and single rows mix without the host knowing a length.  Where a run
+// changes from one item to the next it leaves the item's partial state in the workspace; a second small kernel merges
+// the states of each output row.  Lengths, tables and group boundaries are read on the device: a captured graph follows
+// them.  The grid is what fits the GPU; there are up to four times as many runs as blocks.  A block begins with the run
+// of its own index and then claims runs from a counter.  SMs differ in the bandwidth they get and items in their cost per tile: with
+// one run per block the slowest block took 279 us where the median took 225 (64 rows of 2304 x 32 heads x 100 elements).
+// What a run leaves does not depend on who ran it.
 //
-// What a warp does per 16 cached rows: S = Q K^T and O += P V on mma.sync tiles of 16 query rows.  Where 16 query rows
-// or fewer share a key head the four warps of a block split the cached rows of a tile, with up to 64 they split the query rows.
-// One query row per cached row is 1 flop per byte: HBM bounds it, and the products run on the tensor cores only
-// because that takes the fewest instructions per byte.
+// What a warp does per 16 cached rows: S^T = K Q^T and O^T += V^T P^T on mma.sync tiles with the cached rows as M and
+// eight query rows as N (the fewest that the instruction takes).  Up to 8 query rows of a key head: the four warps of a
+// block split the cached rows of a tile; up to 16: two and two; up to 32: each warp has its own eight query rows.  One query
+// row per cached row is 1 flop per byte: HBM bounds it, and the products run on the tensor cores only because that takes
+// the fewest instructions per byte.
 #include <cuda.h>
 #include <float.h>
 #include <math.h>
@@ -27,10 +32,19 @@
 namespace adsa {
 
 constexpr int kPaTile = 64;                 // cached rows of a unit
+constexpr int kPaQueries = 32;              // query rows of an item at most
 constexpr int kPaWarps = 4;                 // warps that compute; one more warp copies
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
 constexpr int kPaMaxEntries = 8192;         // groups + batch rows of a call
 constexpr int kPaMergeThreads = 128;
+
+// Hands out runs.  The merge of every call leaves it at zero behind the mark; where the mark is missing (a workspace's
+// first call) blocks take the runs in fixed turns instead, so a workspace needs no initialisation.
+struct RunCounter {
+    unsigned long long mark;
+    uint32_t next, spare;
+};
+constexpr unsigned long long kRunMark = 0xad5a5eedc0117e2bull;
 
 struct PrefixArgs {
     const void *q;
@@ -46,11 +60,18 @@ struct PrefixArgs {
     uint32_t *plan;                         // [entries + 1] first unit of every entry (groups, then batch rows)
     float *p_state, *p_ml, *o_state, *o_ml; // prefix slots, own-row slots: rows of d_pad floats, (m, l) pairs
     int n_p_slots, n_o_slots;
-    int blocks;                             // of the sweep kernel
+    RunCounter *counter;
+    int runs;
 };
 
-// how many warps share the query rows of an item with m of them (the rest share its cached rows)
-__host__ __device__ __forceinline__ int query_warps(int m) { return m <= 16 ? 1 : m <= 32 ? 2 : 4; }
+// how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
+__host__ __device__ __forceinline__ int query_warps(int m) { return m <= 8 ? 1 : m <= 16 ? 2 : 4; }
+// items of a key head with m query rows, and the query rows a slot of a batch row's own items must hold
+__host__ __device__ __forceinline__ int query_items(int m) { return (m + kPaQueries - 1) / kPaQueries; }
+__host__ __device__ __forceinline__ int own_slot_rows(int per_kv)
+{
+    return per_kv >= kPaQueries ? kPaQueries : kPaWarps / query_warps(per_kv) * per_kv;
+}
 
 __device__ __forceinline__ int clamp_rows(int n, int max_pages, int page_rows)
 {
@@ -66,21 +87,27 @@ __device__ __forceinline__ uint32_t entry_units(const PrefixArgs &a, int e)
     if (e < a.groups) {
         const int m = group_members(a, e) * a.per_kv;
         const int n = clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows);
-        return (uint32_t)((m + 63) / 64) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
+        return (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
     }
     const int n = clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
-    return (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
+    return (uint32_t)query_items(a.per_kv) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
 }
 
-// Every one of these blocks has a unit, so every state between an item's first and last block exists.
-__device__ __forceinline__ uint32_t working_blocks(const PrefixArgs &a, uint32_t total) { return min((uint32_t)a.blocks, total); }
+// A number no larger item of an earlier group reaches: sum of query_items over groups 0 .. g-1 <= begin per_kv / 32 + g
+__device__ __forceinline__ int first_p_item(const PrefixArgs &a, int g, int begin)
+{
+    return (int)(((long long)begin * a.per_kv / kPaQueries + g) * a.kv_heads);
+}
 
-// A run of units of one item inside a block's range.
+// Every one of these runs has a unit, so every state between an item's first and last run exists.
+__device__ __forceinline__ uint32_t working_runs(const PrefixArgs &a, uint32_t total) { return min((uint32_t)a.runs, total); }
+
+// Neighbouring units of one item inside a run.
 struct Segment {
     const int32_t *pages;                   // page table of the cached rows
     int n;                                  // cached rows of the item
     int head;                               // key head
-    int tile0, tiles;                       // the run
+    int tile0, tiles;                       // the units
     int row0, rows;                         // packed query rows (batch row * per_kv + head in the key head): first, count
     int slot;                               // of the partial state
     bool prefix;
@@ -89,17 +116,17 @@ struct Segment {
 struct Walk {
     const uint32_t *plan;                   // shared copy
     uint32_t u, end;
-    int e, entries, block;
-    __device__ void begin(const PrefixArgs &a, const uint32_t *plan_, int block_)
+    int e, run;
+    __device__ void begin(const PrefixArgs &a, const uint32_t *plan_, int run_)
     {
         plan = plan_;
-        entries = a.groups + a.batch;
-        block = block_;
-        const uint32_t total = plan[entries], blocks = working_blocks(a, total);
+        run = run_;
+        const int entries = a.groups + a.batch;
+        const uint32_t total = plan[entries], runs = working_runs(a, total);
         u = end = 0;
-        if ((uint32_t)block < blocks) {
-            u = (uint32_t)((unsigned long long)block * total / blocks);
-            end = (uint32_t)((unsigned long long)(block + 1) * total / blocks);
+        if ((uint32_t)run < runs) {
+            u = (uint32_t)((unsigned long long)run * total / runs);
+            end = (uint32_t)((unsigned long long)(run + 1) * total / runs);
         }
         int lo = 0, hi = entries;           // the last entry whose first unit is <= u
         while (lo < hi) {
@@ -114,32 +141,19 @@ struct Walk {
         if (u >= end) return false;
         while (u >= plan[e + 1]) ++e;
         const uint32_t at = u - plan[e];
-        uint32_t tiles;
-        if (e < a.groups) {
-            const int members = group_members(a, e), m = members * a.per_kv, mt = (m + 63) / 64;
-            s.n = clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows);
-            tiles = (uint32_t)((s.n + kPaTile - 1) / kPaTile);
-            const int item = (int)(at / tiles), b0 = group_begin(a, e);
-            s.head = item / mt;
-            const int q = item - s.head * mt;
-            s.row0 = b0 * a.per_kv + q * 64;
-            s.rows = min(m - q * 64, 64);
-            s.pages = a.p_table + (size_t)e * a.max_p_pages;
-            s.slot = (int)(((long long)b0 * a.per_kv / 64 + e) * a.kv_heads) + item + block;
-            s.prefix = true;
-            s.tile0 = (int)(at - (uint32_t)item * tiles);
-        } else {
-            const int b = e - a.groups;
-            s.n = clamp_rows(a.n_rows[b], a.max_pages, a.page_rows);
-            tiles = (uint32_t)((s.n + kPaTile - 1) / kPaTile);
-            s.head = (int)(at / tiles);
-            s.row0 = b * a.per_kv;
-            s.rows = a.per_kv;
-            s.pages = a.table + (size_t)b * a.max_pages;
-            s.slot = b * a.kv_heads + s.head + block;
-            s.prefix = false;
-            s.tile0 = (int)(at - (uint32_t)s.head * tiles);
-        }
+        const bool pre = e < a.groups;
+        const int b0 = pre ? group_begin(a, e) : e - a.groups, m = (pre ? group_members(a, e) : 1) * a.per_kv, mt = query_items(m);
+        s.n = pre ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[b0], a.max_pages, a.page_rows);
+        const uint32_t tiles = (uint32_t)((s.n + kPaTile - 1) / kPaTile);
+        const int item = (int)(at / tiles);                        // (key head, then query rows)
+        s.head = item / mt;
+        const int q = item - s.head * mt;
+        s.row0 = b0 * a.per_kv + q * kPaQueries;
+        s.rows = min(m - q * kPaQueries, kPaQueries);
+        s.pages = pre ? a.p_table + (size_t)e * a.max_p_pages : a.table + (size_t)b0 * a.max_pages;
+        s.slot = (pre ? first_p_item(a, e, b0) : b0 * a.kv_heads * mt) + item + run;
+        s.prefix = pre;
+        s.tile0 = (int)(at - (uint32_t)item * tiles);
         s.tiles = (int)min(tiles - (uint32_t)s.tile0, end - u);
         u += (uint32_t)s.tiles;
         return true;
@@ -184,6 +198,14 @@ __device__ __forceinline__ float pa_exp2(float x)
 template <typename T> struct WeightBias { static constexpr float value = 0.f; };
 template <> struct WeightBias<__half> { static constexpr float value = 8.f; };
 
+// the transpose of an 8 x 8 matrix of 16-bit elements held by a warp (row lane / 4, columns 2 (lane % 4), + 1)
+__device__ __forceinline__ uint32_t pa_transpose(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // NSUB: 64-element sub-tiles of a row (head elements / 64, rounded up).  STAGES: tiles in flight per block.
 template <typename T, int NSUB, int STAGES>
 __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
@@ -194,16 +216,18 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     constexpr int DP = 64 * NSUB;                                  // floats of a state row
     constexpr float kBias = WeightBias<T>::value;
     extern __shared__ unsigned char pa_smem[];
-    __shared__ uint64_t bars[2 * STAGES];
+    __shared__ uint64_t bars[2 * STAGES + 4];
+    __shared__ volatile int answers[2];
     __shared__ uint32_t warp_sums[kPaThreads / 32];
     const uint32_t ring = (smem_u32(pa_smem) + 1023u) & ~1023u;
     uint32_t *plan = reinterpret_cast<uint32_t *>(pa_smem + (ring - smem_u32(pa_smem)) + (size_t)STAGES * 2 * kHalf);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, asked = empty + 8 * STAGES, heard = asked + 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int entries = a.groups + a.batch;
 
     if (tid == 0) {
         for (int i = 0; i < STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, kPaWarps); }
+        for (int i = 0; i < 2; ++i) { mbar_init(asked + 8 * i, 1); mbar_init(heard + 8 * i, kPaWarps + 1); }
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
@@ -225,17 +249,47 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     for (int e = e0; e < e1; ++e) plan[e] += before;
     if (tid == kPaThreads - 1) plan[entries] = before + mine;
     __syncthreads();
-    if (blockIdx.x == 0)
-        for (int e = tid; e <= entries; e += kPaThreads) a.plan[e] = plan[e];
-
     Walk walk;
     walk.begin(a, plan, blockIdx.x);
     Segment s;
+    // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp claims the next run
+    // when it begins one, into the answer slot that all warps have read the last time.
+    const bool counted = a.counter->mark == kRunMark;              // (nobody writes the mark during a sweep)
+    const int runs = (int)working_runs(a, plan[entries]);
+    int limit = kCopySpinLimit;
+    uint32_t turns = 0;                                            // runs finished by this warp
+    const auto claim = [&]() {
+        const uint32_t i = turns & 1u;
+        if (!mbar_wait_bounded(heard + 8 * i, ((turns >> 1) & 1u) ^ 1u, limit)) limit = kCopySpinAfterTimeout;
+        answers[i] = counted ? (int)(gridDim.x + atomicAdd(&a.counter->next, 1u)) : (int)(blockIdx.x + (turns + 1u) * gridDim.x);
+        mbar_arrive(asked + 8 * i);
+    };
+    const auto advance = [&](Segment &n) {
+        while (!walk.next(a, n)) {
+            const uint32_t i = turns & 1u;
+            int run = runs;
+            if (mbar_wait_bounded(asked + 8 * i, (turns >> 1) & 1u, limit)) run = answers[i];
+            else {
+                limit = kCopySpinAfterTimeout;
+                if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(heard + 8 * i);
+            ++turns;
+            if (run >= runs) return false;
+            if (warp == kPaWarps && lane == 0) claim();
+            walk.begin(a, plan, run);
+        }
+        return true;
+    };
 
     if (warp == kPaWarps) {                                        // ---- the copying warp ----
-        int stage = 0, limit = kCopySpinLimit;
+        int stage = 0;
         uint32_t phase = 0;
-        while (walk.next(a, s)) {
+        if (lane == 0) claim();
+        if (blockIdx.x == 0)                                       // for the merge
+            for (int e = lane; e <= entries; e += 32) a.plan[e] = plan[e];
+        while (advance(s)) {
             for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
                 if (!mbar_wait_bounded(empty + 8 * stage, phase ^ 1u, limit)) {
                     limit = kCopySpinAfterTimeout;
@@ -268,32 +322,42 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
 
     // ---- the computing warps ----
     const int g = lane >> 2, t4 = lane & 3, mi = lane >> 3, lr = lane & 7;
-    int stage = 0, limit = kCopySpinLimit;
+    // lane's row address in a 16-row block for K (as A: cached rows x elements) and V (transposed: elements x cached rows)
+    const uint32_t k_row = (uint32_t)((mi & 1) * 8 + lr) * 128u, v_row = (uint32_t)((mi >> 1) * 8 + lr) * 128u;
+    const int k_ch = mi >> 1, v_ch = mi & 1;
+    int stage = 0;
     uint32_t phase = 0;
-    while (walk.next(a, s)) {
-        const int wq = query_warps(s.rows), wk = kPaWarps / wq;     // warps over query rows, warps over cached rows
-        const int qb = warp & (wq - 1), kb = warp / wq;
-        // Q as the A operand: rows g and g + 8 of this warp's sixteen, elements 16 ks + 2 t4, + 1 and + 8, + 9
-        uint32_t qa[KS][4];
-        {
-            const T *qp[2];
+    // Q^T as the B operand: query row g of this warp's eight, elements 16 ks + 2 t4, + 1 and + 8, + 9; asked for one segment ahead
+    uint32_t qn[KS][2];
+    const auto ask_q = [&](const Segment &n) {
+        const int qb = warp & (query_warps(n.rows) - 1), r = qb * 8 + g, packed = n.row0 + r, b = packed / a.per_kv, j = packed - b * a.per_kv;
+        const T *qp = (const T *)a.q + b * a.q_row + (n.head * a.per_kv + j) * a.q_head;
+        const bool there = r < n.rows;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = qb * 16 + g + 8 * h, packed = s.row0 + r, b = packed / a.per_kv, j = packed - b * a.per_kv;
-                qp[h] = r < s.rows ? (const T *)a.q + b * a.q_row + (s.head * a.per_kv + j) * a.q_head : nullptr;
-            }
+        for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int col = 16 * ks + 2 * t4 + (i >> 1) * 8;
-                    qa[ks][i] = qp[i & 1] && col < a.d ? *reinterpret_cast<const uint32_t *>(qp[i & 1] + col) : 0u;
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int col = 16 * ks + 2 * t4 + i * 8;
+                qn[ks][i] = there && col < a.d ? __ldg(reinterpret_cast<const uint32_t *>(qp + col)) : 0u;
             }
         }
-        float o[2 * KS][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+    };
+    Segment nxt;
+    bool more = advance(nxt);
+    if (more) ask_q(nxt);
+    while (more) {
+        s = nxt;
+        uint32_t qa[KS][2];
 #pragma unroll
-        for (int nb = 0; nb < 2 * KS; ++nb) { o[nb][0] = o[nb][1] = o[nb][2] = o[nb][3] = 0.f; }
+        for (int ks = 0; ks < KS; ++ks) { qa[ks][0] = qn[ks][0]; qa[ks][1] = qn[ks][1]; }
+        more = advance(nxt);
+        if (more) ask_q(nxt);
+        const int wq = query_warps(s.rows), wk = kPaWarps / wq;     // warps over query rows, warps over cached rows
+        const int qb = warp & (wq - 1), kb = warp / wq;
+        // state of query rows 2 t4 and 2 t4 + 1: maximum (alike in the eight lanes of a t4), this lane's share of the sum, O^T
+        float o[KS][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+#pragma unroll
+        for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
 
         for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
             if (!mbar_wait_bounded(full + 8 * stage, phase, limit)) {
@@ -303,102 +367,93 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             const uint32_t ks_u32 = ring + stage * 2 * kHalf, vs_u32 = ks_u32 + kHalf;
             const int valid = min(kPaTile, s.n - t * kPaTile);
             for (int c0 = kb * 16; c0 < valid; c0 += wk * 16) {     // sixteen cached rows
-                if (c0 + 16 > valid) {
-                    // rows behind the end hold anything; a weight of zero does not silence an infinity or a NaN of V
-                    for (int i = lane; i < 16 * 8 * NSUB; i += 32) {
-                        const int r = c0 + i / (8 * NSUB), ch = i % (8 * NSUB);
-                        if (r >= valid)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};"
-                                         ::"r"(vs_u32 + (ch >> 3) * kSub + r * 128 + (ch & 7) * 16), "r"(0u) : "memory");
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before the next copy into these bytes
-                    __syncwarp();
-                }
-                float sc[2][4];
-#pragma unroll
-                for (int nb = 0; nb < 2; ++nb) sc[nb][0] = sc[nb][1] = sc[nb][2] = sc[nb][3] = 0.f;
+                const bool tail = c0 + 16 > valid;
+                const uint32_t v_at = vs_u32 + (uint32_t)c0 * 128u + v_row;
+                float sc[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};   // two chains of products
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
                     uint32_t kf[4];
-                    const int row = c0 + (mi >> 1) * 8 + lr, ch = (2 * ks + (mi & 1)) & 7;
-                    pa_ldsm(ks_u32 + (ks >> 2) * kSub + row * 128 + ((ch ^ lr) << 4), kf);
-                    pa_mma<T>(sc[0], qa[ks], kf[0], kf[1]);
-                    pa_mma<T>(sc[1], qa[ks], kf[2], kf[3]);
+                    pa_ldsm(ks_u32 + (uint32_t)c0 * 128u + (ks >> 2) * kSub + k_row + ((((2 * ks + k_ch) & 7) ^ lr) << 4), kf);
+                    if (ks & 1) pa_mma<T>(s2, kf, qa[ks][0], qa[ks][1]);
+                    else pa_mma<T>(sc, kf, qa[ks][0], qa[ks][1]);
                 }
-                float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int nb = 0; nb < 2; ++nb) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int col = c0 + nb * 8 + 2 * t4 + (i & 1);
-                        sc[nb][i] = col < valid ? sc[nb][i] * a.scale_log2e : -INFINITY;
-                        mx[i >> 1] = fmaxf(mx[i >> 1], sc[nb][i]);
-                    }
+                for (int i = 0; i < 4; ++i) sc[i] += s2[i];
+                if (tail) {
+                    if (c0 + g >= valid) sc[0] = sc[1] = -INFINITY;
+                    if (c0 + g + 8 >= valid) sc[2] = sc[3] = -INFINITY;
                 }
-                // a new maximum anywhere in the warp: find it over the four lanes of a row, rescale what was summed
+                // a new maximum anywhere in the warp: find it over the rows of the block, rescale what was summed
+                float mx[2] = {fmaxf(sc[0], sc[2]), fmaxf(sc[1], sc[3])};
                 if (__any_sync(0xffffffffu, mx[0] > m_run[0] || mx[1] > m_run[1])) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-                        mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], x));
                         const float m_new = fmaxf(m_run[h], mx[h]);
-                        const float corr = m_new == -INFINITY ? 1.f : pa_exp2(m_run[h] - m_new);
+                        const float corr = m_new == -INFINITY ? 1.f : pa_exp2((m_run[h] - m_new) * a.scale_log2e);
                         m_run[h] = m_new;
                         l_run[h] *= corr;
 #pragma unroll
-                        for (int nb = 0; nb < 2 * KS; ++nb) { o[nb][2 * h] *= corr; o[nb][2 * h + 1] *= corr; }
+                        for (int dp = 0; dp < KS; ++dp) { o[dp][h] *= corr; o[dp][h + 2] *= corr; }
                     }
                 }
-                uint32_t pa[4];
+                uint32_t pb[2];
                 {
-                    float p[2][4];
+                    float p[4];
 #pragma unroll
-                    for (int nb = 0; nb < 2; ++nb) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float m = m_run[i >> 1];
-                            p[nb][i] = pa_exp2(sc[nb][i] - (m == -INFINITY ? 0.f : m) + kBias);
-                            l_run[i >> 1] += p[nb][i];              // the sum takes the weights before they are rounded
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        const float m = m_run[i & 1];
+                        p[i] = pa_exp2(fmaf(sc[i], a.scale_log2e, kBias - (m == -INFINITY ? 0.f : m) * a.scale_log2e));
+                        l_run[i & 1] += p[i];                       // the sum takes the weights before they are rounded
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pa[i] = pack2<T>(p[i >> 1][(i & 1) * 2], p[i >> 1][(i & 1) * 2 + 1]);
+                    pb[0] = pa_transpose(pack2<T>(p[0], p[1]));
+                    pb[1] = pa_transpose(pack2<T>(p[2], p[3]));
                 }
+                // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN of V
+                if (!tail) {
 #pragma unroll
-                for (int dp = 0; dp < KS; ++dp) {
-                    uint32_t vf[4];
-                    const int row = c0 + (mi & 1) * 8 + lr, ch = (2 * dp + (mi >> 1)) & 7;
-                    pa_ldsm_t(vs_u32 + (dp >> 2) * kSub + row * 128 + ((ch ^ lr) << 4), vf);
-                    pa_mma<T>(o[2 * dp], pa, vf[0], vf[1]);
-                    pa_mma<T>(o[2 * dp + 1], pa, vf[2], vf[3]);
+                    for (int dp = 0; dp < KS; ++dp) {
+                        uint32_t vf[4];
+                        pa_ldsm_t(v_at + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
+                        pa_mma<T>(o[dp], vf, pb[0], pb[1]);
+                    }
+                } else {
+                    const int left = valid - c0 - 2 * t4;           // of the cached rows 2 t4, + 1 and + 8, + 9
+                    const uint32_t lo = left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u, hi = left >= 10 ? 0xffffffffu : left == 9 ? 0xffffu : 0u;
+#pragma unroll
+                    for (int dp = 0; dp < KS; ++dp) {
+                        uint32_t vf[4];
+                        pa_ldsm_t(v_at + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
+                        vf[0] &= lo; vf[1] &= lo; vf[2] &= hi; vf[3] &= hi;
+                        pa_mma<T>(o[dp], vf, pb[0], pb[1]);
+                    }
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
-        // ---- the partial state ----
+        // ---- the partial state: a slot holds wk states of s.rows rows ----
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], 1);
-            l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], 2);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], x);
         }
-        // a slot holds wk states of s.rows rows
         const bool fits = s.slot < (s.prefix ? a.n_p_slots : a.n_o_slots);
         if (!fits && a.status && lane == 0) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
         if (fits) {
-            const size_t slot_rows = s.prefix ? 64 : (size_t)(kPaWarps / query_warps(a.per_kv)) * a.per_kv;
-            const size_t first = (size_t)s.slot * slot_rows + (size_t)kb * s.rows;
+            const size_t first = (size_t)s.slot * (s.prefix ? kPaQueries : own_slot_rows(a.per_kv)) + (size_t)kb * s.rows;
             float *st = s.prefix ? a.p_state : a.o_state, *ml = s.prefix ? a.p_ml : a.o_ml;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int r = qb * 16 + g + 8 * h;
+                const int r = qb * 8 + 2 * t4 + h;
                 if (r < s.rows) {
-                    if (t4 == 0) *reinterpret_cast<float2 *>(ml + 2 * (first + r)) = make_float2(m_run[h] - kBias, l_run[h]);
+                    if (g == 0) *reinterpret_cast<float2 *>(ml + 2 * (first + r)) = make_float2(m_run[h] * a.scale_log2e - kBias, l_run[h]);
 #pragma unroll
-                    for (int nb = 0; nb < 2 * KS; ++nb) {
-                        const int col = nb * 8 + 2 * t4;
-                        if (col < a.d) *reinterpret_cast<float2 *>(st + (first + r) * DP + col) = make_float2(o[nb][2 * h], o[nb][2 * h + 1]);
+                    for (int dp = 0; dp < KS; ++dp) {
+                        if (dp * 16 + g < a.d) st[(first + r) * DP + dp * 16 + g] = o[dp][h];
+                        if (dp * 16 + g + 8 < a.d) st[(first + r) * DP + dp * 16 + g + 8] = o[dp][h + 2];
                     }
                 }
             }
@@ -418,9 +473,10 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     const int b = blockIdx.x / heads, qh = blockIdx.x - b * heads, head = qh / a.per_kv, j = qh - head * a.per_kv;
     pdl_wait();
     pdl_launch();
-    const uint32_t total = a.plan[a.groups + a.batch], blocks = working_blocks(a, total);
-    // the block that holds unit u: the last c with floor(c total / blocks) <= u
-    const auto block_of = [&](uint32_t u) { return (int)((((unsigned long long)u + 1) * blocks - 1) / total); };
+    const uint32_t total = a.plan[a.groups + a.batch], runs = working_runs(a, total);
+    if (blockIdx.x == 0 && threadIdx.x == 0) { a.counter->next = 0; a.counter->mark = kRunMark; }
+    // the run that holds unit u: the last c with floor(c total / runs) <= u
+    const auto run_of = [&](uint32_t u) { return (int)min((((unsigned long long)u + 1) * runs - 1) / total, (unsigned long long)runs - 1); };
 
     // the group of the batch row: the last one that begins at or before it
     int grp = -1;
@@ -436,30 +492,33 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     // runs of states: prefix, then own rows
     size_t p_first = 0, o_first;
     int p_segs = 0, p_step = 0, p_subs = 0, o_segs = 0;
-    const int o_subs = kPaWarps / query_warps(a.per_kv), o_step = o_subs * a.per_kv;
+    const int own_mt = query_items(a.per_kv), own_q = j / kPaQueries, own_rows = min(a.per_kv - own_q * kPaQueries, kPaQueries);
+    const int o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
     if (grp >= 0) {
-        const int b0 = group_begin(a, grp), m = group_members(a, grp) * a.per_kv, mt = (m + 63) / 64;
-        const int packed = (b - b0) * a.per_kv + j, q = packed / 64, rows = min(m - q * 64, 64);
+        const int b0 = group_begin(a, grp), m = group_members(a, grp) * a.per_kv, mt = query_items(m);
+        const int packed = (b - b0) * a.per_kv + j, q = packed / kPaQueries, rows = min(m - q * kPaQueries, kPaQueries);
         const int n = clamp_rows(a.p_rows[grp], a.max_p_pages, a.page_rows), tiles = (n + kPaTile - 1) / kPaTile;
-        if (tiles > 0) {
+        if (tiles > 0 && runs > 0) {
             const int item = head * mt + q;
             const uint32_t u = a.plan[grp] + (uint32_t)item * (uint32_t)tiles;
-            const int c0 = block_of(u), c1 = block_of(u + tiles - 1);
-            const long long slot = ((long long)b0 * a.per_kv / 64 + grp) * a.kv_heads + item + c0;
+            const int c0 = run_of(u), c1 = run_of(u + tiles - 1);
+            const long long slot = (long long)first_p_item(a, grp, b0) + item + c0;
             p_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_p_slots - slot));
             p_subs = kPaWarps / query_warps(rows);
             p_step = rows;
-            p_first = (size_t)slot * 64 + (packed - q * 64);
+            p_first = (size_t)slot * kPaQueries + (packed - q * kPaQueries);
         }
     }
     {
         const int n = clamp_rows(a.n_rows[b], a.max_pages, a.page_rows), tiles = (n + kPaTile - 1) / kPaTile;
         o_first = 0;
-        if (tiles > 0) {
-            const uint32_t u = a.plan[a.groups + b] + (uint32_t)head * (uint32_t)tiles;
-            const int c0 = block_of(u), c1 = block_of(u + tiles - 1);
-            o_segs = c1 - c0 + 1;
-            o_first = (size_t)(b * a.kv_heads + head + c0) * o_step + j;
+        if (tiles > 0 && runs > 0) {
+            const int item = head * own_mt + own_q;
+            const uint32_t u = a.plan[a.groups + b] + (uint32_t)item * (uint32_t)tiles;
+            const int c0 = run_of(u), c1 = run_of(u + tiles - 1);
+            const long long slot = (long long)b * a.kv_heads * own_mt + item + c0;
+            o_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_o_slots - slot));
+            o_first = (size_t)slot * o_step + (j - own_q * kPaQueries);
         }
     }
     const int n_p = p_segs * p_subs, n_states = n_p + o_segs * o_subs;
@@ -470,11 +529,11 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
         const float *st, *ml;
         if (i < n_p) {
             const int seg = i / p_subs, sub = i - seg * p_subs;
-            const size_t row = p_first + (size_t)seg * 64 + (size_t)sub * p_step;
+            const size_t row = p_first + (size_t)seg * kPaQueries + (size_t)sub * p_step;
             st = a.p_state + row * DP; ml = a.p_ml + 2 * row;
         } else {
             const int k = i - n_p, seg = k / o_subs, sub = k - seg * o_subs;
-            const size_t row = o_first + (size_t)seg * o_step + (size_t)sub * a.per_kv;
+            const size_t row = o_first + (size_t)seg * o_step + (size_t)sub * own_rows;
             st = a.o_state + row * DP; ml = a.o_ml + 2 * row;
         }
         const float2 s = *reinterpret_cast<const float2 *>(ml);
@@ -520,7 +579,7 @@ namespace {
 struct PrefixLayout {
     size_t plan, p_state, p_ml, o_state, o_ml, bytes;
     long long p_slots, o_slots;
-    int nsub, blocks;
+    int nsub, blocks, max_runs;              // blocks that fit the GPU; runs of the largest call
 };
 
 int sm_count()
@@ -541,13 +600,14 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     const int per_kv = n_heads / kv_heads;
     o->nsub = (head_dim + 63) / 64;
     o->blocks = sm_count() * (o->nsub <= 2 ? 2 : 1);
+    o->max_runs = 4 * o->blocks;
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-    o->p_slots = groups ? ((long long)batch * per_kv / 64 + groups) * kv_heads + o->blocks : 0;
-    o->o_slots = (long long)batch * kv_heads + o->blocks;
-    const size_t dp = 64 * o->nsub, p_rows = (size_t)o->p_slots * 64, o_rows = (size_t)o->o_slots * (kPaWarps / query_warps(per_kv)) * per_kv;
+    o->p_slots = groups ? ((long long)batch * per_kv / kPaQueries + groups) * kv_heads + o->max_runs : 0;
+    o->o_slots = (long long)batch * kv_heads * query_items(per_kv) + o->max_runs;
+    const size_t dp = 64 * o->nsub, p_rows = (size_t)o->p_slots * kPaQueries, o_rows = (size_t)o->o_slots * own_slot_rows(per_kv);
     if (o->p_slots > 0x7fffffffLL || o->o_slots > 0x7fffffffLL || (long long)batch * n_heads > 0x7fffffffLL) return false;
-    o->plan = 0;
-    o->p_state = up((size_t)(batch + groups + 1) * 4);
+    o->plan = 256;                           // behind the run counter
+    o->p_state = o->plan + up((size_t)(batch + groups + 1) * 4);
     o->p_ml = o->p_state + up(p_rows * dp * 4);
     o->o_state = o->p_ml + up(p_rows * 8);
     o->o_ml = o->o_state + up(o_rows * dp * 4);
@@ -587,26 +647,26 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
 }
 
 template <typename T, int NSUB, int STAGES>
-cudaError_t launch_prefix(const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
+cudaError_t launch_prefix(const PrefixArgs &a, int blocks, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
 {
     const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * kPaTile * 128 + (size_t)(a.batch + a.groups + 1) * 4;
     const auto kern = prefix_sweep_kernel<T, NSUB, STAGES>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(kern, dim3((unsigned)a.blocks), kPaThreads, smem, st, a, km, vm);
+    e = launch_pdl(kern, dim3((unsigned)blocks), kPaThreads, smem, st, a, km, vm);
     if (e != cudaSuccess) return e;
     return launch_pdl(prefix_merge_kernel<T, NSUB>, dim3((unsigned)(a.batch * a.kv_heads * a.per_kv)), kPaMergeThreads, 0, st, a, (T *)out, out_f32, lse);
 }
 
 template <typename T>
-cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
+cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, int blocks, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
                                float *lse, cudaStream_t st)
 {
     switch (nsub) {                          // 96 KB of tiles in flight per block, two blocks per SM; wide rows: one block
-    case 1: return launch_prefix<T, 1, 6>(a, km, vm, out, out_f32, lse, st);
-    case 2: return launch_prefix<T, 2, 3>(a, km, vm, out, out_f32, lse, st);
-    case 3: return launch_prefix<T, 3, 4>(a, km, vm, out, out_f32, lse, st);
-    default: return launch_prefix<T, 4, 3>(a, km, vm, out, out_f32, lse, st);
+    case 1: return launch_prefix<T, 1, 6>(a, blocks, km, vm, out, out_f32, lse, st);
+    case 2: return launch_prefix<T, 2, 3>(a, blocks, km, vm, out, out_f32, lse, st);
+    case 3: return launch_prefix<T, 3, 4>(a, blocks, km, vm, out, out_f32, lse, st);
+    default: return launch_prefix<T, 4, 3>(a, blocks, km, vm, out, out_f32, lse, st);
     }
 }
 
@@ -642,8 +702,8 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
         return ADSA_EINVAL;
     if ((long long)max_pages * kv->page_rows > 0x7fffffc0LL || (long long)max_prefix_pages * kv->page_rows > 0x7fffffc0LL) return ADSA_EINVAL;
     // the units of a call are counted in 32 bits
-    const double own_units = (double)batch * kv->n_kv_heads * ((double)max_pages * kv->page_rows / kPaTile + 1);
-    const double p_units = ((double)batch * (n_heads / kv->n_kv_heads) / 64 + n_groups) * kv->n_kv_heads *
+    const double own_units = (double)batch * kv->n_kv_heads * 2 * ((double)max_pages * kv->page_rows / kPaTile + 1);
+    const double p_units = ((double)batch * (n_heads / kv->n_kv_heads) / kPaQueries + n_groups) * kv->n_kv_heads *
                            ((double)max_prefix_pages * kv->page_rows / kPaTile + 1);
     if (own_units + (n_groups ? p_units : 0) > 4e9) return ADSA_EINVAL;
     if (workspace_bytes < l.bytes) return ADSA_ENOMEM;
@@ -664,10 +724,14 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.plan = (uint32_t *)(ws + l.plan);
     a.p_state = (float *)(ws + l.p_state); a.p_ml = (float *)(ws + l.p_ml);
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
-    a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots; a.blocks = l.blocks;
+    a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots; 
+    // runs of eight tiles or more where the tables are full, at least one per block
+    const double runs = (own_units + (n_groups ? p_units : 0)) / 8;
+    a.counter = (RunCounter *)ws;
+    a.runs = runs <= l.blocks ? l.blocks : runs >= l.max_runs ? l.max_runs : (int)runs;
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, km, vm, out, out_f32, lse, st)
-                                                  : launch_prefix_type<__half>(l.nsub, a, km, vm, out, out_f32, lse, st);
+    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, l.blocks, km, vm, out, out_f32, lse, st)
+                                                  : launch_prefix_type<__half>(l.nsub, a, l.blocks, km, vm, out, out_f32, lse, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 

@@ -453,7 +453,7 @@ def test_shared_prefix_attn_replays_with_new_lengths_and_groups():
         gr = torch.cuda.CUDAGraph()
         with torch.cuda.graph(gr):
             A.shared_prefix_attn(**a, out=o, workspace=ws)
-        graphs.append((gr, o, torch.cuda.Stream()))
+        graphs.append((gr, o, torch.cuda.Stream(), ws))                           # a graph's workspace lives as long as the graph
     for own, prefix, start in (([100, 37, 64, 1], [90, 200], [0, 2, 4]), ([1, 0, 64, 1], [5, 64], [0, 1, 1]), ([99, 37, 0, 0], [0, 199], [0, 3, 4])):
         a["n_rows"].copy_(torch.tensor(own, dtype=torch.int32))
         a["prefix_rows"].copy_(torch.tensor(prefix, dtype=torch.int32))
@@ -461,12 +461,12 @@ def test_shared_prefix_attn_replays_with_new_lengths_and_groups():
         a["q"].normal_()
         want = A.shared_prefix_attn(**a)
         torch.cuda.synchronize()
-        for gr, o, st in graphs:
+        for gr, o, st, _ in graphs:
             with torch.cuda.stream(st):
                 for _ in range(3):
                     gr.replay()
         torch.cuda.synchronize()
-        for gr, o, st in graphs:
+        for gr, o, st, _ in graphs:
             assert torch.equal(o, want)
 
 
