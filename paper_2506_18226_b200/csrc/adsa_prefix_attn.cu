@@ -11,10 +11,10 @@
 // they belong to, so long and short rows, prefixes and single rows mix without the host knowing a length.  Where a run
 // changes from one item to the next it leaves the item's partial state in the workspace; a second small kernel merges
 // the states of each output row.  Lengths, tables and group boundaries are read on the device: a captured graph follows
-// them.  The grid is what fits the GPU; there are up to four times as many runs as blocks.  A block begins with the run
-// of its own index and then claims runs from a counter.  SMs differ in the bandwidth they get and items in their cost per tile: with
-// one run per block the slowest block took 279 us where the median took 225 (64 rows of 2304 x 32 heads x 100 elements).
-// What a run leaves does not depend on who ran it.
+// them.  A run is a block of the grid, and a grid has up to four times as many blocks as fit the GPU; a resident block that
+// has finished its run takes over one that has not started (cluster launch control), without refilling its pipeline.  SMs
+// differ in the bandwidth they get and items in their cost per tile: with one run per block the slowest block took 279 us
+// where the median took 225 (64 rows of 2304 x 32 heads x 100 elements).
 //
 // What a warp does per 16 cached rows: S^T = K Q^T and O^T += V^T P^T on mma.sync tiles with the cached rows as M and
 // eight query rows as N (the fewest that the instruction takes).  Up to 8 query rows of a key head: the four warps of a
@@ -38,14 +38,6 @@ constexpr int kPaThreads = (kPaWarps + 1) * 32;
 constexpr int kPaMaxEntries = 8192;         // groups + batch rows of a call
 constexpr int kPaMergeThreads = 128;
 
-// Hands out runs.  The merge of every call leaves it at zero behind the mark; where the mark is missing (a workspace's
-// first call) blocks take the runs in fixed turns instead, so a workspace needs no initialisation.
-struct RunCounter {
-    unsigned long long mark;
-    uint32_t next, spare;
-};
-constexpr unsigned long long kRunMark = 0xad5a5eedc0117e2bull;
-
 struct PrefixArgs {
     const void *q;
     long long q_row, q_head;                // element strides of q
@@ -60,8 +52,7 @@ struct PrefixArgs {
     uint32_t *plan;                         // [entries + 1] first unit of every entry (groups, then batch rows)
     float *p_state, *p_ml, *o_state, *o_ml; // prefix slots, own-row slots: rows of d_pad floats, (m, l) pairs
     int n_p_slots, n_o_slots;
-    RunCounter *counter;
-    int runs;
+    int runs;                               // blocks of the sweep kernel's grid
 };
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
@@ -206,6 +197,22 @@ __device__ __forceinline__ uint32_t pa_transpose(uint32_t x)
     return y;
 }
 
+// A block that has not started: asked for with pa_ask_block, its index (or -1: every block has started) read from the
+// 16-byte answer once the barrier has counted it.
+__device__ __forceinline__ void pa_ask_block(uint32_t answer, uint32_t bar)
+{
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
+}
+__device__ __forceinline__ int pa_answer(uint32_t answer)
+{
+    uint32_t ok, x;
+    asm volatile("{\n\t.reg .b128 r;\n\t.reg .pred p;\n\tld.shared.b128 r, [%2];\n\t"
+                 "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\tselp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+                 "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+                 : "=r"(ok), "=r"(x) : "r"(answer) : "memory");
+    return ok ? (int)x : -1;
+}
+
 // NSUB: 64-element sub-tiles of a row (head elements / 64, rounded up).  STAGES: tiles in flight per block.
 template <typename T, int NSUB, int STAGES>
 __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
@@ -217,11 +224,11 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     constexpr float kBias = WeightBias<T>::value;
     extern __shared__ unsigned char pa_smem[];
     __shared__ uint64_t bars[2 * STAGES + 4];
-    __shared__ volatile int answers[2];
+    __shared__ __align__(16) uint4 answers[2];
     __shared__ uint32_t warp_sums[kPaThreads / 32];
     const uint32_t ring = (smem_u32(pa_smem) + 1023u) & ~1023u;
     uint32_t *plan = reinterpret_cast<uint32_t *>(pa_smem + (ring - smem_u32(pa_smem)) + (size_t)STAGES * 2 * kHalf);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, asked = empty + 8 * STAGES, heard = asked + 16;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, asked = empty + 8 * STAGES, heard = asked + 16, answer = smem_u32(answers);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int entries = a.groups + a.batch;
 
@@ -252,32 +259,36 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     Walk walk;
     walk.begin(a, plan, blockIdx.x);
     Segment s;
-    // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp claims the next run
-    // when it begins one, into the answer slot that all warps have read the last time.
-    const bool counted = a.counter->mark == kRunMark;              // (nobody writes the mark during a sweep)
-    const int runs = (int)working_runs(a, plan[entries]);
+    // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp asks for the next
+    // run when it begins one, into the answer slot that all warps have read the last time, and leaves the plan for the
+    // merge if it has run 0 (block 0 may itself be taken over before it starts, where another grid holds the SMs).
     int limit = kCopySpinLimit;
     uint32_t turns = 0;                                            // runs finished by this warp
-    const auto claim = [&]() {
-        const uint32_t i = turns & 1u;
-        if (!mbar_wait_bounded(heard + 8 * i, ((turns >> 1) & 1u) ^ 1u, limit)) limit = kCopySpinAfterTimeout;
-        answers[i] = counted ? (int)(gridDim.x + atomicAdd(&a.counter->next, 1u)) : (int)(blockIdx.x + (turns + 1u) * gridDim.x);
-        mbar_arrive(asked + 8 * i);
+    const auto begin_run = [&](int run) {
+        if (lane == 0) {
+            const uint32_t i = turns & 1u;
+            if (!mbar_wait_bounded(heard + 8 * i, ((turns >> 1) & 1u) ^ 1u, limit)) limit = kCopySpinAfterTimeout;
+            mbar_expect_tx(asked + 8 * i, 16);
+            pa_ask_block(answer + 16 * i, asked + 8 * i);
+        }
+        if (run == 0)
+            for (int e = lane; e <= entries; e += 32) a.plan[e] = plan[e];
     };
     const auto advance = [&](Segment &n) {
         while (!walk.next(a, n)) {
             const uint32_t i = turns & 1u;
-            int run = runs;
-            if (mbar_wait_bounded(asked + 8 * i, (turns >> 1) & 1u, limit)) run = answers[i];
+            int run = -1;
+            if (mbar_wait_bounded(asked + 8 * i, (turns >> 1) & 1u, limit)) run = pa_answer(answer + 16 * i);
             else {
                 limit = kCopySpinAfterTimeout;
                 if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the answer is read before the slot is asked into again
             __syncwarp();
             if (lane == 0) mbar_arrive(heard + 8 * i);
             ++turns;
-            if (run >= runs) return false;
-            if (warp == kPaWarps && lane == 0) claim();
+            if (run < 0) return false;
+            if (warp == kPaWarps) begin_run(run);
             walk.begin(a, plan, run);
         }
         return true;
@@ -286,9 +297,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     if (warp == kPaWarps) {                                        // ---- the copying warp ----
         int stage = 0;
         uint32_t phase = 0;
-        if (lane == 0) claim();
-        if (blockIdx.x == 0)                                       // for the merge
-            for (int e = lane; e <= entries; e += 32) a.plan[e] = plan[e];
+        begin_run(blockIdx.x);
         while (advance(s)) {
             for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
                 if (!mbar_wait_bounded(empty + 8 * stage, phase ^ 1u, limit)) {
@@ -474,7 +483,6 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     pdl_wait();
     pdl_launch();
     const uint32_t total = a.plan[a.groups + a.batch], runs = working_runs(a, total);
-    if (blockIdx.x == 0 && threadIdx.x == 0) { a.counter->next = 0; a.counter->mark = kRunMark; }
     // the run that holds unit u: the last c with floor(c total / runs) <= u
     const auto run_of = [&](uint32_t u) { return (int)min((((unsigned long long)u + 1) * runs - 1) / total, (unsigned long long)runs - 1); };
 
@@ -606,7 +614,7 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     o->o_slots = (long long)batch * kv_heads * query_items(per_kv) + o->max_runs;
     const size_t dp = 64 * o->nsub, p_rows = (size_t)o->p_slots * kPaQueries, o_rows = (size_t)o->o_slots * own_slot_rows(per_kv);
     if (o->p_slots > 0x7fffffffLL || o->o_slots > 0x7fffffffLL || (long long)batch * n_heads > 0x7fffffffLL) return false;
-    o->plan = 256;                           // behind the run counter
+    o->plan = 0;
     o->p_state = o->plan + up((size_t)(batch + groups + 1) * 4);
     o->p_ml = o->p_state + up(p_rows * dp * 4);
     o->o_state = o->p_ml + up(p_rows * 8);
@@ -647,26 +655,26 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
 }
 
 template <typename T, int NSUB, int STAGES>
-cudaError_t launch_prefix(const PrefixArgs &a, int blocks, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
+cudaError_t launch_prefix(const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
 {
     const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * kPaTile * 128 + (size_t)(a.batch + a.groups + 1) * 4;
     const auto kern = prefix_sweep_kernel<T, NSUB, STAGES>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(kern, dim3((unsigned)blocks), kPaThreads, smem, st, a, km, vm);
+    e = launch_pdl(kern, dim3((unsigned)a.runs), kPaThreads, smem, st, a, km, vm);
     if (e != cudaSuccess) return e;
     return launch_pdl(prefix_merge_kernel<T, NSUB>, dim3((unsigned)(a.batch * a.kv_heads * a.per_kv)), kPaMergeThreads, 0, st, a, (T *)out, out_f32, lse);
 }
 
 template <typename T>
-cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, int blocks, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
+cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
                                float *lse, cudaStream_t st)
 {
     switch (nsub) {                          // 96 KB of tiles in flight per block, two blocks per SM; wide rows: one block
-    case 1: return launch_prefix<T, 1, 6>(a, blocks, km, vm, out, out_f32, lse, st);
-    case 2: return launch_prefix<T, 2, 3>(a, blocks, km, vm, out, out_f32, lse, st);
-    case 3: return launch_prefix<T, 3, 4>(a, blocks, km, vm, out, out_f32, lse, st);
-    default: return launch_prefix<T, 4, 3>(a, blocks, km, vm, out, out_f32, lse, st);
+    case 1: return launch_prefix<T, 1, 6>(a, km, vm, out, out_f32, lse, st);
+    case 2: return launch_prefix<T, 2, 3>(a, km, vm, out, out_f32, lse, st);
+    case 3: return launch_prefix<T, 3, 4>(a, km, vm, out, out_f32, lse, st);
+    default: return launch_prefix<T, 4, 3>(a, km, vm, out, out_f32, lse, st);
     }
 }
 
@@ -727,11 +735,10 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots; 
     // runs of eight tiles or more where the tables are full, at least one per block
     const double runs = (own_units + (n_groups ? p_units : 0)) / 8;
-    a.counter = (RunCounter *)ws;
     a.runs = runs <= l.blocks ? l.blocks : runs >= l.max_runs ? l.max_runs : (int)runs;
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, l.blocks, km, vm, out, out_f32, lse, st)
-                                                  : launch_prefix_type<__half>(l.nsub, a, l.blocks, km, vm, out, out_f32, lse, st);
+    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, km, vm, out, out_f32, lse, st)
+                                                  : launch_prefix_type<__half>(l.nsub, a, km, vm, out, out_f32, lse, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 
