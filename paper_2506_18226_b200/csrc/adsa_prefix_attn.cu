@@ -21,13 +21,10 @@
 // block split the cached rows of a tile; up to 16: two and two; up to 32: each warp has its own eight query rows.  One query
 // row per cached row is 1 flop per byte: HBM bounds it, and the products run on the tensor cores only because that takes
 // the fewest instructions per byte.
-#include <cuda.h>
-#include <float.h>
 #include <math.h>
 #include <type_traits>
 
-#include "adsa_async.cuh"
-#include "adsa_half.cuh"
+#include "adsa_prefix.cuh"
 
 namespace adsa {
 
@@ -37,23 +34,8 @@ constexpr int kPaWarps = 4;                 // warps that compute; one more warp
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
 constexpr int kPaMaxEntries = 8192;         // groups + batch rows of a call
 constexpr int kPaMergeThreads = 128;
+constexpr int kWideAbove = 32;               // query rows of a key head from which a group's prefix goes to the wide kernel
 
-struct PrefixArgs {
-    const void *q;
-    long long q_row, q_head;                // element strides of q
-    const int32_t *table, *n_rows;          // [batch][max_pages], [batch]
-    const int32_t *p_table, *p_rows, *start;   // [groups][max_p_pages], [groups], [groups + 1]
-    uint32_t *status;
-    int batch, groups, kv_heads, per_kv;    // per_kv: query heads of a key head
-    int max_pages, max_p_pages, page_rows, n_pages, box_rows;
-    int d;
-    float scale_log2e;
-    // workspace
-    uint32_t *plan;                         // [entries + 1] first unit of every entry (groups, then batch rows)
-    float *p_state, *p_ml, *o_state, *o_ml; // prefix slots, own-row slots: rows of d_pad floats, (m, l) pairs
-    int n_p_slots, n_o_slots;
-    int runs;                               // blocks of the sweep kernel's grid
-};
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
 __host__ __device__ __forceinline__ int query_warps(int m) { return m <= 8 ? 1 : m <= 16 ? 2 : 4; }
@@ -64,30 +46,17 @@ __host__ __device__ __forceinline__ int own_slot_rows(int per_kv)
     return per_kv >= kPaQueries ? kPaQueries : kPaWarps / query_warps(per_kv) * per_kv;
 }
 
-__device__ __forceinline__ int clamp_rows(int n, int max_pages, int page_rows)
-{
-    const long long most = (long long)max_pages * page_rows;
-    return n < 0 ? 0 : n > most ? (int)most : n;
-}
-__device__ __forceinline__ int group_begin(const PrefixArgs &a, int g) { return min(max(a.start[g], 0), a.batch); }
-__device__ __forceinline__ int group_members(const PrefixArgs &a, int g) { return max(group_begin(a, g + 1) - group_begin(a, g), 0); }
-
 // units of an entry: groups first, then batch rows
 __device__ __forceinline__ uint32_t entry_units(const PrefixArgs &a, int e)
 {
     if (e < a.groups) {
         const int m = group_members(a, e) * a.per_kv;
+        if (m > a.wide_above) return 0;
         const int n = clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows);
         return (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
     }
     const int n = clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
     return (uint32_t)query_items(a.per_kv) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
-}
-
-// A number no larger item of an earlier group reaches: sum of query_items over groups 0 .. g-1 <= begin per_kv / 32 + g
-__device__ __forceinline__ int first_p_item(const PrefixArgs &a, int g, int begin)
-{
-    return (int)(((long long)begin * a.per_kv / kPaQueries + g) * a.kv_heads);
 }
 
 // Every one of these runs has a unit, so every state between an item's first and last run exists.
@@ -142,7 +111,7 @@ struct Walk {
         s.row0 = b0 * a.per_kv + q * kPaQueries;
         s.rows = min(m - q * kPaQueries, kPaQueries);
         s.pages = pre ? a.p_table + (size_t)e * a.max_p_pages : a.table + (size_t)b0 * a.max_pages;
-        s.slot = (pre ? first_p_item(a, e, b0) : b0 * a.kv_heads * mt) + item + run;
+        s.slot = (pre ? first_group_item(a, e, b0, kPaQueries) : b0 * a.kv_heads * mt) + item + run;
         s.prefix = pre;
         s.tile0 = (int)(at - (uint32_t)item * tiles);
         s.tiles = (int)min(tiles - (uint32_t)s.tile0, end - u);
@@ -171,24 +140,6 @@ __device__ __forceinline__ void pa_mma(float (&d)[4], const uint32_t (&a)[4], ui
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void pa_tma(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-__device__ __forceinline__ float pa_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// P is rounded to 16 bits for the second product.  It lies in 0 .. 1 relative to the running maximum; 16-bit floats of
-// the half type lose precision below 2^-14, so there P is scaled by 2^8 (it cancels in o / l; the states carry it in m).
-template <typename T> struct WeightBias { static constexpr float value = 0.f; };
-template <> struct WeightBias<__half> { static constexpr float value = 8.f; };
-
 // the transpose of an 8 x 8 matrix of 16-bit elements held by a warp (row lane / 4, columns 2 (lane % 4), + 1)
 __device__ __forceinline__ uint32_t pa_transpose(uint32_t x)
 {
@@ -239,7 +190,10 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
     }
-    pdl_wait();
+    // Behind the wide kernel of the same call (which has waited for what was ahead of it before this one could begin) there
+    // is nothing to wait for here; each block waits before it ends, so that the merge finds both kernels' states.
+    const bool behind_wide = a.w_runs > 0;
+    if (!behind_wide) pdl_wait();
     pdl_launch();
 
     // ---- first unit of every entry: each thread sums a run of entries, the runs are scanned over the block ----
@@ -326,6 +280,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
         }
+        if (behind_wide) pdl_wait();
         return;
     }
 
@@ -483,8 +438,8 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     pdl_wait();
     pdl_launch();
     const uint32_t total = a.plan[a.groups + a.batch], runs = working_runs(a, total);
-    // the run that holds unit u: the last c with floor(c total / runs) <= u
-    const auto run_of = [&](uint32_t u) { return (int)min((((unsigned long long)u + 1) * runs - 1) / total, (unsigned long long)runs - 1); };
+    // the run that holds unit u: the last c with floor(c n / runs) <= u
+    const auto run_of = [](uint32_t u, uint32_t n, uint32_t c) { return (int)min((((unsigned long long)u + 1) * c - 1) / n, (unsigned long long)c - 1); };
 
     // the group of the batch row: the last one that begins at or before it
     int grp = -1;
@@ -498,23 +453,30 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
         if (lo >= 0 && b < group_begin(a, lo + 1)) grp = lo;
     }
     // runs of states: prefix, then own rows
-    size_t p_first = 0, o_first;
-    int p_segs = 0, p_step = 0, p_subs = 0, o_segs = 0;
+    const float *p_state = a.p_state, *p_ml = a.p_ml;
+    size_t p_first = 0, o_first, p_slot = kPaQueries;
+    int p_segs = 0, p_step = 0, p_subs = 1, o_segs = 0;
     const int own_mt = query_items(a.per_kv), own_q = j / kPaQueries, own_rows = min(a.per_kv - own_q * kPaQueries, kPaQueries);
     const int o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
     if (grp >= 0) {
-        const int b0 = group_begin(a, grp), m = group_members(a, grp) * a.per_kv, mt = query_items(m);
-        const int packed = (b - b0) * a.per_kv + j, q = packed / kPaQueries, rows = min(m - q * kPaQueries, kPaQueries);
-        const int n = clamp_rows(a.p_rows[grp], a.max_p_pages, a.page_rows), tiles = (n + kPaTile - 1) / kPaTile;
-        if (tiles > 0 && runs > 0) {
+        const int b0 = group_begin(a, grp), m = group_members(a, grp) * a.per_kv;
+        const bool wide = m > a.wide_above;
+        const int queries = wide ? kWideQueries : kPaQueries, tile = wide ? kWideTile : kPaTile, mt = (m + queries - 1) / queries;
+        const int packed = (b - b0) * a.per_kv + j, q = packed / queries, rows = min(m - q * queries, queries);
+        const int n = clamp_rows(a.p_rows[grp], a.max_p_pages, a.page_rows), tiles = (n + tile - 1) / tile;
+        const uint32_t *plan = wide ? a.w_plan : a.plan;
+        const uint32_t p_total = wide ? plan[a.groups] : total, p_runs = wide ? min((uint32_t)a.w_runs, p_total) : runs;
+        if (tiles > 0 && p_runs > 0) {
             const int item = head * mt + q;
-            const uint32_t u = a.plan[grp] + (uint32_t)item * (uint32_t)tiles;
-            const int c0 = run_of(u), c1 = run_of(u + tiles - 1);
-            const long long slot = (long long)first_p_item(a, grp, b0) + item + c0;
-            p_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_p_slots - slot));
-            p_subs = kPaWarps / query_warps(rows);
+            const uint32_t u = plan[grp] + (uint32_t)item * (uint32_t)tiles;
+            const int c0 = run_of(u, p_total, p_runs), c1 = run_of(u + tiles - 1, p_total, p_runs);
+            const long long slot = (long long)first_group_item(a, grp, b0, queries) + item + c0;
+            p_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, (wide ? a.n_w_slots : a.n_p_slots) - slot));
+            p_subs = wide ? 1 : kPaWarps / query_warps(rows);
             p_step = rows;
-            p_first = (size_t)slot * kPaQueries + (packed - q * kPaQueries);
+            p_slot = queries;
+            p_first = (size_t)slot * p_slot + (packed - q * queries);
+            if (wide) { p_state = a.w_state; p_ml = a.w_ml; }
         }
     }
     {
@@ -523,7 +485,7 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
         if (tiles > 0 && runs > 0) {
             const int item = head * own_mt + own_q;
             const uint32_t u = a.plan[a.groups + b] + (uint32_t)item * (uint32_t)tiles;
-            const int c0 = run_of(u), c1 = run_of(u + tiles - 1);
+            const int c0 = run_of(u, total, runs), c1 = run_of(u + tiles - 1, total, runs);
             const long long slot = (long long)b * a.kv_heads * own_mt + item + c0;
             o_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_o_slots - slot));
             o_first = (size_t)slot * o_step + (j - own_q * kPaQueries);
@@ -537,8 +499,8 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
         const float *st, *ml;
         if (i < n_p) {
             const int seg = i / p_subs, sub = i - seg * p_subs;
-            const size_t row = p_first + (size_t)seg * kPaQueries + (size_t)sub * p_step;
-            st = a.p_state + row * DP; ml = a.p_ml + 2 * row;
+            const size_t row = p_first + (size_t)seg * p_slot + (size_t)sub * p_step;
+            st = p_state + row * DP; ml = p_ml + 2 * row;
         } else {
             const int k = i - n_p, seg = k / o_subs, sub = k - seg * o_subs;
             const size_t row = o_first + (size_t)seg * o_step + (size_t)sub * own_rows;
@@ -585,8 +547,9 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
 namespace {
 
 struct PrefixLayout {
-    size_t plan, p_state, p_ml, o_state, o_ml, bytes;
-    long long p_slots, o_slots;
+    size_t plan, p_state, p_ml, o_state, o_ml, w_plan, w_state, w_ml, bytes;
+    long long p_slots, o_slots, w_slots;
+    int wide_blocks;                         // of the wide kernel; 0: no group can be large enough for it
     int nsub, blocks, max_runs;              // blocks that fit the GPU; runs of the largest call
 };
 
@@ -609,6 +572,8 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     o->nsub = (head_dim + 63) / 64;
     o->blocks = sm_count() * (o->nsub <= 2 ? 2 : 1);
     o->max_runs = 4 * o->blocks;
+    o->wide_blocks = groups && o->nsub <= 2 && (long long)batch * per_kv > kWideAbove ? 2 * sm_count() : 0;
+    o->w_slots = o->wide_blocks ? ((long long)batch * per_kv / kWideQueries + groups) * kv_heads + o->wide_blocks : 0;
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     o->p_slots = groups ? ((long long)batch * per_kv / kPaQueries + groups) * kv_heads + o->max_runs : 0;
     o->o_slots = (long long)batch * kv_heads * query_items(per_kv) + o->max_runs;
@@ -619,7 +584,10 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     o->p_ml = o->p_state + up(p_rows * dp * 4);
     o->o_state = o->p_ml + up(p_rows * 8);
     o->o_ml = o->o_state + up(o_rows * dp * 4);
-    o->bytes = o->o_ml + up(o_rows * 8);
+    o->w_plan = o->o_ml + up(o_rows * 8);
+    o->w_state = o->w_plan + up((size_t)(groups + 1) * 4);
+    o->w_ml = o->w_state + up((size_t)o->w_slots * kWideQueries * dp * 4);
+    o->bytes = o->w_ml + up((size_t)o->w_slots * kWideQueries * 8);
     return true;
 }
 
@@ -732,11 +700,16 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.plan = (uint32_t *)(ws + l.plan);
     a.p_state = (float *)(ws + l.p_state); a.p_ml = (float *)(ws + l.p_ml);
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
-    a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots; 
+    a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
+    a.wide_above = l.wide_blocks ? kWideAbove : 0x7fffffff;
+    a.w_plan = (uint32_t *)(ws + l.w_plan); a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
+    a.n_w_slots = (int)l.w_slots; a.w_runs = l.wide_blocks;
+
     // runs of eight tiles or more where the tables are full, at least one per block
     const double runs = (own_units + (n_groups ? p_units : 0)) / 8;
     a.runs = runs <= l.blocks ? l.blocks : runs >= l.max_runs ? l.max_runs : (int)runs;
     cudaStream_t st = (cudaStream_t)stream;
+    if (a.w_runs && launch_prefix_wide(kv->dtype, l.nsub, a, km, vm, st) != cudaSuccess) return ADSA_ECUDA;
     const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, km, vm, out, out_f32, lse, st)
                                                   : launch_prefix_type<__half>(l.nsub, a, km, vm, out, out_f32, lse, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;

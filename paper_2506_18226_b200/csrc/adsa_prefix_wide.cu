@@ -1,0 +1,447 @@
+// The prefix of a large group: many query rows per key head against one long run of cached rows, which is a real matrix
+// product, on the fifth-generation tensor cores.
+//
+// A block takes 128 query rows of one key head and a run of 128-row tiles of the prefix.  Per tile: S = Q K^T (tcgen05,
+// 128 x 128, operands in shared memory, accumulator in tensor memory), softmax weights by four warps that own a query row
+// per thread (row maxima and sums need no exchange between threads), P written back over S in tensor memory as 16-bit
+// values, O += P V (tcgen05, P as the tensor-memory operand, V as it lies: rows of K, elements contiguous).  One warp copies
+// (TMA), one thread issues the products.  Two such blocks share an SM: 256 of the 512 tensor-memory columns each, and one
+// block's products run under the other's softmax.
+//
+// The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units); until then weights up to
+// 2^8 are allowed, sums and products stay exact multiples, and O in tensor memory is rarely rescaled.
+#include <type_traits>
+
+#include "adsa_prefix.cuh"
+
+namespace adsa {
+
+constexpr int kWideThreads = 192;           // warps 0 .. 3: a query row per thread; warp 4 copies; warp 5 issues the products
+constexpr int kWideColumns = 256;           // tensor-memory columns of a block: S and P 128, O up to 128
+constexpr float kWideSlack = 8.f;
+
+// ---- tcgen05 ----------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tc_alloc(uint32_t slot, uint32_t columns)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_dealloc(uint32_t at, uint32_t columns)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// both operands in shared memory
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// A in tensor memory
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 32 columns of the warp's 32 rows: one row per lane
+__device__ __forceinline__ void tc_load32(uint32_t at, float (&v)[32])
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+                 "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+                   "=r"(r[31])
+                 : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_store16(uint32_t at, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tc_store32(uint32_t at, const float (&v)[32])
+{
+    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+                 "%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+                 "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+
+// Shared-memory operand of rows of 128 bytes in the 128-byte swizzle: start, stride between 64-element columns of the
+// operand where it has several (only a transposed operand uses it), 1024 bytes between groups of eight rows.
+__device__ __forceinline__ uint64_t tc_operand(uint32_t at, uint32_t column_stride)
+{
+    return (uint64_t)((at & 0x3ffffu) >> 4) | ((uint64_t)(column_stride >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// fp32 accumulator, 16-bit A and B of one type, M = 128; transposed: B's elements lie contiguous along N
+template <typename T>
+__device__ __forceinline__ uint32_t tc_shape(int n, bool transposed)
+{
+    const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return (1u << 4) | (type << 7) | (type << 10) | (transposed ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+// two 32-bit operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t &>(d))
+        : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return d;
+}
+
+// Half-type weights carry a factor of 2^6 (up to 2^14 with the slack), so that small ones keep their precision.
+template <typename T> struct WideBias { static constexpr float value = 0.f; };
+template <> struct WideBias<__half> { static constexpr float value = 6.f; };
+
+__device__ __forceinline__ int wide_items(int m) { return (m + kWideQueries - 1) / kWideQueries; }
+
+struct WideSegment {
+    const int32_t *pages;
+    int n, head, tile0, tiles, row0, rows, slot;
+};
+
+// Follows a run of units as the sweep of the smaller items does; entries are groups.
+struct WideWalk {
+    const uint32_t *plan;
+    uint32_t u, end;
+    int e, run;
+    __device__ void begin(const PrefixArgs &a, const uint32_t *plan_, int run_)
+    {
+        plan = plan_;
+        run = run_;
+        const uint32_t total = plan[a.groups], runs = min((uint32_t)a.w_runs, total);
+        u = end = 0;
+        if ((uint32_t)run < runs) {
+            u = (uint32_t)((unsigned long long)run * total / runs);
+            end = (uint32_t)((unsigned long long)(run + 1) * total / runs);
+        }
+        e = 0;
+    }
+    __device__ bool next(const PrefixArgs &a, WideSegment &s)
+    {
+        if (u >= end) return false;
+        while (u >= plan[e + 1]) ++e;
+        const uint32_t at = u - plan[e];
+        const int b0 = group_begin(a, e), m = group_members(a, e) * a.per_kv, mt = wide_items(m);
+        s.n = clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows);
+        const uint32_t tiles = (uint32_t)((s.n + kWideTile - 1) / kWideTile);
+        const int item = (int)(at / tiles);
+        s.head = item / mt;
+        const int q = item - s.head * mt;
+        s.row0 = b0 * a.per_kv + q * kWideQueries;
+        s.rows = min(m - q * kWideQueries, kWideQueries);
+        s.pages = a.p_table + (size_t)e * a.max_p_pages;
+        s.slot = first_group_item(a, e, b0, kWideQueries) + item + run;
+        s.tile0 = (int)(at - (uint32_t)item * tiles);
+        s.tiles = (int)min(tiles - (uint32_t)s.tile0, end - u);
+        u += (uint32_t)s.tiles;
+        return true;
+    }
+};
+
+// SLOTS: K or V tiles in shared memory (they alternate: K0 V0 K1 V1 ..)
+template <typename T, int NSUB, int SLOTS>
+__global__ void __launch_bounds__(kWideThreads, 2)
+prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
+{
+    constexpr int DP = 64 * NSUB;
+    constexpr uint32_t kSub = kWideTile * 128, kTile = NSUB * kSub;   // bytes of a 64-element column of a tile, of a tile
+    constexpr float kBias = WideBias<T>::value;
+    extern __shared__ unsigned char wide_smem[];
+    __shared__ uint64_t bars[2 * SLOTS + 3];
+    __shared__ uint32_t s_tmem;
+    const uint32_t base = (smem_u32(wide_smem) + 1023u) & ~1023u;
+    const uint32_t q_at = base, ring = base + kTile;
+    uint32_t *plan = reinterpret_cast<uint32_t *>(wide_smem + (base - smem_u32(wide_smem)) + (size_t)(1 + SLOTS) * kTile);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, s_full = q_full + 8, p_full = s_full + 8;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (tid == 0) {
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        mbar_init(q_full, 4); mbar_init(s_full, 1); mbar_init(p_full, 4);
+        mbar_init_fence();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    }
+    pdl_wait();
+    pdl_launch();
+    if (warp == 5) tc_alloc(smem_u32(&s_tmem), kWideColumns);
+    // first unit of every group: one warp, 32 groups at a time
+    if (warp == 4) {
+        uint32_t before = 0;
+        for (int g0 = 0; g0 < a.groups; g0 += 32) {
+            const int g = g0 + lane;
+            uint32_t w = 0;
+            if (g < a.groups) {
+                const int m = group_members(a, g) * a.per_kv;
+                const int n = clamp_rows(a.p_rows[g], a.max_p_pages, a.page_rows);
+                if (m > a.wide_above) w = (uint32_t)wide_items(m) * (uint32_t)a.kv_heads * (uint32_t)((n + kWideTile - 1) / kWideTile);
+            }
+            uint32_t incl = w;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+            if (g < a.groups) plan[g] = before + incl - w;
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) plan[a.groups] = before;
+        __syncwarp();
+        if (blockIdx.x == 0)
+            for (int g = lane; g <= a.groups; g += 32) a.w_plan[g] = plan[g];
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = s_tmem, s_col = tmem, o_col = tmem + 128;
+
+    WideWalk walk;
+    walk.begin(a, plan, blockIdx.x);
+    WideSegment s;
+    int limit = kCopySpinLimit;
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (!mbar_wait_bounded(bar, parity, limit)) {
+            limit = kCopySpinAfterTimeout;
+            if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+        }
+    };
+
+    if (warp == 4) {                                               // ---- copies ----
+        int slot = 0;
+        uint32_t phase = 0;
+        while (walk.next(a, s)) {
+            for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
+                const int rows = min(kWideTile, s.n - t * kWideTile), boxes = (rows + a.box_rows - 1) / a.box_rows;
+                for (int kv = 0; kv < 2; ++kv) {
+                    wait(empty + 8 * slot, phase ^ 1u);
+                    if (lane == 0) mbar_expect_tx(full + 8 * slot, (uint32_t)(boxes * a.box_rows) * 128u * NSUB);
+                    __syncwarp();
+                    for (int i = lane; i < boxes; i += 32) {
+                        const int row = t * kWideTile + i * a.box_rows, pg = row / a.page_rows;
+                        int page = s.pages[pg];
+                        if (page < 0 || page >= a.n_pages) {       // (the group's result is then unspecified)
+                            page = 0;
+                            if (a.status) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
+                        }
+                        const int y = (page * a.kv_heads + s.head) * a.page_rows + row - pg * a.page_rows;
+                        const uint32_t dst = ring + (uint32_t)slot * kTile + (uint32_t)(i * a.box_rows) * 128u;
+#pragma unroll
+                        for (int c = 0; c < NSUB; ++c) pa_tma(dst + c * kSub, kv ? &v_map : &k_map, c * 64, y, full + 8 * slot);
+                    }
+                    if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 5) {                                        // ---- products ----
+        const int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;
+        const uint32_t s_shape = tc_shape<T>(kWideTile, false), o_shape = tc_shape<T>(d_cols, true);
+        int slot = 0;
+        uint32_t phase = 0, q_phase = 0, p_phase = 0;
+        const auto score = [&]() {                                 // S = Q K^T with the K tile in `slot`
+            wait(full + 8 * slot, phase);
+            if (lane == 0) {
+                for (int ks = 0; ks < k_steps; ++ks) {
+                    const uint32_t off = (uint32_t)(ks >> 2) * kSub + (uint32_t)(ks & 3) * 32u;
+                    tc_mma_ss(s_col, tc_operand(q_at + off, 16), tc_operand(ring + (uint32_t)slot * kTile + off, 16), s_shape, ks > 0);
+                }
+                tc_commit(empty + 8 * slot);
+                tc_commit(s_full);
+            }
+            __syncwarp();
+            if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+        };
+        while (walk.next(a, s)) {
+            wait(q_full, q_phase);
+            q_phase ^= 1u;
+            tc_after();
+            score();
+            for (int t = 0; t < s.tiles; ++t) {
+                const uint32_t v_at = ring + (uint32_t)slot * kTile;
+                wait(full + 8 * slot, phase);
+                const int valid = s.n - (s.tile0 + t) * kWideTile;
+                if (valid < kWideTile) {
+                    // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN
+                    for (int i = lane; i < (kWideTile - valid) * 8 * NSUB; i += 32) {
+                        const int r = valid + i / (8 * NSUB), ch = i % (8 * NSUB);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};"
+                                     ::"r"(v_at + (ch >> 3) * kSub + r * 128 + (ch & 7) * 16), "r"(0u) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                wait(p_full, p_phase);
+                p_phase ^= 1u;
+                tc_after();
+                if (lane == 0) {
+#pragma unroll
+                    for (int ks = 0; ks < kWideTile / 16; ++ks)
+                        tc_mma_ts(o_col, s_col + ks * 8, tc_operand(v_at + (uint32_t)ks * 2048u, kSub), o_shape, t > 0 || ks > 0);
+                    tc_commit(empty + 8 * slot);
+                    if (t + 1 == s.tiles) tc_commit(s_full);       // the last products of the item: O is whole
+                }
+                __syncwarp();
+                if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                if (t + 1 < s.tiles) score();
+            }
+        }
+    } else {                                                       // ---- a query row per thread ----
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const int row = warp * 32 + lane;
+        uint32_t s_phase = 0;
+        while (walk.next(a, s)) {
+            {
+                // the row of Q into shared memory, zero beyond the head elements and the group's rows
+                const int packed = s.row0 + row, b = packed / a.per_kv, j = packed - b * a.per_kv;
+                const T *qp = (const T *)a.q + b * a.q_row + (s.head * a.per_kv + j) * a.q_head;
+#pragma unroll 4
+                for (int ch = 0; ch < 8 * NSUB; ++ch) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = ch * 8 + 2 * i;
+                        w[i] = row < s.rows && e < a.d ? __ldg(reinterpret_cast<const uint32_t *>(qp + e)) : 0u;
+                    }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
+                                 ::"r"(q_at + (uint32_t)(ch >> 3) * kSub + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) << 4)),
+                                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full);
+            }
+            float m = -INFINITY;                                   // raw units; the row's weights are relative to it
+            float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            for (int t = 0; t < s.tiles; ++t) {
+                wait(s_full, s_phase);
+                s_phase ^= 1u;
+                tc_after();
+                const int valid = s.n - (s.tile0 + t) * kWideTile;   // cached rows of the tile
+                float mx = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < kWideTile; c += 32) {
+                    float v[32];
+                    tc_load32(s_col + lanes + c, v);
+                    tc_load_wait();
+                    if (c + 32 <= valid) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, v[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) mx = c + i < valid ? fmaxf(mx, v[i]) : mx;
+                    }
+                }
+                const bool move = (mx - m) * a.scale_log2e > kWideSlack || m == -INFINITY;
+                if (__any_sync(0xffffffffu, move)) {
+                    const float m_new = move ? fmaxf(m, mx) : m;
+                    const float corr = m_new == -INFINITY || m == -INFINITY ? (m == m_new ? 1.f : 0.f) : pa_exp2((m - m_new) * a.scale_log2e);
+                    m = m_new;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) { l2[i].x *= corr; l2[i].y *= corr; }
+                    if (t > 0) {                                   // the products before this tile's are complete: their S is
+#pragma unroll 1
+                        for (int c = 0; c < DP; c += 32) {
+                            float v[32];
+                            tc_load32(o_col + lanes + c, v);
+                            tc_load_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] *= corr;
+                            tc_store32(o_col + lanes + c, v);
+                        }
+                    }
+                }
+                const float shift = kBias - (m == -INFINITY ? 0.f : m) * a.scale_log2e;
+                const float2 scale2 = make_float2(a.scale_log2e, a.scale_log2e), shift2 = make_float2(shift, shift);
+#pragma unroll
+                for (int c = 0; c < kWideTile; c += 32) {
+                    float v[32];
+                    tc_load32(s_col + lanes + c, v);
+                    tc_load_wait();
+                    if (c + 32 > valid) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = c + i < valid ? v[i] : -INFINITY;
+                    }
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float2 x = fma2(make_float2(v[2 * i], v[2 * i + 1]), scale2, shift2);
+                        x.x = pa_exp2(x.x);
+                        x.y = pa_exp2(x.y);
+                        l2[i & 1] = add2(l2[i & 1], x);            // the sum takes the weights before they are rounded
+                        p[i] = pack2<T>(x.x, x.y);
+                    }
+                    tc_store16(s_col + lanes + c / 2, p);          // over columns whose scores have been read
+                }
+                tc_store_wait();
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+            }
+            wait(s_full, s_phase);
+            s_phase ^= 1u;
+            tc_after();
+            const bool fits = s.slot < a.n_w_slots;
+            if (!fits && a.status && lane == 0) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
+            const size_t at = (size_t)s.slot * kWideQueries + row;
+            if (fits && row < s.rows)
+                *reinterpret_cast<float2 *>(a.w_ml + 2 * at) = make_float2(m * a.scale_log2e - kBias, l2[0].x + l2[0].y + l2[1].x + l2[1].y);
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 32) {
+                float v[32];
+                tc_load32(o_col + lanes + c, v);
+                tc_load_wait();
+                if (fits && row < s.rows) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<float4 *>(a.w_state + at * DP + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+            }
+            tc_before();                                           // read before the next item's products write O
+        }
+    }
+    tc_before();
+    __syncthreads();
+    if (warp == 5) {
+        tc_after();
+        tc_dealloc(tmem, kWideColumns);
+    }
+}
+
+namespace {
+
+template <typename T, int NSUB, int SLOTS>
+cudaError_t launch_wide(const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+{
+    const size_t smem = 1024 + (size_t)(1 + SLOTS) * NSUB * kWideTile * 128 + (size_t)(a.groups + 1) * 4;
+    const auto kern = prefix_wide_kernel<T, NSUB, SLOTS>;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kern, dim3((unsigned)a.w_runs), kWideThreads, smem, st, a, km, vm);
+}
+
+}  // namespace
+
+cudaError_t launch_prefix_wide(int dtype, int nsub, const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+{
+    if (dtype == ADSA_BF16) return nsub == 1 ? launch_wide<__nv_bfloat16, 1, 5>(a, km, vm, st) : launch_wide<__nv_bfloat16, 2, 2>(a, km, vm, st);
+    return nsub == 1 ? launch_wide<__half, 1, 5>(a, km, vm, st) : launch_wide<__half, 2, 2>(a, km, vm, st);
+}
+
+}  // namespace adsa
