@@ -24,15 +24,15 @@ struct PrefixArgs {
     int d;
     float scale_log2e;
     // workspace
-    uint32_t *plan;                         // [entries + 1] first unit of every entry (groups, then batch rows)
+    uint4 *plan;                            // [1 + 2 batch] for the merge: number of units; two words of four per batch row
     float *p_state, *p_ml, *o_state, *o_ml; // prefix slots, own-row slots: rows of d_pad floats, (m, l) pairs
     int n_p_slots, n_o_slots;
     // groups with more query rows per key head than this go to the wide kernel, with a plan and slots of its own
     int wide_above;
     uint32_t *w_plan;                       // [groups + 1]
     float *w_state, *w_ml;                  // slots of kWideQueries rows
-    int n_w_slots, w_runs;
-    int runs;                               // blocks of the sweep kernel's grid
+    int n_w_slots, w_resident;              // w_resident: blocks of the wide kernel that fit the GPU at a time; 0: it does not run
+    int resident;                           // blocks of the sweep kernel that fit the GPU at a time
 };
 
 __device__ __forceinline__ int clamp_rows(int n, int max_pages, int page_rows)
@@ -67,6 +67,44 @@ __device__ __forceinline__ float pa_exp2(float x)
 // the half type lose precision below 2^-14, so there P is scaled by 2^8 (it cancels in o / l; the states carry it in m).
 template <typename T> struct WeightBias { static constexpr float value = 0.f; };
 template <> struct WeightBias<__half> { static constexpr float value = 8.f; };
+
+// How a list of units is cut into runs: `resident` runs of 2^(K-2) pieces, as many of half that, .. of one piece, and
+// as many of one piece again (K = 1: a run a block).  Blocks that are quick take more of the shrinking runs, and all end
+// within a short one.  A piece has at least four units, as a run costs about two (its state, its first queries); K is at
+// most 5, and 1 where the partial states are large (`even`).
+struct Cut {
+    uint32_t resident, runs, half, base, rem;   // half = 2^(K-1); piece p begins at unit p base + min(p, rem)
+    __device__ __forceinline__ Cut(uint32_t total, uint32_t resident_, bool even = false) : resident(resident_)
+    {
+        const uint32_t fours = even ? 0u : min(total / (4u * resident), 16u);
+        const uint32_t K = fours < 2u ? 1u : 32u - __clz(fours);
+        half = 1u << (K - 1u);
+        uint32_t pieces = half * resident;
+        runs = K * resident;
+        if (total < resident) pieces = runs = max(total, 1u);
+        base = total / pieces;
+        rem = total - base * pieces;
+        if (total == 0u) runs = 0u;
+    }
+    __device__ __forceinline__ uint32_t begin_of(uint32_t run) const
+    {
+        uint32_t p = run;
+        if (half > 1u) {
+            const uint32_t k = run / resident;
+            p = (half - (half >> k)) * resident + (run - k * resident) * max(1u, half >> (k + 1u));
+            p = min(p, half * resident);
+        }
+        return p * base + min(p, rem);
+    }
+    __device__ __forceinline__ uint32_t run_of(uint32_t unit) const
+    {
+        const uint32_t big = rem * (base + 1u), p = unit < big ? unit / (base + 1u) : rem + (unit - big) / max(base, 1u);
+        if (half == 1u) return min(p, runs - 1u);
+        const uint32_t left = half - p / resident;       // half >> (k+1) < left <= half >> k
+        const uint32_t k = 31u - __clz(half) - (32u - __clz(left - 1u));
+        return min(k * resident + (p - (half - (half >> k)) * resident) / max(1u, half >> (k + 1u)), runs - 1u);
+    }
+};
 
 cudaError_t launch_prefix_wide(int dtype, int nsub, const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st);
 

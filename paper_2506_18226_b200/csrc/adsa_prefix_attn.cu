@@ -46,21 +46,13 @@ __host__ __device__ __forceinline__ int own_slot_rows(int per_kv)
     return per_kv >= kPaQueries ? kPaQueries : kPaWarps / query_warps(per_kv) * per_kv;
 }
 
-// units of an entry: groups first, then batch rows
-__device__ __forceinline__ uint32_t entry_units(const PrefixArgs &a, int e)
-{
-    if (e < a.groups) {
-        const int m = group_members(a, e) * a.per_kv;
-        if (m > a.wide_above) return 0;
-        const int n = clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows);
-        return (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
-    }
-    const int n = clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
-    return (uint32_t)query_items(a.per_kv) * (uint32_t)a.kv_heads * (uint32_t)((n + kPaTile - 1) / kPaTile);
-}
-
-// Every one of these runs has a unit, so every state between an item's first and last run exists.
-__device__ __forceinline__ uint32_t working_runs(const PrefixArgs &a, uint32_t total) { return min((uint32_t)a.runs, total); }
+// Lengths and boundaries as read (and clamped) once per block; entries are groups, then batch rows.
+struct Shared {
+    uint32_t *plan;                         // [entries + 1] first unit of every entry
+    int *len;                               // [entries] cached rows
+    int *begin;                             // [groups + 1]
+};
+__device__ __forceinline__ int members(const Shared &c, int g) { return max(c.begin[g + 1] - c.begin[g], 0); }
 
 // Neighbouring units of one item inside a run.
 struct Segment {
@@ -74,46 +66,41 @@ struct Segment {
 };
 
 struct Walk {
-    const uint32_t *plan;                   // shared copy
     uint32_t u, end;
     int e, run;
-    __device__ void begin(const PrefixArgs &a, const uint32_t *plan_, int run_)
+    bool empty;                             // the run has no units at all
+    __device__ void begin(const PrefixArgs &a, const Shared &c, const Cut &cut, int run_)
     {
-        plan = plan_;
         run = run_;
         const int entries = a.groups + a.batch;
-        const uint32_t total = plan[entries], runs = working_runs(a, total);
         u = end = 0;
-        if ((uint32_t)run < runs) {
-            u = (uint32_t)((unsigned long long)run * total / runs);
-            end = (uint32_t)((unsigned long long)(run + 1) * total / runs);
-        }
+        if ((uint32_t)run < cut.runs) { u = cut.begin_of(run); end = cut.begin_of(run + 1); }
+        empty = u >= end;
         int lo = 0, hi = entries;           // the last entry whose first unit is <= u
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (plan[mid] <= u) lo = mid;
+            if (c.plan[mid] <= u) lo = mid;
             else hi = mid - 1;
         }
         e = lo;
     }
-    __device__ bool next(const PrefixArgs &a, Segment &s)
+    __device__ bool next(const PrefixArgs &a, const Shared &c, Segment &s)
     {
         if (u >= end) return false;
-        while (u >= plan[e + 1]) ++e;
-        const uint32_t at = u - plan[e];
+        while (u >= c.plan[e + 1]) ++e;
+        const uint32_t at = u - c.plan[e];
         const bool pre = e < a.groups;
-        const int b0 = pre ? group_begin(a, e) : e - a.groups, m = (pre ? group_members(a, e) : 1) * a.per_kv, mt = query_items(m);
-        s.n = pre ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[b0], a.max_pages, a.page_rows);
-        const uint32_t tiles = (uint32_t)((s.n + kPaTile - 1) / kPaTile);
-        const int item = (int)(at / tiles);                        // (key head, then query rows)
-        s.head = item / mt;
-        const int q = item - s.head * mt;
+        const int b0 = pre ? c.begin[e] : e - a.groups, m = (pre ? members(c, e) : 1) * a.per_kv, mt = query_items(m);
+        s.n = c.len[e];
+        const uint32_t tiles = (uint32_t)((s.n + kPaTile - 1) / kPaTile), item = at / tiles;   // (key head, then query rows)
+        s.head = mt == 1 ? (int)item : (int)item / mt;
+        const int q = (int)item - s.head * mt;
         s.row0 = b0 * a.per_kv + q * kPaQueries;
         s.rows = min(m - q * kPaQueries, kPaQueries);
         s.pages = pre ? a.p_table + (size_t)e * a.max_p_pages : a.table + (size_t)b0 * a.max_pages;
-        s.slot = (pre ? first_group_item(a, e, b0, kPaQueries) : b0 * a.kv_heads * mt) + item + run;
+        s.slot = (pre ? first_group_item(a, e, b0, kPaQueries) : b0 * a.kv_heads * mt) + (int)item + run;
         s.prefix = pre;
-        s.tile0 = (int)(at - (uint32_t)item * tiles);
+        s.tile0 = (int)(at - item * tiles);
         s.tiles = (int)min(tiles - (uint32_t)s.tile0, end - u);
         u += (uint32_t)s.tiles;
         return true;
@@ -178,7 +165,10 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     __shared__ __align__(16) uint4 answers[2];
     __shared__ uint32_t warp_sums[kPaThreads / 32];
     const uint32_t ring = (smem_u32(pa_smem) + 1023u) & ~1023u;
-    uint32_t *plan = reinterpret_cast<uint32_t *>(pa_smem + (ring - smem_u32(pa_smem)) + (size_t)STAGES * 2 * kHalf);
+    Shared c;
+    c.plan = reinterpret_cast<uint32_t *>(pa_smem + (ring - smem_u32(pa_smem)) + (size_t)STAGES * 2 * kHalf);
+    c.len = reinterpret_cast<int *>(c.plan + a.groups + a.batch + 1);
+    c.begin = c.len + a.groups + a.batch;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, asked = empty + 8 * STAGES, heard = asked + 16, answer = smem_u32(answers);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int entries = a.groups + a.batch;
@@ -192,30 +182,39 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     }
     // Behind the wide kernel of the same call (which has waited for what was ahead of it before this one could begin) there
     // is nothing to wait for here; each block waits before it ends, so that the merge finds both kernels' states.
-    const bool behind_wide = a.w_runs > 0;
+    const bool behind_wide = a.w_resident > 0;
     if (!behind_wide) pdl_wait();
     pdl_launch();
 
-    // ---- first unit of every entry: each thread sums a run of entries, the runs are scanned over the block ----
-    const int run = (entries + kPaThreads - 1) / kPaThreads, e0 = min(tid * run, entries), e1 = min(e0 + run, entries);
+    // ---- lengths, boundaries, first unit of every entry: each thread sums a few entries, the sums are scanned over the block ----
+    const int per = (entries + kPaThreads - 1) / kPaThreads, e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
+    for (int g = tid; g <= a.groups && a.groups > 0; g += kPaThreads) c.begin[g] = group_begin(a, g);
+    for (int e = e0; e < e1; ++e)
+        c.len[e] = e < a.groups ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
+    __syncthreads();
     uint32_t mine = 0;
-    for (int e = e0; e < e1; ++e) { const uint32_t w = entry_units(a, e); plan[e] = mine; mine += w; }
+    for (int e = e0; e < e1; ++e) {
+        const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;
+        c.plan[e] = mine;
+        if (e >= a.groups || m <= a.wide_above) mine += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + kPaTile - 1) / kPaTile);
+    }
     uint32_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
-    uint32_t before = incl - mine;
-    for (int w = 0; w < warp; ++w) before += warp_sums[w];
-    for (int e = e0; e < e1; ++e) plan[e] += before;
-    if (tid == kPaThreads - 1) plan[entries] = before + mine;
+    uint32_t before = incl - mine, total = 0;
+    for (int w = 0; w < kPaThreads / 32; ++w) { if (w < warp) before += warp_sums[w]; total += warp_sums[w]; }
+    for (int e = e0; e < e1; ++e) c.plan[e] += before;
+    if (tid == 0) c.plan[entries] = total;
     __syncthreads();
+    const Cut cut(total, (uint32_t)a.resident);
     Walk walk;
-    walk.begin(a, plan, blockIdx.x);
+    walk.begin(a, c, cut, blockIdx.x);
     Segment s;
     // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp asks for the next
-    // run when it begins one, into the answer slot that all warps have read the last time, and leaves the plan for the
-    // merge if it has run 0 (block 0 may itself be taken over before it starts, where another grid holds the SMs).
+    // run when it begins one, into the answer slot that all warps have read the last time, and leaves its share of the
+    // plan for the merge: that goes by run, as any block may be taken over before it starts.
     int limit = kCopySpinLimit;
     uint32_t turns = 0;                                            // runs finished by this warp
     const auto begin_run = [&](int run) {
@@ -225,11 +224,34 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             mbar_expect_tx(asked + 8 * i, 16);
             pa_ask_block(answer + 16 * i, asked + 8 * i);
         }
-        if (run == 0)
-            for (int e = lane; e <= entries; e += 32) a.plan[e] = plan[e];
+        __syncwarp();                                              // the other lanes must not spin for the answer before it is asked for
+        if (run == 0 && lane == 0) a.plan[0] = make_uint4(total, 0u, 0u, 0u);
+        const uint32_t share = max(cut.runs, 1u);
+        for (int b = (uint32_t)run < share ? run + lane * (int)share : a.batch; b < a.batch; b += 32 * (int)share) {
+            // the batch row's own units, and its group's: the last group that begins at or before it
+            uint4 own_part = make_uint4(c.plan[a.groups + b], (uint32_t)(c.len[a.groups + b] + kPaTile - 1) / kPaTile, 0u, 0u), group = make_uint4(0u, 0u, 0u, 0u);
+            int lo = -1, hi = a.groups - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (c.begin[mid] <= b) lo = mid;
+                else hi = mid - 1;
+            }
+            if (lo >= 0 && b < c.begin[lo + 1]) {
+                const int m = members(c, lo) * a.per_kv, tile = m > a.wide_above ? kWideTile : kPaTile;
+                group = make_uint4(c.plan[lo], (uint32_t)(c.len[lo] + tile - 1) / tile, (uint32_t)c.begin[lo], (uint32_t)m);
+                own_part.z = (uint32_t)lo;
+            }
+            a.plan[1 + 2 * b] = own_part;
+            a.plan[2 + 2 * b] = group;
+        }
+        __syncwarp();
     };
-    const auto advance = [&](Segment &n) {
-        while (!walk.next(a, n)) {
+    // patient: wait for whatever comes.  Otherwise only go as far as an answer that is already asked for: behind an empty run the
+    // next answer is asked for when the copying warp gets there, which may first need tiles of the segment in hand to be freed.
+    enum { kEnd, kSegment, kLater };
+    const auto advance = [&](Segment &n, bool patient) {
+        while (!walk.next(a, c, n)) {
+            if (!patient && walk.empty) return kLater;
             const uint32_t i = turns & 1u;
             int run = -1;
             if (mbar_wait_bounded(asked + 8 * i, (turns >> 1) & 1u, limit)) run = pa_answer(answer + 16 * i);
@@ -241,18 +263,21 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive(heard + 8 * i);
             ++turns;
-            if (run < 0) return false;
+            if (run < 0) return kEnd;
             if (warp == kPaWarps) begin_run(run);
-            walk.begin(a, plan, run);
+            walk.begin(a, c, cut, run);
         }
-        return true;
+        return kSegment;
     };
 
     if (warp == kPaWarps) {                                        // ---- the copying warp ----
         int stage = 0;
         uint32_t phase = 0;
         begin_run(blockIdx.x);
-        while (advance(s)) {
+        while (advance(s, true) == kSegment) {
+            // page ids are read 32 at a time, a lane each
+            const int last_page = (s.n - 1) / a.page_rows;
+            int window = -64, ids = 0;
             for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
                 if (!mbar_wait_bounded(empty + 8 * stage, phase ^ 1u, limit)) {
                     limit = kCopySpinAfterTimeout;
@@ -262,9 +287,16 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 if (lane == 0) mbar_expect_tx(full + 8 * stage, (uint32_t)(boxes * a.box_rows) * 128u * 2u * NSUB);
                 __syncwarp();
                 const uint32_t k_dst = ring + stage * 2 * kHalf;
-                for (int i = lane; i < boxes; i += 32) {
-                    const int row = t * kPaTile + i * a.box_rows, pg = row / a.page_rows;
-                    int page = s.pages[pg];
+                const int page0 = t * kPaTile / a.page_rows, page1 = (t * kPaTile + rows - 1) / a.page_rows;
+                if (page1 >= window + 32) {
+                    window = page0;
+                    ids = window + lane <= last_page ? s.pages[window + lane] : 0;
+                }
+                for (int i0 = 0; i0 < boxes; i0 += 32) {
+                    const int i = i0 + lane, row = t * kPaTile + min(i, boxes - 1) * a.box_rows, pg = row / a.page_rows;
+                    int page = __shfl_sync(0xffffffffu, ids, (pg - window) & 31);
+                    if (i >= boxes) continue;
+                    if (pg - window >= 32) page = s.pages[pg];     // a tile of more than 32 pages
                     if (page < 0 || page >= a.n_pages) {           // (the row's result is then unspecified)
                         page = 0;
                         if (a.status) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
@@ -307,15 +339,15 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         }
     };
     Segment nxt;
-    bool more = advance(nxt);
-    if (more) ask_q(nxt);
-    while (more) {
+    auto more = advance(nxt, true);
+    if (more == kSegment) ask_q(nxt);
+    while (more == kSegment) {
         s = nxt;
         uint32_t qa[KS][2];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) { qa[ks][0] = qn[ks][0]; qa[ks][1] = qn[ks][1]; }
-        more = advance(nxt);
-        if (more) ask_q(nxt);
+        more = advance(nxt, false);
+        if (more == kSegment) ask_q(nxt);
         const int wq = query_warps(s.rows), wk = kPaWarps / wq;     // warps over query rows, warps over cached rows
         const int qb = warp & (wq - 1), kb = warp / wq;
         // state of query rows 2 t4 and 2 t4 + 1: maximum (alike in the eight lanes of a t4), this lane's share of the sum, O^T
@@ -422,6 +454,10 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 }
             }
         }
+        if (more == kLater) {
+            more = advance(nxt, true);
+            if (more == kSegment) ask_q(nxt);
+        }
     }
 }
 
@@ -437,85 +473,75 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     const int b = blockIdx.x / heads, qh = blockIdx.x - b * heads, head = qh / a.per_kv, j = qh - head * a.per_kv;
     pdl_wait();
     pdl_launch();
-    const uint32_t total = a.plan[a.groups + a.batch], runs = working_runs(a, total);
-    // the run that holds unit u: the last c with floor(c n / runs) <= u
-    const auto run_of = [](uint32_t u, uint32_t n, uint32_t c) { return (int)min((((unsigned long long)u + 1) * c - 1) / n, (unsigned long long)c - 1); };
-
-    // the group of the batch row: the last one that begins at or before it
-    int grp = -1;
-    {
-        int lo = -1, hi = a.groups - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (group_begin(a, mid) <= b) lo = mid;
-            else hi = mid - 1;
-        }
-        if (lo >= 0 && b < group_begin(a, lo + 1)) grp = lo;
-    }
+    const uint32_t total = a.plan[0].x;
+    const uint4 own_part = a.plan[1 + 2 * b], group = a.plan[2 + 2 * b];
     // runs of states: prefix, then own rows
     const float *p_state = a.p_state, *p_ml = a.p_ml;
-    size_t p_first = 0, o_first, p_slot = kPaQueries;
+    size_t p_first = 0, o_first = 0, p_slot = kPaQueries;
     int p_segs = 0, p_step = 0, p_subs = 1, o_segs = 0;
     const int own_mt = query_items(a.per_kv), own_q = j / kPaQueries, own_rows = min(a.per_kv - own_q * kPaQueries, kPaQueries);
     const int o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
-    if (grp >= 0) {
-        const int b0 = group_begin(a, grp), m = group_members(a, grp) * a.per_kv;
+    const Cut cut(total, (uint32_t)a.resident);
+    if (group.y > 0) {                       // tiles of the group's prefix
+        const int b0 = (int)group.z, m = (int)group.w, grp = (int)own_part.z;
         const bool wide = m > a.wide_above;
-        const int queries = wide ? kWideQueries : kPaQueries, tile = wide ? kWideTile : kPaTile, mt = (m + queries - 1) / queries;
-        const int packed = (b - b0) * a.per_kv + j, q = packed / queries, rows = min(m - q * queries, queries);
-        const int n = clamp_rows(a.p_rows[grp], a.max_p_pages, a.page_rows), tiles = (n + tile - 1) / tile;
-        const uint32_t *plan = wide ? a.w_plan : a.plan;
-        const uint32_t p_total = wide ? plan[a.groups] : total, p_runs = wide ? min((uint32_t)a.w_runs, p_total) : runs;
-        if (tiles > 0 && p_runs > 0) {
-            const int item = head * mt + q;
-            const uint32_t u = plan[grp] + (uint32_t)item * (uint32_t)tiles;
-            const int c0 = run_of(u, p_total, p_runs), c1 = run_of(u + tiles - 1, p_total, p_runs);
-            const long long slot = (long long)first_group_item(a, grp, b0, queries) + item + c0;
-            p_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, (wide ? a.n_w_slots : a.n_p_slots) - slot));
-            p_subs = wide ? 1 : kPaWarps / query_warps(rows);
-            p_step = rows;
-            p_slot = queries;
-            p_first = (size_t)slot * p_slot + (packed - q * queries);
-            if (wide) { p_state = a.w_state; p_ml = a.w_ml; }
+        const int queries = wide ? kWideQueries : kPaQueries, mt = (m + queries - 1) / queries;
+        const int packed = (b - b0) * a.per_kv + j, q = packed / queries, rows = min(m - q * queries, queries), item = head * mt + q;
+        uint32_t c0, c1;
+        if (wide) {
+            const Cut wide_cut(a.w_plan[a.groups], (uint32_t)a.w_resident, true);
+            const uint32_t u = a.w_plan[grp] + (uint32_t)item * group.y;
+            c0 = wide_cut.run_of(u); c1 = wide_cut.run_of(u + group.y - 1);
+            p_state = a.w_state; p_ml = a.w_ml;
+        } else {
+            const uint32_t u = group.x + (uint32_t)item * group.y;
+            c0 = cut.run_of(u); c1 = cut.run_of(u + group.y - 1);
         }
+        const long long slot = (long long)first_group_item(a, grp, b0, queries) + item + c0;
+        p_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, (wide ? a.n_w_slots : a.n_p_slots) - slot));
+        p_subs = wide ? 1 : kPaWarps / query_warps(rows);
+        p_step = rows;
+        p_slot = queries;
+        p_first = (size_t)slot * p_slot + (packed - q * queries);
     }
-    {
-        const int n = clamp_rows(a.n_rows[b], a.max_pages, a.page_rows), tiles = (n + kPaTile - 1) / kPaTile;
-        o_first = 0;
-        if (tiles > 0 && runs > 0) {
-            const int item = head * own_mt + own_q;
-            const uint32_t u = a.plan[a.groups + b] + (uint32_t)item * (uint32_t)tiles;
-            const int c0 = run_of(u, total, runs), c1 = run_of(u + tiles - 1, total, runs);
-            const long long slot = (long long)b * a.kv_heads * own_mt + item + c0;
-            o_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_o_slots - slot));
-            o_first = (size_t)slot * o_step + (j - own_q * kPaQueries);
-        }
+    if (own_part.y > 0) {
+        const int item = head * own_mt + own_q;
+        const uint32_t u = own_part.x + (uint32_t)item * own_part.y, c0 = cut.run_of(u), c1 = cut.run_of(u + own_part.y - 1);
+        const long long slot = (long long)b * a.kv_heads * own_mt + item + c0;
+        o_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_o_slots - slot));
+        o_first = (size_t)slot * o_step + (j - own_q * kPaQueries);
     }
     const int n_p = p_segs * p_subs, n_states = n_p + o_segs * o_subs;
     float m = -INFINITY, l = 0.f, o[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) o[e] = 0.f;
-    for (int i = warp; i < n_states; i += WARPS) {
-        const float *st, *ml;
-        if (i < n_p) {
-            const int seg = i / p_subs, sub = i - seg * p_subs;
-            const size_t row = p_first + (size_t)seg * p_slot + (size_t)sub * p_step;
-            st = p_state + row * DP; ml = p_ml + 2 * row;
-        } else {
-            const int k = i - n_p, seg = k / o_subs, sub = k - seg * o_subs;
-            const size_t row = o_first + (size_t)seg * o_step + (size_t)sub * own_rows;
-            st = a.o_state + row * DP; ml = a.o_ml + 2 * row;
+    constexpr int AHEAD = 4;                // states in flight per warp
+    for (int i0 = warp; i0 < n_states; i0 += AHEAD * WARPS) {
+        float2 ml[AHEAD];
+        float x[AHEAD][PER];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * WARPS;
+            ml[k] = make_float2(-INFINITY, 0.f);
+            if (i < n_states) {
+                const bool pre = i < n_p;
+                const int at = pre ? i : i - n_p, subs = pre ? p_subs : o_subs, seg = at / subs, sub = at - seg * subs;
+                const size_t row = pre ? p_first + (size_t)seg * p_slot + (size_t)sub * p_step : o_first + (size_t)seg * o_step + (size_t)sub * own_rows;
+                ml[k] = *reinterpret_cast<const float2 *>((pre ? p_ml : a.o_ml) + 2 * row);
+                const float *st = (pre ? p_state : a.o_state) + row * DP;
+#pragma unroll
+                for (int e = 0; e < PER; e += 2) *reinterpret_cast<float2 *>(&x[k][e]) = *reinterpret_cast<const float2 *>(st + e * 32 + 2 * lane);
+            }
         }
-        const float2 s = *reinterpret_cast<const float2 *>(ml);
-        float x[PER];
 #pragma unroll
-        for (int e = 0; e < PER; e += 2) *reinterpret_cast<float2 *>(x + e) = *reinterpret_cast<const float2 *>(st + e * 32 + 2 * lane);
-        if (s.y == 0.f && s.x == -INFINITY) continue;               // an empty state
-        const float M = fmaxf(m, s.x), w1 = m == -INFINITY ? 0.f : pa_exp2(m - M), w2 = s.x == -INFINITY ? 0.f : pa_exp2(s.x - M);
-        l = l * w1 + s.y * w2;
+        for (int k = 0; k < AHEAD; ++k) {
+            if (ml[k].y == 0.f && ml[k].x == -INFINITY) continue;   // an empty state
+            const float M = fmaxf(m, ml[k].x), w1 = m == -INFINITY ? 0.f : pa_exp2(m - M), w2 = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
+            l = l * w1 + ml[k].y * w2;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] = o[e] * w1 + x[e] * w2;
-        m = M;
+            for (int e = 0; e < PER; ++e) o[e] = o[e] * w1 + x[k][e] * w2;
+            m = M;
+        }
     }
     if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
 #pragma unroll
@@ -571,7 +597,7 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     const int per_kv = n_heads / kv_heads;
     o->nsub = (head_dim + 63) / 64;
     o->blocks = sm_count() * (o->nsub <= 2 ? 2 : 1);
-    o->max_runs = 4 * o->blocks;
+    o->max_runs = 5 * o->blocks;
     o->wide_blocks = groups && o->nsub <= 2 && (long long)batch * per_kv > kWideAbove ? 2 * sm_count() : 0;
     o->w_slots = o->wide_blocks ? ((long long)batch * per_kv / kWideQueries + groups) * kv_heads + o->wide_blocks : 0;
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
@@ -580,7 +606,7 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     const size_t dp = 64 * o->nsub, p_rows = (size_t)o->p_slots * kPaQueries, o_rows = (size_t)o->o_slots * own_slot_rows(per_kv);
     if (o->p_slots > 0x7fffffffLL || o->o_slots > 0x7fffffffLL || (long long)batch * n_heads > 0x7fffffffLL) return false;
     o->plan = 0;
-    o->p_state = o->plan + up((size_t)(batch + groups + 1) * 4);
+    o->p_state = o->plan + up((size_t)(1 + 2 * (size_t)batch) * 16);
     o->p_ml = o->p_state + up(p_rows * dp * 4);
     o->o_state = o->p_ml + up(p_rows * 8);
     o->o_ml = o->o_state + up(o_rows * dp * 4);
@@ -623,26 +649,26 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
 }
 
 template <typename T, int NSUB, int STAGES>
-cudaError_t launch_prefix(const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
+cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
 {
-    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * kPaTile * 128 + (size_t)(a.batch + a.groups + 1) * 4;
+    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * kPaTile * 128 + (size_t)(2 * a.batch + 3 * a.groups + 2) * 4;
     const auto kern = prefix_sweep_kernel<T, NSUB, STAGES>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(kern, dim3((unsigned)a.runs), kPaThreads, smem, st, a, km, vm);
+    e = launch_pdl(kern, dim3(runs), kPaThreads, smem, st, a, km, vm);
     if (e != cudaSuccess) return e;
     return launch_pdl(prefix_merge_kernel<T, NSUB>, dim3((unsigned)(a.batch * a.kv_heads * a.per_kv)), kPaMergeThreads, 0, st, a, (T *)out, out_f32, lse);
 }
 
 template <typename T>
-cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
+cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
                                float *lse, cudaStream_t st)
 {
     switch (nsub) {                          // 96 KB of tiles in flight per block, two blocks per SM; wide rows: one block
-    case 1: return launch_prefix<T, 1, 6>(a, km, vm, out, out_f32, lse, st);
-    case 2: return launch_prefix<T, 2, 3>(a, km, vm, out, out_f32, lse, st);
-    case 3: return launch_prefix<T, 3, 4>(a, km, vm, out, out_f32, lse, st);
-    default: return launch_prefix<T, 4, 3>(a, km, vm, out, out_f32, lse, st);
+    case 1: return launch_prefix<T, 1, 6>(a, runs, km, vm, out, out_f32, lse, st);
+    case 2: return launch_prefix<T, 2, 3>(a, runs, km, vm, out, out_f32, lse, st);
+    case 3: return launch_prefix<T, 3, 4>(a, runs, km, vm, out, out_f32, lse, st);
+    default: return launch_prefix<T, 4, 3>(a, runs, km, vm, out, out_f32, lse, st);
     }
 }
 
@@ -697,21 +723,21 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.d = kv->head_dim;
     const float scale = softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale;
     a.scale_log2e = scale * 1.44269504088896341f;
-    a.plan = (uint32_t *)(ws + l.plan);
+    a.plan = (uint4 *)(ws + l.plan);
     a.p_state = (float *)(ws + l.p_state); a.p_ml = (float *)(ws + l.p_ml);
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
     a.wide_above = l.wide_blocks ? kWideAbove : 0x7fffffff;
     a.w_plan = (uint32_t *)(ws + l.w_plan); a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
-    a.n_w_slots = (int)l.w_slots; a.w_runs = l.wide_blocks;
+    a.n_w_slots = (int)l.w_slots; a.w_resident = l.wide_blocks; a.resident = l.blocks;
 
-    // runs of eight tiles or more where the tables are full, at least one per block
-    const double runs = (own_units + (n_groups ? p_units : 0)) / 8;
-    a.runs = runs <= l.blocks ? l.blocks : runs >= l.max_runs ? l.max_runs : (int)runs;
+    // as many blocks as there can be runs, and no more than there can be units
+    const double units = own_units + (n_groups ? p_units : 0);
+    const unsigned runs = units < l.max_runs ? (unsigned)units : (unsigned)l.max_runs;
     cudaStream_t st = (cudaStream_t)stream;
-    if (a.w_runs && launch_prefix_wide(kv->dtype, l.nsub, a, km, vm, st) != cudaSuccess) return ADSA_ECUDA;
-    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, km, vm, out, out_f32, lse, st)
-                                                  : launch_prefix_type<__half>(l.nsub, a, km, vm, out, out_f32, lse, st);
+    if (a.w_resident && launch_prefix_wide(kv->dtype, l.nsub, a, km, vm, st) != cudaSuccess) return ADSA_ECUDA;
+    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, runs, km, vm, out, out_f32, lse, st)
+                                                  : launch_prefix_type<__half>(l.nsub, a, runs, km, vm, out, out_f32, lse, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 

@@ -128,12 +128,9 @@ struct WideWalk {
     {
         plan = plan_;
         run = run_;
-        const uint32_t total = plan[a.groups], runs = min((uint32_t)a.w_runs, total);
+        const Cut cut(plan[a.groups], (uint32_t)a.w_resident, true);
         u = end = 0;
-        if ((uint32_t)run < runs) {
-            u = (uint32_t)((unsigned long long)run * total / runs);
-            end = (uint32_t)((unsigned long long)(run + 1) * total / runs);
-        }
+        if ((uint32_t)run < cut.runs) { u = cut.begin_of(run); end = cut.begin_of(run + 1); }
         e = 0;
     }
     __device__ bool next(const PrefixArgs &a, WideSegment &s)
@@ -433,7 +430,7 @@ cudaError_t launch_wide(const PrefixArgs &a, const CUtensorMap &km, const CUtens
     const auto kern = prefix_wide_kernel<T, NSUB, SLOTS>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, dim3((unsigned)a.w_runs), kWideThreads, smem, st, a, km, vm);
+    return launch_pdl(kern, dim3((unsigned)a.w_resident), kWideThreads, smem, st, a, km, vm);
 }
 
 }  // namespace
