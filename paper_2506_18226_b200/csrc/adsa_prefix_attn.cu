@@ -6,7 +6,7 @@
 // so the prefix is swept ONCE per group and key head, by all of the group's queries together (a real matrix product:
 // members x query heads per key head rows against the prefix), and each batch row's own rows by its queries alone.
 //
-// Work split.  The unit is a tile of 64 cached rows of one key head.  All units of a call (of every prefix, 32 query
+// Work split.  The unit is a tile of 128 (wider rows: 64) cached rows of one key head.  All units of a call (of every prefix, 32 query
 // rows at a time, then of every batch row) form one list; run c of C takes units c U / C .. (c + 1) U / C, whatever
 // they belong to, so long and short rows, prefixes and single rows mix without the host knowing a length.  Where a run
 // changes from one item to the next it leaves the item's partial state in the workspace; a second small kernel merges
@@ -28,7 +28,8 @@
 
 namespace adsa {
 
-constexpr int kPaTile = 64;                 // cached rows of a unit
+// cached rows of a unit: 32 KB of K and V for rows of up to 128 elements
+__host__ __device__ constexpr int tile_rows(int nsub) { return nsub == 1 ? 128 : 64; }
 constexpr int kPaQueries = 32;              // query rows of an item at most
 constexpr int kPaWarps = 4;                 // warps that compute; one more warp copies
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
@@ -65,6 +66,7 @@ struct Segment {
     bool prefix;
 };
 
+template <int TILE>
 struct Walk {
     uint32_t u, end;
     int e, run;
@@ -92,7 +94,7 @@ struct Walk {
         const bool pre = e < a.groups;
         const int b0 = pre ? c.begin[e] : e - a.groups, m = (pre ? members(c, e) : 1) * a.per_kv, mt = query_items(m);
         s.n = c.len[e];
-        const uint32_t tiles = (uint32_t)((s.n + kPaTile - 1) / kPaTile), item = at / tiles;   // (key head, then query rows)
+        const uint32_t tiles = (uint32_t)((s.n + TILE - 1) / TILE), item = at / tiles;   // (key head, then query rows)
         s.head = mt == 1 ? (int)item : (int)item / mt;
         const int q = (int)item - s.head * mt;
         s.row0 = b0 * a.per_kv + q * kPaQueries;
@@ -157,7 +159,8 @@ __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
 prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
     constexpr int KS = 4 * NSUB;                                   // 16-element steps over a row
-    constexpr uint32_t kSub = kPaTile * 128, kHalf = NSUB * kSub;  // bytes: a sub-tile; K (or V) of a tile
+    constexpr int TILE = tile_rows(NSUB), NB = TILE / 64;          // blocks of 16 cached rows that a warp has in hand at a time
+    constexpr uint32_t kSub = TILE * 128, kHalf = NSUB * kSub;  // bytes: a sub-tile; K (or V) of a tile
     constexpr int DP = 64 * NSUB;                                  // floats of a state row
     constexpr float kBias = WeightBias<T>::value;
     extern __shared__ unsigned char pa_smem[];
@@ -196,7 +199,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     for (int e = e0; e < e1; ++e) {
         const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;
         c.plan[e] = mine;
-        if (e >= a.groups || m <= a.wide_above) mine += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + kPaTile - 1) / kPaTile);
+        if (e >= a.groups || m <= a.wide_above) mine += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
     }
     uint32_t incl = mine;
 #pragma unroll
@@ -209,7 +212,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     if (tid == 0) c.plan[entries] = total;
     __syncthreads();
     const Cut cut(total, (uint32_t)a.resident);
-    Walk walk;
+    Walk<TILE> walk;
     walk.begin(a, c, cut, blockIdx.x);
     Segment s;
     // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp asks for the next
@@ -229,7 +232,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         const uint32_t share = max(cut.runs, 1u);
         for (int b = (uint32_t)run < share ? run + lane * (int)share : a.batch; b < a.batch; b += 32 * (int)share) {
             // the batch row's own units, and its group's: the last group that begins at or before it
-            uint4 own_part = make_uint4(c.plan[a.groups + b], (uint32_t)(c.len[a.groups + b] + kPaTile - 1) / kPaTile, 0u, 0u), group = make_uint4(0u, 0u, 0u, 0u);
+            uint4 own_part = make_uint4(c.plan[a.groups + b], (uint32_t)(c.len[a.groups + b] + TILE - 1) / TILE, 0u, 0u), group = make_uint4(0u, 0u, 0u, 0u);
             int lo = -1, hi = a.groups - 1;
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
@@ -237,7 +240,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 else hi = mid - 1;
             }
             if (lo >= 0 && b < c.begin[lo + 1]) {
-                const int m = members(c, lo) * a.per_kv, tile = m > a.wide_above ? kWideTile : kPaTile;
+                const int m = members(c, lo) * a.per_kv, tile = m > a.wide_above ? kWideTile : TILE;
                 group = make_uint4(c.plan[lo], (uint32_t)(c.len[lo] + tile - 1) / tile, (uint32_t)c.begin[lo], (uint32_t)m);
                 own_part.z = (uint32_t)lo;
             }
@@ -273,29 +276,25 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     if (warp == kPaWarps) {                                        // ---- the copying warp ----
         int stage = 0;
         uint32_t phase = 0;
+        const int page_shift = (a.page_rows & (a.page_rows - 1)) == 0 ? 31 - __clz(a.page_rows) : -1;
+        const auto page_of = [&](int row) { return page_shift >= 0 ? row >> page_shift : row / a.page_rows; };
         begin_run(blockIdx.x);
         while (advance(s, true) == kSegment) {
             // page ids are read 32 at a time, a lane each
-            const int last_page = (s.n - 1) / a.page_rows;
+            const int last_page = page_of(s.n - 1);
             int window = -64, ids = 0;
             for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
-                if (!mbar_wait_bounded(empty + 8 * stage, phase ^ 1u, limit)) {
-                    limit = kCopySpinAfterTimeout;
-                    if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
-                }
-                const int rows = min(kPaTile, s.n - t * kPaTile), boxes = (rows + a.box_rows - 1) / a.box_rows;
-                if (lane == 0) mbar_expect_tx(full + 8 * stage, (uint32_t)(boxes * a.box_rows) * 128u * 2u * NSUB);
-                __syncwarp();
-                const uint32_t k_dst = ring + stage * 2 * kHalf;
-                const int page0 = t * kPaTile / a.page_rows, page1 = (t * kPaTile + rows - 1) / a.page_rows;
+                const int rows = min(TILE, s.n - t * TILE), boxes = (rows + a.box_rows - 1) / a.box_rows;
+                const int page0 = page_of(t * TILE), page1 = page_of(t * TILE + rows - 1);
                 if (page1 >= window + 32) {
                     window = page0;
                     ids = window + lane <= last_page ? s.pages[window + lane] : 0;
                 }
+                const uint32_t k_dst = ring + stage * 2 * kHalf;
+                bool waited = false;
                 for (int i0 = 0; i0 < boxes; i0 += 32) {
-                    const int i = i0 + lane, row = t * kPaTile + min(i, boxes - 1) * a.box_rows, pg = row / a.page_rows;
+                    const int i = i0 + lane, row = t * TILE + min(i, boxes - 1) * a.box_rows, pg = page_of(row);
                     int page = __shfl_sync(0xffffffffu, ids, (pg - window) & 31);
-                    if (i >= boxes) continue;
                     if (pg - window >= 32) page = s.pages[pg];     // a tile of more than 32 pages
                     if (page < 0 || page >= a.n_pages) {           // (the row's result is then unspecified)
                         page = 0;
@@ -303,10 +302,21 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                     }
                     const int y = (page * a.kv_heads + s.head) * a.page_rows + row - pg * a.page_rows;
                     const uint32_t dst = k_dst + (uint32_t)(i * a.box_rows) * 128u;
+                    if (!waited) {                                 // the addresses are ready when the stage is
+                        waited = true;
+                        if (!mbar_wait_bounded(empty + 8 * stage, phase ^ 1u, limit)) {
+                            limit = kCopySpinAfterTimeout;
+                            if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+                        }
+                        if (lane == 0) mbar_expect_tx(full + 8 * stage, (uint32_t)(boxes * a.box_rows) * 128u * 2u * NSUB);
+                        __syncwarp();
+                    }
+                    if (i < boxes) {
 #pragma unroll
-                    for (int c = 0; c < NSUB; ++c) {
-                        pa_tma(dst + c * kSub, &k_map, c * 64, y, full + 8 * stage);
-                        pa_tma(dst + kHalf + c * kSub, &v_map, c * 64, y, full + 8 * stage);
+                        for (int c = 0; c < NSUB; ++c) {
+                            pa_tma(dst + c * kSub, &k_map, c * 64, y, full + 8 * stage);
+                            pa_tma(dst + kHalf + c * kSub, &v_map, c * 64, y, full + 8 * stage);
+                        }
                     }
                 }
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -361,26 +371,36 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
             }
             const uint32_t ks_u32 = ring + stage * 2 * kHalf, vs_u32 = ks_u32 + kHalf;
-            const int valid = min(kPaTile, s.n - t * kPaTile);
-            for (int c0 = kb * 16; c0 < valid; c0 += wk * 16) {     // sixteen cached rows
-                const bool tail = c0 + 16 > valid;
+            const int valid = min(TILE, s.n - t * TILE);
+            for (int c0 = kb * 16 * NB; c0 < valid; c0 += wk * 16 * NB) {   // NB times sixteen cached rows
+                const bool tail = c0 + 16 * NB > valid;
                 const uint32_t v_at = vs_u32 + (uint32_t)c0 * 128u + v_row;
-                float sc[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};   // two chains of products
+                float sc[NB][4];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    uint32_t kf[4];
-                    pa_ldsm(ks_u32 + (uint32_t)c0 * 128u + (ks >> 2) * kSub + k_row + ((((2 * ks + k_ch) & 7) ^ lr) << 4), kf);
-                    if (ks & 1) pa_mma<T>(s2, kf, qa[ks][0], qa[ks][1]);
-                    else pa_mma<T>(sc, kf, qa[ks][0], qa[ks][1]);
+                for (int n = 0; n < NB; ++n) {
+                    float s2[4] = {0.f, 0.f, 0.f, 0.f};              // two chains of products
+                    sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        uint32_t kf[4];
+                        pa_ldsm(ks_u32 + (uint32_t)(c0 + 16 * n) * 128u + (ks >> 2) * kSub + k_row + ((((2 * ks + k_ch) & 7) ^ lr) << 4), kf);
+                        if (ks & 1) pa_mma<T>(s2, kf, qa[ks][0], qa[ks][1]);
+                        else pa_mma<T>(sc[n], kf, qa[ks][0], qa[ks][1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[n][i] += s2[i];
                 }
+                float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[i] += s2[i];
-                if (tail) {
-                    if (c0 + g >= valid) sc[0] = sc[1] = -INFINITY;
-                    if (c0 + g + 8 >= valid) sc[2] = sc[3] = -INFINITY;
+                for (int n = 0; n < NB; ++n) {
+                    if (tail) {
+                        if (c0 + 16 * n + g >= valid) sc[n][0] = sc[n][1] = -INFINITY;
+                        if (c0 + 16 * n + g + 8 >= valid) sc[n][2] = sc[n][3] = -INFINITY;
+                    }
+                    mx[0] = fmaxf(mx[0], fmaxf(sc[n][0], sc[n][2]));
+                    mx[1] = fmaxf(mx[1], fmaxf(sc[n][1], sc[n][3]));
                 }
                 // a new maximum anywhere in the warp: find it over the rows of the block, rescale what was summed
-                float mx[2] = {fmaxf(sc[0], sc[2]), fmaxf(sc[1], sc[3])};
                 if (__any_sync(0xffffffffu, mx[0] > m_run[0] || mx[1] > m_run[1])) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -394,35 +414,46 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                         for (int dp = 0; dp < KS; ++dp) { o[dp][h] *= corr; o[dp][h + 2] *= corr; }
                     }
                 }
-                uint32_t pb[2];
+                uint32_t pb[NB][2];
                 {
-                    float p[4];
+                    float shift[2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float m = m_run[i & 1];
-                        p[i] = pa_exp2(fmaf(sc[i], a.scale_log2e, kBias - (m == -INFINITY ? 0.f : m) * a.scale_log2e));
-                        l_run[i & 1] += p[i];                       // the sum takes the weights before they are rounded
+                    for (int h = 0; h < 2; ++h) shift[h] = kBias - (m_run[h] == -INFINITY ? 0.f : m_run[h]) * a.scale_log2e;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        float p[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            p[i] = pa_exp2(fmaf(sc[n][i], a.scale_log2e, shift[i & 1]));
+                            l_run[i & 1] += p[i];                   // the sum takes the weights before they are rounded
+                        }
+                        pb[n][0] = pa_transpose(pack2<T>(p[0], p[1]));
+                        pb[n][1] = pa_transpose(pack2<T>(p[2], p[3]));
                     }
-                    pb[0] = pa_transpose(pack2<T>(p[0], p[1]));
-                    pb[1] = pa_transpose(pack2<T>(p[2], p[3]));
                 }
                 // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN of V
                 if (!tail) {
 #pragma unroll
-                    for (int dp = 0; dp < KS; ++dp) {
-                        uint32_t vf[4];
-                        pa_ldsm_t(v_at + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
-                        pa_mma<T>(o[dp], vf, pb[0], pb[1]);
+                    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+                        for (int dp = 0; dp < KS; ++dp) {
+                            uint32_t vf[4];
+                            pa_ldsm_t(v_at + n * 2048u + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
+                            pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
+                        }
                     }
                 } else {
-                    const int left = valid - c0 - 2 * t4;           // of the cached rows 2 t4, + 1 and + 8, + 9
-                    const uint32_t lo = left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u, hi = left >= 10 ? 0xffffffffu : left == 9 ? 0xffffu : 0u;
 #pragma unroll
-                    for (int dp = 0; dp < KS; ++dp) {
-                        uint32_t vf[4];
-                        pa_ldsm_t(v_at + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
-                        vf[0] &= lo; vf[1] &= lo; vf[2] &= hi; vf[3] &= hi;
-                        pa_mma<T>(o[dp], vf, pb[0], pb[1]);
+                    for (int n = 0; n < NB; ++n) {
+                        const int left = valid - c0 - 16 * n - 2 * t4;   // of the cached rows 2 t4, + 1 and + 8, + 9
+                        const uint32_t lo = left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u, hi = left >= 10 ? 0xffffffffu : left == 9 ? 0xffffu : 0u;
+#pragma unroll
+                        for (int dp = 0; dp < KS; ++dp) {
+                            uint32_t vf[4];
+                            pa_ldsm_t(v_at + n * 2048u + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
+                            vf[0] &= lo; vf[1] &= lo; vf[2] &= hi; vf[3] &= hi;
+                            pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
+                        }
                     }
                 }
             }
@@ -651,7 +682,7 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
 template <typename T, int NSUB, int STAGES>
 cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
 {
-    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * kPaTile * 128 + (size_t)(2 * a.batch + 3 * a.groups + 2) * 4;
+    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128 + (size_t)(2 * a.batch + 3 * a.groups + 2) * 4;
     const auto kern = prefix_sweep_kernel<T, NSUB, STAGES>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
@@ -665,7 +696,7 @@ cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, unsigned runs, con
                                float *lse, cudaStream_t st)
 {
     switch (nsub) {                          // 96 KB of tiles in flight per block, two blocks per SM; wide rows: one block
-    case 1: return launch_prefix<T, 1, 6>(a, runs, km, vm, out, out_f32, lse, st);
+    case 1: return launch_prefix<T, 1, 3>(a, runs, km, vm, out, out_f32, lse, st);
     case 2: return launch_prefix<T, 2, 3>(a, runs, km, vm, out, out_f32, lse, st);
     case 3: return launch_prefix<T, 3, 4>(a, runs, km, vm, out, out_f32, lse, st);
     default: return launch_prefix<T, 4, 3>(a, runs, km, vm, out, out_f32, lse, st);
@@ -704,9 +735,9 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
         return ADSA_EINVAL;
     if ((long long)max_pages * kv->page_rows > 0x7fffffc0LL || (long long)max_prefix_pages * kv->page_rows > 0x7fffffc0LL) return ADSA_EINVAL;
     // the units of a call are counted in 32 bits
-    const double own_units = (double)batch * kv->n_kv_heads * 2 * ((double)max_pages * kv->page_rows / kPaTile + 1);
+    const double own_units = (double)batch * kv->n_kv_heads * 2 * ((double)max_pages * kv->page_rows / tile_rows(l.nsub) + 1);
     const double p_units = ((double)batch * (n_heads / kv->n_kv_heads) / kPaQueries + n_groups) * kv->n_kv_heads *
-                           ((double)max_prefix_pages * kv->page_rows / kPaTile + 1);
+                           ((double)max_prefix_pages * kv->page_rows / tile_rows(l.nsub) + 1);
     if (own_units + (n_groups ? p_units : 0) > 4e9) return ADSA_EINVAL;
     if (workspace_bytes < l.bytes) return ADSA_ENOMEM;
     int box = 64;
