@@ -435,7 +435,8 @@ typedef enum { ADSA_BF16 = 0, ADSA_F16 = 1, ADSA_F32 = 2 } adsa_dtype;
 /* A paged pool of whole tokens: k_pool, v_pool [n_pages][n_kv_heads][page_rows][row_stride], 16-byte aligned.  Logical
  * row r of a sequence with page table t lies in page t[r / page_rows], row r % page_rows.  row_stride is a multiple of
  * 8; elements past head_dim are padding, which the append writes as zero and the attention does not read.  Any
- * page_rows works; the attention copies boxes of the largest power of two (up to 64 rows) that divides it. */
+ * page_rows works; the attention is quickest where a page is a multiple of 64 rows (of 16 at least), or row_stride an odd
+ * multiple of 8. */
 typedef struct {
     void *k_pool, *v_pool;
     int32_t dtype;                    /* ADSA_BF16 or ADSA_F16 */

@@ -14,14 +14,14 @@ constexpr int kWideQueries = 128;           // query rows of an item of the wide
 constexpr int kWideTile = 128;              // cached rows of a unit of the wide kernel
 
 struct PrefixArgs {
-    const void *q;
+    const void *q, *k_pool, *v_pool;
     long long q_row, q_head;                // element strides of q
     const int32_t *table, *n_rows;          // [batch][max_pages], [batch]
     const int32_t *p_table, *p_rows, *start;   // [groups][max_p_pages], [groups], [groups + 1]
     uint32_t *status;
     int batch, groups, kv_heads, per_kv;    // per_kv: query heads of a key head
     int max_pages, max_p_pages, page_rows, n_pages, box_rows;
-    int d;
+    int d, row_stride;
     float scale_log2e;
     // workspace
     uint4 *plan;                            // [1 + 2 batch] for the merge: number of units; two words of four per batch row

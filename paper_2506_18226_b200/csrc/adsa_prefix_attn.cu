@@ -154,7 +154,11 @@ __device__ __forceinline__ int pa_answer(uint32_t answer)
 }
 
 // NSUB: 64-element sub-tiles of a row (head elements / 64, rounded up).  STAGES: tiles in flight per block.
-template <typename T, int NSUB, int STAGES>
+// PACKED: the rows of a page are copied as they lie, one bulk copy per page, instead of 64-element columns in the
+// 128-byte swizzle.  Rows whose 16-byte pieces are odd in number put the eight rows of an ldmatrix on eight different
+// banks without a swizzle, and such rows straddle memory sectors when they are fetched column by column: with 208-byte rows
+// the columns ran at 4.4 TB/s where 256-byte rows run at 6.2.
+template <typename T, int NSUB, int STAGES, bool PACKED>
 __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
 prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
@@ -167,7 +171,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     __shared__ uint64_t bars[2 * STAGES + 4];
     __shared__ __align__(16) uint4 answers[2];
     __shared__ uint32_t warp_sums[kPaThreads / 32];
-    const uint32_t ring = (smem_u32(pa_smem) + 1023u) & ~1023u;
+    const uint32_t ring = (smem_u32(pa_smem) + 1023u) & ~1023u, pitch = PACKED ? (uint32_t)a.row_stride * 2u : 128u;
     Shared c;
     c.plan = reinterpret_cast<uint32_t *>(pa_smem + (ring - smem_u32(pa_smem)) + (size_t)STAGES * 2 * kHalf);
     c.len = reinterpret_cast<int *>(c.plan + a.groups + a.batch + 1);
@@ -284,16 +288,17 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             const int last_page = page_of(s.n - 1);
             int window = -64, ids = 0;
             for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
-                const int rows = min(TILE, s.n - t * TILE), boxes = (rows + a.box_rows - 1) / a.box_rows;
-                const int page0 = page_of(t * TILE), page1 = page_of(t * TILE + rows - 1);
+                const int rows = min(TILE, s.n - t * TILE), page0 = page_of(t * TILE), page1 = page_of(t * TILE + rows - 1);
+                const int pieces = PACKED ? page1 - page0 + 1 : (rows + a.box_rows - 1) / a.box_rows;
                 if (page1 >= window + 32) {
                     window = page0;
                     ids = window + lane <= last_page ? s.pages[window + lane] : 0;
                 }
                 const uint32_t k_dst = ring + stage * 2 * kHalf;
                 bool waited = false;
-                for (int i0 = 0; i0 < boxes; i0 += 32) {
-                    const int i = i0 + lane, row = t * TILE + min(i, boxes - 1) * a.box_rows, pg = page_of(row);
+                for (int i0 = 0; i0 < pieces; i0 += 32) {
+                    const int i = min(i0 + lane, pieces - 1), row = PACKED ? max(t * TILE, (page0 + i) * a.page_rows) : t * TILE + i * a.box_rows;
+                    const int pg = PACKED ? page0 + i : page_of(row);
                     int page = __shfl_sync(0xffffffffu, ids, (pg - window) & 31);
                     if (pg - window >= 32) page = s.pages[pg];     // a tile of more than 32 pages
                     if (page < 0 || page >= a.n_pages) {           // (the row's result is then unspecified)
@@ -301,21 +306,27 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                         if (a.status) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
                     }
                     const int y = (page * a.kv_heads + s.head) * a.page_rows + row - pg * a.page_rows;
-                    const uint32_t dst = k_dst + (uint32_t)(i * a.box_rows) * 128u;
+                    const uint32_t dst = k_dst + (uint32_t)(row - t * TILE) * (PACKED ? pitch : 128u);
                     if (!waited) {                                 // the addresses are ready when the stage is
                         waited = true;
                         if (!mbar_wait_bounded(empty + 8 * stage, phase ^ 1u, limit)) {
                             limit = kCopySpinAfterTimeout;
                             if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
                         }
-                        if (lane == 0) mbar_expect_tx(full + 8 * stage, (uint32_t)(boxes * a.box_rows) * 128u * 2u * NSUB);
+                        if (lane == 0) mbar_expect_tx(full + 8 * stage, PACKED ? (uint32_t)rows * pitch * 2u : (uint32_t)(pieces * a.box_rows) * 128u * 2u * NSUB);
                         __syncwarp();
                     }
-                    if (i < boxes) {
+                    if (i0 + lane < pieces) {
+                        if constexpr (PACKED) {
+                            const uint32_t bytes = (uint32_t)(min((pg + 1) * a.page_rows, t * TILE + rows) - row) * pitch;
+                            bulk_g2s(dst, (const unsigned char *)a.k_pool + (size_t)y * pitch, bytes, full + 8 * stage);
+                            bulk_g2s(dst + kHalf, (const unsigned char *)a.v_pool + (size_t)y * pitch, bytes, full + 8 * stage);
+                        } else {
 #pragma unroll
-                        for (int c = 0; c < NSUB; ++c) {
-                            pa_tma(dst + c * kSub, &k_map, c * 64, y, full + 8 * stage);
-                            pa_tma(dst + kHalf + c * kSub, &v_map, c * 64, y, full + 8 * stage);
+                            for (int c = 0; c < NSUB; ++c) {
+                                pa_tma(dst + c * kSub, &k_map, c * 64, y, full + 8 * stage);
+                                pa_tma(dst + kHalf + c * kSub, &v_map, c * 64, y, full + 8 * stage);
+                            }
                         }
                     }
                 }
@@ -329,8 +340,12 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     // ---- the computing warps ----
     const int g = lane >> 2, t4 = lane & 3, mi = lane >> 3, lr = lane & 7;
     // lane's row address in a 16-row block for K (as A: cached rows x elements) and V (transposed: elements x cached rows)
-    const uint32_t k_row = (uint32_t)((mi & 1) * 8 + lr) * 128u, v_row = (uint32_t)((mi >> 1) * 8 + lr) * 128u;
+    const uint32_t k_row = (uint32_t)((mi & 1) * 8 + lr) * pitch, v_row = (uint32_t)((mi >> 1) * 8 + lr) * pitch;
     const int k_ch = mi >> 1, v_ch = mi & 1;
+    // byte offset of 16-byte piece 2 step + half of a row
+    const auto piece_at = [&](int step, int half) {
+        return PACKED ? (uint32_t)(32 * step + 16 * half) : (uint32_t)(step >> 2) * kSub + (uint32_t)((((2 * step + half) & 7) ^ lr) << 4);
+    };
     int stage = 0;
     uint32_t phase = 0;
     // Q^T as the B operand: query row g of this warp's eight, elements 16 ks + 2 t4, + 1 and + 8, + 9; asked for one segment ahead
@@ -374,7 +389,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             const int valid = min(TILE, s.n - t * TILE);
             for (int c0 = kb * 16 * NB; c0 < valid; c0 += wk * 16 * NB) {   // NB times sixteen cached rows
                 const bool tail = c0 + 16 * NB > valid;
-                const uint32_t v_at = vs_u32 + (uint32_t)c0 * 128u + v_row;
+                const uint32_t v_at = vs_u32 + (uint32_t)c0 * pitch + v_row;
                 float sc[NB][4];
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
@@ -382,8 +397,13 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                     sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
+                        if (PACKED && ks >= KS - 4 && 16 * ks >= a.d) break;
                         uint32_t kf[4];
-                        pa_ldsm(ks_u32 + (uint32_t)(c0 + 16 * n) * 128u + (ks >> 2) * kSub + k_row + ((((2 * ks + k_ch) & 7) ^ lr) << 4), kf);
+                        pa_ldsm(ks_u32 + (uint32_t)(c0 + 16 * n) * pitch + k_row + piece_at(ks, k_ch), kf);
+                        if (PACKED && ks >= KS - 4 && 16 * ks + 16 > a.d) {   // padding and the next row: not part of this one
+                            if (16 * ks + 2 * t4 >= a.d) kf[0] = kf[1] = 0u;
+                            if (16 * ks + 8 + 2 * t4 >= a.d) kf[2] = kf[3] = 0u;
+                        }
                         if (ks & 1) pa_mma<T>(s2, kf, qa[ks][0], qa[ks][1]);
                         else pa_mma<T>(sc[n], kf, qa[ks][0], qa[ks][1]);
                     }
@@ -437,8 +457,9 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                     for (int n = 0; n < NB; ++n) {
 #pragma unroll
                         for (int dp = 0; dp < KS; ++dp) {
+                            if (PACKED && dp >= KS - 4 && 16 * dp >= a.d) break;   // (rows of O past the head elements are not kept)
                             uint32_t vf[4];
-                            pa_ldsm_t(v_at + n * 2048u + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
+                            pa_ldsm_t(v_at + n * 16u * pitch + piece_at(dp, v_ch), vf);
                             pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
                         }
                     }
@@ -449,8 +470,9 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                         const uint32_t lo = left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u, hi = left >= 10 ? 0xffffffffu : left == 9 ? 0xffffu : 0u;
 #pragma unroll
                         for (int dp = 0; dp < KS; ++dp) {
+                            if (PACKED && dp >= KS - 4 && 16 * dp >= a.d) break;   // (rows of O past the head elements are not kept)
                             uint32_t vf[4];
-                            pa_ldsm_t(v_at + n * 2048u + (dp >> 2) * kSub + ((((2 * dp + v_ch) & 7) ^ lr) << 4), vf);
+                            pa_ldsm_t(v_at + n * 16u * pitch + piece_at(dp, v_ch), vf);
                             vf[0] &= lo; vf[1] &= lo; vf[2] &= hi; vf[3] &= hi;
                             pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
                         }
@@ -679,11 +701,11 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int NSUB, int STAGES>
+template <typename T, int NSUB, int STAGES, bool PACKED>
 cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
 {
     const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128 + (size_t)(2 * a.batch + 3 * a.groups + 2) * 4;
-    const auto kern = prefix_sweep_kernel<T, NSUB, STAGES>;
+    const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     e = launch_pdl(kern, dim3(runs), kPaThreads, smem, st, a, km, vm);
@@ -695,12 +717,18 @@ template <typename T>
 cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
                                float *lse, cudaStream_t st)
 {
-    switch (nsub) {                          // 96 KB of tiles in flight per block, two blocks per SM; wide rows: one block
-    case 1: return launch_prefix<T, 1, 3>(a, runs, km, vm, out, out_f32, lse, st);
-    case 2: return launch_prefix<T, 2, 3>(a, runs, km, vm, out, out_f32, lse, st);
-    case 3: return launch_prefix<T, 3, 4>(a, runs, km, vm, out, out_f32, lse, st);
-    default: return launch_prefix<T, 4, 3>(a, runs, km, vm, out, out_f32, lse, st);
+    // 96 KB of tiles in flight per block and two blocks per SM; wide rows: 192 KB and one block
+    const bool packed = a.row_stride / 8 % 2 != 0 && a.row_stride <= 64 * nsub;   // (a stage holds rows of 64 nsub elements)
+#define ADSA_PREFIX(NSUB, STAGES) \
+    return packed ? launch_prefix<T, NSUB, STAGES, true>(a, runs, km, vm, out, out_f32, lse, st) \
+                  : launch_prefix<T, NSUB, STAGES, false>(a, runs, km, vm, out, out_f32, lse, st)
+    switch (nsub) {
+    case 1: ADSA_PREFIX(1, 3);
+    case 2: ADSA_PREFIX(2, 3);
+    case 3: ADSA_PREFIX(3, 4);
+    default: ADSA_PREFIX(4, 3);
     }
+#undef ADSA_PREFIX
 }
 
 }  // namespace
@@ -751,7 +779,7 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.status = status;
     a.batch = batch; a.groups = n_groups; a.kv_heads = kv->n_kv_heads; a.per_kv = n_heads / kv->n_kv_heads;
     a.max_pages = max_pages; a.max_p_pages = max_prefix_pages; a.page_rows = kv->page_rows; a.n_pages = kv->n_pages; a.box_rows = box;
-    a.d = kv->head_dim;
+    a.d = kv->head_dim; a.row_stride = kv->row_stride; a.k_pool = kv->k_pool; a.v_pool = kv->v_pool;
     const float scale = softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale;
     a.scale_log2e = scale * 1.44269504088896341f;
     a.plan = (uint4 *)(ws + l.plan);
