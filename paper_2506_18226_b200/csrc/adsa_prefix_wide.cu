@@ -92,22 +92,6 @@ __device__ __forceinline__ uint32_t tc_shape(int n, bool transposed)
     return (1u << 4) | (type << 7) | (type << 10) | (transposed ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// two 32-bit operations in one instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<uint64_t &>(d))
-        : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
-    return d;
-}
-
 // Half-type weights carry a factor of 2^6 (up to 2^14 with the slack), so that small ones keep their precision.
 template <typename T> struct WideBias { static constexpr float value = 0.f; };
 template <> struct WideBias<__half> { static constexpr float value = 6.f; };

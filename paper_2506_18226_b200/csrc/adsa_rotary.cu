@@ -6,9 +6,11 @@
 // of a turn of error) handed to sincospif in 32 bits.  A position of a million times a frequency of one would keep only
 // four bits of its turn's fraction in 32 bits.
 //
-// Both operators move every byte once, so HBM bounds them; the sines are what could cost more.  A thread owns a few
-// pairs of ONE token and walks the heads with them: one sine and cosine per pair and token, whatever the number of
-// heads, and the accesses of a warp stay whole 128-byte lines (the units of a head lie side by side).
+// Both operators move every byte once, so HBM bounds them.  A block takes a few tokens: it asks for its first elements,
+// makes one table of sines and cosines per token in shared memory (once, whatever the number of heads), and then walks
+// the tokens' heads in the order they lie in memory, 16 bytes per thread and access.  (A first version gave a thread the
+// pairs of one token and walked the heads from there, sines in registers: every access of a warp was whole lines, but
+// 256 bytes here and 256 there; 18432 tokens x 32 heads x 128 elements took 89 us.)
 #include <math.h>
 
 #include "adsa_half.cuh"
@@ -17,6 +19,7 @@ namespace adsa {
 
 constexpr int kTurnThreads = 256;
 constexpr int kTurnMaxPairs = ADSA_MAX_HEAD_DIM / 2;
+constexpr int kTurnMaxTokens = 16;         // tokens of a block
 
 struct TurnRows {            // rows of one tensor, element strides
     const void *src;
@@ -33,7 +36,8 @@ struct TurnArgs {
     long long tokens;
     int per_row;             // tokens per batch row where cu_tokens is null
     int batch, max_pages, n_pages, page_rows, row_stride;
-    int head_chunk;          // heads a block walks
+    int tokens_block;        // tokens a block takes
+    int head_chunk;          // heads it walks (blockIdx.y: which)
     int d, n, n_axes;        // head elements, rotated pairs, axes
     int rot_units, units;    // units of a head that turn (halves only), all of them
 };
@@ -50,140 +54,198 @@ __device__ __forceinline__ int find_row(const int32_t *cu, int batch, long long 
     return lo;
 }
 
-template <typename T, int ACC, bool HALVES, bool ROTATE>
-__device__ __forceinline__ void turn_heads(const T *src, T *dst, long long src_head, long long dst_head, int count, int e0, int e1,
-                                           const float (&cs)[ACC], const float (&sn)[ACC], int turned)
-{
+// A unit of a head is ACC neighbouring elements (pairs side by side; with ACC = 1 a pair is two accesses), or ACC
+// elements and their partners half a rotation further on.  The table holds, for the pairs of a unit two by two, their
+// cosines and sines {c, c', s, s'}: entry [two][unit], so that neighbouring threads read neighbouring 16 bytes.
+template <typename T, int ACC, bool HALVES>
+struct Piece {
     typedef Pack<T, ACC> P;
-#pragma unroll 4
-    for (int h = 0; h < count; ++h) {
-        const T *s = src + h * src_head;
-        T *o = dst + h * dst_head;
-        P a = *reinterpret_cast<const P *>(s + e0);
-        if constexpr (HALVES || ACC == 1) {        // a second access: the partner elements (e1 < 0: a lone copied piece)
-            if (e1 >= 0) {
-                P b = *reinterpret_cast<const P *>(s + e1);
-                if (ROTATE) {
+    static constexpr bool kTwo = HALVES || ACC == 1;               // two accesses
+    static constexpr int kPairs = kTwo ? ACC : ACC / 2;            // pairs of a unit
+    static constexpr int kTwos = (kPairs + 1) / 2;
+    P a, b;
+    T *dst;                                                        // null: nothing to do
+    int partner;                                                   // elements to the second access; 0: none
+    int at;                                                        // table entry; -1: copied as it is
+    int turned;                                                    // pairs of the unit that turn
+
+    __device__ __forceinline__ void load(const T *src)
+    {
+        a = *reinterpret_cast<const P *>(src);
+        if constexpr (kTwo)
+            if (partner) b = *reinterpret_cast<const P *>(src + partner);
+    }
+    __device__ __forceinline__ void turn(const float4 *table, int units)
+    {
+        if (at < 0) return;
+        if (ACC > 1 && turned == kPairs) {
+            uint32_t *wa = reinterpret_cast<uint32_t *>(&a), *wb = reinterpret_cast<uint32_t *>(&b);
 #pragma unroll
-                    for (int i = 0; i < ACC; ++i) {
-                        if (i >= turned) break;
-                        const float x = to_f32(a.e[i]), y = to_f32(b.e[i]);
-                        a.e[i] = from_f32<T>(x * cs[i] - y * sn[i]);
-                        b.e[i] = from_f32<T>(x * sn[i] + y * cs[i]);
+            for (int i = 0; i < kTwos; ++i) {
+                const float4 t = table[at + i * units];
+                if constexpr (HALVES) {
+                    const float2 c = make_float2(t.x, t.y), s = make_float2(t.z, t.w), x = unpack2<T>(wa[i]), y = unpack2<T>(wb[i]);
+                    const float2 u = fma2(x, c, mul2(y, make_float2(-s.x, -s.y))), v = fma2(x, s, mul2(y, c));
+                    wa[i] = pack2<T>(u.x, u.y);
+                    wb[i] = pack2<T>(v.x, v.y);
+                } else {
+                    const float2 x = unpack2<T>(wa[2 * i]);
+                    wa[2 * i] = pack2<T>(x.x * t.x - x.y * t.z, x.x * t.z + x.y * t.x);
+                    if (2 * i + 1 < kPairs) {
+                        const float2 y = unpack2<T>(wa[2 * i + 1]);
+                        wa[2 * i + 1] = pack2<T>(y.x * t.y - y.y * t.w, y.x * t.w + y.y * t.y);
                     }
                 }
-                *reinterpret_cast<P *>(o + e1) = b;
             }
-        } else if (ROTATE) {
+        } else {                                                   // single elements, or a unit where the rotation ends
 #pragma unroll
-            for (int i = 0; i < ACC / 2; ++i) {
+            for (int i = 0; i < kPairs; ++i) {
                 if (i < turned) {
-                    const float x = to_f32(a.e[2 * i]), y = to_f32(a.e[2 * i + 1]);
-                    a.e[2 * i] = from_f32<T>(x * cs[i] - y * sn[i]);
-                    a.e[2 * i + 1] = from_f32<T>(x * sn[i] + y * cs[i]);
+                    const float4 t = table[at + (i >> 1) * units];
+                    const float c = i & 1 ? t.y : t.x, s = i & 1 ? t.w : t.z;
+                    T *pa = kTwo ? &a.e[i] : &a.e[2 * i], *pb = kTwo ? &b.e[i] : &a.e[2 * i + 1];
+                    const float x = to_f32(*pa), y = to_f32(*pb);
+                    *pa = from_f32<T>(x * c - y * s);
+                    *pb = from_f32<T>(x * s + y * c);
                 }
             }
         }
-        *reinterpret_cast<P *>(o + e0) = a;
     }
-}
+    __device__ __forceinline__ void store()
+    {
+        *reinterpret_cast<P *>(dst) = a;
+        if constexpr (kTwo)
+            if (partner) *reinterpret_cast<P *>(dst + partner) = b;
+    }
+};
 
-// A unit of a head is ACC neighbouring elements (pairs side by side; with ACC = 1 a pair is two accesses), or ACC
-// elements and their partners half a rotation further on.  blockIdx.y: a chunk of the q, k and v heads taken as one list.
+// blockIdx.x: tokens; blockIdx.y: a chunk of the q, k and v heads taken as one list
 template <typename T, int ACC, bool HALVES>
 __global__ void __launch_bounds__(kTurnThreads)
 turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ adsa_rotary rot)
 {
+    typedef Piece<T, ACC, HALVES> PieceT;
+    extern __shared__ float4 table[];                              // [tokens][twos of a unit][units]
+    __shared__ int s_row[kTurnMaxTokens], s_page[kTurnMaxTokens];  // row in its page (-1: not placed, -2: padding), page
+    const long long t0 = (long long)blockIdx.x * a.tokens_block;
+    const int tokens = (int)min((long long)a.tokens_block, a.tokens - t0);
+    const int h0 = blockIdx.y * a.head_chunk, heads = min(a.head_chunk, a.q.heads + a.k.heads + a.v.heads - h0);
+    const int k_first = a.q.heads, v_first = a.q.heads + a.k.heads;
+    const int pieces = tokens * heads * a.units;
     pdl_wait();
     pdl_launch();
-    const long long idx = (long long)blockIdx.x * kTurnThreads + threadIdx.x;
-    long long t;
-    int u;
-    if (a.tokens * a.units <= 0x7fffffffLL) { t = (uint32_t)idx / (uint32_t)a.units; u = (int)((uint32_t)idx - (uint32_t)t * (uint32_t)a.units); }
-    else { t = idx / a.units; u = (int)(idx - t * a.units); }
-    if (t >= a.tokens) return;
 
-    // where the token's rows go
-    long long cache_row = -1;            // ((page * heads) * page_rows + row) without the head, in rows
-    int page = 0;
+    // where the tokens' rows go
     if (a.page_table) {
-        int b, j;
-        if (a.cu_tokens) {
-            b = find_row(a.cu_tokens, a.batch, t);
-            if (b >= a.batch || t < a.cu_tokens[b] || t >= a.cu_tokens[b + 1]) return;   // padding behind or before the rows
-            j = (int)(t - a.cu_tokens[b]);
-        } else {
-            b = (int)(t / a.per_row);
-            j = (int)(t - (long long)b * a.per_row);
-        }
-        const long long row = (long long)a.n_rows[b] + j;
-        const long long pg = row / a.page_rows;
-        if (a.n_rows[b] < 0 || pg >= a.max_pages) {
-            if (a.status && u == 0 && blockIdx.y == 0) atomicOr(a.status, ADSA_DEV_ROW_OVERFLOW);
-        } else {
-            page = a.page_table[(size_t)b * a.max_pages + pg];
-            if (page < 0 || page >= a.n_pages) {
-                if (a.status && u == 0 && blockIdx.y == 0) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
+        if (threadIdx.x < tokens) {
+            const long long t = t0 + threadIdx.x;
+            int b, j, row = -2, page = 0;
+            if (a.cu_tokens) {
+                b = find_row(a.cu_tokens, a.batch, t);
+                const bool in = b < a.batch && t >= a.cu_tokens[b] && t < a.cu_tokens[b + 1];
+                j = in ? (int)(t - a.cu_tokens[b]) : -1;
             } else {
-                cache_row = row - pg * a.page_rows;
+                b = (int)(t / a.per_row);
+                j = (int)(t - (long long)b * a.per_row);
             }
-        }
-    }
-
-    // which elements, which pairs
-    int e0, e1 = -1, pair0 = 0, turned = 0;
-    if constexpr (HALVES) {
-        if (u < a.rot_units) { e0 = u * ACC; e1 = e0 + a.n; pair0 = e0; turned = ACC; }
-        else e0 = 2 * a.n + (u - a.rot_units) * ACC;
-    } else if constexpr (ACC == 1) {
-        e0 = 2 * u; e1 = e0 + 1; pair0 = u; turned = u < a.n ? 1 : 0;
-    } else {
-        e0 = u * ACC; pair0 = e0 / 2;
-        turned = a.n - pair0;
-        turned = turned < 0 ? 0 : turned > ACC / 2 ? ACC / 2 : turned;
-    }
-    const int h0 = blockIdx.y * a.head_chunk, h1 = min(h0 + a.head_chunk, a.q.heads + a.k.heads + a.v.heads);
-    const int k_first = a.q.heads, v_first = a.q.heads + a.k.heads;
-    float cs[ACC], sn[ACC];
-    if (h0 < v_first) {                  // (v does not turn)
-#pragma unroll
-        for (int i = 0; i < ACC; ++i) {
-            cs[i] = 1.f; sn[i] = 0.f;
-            if (i < turned) {
-                const double turns = (double)a.pos[t * a.n_axes + rot.axis[pair0 + i]] * rot.turns[pair0 + i];
-                sincospif((float)(2.0 * (turns - rint(turns))), &sn[i], &cs[i]);
+            if (j >= 0) {
+                row = -1;
+                const int first = a.n_rows[b];
+                const long long at = (long long)first + j, pg = at / a.page_rows;
+                if (first < 0 || pg >= a.max_pages) {
+                    if (a.status && blockIdx.y == 0) atomicOr(a.status, ADSA_DEV_ROW_OVERFLOW);
+                } else {
+                    page = a.page_table[(size_t)b * a.max_pages + pg];
+                    if (page < 0 || page >= a.n_pages) {
+                        if (a.status && blockIdx.y == 0) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
+                    } else {
+                        row = (int)(at - pg * a.page_rows);
+                    }
+                }
             }
+            s_row[threadIdx.x] = row;
+            s_page[threadIdx.x] = page;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < ACC; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+        __syncthreads();
     }
-
-    if (h0 < k_first) {
-        const int n = min(h1, k_first) - h0;
-        const T *s = (const T *)a.q.src + t * a.q.src_token + h0 * a.q.src_head;
-        T *o = (T *)a.q.dst + t * a.q.dst_token + h0 * a.q.dst_head;
-        turn_heads<T, ACC, HALVES, true>(s, o, a.q.src_head, a.q.dst_head, n, e0, e1, cs, sn, turned);
-    }
-    if (cache_row < 0) return;
     const long long head_rows = (long long)a.page_rows * a.row_stride;
-    if (h0 < v_first && h1 > k_first) {
-        const int f = max(h0, k_first) - k_first, n = min(h1, v_first) - k_first - f;
-        const T *s = (const T *)a.k.src + t * a.k.src_token + f * a.k.src_head;
-        T *o = (T *)a.k.dst + ((long long)page * a.k.heads + f) * head_rows + cache_row * a.row_stride;
-        turn_heads<T, ACC, HALVES, true>(s, o, a.k.src_head, head_rows, n, e0, e1, cs, sn, turned);
-        if (u == 0)
-            for (int h = 0; h < n; ++h)
-                for (int e = a.d; e < a.row_stride; ++e) o[h * head_rows + e] = from_f32<T>(0.f);
+    const int turn_units = HALVES ? a.rot_units : a.units;         // units of the table
+    // Pieces in the order they lie in memory: this thread's token, head and unit, moved on by the block's threads at a time
+    int u, h, tk;
+    {
+        const int th = (int)threadIdx.x / a.units;
+        u = (int)threadIdx.x - th * a.units;
+        tk = th / heads;
+        h = th - tk * heads;
     }
-    if (h1 > v_first) {
-        const int f = max(h0, v_first) - v_first, n = h1 - v_first - f;
-        const T *s = (const T *)a.v.src + t * a.v.src_token + f * a.v.src_head;
-        T *o = (T *)a.v.dst + ((long long)page * a.v.heads + f) * head_rows + cache_row * a.row_stride;
-        turn_heads<T, ACC, HALVES, false>(s, o, a.v.src_head, head_rows, n, e0, e1, cs, sn, 0);
-        if (u == 0)
-            for (int h = 0; h < n; ++h)
-                for (int e = a.d; e < a.row_stride; ++e) o[h * head_rows + e] = from_f32<T>(0.f);
+    const int step_th = kTurnThreads / a.units, step_u = kTurnThreads - step_th * a.units, step_tk = step_th / heads, step_h = step_th - step_tk * heads;
+    const auto fetch = [&](PieceT &p) {
+        p.dst = nullptr;
+        if (tk < tokens) {
+            int e0, pair0 = 0;
+            p.partner = 0;
+            p.turned = 0;
+            if constexpr (HALVES) {
+                if (u < a.rot_units) { e0 = u * ACC; p.partner = a.n; p.turned = ACC; }
+                else e0 = 2 * a.n + (u - a.rot_units) * ACC;
+            } else if constexpr (ACC == 1) {
+                e0 = 2 * u; p.partner = 1; p.turned = u < a.n ? 1 : 0;
+            } else {
+                e0 = u * ACC; pair0 = e0 / 2;
+                p.turned = max(0, min(a.n - pair0, PieceT::kPairs));
+            }
+            const int row = a.page_table ? s_row[tk] : -1, hh = h + h0;
+            const T *src = nullptr;
+            if (hh < k_first) {
+                if (row != -2) {
+                    src = (const T *)a.q.src + (t0 + tk) * a.q.src_token + hh * a.q.src_head + e0;
+                    p.dst = (T *)a.q.dst + (t0 + tk) * a.q.dst_token + hh * a.q.dst_head + e0;
+                }
+            } else if (row >= 0) {
+                const bool key = hh < v_first;
+                const int kh = hh - (key ? k_first : v_first);
+                if (!key) p.turned = 0;
+                src = (key ? (const T *)a.k.src + (t0 + tk) * a.k.src_token + kh * a.k.src_head
+                           : (const T *)a.v.src + (t0 + tk) * a.v.src_token + kh * a.v.src_head) + e0;
+                p.dst = (T *)(key ? a.k.dst : a.v.dst) + ((long long)s_page[tk] * a.k.heads + kh) * head_rows + (long long)row * a.row_stride + e0;
+                if (u == 0)
+                    for (int e = a.d; e < a.row_stride; ++e) p.dst[e] = from_f32<T>(0.f);
+            }
+            p.at = p.turned > 0 ? tk * PieceT::kTwos * turn_units + u : -1;
+            if (src) p.load(src);
+        }
+        u += step_u; h += step_h; tk += step_tk;
+        if (u >= a.units) { u -= a.units; ++h; }
+        if (h >= heads) { h -= heads; ++tk; }
+    };
+    constexpr int AHEAD = HALVES ? 2 : 4;                          // pieces a thread has in flight
+    PieceT p[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) fetch(p[k]);
+    // the sines and cosines of the tokens, while the first pieces are on their way (v does not turn)
+    if (h0 < v_first && a.n > 0) {
+        float *out = reinterpret_cast<float *>(table);
+        for (int i = threadIdx.x; i < tokens * a.n; i += kTurnThreads) {
+            const int t = i / a.n, pair = i - t * a.n, unit = pair / PieceT::kPairs, in = pair - unit * PieceT::kPairs;
+            const double turns = (double)a.pos[(t0 + t) * a.n_axes + rot.axis[pair]] * rot.turns[pair];
+            float sn, cs;
+            sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
+            float *entry = out + 4 * ((t * PieceT::kTwos + (in >> 1)) * turn_units + unit) + (in & 1);
+            entry[0] = cs;
+            entry[2] = sn;
+        }
+        __syncthreads();
+    }
+    for (int i = 0; i < pieces; i += AHEAD * kTurnThreads) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (p[k].dst) {
+                p[k].turn(table, turn_units);
+                p[k].store();
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) fetch(p[k]);
     }
 }
 
@@ -203,11 +265,11 @@ int fit(int acc, const TurnRows &r)
 }
 
 template <typename T>
-cudaError_t launch_turn(const TurnArgs &a, const adsa_rotary &rot, int acc, bool halves, dim3 grid, cudaStream_t st)
+cudaError_t launch_turn(const TurnArgs &a, const adsa_rotary &rot, int acc, bool halves, dim3 grid, size_t smem, cudaStream_t st)
 {
 #define ADSA_TURN(A) \
-    if (acc == A) return halves ? launch_pdl(turn_kernel<T, A, true>, grid, kTurnThreads, 0, st, a, rot) \
-                                : launch_pdl(turn_kernel<T, A, false>, grid, kTurnThreads, 0, st, a, rot)
+    if (acc == A) return halves ? launch_pdl(turn_kernel<T, A, true>, grid, kTurnThreads, smem, st, a, rot) \
+                                : launch_pdl(turn_kernel<T, A, false>, grid, kTurnThreads, smem, st, a, rot)
     ADSA_TURN(8);
     ADSA_TURN(4);
     ADSA_TURN(2);
@@ -228,16 +290,25 @@ int run_turn(TurnArgs &a, const adsa_rotary &rot, int dtype, cudaStream_t st)
     a.rot_units = halves ? a.n / acc : 0;
     a.units = halves ? a.rot_units + (a.d - 2 * a.n) / acc : acc == 1 ? a.d / 2 : a.d / acc;
     const int heads = a.q.heads + a.k.heads + a.v.heads;
-    const long long blocks = (a.tokens * a.units + kTurnThreads - 1) / kTurnThreads;
+    // Enough blocks for every SM before anything else (fewer heads a block), then about eight pieces a thread (more tokens
+    // a block), so that a table of sines serves many heads.
+    const int per_token = heads * a.units;
+    int tokens = 8 * kTurnThreads / per_token;
+    if (tokens > kTurnMaxTokens) tokens = kTurnMaxTokens;
+    while (tokens > 1 && a.tokens / tokens < 148 * 4) tokens /= 2;
+    if (tokens < 1) tokens = 1;
+    const long long blocks = (a.tokens + tokens - 1) / tokens;
     if (blocks > 0x7fffffffLL) return ADSA_EINVAL;
-    // Few tokens: a block per head, so that the call is one load deep; many: a thread keeps its sines for many heads.
-    // 148 SMs hold eight blocks each.
     int chunk = heads;
-    while (chunk > 1 && blocks * ((heads + chunk - 1) / chunk) < 148 * 8) chunk = (chunk + 1) / 2;
-    if ((heads + chunk - 1) / chunk > 65535) chunk = (heads + 65534) / 65535;
+    while (chunk * a.units > kTurnThreads && (blocks * ((heads + chunk - 1) / chunk) < 148 * 4 || chunk * a.units > 16 * kTurnThreads)) chunk = (chunk + 1) / 2;
+    if ((heads + chunk - 1) / chunk > 65535) return ADSA_EINVAL;
+    a.tokens_block = tokens;
     a.head_chunk = chunk;
+    // table bytes: at most kTurnMaxTokens x 128 pairs x 8 (with one pair a unit half of an entry is not used)
+    const int pairs = halves || acc == 1 ? acc : acc / 2;
+    const size_t smem = (size_t)tokens * ((pairs + 1) / 2) * (halves ? a.rot_units : a.units) * 16;
     const dim3 grid((unsigned)blocks, (unsigned)((heads + chunk - 1) / chunk));
-    const cudaError_t e = dtype == ADSA_BF16 ? launch_turn<__nv_bfloat16>(a, rot, acc, halves, grid, st) : launch_turn<__half>(a, rot, acc, halves, grid, st);
+    const cudaError_t e = dtype == ADSA_BF16 ? launch_turn<__nv_bfloat16>(a, rot, acc, halves, grid, smem, st) : launch_turn<__half>(a, rot, acc, halves, grid, smem, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 

@@ -487,7 +487,8 @@ def norm64(y, x, w_pre, w_post, gate, scale, eps):
 @pytest.mark.parametrize("dtype", HALF)
 @pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("rows,dim,gates", [(1, 8, 0), (32, 1280, 32), (7, 96, 1), (129, 264, 3), (2, 16384, 2), (5, 8200, 0), (1000, 768, 10),
-                                            (3, 4096, 3), (66, 2048, 0)])
+                                            (3, 4096, 3), (66, 2048, 0), (3000, 8, 0), (2400, 1280, 24), (2400, 2056, 1), (2368, 6000, 2),
+                                            (2369, 16384, 1)])
 def test_norm_residual_matches_64_bits(rows, dim, gates, wide, dtype):
     import paper_2506_18226_b200 as A
     g = _gen(rows + dim)
