@@ -467,7 +467,7 @@ ADSA_API int adsa_rope_axes(const adsa_rotary *rot, int dtype, const void *x, lo
 /* New rows into the cache, k turned on the way (and q, in the same launch, if given).
  *   page_table  int32 [batch][max_pages];  n_rows  int32 [batch]: rows of each batch row's sequence before the call
  *   cu_tokens   int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 belong to batch row b; tokens before cu[0] and
- *               from cu[batch] on are padding (nothing is read or written for them).  NULL: n_tokens / batch tokens each
+ *               from cu[batch] on are padding (nothing is written for them).  NULL: n_tokens / batch tokens each
  *   k, v        [n_tokens][n_kv_heads][head_dim];  token j of batch row b becomes logical row n_rows[b] + j
  *   rot, pos    as adsa_rope_axes, rot->head_dim == kv->head_dim; rot NULL: nothing turns and pos is not read
  *   q, q_out    [n_tokens][n_heads][head_dim], turned like k; n_heads 0: none; q_out may be q (same strides)

@@ -6,18 +6,17 @@
 // of a turn of error) handed to sincospif in 32 bits.  A position of a million times a frequency of one would keep only
 // four bits of its turn's fraction in 32 bits.
 //
-// Both operators move every byte once, so HBM bounds them.  A block takes a few tokens: it asks for its first elements,
-// makes one table of sines and cosines per token in shared memory (once, whatever the number of heads), and then walks
-// the tokens' heads in the order they lie in memory, 16 bytes per thread and access.  (A first version gave a thread the
-// pairs of one token and walked the heads from there, sines in registers: every access of a warp was whole lines, but
-// 256 bytes here and 256 there; 18432 tokens x 32 heads x 128 elements took 89 us.)
+// Both operators move every byte once, so HBM bounds them, and next the instructions per access.  A thread owns one unit
+// of one head for all the tokens of its block: what it turns with lies at a fixed place of a table of sines and cosines
+// that the block makes once per token in shared memory (whatever the number of heads), its addresses move on by a
+// constant, and the block's accesses run through a token's heads in the order they lie in memory.
 #include <math.h>
 
 #include "adsa_half.cuh"
 
 namespace adsa {
 
-constexpr int kTurnThreads = 256;
+constexpr int kTurnMaxThreads = 512;
 constexpr int kTurnMaxPairs = ADSA_MAX_HEAD_DIM / 2;
 constexpr int kTurnMaxTokens = 16;         // tokens of a block
 
@@ -64,25 +63,27 @@ struct Piece {
     static constexpr int kPairs = kTwo ? ACC : ACC / 2;            // pairs of a unit
     static constexpr int kTwos = (kPairs + 1) / 2;
     P a, b;
-    T *dst;                                                        // null: nothing to do
-    int partner;                                                   // elements to the second access; 0: none
-    int at;                                                        // table entry; -1: copied as it is
-    int turned;                                                    // pairs of the unit that turn
 
-    __device__ __forceinline__ void load(const T *src)
+    __device__ __forceinline__ void load(const T *src, int partner)
     {
         a = *reinterpret_cast<const P *>(src);
         if constexpr (kTwo)
             if (partner) b = *reinterpret_cast<const P *>(src + partner);
     }
-    __device__ __forceinline__ void turn(const float4 *table, int units)
+    __device__ __forceinline__ void store(T *dst, int partner) const
     {
-        if (at < 0) return;
+        *reinterpret_cast<P *>(dst) = a;
+        if constexpr (kTwo)
+            if (partner) *reinterpret_cast<P *>(dst + partner) = b;
+    }
+    // table: the unit's entries of the token, `units` apart; turned: pairs of the unit that turn
+    __device__ __forceinline__ void turn(const float4 *table, int units, int turned)
+    {
         if (ACC > 1 && turned == kPairs) {
             uint32_t *wa = reinterpret_cast<uint32_t *>(&a), *wb = reinterpret_cast<uint32_t *>(&b);
 #pragma unroll
             for (int i = 0; i < kTwos; ++i) {
-                const float4 t = table[at + i * units];
+                const float4 t = table[i * units];
                 if constexpr (HALVES) {
                     const float2 c = make_float2(t.x, t.y), s = make_float2(t.z, t.w), x = unpack2<T>(wa[i]), y = unpack2<T>(wb[i]);
                     const float2 u = fma2(x, c, mul2(y, make_float2(-s.x, -s.y))), v = fma2(x, s, mul2(y, c));
@@ -101,7 +102,7 @@ struct Piece {
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
                 if (i < turned) {
-                    const float4 t = table[at + (i >> 1) * units];
+                    const float4 t = table[(i >> 1) * units];
                     const float c = i & 1 ? t.y : t.x, s = i & 1 ? t.w : t.z;
                     T *pa = kTwo ? &a.e[i] : &a.e[2 * i], *pb = kTwo ? &b.e[i] : &a.e[2 * i + 1];
                     const float x = to_f32(*pa), y = to_f32(*pb);
@@ -111,32 +112,57 @@ struct Piece {
             }
         }
     }
-    __device__ __forceinline__ void store()
-    {
-        *reinterpret_cast<P *>(dst) = a;
-        if constexpr (kTwo)
-            if (partner) *reinterpret_cast<P *>(dst + partner) = b;
-    }
 };
 
 // blockIdx.x: tokens; blockIdx.y: a chunk of the q, k and v heads taken as one list
 template <typename T, int ACC, bool HALVES>
-__global__ void __launch_bounds__(kTurnThreads)
+__global__ void __launch_bounds__(kTurnMaxThreads)
 turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ adsa_rotary rot)
 {
     typedef Piece<T, ACC, HALVES> PieceT;
     extern __shared__ float4 table[];                              // [tokens][twos of a unit][units]
     __shared__ int s_row[kTurnMaxTokens], s_page[kTurnMaxTokens];  // row in its page (-1: not placed, -2: padding), page
+    __shared__ int s_pos[kTurnMaxTokens * 4];
+    __shared__ double s_turns[kTurnMaxPairs];
+    __shared__ uint8_t s_axis[kTurnMaxPairs];
     const long long t0 = (long long)blockIdx.x * a.tokens_block;
     const int tokens = (int)min((long long)a.tokens_block, a.tokens - t0);
     const int h0 = blockIdx.y * a.head_chunk, heads = min(a.head_chunk, a.q.heads + a.k.heads + a.v.heads - h0);
     const int k_first = a.q.heads, v_first = a.q.heads + a.k.heads;
-    const int pieces = tokens * heads * a.units;
+    // this thread's head and unit
+    const int u = (int)threadIdx.x % a.units, h = h0 + (int)threadIdx.x / a.units;
+    const bool live = h < h0 + heads;
+    const int kind = h < k_first ? 0 : h < v_first ? 1 : 2, head = h - (kind == 0 ? 0 : kind == 1 ? k_first : v_first);
+    const TurnRows &r = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+    int e0, partner = 0, turned = 0;
+    if constexpr (HALVES) {
+        if (u < a.rot_units) { e0 = u * ACC; partner = a.n; turned = ACC; }
+        else e0 = 2 * a.n + (u - a.rot_units) * ACC;
+    } else if constexpr (ACC == 1) {
+        e0 = 2 * u; partner = 1; turned = u < a.n ? 1 : 0;
+    } else {
+        e0 = u * ACC;
+        turned = max(0, min(a.n - e0 / 2, PieceT::kPairs));
+    }
+    if (kind == 2) turned = 0;
+    const long long head_rows = (long long)a.page_rows * a.row_stride, src_token = r.src_token, dst_token = r.dst_token;
+    const T *src = (const T *)r.src + t0 * src_token + head * r.src_head + e0;
+    T *dst = (T *)r.dst + (kind == 0 ? t0 * dst_token + head * r.dst_head : head * head_rows) + e0;
+    const long long page_elements = (kind == 0 ? 0 : r.heads) * head_rows;
+    const bool turns_here = h0 < v_first && a.n > 0;              // (v does not turn)
+    if (turns_here)
+        for (int i = threadIdx.x; i < a.n; i += blockDim.x) { s_turns[i] = rot.turns[i]; s_axis[i] = rot.axis[i]; }
     pdl_wait();
     pdl_launch();
-
-    // where the tokens' rows go
-    if (a.page_table) {
+    // everything that comes from memory is asked for at once: the first two tokens' elements, positions, rows
+    PieceT p, q;
+    if (live) {
+        p.load(src, partner);
+        if (tokens > 1) q.load(src + src_token, partner);
+    }
+    if (turns_here)
+        for (int i = threadIdx.x; i < tokens * a.n_axes; i += blockDim.x) s_pos[i] = a.pos[t0 * a.n_axes + i];
+    if (a.page_table) {                                            // where the tokens' rows go
         if (threadIdx.x < tokens) {
             const long long t = t0 + threadIdx.x;
             int b, j, row = -2, page = 0;
@@ -166,68 +192,15 @@ turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ adsa_rot
             s_row[threadIdx.x] = row;
             s_page[threadIdx.x] = page;
         }
-        __syncthreads();
     }
-    const long long head_rows = (long long)a.page_rows * a.row_stride;
+    __syncthreads();
+    // the tokens' sines and cosines
     const int turn_units = HALVES ? a.rot_units : a.units;         // units of the table
-    // Pieces in the order they lie in memory: this thread's token, head and unit, moved on by the block's threads at a time
-    int u, h, tk;
-    {
-        const int th = (int)threadIdx.x / a.units;
-        u = (int)threadIdx.x - th * a.units;
-        tk = th / heads;
-        h = th - tk * heads;
-    }
-    const int step_th = kTurnThreads / a.units, step_u = kTurnThreads - step_th * a.units, step_tk = step_th / heads, step_h = step_th - step_tk * heads;
-    const auto fetch = [&](PieceT &p) {
-        p.dst = nullptr;
-        if (tk < tokens) {
-            int e0, pair0 = 0;
-            p.partner = 0;
-            p.turned = 0;
-            if constexpr (HALVES) {
-                if (u < a.rot_units) { e0 = u * ACC; p.partner = a.n; p.turned = ACC; }
-                else e0 = 2 * a.n + (u - a.rot_units) * ACC;
-            } else if constexpr (ACC == 1) {
-                e0 = 2 * u; p.partner = 1; p.turned = u < a.n ? 1 : 0;
-            } else {
-                e0 = u * ACC; pair0 = e0 / 2;
-                p.turned = max(0, min(a.n - pair0, PieceT::kPairs));
-            }
-            const int row = a.page_table ? s_row[tk] : -1, hh = h + h0;
-            const T *src = nullptr;
-            if (hh < k_first) {
-                if (row != -2) {
-                    src = (const T *)a.q.src + (t0 + tk) * a.q.src_token + hh * a.q.src_head + e0;
-                    p.dst = (T *)a.q.dst + (t0 + tk) * a.q.dst_token + hh * a.q.dst_head + e0;
-                }
-            } else if (row >= 0) {
-                const bool key = hh < v_first;
-                const int kh = hh - (key ? k_first : v_first);
-                if (!key) p.turned = 0;
-                src = (key ? (const T *)a.k.src + (t0 + tk) * a.k.src_token + kh * a.k.src_head
-                           : (const T *)a.v.src + (t0 + tk) * a.v.src_token + kh * a.v.src_head) + e0;
-                p.dst = (T *)(key ? a.k.dst : a.v.dst) + ((long long)s_page[tk] * a.k.heads + kh) * head_rows + (long long)row * a.row_stride + e0;
-                if (u == 0)
-                    for (int e = a.d; e < a.row_stride; ++e) p.dst[e] = from_f32<T>(0.f);
-            }
-            p.at = p.turned > 0 ? tk * PieceT::kTwos * turn_units + u : -1;
-            if (src) p.load(src);
-        }
-        u += step_u; h += step_h; tk += step_tk;
-        if (u >= a.units) { u -= a.units; ++h; }
-        if (h >= heads) { h -= heads; ++tk; }
-    };
-    constexpr int AHEAD = HALVES ? 2 : 4;                          // pieces a thread has in flight
-    PieceT p[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) fetch(p[k]);
-    // the sines and cosines of the tokens, while the first pieces are on their way (v does not turn)
-    if (h0 < v_first && a.n > 0) {
+    if (turns_here) {
         float *out = reinterpret_cast<float *>(table);
-        for (int i = threadIdx.x; i < tokens * a.n; i += kTurnThreads) {
+        for (int i = threadIdx.x; i < tokens * a.n; i += blockDim.x) {
             const int t = i / a.n, pair = i - t * a.n, unit = pair / PieceT::kPairs, in = pair - unit * PieceT::kPairs;
-            const double turns = (double)a.pos[(t0 + t) * a.n_axes + rot.axis[pair]] * rot.turns[pair];
+            const double turns = (double)s_pos[t * a.n_axes + s_axis[pair]] * s_turns[pair];
             float sn, cs;
             sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
             float *entry = out + 4 * ((t * PieceT::kTwos + (in >> 1)) * turn_units + unit) + (in & 1);
@@ -236,16 +209,25 @@ turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ adsa_rot
         }
         __syncthreads();
     }
-    for (int i = 0; i < pieces; i += AHEAD * kTurnThreads) {
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (p[k].dst) {
-                p[k].turn(table, turn_units);
-                p[k].store();
-            }
+    if (!live) return;
+    const float4 *entries = table + u;
+    const int token_entries = PieceT::kTwos * turn_units;
+    const auto placed = [&](int t) { return !a.page_table || (kind == 0 ? s_row[t] != -2 : s_row[t] >= 0); };
+    const auto finish = [&](PieceT &p, int t) {
+        if (turned) p.turn(entries + t * token_entries, turn_units, turned);
+        T *o = dst + (kind == 0 ? t * dst_token : s_page[t] * page_elements + (long long)s_row[t] * a.row_stride);
+        p.store(o, partner);
+        if (kind != 0 && u == 0)                                   // the row's padding
+            for (int e = a.d; e < a.row_stride; ++e) o[e] = from_f32<T>(0.f);
+    };
+    // two tokens in hand, (padding is read and not written)
+    for (int t = 0; t < tokens; t += 2) {
+        if (t > 0) {
+            p.load(src + t * src_token, partner);
+            if (t + 1 < tokens) q.load(src + (t + 1) * src_token, partner);
         }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) fetch(p[k]);
+        if (placed(t)) finish(p, t);
+        if (t + 1 < tokens && placed(t + 1)) finish(q, t + 1);
     }
 }
 
@@ -265,11 +247,11 @@ int fit(int acc, const TurnRows &r)
 }
 
 template <typename T>
-cudaError_t launch_turn(const TurnArgs &a, const adsa_rotary &rot, int acc, bool halves, dim3 grid, size_t smem, cudaStream_t st)
+cudaError_t launch_turn(const TurnArgs &a, const adsa_rotary &rot, int acc, bool halves, dim3 grid, unsigned threads, size_t smem, cudaStream_t st)
 {
 #define ADSA_TURN(A) \
-    if (acc == A) return halves ? launch_pdl(turn_kernel<T, A, true>, grid, kTurnThreads, smem, st, a, rot) \
-                                : launch_pdl(turn_kernel<T, A, false>, grid, kTurnThreads, smem, st, a, rot)
+    if (acc == A) return halves ? launch_pdl(turn_kernel<T, A, true>, grid, threads, smem, st, a, rot) \
+                                : launch_pdl(turn_kernel<T, A, false>, grid, threads, smem, st, a, rot)
     ADSA_TURN(8);
     ADSA_TURN(4);
     ADSA_TURN(2);
@@ -290,25 +272,26 @@ int run_turn(TurnArgs &a, const adsa_rotary &rot, int dtype, cudaStream_t st)
     a.rot_units = halves ? a.n / acc : 0;
     a.units = halves ? a.rot_units + (a.d - 2 * a.n) / acc : acc == 1 ? a.d / 2 : a.d / acc;
     const int heads = a.q.heads + a.k.heads + a.v.heads;
-    // Enough blocks for every SM before anything else (fewer heads a block), then about eight pieces a thread (more tokens
-    // a block), so that a table of sines serves many heads.
-    const int per_token = heads * a.units;
-    int tokens = 8 * kTurnThreads / per_token;
-    if (tokens > kTurnMaxTokens) tokens = kTurnMaxTokens;
-    while (tokens > 1 && a.tokens / tokens < 148 * 4) tokens /= 2;
-    if (tokens < 1) tokens = 1;
+    // Heads a block: all of them if they make up to 512 units, fewer until every SM has a block.  Tokens a block: as many as
+    // let all blocks run at once (2048 threads an SM), at most 16: a second, thinner wave costs as much as a full one.
+    int chunks = (heads * a.units + kTurnMaxThreads - 1) / kTurnMaxThreads;
+    while (chunks < heads && (heads + chunks - 1) / chunks * a.units > kTurnMaxThreads) ++chunks;
+    while (chunks < heads && a.tokens * chunks < 148 && (heads + chunks - 1) / chunks * a.units > 128) ++chunks;
+    const int chunk = (heads + chunks - 1) / chunks;
+    chunks = (heads + chunk - 1) / chunk;
+    const unsigned threads = (unsigned)((chunk * a.units + 31) / 32 * 32);
+    const long long resident = 148 * (2048 / threads);
+    long long tokens = (a.tokens * chunks + resident - 1) / resident;
+    tokens = tokens < 1 ? 1 : tokens > kTurnMaxTokens ? kTurnMaxTokens : tokens;
     const long long blocks = (a.tokens + tokens - 1) / tokens;
-    if (blocks > 0x7fffffffLL) return ADSA_EINVAL;
-    int chunk = heads;
-    while (chunk * a.units > kTurnThreads && (blocks * ((heads + chunk - 1) / chunk) < 148 * 4 || chunk * a.units > 16 * kTurnThreads)) chunk = (chunk + 1) / 2;
-    if ((heads + chunk - 1) / chunk > 65535) return ADSA_EINVAL;
-    a.tokens_block = tokens;
+    if (blocks > 0x7fffffffLL || chunks > 65535) return ADSA_EINVAL;
+    a.tokens_block = (int)tokens;
     a.head_chunk = chunk;
     // table bytes: at most kTurnMaxTokens x 128 pairs x 8 (with one pair a unit half of an entry is not used)
     const int pairs = halves || acc == 1 ? acc : acc / 2;
     const size_t smem = (size_t)tokens * ((pairs + 1) / 2) * (halves ? a.rot_units : a.units) * 16;
-    const dim3 grid((unsigned)blocks, (unsigned)((heads + chunk - 1) / chunk));
-    const cudaError_t e = dtype == ADSA_BF16 ? launch_turn<__nv_bfloat16>(a, rot, acc, halves, grid, smem, st) : launch_turn<__half>(a, rot, acc, halves, grid, smem, st);
+    const dim3 grid((unsigned)blocks, (unsigned)chunks);
+    const cudaError_t e = dtype == ADSA_BF16 ? launch_turn<__nv_bfloat16>(a, rot, acc, halves, grid, threads, smem, st) : launch_turn<__half>(a, rot, acc, halves, grid, threads, smem, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 
