@@ -583,7 +583,7 @@ def model_shell(args, dev):
     """Whole generations through the LlamaGen-shaped shell (random weights): the condition is prefilled, every grid
     cell is decoded through all layers (torch GEMMs around libadsa's kernels, one ADSA layer-step launch per layer,
     because every layer's q/k/v depend on the layer before), ids go to the host as they are drawn."""
-    from paper_2506_18226_b200.shell import SHAPES, LlamaGenShell, ShellConfig
+    from paper_2506_18226_b200.shell import SHAPES, LlamaGenShell, SharedPromptShell, ShellConfig
     grid = {"B": 16, "L": 24, "XL": 32}[args.shell]
     n_images = {"B": 1, "L": 8, "XL": 16}[args.shell]
     cfg = ShellConfig(grid_h=grid, grid_w=grid, n_images=n_images, **SHAPES[args.shell])
@@ -646,6 +646,19 @@ def model_shell(args, dev):
     t_dense = time.perf_counter() - t0
     del dense
     torch.cuda.empty_cache()
+    # the same for images of one prompt: whole context, the condition's rows kept and read once for all images
+    base = torch.cuda.memory_allocated(dev)
+    shared = SharedPromptShell(cfg, seed=args.seed, device=str(dev))
+    shared_bytes = torch.cuda.memory_allocated(dev) - base
+    one = torch.stack([text[0], text[n_images]])
+    shared.generate(one, n_cells=min(64, grid * grid))
+    torch.cuda.synchronize(dev)
+    t0 = time.perf_counter()
+    shared.generate(one)
+    t_shared = time.perf_counter() - t0
+    status |= int(shared.status)
+    del shared
+    torch.cuda.empty_cache()
     mem = []
     for n_img in (1, 2, 4, 8, 16, 32):
         row = {"n_images": n_img, "batch_rows": 2 * n_img}
@@ -663,6 +676,8 @@ def model_shell(args, dev):
             "image_tokens_per_s": n_images * cells / t, "ms_per_token": t / cells * 1e3, "seconds_per_generation": t,
             "whole_context_cache": {"ms_per_token": t_dense / cells * 1e3, "image_tokens_per_s": n_images * cells / t_dense,
                                     "time_ratio_adsa_over_dense": t / t_dense},
+            "one_prompt_shared_condition": {"ms_per_token": t_shared / cells * 1e3, "image_tokens_per_s": n_images * cells / t_shared,
+                                            "time_ratio_over_private_whole_context": t_shared / t_dense, "bytes_allocated": shared_bytes},
             "weights_bytes": weights, "ids_on_host": n_ids, "data": "random weights, random condition embeddings",
             "timing": "wall clock around prefill + every decode step + the final synchronisation, best of 2",
             "kernels_alone": ops, "memory_vs_images_allocated": mem, "status": status}

@@ -11,6 +11,11 @@ One block: x -> RMSNorm -> q, k, v projections -> 2-D RoPE on q and k -> ADSA la
 (+ residual) -> RMSNorm -> gate/up projection -> silu(gate) * up -> down projection (+ residual).  Classifier-free
 guidance doubles the batch: rows [0, n_images) are conditional, rows [n_images, 2 n_images) unconditional; both
 halves are fed the same sampled ids.
+
+SharedPromptShell is the same decoder for several images of ONE prompt, nothing evicted: the condition's rows are kept
+once per guidance half in a paged cache and every decode step sweeps them once for all images, the new rows are rotated
+on their way into the cache, the residual additions and normalisations are one call each, and a whole decode step is one
+CUDA graph (every length and position it needs lies on the device).
 """
 from __future__ import annotations
 
@@ -37,6 +42,7 @@ class ShellConfig:
     top_k: int = 2000
     temperature: float = 1.0
     norm_eps: float = 1e-5
+    sandwich_norm: bool = False         # SharedPromptShell: a normalisation after each block too, before its residual addition
 
     @property
     def head_dim(self) -> int:
@@ -59,10 +65,11 @@ SHAPES = {
 }
 
 
-class LlamaGenShell:
-    def __init__(self, cfg: ShellConfig, seed: int = 0, device: str = "cuda:0", use_graphs: bool = True):
+class _Decoder:
+    """Random weights and the buffers of a decode step; what both shells share."""
+
+    def __init__(self, cfg: ShellConfig, seed: int, device: str):
         self.cfg, self.dev = cfg, torch.device(device)
-        self.use_graphs, self.graphs = use_graphs, None
         g = torch.Generator(device=self.dev).manual_seed(seed)
         bf = dict(dtype=torch.bfloat16, device=self.dev)
 
@@ -79,12 +86,6 @@ class LlamaGenShell:
         self.norm2 = torch.ones(L, D, **bf)
         self.norm_f = torch.ones(D, **bf)
         self.head = w(V, D)
-        C = self.budget = max(cfg.capacity, cfg.n_text + 1)   # rows a stream may hold (a row is evicted before one is inserted)
-        # rows per pool page: the largest divisor of the capacity up to 1024 rows, so that a full stream fills whole pages
-        page_rows = next((pr for pr in range(min(C, 1024), 15, -1) if C % pr == 0), 32)
-        self.eng = B.AdsaEngine(n_layers=L, batch=cfg.batch, n_heads=cfg.n_heads, head_dim=cfg.head_dim, n_text=cfg.n_text,
-                                grid_h=cfg.grid_h, grid_w=cfg.grid_w, max_rows_per_stream=C,
-                                page_rows=page_rows, device=device)
         Bt, H, d = cfg.batch, cfg.n_heads, cfg.head_dim
         self.qkv = torch.empty(3, Bt, H, d, **bf)    # q, k, v of a decode step, each dense [batch, heads, head_dim]
         self.q, self.k, self.v = self.qkv[0], self.qkv[1], self.qkv[2]
@@ -93,7 +94,6 @@ class LlamaGenShell:
         self.gu = torch.empty(Bt, 2 * Hd, **bf)
         self.act = torch.empty(Bt, Hd, **bf)
         self.logits = torch.empty(Bt, V, **bf)
-        self.pos = torch.zeros(2 * Bt * H, dtype=torch.int32, device=self.dev)   # one per row of q and of k
         self.tokens = torch.zeros(cfg.n_images, dtype=torch.int32, device=self.dev)
         self.ids_host = torch.zeros(cfg.grid_h * cfg.grid_w, cfg.n_images, dtype=torch.int32).pin_memory()
         # the random numbers of the whole generation, drawn once (the sampling call takes them as an input)
@@ -106,6 +106,28 @@ class LlamaGenShell:
     wq = property(lambda self: self.wqkv_t[:, 0].transpose(1, 2))
     wk = property(lambda self: self.wqkv_t[:, 1].transpose(1, 2))
     wv = property(lambda self: self.wqkv_t[:, 2].transpose(1, 2))
+
+    def generate(self, text_emb, n_cells=None):
+        """Prefill and decode `n_cells` grid cells (default: the whole grid); returns the ids on the host, [cells, n_images]."""
+        n = self.cfg.grid_h * self.cfg.grid_w if n_cells is None else n_cells
+        self.prefill(text_emb)
+        for cell in range(1, n):
+            self.decode_step(cell)
+        torch.cuda.synchronize(self.dev)
+        return self.ids_host[:n]
+
+
+class LlamaGenShell(_Decoder):
+    def __init__(self, cfg: ShellConfig, seed: int = 0, device: str = "cuda:0", use_graphs: bool = True):
+        super().__init__(cfg, seed, device)
+        self.use_graphs, self.graphs = use_graphs, None
+        C = self.budget = max(cfg.capacity, cfg.n_text + 1)   # rows a stream may hold (a row is evicted before one is inserted)
+        # rows per pool page: the largest divisor of the capacity up to 1024 rows, so that a full stream fills whole pages
+        page_rows = next((pr for pr in range(min(C, 1024), 15, -1) if C % pr == 0), 32)
+        self.eng = B.AdsaEngine(n_layers=cfg.n_layers, batch=cfg.batch, n_heads=cfg.n_heads, head_dim=cfg.head_dim, n_text=cfg.n_text,
+                                grid_h=cfg.grid_h, grid_w=cfg.grid_w, max_rows_per_stream=C,
+                                page_rows=page_rows, device=device)
+        self.pos = torch.zeros(2 * cfg.batch * cfg.n_heads, dtype=torch.int32, device=self.dev)   # one per row of q and of k
 
     # -- one block on a [rows, dim] activation; `attend` does the attention for this layer ------------------------
     def _block(self, layer, x, attend):
@@ -241,11 +263,130 @@ class LlamaGenShell:
         self.kernel_calls += 2
         return self.tokens
 
-    def generate(self, text_emb, n_cells=None):
-        """Prefill and decode `n_cells` grid cells (default: the whole grid); returns the ids on the host, [cells, n_images]."""
-        n = self.cfg.grid_h * self.cfg.grid_w if n_cells is None else n_cells
-        self.prefill(text_emb)
-        for cell in range(1, n):
-            self.decode_step(cell)
-        torch.cuda.synchronize(self.dev)
-        return self.ids_host[:n]
+
+class SharedPromptShell(_Decoder):
+    """n_images images of one prompt with guidance: two groups of batch rows (conditional, unconditional), each with its
+    condition's rows kept once.  Nothing is evicted."""
+
+    PAGE_ROWS = 64
+
+    def __init__(self, cfg: ShellConfig, seed: int = 0, device: str = "cuda:0", use_graphs: bool = True):
+        super().__init__(cfg, seed, device)
+        self.use_graphs, self.graph = use_graphs, None
+        L, H, d, n, pr = cfg.n_layers, cfg.n_heads, cfg.head_dim, cfg.n_images, self.PAGE_ROWS
+        bf, i32 = dict(dtype=torch.bfloat16, device=self.dev), dict(dtype=torch.int32, device=self.dev)
+        cells = cfg.grid_h * cfg.grid_w
+        own, text = (cells + pr - 1) // pr, (cfg.n_text + pr - 1) // pr      # pages per batch row, per condition
+        pages = 2 * text + cfg.batch * own
+        self.k_pool, self.v_pool = torch.zeros(L, pages, H, pr, d, **bf), torch.zeros(L, pages, H, pr, d, **bf)
+        self.prefix_table = torch.arange(2 * text, **i32).view(2, text)
+        self.page_table = torch.arange(2 * text, pages, **i32).view(cfg.batch, own)
+        self.prefix_rows = torch.full((2,), cfg.n_text, **i32)
+        self.group_start = torch.tensor([0, n, 2 * n], **i32)
+        # rows in the cache before and after this step's append, and the cell that is fed in: moved on by the step itself
+        self.n_before, self.n_after = torch.zeros(cfg.batch, **i32), torch.ones(cfg.batch, **i32)
+        self.cell = torch.zeros(1, dtype=torch.int64, device=self.dev)
+        # grid row and column of every cell; the condition is not rotated (position 0, 0)
+        c = torch.arange(cells, device=self.dev)
+        self.positions = torch.stack([c // cfg.grid_w, c % cfg.grid_w], 1).to(torch.int32).contiguous()
+        self.pos = torch.zeros(cfg.batch, 2, **i32)
+        self.rotary = B.Rotary(d, (d // 4, d // 4))
+        self.y = torch.empty(cfg.batch, cfg.dim, **bf)                       # a block's output, before the residual addition
+        self.post1 = torch.ones(L, cfg.dim, **bf) if cfg.sandwich_norm else None
+        self.post2 = torch.ones(L, cfg.dim, **bf) if cfg.sandwich_norm else None
+        self.workspace = B.shared_prefix_workspace(self.q, self.k_pool[0], self.page_table, self.prefix_table)
+        self.status = torch.zeros(1, **i32)
+
+    # -- one block: h = norm1(x) of `rows` rows in, the residual stream x moved on, h = the next block's norm1 (or the last norm) out
+    def _block(self, layer, x, h, y, attend):
+        c = self.cfg
+        post = (None, None) if self.post1 is None else (self.post1[layer], self.post2[layer])
+        torch.mm(attend(layer, h), self.wo[layer].t(), out=y)
+        B.norm_residual(y, x, self.norm2[layer], w_post=post[0], eps=c.norm_eps, x_out=x, h=h)
+        step = x is self.x
+        gu = torch.mm(h, self.w13[layer].t(), out=self.gu if step else None)
+        act = B.swiglu(gu[:, :c.ffn_hidden], gu[:, c.ffn_hidden:], out=self.act if step else None)
+        torch.mm(act, self.w2[layer].t(), out=y)
+        after = self.norm1[layer + 1] if layer + 1 < c.n_layers else self.norm_f
+        B.norm_residual(y, x, after, w_post=post[1], eps=c.norm_eps, x_out=x, h=h)
+
+    def prefill(self, text_emb):
+        """The condition, text_emb [2, n_text, dim] bf16 (conditional, unconditional), enters the shared pages; row i of it
+        attends rows 0 .. i, as so many queries over the same pages with lengths 1, 2, ..  Draws the first tokens."""
+        c, T, H, d = self.cfg, self.cfg.n_text, self.cfg.n_heads, self.cfg.head_dim
+        i32 = dict(dtype=torch.int32, device=self.dev)
+        x = text_emb.reshape(2 * T, c.dim).clone()
+        h, y = B.rmsnorm(x, self.norm1[0], eps=c.norm_eps), torch.empty_like(x)
+        pos, none = torch.zeros(2 * T, 2, **i32), torch.zeros(2, **i32)
+        tables = self.prefix_table.repeat_interleave(T, 0)
+        lengths = torch.arange(1, T + 1, **i32).repeat(2)
+        out = torch.empty(2 * T, H, d, dtype=torch.bfloat16, device=self.dev)
+
+        def attend(layer, h):
+            q, k, v = torch.matmul(h.unsqueeze(0), self.wqkv_t[layer]).view(3, 2 * T, H, d)
+            B.rope_axes(self.rotary, q, pos, out=q)
+            B.paged_append(k, v, self.k_pool[layer], self.v_pool[layer], self.prefix_table, none, rotary=self.rotary, pos=pos, status=self.status)
+            B.shared_prefix_attn(q, self.k_pool[layer], self.v_pool[layer], tables, lengths, out=out, status=self.status)
+            return out.view(2 * T, c.dim)
+
+        for layer in range(c.n_layers):
+            self._block(layer, x, h, y, attend)
+        self.kernel_calls += 1 + 6 * c.n_layers + 1
+        self.n_before.zero_()
+        self.n_after.fill_(1)
+        self.cell.fill_(0)
+        self.h.copy_(h.view(2, T, c.dim)[:, -1].repeat_interleave(c.n_images, 0))   # every image starts from the same row
+        self._sample()
+        self.ids_host[0].copy_(self.tokens, non_blocking=True)
+        return self.tokens
+
+    def _sample(self):
+        """The next token of every image from h, with the uniform numbers of `cell`."""
+        c = self.cfg
+        torch.mm(self.h, self.head.t(), out=self.logits)
+        torch.index_select(self.uniforms, 0, self.cell, out=self.u.view(1, -1))
+        B.cfg_sample(self.logits, c.cfg_scale, min(c.top_k, c.vocab), c.temperature, self.u, tokens=self.tokens)
+
+    def _attend(self, layer, h):
+        c = self.cfg
+        torch.bmm(h.unsqueeze(0).expand(3, -1, -1), self.wqkv_t[layer], out=self.qkv.view(3, c.batch, c.dim))
+        B.paged_append(self.k, self.v, self.k_pool[layer], self.v_pool[layer], self.page_table, self.n_before, rotary=self.rotary, pos=self.pos,
+                       q=self.q, q_out=self.q, status=self.status)
+        B.shared_prefix_attn(self.q, self.k_pool[layer], self.v_pool[layer], self.page_table, self.n_after, self.prefix_table, self.prefix_rows,
+                             self.group_start, out=self.o, workspace=self.workspace, status=self.status)
+        return self.o.view(c.batch, c.dim)
+
+    def _step(self):
+        c, n = self.cfg, self.cfg.n_images
+        self.pos.copy_(self.positions.index_select(0, self.cell).expand(c.batch, 2))
+        torch.index_select(self.tok_emb, 0, self.tokens, out=self.x[:n])
+        self.x[n:].copy_(self.x[:n])                                       # conditional and unconditional rows
+        B.rmsnorm(self.x, self.norm1[0], out=self.h, eps=c.norm_eps)
+        for layer in range(c.n_layers):
+            self._block(layer, self.x, self.h, self.y, self._attend)
+        for t in (self.n_before, self.n_after, self.cell):
+            t.add_(1)
+        self._sample()
+
+    def decode_step(self, cell):
+        """The image token of grid cell `cell` (>= 1, in order) from the token of cell - 1."""
+        if not self.use_graphs:
+            self._step()
+        else:
+            if self.graph is None:
+                side = torch.cuda.Stream(device=self.dev)
+                kept = [t.clone() for t in (self.n_before, self.n_after, self.cell, self.tokens)]
+                side.wait_stream(torch.cuda.current_stream(self.dev))
+                with torch.cuda.stream(side):                              # once eagerly: libraries make their handles and workspaces
+                    self._step()
+                torch.cuda.current_stream(self.dev).wait_stream(side)
+                torch.cuda.synchronize(self.dev)
+                self.graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(self.graph):
+                    self._step()
+                for t, was in zip((self.n_before, self.n_after, self.cell, self.tokens), kept):
+                    t.copy_(was)                                           # (the trial run moved them on; its rows are written again)
+            self.graph.replay()
+        self.ids_host[cell].copy_(self.tokens, non_blocking=True)
+        self.kernel_calls += 1 + 5 * self.cfg.n_layers + 1
+        return self.tokens

@@ -612,3 +612,45 @@ def test_calls_on_another_stream_and_empty_calls():
     x = _randn(g, 4, 2, 64)
     assert A.rope_axes(rot, x[:0], torch.zeros((0, 1), dtype=torch.int32, device=DEV)).shape == (0, 2, 64)
     assert A.rope_axes(rot, x[:, :0], torch.zeros((4, 1), dtype=torch.int32, device=DEV)).shape == (4, 0, 64)
+
+
+# ---- the model shell for images of one prompt ---------------------------------------------------------------------------
+
+def _shells(**kw):
+    from paper_2506_18226_b200.shell import LlamaGenShell, SharedPromptShell, ShellConfig
+    cfg = ShellConfig(n_layers=3, dim=128, n_heads=2, ffn_hidden=256, vocab=512, n_text=8, grid_h=6, grid_w=6, n_images=3, top_k=50,
+                      budget_fraction=1.0, **kw)
+    g = _gen(4)
+    text = torch.randn(2, cfg.n_text, cfg.dim, generator=g, device=DEV).to(torch.bfloat16)
+    return cfg, text, LlamaGenShell, SharedPromptShell
+
+
+def test_shared_prompt_shell_follows_the_shell_with_private_caches():
+    """The same weights, every image with its own copy of the same condition and nothing evicted: the logits after the
+    condition and after five steps (fed the same ids) agree as two bf16 evaluations of one decoder do."""
+    cfg, text, Private, Shared = _shells()
+    a, b = Private(cfg, seed=2, use_graphs=False), Shared(cfg, seed=2, use_graphs=False)
+    a.prefill(text.repeat_interleave(cfg.n_images, 0).contiguous())
+    b.prefill(text)
+    for cell in range(1, 7):
+        x, y = a.logits.double(), b.logits.double()
+        assert float((x - y).norm() / x.norm()) <= 3e-2 and float((x * y).sum() / (x.norm() * y.norm())) >= 0.999
+        a.tokens.copy_(b.tokens)
+        if cell < 6:
+            a.decode_step(cell)
+            b.decode_step(cell)
+    assert int(b.status) == 0 and a.eng.get_status()[0] == 0
+
+
+@pytest.mark.parametrize("sandwich", [False, True])
+def test_shared_prompt_shell_graph_and_eager_steps_draw_the_same_ids(sandwich):
+    cfg, text, _, Shared = _shells(sandwich_norm=sandwich)
+    ids = []
+    for graphs in (True, False, True):
+        sh = Shared(cfg, seed=3, use_graphs=graphs)
+        ids.append(sh.generate(text).clone())
+        assert int(sh.status) == 0 and sh.n_before.tolist() == [35] * cfg.batch
+    assert torch.equal(ids[0], ids[1]) and torch.equal(ids[0], ids[2])
+    assert int(ids[0].min()) >= 0 and int(ids[0].max()) < cfg.vocab and len(set(ids[0].flatten().tolist())) > 8
+    again = sh.generate(text).clone()                                             # the cache and the graph serve a second generation
+    assert torch.equal(again, ids[0])
