@@ -487,7 +487,7 @@ ADSA_API int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_tabl
  *   n_rows, prefix_rows   int32, each clamped to 0 .. what its table holds; table entries past them are not read
  *   group_start  int32 [n_groups + 1], ascending: batch rows group_start[g] .. group_start[g+1]-1 are group g; batch
  *                rows of no group have no prefix.  n_groups may be 0.  Boundaries are clamped to 0 .. batch
- *   out, out_f32 16-bit / float [batch][n_heads][head_dim], either may be NULL, not both
+ *   out, out_f32 16-bit / float [batch][n_heads][head_dim], 4- / 8-byte aligned; either may be NULL, not both
  *   lse          float [batch][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
  * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).
  * batch + n_groups <= 8192.  workspace: [device] 256-byte aligned, adsa_shared_prefix_workspace_bytes of them, nothing

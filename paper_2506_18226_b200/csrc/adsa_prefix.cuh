@@ -24,12 +24,12 @@ struct PrefixArgs {
     int d, row_stride;
     float scale_log2e;
     // workspace
-    uint4 *plan;                            // [1 + 2 batch] for the merge: number of units; two words of four per batch row
+    uint4 *plan;                            // [batch][3] for the merge: {first own unit, tiles, units, group's first slot}, {group's first unit,
+                                            // tiles, first batch row, query rows}, {units of the wide kernel}
     float *p_state, *p_ml, *o_state, *o_ml; // prefix slots, own-row slots: rows of d_pad floats, (m, l) pairs
     int n_p_slots, n_o_slots;
     // groups with more query rows per key head than this go to the wide kernel, with a plan and slots of its own
     int wide_above;
-    uint32_t *w_plan;                       // [groups + 1]
     float *w_state, *w_ml;                  // slots of kWideQueries rows
     int n_w_slots, w_resident;              // w_resident: blocks of the wide kernel that fit the GPU at a time; 0: it does not run
     int resident;                           // blocks of the sweep kernel that fit the GPU at a time

@@ -52,6 +52,7 @@ struct Shared {
     uint32_t *plan;                         // [entries + 1] first unit of every entry
     int *len;                               // [entries] cached rows
     int *begin;                             // [groups + 1]
+    uint32_t *wide;                         // [groups] first unit of every group in the wide kernel's list
 };
 __device__ __forceinline__ int members(const Shared &c, int g) { return max(c.begin[g + 1] - c.begin[g], 0); }
 
@@ -170,12 +171,13 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     extern __shared__ unsigned char pa_smem[];
     __shared__ uint64_t bars[2 * STAGES + 4];
     __shared__ __align__(16) uint4 answers[2];
-    __shared__ uint32_t warp_sums[kPaThreads / 32];
+    __shared__ uint2 warp_sums[kPaThreads / 32];
     const uint32_t ring = (smem_u32(pa_smem) + 1023u) & ~1023u, pitch = PACKED ? (uint32_t)a.row_stride * 2u : 128u;
     Shared c;
     c.plan = reinterpret_cast<uint32_t *>(pa_smem + (ring - smem_u32(pa_smem)) + (size_t)STAGES * 2 * kHalf);
     c.len = reinterpret_cast<int *>(c.plan + a.groups + a.batch + 1);
     c.begin = c.len + a.groups + a.batch;
+    c.wide = reinterpret_cast<uint32_t *>(c.begin + a.groups + 1);
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, asked = empty + 8 * STAGES, heard = asked + 16, answer = smem_u32(answers);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int entries = a.groups + a.batch;
@@ -186,6 +188,18 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    }
+    // The small tables into L2 while the kernel ahead still runs (hints; they are read after the wait)
+    {
+        const auto hint = [&](const int32_t *p, long long n) {
+            for (long long i = ((long long)blockIdx.x * kPaThreads + tid) * 32; i < min(n, 65536LL); i += (long long)gridDim.x * kPaThreads * 32)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
+        };
+        hint(a.table, (long long)a.batch * a.max_pages);
+        hint(a.n_rows, a.batch);
+        hint(a.p_table, (long long)a.groups * a.max_p_pages);
+        hint(a.p_rows, a.groups);
+        hint(a.start, a.groups > 0 ? a.groups + 1 : 0);
     }
     // Behind the wide kernel of the same call (which has waited for what was ahead of it before this one could begin) there
     // is nothing to wait for here; each block waits before it ends, so that the merge finds both kernels' states.
@@ -199,20 +213,36 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     for (int e = e0; e < e1; ++e)
         c.len[e] = e < a.groups ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
     __syncthreads();
-    uint32_t mine = 0;
+    uint2 mine = make_uint2(0u, 0u);                               // units of this list, of the wide kernel's
     for (int e = e0; e < e1; ++e) {
         const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;
-        c.plan[e] = mine;
-        if (e >= a.groups || m <= a.wide_above) mine += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
+        c.plan[e] = mine.x;
+        if (e < a.groups) c.wide[e] = mine.y;
+        if (e < a.groups && m > a.wide_above)
+            mine.y += (uint32_t)((m + kWideQueries - 1) / kWideQueries) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + kWideTile - 1) / kWideTile);
+        else
+            mine.x += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
     }
-    uint32_t incl = mine;
+    uint2 incl = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
+        if (lane >= o) { incl.x += x; incl.y += y; }
+    }
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
-    uint32_t before = incl - mine, total = 0;
-    for (int w = 0; w < kPaThreads / 32; ++w) { if (w < warp) before += warp_sums[w]; total += warp_sums[w]; }
-    for (int e = e0; e < e1; ++e) c.plan[e] += before;
+    uint2 before = make_uint2(incl.x - mine.x, incl.y - mine.y);
+    uint32_t total = 0, wide_total = 0;
+    for (int w = 0; w < kPaThreads / 32; ++w) {
+        const uint2 s = warp_sums[w];
+        if (w < warp) { before.x += s.x; before.y += s.y; }
+        total += s.x;
+        wide_total += s.y;
+    }
+    for (int e = e0; e < e1; ++e) {
+        c.plan[e] += before.x;
+        if (e < a.groups) c.wide[e] += before.y;
+    }
     if (tid == 0) c.plan[entries] = total;
     __syncthreads();
     const Cut cut(total, (uint32_t)a.resident);
@@ -220,11 +250,11 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     walk.begin(a, c, cut, blockIdx.x);
     Segment s;
     // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp asks for the next
-    // run when it begins one, into the answer slot that all warps have read the last time, and leaves its share of the
-    // plan for the merge: that goes by run, as any block may be taken over before it starts.
+    // run when it begins one, into the answer slot that all warps have read the last time; warp 0 leaves the run's share
+    // of the plan for the merge (that goes by run, as any block may be taken over before it starts).
     int limit = kCopySpinLimit;
     uint32_t turns = 0;                                            // runs finished by this warp
-    const auto begin_run = [&](int run) {
+    const auto ask = [&]() {
         if (lane == 0) {
             const uint32_t i = turns & 1u;
             if (!mbar_wait_bounded(heard + 8 * i, ((turns >> 1) & 1u) ^ 1u, limit)) limit = kCopySpinAfterTimeout;
@@ -232,11 +262,14 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             pa_ask_block(answer + 16 * i, asked + 8 * i);
         }
         __syncwarp();                                              // the other lanes must not spin for the answer before it is asked for
-        if (run == 0 && lane == 0) a.plan[0] = make_uint4(total, 0u, 0u, 0u);
+    };
+    const auto leave_plan = [&](int run) {
         const uint32_t share = max(cut.runs, 1u);
         for (int b = (uint32_t)run < share ? run + lane * (int)share : a.batch; b < a.batch; b += 32 * (int)share) {
-            // the batch row's own units, and its group's: the last group that begins at or before it
-            uint4 own_part = make_uint4(c.plan[a.groups + b], (uint32_t)(c.len[a.groups + b] + TILE - 1) / TILE, 0u, 0u), group = make_uint4(0u, 0u, 0u, 0u);
+            // the batch row's own units, and its group's: the last group that begins at or before it.  Everything a merging
+            // warp needs is in the row's own three words of four: one line that all of them read would hold them up.
+            uint4 group = make_uint4(0u, 0u, 0u, 0u);
+            uint32_t slot = 0u;
             int lo = -1, hi = a.groups - 1;
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
@@ -244,12 +277,15 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 else hi = mid - 1;
             }
             if (lo >= 0 && b < c.begin[lo + 1]) {
-                const int m = members(c, lo) * a.per_kv, tile = m > a.wide_above ? kWideTile : TILE;
-                group = make_uint4(c.plan[lo], (uint32_t)(c.len[lo] + tile - 1) / tile, (uint32_t)c.begin[lo], (uint32_t)m);
-                own_part.z = (uint32_t)lo;
+                const int m = members(c, lo) * a.per_kv;
+                const bool wide = m > a.wide_above;
+                const int tile = wide ? kWideTile : TILE;
+                group = make_uint4(wide ? c.wide[lo] : c.plan[lo], (uint32_t)(c.len[lo] + tile - 1) / tile, (uint32_t)c.begin[lo], (uint32_t)m);
+                slot = (uint32_t)first_group_item(a, lo, c.begin[lo], wide ? kWideQueries : kPaQueries);
             }
-            a.plan[1 + 2 * b] = own_part;
-            a.plan[2 + 2 * b] = group;
+            a.plan[3 * b] = make_uint4(c.plan[a.groups + b], (uint32_t)(c.len[a.groups + b] + TILE - 1) / TILE, total, slot);
+            a.plan[3 * b + 1] = group;
+            a.plan[3 * b + 2] = make_uint4(wide_total, 0u, 0u, 0u);
         }
         __syncwarp();
     };
@@ -271,7 +307,8 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             if (lane == 0) mbar_arrive(heard + 8 * i);
             ++turns;
             if (run < 0) return kEnd;
-            if (warp == kPaWarps) begin_run(run);
+            if (warp == kPaWarps) ask();
+            if (warp == 0) leave_plan(run);
             walk.begin(a, c, cut, run);
         }
         return kSegment;
@@ -282,7 +319,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         uint32_t phase = 0;
         const int page_shift = (a.page_rows & (a.page_rows - 1)) == 0 ? 31 - __clz(a.page_rows) : -1;
         const auto page_of = [&](int row) { return page_shift >= 0 ? row >> page_shift : row / a.page_rows; };
-        begin_run(blockIdx.x);
+        ask();
         while (advance(s, true) == kSegment) {
             // page ids are read 32 at a time, a lane each
             const int last_page = page_of(s.n - 1);
@@ -366,6 +403,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     Segment nxt;
     auto more = advance(nxt, true);
     if (more == kSegment) ask_q(nxt);
+    if (warp == 0) leave_plan(blockIdx.x);                         // while the first tile is on its way
     while (more == kSegment) {
         s = nxt;
         uint32_t qa[KS][2];
@@ -514,7 +552,8 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     }
 }
 
-// One block per output row (batch row, query head): the states of the prefix units and of the row's own units.
+// An output row (batch row, query head) is merged by a block: the states of the prefix units and of the row's own units,
+// dealt to four warps.  (A warp per row instead: 109.8 us against 97.8 for 2048 rows of about 23 states.)
 template <typename T, int NSUB>
 __global__ void __launch_bounds__(kPaMergeThreads)
 prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32, float *lse)
@@ -523,49 +562,36 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     __shared__ float s_m[WARPS], s_l[WARPS], s_o[WARPS][DP];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int heads = a.kv_heads * a.per_kv;
-    const int b = blockIdx.x / heads, qh = blockIdx.x - b * heads, head = qh / a.per_kv, j = qh - head * a.per_kv;
+    const int b = (int)blockIdx.x / heads, qh = (int)blockIdx.x - b * heads, head = qh / a.per_kv, j = qh - head * a.per_kv;
+    const size_t row = blockIdx.x;
     pdl_wait();
     pdl_launch();
-    const uint32_t total = a.plan[0].x;
-    const uint4 own_part = a.plan[1 + 2 * b], group = a.plan[2 + 2 * b];
-    // runs of states: prefix, then own rows
-    const float *p_state = a.p_state, *p_ml = a.p_ml;
-    size_t p_first = 0, o_first = 0, p_slot = kPaQueries;
-    int p_segs = 0, p_step = 0, p_subs = 1, o_segs = 0;
+    const uint4 own_part = a.plan[3 * (size_t)b], group = a.plan[3 * (size_t)b + 1];
+    const uint32_t wide_total = a.plan[3 * (size_t)b + 2].x;
+    // the prefix's states, then the row's own
+    const int b0 = (int)group.z, m = (int)group.w;
+    const bool pre = group.y > 0, own = own_part.y > 0, wide = pre && m > a.wide_above;   // (y: tiles)
+    const int queries = wide ? kWideQueries : kPaQueries, mt = (m + queries - 1) / queries;
+    const int packed = (b - b0) * a.per_kv + j, q = packed / queries, p_rows = min(m - q * queries, queries), p_item = head * mt + q;
     const int own_mt = query_items(a.per_kv), own_q = j / kPaQueries, own_rows = min(a.per_kv - own_q * kPaQueries, kPaQueries);
-    const int o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
-    const Cut cut(total, (uint32_t)a.resident);
-    if (group.y > 0) {                       // tiles of the group's prefix
-        const int b0 = (int)group.z, m = (int)group.w, grp = (int)own_part.z;
-        const bool wide = m > a.wide_above;
-        const int queries = wide ? kWideQueries : kPaQueries, mt = (m + queries - 1) / queries;
-        const int packed = (b - b0) * a.per_kv + j, q = packed / queries, rows = min(m - q * queries, queries), item = head * mt + q;
-        uint32_t c0, c1;
-        if (wide) {
-            const Cut wide_cut(a.w_plan[a.groups], (uint32_t)a.w_resident, true);
-            const uint32_t u = a.w_plan[grp] + (uint32_t)item * group.y;
-            c0 = wide_cut.run_of(u); c1 = wide_cut.run_of(u + group.y - 1);
-            p_state = a.w_state; p_ml = a.w_ml;
-        } else {
-            const uint32_t u = group.x + (uint32_t)item * group.y;
-            c0 = cut.run_of(u); c1 = cut.run_of(u + group.y - 1);
-        }
-        const long long slot = (long long)first_group_item(a, grp, b0, queries) + item + c0;
-        p_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, (wide ? a.n_w_slots : a.n_p_slots) - slot));
-        p_subs = wide ? 1 : kPaWarps / query_warps(rows);
-        p_step = rows;
-        p_slot = queries;
-        p_first = (size_t)slot * p_slot + (packed - q * queries);
-    }
-    if (own_part.y > 0) {
-        const int item = head * own_mt + own_q;
-        const uint32_t u = own_part.x + (uint32_t)item * own_part.y, c0 = cut.run_of(u), c1 = cut.run_of(u + own_part.y - 1);
-        const long long slot = (long long)b * a.kv_heads * own_mt + item + c0;
-        o_segs = (int)min((long long)(c1 - c0 + 1), max(0LL, a.n_o_slots - slot));
-        o_first = (size_t)slot * o_step + (j - own_q * kPaQueries);
-    }
+    const int own_item = head * own_mt + own_q;
+    // first and last run of both, one division chain for all four: lanes 0, 1 the prefix's, 2, 3 the own rows'
+    const bool of_prefix = (lane & 2) == 0, of_wide = of_prefix && wide;
+    const uint32_t unit = (of_prefix ? group.x + (uint32_t)p_item * group.y : own_part.x + (uint32_t)own_item * own_part.y) +
+                          (lane & 1 ? (of_prefix ? group.y : own_part.y) - 1u : 0u);
+    const Cut cut(of_wide ? wide_total : own_part.z, (uint32_t)(of_wide ? a.w_resident : a.resident), of_wide);
+    const uint32_t run = (of_prefix ? pre : own) ? cut.run_of(unit) : 0u;
+    const uint32_t p0 = __shfl_sync(0xffffffffu, run, 0), p1 = __shfl_sync(0xffffffffu, run, 1), o0 = __shfl_sync(0xffffffffu, run, 2),
+                   o1 = __shfl_sync(0xffffffffu, run, 3);
+    const float *p_state = wide ? a.w_state : a.p_state, *p_ml = wide ? a.w_ml : a.p_ml;
+    const int p_subs = wide ? 1 : kPaWarps / query_warps(p_rows), p_step = p_rows, o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
+    const long long p_slot0 = (long long)own_part.w + p_item + p0, o_slot0 = (long long)b * a.kv_heads * own_mt + own_item + o0;
+    const int p_segs = pre ? (int)min((long long)(p1 - p0 + 1), max(0LL, (wide ? a.n_w_slots : a.n_p_slots) - p_slot0)) : 0;
+    const int o_segs = own ? (int)min((long long)(o1 - o0 + 1), max(0LL, a.n_o_slots - o_slot0)) : 0;
+    const size_t p_slot = queries, p_first = (size_t)p_slot0 * p_slot + (packed - q * queries);
+    const size_t o_first = (size_t)o_slot0 * o_step + (j - own_q * kPaQueries);
     const int n_p = p_segs * p_subs, n_states = n_p + o_segs * o_subs;
-    float m = -INFINITY, l = 0.f, o[PER];
+    float m_run = -INFINITY, l = 0.f, o[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) o[e] = 0.f;
     constexpr int AHEAD = 4;                // states in flight per warp
@@ -577,11 +603,11 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
             const int i = i0 + k * WARPS;
             ml[k] = make_float2(-INFINITY, 0.f);
             if (i < n_states) {
-                const bool pre = i < n_p;
-                const int at = pre ? i : i - n_p, subs = pre ? p_subs : o_subs, seg = at / subs, sub = at - seg * subs;
-                const size_t row = pre ? p_first + (size_t)seg * p_slot + (size_t)sub * p_step : o_first + (size_t)seg * o_step + (size_t)sub * own_rows;
-                ml[k] = *reinterpret_cast<const float2 *>((pre ? p_ml : a.o_ml) + 2 * row);
-                const float *st = (pre ? p_state : a.o_state) + row * DP;
+                const bool first = i < n_p;
+                const int at = first ? i : i - n_p, subs = first ? p_subs : o_subs, seg = at / subs, sub = at - seg * subs;
+                const size_t at_row = first ? p_first + (size_t)seg * p_slot + (size_t)sub * p_step : o_first + (size_t)seg * o_step + (size_t)sub * own_rows;
+                ml[k] = *reinterpret_cast<const float2 *>((first ? p_ml : a.o_ml) + 2 * at_row);
+                const float *st = (first ? p_state : a.o_state) + at_row * DP;
 #pragma unroll
                 for (int e = 0; e < PER; e += 2) *reinterpret_cast<float2 *>(&x[k][e]) = *reinterpret_cast<const float2 *>(st + e * 32 + 2 * lane);
             }
@@ -589,14 +615,15 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             if (ml[k].y == 0.f && ml[k].x == -INFINITY) continue;   // an empty state
-            const float M = fmaxf(m, ml[k].x), w1 = m == -INFINITY ? 0.f : pa_exp2(m - M), w2 = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
+            const float M = fmaxf(m_run, ml[k].x), w1 = m_run == -INFINITY ? 0.f : pa_exp2(m_run - M), w2 = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
             l = l * w1 + ml[k].y * w2;
 #pragma unroll
             for (int e = 0; e < PER; ++e) o[e] = o[e] * w1 + x[k][e] * w2;
-            m = M;
+            m_run = M;
         }
     }
-    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+    const bool empty = n_states == 0;
+    if (lane == 0) { s_m[warp] = m_run; s_l[warp] = l; }
 #pragma unroll
     for (int e = 0; e < PER; e += 2) *reinterpret_cast<float2 *>(&s_o[warp][e * 32 + 2 * lane]) = make_float2(o[e], o[e + 1]);
     __syncthreads();
@@ -609,16 +636,14 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
         wgt[w] = s_m[w] == -INFINITY ? 0.f : pa_exp2(s_m[w] - M);
         L += s_l[w] * wgt[w];
     }
-    const bool empty = n_states == 0;
     const float inv = empty ? 0.f : 1.f / L;
-    const size_t row = (size_t)b * heads + qh;
-    for (int e = threadIdx.x; e < a.d; e += kPaMergeThreads) {
-        float x = 0.f;
+    for (int e = 2 * threadIdx.x; e < a.d; e += 2 * kPaMergeThreads) {
+        float2 x = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) x += s_o[w][e] * wgt[w];
-        x = empty ? 0.f : x * inv;
-        if (out) out[row * a.d + e] = from_f32<T>(x);
-        if (out_f32) out_f32[row * a.d + e] = x;
+        for (int w = 0; w < WARPS; ++w) { x.x += s_o[w][e] * wgt[w]; x.y += s_o[w][e + 1] * wgt[w]; }
+        x = empty ? make_float2(0.f, 0.f) : make_float2(x.x * inv, x.y * inv);
+        if (out) *reinterpret_cast<uint32_t *>(out + row * a.d + e) = pack2<T>(x.x, x.y);
+        if (out_f32) *reinterpret_cast<float2 *>(out_f32 + row * a.d + e) = x;
     }
     if (lse && threadIdx.x == 0) lse[row] = empty ? -INFINITY : (M + log2f(L)) * 0.693147180559945309f;
 }
@@ -626,9 +651,9 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
 namespace {
 
 struct PrefixLayout {
-    size_t plan, p_state, p_ml, o_state, o_ml, w_plan, w_state, w_ml, bytes;
+    size_t plan, p_state, p_ml, o_state, o_ml, w_state, w_ml, bytes;
     long long p_slots, o_slots, w_slots;
-    int wide_blocks;                         // of the wide kernel; 0: no group can be large enough for it
+    int wide_blocks;                         // of the wide kernel; 0: the mean group is too small for it
     int nsub, blocks, max_runs;              // blocks that fit the GPU; runs of the largest call
 };
 
@@ -651,7 +676,7 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     o->nsub = (head_dim + 63) / 64;
     o->blocks = sm_count() * (o->nsub <= 2 ? 2 : 1);
     o->max_runs = 5 * o->blocks;
-    o->wide_blocks = groups && o->nsub <= 2 && (long long)batch * per_kv > kWideAbove ? 2 * sm_count() : 0;
+    o->wide_blocks = groups && o->nsub <= 2 && (long long)batch * per_kv > (long long)kWideAbove * groups ? 2 * sm_count() : 0;
     o->w_slots = o->wide_blocks ? ((long long)batch * per_kv / kWideQueries + groups) * kv_heads + o->wide_blocks : 0;
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     o->p_slots = groups ? ((long long)batch * per_kv / kPaQueries + groups) * kv_heads + o->max_runs : 0;
@@ -659,12 +684,11 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     const size_t dp = 64 * o->nsub, p_rows = (size_t)o->p_slots * kPaQueries, o_rows = (size_t)o->o_slots * own_slot_rows(per_kv);
     if (o->p_slots > 0x7fffffffLL || o->o_slots > 0x7fffffffLL || (long long)batch * n_heads > 0x7fffffffLL) return false;
     o->plan = 0;
-    o->p_state = o->plan + up((size_t)(1 + 2 * (size_t)batch) * 16);
+    o->p_state = o->plan + up((size_t)batch * 48);
     o->p_ml = o->p_state + up(p_rows * dp * 4);
     o->o_state = o->p_ml + up(p_rows * 8);
     o->o_ml = o->o_state + up(o_rows * dp * 4);
-    o->w_plan = o->o_ml + up(o_rows * 8);
-    o->w_state = o->w_plan + up((size_t)(groups + 1) * 4);
+    o->w_state = o->o_ml + up(o_rows * 8);
     o->w_ml = o->w_state + up((size_t)o->w_slots * kWideQueries * dp * 4);
     o->bytes = o->w_ml + up((size_t)o->w_slots * kWideQueries * 8);
     return true;
@@ -704,7 +728,7 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
 template <typename T, int NSUB, int STAGES, bool PACKED>
 cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
 {
-    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128 + (size_t)(2 * a.batch + 3 * a.groups + 2) * 4;
+    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128 + (size_t)(2 * a.batch + 4 * a.groups + 2) * 4;
     const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
@@ -757,9 +781,9 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     if (!layout_of(batch, n_groups, n_heads, kv->n_kv_heads, kv->head_dim, &l)) return ADSA_EINVAL;
     if (!q || !page_table || !n_rows || (!out && !out_f32) || !workspace || !(softmax_scale >= 0.f)) return ADSA_EINVAL;
     if (n_groups && (!prefix_table || !prefix_rows || !group_start || max_prefix_pages < 1)) return ADSA_EINVAL;
-    if (((uintptr_t)q & 3) || q_row % 2 || q_head % 2 || ((uintptr_t)workspace & 255) || ((uintptr_t)out & 1)) return ADSA_EINVAL;
+    if (((uintptr_t)q & 3) || q_row % 2 || q_head % 2 || ((uintptr_t)workspace & 255) || ((uintptr_t)out & 3) || ((uintptr_t)out_f32 & 7)) return ADSA_EINVAL;
     if (((uintptr_t)page_table | (uintptr_t)n_rows | (uintptr_t)prefix_table | (uintptr_t)prefix_rows | (uintptr_t)group_start |
-         (uintptr_t)out_f32 | (uintptr_t)lse | (uintptr_t)status) & 3)
+         (uintptr_t)lse | (uintptr_t)status) & 3)
         return ADSA_EINVAL;
     if ((long long)max_pages * kv->page_rows > 0x7fffffc0LL || (long long)max_prefix_pages * kv->page_rows > 0x7fffffc0LL) return ADSA_EINVAL;
     // the units of a call are counted in 32 bits
@@ -787,7 +811,7 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
     a.wide_above = l.wide_blocks ? kWideAbove : 0x7fffffff;
-    a.w_plan = (uint32_t *)(ws + l.w_plan); a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
+    a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
     a.n_w_slots = (int)l.w_slots; a.w_resident = l.wide_blocks; a.resident = l.blocks;
 
     // as many blocks as there can be runs, and no more than there can be units

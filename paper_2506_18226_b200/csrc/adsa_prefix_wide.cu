@@ -184,9 +184,6 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
         if (lane == 0) plan[a.groups] = before;
-        __syncwarp();
-        if (blockIdx.x == 0)
-            for (int g = lane; g <= a.groups; g += 32) a.w_plan[g] = plan[g];
     }
     tc_before();
     __syncthreads();
@@ -285,24 +282,34 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
     } else {                                                       // ---- a query row per thread ----
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         const int row = warp * 32 + lane;
+        const bool wide_q = a.d % 8 == 0 && (((uintptr_t)a.q | (uintptr_t)(a.q_row * 2) | (uintptr_t)(a.q_head * 2)) & 15) == 0;
         uint32_t s_phase = 0;
         while (walk.next(a, s)) {
             {
                 // the row of Q into shared memory, zero beyond the head elements and the group's rows
                 const int packed = s.row0 + row, b = packed / a.per_kv, j = packed - b * a.per_kv;
                 const T *qp = (const T *)a.q + b * a.q_row + (s.head * a.per_kv + j) * a.q_head;
-#pragma unroll 4
-                for (int ch = 0; ch < 8 * NSUB; ++ch) {
-                    uint32_t w[4];
+                uint4 w[8 * NSUB];                                 // the whole row is asked for at once
+                if (wide_q) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int e = ch * 8 + 2 * i;
-                        w[i] = row < s.rows && e < a.d ? __ldg(reinterpret_cast<const uint32_t *>(qp + e)) : 0u;
+                    for (int ch = 0; ch < 8 * NSUB; ++ch)
+                        w[ch] = row < s.rows && ch * 8 < a.d ? __ldg(reinterpret_cast<const uint4 *>(qp + ch * 8)) : make_uint4(0u, 0u, 0u, 0u);
+                } else {
+#pragma unroll
+                    for (int ch = 0; ch < 8 * NSUB; ++ch) {
+                        uint32_t *p = reinterpret_cast<uint32_t *>(&w[ch]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = ch * 8 + 2 * i;
+                            p[i] = row < s.rows && e < a.d ? __ldg(reinterpret_cast<const uint32_t *>(qp + e)) : 0u;
+                        }
                     }
+                }
+#pragma unroll
+                for (int ch = 0; ch < 8 * NSUB; ++ch)
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
                                  ::"r"(q_at + (uint32_t)(ch >> 3) * kSub + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) << 4)),
-                                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                }
+                                 "r"(w[ch].x), "r"(w[ch].y), "r"(w[ch].z), "r"(w[ch].w) : "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 tc_before();
                 __syncwarp();
@@ -390,8 +397,10 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
                 tc_load_wait();
                 if (fits && row < s.rows) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<float4 *>(a.w_state + at * DP + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    for (int i = 0; i < 32; i += 8)                // whole 32-byte sectors: a lane's neighbours write other rows
+                        asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                                     ::"l"(a.w_state + at * DP + c + i), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]), "f"(v[i + 4]),
+                                     "f"(v[i + 5]), "f"(v[i + 6]), "f"(v[i + 7]) : "memory");
                 }
             }
             tc_before();                                           // read before the next item's products write O

@@ -110,7 +110,7 @@ def _attn(kv=None, **kw):
 @pytest.mark.parametrize("kw", [dict(q=None), dict(table=None), dict(n_rows=None), dict(out=None), dict(ws=None), dict(ws=P + 128), dict(q=P + 2),
                                 dict(qr=255), dict(qh=65), dict(batch=-1), dict(batch=8192), dict(heads=3), dict(heads=1), dict(heads=130),
                                 dict(max_pages=0), dict(mpp=0), dict(pt=None), dict(pr=None), dict(start=None), dict(groups=-1), dict(groups=8191),
-                                dict(scale=-1.0), dict(scale=math.nan), dict(out=P + 1), dict(out32=P + 2), dict(lse=P + 1), dict(status=P + 1),
+                                dict(scale=-1.0), dict(scale=math.nan), dict(out=P + 2), dict(out32=P + 4), dict(lse=P + 1), dict(status=P + 1),
                                 dict(max_pages=2**27), dict(mpp=2**27)])
 def test_attention_refusals(kw):
     assert _attn(**kw) == B.EINVAL
