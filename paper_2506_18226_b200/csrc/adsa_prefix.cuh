@@ -10,7 +10,7 @@
 
 namespace adsa {
 
-constexpr int kWideQueries = 128;           // query rows of an item of the wide kernel
+constexpr int kWideQueries = 256;           // query rows of an item of the wide kernel: 128 for each of its two groups
 constexpr int kWideTile = 128;              // cached rows of a unit of the wide kernel
 
 struct PrefixArgs {
@@ -105,6 +105,19 @@ struct Cut {
         return min(k * resident + (p - (half - (half >> k)) * resident) / max(1u, half >> (k + 1u)), runs - 1u);
     }
 };
+
+// Items of a key head in the wide kernel's list: 256 query rows each, two units a tile; the last one, if it has 128 rows or
+// fewer, one unit a tile.
+struct WideItems {
+    int items;
+    uint32_t tiles, head_units;
+    __device__ __forceinline__ WideItems(int m, int n) : items((m + kWideQueries - 1) / kWideQueries), tiles((uint32_t)(n + kWideTile - 1) / kWideTile)
+    {
+        head_units = (uint32_t)(m + 127) / 128u * tiles;
+    }
+};
+// a run has two units or more, so the first unit of a tile
+__device__ __forceinline__ Cut wide_cut(uint32_t total, uint32_t resident) { return Cut(total, min(resident, max(total / 2u, 1u)), true); }
 
 cudaError_t launch_prefix_wide(int dtype, int nsub, const PrefixArgs &a, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st);
 

@@ -219,7 +219,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         c.plan[e] = mine.x;
         if (e < a.groups) c.wide[e] = mine.y;
         if (e < a.groups && m > a.wide_above)
-            mine.y += (uint32_t)((m + kWideQueries - 1) / kWideQueries) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + kWideTile - 1) / kWideTile);
+            mine.y += WideItems(m, c.len[e]).head_units * (uint32_t)a.kv_heads;
         else
             mine.x += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
     }
@@ -577,14 +577,22 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
     const int own_item = head * own_mt + own_q;
     // first and last run of both, one division chain for all four: lanes 0, 1 the prefix's, 2, 3 the own rows'
     const bool of_prefix = (lane & 2) == 0, of_wide = of_prefix && wide;
-    const uint32_t unit = (of_prefix ? group.x + (uint32_t)p_item * group.y : own_part.x + (uint32_t)own_item * own_part.y) +
-                          (lane & 1 ? (of_prefix ? group.y : own_part.y) - 1u : 0u);
-    const Cut cut(of_wide ? wide_total : own_part.z, (uint32_t)(of_wide ? a.w_resident : a.resident), of_wide);
+    uint32_t unit, units;                    // first unit of the item, and from there to the first unit of its last tile
+    if (of_wide) {
+        const uint32_t cost = p_rows > 128 ? 2u : 1u;
+        unit = group.x + (uint32_t)head * ((uint32_t)(m + 127) / 128u * group.y) + (uint32_t)q * 2u * group.y;
+        units = cost * (group.y - 1u);
+    } else {
+        unit = of_prefix ? group.x + (uint32_t)p_item * group.y : own_part.x + (uint32_t)own_item * own_part.y;
+        units = (of_prefix ? group.y : own_part.y) - 1u;
+    }
+    if (lane & 1) unit += units;
+    const Cut cut = of_wide ? wide_cut(wide_total, (uint32_t)a.w_resident) : Cut(own_part.z, (uint32_t)a.resident);
     const uint32_t run = (of_prefix ? pre : own) ? cut.run_of(unit) : 0u;
     const uint32_t p0 = __shfl_sync(0xffffffffu, run, 0), p1 = __shfl_sync(0xffffffffu, run, 1), o0 = __shfl_sync(0xffffffffu, run, 2),
                    o1 = __shfl_sync(0xffffffffu, run, 3);
     const float *p_state = wide ? a.w_state : a.p_state, *p_ml = wide ? a.w_ml : a.p_ml;
-    const int p_subs = wide ? 1 : kPaWarps / query_warps(p_rows), p_step = p_rows, o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
+    const int p_subs = wide ? (p_rows > 128 ? 1 : 2) : kPaWarps / query_warps(p_rows), p_step = wide ? 128 : p_rows, o_subs = kPaWarps / query_warps(own_rows), o_step = own_slot_rows(a.per_kv);
     const long long p_slot0 = (long long)own_part.w + p_item + p0, o_slot0 = (long long)b * a.kv_heads * own_mt + own_item + o0;
     const int p_segs = pre ? (int)min((long long)(p1 - p0 + 1), max(0LL, (wide ? a.n_w_slots : a.n_p_slots) - p_slot0)) : 0;
     const int o_segs = own ? (int)min((long long)(o1 - o0 + 1), max(0LL, a.n_o_slots - o_slot0)) : 0;
@@ -676,7 +684,7 @@ bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, P
     o->nsub = (head_dim + 63) / 64;
     o->blocks = sm_count() * (o->nsub <= 2 ? 2 : 1);
     o->max_runs = 5 * o->blocks;
-    o->wide_blocks = groups && o->nsub <= 2 && (long long)batch * per_kv > (long long)kWideAbove * groups ? 2 * sm_count() : 0;
+    o->wide_blocks = groups && o->nsub <= 2 && (long long)batch * per_kv > (long long)kWideAbove * groups ? sm_count() : 0;
     o->w_slots = o->wide_blocks ? ((long long)batch * per_kv / kWideQueries + groups) * kv_heads + o->wide_blocks : 0;
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     o->p_slots = groups ? ((long long)batch * per_kv / kPaQueries + groups) * kv_heads + o->max_runs : 0;
