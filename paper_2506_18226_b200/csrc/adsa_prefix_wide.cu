@@ -164,18 +164,17 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
     constexpr uint32_t kSub = kWideTile * 128, kTile = NSUB * kSub;   // bytes of a 64-element column of a tile, of a tile
     constexpr float kBias = WideBias<T>::value;
     extern __shared__ unsigned char wide_smem[];
-    __shared__ uint64_t bars[2 * SLOTS + 5];
+    __shared__ uint64_t bars[2 * SLOTS + 8];
     __shared__ uint32_t s_tmem;
     const uint32_t base = (smem_u32(wide_smem) + 1023u) & ~1023u;
     const uint32_t q_at = base, ring = base + 2 * kTile;
     uint32_t *plan = reinterpret_cast<uint32_t *>(wide_smem + (base - smem_u32(wide_smem)) + (size_t)(2 + SLOTS) * kTile);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, s_full = q_full + 8, p_full = s_full + 16;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, s_full = q_full + 16, p_full = s_full + 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
 
     if (tid == 0) {
         for (int i = 0; i < SLOTS; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
-        mbar_init(q_full, 8);
-        for (int g = 0; g < 2; ++g) { mbar_init(s_full + 8 * g, 1); mbar_init(p_full + 8 * g, 4); }
+        for (int g = 0; g < 2; ++g) { mbar_init(q_full + 8 * g, 4); mbar_init(s_full + 8 * g, 1); mbar_init(p_full + 16 * g, 4); mbar_init(p_full + 16 * g + 8, 4); }
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
@@ -252,7 +251,7 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
         const int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;
         const uint32_t s_shape = tc_shape<T>(kWideTile, false), o_shape = tc_shape<T>(d_cols, true);
         int slot = 0, valid = 0;
-        uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+        uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
         const auto take = [&]() {                                  // the next slot, once its tile is there
             wait(full + 8 * slot, phase);
             const int taken = slot;
@@ -285,23 +284,33 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
             return taken;
         };
         const auto weigh = [&](int g, int v_slot, bool first) {    // O += P V, once the group has left P
-            wait(p_full + 8 * g, p_phase[g]);
-            p_phase[g] ^= 1u;
-            tc_after();
             const uint64_t vd = tc_operand(ring + (uint32_t)v_slot * kTile, kSub);
-            if (tc_elect()) {
 #pragma unroll
-                for (int ks = 0; ks < kWideTile / 16; ++ks)
-                    tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, !first || ks > 0);
+            for (int half = 0; half < 2; ++half) {                 // P comes in two halves: the first is used while the second is made
+                wait(p_full + 16 * g + 8 * half, p_phase[g]);
+                tc_after();
+                if (tc_elect()) {
+#pragma unroll
+                    for (int k = 0; k < kWideTile / 32; ++k) {
+                        const int ks = half * (kWideTile / 32) + k;
+                        tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, !first || ks > 0);
+                    }
+                }
+                __syncwarp();
             }
+            p_phase[g] ^= 1u;
         };
         const auto done = [&](uint32_t bar) {                      // counted when everything issued so far is complete
             if (tc_elect()) tc_commit(bar);
             __syncwarp();
         };
         while (walk.next(a, s)) {
-            wait(q_full, q_phase);
-            q_phase ^= 1u;
+            wait(q_full, q_phase[0]);
+            q_phase[0] ^= 1u;
+            if (s.rows > 128) {
+                wait(q_full + 8, q_phase[1]);
+                q_phase[1] ^= 1u;
+            }
             tc_after();
             const int T_ = s.tiles;
             if (s.rows > 128) {
@@ -345,7 +354,7 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
     } else {                                                       // ---- a query row per thread ----
         const int g = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
-        const uint32_t my_s = s_full + 8 * g, my_p = p_full + 8 * g;
+        const uint32_t my_s = s_full + 8 * g, my_p = p_full + 16 * g;
         const bool wide_q = a.d % 8 == 0 && (((uintptr_t)a.q | (uintptr_t)(a.q_row * 2) | (uintptr_t)(a.q_head * 2)) & 15) == 0;
         uint32_t s_phase = 0;
         while (walk.next(a, s)) {
@@ -380,10 +389,11 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
                                  ::"r"(at + (uint32_t)(ch >> 3) * kSub + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) << 4)),
                                  "r"(w[ch].x), "r"(w[ch].y), "r"(w[ch].z), "r"(w[ch].w) : "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tc_before();
+                __syncwarp();
+                // (a group that has no Q to load must not arrive: with no tile either it may be an item ahead)
+                if (lane == 0) mbar_arrive(q_full + 8 * g);
             }
-            tc_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_full);
             float m = -INFINITY;                                   // raw units; the row's weights are relative to it
             float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             for (int i = 0; i < tiles; ++i) {
@@ -436,11 +446,13 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
                         p[k] = pack2<T>(x.x, x.y);
                     }
                     tc_store16(s_col + c / 2, p);                  // over scores that are in registers by now
+                    if (c % 64 == 32) {
+                        tc_store_wait();
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(my_p + 8 * (c / 64));
+                    }
                 }
-                tc_store_wait();
-                tc_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(my_p);
             }
             if (tiles > 0) {
                 wait(my_s, s_phase);

@@ -366,6 +366,8 @@ ATTN = {  # own rows, prefix rows, group starts, key heads, query heads per key 
     "two elements": ([30, 1], [7], [0, 2], 2, 1, 2, 16),
     "30 elements": ([30, 257], [70], [0, 2], 2, 2, 30, 40),
     "long": ([3, 9000], [20000], [0, 2], 2, 4, 128, 64),
+    "large groups of all sizes": ([2] * 513, [100, 700, 130, 1, 128], [0, 40, 180, 480, 480, 513], 3, 1, 64, 16),
+    "many large groups": ([1] * 480, list(range(1, 360, 30)), list(range(0, 481, 40)), 3, 1, 128, 32),
     "big batch": ([n % 90 for n in range(300)], [50, 60, 70], [0, 100, 200, 300], 2, 1, 64, 32),
 }
 
