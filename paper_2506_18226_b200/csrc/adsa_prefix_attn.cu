@@ -35,7 +35,12 @@ constexpr int kPaWarps = 4;                 // warps that compute; one more warp
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
 constexpr int kPaMaxEntries = 8192;         // groups + batch rows of a call
 constexpr int kPaMergeThreads = 128;
-constexpr int kWideAbove = 32;               // query rows of a key head from which a group's prefix goes to the wide kernel
+// A group's prefix goes to the wide kernel if the group has more query rows of a key head than fit one item here, where the
+// mean group has and the prefix tables hold at least 8192 rows of up to 64 elements (4096 of up to 128).  Two groups of 33
+// rows, 8 key heads of 128 (us, here / wide): 512 rows 19 / 20, 4096 36 / 29, 32768 129 / 66; of 128 rows: 34 / 40,
+// 62 / 55, 228 / 90; heads of 64, 33 rows: 17 / 19, 24 / 26, 76 / 57.  20 rows: 16 / 19, 25 / 27, 79 / 64.
+constexpr int kWideAbove = 32;
+constexpr long long kWideRows = 8192;
 
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
@@ -818,9 +823,10 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.p_state = (float *)(ws + l.p_state); a.p_ml = (float *)(ws + l.p_ml);
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
-    a.wide_above = l.wide_blocks ? kWideAbove : 0x7fffffff;
+    const bool wide = l.wide_blocks && (long long)max_prefix_pages * kv->page_rows * l.nsub >= kWideRows;
+    a.wide_above = wide ? kWideAbove : 0x7fffffff;
     a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
-    a.n_w_slots = (int)l.w_slots; a.w_resident = l.wide_blocks; a.resident = l.blocks;
+    a.n_w_slots = (int)l.w_slots; a.w_resident = wide ? l.wide_blocks : 0; a.resident = l.blocks;
 
     // as many blocks as there can be runs, and no more than there can be units
     const double units = own_units + (n_groups ? p_units : 0);

@@ -314,9 +314,10 @@ def check_attn(got, got32, lse, ref, dtype):
     assert ((lse.double() - want_lse).abs()[~empty] <= tol[~empty]).all()
 
 
-def attn_case(gen, own, prefix, start, kv, per, dim, page, dtype, stride=None, q_scale=1.5, clean=False):
+def attn_case(gen, own, prefix, start, kv, per, dim, page, dtype, stride=None, q_scale=1.5, room=0):
+    """room: rows the tables have room for beyond the longest (the choice of kernel goes by what they can hold)."""
     lengths = list(own) + list(prefix)
-    k_pool, v_pool, table = make_cache(gen, lengths, kv, page, dim, dtype, stride=stride, extra_pages=1)
+    k_pool, v_pool, table = make_cache(gen, lengths, kv, page, dim, dtype, stride=stride, extra_pages=1 + room // page)
     for i, n in enumerate(lengths):
         if n:
             r = torch.arange(n, device=DEV)
@@ -373,10 +374,11 @@ ATTN = {  # own rows, prefix rows, group starts, key heads, query heads per key 
 
 
 @pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("room", [0, 8192])
 @pytest.mark.parametrize("name", list(ATTN))
-def test_shared_prefix_attn_matches_64_bits(name, dtype):
+def test_shared_prefix_attn_matches_64_bits(name, room, dtype):
     own, prefix, start, kv, per, dim, page = ATTN[name]
-    c = attn_case(_gen(len(name)), own, prefix, start, kv, per, dim, page, dtype)
+    c = attn_case(_gen(len(name)), own, prefix, start, kv, per, dim, page, dtype, room=room)
     got = run_attn(c)
     ref = attn64(c["q"], c["k_pool"], c["v_pool"], c["page_table"], c["n_rows"], c["prefix_table"], c["prefix_rows"], c["group_start"],
                  1 / math.sqrt(dim))
