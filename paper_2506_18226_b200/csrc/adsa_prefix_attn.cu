@@ -4,23 +4,29 @@
 // own rows.  A softmax over a union of sets is the merge of the sets' own states (maximum m, sum l, weighted rows o):
 //   m = max m_s,  l = sum l_s 2^(m_s - m),  o = sum o_s 2^(m_s - m) / l
 // so the prefix is swept ONCE per group and key head, by all of the group's queries together (a real matrix product:
-// members x query heads per key head rows against the prefix), and each batch row's own rows by its queries alone.
+// members x query heads per key head rows against the prefix), and each batch row's own rows by its queries alone.  Long
+// prefixes of large groups go to a kernel of their own (adsa_prefix_wide.cu); everything else is swept here.
 //
-// Work split.  The unit is a tile of 128 (wider rows: 64) cached rows of one key head.  All units of a call (of every prefix, 32 query
-// rows at a time, then of every batch row) form one list; run c of C takes units c U / C .. (c + 1) U / C, whatever
-// they belong to, so long and short rows, prefixes and single rows mix without the host knowing a length.  Where a run
-// changes from one item to the next it leaves the item's partial state in the workspace; a second small kernel merges
-// the states of each output row.  Lengths, tables and group boundaries are read on the device: a captured graph follows
-// them.  A run is a block of the grid, and a grid has up to four times as many blocks as fit the GPU; a resident block that
-// has finished its run takes over one that has not started (cluster launch control), without refilling its pipeline.  SMs
-// differ in the bandwidth they get and items in their cost per tile: with one run per block the slowest block took 279 us
-// where the median took 225 (64 rows of 2304 x 32 heads x 100 elements).
+// Work split.  The unit is a tile of 128 (wider rows: 64) cached rows of one key head.  All units of a call (of every
+// prefix, 32 query rows at a time, then of every batch row) form one list that is cut into runs, whatever they belong to
+// (Cut), so long and short rows, prefixes and single rows mix without the host knowing a length.  Where a run changes from
+// one item to the next it leaves the item's partial state in the workspace; a small kernel merges the states of each output
+// row.  Lengths, tables and group boundaries are read on the device: a captured graph follows them.  A run is a block of the
+// grid, and a grid may have five times as many blocks as fit the GPU; a resident block that has finished its run takes
+// over one that has not started (cluster launch control), without refilling its pipeline.  SMs differ in the bandwidth
+// they get and items in their cost per tile: with one run per block the slowest block took 279 us where the median took
+// 225 (64 rows of 2304 x 32 heads x 100 elements).
 //
 // What a warp does per 16 cached rows: S^T = K Q^T and O^T += V^T P^T on mma.sync tiles with the cached rows as M and
 // eight query rows as N (the fewest that the instruction takes).  Up to 8 query rows of a key head: the four warps of a
-// block split the cached rows of a tile; up to 16: two and two; up to 32: each warp has its own eight query rows.  One query
-// row per cached row is 1 flop per byte: HBM bounds it, and the products run on the tensor cores only because that takes
-// the fewest instructions per byte.
+// block split the cached rows of a tile; up to 16: two and two; up to 32: each warp has its own eight query rows.  One
+// query row per cached row is 1 flop per byte: HBM bounds it, and the products run on the tensor cores only because that
+// takes the fewest instructions per byte.
+//
+// Measured in a captured graph: 64 rows x 32 heads of 100 elements over 2424 shared (four groups) and up to 2304 own rows,
+// 1.19 GB: 197 us, 6.0 TB/s.  32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39 us, of which 27 stream;
+// 2 us go by until the lengths are read and cut, 1.5 until the first tile, 4 in the merge, the rest between the launches.  Two
+// rows x 12 heads, 100 own rows: 8.7 us, a chain of five dependent reads in two kernels.
 #include <math.h>
 #include <type_traits>
 
@@ -41,7 +47,6 @@ constexpr int kPaMergeThreads = 128;
 // 62 / 55, 228 / 90; heads of 64, 33 rows: 17 / 19, 24 / 26, 76 / 57.  20 rows: 16 / 19, 25 / 27, 79 / 64.
 constexpr int kWideAbove = 32;
 constexpr long long kWideRows = 8192;
-
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
 __host__ __device__ __forceinline__ int query_warps(int m) { return m <= 8 ? 1 : m <= 16 ? 2 : 4; }
@@ -223,10 +228,8 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;
         c.plan[e] = mine.x;
         if (e < a.groups) c.wide[e] = mine.y;
-        if (e < a.groups && m > a.wide_above)
-            mine.y += WideItems(m, c.len[e]).head_units * (uint32_t)a.kv_heads;
-        else
-            mine.x += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
+        if (e < a.groups && m > a.wide_above) mine.y += WideItems(m, c.len[e]).head_units * (uint32_t)a.kv_heads;
+        else mine.x += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
     }
     uint2 incl = mine;
 #pragma unroll
@@ -592,8 +595,9 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
         units = (of_prefix ? group.y : own_part.y) - 1u;
     }
     if (lane & 1) unit += units;
-    const Cut cut = of_wide ? wide_cut(wide_total, (uint32_t)a.w_resident) : Cut(own_part.z, (uint32_t)a.resident);
-    const uint32_t run = (of_prefix ? pre : own) ? cut.run_of(unit) : 0u;
+    uint32_t run = 0u;
+    if (of_wide) run = WideCut(wide_total, (uint32_t)a.w_resident).run_of(unit);
+    else if (of_prefix ? pre : own) run = Cut(own_part.z, (uint32_t)a.resident).run_of(unit);
     const uint32_t p0 = __shfl_sync(0xffffffffu, run, 0), p1 = __shfl_sync(0xffffffffu, run, 1), o0 = __shfl_sync(0xffffffffu, run, 2),
                    o1 = __shfl_sync(0xffffffffu, run, 3);
     const float *p_state = wide ? a.w_state : a.p_state, *p_ml = wide ? a.w_ml : a.p_ml;

@@ -8,8 +8,13 @@
 // rows of K, elements contiguous).  One warp copies (TMA) and one thread issues all products, so that one group's products run
 // under the other's softmax.  An item is 256 query rows of a key head: both groups take every tile of K and V, each with its
 // own 128 rows, so a tile is fetched once for 256 rows; the last 128 or fewer rows of a group are an item whose tiles the
-// two groups take in turns.  (Two blocks of 128 rows per SM, each fetching its own tiles, spent the time waiting for
-// them: 50 us against DUOUS for 256 rows x 8 key heads over 32768 cached rows.)
+// two groups take in turns.
+//
+// 256 rows x 8 key heads of 128 over 32768 cached rows (34 GFLOP) stream in 24 us once every SM has its first tile,
+// 1.4 PFLOP/s; first tiles and the states at the end cost as much again as a third of that.  What bounds an iteration (128 cached
+// rows, both groups: 3580 cycles) is a group's own chain: 2200 cycles of softmax, of which 1024 are exponentials, then its
+// products, 1300 with what wakes them.  Descriptors have to stay in uniform registers: built by `lane == 0` in ordinary
+// ones, the same iteration took 4840 cycles, all of them the issuing thread's.
 //
 // The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units); until then weights up to
 // 2^8 are allowed, sums and products stay exact multiples, and O in tensor memory is rarely rescaled.
@@ -125,7 +130,7 @@ struct WideWalk {
     {
         plan = plan_;
         run = run_;
-        const Cut cut = wide_cut(plan[a.groups], (uint32_t)a.w_resident);
+        const WideCut cut(plan[a.groups], (uint32_t)a.w_resident);
         u = end = 0;
         if ((uint32_t)run < cut.runs) { u = cut.begin_of(run); end = cut.begin_of(run + 1); }
         e = 0;
