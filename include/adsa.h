@@ -490,7 +490,7 @@ ADSA_API int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_tabl
  *   out, out_f32 16-bit / float [batch][n_heads][head_dim], 4- / 8-byte aligned; either may be NULL, not both
  *   lse          float [batch][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
  * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).
- * batch + n_groups <= 8192.  workspace: [device] 256-byte aligned, adsa_shared_prefix_workspace_bytes of them, nothing
+ * batch + 2 n_groups <= 4096.  workspace: [device] 256-byte aligned, adsa_shared_prefix_workspace_bytes of them, nothing
  * kept in it from call to call: calls that may overlap on the GPU (other streams, graphs in flight) need one each, and a captured call's must outlive its graph. */
 ADSA_API int adsa_shared_prefix_workspace_bytes(int batch, int n_groups, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes);
 ADSA_API int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_row, long long q_head, int batch, int n_heads,

@@ -82,6 +82,20 @@ inline bool paged_kv_ok(const adsa_paged_kv *kv)
     return (long long)kv->n_pages * kv->n_kv_heads <= 0x7fffffffLL / kv->page_rows;   // rows are addressed by 32-bit coordinates
 }
 
+// Lets a kernel (with at most 512 bytes of static shared memory) use all of an SM's 227 KB on the current device; asks the
+// driver once per device.  told: one word per device, zero at first.
+inline cudaError_t allow_smem(const void *kernel, int (&told)[64])
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool known = dev >= 0 && dev < 64;
+    if (known && __atomic_load_n(&told[dev], __ATOMIC_ACQUIRE)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 512);
+    if (e == cudaSuccess && known) __atomic_store_n(&told[dev], 1, __ATOMIC_RELEASE);
+    return e;
+}
+
 template <typename... P, typename... A>
 inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A... args)
 {

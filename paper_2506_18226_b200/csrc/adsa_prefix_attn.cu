@@ -39,7 +39,7 @@ __host__ __device__ constexpr int tile_rows(int nsub) { return nsub == 1 ? 128 :
 constexpr int kPaQueries = 32;              // query rows of an item at most
 constexpr int kPaWarps = 4;                 // warps that compute; one more warp copies
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
-constexpr int kPaMaxEntries = 8192;         // groups + batch rows of a call
+constexpr int kPaMaxEntries = 4096;         // batch rows + twice the groups of a call: 8 bytes of shared memory each beside the tiles
 constexpr int kPaMergeThreads = 128;
 // A group's prefix goes to the wide kernel if the group has more query rows of a key head than fit one item here, where the
 // mean group has and the prefix tables hold at least 8192 rows of up to 64 elements (4096 of up to 128).  Two groups of 33
@@ -686,7 +686,7 @@ int sm_count()
 
 bool layout_of(int batch, int groups, int n_heads, int kv_heads, int head_dim, PrefixLayout *o)
 {
-    if (batch < 1 || groups < 0 || batch + (long long)groups > kPaMaxEntries || kv_heads < 1 || n_heads < kv_heads || n_heads % kv_heads ||
+    if (batch < 1 || groups < 0 || batch + 2LL * groups > kPaMaxEntries || kv_heads < 1 || n_heads < kv_heads || n_heads % kv_heads ||
         n_heads / kv_heads > 64 || head_dim < 2 || head_dim % 2 || head_dim > ADSA_MAX_HEAD_DIM)
         return false;
     const int per_kv = n_heads / kv_heads;
@@ -747,7 +747,8 @@ cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, const CUtensorMap 
 {
     const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128 + (size_t)(2 * a.batch + 4 * a.groups + 2) * 4;
     const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static int told[64];
+    cudaError_t e = allow_smem((const void *)kern, told);
     if (e != cudaSuccess) return e;
     e = launch_pdl(kern, dim3(runs), kPaThreads, smem, st, a, km, vm);
     if (e != cudaSuccess) return e;

@@ -502,7 +502,8 @@ cudaError_t launch_wide(const PrefixArgs &a, const CUtensorMap &km, const CUtens
 {
     const size_t smem = 1024 + (size_t)(2 + SLOTS) * NSUB * kWideTile * 128 + (size_t)(a.groups + 1) * 4;
     const auto kern = prefix_wide_kernel<T, NSUB, SLOTS>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static int told[64];
+    const cudaError_t e = allow_smem((const void *)kern, told);
     if (e != cudaSuccess) return e;
     return launch_pdl(kern, dim3((unsigned)a.w_resident), kWideThreads, smem, st, a, km, vm);
 }

@@ -400,6 +400,25 @@ def test_shared_prefix_attn_peaked_scores_scale_stride_and_strided_queries(dtype
     check_attn(*got, ref, dtype)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("batch,groups", [(4096, 0), (2, 2047), (2000, 1048)])
+def test_shared_prefix_attn_largest_batches(batch, groups, dim):
+    own = [(7 * b) % 40 for b in range(batch)]
+    start = sorted(((37 * g) % (batch + 1)) for g in range(groups + 1))
+    c = attn_case(_gen(batch + dim), own, [(5 * g) % 30 for g in range(groups)], start, 1, 1, dim, 16, torch.bfloat16, room=4096)
+    got = run_attn(c)
+    some = sorted({0, 1, batch // 3, batch - 2, batch - 1} - {-1})
+    ref = attn64(c["q"][some], c["k_pool"], c["v_pool"], c["page_table"][some], c["n_rows"][some], None, None, None, dim ** -0.5)
+    for i, b in enumerate(some):                                                  # (a group of one row each, in the reference)
+        g = [k for k in range(groups) if start[k] <= b < start[k + 1]]
+        if g:
+            one = attn64(c["q"][b:b + 1], c["k_pool"], c["v_pool"], c["page_table"][b:b + 1], c["n_rows"][b:b + 1], c["prefix_table"][g[0]:g[0] + 1],
+                         c["prefix_rows"][g[0]:g[0] + 1], torch.tensor([0, 1]), dim ** -0.5)
+            for whole, part in zip(ref, one):
+                whole[i] = part[0]
+    check_attn(*[x[some] for x in got], ref, torch.bfloat16)
+
+
 def test_shared_prefix_attn_equals_private_copies_of_the_prefix():
     """The same rows as one cache per batch row and no prefix: equal up to the merge's roundings."""
     import paper_2506_18226_b200 as A

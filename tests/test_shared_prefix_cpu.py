@@ -108,8 +108,8 @@ def _attn(kv=None, **kw):
 
 
 @pytest.mark.parametrize("kw", [dict(q=None), dict(table=None), dict(n_rows=None), dict(out=None), dict(ws=None), dict(ws=P + 128), dict(q=P + 2),
-                                dict(qr=255), dict(qh=65), dict(batch=-1), dict(batch=8192), dict(heads=3), dict(heads=1), dict(heads=130),
-                                dict(max_pages=0), dict(mpp=0), dict(pt=None), dict(pr=None), dict(start=None), dict(groups=-1), dict(groups=8191),
+                                dict(qr=255), dict(qh=65), dict(batch=-1), dict(batch=4095), dict(heads=3), dict(heads=1), dict(heads=130),
+                                dict(max_pages=0), dict(mpp=0), dict(pt=None), dict(pr=None), dict(start=None), dict(groups=-1), dict(groups=2048),
                                 dict(scale=-1.0), dict(scale=math.nan), dict(out=P + 2), dict(out32=P + 4), dict(lse=P + 1), dict(status=P + 1),
                                 dict(max_pages=2**27), dict(mpp=2**27)])
 def test_attention_refusals(kw):
@@ -124,7 +124,7 @@ def test_workspace_size_and_its_check():
     rc, small = size(2, 1, 4, 2, 64)
     assert rc == 0 and small > 0
     assert size(64, 1, 32, 8, 128)[1] > small
-    for bad in ((0, 1, 4, 2, 64), (2, -1, 4, 2, 64), (2, 1, 4, 3, 64), (2, 1, 4, 0, 64), (2, 1, 4, 2, 65), (2, 1, 4, 2, 258), (8192, 1, 4, 2, 64),
+    for bad in ((0, 1, 4, 2, 64), (2, -1, 4, 2, 64), (2, 1, 4, 3, 64), (2, 1, 4, 0, 64), (2, 1, 4, 2, 65), (2, 1, 4, 2, 258), (4095, 1, 4, 2, 64),
                 (2, 1, 130, 2, 64)):
         assert size(*bad)[0] == B.EINVAL
     assert A.load().adsa_shared_prefix_workspace_bytes(2, 1, 4, 2, 64, None) == B.EINVAL
