@@ -505,8 +505,8 @@ ADSA_API int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, lon
  *   h  = x' / sqrt(mean_j x'_j^2 + eps) * w_pre    (h and w_pre NULL: only x' is wanted)
  *   y, h         16-bit [rows][dim];  w_post, w_pre  16-bit [dim];  x, x_out  [rows][dim], 16-bit or ADSA_F32 (x_dtype)
  *   gate         16-bit [n_gates][dim], rows a multiple of n_gates: row r takes gate r / (rows / n_gates)
- * h is made from x' before x' is rounded.  x_out may be x, h may be y.  dim a multiple of 8, 8 .. 16384; all 16-byte
- * aligned. */
+ * h is made from x' before x' is rounded.  x_out may be x, h may be y.  dim a multiple of 8, 8 .. 16384; rows < 2^31; all
+ * 16-byte aligned. */
 ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const void *x, const void *w_post, const void *gate,
                                 long long n_gates, const void *w_pre, void *x_out, void *h, long long rows, int dim, float scale, float eps,
                                 adsa_stream_t stream);

@@ -41,6 +41,7 @@ constexpr int kPaWarps = 4;                 // warps that compute; one more warp
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
 constexpr int kPaMaxEntries = 4096;         // batch rows + twice the groups of a call: 8 bytes of shared memory each beside the tiles
 constexpr int kPaMergeThreads = 128;
+constexpr long long kPaMaxRows = 0x7fffff00LL;   // a sequence: row numbers stay in 32 bits past the last tile
 // A group's prefix goes to the wide kernel if the group has more query rows of a key head than fit one item here, where the
 // mean group has and the prefix tables hold at least 8192 rows of up to 64 elements (4096 of up to 128).  Two groups of 33
 // rows, 8 key heads of 128 (us, here / wide): 512 rows 19 / 20, 4096 36 / 29, 32768 129 / 66; of 128 rows: 34 / 40,
@@ -803,7 +804,7 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     if (((uintptr_t)page_table | (uintptr_t)n_rows | (uintptr_t)prefix_table | (uintptr_t)prefix_rows | (uintptr_t)group_start |
          (uintptr_t)lse | (uintptr_t)status) & 3)
         return ADSA_EINVAL;
-    if ((long long)max_pages * kv->page_rows > 0x7fffffc0LL || (long long)max_prefix_pages * kv->page_rows > 0x7fffffc0LL) return ADSA_EINVAL;
+    if ((long long)max_pages * kv->page_rows > kPaMaxRows || (long long)max_prefix_pages * kv->page_rows > kPaMaxRows) return ADSA_EINVAL;
     // the units of a call are counted in 32 bits
     const double own_units = (double)batch * kv->n_kv_heads * 2 * ((double)max_pages * kv->page_rows / tile_rows(l.nsub) + 1);
     const double p_units = ((double)batch * (n_heads / kv->n_kv_heads) / kPaQueries + n_groups) * kv->n_kv_heads *

@@ -146,7 +146,6 @@ cudaError_t launch_norm_residual(const void *y, const void *x, const void *w_pos
     const int row_threads = ((pieces + want - 1) / want + 31) / 32 * 32, np = (pieces + row_threads - 1) / row_threads;
     const int parts = row_threads > 32 ? 1 : 4;
     const long long blocks = (rows + parts - 1) / parts;
-    if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
     const unsigned threads = (unsigned)(parts * row_threads);
 #define ADSA_RES(N) \
@@ -167,7 +166,7 @@ extern "C" int adsa_norm_residual(int dtype, int x_dtype, const void *y, const v
                                   adsa_stream_t stream)
 {
     if ((dtype != ADSA_BF16 && dtype != ADSA_F16) || (x_dtype != dtype && x_dtype != ADSA_F32)) return ADSA_EINVAL;
-    if (rows < 0 || dim < 8 || dim % 8 || dim > ADSA_MAX_NORM_DIM || !(eps >= 0.f)) return ADSA_EINVAL;
+    if (rows < 0 || rows > 0x7fffffffLL || dim < 8 || dim % 8 || dim > ADSA_MAX_NORM_DIM || !(eps >= 0.f)) return ADSA_EINVAL;
     if (rows == 0) return ADSA_OK;
     if (!y || !x || !x_out || (h != nullptr) != (w_pre != nullptr)) return ADSA_EINVAL;
     if (gate && (n_gates < 1 || rows % n_gates)) return ADSA_EINVAL;

@@ -297,8 +297,12 @@ int run_turn(TurnArgs &a, const adsa_rotary &rot, int dtype, cudaStream_t st)
 
 bool rotary_ok(const adsa_rotary *r)
 {
-    return r && r->head_dim >= 2 && r->head_dim <= ADSA_MAX_HEAD_DIM && r->head_dim % 2 == 0 && r->n_axes >= 1 && r->n_axes <= 4 &&
-           r->n_pairs >= 0 && 2 * r->n_pairs <= r->head_dim;
+    if (!r || r->head_dim < 2 || r->head_dim > ADSA_MAX_HEAD_DIM || r->head_dim % 2 || r->n_axes < 1 || r->n_axes > 4 || r->n_pairs < 0 ||
+        2 * r->n_pairs > r->head_dim)
+        return false;
+    for (int i = 0; i < r->n_pairs; ++i)
+        if (r->axis[i] >= r->n_axes) return false;
+    return true;
 }
 
 bool rows_ok(const TurnRows &r) { return r.src && r.dst && !(((uintptr_t)r.src | (uintptr_t)r.dst) & 1); }

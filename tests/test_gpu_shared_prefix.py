@@ -367,6 +367,16 @@ ATTN = {  # own rows, prefix rows, group starts, key heads, query heads per key 
     "two elements": ([30, 1], [7], [0, 2], 2, 1, 2, 16),
     "30 elements": ([30, 257], [70], [0, 2], 2, 2, 30, 40),
     "long": ([3, 9000], [20000], [0, 2], 2, 4, 128, 64),
+    "40 elements": ([130, 7], [260], [0, 2], 2, 3, 40, 24),
+    "72 elements": ([130, 64, 1], [260], [0, 3], 2, 1, 72, 64),
+    "130 elements": ([90, 63], [129], [0, 2], 2, 2, 130, 48),
+    "200 elements": ([65, 1], [70], [0, 2], 1, 4, 200, 10),
+    "forty query heads": ([70, 1, 200], [100, 30], [0, 1, 3], 2, 40, 64, 64),
+    "large group, 100 elements": ([5] * 50, [900], [0, 50], 2, 2, 100, 48),
+    "large group, 72 elements": ([1] * 70, [1500], [0, 70], 2, 4, 72, 64),
+    "large group, 30 elements": ([2] * 40, [513, 3], [0, 39, 40], 1, 1, 30, 16),
+    "large groups, one without rows": ([2] * 90, [0, 400], [0, 45, 90], 2, 1, 64, 16),
+    "large group, pages of seven": ([2] * 300, [385], [0, 300], 1, 1, 128, 7),
     "large groups of all sizes": ([2] * 513, [100, 700, 130, 1, 128], [0, 40, 180, 480, 480, 513], 3, 1, 64, 16),
     "many large groups": ([1] * 480, list(range(1, 360, 30)), list(range(0, 481, 40)), 3, 1, 128, 32),
     "big batch": ([n % 90 for n in range(300)], [50, 60, 70], [0, 100, 200, 300], 2, 1, 64, 32),
@@ -388,13 +398,14 @@ def test_shared_prefix_attn_matches_64_bits(name, room, dtype):
 
 
 @pytest.mark.parametrize("dtype", HALF)
-def test_shared_prefix_attn_peaked_scores_scale_stride_and_strided_queries(dtype):
+@pytest.mark.parametrize("rows,room", [(3, 0), (50, 8192)])
+def test_shared_prefix_attn_peaked_scores_scale_stride_and_strided_queries(rows, room, dtype):
     """Scores in the tens (one row takes nearly all the weight, and the maximum keeps moving), a scale of the caller's,
-    padded pool rows that hold NaN, query rows out of a packed tensor."""
+    padded pool rows that hold NaN, query rows out of a packed tensor that start on 4-byte boundaries only."""
     g = _gen(21)
-    c = attn_case(g, [70, 200, 33], [300], [0, 3], 2, 4, 100, 24, dtype, stride=136, q_scale=2.0)
-    packed = _randn(g, 3, 2, 30, 100, dtype=dtype, scale=2.0)
-    c["q"] = packed[:, 1, 3:19:2]
+    c = attn_case(g, [(70, 200, 33)[b % 3] for b in range(rows)], [300], [0, rows], 2, 4, 100, 24, dtype, stride=136, q_scale=2.0, room=room)
+    packed = _randn(g, rows, 2, 30, 102, dtype=dtype, scale=2.0)
+    c["q"] = packed[:, 1, 3:19:2, 2:]
     got = run_attn(c, scale=0.7)
     ref = attn64(c["q"], c["k_pool"], c["v_pool"], c["page_table"], c["n_rows"], c["prefix_table"], c["prefix_rows"], c["group_start"], 0.7)
     check_attn(*got, ref, dtype)
@@ -460,12 +471,13 @@ def test_shared_prefix_attn_lengths_and_boundaries_the_device_finds_wrong():
     assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
 
 
-def test_shared_prefix_attn_replays_with_new_lengths_and_groups():
+@pytest.mark.parametrize("per,room", [(2, 0), (40, 8192)])
+def test_shared_prefix_attn_replays_with_new_lengths_and_groups(per, room):
     """One captured call follows lengths, tables, boundaries and queries; another graph with a workspace of its own may
     run beside it."""
     import paper_2506_18226_b200 as A
     g = _gen(51)
-    a = attn_case(g, [100, 37, 64, 1], [90, 200], [0, 2, 4], 2, 2, 64, 32, torch.bfloat16)
+    a = attn_case(g, [100, 37, 64, 1], [90, 200], [0, 2, 4], 2, per, 64, 32, torch.bfloat16, room=room)
     out = torch.empty_like(a["q"])
     graphs = []
     for _ in range(2):

@@ -51,6 +51,19 @@ def _rope(**kw):
     return A.load().adsa_rope_axes(*a.values(), None)
 
 
+def test_a_rotary_with_an_axis_it_does_not_have_is_refused():
+    r = _rot()[1]
+    r.axis[5] = 2
+    assert _rope(rot=C.byref(r)) == B.EINVAL and _append(rot=C.byref(r), pos=P) == B.EINVAL
+
+
+def test_the_header_is_plain_c():
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-fsyntax-only", "-x", "c", os.path.join(root, "include", "adsa.h")], check=True)
+
+
 @pytest.mark.parametrize("kw", [dict(rot=None), dict(dtype=2), dict(dtype=-1), dict(x=None), dict(out=None), dict(pos=None), dict(tokens=-1),
                                 dict(heads=-1), dict(x=P + 1), dict(out=P + 1), dict(pos=P + 2), dict(out=P, ot=256)])
 def test_rope_axes_refusals(kw):
@@ -111,7 +124,7 @@ def _attn(kv=None, **kw):
                                 dict(qr=255), dict(qh=65), dict(batch=-1), dict(batch=4095), dict(heads=3), dict(heads=1), dict(heads=130),
                                 dict(max_pages=0), dict(mpp=0), dict(pt=None), dict(pr=None), dict(start=None), dict(groups=-1), dict(groups=2048),
                                 dict(scale=-1.0), dict(scale=math.nan), dict(out=P + 2), dict(out32=P + 4), dict(lse=P + 1), dict(status=P + 1),
-                                dict(max_pages=2**27), dict(mpp=2**27)])
+                                dict(max_pages=2**27), dict(mpp=2**27), dict(max_pages=2**27 - 8)])
 def test_attention_refusals(kw):
     assert _attn(**kw) == B.EINVAL
 
@@ -138,7 +151,7 @@ def _norm(**kw):
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=2), dict(xdtype=1), dict(xdtype=3), dict(y=None), dict(x=None), dict(x_out=None), dict(h=None), dict(w_pre=None),
-                                dict(n_gates=3), dict(n_gates=0), dict(rows=-1), dict(dim=60), dict(dim=0), dict(dim=16392), dict(eps=-1.0),
+                                dict(n_gates=3), dict(n_gates=0), dict(rows=-1), dict(rows=2**31), dict(dim=60), dict(dim=0), dict(dim=16392), dict(eps=-1.0),
                                 dict(eps=math.nan), dict(y=P + 8), dict(gate=P + 2), dict(x_out=P + 4)])
 def test_norm_residual_refusals(kw):
     assert _norm(**kw) == B.EINVAL
