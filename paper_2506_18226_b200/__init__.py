@@ -19,4 +19,4 @@ from .binding import (  # noqa: F401
     swiglu,
     workspace_bytes,
 )
-from .build import build_lib  # noqa: F401
+from .build import build_lib, build_marshal  # noqa: F401

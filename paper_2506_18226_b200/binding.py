@@ -2,26 +2,24 @@
 
 Every step of the path (scoring, selection, attention, cache update, paging)
 runs inside the CUDA kernels of libadsa.so; this module turns torch tensors
-into device pointers and calls the C functions of the same names.  torch is
-used for device memory and streams, nothing else.  There is no CPU fallback:
+into device pointers and calls the C functions of the same names (ctypes; the
+four calls of a decode step on a shared prefix through a small C++ module).
+torch is used for device memory and streams, nothing else.  There is no CPU fallback:
 if the library cannot be loaded or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
 import ctypes as C
-import struct
 
 import torch
 
-from .build import build_lib
+from .build import build_lib, build_marshal
 
 OK, EINVAL, ESTATE, ENOMEM, ECUDA = 0, -1, -2, -3, -4
 DEV_POOL_EXHAUSTED, DEV_BAD_POSITION, DEV_ROW_OVERFLOW, DEV_RING_TIMEOUT, DEV_BAD_EVICT, DEV_COPY_TIMEOUT = \
     1, 2, 4, 8, 16, 32
 DEV_BAD_PAGE, DEV_BAD_GROUPS = 64, 128
 BF16, F16, F32 = 0, 1, 2
-_DTYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
-_DTYPES16 = {torch.bfloat16: BF16, torch.float16: F16}
 
 EXPORTS = [
     "adsa_workspace_bytes", "adsa_create", "adsa_destroy", "adsa_reset", "adsa_prefill_rows",
@@ -64,12 +62,11 @@ class AdsaError(RuntimeError):
 
 
 _lib = None
-_fns = {}                                      # functions by name, looked up once
 
 
 def load(rebuild: bool = False) -> C.CDLL:
     """Load libadsa.so, building it first if it is missing or older than its sources."""
-    global _lib
+    global _lib, _marshal_module
     if _lib is None or rebuild:
         lib = C.CDLL(build_lib(rebuild))
         vp, i32, sz, ll = C.c_void_p, C.c_int, C.c_size_t, C.c_longlong
@@ -120,7 +117,7 @@ def load(rebuild: bool = False) -> C.CDLL:
         lib.adsa_launch_count.argtypes, lib.adsa_launch_count.restype = [vp], C.c_int64
         lib.adsa_strerror.argtypes, lib.adsa_strerror.restype = [C.c_int], C.c_char_p
         _lib = lib
-        _fns.clear()
+        _marshal_module = None                 # it holds the other library's functions
     return _lib
 
 
@@ -198,44 +195,25 @@ def cfg_sample(logits, scale, top_k, temperature, uniforms, tokens=None):
 
 # ---- many images of one prompt: rotary positions, paged append, shared-prefix attention, norms with the residual ----
 
-# A decode step makes these calls once per layer, so what a call checks is written for speed: one combined condition, and
-# only where it fails the messages of _refuse.
+# A decode step makes these calls once per layer, so their tensors are read and checked in C++ (adsa_marshal.cpp): what is
+# not as it should be raises ValueError; a status comes back as an int.
 
-_I32 = torch.int32
-_KV = struct.Struct("PP6i")                    # adsa_paged_kv
-
-
-def _fn(name):
-    fn = _fns.get(name)
-    if fn is None or _lib is None:
-        fn = _fns[name] = getattr(load(), name)
-    return fn
+_marshal_module = None
 
 
-def _launch(name, dev, *args):
-    """Call a stateless function on CUDA device `dev` and torch's current stream there."""
-    if dev == torch._C._cuda_getDevice():
-        rc = _fn(name)(*args, torch._C._cuda_getCurrentRawStream(dev))
-    else:
-        with torch.cuda.device(dev):
-            rc = _fn(name)(*args, torch._C._cuda_getCurrentRawStream(dev))
-    if rc:
-        raise AdsaError(rc, name)
-
-
-def _refuse(call, dev, *wants):
-    """Names the first tensor that is not what a call wants: (name, tensor, type, shape with None for any size, whole:
-    dense throughout, else along the last dimension)."""
-    for name, t, dtype, shape, whole in wants:
-        if t is None:
-            continue
-        if t.dtype is not dtype or t.dim() != len(shape) or any(w is not None and w != s for w, s in zip(shape, t.shape)):
-            raise ValueError(f"{call}: {name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-        if not (t.is_contiguous() if whole else t.stride(-1) == 1):
-            raise ValueError(f"{call}: {name} must be dense{'' if whole else ' along its last dimension'}")
-        if t.get_device() != dev or dev < 0:
-            raise ValueError(f"{call}: {name} must be on a CUDA device, the same for all tensors")
-    raise ValueError(f"{call}: bad arguments")
+def _marshal():
+    global _marshal_module
+    if _marshal_module is None:
+        import importlib.machinery
+        import importlib.util
+        lib = load()
+        loader = importlib.machinery.ExtensionFileLoader("adsa_marshal", build_marshal())
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("adsa_marshal", loader))
+        loader.exec_module(module)
+        module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value for name in (
+            "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn", "adsa_norm_residual")))
+        _marshal_module = module
+    return _marshal_module
 
 
 class Rotary:
@@ -259,22 +237,10 @@ class Rotary:
 def rope_axes(rotary, x, pos, out=None):
     """adsa_rope_axes: x [n_tokens, n_heads, head_dim] (any token and head stride) turned by pos, int32
     [n_tokens, n_axes].  out may be x; default: a new tensor."""
-    dtype, shape, dev = x.dtype, x.shape, x.get_device()
-    code = _DTYPES16.get(dtype)
-    if len(shape) != 3 or code is None:
-        raise ValueError(f"rope_axes: x must be bfloat16 or float16 [n_tokens, n_heads, head_dim], got {dtype} {list(shape)}")
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=x.device)
-    tokens, heads, d = shape
-    n_axes = rotary.n_axes
-    x0, x1, x2 = x.stride()
-    o = out.stride()
-    if (d != rotary.head_dim or x2 != 1 or out.shape != shape or out.dtype is not dtype or o[2] != 1 or pos.dtype is not _I32
-            or pos.shape != (tokens, n_axes) or not pos.is_contiguous() or dev < 0 or out.get_device() != dev or pos.get_device() != dev):
-        _refuse("rope_axes", dev, ("x", x, dtype, (tokens, heads, rotary.head_dim), False), ("out", out, dtype, shape, False),
-                ("pos", pos, _I32, (tokens, n_axes), True))
-    _launch("adsa_rope_axes", dev, rotary.ref, code, x.data_ptr(), x0, x1, pos.data_ptr(), tokens, heads, out.data_ptr(), o[0], o[1])
-    return out
+    r = (_marshal_module or _marshal()).rope_axes(rotary.ref, x, pos, out)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_rope_axes")
+    return r
 
 
 def paged_append(k, v, k_pool, v_pool, page_table, n_rows, *, cu_tokens=None, rotary=None, pos=None, q=None, q_out=None,
@@ -285,54 +251,11 @@ def paged_append(k, v, k_pool, v_pool, page_table, n_rows, *, cu_tokens=None, ro
     page_table int32 [batch, max_pages]; n_rows int32 [batch], rows before the call (not changed); cu_tokens int32
     [batch + 1] or None (the same number of tokens for every batch row).  status: int32 [1] that device-side errors are
     ORed into.  Returns q_out (a new tensor by default, q itself to turn in place), None without q."""
-    dtype, shape, dev = k.dtype, k.shape, k.get_device()
-    code, pool, tables = _DTYPES16.get(dtype), k_pool.shape, page_table.shape
-    if len(shape) != 3 or len(pool) != 4 or len(tables) != 2 or code is None:
-        raise ValueError(f"paged_append: k must be bfloat16 or float16 [n_tokens, n_kv_heads, head_dim], the pools [n_pages, n_kv_heads, "
-                         f"page_rows, row_stride], page_table [batch, max_pages]; got {dtype} {list(shape)}, {list(pool)}, {list(tables)}")
-    tokens, kv_heads, d = shape
-    pages, pool_heads, page_rows, stride = pool
-    batch, max_pages = tables
-    k0, k1, k2 = k.stride()
-    v0, v1, v2 = v.stride()
-    ok = (pool_heads == kv_heads and k2 == 1 and v2 == 1 and v.shape == shape and v.dtype is dtype and k_pool.dtype is dtype
-          and v_pool.dtype is dtype and v_pool.shape == pool and k_pool.is_contiguous() and v_pool.is_contiguous()
-          and page_table.dtype is _I32 and page_table.is_contiguous() and n_rows.dtype is _I32 and n_rows.shape == (batch,)
-          and n_rows.is_contiguous() and dev >= 0 and v.get_device() == dev and k_pool.get_device() == dev and v_pool.get_device() == dev
-          and page_table.get_device() == dev and n_rows.get_device() == dev)
-    cu_at = rot = pos_at = status_at = q_at = qo_at = None
-    if cu_tokens is not None:
-        ok = ok and cu_tokens.dtype is _I32 and cu_tokens.shape == (batch + 1,) and cu_tokens.is_contiguous() and cu_tokens.get_device() == dev
-        cu_at = cu_tokens.data_ptr()
-    if rotary is not None:
-        if rotary.head_dim != d or pos is None:
-            raise ValueError("paged_append: the rotary needs pos and the head dimension of k")
-        ok = ok and pos.dtype is _I32 and pos.shape == (tokens, rotary.n_axes) and pos.is_contiguous() and pos.get_device() == dev
-        rot, pos_at = rotary.ref, pos.data_ptr()
-    heads = q0 = q1 = o0 = o1 = 0
-    if q is not None:
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        q_shape, qs, os = q.shape, q.stride(), q_out.stride()
-        ok = (ok and len(q_shape) == 3 and q_shape[0] == tokens and q_shape[2] == d and qs[2] == 1 and q.dtype is dtype and q_out.shape == q_shape
-              and q_out.dtype is dtype and os[2] == 1 and q.get_device() == dev and q_out.get_device() == dev)
-        if ok:
-            heads, q0, q1, o0, o1 = q_shape[1], qs[0], qs[1], os[0], os[1]
-        q_at, qo_at = q.data_ptr(), q_out.data_ptr()
-    if status is not None:
-        ok = ok and status.dtype is _I32 and status.numel() == 1 and status.get_device() == dev
-        status_at = status.data_ptr()
-    if not ok:
-        n_heads = None if q is None or q.dim() != 3 else q.shape[1]
-        _refuse("paged_append", dev, ("k", k, dtype, (tokens, pool_heads, d), False), ("v", v, dtype, shape, False), ("k_pool", k_pool, dtype, pool, True),
-                ("v_pool", v_pool, dtype, pool, True), ("page_table", page_table, _I32, tables, True), ("n_rows", n_rows, _I32, (batch,), True),
-                ("cu_tokens", cu_tokens, _I32, (batch + 1,), True), ("pos", pos if rotary else None, _I32, (tokens, rotary.n_axes if rotary else 0), True),
-                ("q", q, dtype, (tokens, n_heads, d), False), ("q_out", q_out if q is not None else None, dtype, (tokens, n_heads, d), False),
-                ("status", status, _I32, (1,), True))
-    _launch("adsa_paged_append", dev, _KV.pack(k_pool.data_ptr(), v_pool.data_ptr(), code, pages, kv_heads, page_rows, d, stride),
-            page_table.data_ptr(), batch, max_pages, n_rows.data_ptr(), cu_at, tokens, k.data_ptr(), k0, k1, v.data_ptr(), v0, v1, rot, pos_at,
-            q_at, heads, q0, q1, qo_at, o0, o1, status_at)
-    return q_out if q is not None else None
+    r = (_marshal_module or _marshal()).paged_append(k, v, k_pool, v_pool, page_table, n_rows, cu_tokens, None if rotary is None else rotary.ref,
+                                                     pos, q, q_out, status)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_paged_append")
+    return r
 
 
 def shared_prefix_workspace(q, k_pool, page_table, prefix_table=None):
@@ -355,58 +278,12 @@ def shared_prefix_attn(q, k_pool, v_pool, page_table, n_rows, prefix_table=None,
     page_table int32 [batch, max_pages], n_rows int32 [batch]; prefix_table int32 [n_groups, max_prefix_pages],
     prefix_rows int32 [n_groups], group_start int32 [n_groups + 1] (all three None: no prefix).  out 16-bit or out_f32
     float [batch, n_heads, head_dim] (default: a new tensor like q), lse float [batch, n_heads].  workspace: from
-    shared_prefix_workspace; None takes one from torch's allocator for this call."""
-    dtype, shape, dev = q.dtype, q.shape, q.get_device()
-    code, pool, tables = _DTYPES16.get(dtype), k_pool.shape, page_table.shape
-    if len(shape) != 3 or len(pool) != 4 or len(tables) != 2 or code is None:
-        raise ValueError(f"shared_prefix_attn: q must be bfloat16 or float16 [batch, n_heads, head_dim], the pools [n_pages, n_kv_heads, "
-                         f"page_rows, row_stride], page_table [batch, max_pages]; got {dtype} {list(shape)}, {list(pool)}, {list(tables)}")
-    batch, heads, d = shape
-    pages, kv_heads, page_rows, stride = pool
-    q0, q1, q2 = q.stride()
-    if out is None and out_f32 is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
-    ok = (q2 == 1 and k_pool.dtype is dtype and v_pool.dtype is dtype and v_pool.shape == pool and k_pool.is_contiguous() and v_pool.is_contiguous()
-          and tables[0] == batch and page_table.dtype is _I32 and page_table.is_contiguous() and n_rows.dtype is _I32
-          and n_rows.shape == (batch,) and n_rows.is_contiguous() and dev >= 0 and k_pool.get_device() == dev and v_pool.get_device() == dev
-          and page_table.get_device() == dev and n_rows.get_device() == dev)
-    groups = max_pp = 0
-    pt_at = pr_at = gs_at = out_at = o32_at = lse_at = status_at = None
-    if prefix_table is not None:
-        if prefix_table.dim() != 2 or prefix_rows is None or group_start is None:
-            raise ValueError("shared_prefix_attn: a prefix needs prefix_table [n_groups, max_prefix_pages], prefix_rows and group_start")
-        groups, max_pp = prefix_table.shape
-        ok = (ok and prefix_table.dtype is _I32 and prefix_table.is_contiguous() and prefix_rows.dtype is _I32 and prefix_rows.shape == (groups,)
-              and prefix_rows.is_contiguous() and group_start.dtype is _I32 and group_start.shape == (groups + 1,) and group_start.is_contiguous()
-              and prefix_table.get_device() == dev and prefix_rows.get_device() == dev and group_start.get_device() == dev)
-        pt_at, pr_at, gs_at = prefix_table.data_ptr(), prefix_rows.data_ptr(), group_start.data_ptr()
-    if out is not None:
-        ok = ok and out.dtype is dtype and out.shape == shape and out.is_contiguous() and out.get_device() == dev
-        out_at = out.data_ptr()
-    if out_f32 is not None:
-        ok = ok and out_f32.dtype is torch.float32 and out_f32.shape == shape and out_f32.is_contiguous() and out_f32.get_device() == dev
-        o32_at = out_f32.data_ptr()
-    if lse is not None:
-        ok = ok and lse.dtype is torch.float32 and lse.shape == (batch, heads) and lse.is_contiguous() and lse.get_device() == dev
-        lse_at = lse.data_ptr()
-    if status is not None:
-        ok = ok and status.dtype is _I32 and status.numel() == 1 and status.get_device() == dev
-        status_at = status.data_ptr()
-    if workspace is not None:
-        ok = ok and workspace.is_contiguous() and workspace.get_device() == dev
-    if not ok:
-        _refuse("shared_prefix_attn", dev, ("q", q, dtype, shape, False), ("k_pool", k_pool, dtype, pool, True), ("v_pool", v_pool, dtype, pool, True),
-                ("page_table", page_table, _I32, (batch, None), True), ("n_rows", n_rows, _I32, (batch,), True),
-                ("prefix_table", prefix_table, _I32, (groups, max_pp), True), ("prefix_rows", prefix_rows, _I32, (groups,), True),
-                ("group_start", group_start, _I32, (groups + 1,), True), ("out", out, dtype, shape, True), ("out_f32", out_f32, torch.float32, shape, True),
-                ("lse", lse, torch.float32, (batch, heads), True), ("status", status, _I32, (1,), True),
-                ("workspace", workspace, workspace.dtype if workspace is not None else None, tuple(workspace.shape) if workspace is not None else (), True))
-    if workspace is None:
-        workspace = shared_prefix_workspace(q, k_pool, page_table, prefix_table) if batch else torch.empty(0, dtype=torch.uint8, device=q.device)
-    _launch("adsa_shared_prefix_attn", dev, _KV.pack(k_pool.data_ptr(), v_pool.data_ptr(), code, pages, kv_heads, page_rows, d, stride),
-            q.data_ptr(), q0, q1, batch, heads, page_table.data_ptr(), tables[1], n_rows.data_ptr(), pt_at, max_pp, pr_at, gs_at, groups, scale,
-            out_at, o32_at, lse_at, workspace.data_ptr(), workspace.nbytes, status_at)
-    return out if out is not None else out_f32
+    shared_prefix_workspace; None takes one from torch's allocator for this call.  Returns out, or out_f32 without one."""
+    r = (_marshal_module or _marshal()).shared_prefix_attn(q, k_pool, v_pool, page_table, n_rows, prefix_table, prefix_rows, group_start, scale,
+                                                           out, out_f32, lse, workspace, status)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_shared_prefix_attn")
+    return r
 
 
 def norm_residual(y, x, w_pre=None, *, w_post=None, gate=None, scale=1.0, eps=1e-5, x_out=None, h=None):
@@ -415,38 +292,10 @@ def norm_residual(y, x, w_pre=None, *, w_post=None, gate=None, scale=1.0, eps=1e
     y [rows, dim] 16-bit, x [rows, dim] of the same type or float32; w_post [dim] or None (no norm on y); gate
     [n_gates, dim] (rows / n_gates rows take each) or None; w_pre [dim] or None (then h is None).  x_out may be x, h
     may be y; by default both are new."""
-    dtype, shape, dev = y.dtype, y.shape, y.get_device()
-    code, x_dtype = _DTYPES16.get(dtype), x.dtype
-    if len(shape) != 2 or code is None or (x_dtype is not dtype and x_dtype is not torch.float32):
-        raise ValueError(f"norm_residual: y must be bfloat16 or float16 [rows, dim] and x of its type or float32, got {dtype} {list(shape)} and {x_dtype}")
-    rows, dim = shape
-    if x_out is None:
-        x_out = torch.empty(shape, dtype=x_dtype, device=x.device)
-    ok = (x.shape == shape and x_out.shape == shape and x_out.dtype is x_dtype and y.is_contiguous() and x.is_contiguous() and x_out.is_contiguous()
-          and dev >= 0 and x.get_device() == dev and x_out.get_device() == dev)
-    post_at = gate_at = pre_at = h_at = None
-    gates = 0
-    if w_post is not None:
-        ok = ok and w_post.dtype is dtype and w_post.shape == (dim,) and w_post.is_contiguous() and w_post.get_device() == dev
-        post_at = w_post.data_ptr()
-    if gate is not None:
-        ok = ok and gate.dtype is dtype and gate.dim() == 2 and gate.shape[1] == dim and gate.is_contiguous() and gate.get_device() == dev
-        gates, gate_at = gate.shape[0], gate.data_ptr()
-    if w_pre is not None:
-        if h is None:
-            h = torch.empty(shape, dtype=dtype, device=y.device)
-        ok = (ok and w_pre.dtype is dtype and w_pre.shape == (dim,) and w_pre.is_contiguous() and w_pre.get_device() == dev and h.dtype is dtype
-              and h.shape == shape and h.is_contiguous() and h.get_device() == dev)
-        pre_at, h_at = w_pre.data_ptr(), h.data_ptr()
-    elif h is not None:
-        raise ValueError("norm_residual: h needs w_pre")
-    if not ok:
-        _refuse("norm_residual", dev, ("y", y, dtype, shape, True), ("x", x, x_dtype, shape, True), ("x_out", x_out, x_dtype, shape, True),
-                ("w_post", w_post, dtype, (dim,), True), ("gate", gate, dtype, (None, dim), True), ("w_pre", w_pre, dtype, (dim,), True),
-                ("h", h, dtype, shape, True))
-    _launch("adsa_norm_residual", dev, code, _DTYPES[x_dtype], y.data_ptr(), x.data_ptr(), post_at, gate_at, gates, pre_at, x_out.data_ptr(), h_at,
-            rows, dim, scale, eps)
-    return x_out, h
+    r = (_marshal_module or _marshal()).norm_residual(y, x, w_pre, w_post, gate, scale, eps, x_out, h)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_norm_residual")
+    return r
 
 
 class AdsaEngine:

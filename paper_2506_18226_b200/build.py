@@ -1,4 +1,5 @@
-"""Builds libadsa.so (sm_100a) in-tree with nvcc.  No torch extension machinery is involved."""
+"""Builds, in-tree: libadsa.so (sm_100a) with nvcc, which knows nothing of torch; and adsa_marshal.so with g++, the part of the
+Python binding that reads torch tensors in C++ (plain compiler calls, no torch extension machinery)."""
 from __future__ import annotations
 
 import os
@@ -13,17 +14,38 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(_HERE, "..", "include", "adsa.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+MARSHAL = os.path.join(_HERE, "adsa_marshal.so")
+MARSHAL_SOURCE = os.path.join(CSRC, "adsa_marshal.cpp")
+HEADER = os.path.join(_HERE, "..", "include", "adsa.h")
+
+
+def _stale(target: str, deps: list) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
+
+
+def build_marshal(force: bool = False) -> str:
+    """Compile the tensor-reading half of the binding against the running torch."""
+    if not force and not _stale(MARSHAL, [MARSHAL_SOURCE, HEADER]):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    include = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    libs = os.path.join(base, "lib")
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{i}" for i in include], MARSHAL_SOURCE,
+                           "-o", tmp, f"-L{libs}", f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
 
 
 def build_lib(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu of the library for sm_100a and link libadsa.so next to this file."""
-    if not force and not _stale():
+    if not force and not _stale(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [HEADER]):
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
@@ -40,3 +62,4 @@ def build_lib(force: bool = False, verbose: bool = False) -> str:
 if __name__ == "__main__":
     import sys
     print(build_lib(force=True, verbose="-v" in sys.argv))
+    print(build_marshal(force=True))
