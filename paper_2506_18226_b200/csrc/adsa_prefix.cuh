@@ -23,6 +23,8 @@ struct PrefixArgs {
     int max_pages, max_p_pages, page_rows, n_pages, box_rows;
     int d, row_stride;
     float scale_log2e;
+    void *out;                              // 16-bit, or null
+    float *out_f32, *lse;                   // or null
     // workspace
     uint4 *plan;                            // [batch][3] for the merge: {first own unit, tiles, units, group's first slot}, {group's first unit,
                                             // tiles, first batch row, query rows}, {units of the wide kernel}

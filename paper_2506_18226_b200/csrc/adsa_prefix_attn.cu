@@ -47,6 +47,8 @@ constexpr long long kPaMaxRows = 0x7fffff00LL;   // a sequence: row numbers stay
 // rows, 8 key heads of 128 (us, here / wide): 512 rows 19 / 20, 4096 36 / 29, 32768 129 / 66; of 128 rows: 34 / 40,
 // 62 / 55, 228 / 90; heads of 64, 33 rows: 17 / 19, 24 / 26, 76 / 57.  20 rows: 16 / 19, 25 / 27, 79 / 64.
 constexpr int kWideAbove = 32;
+constexpr double kDirectBytes = 192 * 1024;
+
 constexpr long long kWideRows = 8192;
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
@@ -170,7 +172,10 @@ __device__ __forceinline__ int pa_answer(uint32_t answer)
 // 128-byte swizzle.  Rows whose 16-byte pieces are odd in number put the eight rows of an ldmatrix on eight different
 // banks without a swizzle, and such rows straddle memory sectors when they are fetched column by column: with 208-byte rows
 // the columns ran at 4.4 TB/s where 256-byte rows run at 6.2.
-template <typename T, int NSUB, int STAGES, bool PACKED>
+// DIRECT: no list and no merge: a block sweeps all that one batch row's queries of one key head attend, prefix and own rows, and
+// writes the output.  For calls so small that reading and cutting the lengths and the second kernel would cost more than
+// the sweep (see kDirectBytes).
+template <typename T, int NSUB, int STAGES, bool PACKED, bool DIRECT>
 __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
 prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
@@ -200,6 +205,27 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
     }
+    int part = 0, own_b = 0, own_q = 0, parts_n[2] = {0, 0}, group = -1;   // DIRECT: the batch row, its query item, rows of prefix and own
+    uint32_t total = 0, wide_total = 0;
+    Walk<TILE> walk = {};
+    const bool behind_wide = !DIRECT && a.w_resident > 0;
+    if constexpr (DIRECT) {
+        const int qi = query_items(a.per_kv), rest = (int)blockIdx.x / qi;
+        own_q = (int)blockIdx.x - rest * qi;
+        own_b = rest / a.kv_heads;
+        pdl_wait();
+        pdl_launch();
+        parts_n[1] = clamp_rows(a.n_rows[own_b], a.max_pages, a.page_rows);
+        for (int g0 = 0; g0 < a.groups && group < 0; g0 += 32) {    // the group that holds the batch row
+            const int g = g0 + lane;
+            const bool in = g < a.groups && group_begin(a, g) <= own_b && own_b < group_begin(a, g + 1);
+            const uint32_t who = __ballot_sync(0xffffffffu, in);
+            if (who) group = g0 + __ffs((int)who) - 1;
+        }
+        if (group >= 0) parts_n[0] = clamp_rows(a.p_rows[group], a.max_p_pages, a.page_rows);
+        __syncthreads();                                           // (the barriers are set up)
+    }
+    if constexpr (!DIRECT) {
     // The small tables into L2 while the kernel ahead still runs (hints; they are read after the wait)
     {
         const auto hint = [&](const int32_t *p, long long n) {
@@ -214,7 +240,6 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     }
     // Behind the wide kernel of the same call (which has waited for what was ahead of it before this one could begin) there
     // is nothing to wait for here; each block waits before it ends, so that the merge finds both kernels' states.
-    const bool behind_wide = a.w_resident > 0;
     if (!behind_wide) pdl_wait();
     pdl_launch();
 
@@ -241,7 +266,6 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
     uint2 before = make_uint2(incl.x - mine.x, incl.y - mine.y);
-    uint32_t total = 0, wide_total = 0;
     for (int w = 0; w < kPaThreads / 32; ++w) {
         const uint2 s = warp_sums[w];
         if (w < warp) { before.x += s.x; before.y += s.y; }
@@ -254,9 +278,9 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     }
     if (tid == 0) c.plan[entries] = total;
     __syncthreads();
-    const Cut cut(total, (uint32_t)a.resident);
-    Walk<TILE> walk;
-    walk.begin(a, c, cut, blockIdx.x);
+    }
+    const Cut cut(total, (uint32_t)max(a.resident, 1));
+    if constexpr (!DIRECT) walk.begin(a, c, cut, blockIdx.x);
     Segment s;
     // The next segment of this block's runs.  Each warp follows the runs by itself; the copying warp asks for the next
     // run when it begins one, into the answer slot that all warps have read the last time; warp 0 leaves the run's share
@@ -302,25 +326,40 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     // next answer is asked for when the copying warp gets there, which may first need tiles of the segment in hand to be freed.
     enum { kEnd, kSegment, kLater };
     const auto advance = [&](Segment &n, bool patient) {
-        while (!walk.next(a, c, n)) {
-            if (!patient && walk.empty) return kLater;
-            const uint32_t i = turns & 1u;
-            int run = -1;
-            if (mbar_wait_bounded(asked + 8 * i, (turns >> 1) & 1u, limit)) run = pa_answer(answer + 16 * i);
-            else {
-                limit = kCopySpinAfterTimeout;
-                if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+        if constexpr (DIRECT) {
+            while (part < 2 && parts_n[part] == 0) ++part;
+            if (part == 2) return kEnd;
+            const int rest = (int)blockIdx.x / query_items(a.per_kv);
+            n.pages = part == 0 ? a.p_table + (size_t)group * a.max_p_pages : a.table + (size_t)own_b * a.max_pages;
+            n.n = parts_n[part];
+            n.head = rest - own_b * a.kv_heads;
+            n.tile0 = 0;
+            n.tiles = (n.n + TILE - 1) / TILE;
+            n.row0 = own_b * a.per_kv + own_q * kPaQueries;
+            n.rows = min(a.per_kv - own_q * kPaQueries, kPaQueries);
+            ++part;
+            return kSegment;
+        } else {
+            while (!walk.next(a, c, n)) {
+                if (!patient && walk.empty) return kLater;
+                const uint32_t i = turns & 1u;
+                int run = -1;
+                if (mbar_wait_bounded(asked + 8 * i, (turns >> 1) & 1u, limit)) run = pa_answer(answer + 16 * i);
+                else {
+                    limit = kCopySpinAfterTimeout;
+                    if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the answer is read before the slot is asked into again
+                __syncwarp();
+                if (lane == 0) mbar_arrive(heard + 8 * i);
+                ++turns;
+                if (run < 0) return kEnd;
+                if (warp == kPaWarps) ask();
+                if (warp == 0) leave_plan(run);
+                walk.begin(a, c, cut, run);
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the answer is read before the slot is asked into again
-            __syncwarp();
-            if (lane == 0) mbar_arrive(heard + 8 * i);
-            ++turns;
-            if (run < 0) return kEnd;
-            if (warp == kPaWarps) ask();
-            if (warp == 0) leave_plan(run);
-            walk.begin(a, c, cut, run);
+            return kSegment;
         }
-        return kSegment;
     };
 
     if (warp == kPaWarps) {                                        // ---- the copying warp ----
@@ -328,7 +367,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         uint32_t phase = 0;
         const int page_shift = (a.page_rows & (a.page_rows - 1)) == 0 ? 31 - __clz(a.page_rows) : -1;
         const auto page_of = [&](int row) { return page_shift >= 0 ? row >> page_shift : row / a.page_rows; };
-        ask();
+        if (!DIRECT) ask();
         while (advance(s, true) == kSegment) {
             // page ids are read 32 at a time, a lane each
             const int last_page = page_of(s.n - 1);
@@ -412,7 +451,11 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     Segment nxt;
     auto more = advance(nxt, true);
     if (more == kSegment) ask_q(nxt);
-    if (warp == 0) leave_plan(blockIdx.x);                         // while the first tile is on its way
+    if (!DIRECT && warp == 0) leave_plan(blockIdx.x);              // while the first tile is on its way
+    // state of query rows 2 t4 and 2 t4 + 1: maximum (alike in the eight lanes of a t4), this lane's share of the sum, O^T
+    float o[KS][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+#pragma unroll
+    for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
     while (more == kSegment) {
         s = nxt;
         uint32_t qa[KS][2];
@@ -422,11 +465,6 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         if (more == kSegment) ask_q(nxt);
         const int wq = query_warps(s.rows), wk = kPaWarps / wq;     // warps over query rows, warps over cached rows
         const int qb = warp & (wq - 1), kb = warp / wq;
-        // state of query rows 2 t4 and 2 t4 + 1: maximum (alike in the eight lanes of a t4), this lane's share of the sum, O^T
-        float o[KS][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
-#pragma unroll
-        for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
-
         for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
             if (!mbar_wait_bounded(full + 8 * stage, phase, limit)) {
                 limit = kCopySpinAfterTimeout;
@@ -530,6 +568,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             if (lane == 0) mbar_arrive(empty + 8 * stage);
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
+        if constexpr (!DIRECT) {                                   // (else the own rows carry the state of the prefix on)
         // ---- the partial state: a slot holds wk states of s.rows rows ----
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -538,25 +577,71 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         }
         const bool fits = s.slot < (s.prefix ? a.n_p_slots : a.n_o_slots);
         if (!fits && a.status && lane == 0) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
-        if (fits) {
-            const size_t first = (size_t)s.slot * (s.prefix ? kPaQueries : own_slot_rows(a.per_kv)) + (size_t)kb * s.rows;
-            float *st = s.prefix ? a.p_state : a.o_state, *ml = s.prefix ? a.p_ml : a.o_ml;
+        const size_t first = (size_t)s.slot * (s.prefix ? kPaQueries : own_slot_rows(a.per_kv)) + (size_t)kb * s.rows;
+        float *st = s.prefix ? a.p_state : a.o_state, *ml = s.prefix ? a.p_ml : a.o_ml;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = qb * 8 + 2 * t4 + h;
-                if (r < s.rows) {
-                    if (g == 0) *reinterpret_cast<float2 *>(ml + 2 * (first + r)) = make_float2(m_run[h] * a.scale_log2e - kBias, l_run[h]);
+        for (int h = 0; h < 2; ++h) {
+            const int r = qb * 8 + 2 * t4 + h;
+            if (fits && r < s.rows) {
+                if (g == 0) *reinterpret_cast<float2 *>(ml + 2 * (first + r)) = make_float2(m_run[h] * a.scale_log2e - kBias, l_run[h]);
 #pragma unroll
-                    for (int dp = 0; dp < KS; ++dp) {
-                        if (dp * 16 + g < a.d) st[(first + r) * DP + dp * 16 + g] = o[dp][h];
-                        if (dp * 16 + g + 8 < a.d) st[(first + r) * DP + dp * 16 + g + 8] = o[dp][h + 2];
-                    }
+                for (int dp = 0; dp < KS; ++dp) {
+                    if (dp * 16 + g < a.d) st[(first + r) * DP + dp * 16 + g] = o[dp][h];
+                    if (dp * 16 + g + 8 < a.d) st[(first + r) * DP + dp * 16 + g + 8] = o[dp][h + 2];
                 }
             }
+            m_run[h] = -INFINITY;
+            l_run[h] = 0.f;
         }
+#pragma unroll
+        for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
         if (more == kLater) {
             more = advance(nxt, true);
             if (more == kSegment) ask_q(nxt);
+        }
+        }
+    }
+    if constexpr (DIRECT) {
+        // ---- the warps' states to shared memory (the tiles have been read), then the outputs ----
+        const int rows = min(a.per_kv - own_q * kPaQueries, kPaQueries), wq = query_warps(rows), wk = kPaWarps / wq, qb = warp & (wq - 1), kb = warp / wq;
+        float *states = reinterpret_cast<float *>(pa_smem + (ring - smem_u32(pa_smem))), *mls = states + kPaQueries * DP;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], x);
+            const int r = qb * 8 + 2 * t4 + h;
+            if (r < rows) {
+                if (g == 0) { mls[2 * (kb * rows + r)] = m_run[h] * a.scale_log2e - kBias; mls[2 * (kb * rows + r) + 1] = l_run[h]; }
+#pragma unroll
+                for (int dp = 0; dp < KS; ++dp) {
+                    states[(kb * rows + r) * DP + dp * 16 + g] = o[dp][h];
+                    states[(kb * rows + r) * DP + dp * 16 + g + 8] = o[dp][h + 2];
+                }
+            }
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const bool empty = parts_n[0] + parts_n[1] == 0;
+        const int head = (int)blockIdx.x / query_items(a.per_kv) - own_b * a.kv_heads, half = a.d / 2;
+        const size_t out_row = ((size_t)own_b * a.kv_heads + head) * a.per_kv + own_q * kPaQueries;
+        for (int i = tid; i < rows * half; i += kPaWarps * 32) {
+            const int r = i / half, e = 2 * (i - r * half);
+            float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
+            for (int k = 0; k < wk; ++k) M = fmaxf(M, mls[2 * (k * rows + r)]);
+            for (int k = 0; k < wk; ++k) {
+                const float m = mls[2 * (k * rows + r)], w = m == -INFINITY ? 0.f : pa_exp2(m - M);
+                if (m == -INFINITY && mls[2 * (k * rows + r) + 1] == 0.f) continue;   // an empty state
+                L += mls[2 * (k * rows + r) + 1] * w;
+                x += states[(k * rows + r) * DP + e] * w;
+                y += states[(k * rows + r) * DP + e + 1] * w;
+            }
+            const float inv = empty ? 0.f : 1.f / L;
+            x = empty ? 0.f : x * inv;
+            y = empty ? 0.f : y * inv;
+            const size_t at = (out_row + r) * a.d + e;
+            if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + at) = pack2<T>(x, y);
+            if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + at) = make_float2(x, y);
+            if (a.lse && e == 0) a.lse[out_row + r] = empty ? -INFINITY : (M + log2f(L)) * 0.693147180559945309f;
         }
     }
 }
@@ -565,7 +650,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
 // dealt to four warps.  (A warp per row instead: 109.8 us against 97.8 for 2048 rows of about 23 states.)
 template <typename T, int NSUB>
 __global__ void __launch_bounds__(kPaMergeThreads)
-prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32, float *lse)
+prefix_merge_kernel(const __grid_constant__ PrefixArgs a)
 {
     constexpr int DP = 64 * NSUB, WARPS = kPaMergeThreads / 32, PER = 2 * NSUB;   // PER floats per lane
     __shared__ float s_m[WARPS], s_l[WARPS], s_o[WARPS][DP];
@@ -660,10 +745,10 @@ prefix_merge_kernel(const __grid_constant__ PrefixArgs a, T *out, float *out_f32
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) { x.x += s_o[w][e] * wgt[w]; x.y += s_o[w][e + 1] * wgt[w]; }
         x = empty ? make_float2(0.f, 0.f) : make_float2(x.x * inv, x.y * inv);
-        if (out) *reinterpret_cast<uint32_t *>(out + row * a.d + e) = pack2<T>(x.x, x.y);
-        if (out_f32) *reinterpret_cast<float2 *>(out_f32 + row * a.d + e) = x;
+        if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + e) = pack2<T>(x.x, x.y);
+        if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + e) = x;
     }
-    if (lse && threadIdx.x == 0) lse[row] = empty ? -INFINITY : (M + log2f(L)) * 0.693147180559945309f;
+    if (a.lse && threadIdx.x == 0) a.lse[row] = empty ? -INFINITY : (M + log2f(L)) * 0.693147180559945309f;
 }
 
 namespace {
@@ -744,27 +829,30 @@ bool pool_map(CUtensorMap *m, const adsa_paged_kv &kv, void *pool, int box_rows)
 }
 
 template <typename T, int NSUB, int STAGES, bool PACKED>
-cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32, float *lse, cudaStream_t st)
+cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, bool direct, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
-    const size_t smem = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128 + (size_t)(2 * a.batch + 4 * a.groups + 2) * 4;
-    const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED>;
-    static int told[64];
-    cudaError_t e = allow_smem((const void *)kern, told);
+    const size_t tiles = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128, plan = (size_t)(2 * a.batch + 4 * a.groups + 2) * 4;
+    static int told[2][64];
+    if (direct) {
+        const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, true>;
+        const cudaError_t e = allow_smem((const void *)kern, told[0]);
+        return e != cudaSuccess ? e : launch_pdl(kern, dim3((unsigned)(a.batch * a.kv_heads * query_items(a.per_kv))), kPaThreads, tiles, st, a, km, vm);
+    }
+    const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, false>;
+    cudaError_t e = allow_smem((const void *)kern, told[1]);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(kern, dim3(runs), kPaThreads, smem, st, a, km, vm);
+    e = launch_pdl(kern, dim3(runs), kPaThreads, tiles + plan, st, a, km, vm);
     if (e != cudaSuccess) return e;
-    return launch_pdl(prefix_merge_kernel<T, NSUB>, dim3((unsigned)(a.batch * a.kv_heads * a.per_kv)), kPaMergeThreads, 0, st, a, (T *)out, out_f32, lse);
+    return launch_pdl(prefix_merge_kernel<T, NSUB>, dim3((unsigned)(a.batch * a.kv_heads * a.per_kv)), kPaMergeThreads, 0, st, a);
 }
 
 template <typename T>
-cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, unsigned runs, const CUtensorMap &km, const CUtensorMap &vm, void *out, float *out_f32,
-                               float *lse, cudaStream_t st)
+cudaError_t launch_prefix_type(int nsub, const PrefixArgs &a, unsigned runs, bool direct, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
     // 96 KB of tiles in flight per block and two blocks per SM; wide rows: 192 KB and one block
     const bool packed = a.row_stride / 8 % 2 != 0 && a.row_stride <= 64 * nsub;   // (a stage holds rows of 64 nsub elements)
 #define ADSA_PREFIX(NSUB, STAGES) \
-    return packed ? launch_prefix<T, NSUB, STAGES, true>(a, runs, km, vm, out, out_f32, lse, st) \
-                  : launch_prefix<T, NSUB, STAGES, false>(a, runs, km, vm, out, out_f32, lse, st)
+    return packed ? launch_prefix<T, NSUB, STAGES, true>(a, runs, direct, km, vm, st) : launch_prefix<T, NSUB, STAGES, false>(a, runs, direct, km, vm, st)
     switch (nsub) {
     case 1: ADSA_PREFIX(1, 3);
     case 2: ADSA_PREFIX(2, 3);
@@ -825,11 +913,15 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.d = kv->head_dim; a.row_stride = kv->row_stride; a.k_pool = kv->k_pool; a.v_pool = kv->v_pool;
     const float scale = softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale;
     a.scale_log2e = scale * 1.44269504088896341f;
+    a.out = out; a.out_f32 = out_f32; a.lse = lse;
     a.plan = (uint4 *)(ws + l.plan);
     a.p_state = (float *)(ws + l.p_state); a.p_ml = (float *)(ws + l.p_ml);
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
-    const bool wide = l.wide_blocks && (long long)max_prefix_pages * kv->page_rows * l.nsub >= kWideRows;
+    // a block per batch row and key head where they are few and what each attends is little, whatever the lengths turn out to be
+    const double most = ((double)max_pages + (n_groups ? max_prefix_pages : 0)) * kv->page_rows * l.nsub * 256;
+    const bool direct = (long long)batch * kv->n_kv_heads * query_items(a.per_kv) <= l.blocks && most <= kDirectBytes;
+    const bool wide = !direct && l.wide_blocks && (long long)max_prefix_pages * kv->page_rows * l.nsub >= kWideRows;
     a.wide_above = wide ? kWideAbove : 0x7fffffff;
     a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
     a.n_w_slots = (int)l.w_slots; a.w_resident = wide ? l.wide_blocks : 0; a.resident = l.blocks;
@@ -839,8 +931,8 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     const unsigned runs = units < l.max_runs ? (unsigned)units : (unsigned)l.max_runs;
     cudaStream_t st = (cudaStream_t)stream;
     if (a.w_resident && launch_prefix_wide(kv->dtype, l.nsub, a, km, vm, st) != cudaSuccess) return ADSA_ECUDA;
-    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, runs, km, vm, out, out_f32, lse, st)
-                                                  : launch_prefix_type<__half>(l.nsub, a, runs, km, vm, out, out_f32, lse, st);
+    const cudaError_t e = kv->dtype == ADSA_BF16 ? launch_prefix_type<__nv_bfloat16>(l.nsub, a, runs, direct, km, vm, st)
+                                                  : launch_prefix_type<__half>(l.nsub, a, runs, direct, km, vm, st);
     return e == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 
