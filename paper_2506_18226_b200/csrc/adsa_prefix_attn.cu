@@ -15,7 +15,8 @@
 // grid, and a grid may have five times as many blocks as fit the GPU; a resident block that has finished its run takes
 // over one that has not started (cluster launch control), without refilling its pipeline.  SMs differ in the bandwidth
 // they get and items in their cost per tile: with one run per block the slowest block took 279 us where the median took
-// 225 (64 rows of 2304 x 32 heads x 100 elements).
+// 225 (64 rows of 2304 x 32 heads x 100 elements).  Where the tables are short this is not worth its fixed cost: a block takes
+// all cached rows of one batch row and key head, prefix first, and writes the output itself (DIRECT; direct_pays has the rule).
 //
 // What a warp does per 16 cached rows: S^T = K Q^T and O^T += V^T P^T on mma.sync tiles with the cached rows as M and
 // eight query rows as N (the fewest that the instruction takes).  Up to 8 query rows of a key head: the four warps of a
@@ -24,9 +25,9 @@
 // takes the fewest instructions per byte.
 //
 // Measured in a captured graph: 64 rows x 32 heads of 100 elements over 2424 shared (four groups) and up to 2304 own rows,
-// 1.19 GB: 197 us, 6.0 TB/s.  32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39 us, of which 27 stream;
-// 2 us go by until the lengths are read and cut, 1.5 until the first tile, 4 in the merge, the rest between the launches.  Two
-// rows x 12 heads, 100 own rows: 8.7 us, a chain of five dependent reads in two kernels.
+// 1.19 GB: 197 us, 6.0 TB/s; 2 us of it go by until the lengths are read and cut, 1.5 until the first tile, 4 in the merge.
+// DIRECT: 32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39 us, 4.3 TB/s, as 640 blocks are 2.2 turns of
+// the 296 that the GPU holds; two rows x 12 heads over 120 shared and 100 own rows: 5.0 us, a chain of three dependent reads.
 #include <math.h>
 #include <type_traits>
 
@@ -47,9 +48,21 @@ constexpr long long kPaMaxRows = 0x7fffff00LL;   // a sequence: row numbers stay
 // rows, 8 key heads of 128 (us, here / wide): 512 rows 19 / 20, 4096 36 / 29, 32768 129 / 66; of 128 rows: 34 / 40,
 // 62 / 55, 228 / 90; heads of 64, 33 rows: 17 / 19, 24 / 26, 76 / 57.  20 rows: 16 / 19, 25 / 27, 79 / 64.
 constexpr int kWideAbove = 32;
-constexpr double kDirectBytes = 192 * 1024;
-
 constexpr long long kWideRows = 8192;
+
+// A block per batch row and key head (DIRECT), by the bytes of K and V that the tables hold for one of them (most) and how many
+// of these the list would not read, as the other rows of a group have (again).  It does not split, and saves the list, the second
+// kernel and the states, of which every query head has its own.  Measured, list / direct in us.  While each has a block at once: 2 rows x 12 heads of 64, 32 KB 7.8 / 4.9, 256 KB
+// 12.5 / 9.0, 512 KB 16.3 / 14.3; 2 x 8 heads of 128, 512 KB 13.4 / 14.3, 1 MB 18.7 / 24.2.  In two turns: 20 rows x 20 heads of
+// 64, 32 KB 13.8 / 9.1, 192 KB 23.2 / 15.6, 256 KB of which half prefix 19.3 / 18.1, 528 KB of which 512 prefix 17.7 / 30.0.  In
+// more, heads of 64: 256 rows x 32 heads on 8, 48 KB of which a third prefix 44.8 / 33.1, 192 KB of which a third 77.9 / 67.3,
+// 288 KB of which 32 prefix 135.7 / 96.0; 128 x 32 on 32, 96 KB of which a third 74.7 / 84.8, 288 KB of which 32 205 / 168.
+inline bool direct_pays(long long items, long long blocks, int per_kv, double most, double again)
+{
+    if (items <= blocks) return most <= 448 * 1024;
+    const bool two_turns = items <= 2 * blocks;
+    return (two_turns && most <= 256 * 1024) || (most <= 600 * 1024 && most - again >= (two_turns || per_kv > 1 ? 2 : 8) * again);
+}
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
 __host__ __device__ __forceinline__ int query_warps(int m) { return m <= 8 ? 1 : m <= 16 ? 2 : 4; }
@@ -174,7 +187,7 @@ __device__ __forceinline__ int pa_answer(uint32_t answer)
 // the columns ran at 4.4 TB/s where 256-byte rows run at 6.2.
 // DIRECT: no list and no merge: a block sweeps all that one batch row's queries of one key head attend, prefix and own rows, and
 // writes the output.  For calls so small that reading and cutting the lengths and the second kernel would cost more than
-// the sweep (see kDirectBytes).
+// the sweep (direct_pays).
 template <typename T, int NSUB, int STAGES, bool PACKED, bool DIRECT>
 __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
 prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
@@ -216,68 +229,71 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         pdl_wait();
         pdl_launch();
         parts_n[1] = clamp_rows(a.n_rows[own_b], a.max_pages, a.page_rows);
-        for (int g0 = 0; g0 < a.groups && group < 0; g0 += 32) {    // the group that holds the batch row
-            const int g = g0 + lane;
-            const bool in = g < a.groups && group_begin(a, g) <= own_b && own_b < group_begin(a, g + 1);
-            const uint32_t who = __ballot_sync(0xffffffffu, in);
-            if (who) group = g0 + __ffs((int)who) - 1;
+        for (int g0 = 0; g0 < a.groups && group < 0; g0 += 128) {   // the first group that holds the batch row
+            uint32_t first = 0xffffffffu;
+#pragma unroll
+            for (int j = 3; j >= 0; --j) {
+                const int g = g0 + 32 * j + lane;
+                if (g < a.groups && group_begin(a, g) <= own_b && own_b < group_begin(a, g + 1)) first = (uint32_t)g;
+            }
+            group = (int)__reduce_min_sync(0xffffffffu, first);
         }
         if (group >= 0) parts_n[0] = clamp_rows(a.p_rows[group], a.max_p_pages, a.page_rows);
         __syncthreads();                                           // (the barriers are set up)
     }
     if constexpr (!DIRECT) {
-    // The small tables into L2 while the kernel ahead still runs (hints; they are read after the wait)
-    {
-        const auto hint = [&](const int32_t *p, long long n) {
-            for (long long i = ((long long)blockIdx.x * kPaThreads + tid) * 32; i < min(n, 65536LL); i += (long long)gridDim.x * kPaThreads * 32)
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
-        };
-        hint(a.table, (long long)a.batch * a.max_pages);
-        hint(a.n_rows, a.batch);
-        hint(a.p_table, (long long)a.groups * a.max_p_pages);
-        hint(a.p_rows, a.groups);
-        hint(a.start, a.groups > 0 ? a.groups + 1 : 0);
-    }
-    // Behind the wide kernel of the same call (which has waited for what was ahead of it before this one could begin) there
-    // is nothing to wait for here; each block waits before it ends, so that the merge finds both kernels' states.
-    if (!behind_wide) pdl_wait();
-    pdl_launch();
+        // The small tables into L2 while the kernel ahead still runs (hints; they are read after the wait)
+        {
+            const auto hint = [&](const int32_t *p, long long n) {
+                for (long long i = ((long long)blockIdx.x * kPaThreads + tid) * 32; i < min(n, 65536LL); i += (long long)gridDim.x * kPaThreads * 32)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
+            };
+            hint(a.table, (long long)a.batch * a.max_pages);
+            hint(a.n_rows, a.batch);
+            hint(a.p_table, (long long)a.groups * a.max_p_pages);
+            hint(a.p_rows, a.groups);
+            hint(a.start, a.groups > 0 ? a.groups + 1 : 0);
+        }
+        // Behind the wide kernel of the same call (which has waited for what was ahead of it before this one could begin) there
+        // is nothing to wait for here; each block waits before it ends, so that the merge finds both kernels' states.
+        if (!behind_wide) pdl_wait();
+        pdl_launch();
 
-    // ---- lengths, boundaries, first unit of every entry: each thread sums a few entries, the sums are scanned over the block ----
-    const int per = (entries + kPaThreads - 1) / kPaThreads, e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
-    for (int g = tid; g <= a.groups && a.groups > 0; g += kPaThreads) c.begin[g] = group_begin(a, g);
-    for (int e = e0; e < e1; ++e)
-        c.len[e] = e < a.groups ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
-    __syncthreads();
-    uint2 mine = make_uint2(0u, 0u);                               // units of this list, of the wide kernel's
-    for (int e = e0; e < e1; ++e) {
-        const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;
-        c.plan[e] = mine.x;
-        if (e < a.groups) c.wide[e] = mine.y;
-        if (e < a.groups && m > a.wide_above) mine.y += WideItems(m, c.len[e]).head_units * (uint32_t)a.kv_heads;
-        else mine.x += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
-    }
-    uint2 incl = mine;
+        // ---- lengths, boundaries, first unit of every entry: each thread sums a few entries, the sums are scanned over the block ----
+        const int per = (entries + kPaThreads - 1) / kPaThreads, e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
+        for (int g = tid; g <= a.groups && a.groups > 0; g += kPaThreads) c.begin[g] = group_begin(a, g);
+        for (int e = e0; e < e1; ++e)
+            c.len[e] = e < a.groups ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
+        __syncthreads();
+        uint2 mine = make_uint2(0u, 0u);                               // units of this list, of the wide kernel's
+        for (int e = e0; e < e1; ++e) {
+            const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;
+            c.plan[e] = mine.x;
+            if (e < a.groups) c.wide[e] = mine.y;
+            if (e < a.groups && m > a.wide_above) mine.y += WideItems(m, c.len[e]).head_units * (uint32_t)a.kv_heads;
+            else mine.x += (uint32_t)query_items(m) * (uint32_t)a.kv_heads * (uint32_t)((c.len[e] + TILE - 1) / TILE);
+        }
+        uint2 incl = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
-        if (lane >= o) { incl.x += x; incl.y += y; }
-    }
-    if (lane == 31) warp_sums[warp] = incl;
-    __syncthreads();
-    uint2 before = make_uint2(incl.x - mine.x, incl.y - mine.y);
-    for (int w = 0; w < kPaThreads / 32; ++w) {
-        const uint2 s = warp_sums[w];
-        if (w < warp) { before.x += s.x; before.y += s.y; }
-        total += s.x;
-        wide_total += s.y;
-    }
-    for (int e = e0; e < e1; ++e) {
-        c.plan[e] += before.x;
-        if (e < a.groups) c.wide[e] += before.y;
-    }
-    if (tid == 0) c.plan[entries] = total;
-    __syncthreads();
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
+            if (lane >= o) { incl.x += x; incl.y += y; }
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        uint2 before = make_uint2(incl.x - mine.x, incl.y - mine.y);
+        for (int w = 0; w < kPaThreads / 32; ++w) {
+            const uint2 s = warp_sums[w];
+            if (w < warp) { before.x += s.x; before.y += s.y; }
+            total += s.x;
+            wide_total += s.y;
+        }
+        for (int e = e0; e < e1; ++e) {
+            c.plan[e] += before.x;
+            if (e < a.groups) c.wide[e] += before.y;
+        }
+        if (tid == 0) c.plan[entries] = total;
+        __syncthreads();
     }
     const Cut cut(total, (uint32_t)max(a.resident, 1));
     if constexpr (!DIRECT) walk.begin(a, c, cut, blockIdx.x);
@@ -569,36 +585,36 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
         if constexpr (!DIRECT) {                                   // (else the own rows carry the state of the prefix on)
-        // ---- the partial state: a slot holds wk states of s.rows rows ----
+            // ---- the partial state: a slot holds wk states of s.rows rows ----
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], x);
-        }
-        const bool fits = s.slot < (s.prefix ? a.n_p_slots : a.n_o_slots);
-        if (!fits && a.status && lane == 0) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
-        const size_t first = (size_t)s.slot * (s.prefix ? kPaQueries : own_slot_rows(a.per_kv)) + (size_t)kb * s.rows;
-        float *st = s.prefix ? a.p_state : a.o_state, *ml = s.prefix ? a.p_ml : a.o_ml;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = qb * 8 + 2 * t4 + h;
-            if (fits && r < s.rows) {
-                if (g == 0) *reinterpret_cast<float2 *>(ml + 2 * (first + r)) = make_float2(m_run[h] * a.scale_log2e - kBias, l_run[h]);
-#pragma unroll
-                for (int dp = 0; dp < KS; ++dp) {
-                    if (dp * 16 + g < a.d) st[(first + r) * DP + dp * 16 + g] = o[dp][h];
-                    if (dp * 16 + g + 8 < a.d) st[(first + r) * DP + dp * 16 + g + 8] = o[dp][h + 2];
-                }
+                for (int x = 4; x < 32; x <<= 1) l_run[h] += __shfl_xor_sync(0xffffffffu, l_run[h], x);
             }
-            m_run[h] = -INFINITY;
-            l_run[h] = 0.f;
-        }
+            const bool fits = s.slot < (s.prefix ? a.n_p_slots : a.n_o_slots);
+            if (!fits && a.status && lane == 0) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
+            const size_t first = (size_t)s.slot * (s.prefix ? kPaQueries : own_slot_rows(a.per_kv)) + (size_t)kb * s.rows;
+            float *st = s.prefix ? a.p_state : a.o_state, *ml = s.prefix ? a.p_ml : a.o_ml;
 #pragma unroll
-        for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
-        if (more == kLater) {
-            more = advance(nxt, true);
-            if (more == kSegment) ask_q(nxt);
-        }
+            for (int h = 0; h < 2; ++h) {
+                const int r = qb * 8 + 2 * t4 + h;
+                if (fits && r < s.rows) {
+                    if (g == 0) *reinterpret_cast<float2 *>(ml + 2 * (first + r)) = make_float2(m_run[h] * a.scale_log2e - kBias, l_run[h]);
+#pragma unroll
+                    for (int dp = 0; dp < KS; ++dp) {
+                        if (dp * 16 + g < a.d) st[(first + r) * DP + dp * 16 + g] = o[dp][h];
+                        if (dp * 16 + g + 8 < a.d) st[(first + r) * DP + dp * 16 + g + 8] = o[dp][h + 2];
+                    }
+                }
+                m_run[h] = -INFINITY;
+                l_run[h] = 0.f;
+            }
+#pragma unroll
+            for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
+            if (more == kLater) {
+                more = advance(nxt, true);
+                if (more == kSegment) ask_q(nxt);
+            }
         }
     }
     if constexpr (DIRECT) {
@@ -918,9 +934,10 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.p_state = (float *)(ws + l.p_state); a.p_ml = (float *)(ws + l.p_ml);
     a.o_state = (float *)(ws + l.o_state); a.o_ml = (float *)(ws + l.o_ml);
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
-    // a block per batch row and key head where they are few and what each attends is little, whatever the lengths turn out to be
-    const double most = ((double)max_pages + (n_groups ? max_prefix_pages : 0)) * kv->page_rows * l.nsub * 256;
-    const bool direct = (long long)batch * kv->n_kv_heads * query_items(a.per_kv) <= l.blocks && most <= kDirectBytes;
+    const double row_bytes = (double)kv->page_rows * l.nsub * 256;
+    const double prefix_bytes = n_groups ? max_prefix_pages * row_bytes : 0.0;
+    const bool direct = direct_pays((long long)batch * kv->n_kv_heads * query_items(a.per_kv), l.blocks, a.per_kv,
+                                    max_pages * row_bytes + prefix_bytes, prefix_bytes * (1.0 - fmin(1.0, (double)n_groups / batch)));
     const bool wide = !direct && l.wide_blocks && (long long)max_prefix_pages * kv->page_rows * l.nsub >= kWideRows;
     a.wide_above = wide ? kWideAbove : 0x7fffffff;
     a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);
