@@ -35,6 +35,7 @@ struct PrefixArgs {
     float *w_state, *w_ml;                  // slots of kWideQueries rows
     int n_w_slots, w_resident;              // w_resident: blocks of the wide kernel that fit the GPU at a time; 0: it does not run
     int resident;                           // blocks of the sweep kernel that fit the GPU at a time
+    int split;                              // blocks of a cluster, which share an item's cached rows (1: no cluster)
 };
 
 __device__ __forceinline__ int clamp_rows(int n, int max_pages, int page_rows)

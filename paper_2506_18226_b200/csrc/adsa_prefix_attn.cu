@@ -17,6 +17,7 @@
 // they get and items in their cost per tile: with one run per block the slowest block took 279 us where the median took
 // 225 (64 rows of 2304 x 32 heads x 100 elements).  Where the tables are short this is not worth its fixed cost: a block takes
 // all cached rows of one batch row and key head, prefix first, and writes the output itself (DIRECT; direct_pays has the rule).
+// With few batch rows a cluster of up to 8 blocks shares them and merges its states through shared memory.
 //
 // What a warp does per 16 cached rows: S^T = K Q^T and O^T += V^T P^T on mma.sync tiles with the cached rows as M and
 // eight query rows as N (the fewest that the instruction takes).  Up to 8 query rows of a key head: the four warps of a
@@ -26,8 +27,9 @@
 //
 // Measured in a captured graph: 64 rows x 32 heads of 100 elements over 2424 shared (four groups) and up to 2304 own rows,
 // 1.19 GB: 197 us, 6.0 TB/s; 2 us of it go by until the lengths are read and cut, 1.5 until the first tile, 4 in the merge.
-// DIRECT: 32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39 us, 4.3 TB/s, as 640 blocks are 2.2 turns of
-// the 296 that the GPU holds; two rows x 12 heads over 120 shared and 100 own rows: 5.0 us, a chain of three dependent reads.
+// 32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39 us, of which 27 stream.  DIRECT: two rows x 12 heads over
+// 120 shared and 100 own rows: 5.0 us, a chain of three dependent reads; two rows x 8 heads of 128 over 128 shared and 4096 own
+// rows, 35 MB, clusters of 8: 11.5 us (list: 20.4).
 #include <math.h>
 #include <type_traits>
 
@@ -42,6 +44,9 @@ constexpr int kPaWarps = 4;                 // warps that compute; one more warp
 constexpr int kPaThreads = (kPaWarps + 1) * 32;
 constexpr int kPaMaxEntries = 4096;         // batch rows + twice the groups of a call: 8 bytes of shared memory each beside the tiles
 constexpr int kPaMergeThreads = 128;
+constexpr int kPaSplit = 8;                 // blocks of a cluster at most
+// how prefix_sweep_kernel gets its work: runs of one list; a batch row and key head to a block; .. to a cluster of blocks
+enum { kModeList, kModeBlocks, kModeClusters };
 constexpr long long kPaMaxRows = 0x7fffff00LL;   // a sequence: row numbers stay in 32 bits past the last tile
 // A group's prefix goes to the wide kernel if the group has more query rows of a key head than fit one item here, where the
 // mean group has and the prefix tables hold at least 8192 rows of up to 64 elements (4096 of up to 128).  Two groups of 33
@@ -50,18 +55,33 @@ constexpr long long kPaMaxRows = 0x7fffff00LL;   // a sequence: row numbers stay
 constexpr int kWideAbove = 32;
 constexpr long long kWideRows = 8192;
 
-// A block per batch row and key head (DIRECT), by the bytes of K and V that the tables hold for one of them (most) and how many
-// of these the list would not read, as the other rows of a group have (again).  It does not split, and saves the list, the second
-// kernel and the states, of which every query head has its own.  Measured, list / direct in us.  While each has a block at once: 2 rows x 12 heads of 64, 32 KB 7.8 / 4.9, 256 KB
-// 12.5 / 9.0, 512 KB 16.3 / 14.3; 2 x 8 heads of 128, 512 KB 13.4 / 14.3, 1 MB 18.7 / 24.2.  In two turns: 20 rows x 20 heads of
-// 64, 32 KB 13.8 / 9.1, 192 KB 23.2 / 15.6, 256 KB of which half prefix 19.3 / 18.1, 528 KB of which 512 prefix 17.7 / 30.0.  In
-// more, heads of 64: 256 rows x 32 heads on 8, 48 KB of which a third prefix 44.8 / 33.1, 192 KB of which a third 77.9 / 67.3,
-// 288 KB of which 32 prefix 135.7 / 96.0; 128 x 32 on 32, 96 KB of which a third 74.7 / 84.8, 288 KB of which 32 205 / 168.
+// Blocks of a cluster that share the cached rows of one item: as many as the GPU holds at once (the eighth is what clusters of 8
+// leave of a group of SMs; in two turns they are slow: 14 rows x 20 heads of 64, 32 KB, 1 / 2 / 4 blocks 5.8 / 11.5 / 23.0 us),
+// while there are tiles for them.  2 rows x 8 heads
+// of 64, 1 / 2 / 4 / 8 blocks in us: 64 KB 5.4 / 5.8 / 6.2 / 6.2, 128 KB 7.0 / 6.6 / 6.2 / 6.5, 288 KB 10.1 / 8.2 / 7.4 / 7.0,
+// 1 MB 25.8 / 16.0 / 11.1 / 8.8.
+inline int direct_split(long long items, long long blocks, double most)
+{
+    int n = 1;
+    while (n < kPaSplit && items * 2 * n <= blocks * 7 / 8 && most >= fmax(128.0, 64.0 * n) * 1024) n *= 2;
+    return n;
+}
+
+// A block (or cluster) per batch row and key head, by the bytes of K and V that the tables hold for one of them (most) and how many
+// of these the list would not read, as the other rows of a group have (again).  It does not balance, and saves the list, the second
+// kernel and the states, of which every query head has its own.  Measured, list / direct in us.  While all are resident at once: 2
+// rows x 12 heads of 64, 32 KB 7.8 / 4.9, 1 MB (8 blocks) 18.7 / 9.2; 8 x 20 of 128, 576 KB 23.4 / 17.6, 1 MB 27.4 / 28.3; longer
+// rows beside short ones leave too much to one block.  In two turns: 20 rows x 20 heads of 64, 32 KB 13.8 / 9.1, 192 KB 23.2 /
+// 15.6, 256 KB of which half prefix 19.3 / 18.1, 528 KB of which 512 prefix 17.7 / 30.0.  In more, heads of 64: 256 rows x 32 heads
+// on 8, 48 KB of which a third prefix 44.8 / 33.1, 192 KB of which a third 77.9 / 67.3, 288 KB of which 32 prefix 135.7 / 96.0; 128
+// x 32 on 32, 96 KB of which a third 74.7 / 84.8, 288 KB of which 32 205 / 168; 32 x 20 of 128, 2.2 turns, 576 KB 62.6 / 67.1.
 inline bool direct_pays(long long items, long long blocks, int per_kv, double most, double again)
 {
-    if (items <= blocks) return most <= 448 * 1024;
+    if (items <= blocks) return most <= direct_split(items, blocks, most) * 640.0 * 1024;
     const bool two_turns = items <= 2 * blocks;
-    return (two_turns && most <= 256 * 1024) || (most <= 600 * 1024 && most - again >= (two_turns || per_kv > 1 ? 2 : 8) * again);
+    if (two_turns && most <= 256 * 1024) return true;
+    if (most > 600 * 1024) return false;
+    return two_turns || per_kv > 1 ? most >= 3 * again : items >= 4 * blocks && most >= 9 * again;
 }
 
 // how many warps share the query rows of an item with m <= kPaQueries of them (the rest share its cached rows)
@@ -136,6 +156,25 @@ struct Walk {
     }
 };
 
+// Every thread of every block of the cluster takes part; what was written to shared memory before is seen after
+__device__ __forceinline__ void pa_cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// the address of block `rank`'s copy of what lies at `addr` in this block's shared memory
+__device__ __forceinline__ uint32_t pa_of_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float2 pa_ld_cluster(uint32_t addr)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+
 __device__ __forceinline__ void pa_ldsm(uint32_t addr, uint32_t (&r)[4])
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -188,10 +227,11 @@ __device__ __forceinline__ int pa_answer(uint32_t answer)
 // DIRECT: no list and no merge: a block sweeps all that one batch row's queries of one key head attend, prefix and own rows, and
 // writes the output.  For calls so small that reading and cutting the lengths and the second kernel would cost more than
 // the sweep (direct_pays).
-template <typename T, int NSUB, int STAGES, bool PACKED, bool DIRECT>
+template <typename T, int NSUB, int STAGES, bool PACKED, int MODE>
 __global__ void __launch_bounds__(kPaThreads, NSUB <= 2 ? 2 : 1)
 prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
+    constexpr bool DIRECT = MODE != kModeList;
     constexpr int KS = 4 * NSUB;                                   // 16-element steps over a row
     constexpr int TILE = tile_rows(NSUB), NB = TILE / 64;          // blocks of 16 cached rows that a warp has in hand at a time
     constexpr uint32_t kSub = TILE * 128, kHalf = NSUB * kSub;  // bytes: a sub-tile; K (or V) of a tile
@@ -209,7 +249,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     c.wide = reinterpret_cast<uint32_t *>(c.begin + a.groups + 1);
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, asked = empty + 8 * STAGES, heard = asked + 16, answer = smem_u32(answers);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int entries = a.groups + a.batch;
+    const int entries = a.groups + a.batch, split = MODE == kModeClusters ? a.split : 1;
 
     if (tid == 0) {
         for (int i = 0; i < STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, kPaWarps); }
@@ -218,13 +258,16 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
     }
-    int part = 0, own_b = 0, own_q = 0, parts_n[2] = {0, 0}, group = -1;   // DIRECT: the batch row, its query item, rows of prefix and own
+    // DIRECT: the batch row, its query item, rows of prefix and own rows, and which of their tiles are this block's
+    int part = 0, own_b = 0, own_q = 0, item = 0, rank = 0, parts_n[2] = {0, 0}, from[2] = {0, 0}, to[2] = {0, 0}, group = -1;
     uint32_t total = 0, wide_total = 0;
     Walk<TILE> walk = {};
     const bool behind_wide = !DIRECT && a.w_resident > 0;
     if constexpr (DIRECT) {
-        const int qi = query_items(a.per_kv), rest = (int)blockIdx.x / qi;
-        own_q = (int)blockIdx.x - rest * qi;
+        item = (int)blockIdx.x / split;
+        rank = (int)blockIdx.x - item * split;
+        const int qi = query_items(a.per_kv), rest = item / qi;
+        own_q = item - rest * qi;
         own_b = rest / a.kv_heads;
         pdl_wait();
         pdl_launch();
@@ -239,6 +282,12 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             group = (int)__reduce_min_sync(0xffffffffu, first);
         }
         if (group >= 0) parts_n[0] = clamp_rows(a.p_rows[group], a.max_p_pages, a.page_rows);
+        const int pre = (parts_n[0] + TILE - 1) / TILE, all = pre + (parts_n[1] + TILE - 1) / TILE;
+        const int lo = (int)((long long)all * rank / split), hi = (int)((long long)all * (rank + 1) / split);
+        from[0] = min(lo, pre);
+        to[0] = min(hi, pre);
+        from[1] = max(lo - pre, 0);
+        to[1] = max(hi - pre, 0);
         __syncthreads();                                           // (the barriers are set up)
     }
     if constexpr (!DIRECT) {
@@ -343,14 +392,14 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     enum { kEnd, kSegment, kLater };
     const auto advance = [&](Segment &n, bool patient) {
         if constexpr (DIRECT) {
-            while (part < 2 && parts_n[part] == 0) ++part;
+            while (part < 2 && from[part] == to[part]) ++part;
             if (part == 2) return kEnd;
-            const int rest = (int)blockIdx.x / query_items(a.per_kv);
+            const int rest = item / query_items(a.per_kv);
             n.pages = part == 0 ? a.p_table + (size_t)group * a.max_p_pages : a.table + (size_t)own_b * a.max_pages;
             n.n = parts_n[part];
             n.head = rest - own_b * a.kv_heads;
-            n.tile0 = 0;
-            n.tiles = (n.n + TILE - 1) / TILE;
+            n.tile0 = from[part];
+            n.tiles = to[part] - from[part];
             n.row0 = own_b * a.per_kv + own_q * kPaQueries;
             n.rows = min(a.per_kv - own_q * kPaQueries, kPaQueries);
             ++part;
@@ -435,6 +484,10 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             }
         }
         if (behind_wide) pdl_wait();
+        if constexpr (MODE == kModeClusters) {
+            pa_cluster_sync();
+            pa_cluster_sync();
+        }
         return;
     }
 
@@ -638,8 +691,19 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");
         const bool empty = parts_n[0] + parts_n[1] == 0;
-        const int head = (int)blockIdx.x / query_items(a.per_kv) - own_b * a.kv_heads, half = a.d / 2;
+        const int head = item / query_items(a.per_kv) - own_b * a.kv_heads, half = a.d / 2;
         const size_t out_row = ((size_t)own_b * a.kv_heads + head) * a.per_kv + own_q * kPaQueries;
+        const auto leave = [&](int r, int e, float M, float L, float x, float y) {
+            const float inv = empty ? 0.f : 1.f / L;
+            x = empty ? 0.f : x * inv;
+            y = empty ? 0.f : y * inv;
+            const size_t at = (out_row + r) * a.d + e;
+            if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + at) = pack2<T>(x, y);
+            if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + at) = make_float2(x, y);
+            if (a.lse && e == 0) a.lse[out_row + r] = empty ? -INFINITY : (M + log2f(L)) * 0.693147180559945309f;
+        };
+        // one state per query row and block, behind the warps' states
+        float *merged = mls + 2 * kPaQueries, *merged_ml = merged + kPaQueries * DP;
         for (int i = tid; i < rows * half; i += kPaWarps * 32) {
             const int r = i / half, e = 2 * (i - r * half);
             float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
@@ -651,13 +715,42 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                 x += states[(k * rows + r) * DP + e] * w;
                 y += states[(k * rows + r) * DP + e + 1] * w;
             }
-            const float inv = empty ? 0.f : 1.f / L;
-            x = empty ? 0.f : x * inv;
-            y = empty ? 0.f : y * inv;
-            const size_t at = (out_row + r) * a.d + e;
-            if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + at) = pack2<T>(x, y);
-            if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + at) = make_float2(x, y);
-            if (a.lse && e == 0) a.lse[out_row + r] = empty ? -INFINITY : (M + log2f(L)) * 0.693147180559945309f;
+            if constexpr (MODE != kModeClusters) leave(r, e, M, L, x, y);
+            else {
+                *reinterpret_cast<float2 *>(merged + r * DP + e) = make_float2(x, y);
+                if (e == 0) *reinterpret_cast<float2 *>(merged_ml + 2 * r) = make_float2(M, L);
+            }
+        }
+        if constexpr (MODE == kModeClusters) {
+            // the blocks of the cluster merge their states the same way, each a part of the outputs
+            pa_cluster_sync();
+            const uint32_t at = smem_u32(merged), at_ml = smem_u32(merged_ml);
+            for (int i = rank * kPaWarps * 32 + tid; i < rows * half; i += split * kPaWarps * 32) {
+                const int r = i / half, e = 2 * (i - r * half);
+                float2 ml[kPaSplit], v[kPaSplit];
+#pragma unroll
+                for (int k = 0; k < kPaSplit; ++k) {
+                    ml[k] = make_float2(-INFINITY, 0.f);
+                    v[k] = make_float2(0.f, 0.f);
+                    if (k < split) {
+                        ml[k] = pa_ld_cluster(pa_of_rank(at_ml + 8 * r, k));
+                        v[k] = pa_ld_cluster(pa_of_rank(at + 4 * (r * DP + e), k));
+                    }
+                }
+                float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+                for (int k = 0; k < kPaSplit; ++k) M = fmaxf(M, ml[k].x);
+#pragma unroll
+                for (int k = 0; k < kPaSplit; ++k) {
+                    if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;   // an empty state
+                    const float w = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
+                    L += ml[k].y * w;
+                    x += v[k].x * w;
+                    y += v[k].y * w;
+                }
+                leave(r, e, M, L, x, y);
+            }
+            pa_cluster_sync();                                     // no block ends while another reads its shared memory
         }
     }
 }
@@ -848,14 +941,16 @@ template <typename T, int NSUB, int STAGES, bool PACKED>
 cudaError_t launch_prefix(const PrefixArgs &a, unsigned runs, bool direct, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
     const size_t tiles = 1024 + (size_t)STAGES * 2 * NSUB * tile_rows(NSUB) * 128, plan = (size_t)(2 * a.batch + 4 * a.groups + 2) * 4;
-    static int told[2][64];
+    static int told[3][64];
     if (direct) {
-        const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, true>;
-        const cudaError_t e = allow_smem((const void *)kern, told[0]);
-        return e != cudaSuccess ? e : launch_pdl(kern, dim3((unsigned)(a.batch * a.kv_heads * query_items(a.per_kv))), kPaThreads, tiles, st, a, km, vm);
+        const auto blocks = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, kModeBlocks>, clusters = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, kModeClusters>;
+        const auto kern = a.split > 1 ? clusters : blocks;
+        const cudaError_t e = allow_smem((const void *)kern, told[a.split > 1 ? 1 : 0]);
+        const unsigned grid = (unsigned)(a.batch * a.kv_heads * query_items(a.per_kv) * a.split);
+        return e != cudaSuccess ? e : launch_pdl_cluster(kern, dim3(grid), (unsigned)a.split, kPaThreads, tiles, st, a, km, vm);
     }
-    const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, false>;
-    cudaError_t e = allow_smem((const void *)kern, told[1]);
+    const auto kern = prefix_sweep_kernel<T, NSUB, STAGES, PACKED, kModeList>;
+    cudaError_t e = allow_smem((const void *)kern, told[2]);
     if (e != cudaSuccess) return e;
     e = launch_pdl(kern, dim3(runs), kPaThreads, tiles + plan, st, a, km, vm);
     if (e != cudaSuccess) return e;
@@ -936,8 +1031,10 @@ int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_
     a.n_p_slots = (int)l.p_slots; a.n_o_slots = (int)l.o_slots;
     const double row_bytes = (double)kv->page_rows * l.nsub * 256;
     const double prefix_bytes = n_groups ? max_prefix_pages * row_bytes : 0.0;
-    const bool direct = direct_pays((long long)batch * kv->n_kv_heads * query_items(a.per_kv), l.blocks, a.per_kv,
-                                    max_pages * row_bytes + prefix_bytes, prefix_bytes * (1.0 - fmin(1.0, (double)n_groups / batch)));
+    const long long items = (long long)batch * kv->n_kv_heads * query_items(a.per_kv);
+    const double most = max_pages * row_bytes + prefix_bytes;
+    const bool direct = direct_pays(items, l.blocks, a.per_kv, most, prefix_bytes * (1.0 - fmin(1.0, (double)n_groups / batch)));
+    a.split = direct ? direct_split(items, l.blocks, most) : 1;
     const bool wide = !direct && l.wide_blocks && (long long)max_prefix_pages * kv->page_rows * l.nsub >= kWideRows;
     a.wide_above = wide ? kWideAbove : 0x7fffffff;
     a.w_state = (float *)(ws + l.w_state); a.w_ml = (float *)(ws + l.w_ml);

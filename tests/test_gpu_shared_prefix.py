@@ -384,7 +384,7 @@ ATTN = {  # own rows, prefix rows, group starts, key heads, query heads per key 
 
 
 @pytest.mark.parametrize("dtype", HALF)
-@pytest.mark.parametrize("room", [0, 1800, 8192])
+@pytest.mark.parametrize("room", [0, 1800, 30000])
 @pytest.mark.parametrize("name", list(ATTN))
 def test_shared_prefix_attn_matches_64_bits(name, room, dtype):
     own, prefix, start, kv, per, dim, page = ATTN[name]
@@ -398,7 +398,7 @@ def test_shared_prefix_attn_matches_64_bits(name, room, dtype):
 
 
 @pytest.mark.parametrize("dtype", HALF)
-@pytest.mark.parametrize("rows,room", [(3, 0), (3, 1800), (50, 8192)])
+@pytest.mark.parametrize("rows,room", [(3, 0), (3, 1800), (3, 30000), (50, 30000)])
 def test_shared_prefix_attn_peaked_scores_scale_stride_and_strided_queries(rows, room, dtype):
     """Scores in the tens (one row takes nearly all the weight, and the maximum keeps moving), a scale of the caller's,
     padded pool rows that hold NaN, query rows out of a packed tensor that start on 4-byte boundaries only."""
@@ -448,7 +448,7 @@ def test_shared_prefix_attn_equals_private_copies_of_the_prefix():
     assert ((a.double() - b.double()).abs() <= tol).all()
 
 
-@pytest.mark.parametrize("times", [1, 50])
+@pytest.mark.parametrize("times", [1, 50, 500])
 def test_shared_prefix_attn_lengths_and_boundaries_the_device_finds_wrong(times):
     """Lengths past the tables are cut to them, negative ones to zero; boundaries outside the batch are cut to it; a page
     outside the pool is reported, and touches no other batch row."""
@@ -474,7 +474,7 @@ def test_shared_prefix_attn_lengths_and_boundaries_the_device_finds_wrong(times)
     assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
 
 
-@pytest.mark.parametrize("per,room", [(2, 0), (2, 1800), (40, 8192)])
+@pytest.mark.parametrize("per,room", [(2, 0), (2, 1800), (2, 30000), (40, 30000)])
 def test_shared_prefix_attn_replays_with_new_lengths_and_groups(per, room):
     """One captured call follows lengths, tables, boundaries and queries; another graph with a workspace of its own may
     run beside it."""
