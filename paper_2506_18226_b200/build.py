@@ -36,7 +36,8 @@ def build_marshal(force: bool = False) -> str:
                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     libs = os.path.join(base, "lib")
     tmp = MARSHAL + f".tmp{os.getpid()}"
-    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+    # the system's g++, whatever CXX says: it links the shared C++ library that torch runs on, so that exceptions cross
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{i}" for i in include], MARSHAL_SOURCE,
                            "-o", tmp, f"-L{libs}", f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"])
     os.replace(tmp, MARSHAL)

@@ -26,6 +26,14 @@ decltype(&adsa_norm_residual) c_norm_residual;
 
 struct Raised {};                            // a Python exception is set
 
+// (no streams here: a compiler that links its own C++ library into this module would mix two libraries' locales)
+template <typename Sizes> std::string list_of(const Sizes &sizes)
+{
+    std::string s = "[";
+    for (int64_t n : sizes) s += (s.size() > 1 ? ", " : "") + (n < 0 ? std::string("any") : std::to_string(n));
+    return s + "]";
+}
+
 [[noreturn]] void refuse(const std::string &what)
 {
     PyErr_SetString(PyExc_ValueError, what.c_str());
@@ -63,10 +71,8 @@ struct Check {
             }
         }
         if (!ok) {
-            std::string s = "[";
-            for (int64_t want : shape) s += (s.size() > 1 ? ", " : "") + (want < 0 ? std::string("any") : std::to_string(want));
-            refuse(std::string(call) + ": " + name + " must be " + c10::toString(type) + " " + s + "], got " +
-                   (t.defined() ? std::string(c10::toString(t.scalar_type())) + " " + c10::str(t.sizes()) : std::string("None")));
+            refuse(std::string(call) + ": " + name + " must be " + c10::toString(type) + " " + list_of(shape) + ", got " +
+                   (t.defined() ? std::string(c10::toString(t.scalar_type())) + " " + list_of(t.sizes()) : std::string("None")));
         }
         if (!(whole ? t.is_contiguous() : t.numel() == 0 || t.stride(-1) == 1))
             refuse(std::string(call) + ": " + name + " must be dense" + (whole ? "" : " along its last dimension"));
@@ -76,7 +82,7 @@ struct Check {
     {
         if (t.dim() != dims || (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kHalf))
             refuse(std::string(call) + ": " + name + " must be bfloat16 or float16 with " + std::to_string(dims) + " dimensions, got " +
-                   c10::toString(t.scalar_type()) + " " + c10::str(t.sizes()));
+                   c10::toString(t.scalar_type()) + " " + list_of(t.sizes()));
         return t.scalar_type() == at::kBFloat16 ? ADSA_BF16 : ADSA_F16;
     }
 };

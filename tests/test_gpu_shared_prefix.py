@@ -183,6 +183,8 @@ APPEND = [  # new tokens per batch row, rows before, kv heads, query heads, dim,
     ([9], [570], 2, 2, 30, 40, 572),
     ([300, 20, 411], [7, 100, 0], 8, 32, 128, 136, 24),
     ([0, 0], [5, 6], 2, 2, 64, 64, 16),
+    ([0] * 40 + [3] + [0] * 70 + [1, 1] + [0] * 33 + [2, 0], list(range(148)), 1, 1, 64, 64, 16),
+    ([n % 3 for n in range(1100)], [n % 50 for n in range(1100)], 1, 2, 64, 64, 32),
 ]
 
 
@@ -630,6 +632,48 @@ def test_a_decode_loop_of_all_four_operators():
         want, want_h, nmag, _ = norm64(attn.view(B, D), x_old, w, w, None, 1.0, 1e-5)
         assert ((x.double() - want).abs() <= 2.0 ** -18 * nmag + _u(torch.bfloat16) * want.abs()).all()
     assert not torch.equal(x, x0)
+
+
+def test_the_binding_refuses_tensors_on_the_gpu_of_wrong_types_shapes_and_strides():
+    import paper_2506_18226_b200 as A
+    bf, i32 = torch.bfloat16, torch.int32
+    x, pos = torch.zeros(4, 2, 64, dtype=bf, device=DEV), torch.zeros(4, 2, dtype=i32, device=DEV)
+    rot = A.Rotary(64, (16, 16))
+    A.rope_axes(rot, x, pos)
+    wide = torch.zeros(4, 2, 128, dtype=bf, device=DEV)
+    for args in ((x.float(), pos), (x[..., :62], pos), (wide[..., ::2], pos), (x[0], pos), (x, pos[:3]), (x, pos.long()), (x, pos[:, :1]), (x, pos.cpu()),
+                 (x, pos.T.contiguous().T), (x, pos, x[:3]), (x, pos, x.half()), (x, pos, x.cpu()), (x.cpu(), pos)):
+        with pytest.raises(ValueError, match="rope_axes: "):
+            A.rope_axes(rot, *args)
+    pool = torch.zeros(5, 2, 16, 64, dtype=bf, device=DEV)
+    table, n = torch.zeros(4, 2, dtype=i32, device=DEV), torch.zeros(4, dtype=i32, device=DEV)
+    table[:, 0] = torch.arange(4)
+    one, cu = torch.zeros(1, dtype=i32, device=DEV), torch.arange(5, dtype=i32, device=DEV)
+    good = dict(k=x, v=x, k_pool=pool, v_pool=pool.clone(), page_table=table, n_rows=n)
+    A.paged_append(**good, rotary=rot, pos=pos, q=x, q_out=x.clone(), status=one, cu_tokens=cu)
+    assert int(one) == 0
+    for kw in (dict(v_pool=pool[:4]), dict(k_pool=pool.half()), dict(k_pool=pool[:, :1]), dict(n_rows=n[:3]), dict(n_rows=n[:, None]), dict(n_rows=None),
+               dict(page_table=table.long()), dict(page_table=table[0]), dict(page_table=table.T), dict(k=x.half()), dict(v=x[:, :1]), dict(v=wide[..., ::2]),
+               dict(rotary=rot), dict(rotary=rot, pos=pos[:2]), dict(rotary=A.Rotary(32, (8, 8)), pos=pos), dict(q=x.half()), dict(q=x[:3]),
+               dict(q=x, q_out=x[:, :1]), dict(cu_tokens=n), dict(cu_tokens=cu.cpu()), dict(status=n), dict(status=cu[:1].long()), dict(v=x.cpu())):
+        with pytest.raises(ValueError, match="paged_append: "):
+            A.paged_append(**dict(good, **kw))
+    good = dict(q=x, k_pool=pool, v_pool=pool, page_table=table, n_rows=n, prefix_table=table[:1], prefix_rows=one, group_start=cu[::4].contiguous())
+    A.shared_prefix_attn(**good)
+    for kw in (dict(q=x.half()), dict(q=x[0]), dict(q=wide[..., ::2]), dict(n_rows=n[:2]), dict(n_rows=None), dict(page_table=table[:3]), dict(v_pool=pool[:4]),
+               dict(prefix_rows=n), dict(prefix_rows=None), dict(group_start=one), dict(group_start=None), dict(prefix_table=table[0]), dict(out=x.half()),
+               dict(out=wide[..., ::2]), dict(lse=n), dict(out_f32=x), dict(status=n), dict(k_pool=pool.cpu()), dict(workspace=torch.zeros(8, dtype=torch.uint8))):
+        with pytest.raises(ValueError, match="shared_prefix_attn: "):
+            A.shared_prefix_attn(**dict(good, **kw))
+    with pytest.raises(A.AdsaError):
+        A.shared_prefix_attn(**good, workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))
+    y, w = torch.zeros(4, 64, dtype=bf, device=DEV), torch.zeros(64, dtype=bf, device=DEV)
+    A.norm_residual(y, y.clone(), w)
+    for a, kw in (((y.float(), y, w), {}), ((y[0], y, w), {}), ((y, y[:3], w), {}), ((y, None, w), {}), ((y, y, w[:32]), {}), ((y, y, w.float()), {}),
+                  ((y, y.long(), w), {}), ((y, y, w), dict(gate=w)), ((y, y, w), dict(w_post=y)), ((y, y, w), dict(h=y.float())), ((y, y, None), dict(h=y)),
+                  ((y, y, w), dict(x_out=y[:2])), ((y, y, w.cpu()), {}), ((y[:, ::2], y[:, ::2], w[:32]), {})):
+        with pytest.raises(ValueError, match="norm_residual: "):
+            A.norm_residual(*a, **kw)
 
 
 def test_calls_on_another_stream_and_empty_calls():
