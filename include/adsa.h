@@ -88,7 +88,7 @@ typedef enum {
 #define ADSA_DEV_COPY_TIMEOUT 32u  /* bounded wait on a bulk copy into shared memory ran out */
 /* ... and of the status words that the calls on a paged whole-token cache take (adsa_paged_append, adsa_shared_prefix_attn) */
 #define ADSA_DEV_BAD_PAGE 64u      /* a page table names a page outside the pool */
-#define ADSA_DEV_BAD_GROUPS 128u   /* group boundaries do not ascend */
+#define ADSA_DEV_BAD_GROUPS 128u   /* group boundaries do not ascend (which rows see a prefix is then unspecified) */
 
 typedef struct {
     int32_t n_layers, batch, n_heads; /* multi-head attention: one KV head per query head */
@@ -481,7 +481,7 @@ ADSA_API int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_tabl
 
 /* Decode attention, one query token per batch row, over a prefix that each group of batch rows shares and the batch
  * row's own rows:  out = softmax_j(q.k_j * scale) . v_j  over rows 0 .. prefix_rows[g]-1 of prefix_table[g] and rows
- * 0 .. n_rows[b]-1 of page_table[b].  A prefix is swept once for all rows of its group.
+ * 0 .. n_rows[b]-1 of page_table[b].  A long prefix is swept once for all rows of its group.
  *   q            16-bit [batch][n_heads][head_dim], 4-byte aligned, even strides; n_heads = g * n_kv_heads with g <= 64:
  *                query head h reads key head h / g
  *   n_rows, prefix_rows   int32, each clamped to 0 .. what its table holds; table entries past them are not read
@@ -491,7 +491,8 @@ ADSA_API int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_tabl
  *   lse          float [batch][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
  * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).
  * batch + 2 n_groups <= 4096.  workspace: [device] 256-byte aligned, adsa_shared_prefix_workspace_bytes of them, nothing
- * kept in it from call to call: calls that may overlap on the GPU (other streams, graphs in flight) need one each, and a captured call's must outlive its graph. */
+ * kept in it from call to call: calls that may overlap on the GPU (other streams, graphs in flight) need one each, and a
+ * captured call's must outlive its graph. */
 ADSA_API int adsa_shared_prefix_workspace_bytes(int batch, int n_groups, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes);
 ADSA_API int adsa_shared_prefix_attn(const adsa_paged_kv *kv, const void *q, long long q_row, long long q_head, int batch, int n_heads,
                                      const int32_t *page_table, int max_pages, const int32_t *n_rows, const int32_t *prefix_table,

@@ -282,6 +282,9 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
             group = (int)__reduce_min_sync(0xffffffffu, first);
         }
         if (group >= 0) parts_n[0] = clamp_rows(a.p_rows[group], a.max_p_pages, a.page_rows);
+        if (blockIdx.x == 0 && a.status)
+            for (int g = tid; g < a.groups; g += kPaThreads)
+                if (a.start[g] > a.start[g + 1]) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
         const int pre = (parts_n[0] + TILE - 1) / TILE, all = pre + (parts_n[1] + TILE - 1) / TILE;
         const int lo = (int)((long long)all * rank / split), hi = (int)((long long)all * (rank + 1) / split);
         from[0] = min(lo, pre);
@@ -310,10 +313,18 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
 
         // ---- lengths, boundaries, first unit of every entry: each thread sums a few entries, the sums are scanned over the block ----
         const int per = (entries + kPaThreads - 1) / kPaThreads, e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
-        for (int g = tid; g <= a.groups && a.groups > 0; g += kPaThreads) c.begin[g] = group_begin(a, g);
+        bool falls = false;
+        for (int g = tid; g <= a.groups && a.groups > 0; g += kPaThreads) {
+            c.begin[g] = group_begin(a, g);
+            falls = falls || (g > 0 && a.start[g - 1] > a.start[g]);
+        }
         for (int e = e0; e < e1; ++e)
             c.len[e] = e < a.groups ? clamp_rows(a.p_rows[e], a.max_p_pages, a.page_rows) : clamp_rows(a.n_rows[e - a.groups], a.max_pages, a.page_rows);
-        __syncthreads();
+        if (__syncthreads_or(falls)) {                             // groups that overlap could be more units than are counted in 32 bits
+            for (int g = tid; g <= a.groups; g += kPaThreads) c.begin[g] = 0;
+            if (a.status && tid == 0) atomicOr(a.status, ADSA_DEV_BAD_GROUPS);
+            __syncthreads();
+        }
         uint2 mine = make_uint2(0u, 0u);                               // units of this list, of the wide kernel's
         for (int e = e0; e < e1; ++e) {
             const int m = (e < a.groups ? members(c, e) : 1) * a.per_kv;

@@ -190,10 +190,12 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
     // first unit of every group: one warp, 32 groups at a time
     if (warp == 8) {
         uint32_t before = 0;
+        bool falls = false;
         for (int g0 = 0; g0 < a.groups; g0 += 32) {
             const int g = g0 + lane;
             uint32_t w = 0;
             if (g < a.groups) {
+                falls = falls || a.start[g] > a.start[g + 1];
                 const int m = group_members(a, g) * a.per_kv;
                 if (m > a.wide_above) w = WideItems(m, clamp_rows(a.p_rows[g], a.max_p_pages, a.page_rows)).head_units * (uint32_t)a.kv_heads;
             }
@@ -204,6 +206,10 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
         if (lane == 0) plan[a.groups] = before;
+        if (__any_sync(0xffffffffu, falls)) {                      // (boundaries that do not ascend: no groups, as in the sweep)
+            __syncwarp();
+            for (int g = lane; g <= a.groups; g += 32) plan[g] = 0;
+        }
     }
     tc_before();
     __syncthreads();

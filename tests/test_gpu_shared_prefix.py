@@ -476,6 +476,19 @@ def test_shared_prefix_attn_lengths_and_boundaries_the_device_finds_wrong(times)
     assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
 
 
+@pytest.mark.parametrize("rows,room", [(8, 0), (8, 1800), (8, 30000), (100, 30000), (700, 0)])
+def test_shared_prefix_attn_reports_boundaries_that_do_not_ascend(rows, room):
+    import paper_2506_18226_b200 as A
+    c = attn_case(_gen(43), [5 + b % 7 for b in range(rows)], [150, 20, 90], [0, rows // 2, rows // 4, rows], 2, 2, 64, 16, torch.bfloat16, room=room)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = A.shared_prefix_attn(**c, status=status)
+    assert int(status) == A.binding.DEV_BAD_GROUPS and got.isfinite().all()
+    status.zero_()
+    c["group_start"].copy_(torch.tensor([0, rows // 4, rows // 2, rows], dtype=torch.int32))
+    A.shared_prefix_attn(**c, status=status)
+    assert int(status) == 0
+
+
 @pytest.mark.parametrize("per,room", [(2, 0), (2, 1800), (2, 30000), (40, 30000)])
 def test_shared_prefix_attn_replays_with_new_lengths_and_groups(per, room):
     """One captured call follows lengths, tables, boundaries and queries; another graph with a workspace of its own may
