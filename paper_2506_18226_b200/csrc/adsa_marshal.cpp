@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/headeronly/version.h>
 
 #include <initializer_list>
 #include <string>
@@ -335,4 +336,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "adsa_marshal", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit_adsa_marshal() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit_adsa_marshal()
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);
+    return m;
+}

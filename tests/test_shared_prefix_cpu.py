@@ -157,6 +157,20 @@ def test_norm_residual_refusals(kw):
     assert _norm(**kw) == B.EINVAL
 
 
+def test_a_copy_of_a_rotary_has_a_schedule_of_its_own():
+    import copy
+    import gc
+    import pickle
+    rot = A.Rotary(64, (8, 12), base=500.0, style="halves", restart=False)
+    want = bytes(rot.c)
+    copies = [copy.copy(rot), copy.deepcopy(rot), pickle.loads(pickle.dumps(rot))]
+    assert len({r.ref for r in copies + [rot]}) == 4
+    del rot
+    gc.collect()
+    for r in copies:
+        assert r.ref == C.addressof(r.c) and bytes(r.c) == want and (r.head_dim, r.n_axes) == (64, 2)
+
+
 def test_the_binding_refuses_wrong_types_shapes_and_devices():
     bf, i32 = torch.bfloat16, torch.int32
     x, pos = torch.zeros(4, 2, 64, dtype=bf), torch.zeros(4, 2, dtype=i32)
