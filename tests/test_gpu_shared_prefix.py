@@ -476,6 +476,30 @@ def test_shared_prefix_attn_lengths_and_boundaries_the_device_finds_wrong(times)
     assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
 
 
+@pytest.mark.parametrize("rows,room", [(3, 0), (3, 1800), (3, 30000), (40, 30000)])
+def test_shared_prefix_attn_scores_that_are_not_finite(rows, room):
+    """A score of -inf has no weight; a softmax over -inf alone, +inf or NaN is NaN, for the rows that attend it and no other."""
+    c = attn_case(_gen(47), [70, 9, 20] + [9] * (rows - 3), [150], [0, rows - 1], 1, 2, 64, 16, torch.bfloat16, room=room)
+    c["q"] = c["q"].abs() + 0.1
+    r = torch.arange(150, device=DEV)
+    prefix = c["prefix_table"][0][r // 16].long()
+    own = c["page_table"][0][33 // 16].long()
+    was = c["k_pool"].clone()
+    plain = run_attn(dict(c, prefix_rows=torch.zeros_like(c["prefix_rows"])))
+    c["k_pool"][prefix, :, r % 16] = -float("inf")
+    got = run_attn(c)
+    # the same weights of the own rows, summed in 32 bits in either case
+    for a, b in zip(got[1:], plain[1:]):
+        assert ((a - b).abs() <= 2.0 ** -18 * (b.abs().amax() + 8)).all()
+    alone = run_attn(dict(c, n_rows=torch.zeros_like(c["n_rows"])))
+    assert alone[1][:-1].isnan().all() and (alone[2] == -float("inf")).all() and (alone[1][-1] == 0).all()
+    c["k_pool"].copy_(was)
+    for bad in (float("inf"), float("nan")):
+        c["k_pool"][own, :, 33 % 16] = bad
+        got = run_attn(c)
+        assert got[1][0].isnan().all() and got[2][0].isnan().all() and got[1][1:].isfinite().all() and got[2][1:].isfinite().all()
+
+
 @pytest.mark.parametrize("rows,room", [(8, 0), (8, 1800), (8, 30000), (100, 30000), (700, 0)])
 def test_shared_prefix_attn_reports_boundaries_that_do_not_ascend(rows, room):
     import paper_2506_18226_b200 as A
