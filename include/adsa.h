@@ -423,7 +423,8 @@ ADSA_API int adsa_cfg_sample(const void *logits, int n_images, int vocab, float 
  *
  * Rules they share.  All pointers are [device] unless marked [host] and belong to the current device.  16-bit tensors
  * are ADSA_BF16 or ADSA_F16, all tensors of a call the same; strides are in elements, the innermost dimension is
- * dense; arithmetic is fp32 and each output is rounded once, to nearest even.  Calls only enqueue kernels on `stream`,
+ * dense; arithmetic is fp32 and each output is rounded once, to nearest even (the attention's weights meet V as the sum of
+ * two 16-bit values: off by at most 2^-16 of themselves for bfloat16, 2^-22, or 2^-30 of the largest, for half).  Calls only enqueue kernels on `stream`,
  * may be captured into a graph, and read lengths, tables and positions when they run.  ADSA_EINVAL (null pointer,
  * misaligned buffer, size outside the stated range) and ADSA_ENOMEM are found before anything is launched.  What only
  * the device can see sets bits of *status (one word, only ever ORed into; NULL: not wanted) and skips the access. */

@@ -513,10 +513,11 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     };
     int stage = 0;
     uint32_t phase = 0;
-    // Q^T as the B operand: query row g of this warp's eight, elements 16 ks + 2 t4, + 1 and + 8, + 9; asked for one segment ahead
+    // Q^T as the B operand: query row g of this warp's eight, elements 16 ks + 2 t4, + 1 and + 8, + 9; asked for one segment ahead.
+    // Up to four query rows are there twice: columns 0 .. 3 of the products carry the weights' hi parts on, columns 4 .. 7 the lo parts.
     uint32_t qn[KS][2];
     const auto ask_q = [&](const Segment &n) {
-        const int qb = warp & (query_warps(n.rows) - 1), r = qb * 8 + g, packed = n.row0 + r, b = packed / a.per_kv, j = packed - b * a.per_kv;
+        const int qb = warp & (query_warps(n.rows) - 1), r = n.rows <= 4 ? g & 3 : qb * 8 + g, packed = n.row0 + r, b = packed / a.per_kv, j = packed - b * a.per_kv;
         const T *qp = (const T *)a.q + b * a.q_row + (n.head * a.per_kv + j) * a.q_head;
         const bool there = r < n.rows;
 #pragma unroll
@@ -536,6 +537,15 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
     float o[KS][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
 #pragma unroll
     for (int dp = 0; dp < KS; ++dp) { o[dp][0] = o[dp][1] = o[dp][2] = o[dp][3] = 0.f; }
+    const float lo_whole = t4 >= 2 ? WeightSplit<T>::one : 0.f;
+    const uint32_t lo_sign = t4 >= 2 ? 0x80000000u : 0u;
+    const auto add_lo_columns = [&]() {
+#pragma unroll
+        for (int dp = 0; dp < KS; ++dp) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[dp][i] += __shfl_xor_sync(0xffffffffu, o[dp][i], 2);
+        }
+    };
     while (more == kSegment) {
         s = nxt;
         uint32_t qa[KS][2];
@@ -545,6 +555,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         if (more == kSegment) ask_q(nxt);
         const int wq = query_warps(s.rows), wk = kPaWarps / wq;     // warps over query rows, warps over cached rows
         const int qb = warp & (wq - 1), kb = warp / wq;
+        const bool apart = s.rows > 4;                              // the lo parts are a product of their own
         for (int t = s.tile0; t < s.tile0 + s.tiles; ++t) {
             if (!mbar_wait_bounded(full + 8 * stage, phase, limit)) {
                 limit = kCopySpinAfterTimeout;
@@ -599,11 +610,13 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                         for (int dp = 0; dp < KS; ++dp) { o[dp][h] *= corr; o[dp][h + 2] *= corr; }
                     }
                 }
-                uint32_t pb[NB][2];
-                {
-                    float shift[2];
+                float shift[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) shift[h] = kBias - (m_run[h] == -INFINITY ? 0.f : m_run[h]) * a.scale_log2e;
+                for (int h = 0; h < 2; ++h) shift[h] = kBias - (m_run[h] == -INFINITY ? 0.f : m_run[h]) * a.scale_log2e;
+                // weights, then O += P V; kApart: a branch around each of the second products would stand between the loads of V
+                const auto weigh = [&](auto kApart) {
+                    constexpr bool APART = decltype(kApart)::value;
+                    uint32_t pb[NB][2], pl[APART ? NB : 1][2];
 #pragma unroll
                     for (int n = 0; n < NB; ++n) {
                         float p[4];
@@ -612,37 +625,51 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
                             p[i] = pa_exp2(fmaf(sc[n][i], a.scale_log2e, shift[i & 1]));
                             l_run[i & 1] += p[i];                   // the sum takes the weights before they are rounded
                         }
-                        pb[n][0] = pa_transpose(pack2<T>(p[0], p[1]));
-                        pb[n][1] = pa_transpose(pack2<T>(p[2], p[3]));
-                    }
-                }
-                // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN of V
-                if (!tail) {
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-#pragma unroll
-                        for (int dp = 0; dp < KS; ++dp) {
-                            if (PACKED && dp >= KS - 4 && 16 * dp >= a.d) break;   // (rows of O past the head elements are not kept)
-                            uint32_t vf[4];
-                            pa_ldsm_t(v_at + n * 16u * pitch + piece_at(dp, v_ch), vf);
-                            pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 w = make_float2(p[2 * i], p[2 * i + 1]);
+                            if constexpr (APART) {
+                                uint32_t hi, lo;
+                                split_weights<T>(w, hi, lo);
+                                pb[n][i] = pa_transpose(hi);
+                                pl[n][i] = pa_transpose(lo);
+                            } else {
+                                pb[n][i] = pa_transpose(weights_of_lane<T>(w, lo_whole, lo_sign));
+                            }
                         }
                     }
-                } else {
+                    // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN of V
+                    if (!tail) {
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-                        const int left = valid - c0 - 16 * n - 2 * t4;   // of the cached rows 2 t4, + 1 and + 8, + 9
-                        const uint32_t lo = left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u, hi = left >= 10 ? 0xffffffffu : left == 9 ? 0xffffu : 0u;
+                        for (int n = 0; n < NB; ++n) {
 #pragma unroll
-                        for (int dp = 0; dp < KS; ++dp) {
-                            if (PACKED && dp >= KS - 4 && 16 * dp >= a.d) break;   // (rows of O past the head elements are not kept)
-                            uint32_t vf[4];
-                            pa_ldsm_t(v_at + n * 16u * pitch + piece_at(dp, v_ch), vf);
-                            vf[0] &= lo; vf[1] &= lo; vf[2] &= hi; vf[3] &= hi;
-                            pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
+                            for (int dp = 0; dp < KS; ++dp) {
+                                if (PACKED && dp >= KS - 4 && 16 * dp >= a.d) break;   // (rows of O past the head elements are not kept)
+                                uint32_t vf[4];
+                                pa_ldsm_t(v_at + n * 16u * pitch + piece_at(dp, v_ch), vf);
+                                pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
+                                if constexpr (APART) pa_mma<T>(o[dp], vf, pl[n][0], pl[n][1]);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) {
+                            const int left = valid - c0 - 16 * n - 2 * t4;   // of the cached rows 2 t4, + 1 and + 8, + 9
+                            const uint32_t lo = left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u, hi = left >= 10 ? 0xffffffffu : left == 9 ? 0xffffu : 0u;
+#pragma unroll
+                            for (int dp = 0; dp < KS; ++dp) {
+                                if (PACKED && dp >= KS - 4 && 16 * dp >= a.d) break;   // (rows of O past the head elements are not kept)
+                                uint32_t vf[4];
+                                pa_ldsm_t(v_at + n * 16u * pitch + piece_at(dp, v_ch), vf);
+                                vf[0] &= lo; vf[1] &= lo; vf[2] &= hi; vf[3] &= hi;
+                                pa_mma<T>(o[dp], vf, pb[n][0], pb[n][1]);
+                                if constexpr (APART) pa_mma<T>(o[dp], vf, pl[n][0], pl[n][1]);
+                            }
                         }
                     }
-                }
+                };
+                if (apart) weigh(std::true_type{});
+                else weigh(std::false_type{});
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);
@@ -650,6 +677,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         }
         if constexpr (!DIRECT) {                                   // (else the own rows carry the state of the prefix on)
             // ---- the partial state: a slot holds wk states of s.rows rows ----
+            if (!apart) add_lo_columns();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -685,6 +713,7 @@ prefix_sweep_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant_
         // ---- the warps' states to shared memory (the tiles have been read), then the outputs ----
         const int rows = min(a.per_kv - own_q * kPaQueries, kPaQueries), wq = query_warps(rows), wk = kPaWarps / wq, qb = warp & (wq - 1), kb = warp / wq;
         float *states = reinterpret_cast<float *>(pa_smem + (ring - smem_u32(pa_smem))), *mls = states + kPaQueries * DP;
+        if (rows <= 4) add_lo_columns();
         asm volatile("bar.sync 1, 128;" ::: "memory");
 #pragma unroll
         for (int h = 0; h < 2; ++h) {

@@ -4,11 +4,11 @@
 // A block (one per SM) has two groups of four warps, a query row per thread, with a 128-row tile of Q, 128 tensor-memory
 // columns of scores and up to 128 of O each.  Per tile of 128 cached rows and group: S = Q K^T (tcgen05, 128 x 128, operands
 // in shared memory), softmax weights by the group's threads (row maxima and sums need no exchange between threads), P
-// written back over S in tensor memory as 16-bit values, O += P V (tcgen05, P as the tensor-memory operand, V as it lies:
-// rows of K, elements contiguous).  One warp copies (TMA) and one thread issues all products, so that one group's products run
-// under the other's softmax.  An item is 256 query rows of a key head: both groups take every tile of K and V, each with its
-// own 128 rows, so a tile is fetched once for 256 rows; the last 128 or fewer rows of a group are an item whose tiles the
-// two groups take in turns.
+// written back over S in tensor memory as 16-bit values, a hi and a lo part (split_weights) over 64 columns each, O += P V for both
+// (tcgen05, P as the tensor-memory operand, V as it lies: rows of K, elements contiguous).  One warp copies (TMA) and one thread
+// issues all products, so that one group's products run under the other's softmax.  An item is 256 query rows of a key head: both
+// groups take every tile of K and V, each with its own 128 rows, so a tile is fetched once for 256 rows; the last 128 or fewer
+// rows of a group are an item whose tiles the two groups take in turns.
 //
 // 256 rows x 8 key heads of 128 over 32768 cached rows (34 GFLOP) stream in 24 us once every SM has its first tile,
 // 1.4 PFLOP/s; first tiles and the states at the end cost as much again as a third of that.  What bounds an iteration (128 cached
@@ -75,6 +75,11 @@ __device__ __forceinline__ void tc_store16(uint32_t at, const uint32_t (&r)[16])
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                  ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
                  "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tc_store8(uint32_t at, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 __device__ __forceinline__ void tc_load16(uint32_t at, float (&v)[16])
 {
@@ -305,6 +310,7 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
                     for (int k = 0; k < kWideTile / 32; ++k) {
                         const int ks = half * (kWideTile / 32) + k;
                         tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, !first || ks > 0);
+                        tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + 64 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, 1u);
                     }
                 }
                 __syncwarp();
@@ -446,18 +452,19 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
                 const float shift = kBias - (m == -INFINITY ? 0.f : m) * a.scale_log2e;
                 const float2 scale2 = make_float2(a.scale_log2e, a.scale_log2e), shift2 = make_float2(shift, shift);
 #pragma unroll
-                for (int c = 0; c < kWideTile; c += 32) {
-                    uint32_t p[16];
+                for (int c = 0; c < kWideTile; c += 16) {
+                    uint32_t p[8], p_lo[8];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
+                    for (int k = 0; k < 8; ++k) {
                         float2 x = fma2(make_float2(v[c + 2 * k], v[c + 2 * k + 1]), scale2, shift2);
                         x.x = pa_exp2(x.x);
                         x.y = pa_exp2(x.y);
                         l2[k & 1] = add2(l2[k & 1], x);            // the sum takes the weights before they are rounded
-                        p[k] = pack2<T>(x.x, x.y);
+                        split_weights<T>(x, p[k], p_lo[k]);
                     }
-                    tc_store16(s_col + c / 2, p);                  // over scores that are in registers by now
-                    if (c % 64 == 32) {
+                    tc_store8(s_col + c / 2, p);                   // over scores that are in registers by now
+                    tc_store8(s_col + 64 + c / 2, p_lo);
+                    if (c % 64 == 48) {
                         tc_store_wait();
                         tc_before();
                         __syncwarp();
