@@ -1,20 +1,24 @@
-"""adsa_shared_prefix_attn against 64 bits, as near as its 32-bit sums of 16-bit products can come.
+"""adsa_shared_prefix_attn against 64 bits where a block has long runs: many tiles of a prefix on tcgen05, and lists that are cut
+into runs of several sizes, with items that go on from one run to the next.
 
 Tolerances.  A weight enters the second product as the sum of two 16-bit values (cut, then rounded): bfloat16 keeps 16 bits of it
 (off by at most 2^-16), float16 22 (2^-22), but no less than 2^-30 of the largest weight.  A score's 32-bit error is counted as in
 test_gpu_shared_prefix.py, which moves a weight and the sum it is divided by.  A state of n cached rows takes 2 n / 16 matrix products
 and as many rescalings at most into its 32-bit sums, each off by 2^-23 of what has been summed (tensor cores cut);
 the merge, exponentials and the rest: 2^-18."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_shared_prefix import HALF, _gen, _u, attn64, attn_case, run_attn
+from prefix_cut import Cut, WideCut, sweep_units, wide_units
+from test_gpu_shared_prefix import DEV, HALF, _gen, _randn, _u, attn64, attn_case, run_attn
 
 pytestmark = pytest.mark.gpu
 
 
 def attn64_of(c, rows, scale):
-    """attn64 for some batch rows, each as a group of its own; and the largest |v| there is."""
+    """attn64 for some batch rows, each as a group of its own."""
     start = c["group_start"].tolist() if c["group_start"] is not None else []
     parts = []
     for b in rows:
@@ -87,3 +91,76 @@ def test_infinities_in_attended_values(per, room, dtype):
         want[0, per:, 8] = -float("inf")
         assert torch.equal(a, want)
     assert torch.equal(got[2], plain[2])
+
+
+# ---- many tiles a block on tcgen05 --------------------------------------------------------------------------------------
+
+def steps_of_scores(c, dim, prefix):
+    """Moves each prefix's keys along a direction that every query shares, further from tile to tile and back again: maxima rise by about three
+    (log2) a tile of 128 rows, so that sums are rescaled, and a run may begin anywhere on the slope."""
+    page = c["k_pool"].shape[2]
+    c["q"].add_(0.5)
+    for g, n in enumerate(prefix):
+        r = torch.arange(n, device=DEV)
+        pg = c["prefix_table"][g][r // page].long()
+        rise = ((r // 128) % 11).double() * (3 * math.log(2) / (0.5 * math.sqrt(dim)))
+        at = c["k_pool"][pg, :, r % page, :dim].double() * 0.3 + rise[:, None, None]
+        c["k_pool"][pg, :, r % page, :dim] = at.to(c["k_pool"].dtype)
+
+
+WIDE = {  # batch rows of each group, prefix rows, key heads, query heads per key head, dim, page rows
+    "256 query rows, 128 elements": ([64], [33000], 8, 4, 128, 64),
+    "256 and 64, 64 elements": ([80], [33000], 4, 4, 64, 64),
+    "256 and 144, 100 elements": ([100], [33001], 4, 4, 100, 64),
+    "100 in turns, 64 elements": ([50], [50000], 8, 2, 64, 128),
+    "70 in turns, 128 elements": ([35], [40077], 8, 2, 128, 48),
+    "three groups, 128 elements": ([64, 30, 45], [30000, 9000, 18001], 4, 4, 128, 64),
+    "three groups, 64 elements": ([65, 45, 3, 30], [30000, 19000, 500, 9127], 4, 4, 64, 572),
+    "three groups, 30 elements": ([128, 33, 66], [30000, 31000, 18001], 4, 2, 30, 40),
+}
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("rising", [False, True])
+@pytest.mark.parametrize("name", list(WIDE))
+def test_many_tiles_of_a_prefix_in_a_block(name, rising, dtype):
+    members, prefix, kv, per, dim, page = WIDE[name]
+    start = [0]
+    for m in members:
+        start.append(start[-1] + m)
+    batch = start[-1]
+    own = [(7 * b) % 41 for b in range(batch)]
+    c = attn_case(_gen(len(name) + dim), own, prefix, start, kv, per, dim, page, dtype, q_scale=1.0)
+    if rising:
+        steps_of_scores(c, dim, prefix)
+    units = wide_units(prefix, start, kv, per)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert units / WideCut(units, sms).runs > 12 and batch * per > 32 * len(prefix)   # the ring goes round more than twice
+    got = run_attn(c)
+    rows = sorted({0, 1, 31, batch // 2, batch - 2, batch - 1} | {min(batch - 1, s + d) for s in start for d in (0, 17)} - {-1})
+    state = (units // sms + 2) * 128
+    check_close(c, got, rows, attn64_of(c, rows, dim ** -0.5), dtype, state, max(prefix) + 41)
+    assert all(torch.equal(a, b) for a, b in zip(got, run_attn(c)))
+
+
+# ---- runs of several sizes ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("dim", [64, 100, 128, 200])
+@pytest.mark.parametrize("K,rows", [(2, 11), (3, 24), (4, 52), (5, 88)])
+def test_runs_of_several_sizes(K, rows, dim, dtype):
+    """Ragged own rows and the prefixes of four groups in one list that is cut into 2 .. 5 sizes of runs: items of up to 40 tiles lie
+    across runs of different sizes."""
+    heads = {64: 32, 100: 16, 128: 16, 200: 8}[dim]
+    own = [[100 + (877 * b) % 2200, 0, 2300, 64 * (b % 30)][b % 4 if b % 5 == 0 else 0] for b in range(rows)]
+    prefix, start = [2424, 1, 700, 2500], [0, rows // 4, rows // 4 + 1, rows // 2, rows - 1]
+    units = sweep_units(own, prefix, start, heads, 1, dim)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    cut = Cut(units, sms * (2 if dim <= 128 else 1))
+    assert cut.K == K or sms != 148
+    c = attn_case(_gen(K + dim), own, prefix, start, heads, 1, dim, 64 if dim != 100 else 48, dtype, room=6000)
+    got = run_attn(c)
+    some = sorted({0, 1, 5, rows // 4, rows // 2, rows - 2, rows - 1} | set(range(0, rows, 7)))
+    ref = attn64_of(c, some, dim ** -0.5)
+    check_close(c, got, some, ref, dtype, 4800, 4800)
+    assert all(torch.equal(a, b) for a, b in zip(got, run_attn(c)))
