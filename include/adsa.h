@@ -461,7 +461,8 @@ ADSA_API int adsa_rotary_init(adsa_rotary *rot, int head_dim, int n_axes, const 
 
 /* out = x turned.  x, out: 16-bit [n_tokens][n_heads][head_dim] with the given token and head strides; out may be x
  * (same strides), and must not overlap it otherwise.  pos: int32 [n_tokens][n_axes], any value.  Angles are reduced
- * in 64 bits, so far positions keep their fraction of a turn. */
+ * in 64 bits, so far positions keep their fraction of a turn.  A token may have 65535 heads (q, k and v of an append
+ * together), more of them if a head is short; what a grid cannot hold is ADSA_EINVAL. */
 ADSA_API int adsa_rope_axes(const adsa_rotary *rot, int dtype, const void *x, long long x_token, long long x_head, const int32_t *pos,
                             long long n_tokens, int n_heads, void *out, long long out_token, long long out_head, adsa_stream_t stream);
 

@@ -151,6 +151,7 @@ PyObject *rope_axes(PyObject *const *a, Py_ssize_t n)
     const int64_t tokens = x.size(0), heads = x.size(1);
     c.wants(x, "x", x.scalar_type(), {-1, -1, rot->head_dim}, false);
     c.wants(pos, "pos", at::kInt, {tokens, rot->n_axes}, true);
+    if (heads > 0x7fffffff) refuse("rope_axes: sizes out of range");
     at::Tensor out = tensor(a[3], c.call, "out");
     if (out.defined()) c.wants(out, "out", x.scalar_type(), {tokens, heads, rot->head_dim}, false);
     else out = at::empty(x.sizes(), x.options());

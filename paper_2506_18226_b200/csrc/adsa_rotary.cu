@@ -297,7 +297,9 @@ int run_turn(TurnArgs &a, const adsa_rotary &rot, int dtype, cudaStream_t st)
     acc = fit(fit(fit(acc, a.q), a.k), a.v);
     a.rot_units = halves ? a.n / acc : 0;
     a.units = halves ? a.rot_units + (a.d - 2 * a.n) / acc : acc == 1 ? a.d / 2 : a.d / acc;
-    const int heads = a.q.heads + a.k.heads + a.v.heads;
+    const long long all_heads = (long long)a.q.heads + a.k.heads + a.v.heads;
+    if (all_heads * a.units > 65535LL * kTurnMaxThreads) return ADSA_EINVAL;      // (a chunk of heads takes up to that many units)
+    const int heads = (int)all_heads;
     // Heads a block: all of them if they make up to 512 units, fewer until every SM has a block.  Tokens a block: as many as
     // let all blocks run at once (2048 threads an SM), at most 16: a second, thinner wave costs as much as a full one.
     int chunks = (heads * a.units + kTurnMaxThreads - 1) / kTurnMaxThreads;
