@@ -187,7 +187,8 @@ PyObject *paged_append(PyObject *const *a, Py_ssize_t n)
         if (rot->head_dim != d) refuse("paged_append: the rotary is for another head dimension than k's");
         c.wants(pos, "pos", at::kInt, {tokens, rot->n_axes}, true);
     }
-    at::Tensor q_out = q.defined() ? tensor(a[10], c.call, "q_out") : none;
+    at::Tensor q_out = tensor(a[10], c.call, "q_out");
+    if (q_out.defined() && !q.defined()) refuse("paged_append: q_out needs q");
     int64_t q_heads = 0, qs[4] = {0, 0, 0, 0};
     if (q.defined()) {
         c.wants(q, "q", type, {tokens, -1, d}, false);
@@ -228,6 +229,8 @@ PyObject *shared_prefix_attn(PyObject *const *a, Py_ssize_t n)
         p_pages = p_table.size(1);
         c.wants(p_rows, "prefix_rows", at::kInt, {groups}, true);
         c.wants(start, "group_start", at::kInt, {groups + 1}, true);
+    } else if (p_rows.defined() || start.defined()) {
+        refuse("shared_prefix_attn: prefix_rows and group_start need prefix_table");
     }
     if (status.defined()) c.wants(status, "status", at::kInt, {1}, true);
     at::Tensor out = tensor(a[9], c.call, "out");
