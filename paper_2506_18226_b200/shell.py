@@ -273,6 +273,7 @@ class SharedPromptShell(_Decoder):
     def __init__(self, cfg: ShellConfig, seed: int = 0, device: str = "cuda:0", use_graphs: bool = True):
         super().__init__(cfg, seed, device)
         self.use_graphs, self.graph = use_graphs, None
+        self.next_cell = None                                              # the grid cell decode_step makes next; None before a prefill
         L, H, d, n, pr = cfg.n_layers, cfg.n_heads, cfg.head_dim, cfg.n_images, self.PAGE_ROWS
         bf, i32 = dict(dtype=torch.bfloat16, device=self.dev), dict(dtype=torch.int32, device=self.dev)
         cells = cfg.grid_h * cfg.grid_w
@@ -338,6 +339,7 @@ class SharedPromptShell(_Decoder):
         self.h.copy_(h.view(2, T, c.dim)[:, -1].repeat_interleave(c.n_images, 0))   # every image starts from the same row
         self._sample()
         self.ids_host[0].copy_(self.tokens, non_blocking=True)
+        self.next_cell = 1
         return self.tokens
 
     def _sample(self):
@@ -369,7 +371,10 @@ class SharedPromptShell(_Decoder):
         self._sample()
 
     def decode_step(self, cell):
-        """The image token of grid cell `cell` (>= 1, in order) from the token of cell - 1."""
+        """The image token of grid cell `cell` (after prefill: 1, 2, .. to the end of the grid) from the token of cell - 1."""
+        cells = self.cfg.grid_h * self.cfg.grid_w
+        if cell != self.next_cell or cell >= cells:                        # (the step follows counters on the device, past the grid's tables too)
+            raise ValueError(f"decode_step: cell {cell} cannot follow, the next is {self.next_cell} of {cells} (None: prefill first)")
         if not self.use_graphs:
             self._step()
         else:
@@ -389,4 +394,5 @@ class SharedPromptShell(_Decoder):
             self.graph.replay()
         self.ids_host[cell].copy_(self.tokens, non_blocking=True)
         self.kernel_calls += 1 + 5 * self.cfg.n_layers + 1
+        self.next_cell = cell + 1
         return self.tokens

@@ -24,3 +24,40 @@ def test_more_heads_than_a_grid_holds_are_refused(heads, halves):
     kv = B.AdsaPagedKv(P, P, 0, 10, 2, 16, 64, 64)
     assert A.load().adsa_paged_append(C.byref(kv), P, 1, 3, P, None, 1, P + 2, 128, 64, P, 128, 64, C.byref(r), P, P, heads, 0, 64, P, 0, 64,
                                       None, None) == B.EINVAL
+
+
+def _shell_without_a_gpu(grid):
+    """A SharedPromptShell whose step does nothing but count."""
+    import torch
+    from paper_2506_18226_b200.shell import SharedPromptShell, ShellConfig
+
+    class Counting(SharedPromptShell):
+        def __init__(self):
+            self.cfg = ShellConfig(n_layers=1, dim=64, n_heads=1, ffn_hidden=64, vocab=8, n_text=1, grid_h=grid, grid_w=grid, n_images=2)
+            self.dev, self.use_graphs, self.graph, self.kernel_calls, self.steps = torch.device("cpu"), False, None, 0, 0
+            self.next_cell = None
+            self.ids_host, self.tokens = torch.zeros(grid * grid, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+
+        def _step(self):
+            self.steps += 1
+
+    return Counting()
+
+
+def test_the_shared_prompt_shell_stops_at_the_end_of_its_grid():
+    """A step beyond it would look up a position and random numbers that the device does not have."""
+    sh = _shell_without_a_gpu(3)
+    for cell in (0, 1, 8):
+        with pytest.raises(ValueError, match="prefill first"):
+            sh.decode_step(cell)
+    sh.next_cell = 1                                                              # as after a prefill
+    for cell in range(1, 9):
+        for other in (0, cell - 1, cell + 1, 9, -1):
+            if other != cell:
+                with pytest.raises(ValueError):
+                    sh.decode_step(other)
+        assert sh.decode_step(cell) is sh.tokens
+    for cell in (8, 9, 10):
+        with pytest.raises(ValueError):
+            sh.decode_step(cell)
+    assert sh.steps == 8
