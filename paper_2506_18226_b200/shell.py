@@ -269,8 +269,11 @@ class SharedPromptShell(_Decoder):
     condition's rows kept once.  Nothing is evicted."""
 
     PAGE_ROWS = 64
+    ATTN_ROWS = 4096            # query rows that one attention call takes
 
     def __init__(self, cfg: ShellConfig, seed: int = 0, device: str = "cuda:0", use_graphs: bool = True):
+        if cfg.n_text < 1:
+            raise ValueError("SharedPromptShell: the condition needs a row at least (the first token is drawn from its last)")
         super().__init__(cfg, seed, device)
         self.use_graphs, self.graph = use_graphs, None
         self.next_cell = None                                              # the grid cell decode_step makes next; None before a prefill
@@ -327,12 +330,14 @@ class SharedPromptShell(_Decoder):
             q, k, v = torch.matmul(h.unsqueeze(0), self.wqkv_t[layer]).view(3, 2 * T, H, d)
             B.rope_axes(self.rotary, q, pos, out=q)
             B.paged_append(k, v, self.k_pool[layer], self.v_pool[layer], self.prefix_table, none, rotary=self.rotary, pos=pos, status=self.status)
-            B.shared_prefix_attn(q, self.k_pool[layer], self.v_pool[layer], tables, lengths, out=out, status=self.status)
+            for i in range(0, 2 * T, self.ATTN_ROWS):
+                part = slice(i, i + self.ATTN_ROWS)
+                B.shared_prefix_attn(q[part], self.k_pool[layer], self.v_pool[layer], tables[part], lengths[part], out=out[part], status=self.status)
             return out.view(2 * T, c.dim)
 
         for layer in range(c.n_layers):
             self._block(layer, x, h, y, attend)
-        self.kernel_calls += 1 + 6 * c.n_layers + 1
+        self.kernel_calls += 1 + (5 + len(range(0, 2 * T, self.ATTN_ROWS))) * c.n_layers + 1
         self.n_before.zero_()
         self.n_after.fill_(1)
         self.cell.fill_(0)

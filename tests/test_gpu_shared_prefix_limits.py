@@ -28,3 +28,23 @@ def test_arguments_that_no_call_would_read_are_refused():
     table[:, 0] = torch.arange(4)
     with pytest.raises(ValueError, match="paged_append: q_out needs q"):
         A.paged_append(x, x, pool, pool.clone(), table, n, q_out=x.clone())
+
+
+def test_the_shared_prompt_shell_takes_long_conditions():
+    """More rows than one attention call has queries for: the logits after the condition agree with the shell that keeps private
+    caches, as two bf16 evaluations of one decoder do, and the first steps follow."""
+    from paper_2506_18226_b200.shell import LlamaGenShell, SharedPromptShell, ShellConfig
+    cfg = ShellConfig(n_layers=2, dim=128, n_heads=2, ffn_hidden=256, vocab=512, n_text=2100, grid_h=2, grid_w=2, n_images=2, top_k=50,
+                      budget_fraction=1.0)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    text = torch.randn(2, cfg.n_text, cfg.dim, generator=g, device=DEV).to(torch.bfloat16)
+    a, b = LlamaGenShell(cfg, seed=2, use_graphs=False), SharedPromptShell(cfg, seed=2)
+    a.prefill(text.repeat_interleave(cfg.n_images, 0).contiguous())
+    b.prefill(text)
+    for cell in range(1, 4):
+        x, y = a.logits.double(), b.logits.double()
+        assert float((x - y).norm() / x.norm()) <= 3e-2 and float((x * y).sum() / (x.norm() * y.norm())) >= 0.999
+        a.tokens.copy_(b.tokens)
+        a.decode_step(cell)
+        b.decode_step(cell)
+    assert int(b.status) == 0

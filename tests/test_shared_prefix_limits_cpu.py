@@ -61,3 +61,9 @@ def test_the_shared_prompt_shell_stops_at_the_end_of_its_grid():
         with pytest.raises(ValueError):
             sh.decode_step(cell)
     assert sh.steps == 8
+
+
+def test_the_shared_prompt_shell_refuses_a_condition_of_no_rows():
+    from paper_2506_18226_b200.shell import SharedPromptShell, ShellConfig
+    with pytest.raises(ValueError, match="condition"):
+        SharedPromptShell(ShellConfig(n_layers=1, dim=64, n_heads=1, ffn_hidden=64, vocab=8, n_text=0, grid_h=2, grid_w=2, n_images=1))
