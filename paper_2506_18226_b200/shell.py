@@ -317,6 +317,11 @@ class SharedPromptShell(_Decoder):
     def prefill(self, text_emb):
         """The condition, text_emb [2, n_text, dim] bf16 (conditional, unconditional), enters the shared pages; row i of it
         attends rows 0 .. i, as so many queries over the same pages with lengths 1, 2, ..  Draws the first tokens."""
+        self.next_cell = None                                              # (until the condition is whole)
+        with torch.cuda.device(self.dev):                                  # (calls go to the current device's stream)
+            return self._prefill(text_emb)
+
+    def _prefill(self, text_emb):
         c, T, H, d = self.cfg, self.cfg.n_text, self.cfg.n_heads, self.cfg.head_dim
         i32 = dict(dtype=torch.int32, device=self.dev)
         x = text_emb.reshape(2 * T, c.dim).clone()
@@ -380,24 +385,25 @@ class SharedPromptShell(_Decoder):
         cells = self.cfg.grid_h * self.cfg.grid_w
         if cell != self.next_cell or cell >= cells:                        # (the step follows counters on the device, past the grid's tables too)
             raise ValueError(f"decode_step: cell {cell} cannot follow, the next is {self.next_cell} of {cells} (None: prefill first)")
-        if not self.use_graphs:
-            self._step()
-        else:
-            if self.graph is None:
-                side = torch.cuda.Stream(device=self.dev)
-                kept = [t.clone() for t in (self.n_before, self.n_after, self.cell, self.tokens)]
-                side.wait_stream(torch.cuda.current_stream(self.dev))
-                with torch.cuda.stream(side):                              # once eagerly: libraries make their handles and workspaces
-                    self._step()
-                torch.cuda.current_stream(self.dev).wait_stream(side)
-                torch.cuda.synchronize(self.dev)
-                self.graph = torch.cuda.CUDAGraph()
-                with torch.cuda.graph(self.graph):
-                    self._step()
-                for t, was in zip((self.n_before, self.n_after, self.cell, self.tokens), kept):
-                    t.copy_(was)                                           # (the trial run moved them on; its rows are written again)
-            self.graph.replay()
-        self.ids_host[cell].copy_(self.tokens, non_blocking=True)
+        with torch.cuda.device(self.dev):
+            if not self.use_graphs:
+                self._step()
+            else:
+                if self.graph is None:
+                    side = torch.cuda.Stream(device=self.dev)
+                    kept = [t.clone() for t in (self.n_before, self.n_after, self.cell, self.tokens)]
+                    side.wait_stream(torch.cuda.current_stream(self.dev))
+                    with torch.cuda.stream(side):                              # once eagerly: libraries make their handles and workspaces
+                        self._step()
+                    torch.cuda.current_stream(self.dev).wait_stream(side)
+                    torch.cuda.synchronize(self.dev)
+                    self.graph = torch.cuda.CUDAGraph()
+                    with torch.cuda.graph(self.graph):
+                        self._step()
+                    for t, was in zip((self.n_before, self.n_after, self.cell, self.tokens), kept):
+                        t.copy_(was)                                           # (the trial run moved them on; its rows are written again)
+                self.graph.replay()
+            self.ids_host[cell].copy_(self.tokens, non_blocking=True)
         self.kernel_calls += 1 + 5 * self.cfg.n_layers + 1
         self.next_cell = cell + 1
         return self.tokens

@@ -26,27 +26,41 @@ def test_more_heads_than_a_grid_holds_are_refused(heads, halves):
                                       None, None) == B.EINVAL
 
 
-def _shell_without_a_gpu(grid):
-    """A SharedPromptShell whose step does nothing but count."""
+def _shell_without_a_gpu(grid, monkeypatch):
+    """A SharedPromptShell whose step does nothing but count, and note on which device it would run."""
+    import contextlib
+
     import torch
     from paper_2506_18226_b200.shell import SharedPromptShell, ShellConfig
+    current = ["cuda:0"]
+
+    @contextlib.contextmanager
+    def device(dev):
+        current.append(str(dev))
+        yield
+        current.pop()
+
+    monkeypatch.setattr(torch.cuda, "device", device)
 
     class Counting(SharedPromptShell):
         def __init__(self):
             self.cfg = ShellConfig(n_layers=1, dim=64, n_heads=1, ffn_hidden=64, vocab=8, n_text=1, grid_h=grid, grid_w=grid, n_images=2)
-            self.dev, self.use_graphs, self.graph, self.kernel_calls, self.steps = torch.device("cpu"), False, None, 0, 0
+            self.dev, self.use_graphs, self.graph, self.kernel_calls, self.steps = torch.device("cuda:1"), False, None, 0, []
             self.next_cell = None
             self.ids_host, self.tokens = torch.zeros(grid * grid, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
 
         def _step(self):
-            self.steps += 1
+            self.steps.append(current[-1])
+
+        def _prefill(self, text_emb):
+            self._step()
 
     return Counting()
 
 
-def test_the_shared_prompt_shell_stops_at_the_end_of_its_grid():
+def test_the_shared_prompt_shell_stops_at_the_end_of_its_grid(monkeypatch):
     """A step beyond it would look up a position and random numbers that the device does not have."""
-    sh = _shell_without_a_gpu(3)
+    sh = _shell_without_a_gpu(3, monkeypatch)
     for cell in (0, 1, 8):
         with pytest.raises(ValueError, match="prefill first"):
             sh.decode_step(cell)
@@ -60,7 +74,16 @@ def test_the_shared_prompt_shell_stops_at_the_end_of_its_grid():
     for cell in (8, 9, 10):
         with pytest.raises(ValueError):
             sh.decode_step(cell)
-    assert sh.steps == 8
+    assert len(sh.steps) == 8
+
+
+def test_the_shared_prompt_shell_runs_on_its_own_device(monkeypatch):
+    """Whatever device is the current one: a kernel launched there could not reach the shell's buffers."""
+    sh = _shell_without_a_gpu(2, monkeypatch)
+    sh.prefill(None)
+    sh.next_cell = 1
+    sh.decode_step(1)
+    assert sh.steps == ["cuda:1", "cuda:1"]
 
 
 def test_the_shared_prompt_shell_refuses_a_condition_of_no_rows():
