@@ -210,9 +210,6 @@ def _marshal():
         loader = importlib.machinery.ExtensionFileLoader("adsa_marshal", build_marshal())
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("adsa_marshal", loader))
         loader.exec_module(module)
-        if module.torch_version != torch.__version__.split("+")[0]:
-            raise ImportError(f"{loader.path} was built against torch {module.torch_version}, this is {torch.__version__}: build it again "
-                              "(build.build_marshal(force=True))")
         module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value for name in (
             "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn", "adsa_norm_residual")))
         _marshal_module = module

@@ -23,9 +23,25 @@ def _stale(target: str, deps: list) -> bool:
     return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
 
 
+def _built_against() -> bytes:
+    """What the running interpreter's module says of itself (in the file, so that it can be asked without loading it)."""
+    import re
+    import sys
+
+    import torch
+    release = re.match(r"\d+\.\d+\.\d+", torch.__version__).group()
+    return b"adsa_marshal built against torch %s, Python %d.%d;" % (release.encode(), *sys.version_info[:2])
+
+
+def _foreign(path: str) -> bool:
+    """Built against another torch or Python than the running one: it may not load, or read tensors wrongly."""
+    with open(path, "rb") as f:
+        return _built_against() not in f.read()
+
+
 def build_marshal(force: bool = False) -> str:
     """Compile the tensor-reading half of the binding against the running torch."""
-    if not force and not _stale(MARSHAL, [MARSHAL_SOURCE, HEADER]):
+    if not force and not _stale(MARSHAL, [MARSHAL_SOURCE, HEADER]) and not _foreign(MARSHAL):
         return MARSHAL
     import sysconfig
 
@@ -41,6 +57,8 @@ def build_marshal(force: bool = False) -> str:
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{i}" for i in include], MARSHAL_SOURCE,
                            "-o", tmp, f"-L{libs}", f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"])
     os.replace(tmp, MARSHAL)
+    if _foreign(MARSHAL):
+        raise ImportError(f"{MARSHAL}: the headers of this torch are another version's than {_built_against().decode()}")
     return MARSHAL
 
 

@@ -340,9 +340,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "adsa_marshal", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit_adsa_marshal()
-{
-    PyObject *m = PyModule_Create(&module);
-    if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);
-    return m;
-}
+// What this module was built against, for build.py to find in the file before anything of it is loaded
+#define ADSA_TEXT_(x) #x
+#define ADSA_TEXT(x) ADSA_TEXT_(x)
+__attribute__((used)) const char built_against[] =
+    "adsa_marshal built against torch " TORCH_VERSION ", Python " ADSA_TEXT(PY_MAJOR_VERSION) "." ADSA_TEXT(PY_MINOR_VERSION) ";";
+
+PyMODINIT_FUNC PyInit_adsa_marshal() { return PyModule_Create(&module); }

@@ -90,3 +90,34 @@ def test_the_shared_prompt_shell_refuses_a_condition_of_no_rows():
     from paper_2506_18226_b200.shell import SharedPromptShell, ShellConfig
     with pytest.raises(ValueError, match="condition"):
         SharedPromptShell(ShellConfig(n_layers=1, dim=64, n_heads=1, ffn_hidden=64, vocab=8, n_text=0, grid_h=2, grid_w=2, n_images=1))
+
+
+@pytest.mark.parametrize("wrong", [b"torch 1.", b"Python 2."])
+def test_a_binding_built_against_another_torch_or_python_is_built_again(wrong, tmp_path, monkeypatch):
+    """Its file is as new as its sources all the same."""
+    import os
+    import shutil
+
+    from paper_2506_18226_b200 import build
+    good = build.build_marshal()
+    mine = str(tmp_path / "adsa_marshal.so")
+    monkeypatch.setattr(build, "MARSHAL", mine)
+    built = []
+
+    def compiler(command):
+        built.append(command)
+        shutil.copyfile(good, command[command.index("-o") + 1])
+
+    monkeypatch.setattr(build.subprocess, "check_call", compiler)
+    shutil.copyfile(good, mine)
+    assert build.build_marshal() == mine and not built
+    with open(good, "rb") as f:
+        whole = f.read()
+    word = wrong.split()[0] + b" "
+    at = whole.index(word, whole.index(b"adsa_marshal built against "))
+    with open(mine, "wb") as f:
+        f.write(whole[:at] + wrong + whole[at + len(wrong):])
+    assert os.path.getmtime(mine) >= os.path.getmtime(build.MARSHAL_SOURCE)
+    assert build.build_marshal() == mine and len(built) == 1
+    with open(mine, "rb") as f:
+        assert f.read() == whole
