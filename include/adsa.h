@@ -460,9 +460,10 @@ typedef struct {
 ADSA_API int adsa_rotary_init(adsa_rotary *rot, int head_dim, int n_axes, const int32_t *pairs, int halves, int restart, double base);
 
 /* out = x turned.  x, out: 16-bit [n_tokens][n_heads][head_dim] with the given token and head strides; out may be x
- * (same strides), and must not overlap it otherwise.  pos: int32 [n_tokens][n_axes], any value.  Angles are reduced
- * in 64 bits, so far positions keep their fraction of a turn.  A token may have 65535 heads (q, k and v of an append
- * together), more of them if a head is short; what a grid cannot hold is ADSA_EINVAL. */
+ * (same strides), and must not overlap it otherwise, nor itself (strides of out below head_dim are ADSA_EINVAL).  pos:
+ * int32 [n_tokens][n_axes], any value.  Angles are reduced in 64 bits, so far positions keep their fraction of a turn.  A
+ * token may have 65535 heads (q, k and v of an append together), more of them if a head is short; what a grid cannot hold is
+ * ADSA_EINVAL. */
 ADSA_API int adsa_rope_axes(const adsa_rotary *rot, int dtype, const void *x, long long x_token, long long x_head, const int32_t *pos,
                             long long n_tokens, int n_heads, void *out, long long out_token, long long out_head, adsa_stream_t stream);
 
@@ -472,7 +473,8 @@ ADSA_API int adsa_rope_axes(const adsa_rotary *rot, int dtype, const void *x, lo
  *               from cu[batch] on are padding (nothing is written for them).  NULL: n_tokens / batch tokens each
  *   k, v        [n_tokens][n_kv_heads][head_dim];  token j of batch row b becomes logical row n_rows[b] + j
  *   rot, pos    as adsa_rope_axes, rot->head_dim == kv->head_dim; rot NULL: nothing turns and pos is not read
- *   q, q_out    [n_tokens][n_heads][head_dim], turned like k; n_heads 0: none; q_out may be q (same strides)
+ *   q, q_out    [n_tokens][n_heads][head_dim], turned like k; n_heads 0: none; q_out may be q (same strides), and overlaps
+ *               neither itself nor k, v or the pools
  * Rows past the page table set ADSA_DEV_ROW_OVERFLOW, pages outside the pool ADSA_DEV_BAD_PAGE; such a token's k and v
  * are not written.  n_rows is not changed.  No two tokens of a call may fall on the same row of the same page. */
 ADSA_API int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_table, int batch, int max_pages, const int32_t *n_rows,

@@ -335,6 +335,12 @@ bool rotary_ok(const adsa_rotary *r)
 
 bool rows_ok(const TurnRows &r) { return r.src && r.dst && !(((uintptr_t)r.src | (uintptr_t)r.dst) & 1); }
 
+// rows of d elements that a stride puts on top of each other (a tensor expanded along tokens or heads), to be written by several threads
+bool rows_overlap(const TurnRows &r, long long tokens, int d)
+{
+    return (tokens > 1 && r.dst_token > -d && r.dst_token < d) || (r.heads > 1 && r.dst_head > -d && r.dst_head < d);
+}
+
 }  // namespace
 }  // namespace adsa
 
@@ -376,7 +382,7 @@ int adsa_rope_axes(const adsa_rotary *rot, int dtype, const void *x, long long x
     if (n_tokens == 0 || n_heads == 0) return ADSA_OK;
     TurnArgs a = {};
     a.q = {x, out, x_token, x_head, out_token, out_head, n_heads};
-    if (!rows_ok(a.q) || !pos || ((uintptr_t)pos & 3)) return ADSA_EINVAL;
+    if (!rows_ok(a.q) || rows_overlap(a.q, n_tokens, rot->head_dim) || !pos || ((uintptr_t)pos & 3)) return ADSA_EINVAL;
     if (x == out && (x_token != out_token || x_head != out_head)) return ADSA_EINVAL;
     a.pos = pos;
     a.tokens = n_tokens;
@@ -404,7 +410,7 @@ int adsa_paged_append(const adsa_paged_kv *kv, const int32_t *page_table, int ba
     a.q = {q, q_out, q_token, q_head, q_out_token, q_out_head, n_heads};
     a.k = {k, kv->k_pool, k_token, k_head, 0, 0, kv->n_kv_heads};
     a.v = {v, kv->v_pool, v_token, v_head, 0, 0, kv->n_kv_heads};
-    if ((n_heads && !rows_ok(a.q)) || !rows_ok(a.k) || !rows_ok(a.v)) return ADSA_EINVAL;
+    if ((n_heads && (!rows_ok(a.q) || rows_overlap(a.q, n_tokens, kv->head_dim))) || !rows_ok(a.k) || !rows_ok(a.v)) return ADSA_EINVAL;
     a.pos = pos;
     a.page_table = page_table; a.n_rows = n_rows; a.cu_tokens = cu_tokens; a.status = status;
     a.tokens = n_tokens; a.per_row = (int)(n_tokens / batch);

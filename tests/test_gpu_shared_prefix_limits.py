@@ -48,3 +48,20 @@ def test_the_shared_prompt_shell_takes_long_conditions():
         a.decode_step(cell)
         b.decode_step(cell)
     assert int(b.status) == 0
+
+
+def test_expanded_tensors_are_read_and_not_written():
+    import paper_2506_18226_b200 as A
+    rot = A.Rotary(64, (32,))
+    x, pos = torch.randn(1, 2, 64, device=DEV).to(torch.bfloat16), torch.arange(5, dtype=torch.int32, device=DEV)[:, None]
+    wide = x.expand(5, 2, 64)
+    assert torch.equal(A.rope_axes(rot, wide, pos), A.rope_axes(rot, wide.contiguous(), pos))
+    for bad in (wide, x[:, :1].expand(1, 2, 64).expand(5, 2, 64)):
+        with pytest.raises(A.AdsaError):
+            A.rope_axes(rot, wide, pos, out=bad)
+    one = x[:1].as_strided((1, 2, 64), (0, 64, 1))                                # a stride that nothing takes
+    want = A.rope_axes(rot, x, pos[3:4])
+    assert torch.equal(A.rope_axes(rot, one, pos[3:4], out=one), want) and torch.equal(x, want)
+    pool, table = torch.zeros(5, 2, 16, 64, dtype=torch.bfloat16, device=DEV), torch.arange(5, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    with pytest.raises(A.AdsaError):
+        A.paged_append(wide, wide, pool, pool.clone(), table, torch.zeros(5, dtype=torch.int32, device=DEV), rotary=rot, pos=pos, q=wide, q_out=wide)

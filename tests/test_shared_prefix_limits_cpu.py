@@ -121,3 +121,13 @@ def test_a_binding_built_against_another_torch_or_python_is_built_again(wrong, t
     assert build.build_marshal() == mine and len(built) == 1
     with open(mine, "rb") as f:
         assert f.read() == whole
+
+
+@pytest.mark.parametrize("token,head", [(0, 64), (128, 0), (63, 256), (-60, 256), (256, 32), (256, -62)])
+def test_outputs_whose_rows_overlap_are_refused(token, head):
+    """An expanded tensor turned in place would be turned several times, by threads that race."""
+    r = _rotary(64, 32, 0)
+    assert A.load().adsa_rope_axes(C.byref(r), 0, P, token, head, P, 3, 2, P, token, head, None) == B.EINVAL
+    kv = B.AdsaPagedKv(P, P, 0, 10, 2, 16, 64, 64)
+    assert A.load().adsa_paged_append(C.byref(kv), P, 1, 3, P, None, 3, P, 128, 64, P, 128, 64, C.byref(r), P, P, 2, token, head, P, token, head,
+                                      None, None) == B.EINVAL
