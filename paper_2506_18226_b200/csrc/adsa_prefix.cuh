@@ -90,11 +90,10 @@ template <typename T>
 __device__ __forceinline__ void split_weights(float2 p, uint32_t &hi, uint32_t &lo)
 {
     typedef WeightSplit<T> S;
-    const float2 minus = make_float2(weight_bits(p.x, S::kept, 0x80000000u), weight_bits(p.y, S::kept, 0x80000000u));
-    const float2 left = fma2(p, make_float2(S::one, S::one), minus);
-    lo = pack2<T>(left.x, left.y);
+    const float hx = weight_bits(p.x, S::kept, 0u), hy = weight_bits(p.y, S::kept, 0u);
+    lo = pack2<T>(fmaf(p.x, S::one, -hx), fmaf(p.y, S::one, -hy));
     if constexpr (std::is_same<T, __half>::value) {
-        hi = pack2<T>(-minus.x, -minus.y);
+        hi = pack2<T>(hx, hy);
         lo = above_zero(lo, hi);
     } else {
         hi = __byte_perm(__float_as_uint(p.x), __float_as_uint(p.y), 0x7632);
