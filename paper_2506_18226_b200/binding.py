@@ -282,7 +282,8 @@ def shared_prefix_attn(q, k_pool, v_pool, page_table, n_rows, prefix_table=None,
     page_table int32 [batch, max_pages], n_rows int32 [batch]; prefix_table int32 [n_groups, max_prefix_pages],
     prefix_rows int32 [n_groups], group_start int32 [n_groups + 1] (all three None: no prefix).  out 16-bit or out_f32
     float [batch, n_heads, head_dim] (default: a new tensor like q), lse float [batch, n_heads].  workspace: from
-    shared_prefix_workspace; None takes one from torch's allocator for this call.  Returns out, or out_f32 without one."""
+    shared_prefix_workspace; None takes one from torch's allocator for this call.  What the tables have room for chooses the
+    kernel: narrow tables are quickest for small calls.  Returns out, or out_f32 without one."""
     r = (_marshal_module or _marshal()).shared_prefix_attn(q, k_pool, v_pool, page_table, n_rows, prefix_table, prefix_rows, group_start, scale,
                                                            out, out_f32, lse, workspace, status)
     if r.__class__ is int:

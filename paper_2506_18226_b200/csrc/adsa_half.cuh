@@ -67,7 +67,8 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack {
 };
 
 // Kernels launched through here call pdl_wait() before they touch global memory: the kernel ahead has then completed
-// and its writes are visible.  pdl_launch() after it lets the next such kernel begin its own set-up.
+// and its writes are visible.  pdl_launch() after it lets the next such kernel begin its own set-up.  (One exception: the sweep of a
+// shared-prefix call behind that call's wide kernel, which has waited for both, in that order; the sweep waits before it ends.)
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -35,7 +35,9 @@ struct PrefixArgs {
     int wide_above;
     float *w_state, *w_ml;                  // slots of kWideQueries rows
     int n_w_slots, w_resident;              // w_resident: blocks of the wide kernel that fit the GPU at a time; 0: it does not run
-    int resident;                           // blocks of the sweep kernel that fit the GPU at a time
+    int resident;                           // blocks of the sweep kernel that the cut counts on at a time: two per SM, one for rows of
+                                            // more than 128 elements (with over some 2000 batch rows + twice the groups the plan
+                                            // leaves room for one: runs then start later, with the same results)
     int split;                              // blocks of a cluster, which share an item's cached rows (1: no cluster)
 };
 
@@ -159,8 +161,7 @@ struct WideItems {
     }
 };
 // Even runs of the wide kernel's list: one per block, two units or more (so the first unit of a tile).  (Leaving out blocks so
-// that no run goes over the end of an item changed nothing: 85.0 us against 85.2 for the long-context call; the sweep of
-// the own rows begins where the other blocks have ended.)
+// that no run goes over the end of an item changed nothing: the sweep of the own rows begins where the other blocks have ended.)
 struct WideCut {
     uint32_t total, runs;
     __device__ __forceinline__ WideCut(uint32_t total_, uint32_t resident) : total(total_), runs(min(resident, total_ / 2u))

@@ -26,10 +26,10 @@
 // takes the fewest instructions per byte.
 //
 // Measured in a captured graph: 64 rows x 32 heads of 100 elements over 2424 shared (four groups) and up to 2304 own rows,
-// 1.19 GB: 197 us, 6.0 TB/s; 2 us of it go by until the lengths are read and cut, 1.5 until the first tile, 4 in the merge.
-// 32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39 us, of which 27 stream.  DIRECT: two rows x 12 heads over
-// 120 shared and 100 own rows: 5.0 us, a chain of three dependent reads; two rows x 8 heads of 128 over 128 shared and 4096 own
-// rows, 35 MB, clusters of 8: 11.5 us (list: 20.4).
+// 1.19 GB: 203 us, 5.8 TB/s; 2 us of it go by until the lengths are read and cut, 1.5 until the first tile, 4 in the merge.
+// 32 rows x 20 heads of 64 over 120 shared and 1024 own rows, 169 MB: 39.7 us, of which 27 stream.  DIRECT: two rows x 12 heads over
+// 120 shared and 100 own rows: 5.2 us, a chain of three dependent reads; two rows x 8 heads of 128 over 128 shared and 4096 own
+// rows, 35 MB, clusters of 8: 11.9 us (list: 23.5).
 #include <math.h>
 #include <type_traits>
 
@@ -50,16 +50,16 @@ enum { kModeList, kModeBlocks, kModeClusters };
 constexpr long long kPaMaxRows = 0x7fffff00LL;   // a sequence: row numbers stay in 32 bits past the last tile
 // A group's prefix goes to the wide kernel if the group has more query rows of a key head than fit one item here, where the
 // mean group has and the prefix tables hold at least 8192 rows of up to 64 elements (4096 of up to 128).  Two groups of 33
-// rows, 8 key heads of 128 (us, here / wide): 512 rows 19 / 20, 4096 36 / 29, 32768 129 / 66; of 128 rows: 34 / 40,
-// 62 / 55, 228 / 90; heads of 64, 33 rows: 17 / 19, 24 / 26, 76 / 57.  20 rows: 16 / 19, 25 / 27, 79 / 64.
+// rows, 8 key heads of 128 (us, here / wide): 512 rows 20 / 21, 4096 40 / 31, 32768 144 / 71; of 128 rows: 36 / 42,
+// 68 / 59, 267 / 98; heads of 64, 33 rows: 18 / 20, 26 / 28, 82 / 62.  20 rows: 17 / 20, 26 / 30, 89 / 70.
 constexpr int kWideAbove = 32;
 constexpr long long kWideRows = 8192;
 
 // Blocks of a cluster that share the cached rows of one item: as many as the GPU holds at once (the eighth is what clusters of 8
-// leave of a group of SMs; in two turns they are slow: 14 rows x 20 heads of 64, 32 KB, 1 / 2 / 4 blocks 5.8 / 11.5 / 23.0 us),
+// leave of a group of SMs; in two turns they are slow: 14 rows x 20 heads of 64, 32 KB, 1 / 2 / 4 blocks 6.1 / 12.6 / 23.9 us),
 // while there are tiles for them.  2 rows x 8 heads
-// of 64, 1 / 2 / 4 / 8 blocks in us: 64 KB 5.4 / 5.8 / 6.2 / 6.2, 128 KB 7.0 / 6.6 / 6.2 / 6.5, 288 KB 10.1 / 8.2 / 7.4 / 7.0,
-// 1 MB 25.8 / 16.0 / 11.1 / 8.8.
+// of 64, 1 / 2 / 4 / 8 blocks in us: 64 KB 5.7 / 6.5 / 6.4 / 6.6, 128 KB 7.0 / 7.1 / 6.5 / 6.7, 288 KB 10.2 / 8.9 / 7.7 / 7.4,
+// 1 MB 25.5 / 16.1 / 11.5 / 9.4.
 inline int direct_split(long long items, long long blocks, double most)
 {
     int n = 1;
@@ -70,11 +70,12 @@ inline int direct_split(long long items, long long blocks, double most)
 // A block (or cluster) per batch row and key head, by the bytes of K and V that the tables hold for one of them (most) and how many
 // of these the list would not read, as the other rows of a group have (again).  It does not balance, and saves the list, the second
 // kernel and the states, of which every query head has its own.  Measured, list / direct in us.  While all are resident at once: 2
-// rows x 12 heads of 64, 32 KB 7.8 / 4.9, 1 MB (8 blocks) 18.7 / 9.2; 8 x 20 of 128, 576 KB 23.4 / 17.6, 1 MB 27.4 / 28.3; longer
-// rows beside short ones leave too much to one block.  In two turns: 20 rows x 20 heads of 64, 32 KB 13.8 / 9.1, 192 KB 23.2 /
-// 15.6, 256 KB of which half prefix 19.3 / 18.1, 528 KB of which 512 prefix 17.7 / 30.0.  In more, heads of 64: 256 rows x 32 heads
-// on 8, 48 KB of which a third prefix 44.8 / 33.1, 192 KB of which a third 77.9 / 67.3, 288 KB of which 32 prefix 135.7 / 96.0; 128
-// x 32 on 32, 96 KB of which a third 74.7 / 84.8, 288 KB of which 32 205 / 168; 32 x 20 of 128, 2.2 turns, 576 KB 62.6 / 67.1.
+// rows x 12 heads of 64, 32 KB 8.4 / 5.6, 1 MB (8 blocks) 19.5 / 9.9; 8 x 20 of 128, 576 KB 24.1 / 18.0, 1 MB 29.5 / 28.7; longer
+// rows beside short ones leave too much to one block.  In two turns: 20 rows x 20 heads of 64, 32 KB 14.6 / 10.4, 192 KB 24.5 /
+// 16.6, 256 KB of which half prefix 20.4 / 19.0, 528 KB of which 512 prefix 18.6 / 30.6.  In more, heads of 64: 256 rows x 32 heads
+// on 8, 48 KB of which a third prefix 46.0 / 35.8, 192 KB of which a third 81.1 / 70.2, 288 KB of which 32 prefix 141 / 99.9; 128
+// x 32 on 32, 96 KB of which a third 77.4 / 90.5, 288 KB of which 32 213 / 173; 32 x 20 of 128, 2.2 turns, 576 KB 63.3 / 67.9.
+// (Lengths are on the device, so what the tables could hold decides; the header tells the caller.)
 inline bool direct_pays(long long items, long long blocks, int per_kv, double most, double again)
 {
     if (items <= blocks) return most <= direct_split(items, blocks, most) * 640.0 * 1024;

@@ -10,11 +10,12 @@
 // groups take every tile of K and V, each with its own 128 rows, so a tile is fetched once for 256 rows; the last 128 or fewer
 // rows of a group are an item whose tiles the two groups take in turns.
 //
-// 256 rows x 8 key heads of 128 over 32768 cached rows (34 GFLOP) stream in 24 us once every SM has its first tile,
-// 1.4 PFLOP/s; first tiles and the states at the end cost as much again as a third of that.  What bounds an iteration (128 cached
-// rows, both groups: 3580 cycles) is a group's own chain: 2200 cycles of softmax, of which 1024 are exponentials, then its
-// products, 1300 with what wakes them.  Descriptors have to stay in uniform registers: built by `lane == 0` in ordinary
-// ones, the same iteration took 4840 cycles, all of them the issuing thread's.
+// 256 rows x 8 key heads of 128: every further 32768 cached rows (34 GFLOP, 52 with the lo parts' products) take 38 us, 1.4
+// PFLOP/s of products done; the launch for 32768 rows takes 52 us by itself, first tiles and the states at the end included.  What
+// bounds an iteration (128 cached rows, both groups: 2.7 us, of which the products keep the tensor cores busy for 1.7) is a
+// group's own chain: its softmax, of which 0.5 us are exponentials, then its products and what wakes them.  (Weights of one
+// 16-bit value: 27 us, 46 for the launch; of the difference the lo parts' products are half, making and storing them the rest.)
+// Descriptors have to stay in uniform registers: built by `lane == 0` in ordinary ones, an iteration took a third longer.
 //
 // The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units); until then weights up to
 // 2^8 are allowed, sums and products stay exact multiples, and O in tensor memory is rarely rescaled.
@@ -189,6 +190,8 @@ prefix_wide_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
     }
+    // The order of these two carries the sweep behind this kernel: it begins as soon as every block here has passed them, and reads
+    // tables, queries and rows and writes its states without a wait of its own, on the strength of this one.
     pdl_wait();
     pdl_launch();
     if (warp == 9) tc_alloc(smem_u32(&s_tmem), kWideColumns);

@@ -9,7 +9,7 @@
 namespace adsa {
 
 constexpr int kResMaxThreads = 1024;
-constexpr int kResDeepRows = 148 * 16;        // rows from which threads hold two pieces
+constexpr int kResDeepRows = 148 * 16;        // rows from which threads hold two pieces: 16 blocks an SM of a B200
 
 // Sum over the `warps` warps of a row (warps 0 .. warps-1 of its part of the block); every thread of the block calls it.
 __device__ __forceinline__ float row_sum(float x, float *slots, int warps, int warp, int lane)

@@ -139,7 +139,8 @@ struct Piece {
 };
 
 // blockIdx.x: tokens; blockIdx.y: a chunk of the q, k and v heads taken as one list.  Accesses of fewer than 16 bytes need
-// all the warps an SM has to keep memory busy: 32 registers (2424 tokens x 32 heads of 100 elements: 13.0 -> 11.1 us).
+// all the warps an SM has to keep memory busy: 32 registers (2424 tokens x 32 heads of 100 elements: 13.0 -> 11.1 us, 60 to 120
+// bytes a thread of spills included).
 template <typename T, int ACC, bool HALVES>
 __global__ void __launch_bounds__(kTurnMaxThreads, ACC < 8 ? 4 : 0)
 turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ adsa_rotary rot)
@@ -259,7 +260,8 @@ turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ adsa_rot
 
 namespace {
 
-// the widest access every row of `r` allows, at most `acc` elements
+// the widest access every row of `r` allows, at most `acc` elements (q, k and v of a call share one: a tensor that is not aligned
+// to 16 bytes, or whose strides are not, slows the others too)
 int fit(int acc, const TurnRows &r)
 {
     if (r.heads == 0) return acc;
@@ -301,7 +303,9 @@ int run_turn(TurnArgs &a, const adsa_rotary &rot, int dtype, cudaStream_t st)
     if (all_heads * a.units > 65535LL * kTurnMaxThreads) return ADSA_EINVAL;      // (a chunk of heads takes up to that many units)
     const int heads = (int)all_heads;
     // Heads a block: all of them if they make up to 512 units, fewer until every SM has a block.  Tokens a block: as many as
-    // let all blocks run at once (2048 threads an SM), at most 16: a second, thinner wave costs as much as a full one.
+    // would let all blocks run at once at 2048 threads on each of 148 SMs, at most 16: a second, thinner wave costs as much as
+    // a full one.  (The forms of under 16 bytes hold that many; the 16-byte forms, with 54 and 64 registers, hold half, and
+    // take a second wave where 16 tokens a block are not enough: a long prompt's 1152 blocks of 256 threads run as nearly two.)
     int chunks = (heads * a.units + kTurnMaxThreads - 1) / kTurnMaxThreads;
     while (chunks < heads && (heads + chunks - 1) / chunks * a.units > kTurnMaxThreads) ++chunks;
     while (chunks < heads && a.tokens * chunks < 148 && (heads + chunks - 1) / chunks * a.units > 128) ++chunks;
