@@ -65,3 +65,47 @@ def test_expanded_tensors_are_read_and_not_written():
     pool, table = torch.zeros(5, 2, 16, 64, dtype=torch.bfloat16, device=DEV), torch.arange(5, dtype=torch.int32, device=DEV)[:, None].contiguous()
     with pytest.raises(A.AdsaError):
         A.paged_append(wide, wide, pool, pool.clone(), table, torch.zeros(5, dtype=torch.int32, device=DEV), rotary=rot, pos=pos, q=wide, q_out=wide)
+
+
+@pytest.mark.parametrize("rows,room", [(6, 0), (6, 2000), (80, 30000)])
+def test_a_step_captured_over_two_streams(rows, room):
+    """q is turned on one stream while k and v enter the cache on another; the attention waits for both, the norm for it."""
+    import paper_2506_18226_b200 as A
+    from test_gpu_shared_prefix import _gen, _randn, attn_case
+    g = _gen(rows + room)
+    c = attn_case(g, [30] * rows, [200], [0, rows], 2, 2, 64, 16, torch.bfloat16, room=room)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    rot, pos = A.Rotary(64, (16, 16)), torch.full((rows, 2), 7, **i32)
+    q, k, v = _randn(g, rows, 4, 64), _randn(g, rows, 2, 64), _randn(g, rows, 2, 64)
+    x, w = _randn(g, rows, 256), _randn(g, 256)
+    before = torch.full((rows,), 29, **i32)
+    turned, out, x_out, h = torch.empty_like(q), torch.empty_like(q), torch.empty_like(x), torch.empty_like(x)
+    ws = A.shared_prefix_workspace(q, c["k_pool"], c["page_table"], c["prefix_table"])
+    side = torch.cuda.Stream()
+
+    def step():
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        A.paged_append(k, v, c["k_pool"], c["v_pool"], c["page_table"], before, rotary=rot, pos=pos)
+        with torch.cuda.stream(side):
+            A.rope_axes(rot, q, pos, out=turned)
+        main.wait_stream(side)
+        A.shared_prefix_attn(**dict(c, q=turned), out=out, workspace=ws)
+        A.norm_residual(out.view(rows, 256), x, w, x_out=x_out, h=h)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(6):
+        for t in (q, k, v, x):
+            t.copy_(_randn(g, *t.shape))
+        step()
+        want = [t.clone() for t in (turned, out, x_out, h)]
+        for t in (turned, out, x_out, h):
+            t.fill_(3.0)
+        for n in range(i + 1):                                                    # several replays one behind the other
+            graph.replay()
+        for t, u in zip((turned, out, x_out, h), want):
+            assert torch.equal(t, u)
