@@ -519,6 +519,44 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
                                 long long n_gates, const void *w_pre, void *x_out, void *h, long long rows, int dim, float scale, float eps,
                                 adsa_stream_t stream);
 
+/* ---- prompts and chunks: many query rows per sequence ------------------------------------------------------------
+ * Rules as for the calls on a paged cache above, but that the softmax weights meet V rounded once to the 16-bit type (each off by
+ * 2^-8 of itself at most for bfloat16, 2^-11 or 2^-31 of the largest for half; their sum is taken before).  An output row
+ * that this arithmetic leaves infinite or NaN is made again in 32 bits throughout, from the rows it attends alone: what lies in
+ * rows that a query does not attend has no effect, infinities and NaN included.
+ *
+ * batch <= 4096 sequences; cu_q, cu_k, cu_tokens: int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 are sequence b (of no
+ * tokens, maybe); tokens before cu[0] and from cu[batch] on are padding, whose output rows are left as they were; boundaries are
+ * clamped to the tokens there are.  NULL: all sequences are equally long.  n_heads = g * n_kv_heads with g <= 64: query head h reads
+ * key head h / g.  head_dim even, 2 .. 256.  q, k, v 4-byte aligned, even strides (quickest: 16 bytes, multiples of 8).
+ *   out, out_f32  16-bit / float [tokens][n_heads][head_dim], 4- / 8-byte aligned; either may be NULL, not both
+ *   lse           float [tokens][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
+ * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).  workspace: [device] 256-byte
+ * aligned, adsa_prompt_workspace_bytes of them, nothing kept in it from call to call: calls that may overlap on the GPU need one
+ * each, and a captured call's must outlive its graph. */
+ADSA_API int adsa_prompt_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes);
+
+/* Attention over whole prompts laid end to end.  q [n_q][n_heads][head_dim], k, v [n_k][n_kv_heads][head_dim] with the given
+ * token and head strides; cu_q, cu_k: their sequences.  Causal: token i of a sequence with m tokens of q and n of k attends
+ * rows 0 .. n - m + i (the last token of q sees every row, and with n = m each sees itself and what is before it; i < m - n:
+ * nothing); else all n rows. */
+ADSA_API int adsa_packed_attn(int dtype, const void *q, long long q_token, long long q_head, const void *k, long long k_token,
+                              long long k_head, const void *v, long long v_token, long long v_head, const int32_t *cu_q,
+                              const int32_t *cu_k, int batch, long long n_q, long long n_k, int n_heads, int n_kv_heads, int head_dim,
+                              int causal, float softmax_scale, void *out, float *out_f32, float *lse, void *workspace,
+                              size_t workspace_bytes, adsa_stream_t stream);
+
+/* Attention of a chunk of new tokens per sequence over a paged cache that holds them already (adsa_paged_append first): with m
+ * tokens (cu_tokens) and n = n_rows[b] rows, clamped to what the table holds, token i attends the prefix_rows[g] rows of its
+ * group's prefix and rows 0 .. n - m + i of page_table[b] (i < m - n: the prefix alone).  page tables, prefixes and groups as
+ * adsa_shared_prefix_attn has them; m = 1 is its step for one token, without the sweep of a long prefix for all rows of a group at once.
+ * A page outside the pool sets ADSA_DEV_BAD_PAGE and is not read. */
+ADSA_API int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, long long q_head, const int32_t *cu_tokens,
+                             int batch, long long n_tokens, int n_heads, const int32_t *page_table, int max_pages, const int32_t *n_rows,
+                             const int32_t *prefix_table, int max_prefix_pages, const int32_t *prefix_rows, const int32_t *group_start,
+                             int n_groups, float softmax_scale, void *out, float *out_f32, float *lse, void *workspace,
+                             size_t workspace_bytes, uint32_t *status, adsa_stream_t stream);
+
 ADSA_API const char *adsa_strerror(int status);
 
 #ifdef __cplusplus

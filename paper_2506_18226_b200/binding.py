@@ -29,6 +29,7 @@ EXPORTS = [
     "adsa_rmsnorm", "adsa_swiglu", "adsa_cfg_sample",
     "adsa_rotary_init", "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn",
     "adsa_norm_residual",
+    "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn",
 ]
 
 
@@ -110,6 +111,9 @@ def load(rebuild: bool = False) -> C.CDLL:
             "adsa_shared_prefix_workspace_bytes": [i32, i32, i32, i32, i32, C.POINTER(sz)],
             "adsa_shared_prefix_attn": [vp, vp, ll, ll, i32, i32, vp, i32, vp, vp, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, sz, vp, vp],
             "adsa_norm_residual": [i32, i32, vp, vp, vp, vp, ll, vp, vp, vp, ll, i32, C.c_float, C.c_float, vp],
+            "adsa_prompt_workspace_bytes": [i32, i32, i32, i32, C.POINTER(sz)],
+            "adsa_packed_attn": [i32, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, i32, ll, ll, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp, sz, vp],
+            "adsa_chunk_attn": [vp, vp, ll, ll, vp, i32, ll, i32, vp, i32, vp, vp, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, sz, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
@@ -211,7 +215,8 @@ def _marshal():
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("adsa_marshal", loader))
         loader.exec_module(module)
         module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value for name in (
-            "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn", "adsa_norm_residual")))
+            "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn", "adsa_norm_residual",
+            "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn")))
         _marshal_module = module
     return _marshal_module
 
@@ -300,6 +305,49 @@ def norm_residual(y, x, w_pre=None, *, w_post=None, gate=None, scale=1.0, eps=1e
     r = (_marshal_module or _marshal()).norm_residual(y, x, w_pre, w_post, gate, scale, eps, x_out, h)
     if r.__class__ is int:
         raise AdsaError(r, "adsa_norm_residual")
+    return r
+
+
+# ---- prompts and chunks: many query rows per sequence ----
+
+def prompt_workspace(q, n_kv_heads, batch):
+    """The workspace packed_attn and chunk_attn need for q [n_tokens, n_heads, head_dim] of `batch` sequences (one for every call
+    that may be in flight at a time; a captured call's must outlive its graph)."""
+    out = C.c_size_t(0)
+    with torch.cuda.device(q.device):
+        rc = load().adsa_prompt_workspace_bytes(batch, q.shape[1], n_kv_heads, q.shape[2], C.byref(out))
+    if rc:
+        raise AdsaError(rc, "adsa_prompt_workspace_bytes")
+    return torch.empty(out.value, dtype=torch.uint8, device=q.device)
+
+
+def packed_attn(q, k, v, cu_q=None, cu_k=None, *, causal=True, scale=0.0, out=None, out_f32=None, lse=None, workspace=None):
+    """adsa_packed_attn: attention over whole prompts laid end to end; q [n_q, n_heads, head_dim], k and v
+    [n_k, n_kv_heads, head_dim] (any token and head stride), query head h on key head h / (n_heads / n_kv_heads).
+
+    cu_q, cu_k: int32 [batch + 1], where the sequences of q and of k begin and end (cu_k None: as cu_q; both None: one
+    sequence).  causal: the last token of a sequence's q sees all its rows, each token before it one row less.  out 16-bit or
+    out_f32 float [n_q, n_heads, head_dim] (default: a new tensor; its rows of no sequence are left as they are), lse float
+    [n_q, n_heads].  workspace: from prompt_workspace; None takes one from torch's allocator for this call.  Returns out, or out_f32
+    without one."""
+    r = (_marshal_module or _marshal()).packed_attn(q, k, v, cu_q, cu_k, causal, scale, out, out_f32, lse, workspace)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_packed_attn")
+    return r
+
+
+def chunk_attn(q, k_pool, v_pool, page_table, n_rows, cu_tokens=None, prefix_table=None, prefix_rows=None, group_start=None, *,
+               scale=0.0, out=None, out_f32=None, lse=None, workspace=None, status=None):
+    """adsa_chunk_attn: new tokens q [n_tokens, n_heads, head_dim] over a paged cache that holds their rows already: with m
+    tokens and n_rows rows, token i of a sequence attends its group's prefix and rows 0 .. n_rows - m + i of its own.
+
+    page_table int32 [batch, max_pages], n_rows int32 [batch]; cu_tokens int32 [batch + 1] or None (the same number of tokens for
+    every sequence); prefix_table, prefix_rows, group_start as in shared_prefix_attn (all three None: no prefix); the rest
+    as in packed_attn.  status: int32 [1] that device-side errors are ORed into."""
+    r = (_marshal_module or _marshal()).chunk_attn(q, k_pool, v_pool, page_table, n_rows, cu_tokens, prefix_table, prefix_rows, group_start,
+                                                   scale, out, out_f32, lse, workspace, status)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_chunk_attn")
     return r
 
 

@@ -24,6 +24,9 @@ decltype(&adsa_paged_append) c_paged_append;
 decltype(&adsa_shared_prefix_workspace_bytes) c_workspace_bytes;
 decltype(&adsa_shared_prefix_attn) c_shared_prefix_attn;
 decltype(&adsa_norm_residual) c_norm_residual;
+decltype(&adsa_prompt_workspace_bytes) c_prompt_workspace_bytes;
+decltype(&adsa_packed_attn) c_packed_attn;
+decltype(&adsa_chunk_attn) c_chunk_attn;
 
 struct Raised {};                            // a Python exception is set
 
@@ -298,12 +301,118 @@ PyObject *norm_residual(PyObject *const *a, Py_ssize_t n)
     return answer(rc, both);
 }
 
+// outputs and workspace of the two calls with many query rows per sequence
+struct RowsOut {
+    at::Tensor out, ws;
+    const at::Tensor &out_f32, &lse;
+    int rc = ADSA_OK;
+    // o: out, out_f32, lse, workspace
+    RowsOut(const Check &c, const at::Tensor &q, PyObject *const *o, int64_t batch, int64_t kv_heads)
+        : out(tensor(o[0], c.call, "out")), ws(tensor(o[3], c.call, "workspace")), out_f32(tensor(o[1], c.call, "out_f32")), lse(tensor(o[2], c.call, "lse"))
+    {
+        const int64_t tokens = q.size(0), heads = q.size(1), d = q.size(2);
+        if (out.defined()) c.wants(out, "out", q.scalar_type(), {tokens, heads, d}, true);
+        if (out_f32.defined()) c.wants(out_f32, "out_f32", at::kFloat, {tokens, heads, d}, true);
+        if (lse.defined()) c.wants(lse, "lse", at::kFloat, {tokens, heads}, true);
+        if (batch > 0x7fffffff || heads > 0x7fffffff || kv_heads > 0x7fffffff || d > 0x7fffffff) refuse(std::string(c.call) + ": sizes out of range");
+        if (!out.defined() && !out_f32.defined()) out = at::empty(q.sizes(), q.options());
+        if (ws.defined()) {
+            if (!ws.is_contiguous() || !ws.is_cuda() || ws.get_device() != c.dev) refuse(std::string(c.call) + ": workspace must be dense, on the device of q");
+        } else if (tokens > 0) {
+            size_t bytes = 0;
+            rc = c_prompt_workspace_bytes((int)batch, (int)heads, (int)kv_heads, (int)d, &bytes);
+            if (rc == ADSA_OK) ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
+        }
+    }
+    size_t ws_bytes() const { return ws.defined() ? ws.nbytes() : 0; }
+    PyObject *result(int status, PyObject *const *o) const { return answer(status, out.defined() ? wrap(out, o[0]) : wrap(out_f32, o[1])); }
+};
+
+// q, k, v, cu_q, cu_k, causal, scale, out, out_f32, lse, workspace
+PyObject *packed_attn(PyObject *const *a, Py_ssize_t n)
+{
+    Check c{"packed_attn"};
+    need(n, 11, c.call);
+    const at::Tensor &q = tensor(a[0], c.call, "q"), &k = tensor(a[1], c.call, "k"), &v = tensor(a[2], c.call, "v"), &cu_q = tensor(a[3], c.call, "cu_q");
+    at::Tensor cu_k = tensor(a[4], c.call, "cu_k");
+    c.device_of(q, "q");
+    const int code = c.code(q, "q", 3);
+    const at::ScalarType type = q.scalar_type();
+    const int64_t d = q.size(2);
+    c.wants(q, "q", type, {-1, -1, -1}, false);
+    c.wants(k, "k", type, {-1, -1, d}, false);
+    c.wants(v, "v", type, {k.size(0), k.size(1), d}, false);
+    int64_t batch = 1;
+    if (cu_q.defined()) {
+        c.wants(cu_q, "cu_q", at::kInt, {-1}, true);
+        batch = cu_q.size(0) - 1;
+        if (batch < 1) refuse("packed_attn: cu_q must have two boundaries at least");
+        if (!cu_k.defined()) cu_k = cu_q;
+    }
+    if (cu_k.defined()) {
+        c.wants(cu_k, "cu_k", at::kInt, {cu_q.defined() ? batch + 1 : -1}, true);
+        if (!cu_q.defined()) refuse("packed_attn: cu_k needs cu_q");
+    }
+    const int causal = PyObject_IsTrue(a[5]);
+    if (causal < 0) throw Raised();
+    const float scale = (float)number(a[6]);
+    const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.dev);
+    const RowsOut o(c, q, a + 7, batch, k.size(1));
+    if (o.rc != ADSA_OK) return PyLong_FromLong(o.rc);
+    const int rc = c_packed_attn(code, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                                 v.stride(1), at_of<int32_t>(cu_q), at_of<int32_t>(cu_k), (int)batch, q.size(0), k.size(0), (int)q.size(1),
+                                 (int)k.size(1), (int)d, causal, scale, at_of<void>(o.out), at_of<float>(o.out_f32), at_of<float>(o.lse),
+                                 at_of<void>(o.ws), o.ws_bytes(), stream_of(c.dev));
+    return o.result(rc, a + 7);
+}
+
+// q, k_pool, v_pool, page_table, n_rows, cu_tokens, prefix_table, prefix_rows, group_start, scale, out, out_f32, lse, workspace, status
+PyObject *chunk_attn(PyObject *const *a, Py_ssize_t n)
+{
+    Check c{"chunk_attn"};
+    need(n, 15, c.call);
+    const at::Tensor &q = tensor(a[0], c.call, "q"), &table = tensor(a[3], c.call, "page_table"), &n_rows = tensor(a[4], c.call, "n_rows"),
+                     &cu = tensor(a[5], c.call, "cu_tokens"), &p_table = tensor(a[6], c.call, "prefix_table"),
+                     &p_rows = tensor(a[7], c.call, "prefix_rows"), &start = tensor(a[8], c.call, "group_start"), &status = tensor(a[14], c.call, "status");
+    c.device_of(q, "q");
+    const int code = c.code(q, "q", 3);
+    const at::ScalarType type = q.scalar_type();
+    c.wants(q, "q", type, {-1, -1, -1}, false);
+    const adsa_paged_kv kv = pool_of(c, tensor(a[1], c.call, "k_pool"), tensor(a[2], c.call, "v_pool"), code, type, -1, q.size(2));
+    c.wants(table, "page_table", at::kInt, {-1, -1}, true);
+    const int64_t batch = table.size(0);
+    c.wants(n_rows, "n_rows", at::kInt, {batch}, true);
+    if (cu.defined()) c.wants(cu, "cu_tokens", at::kInt, {batch + 1}, true);
+    int64_t groups = 0, p_pages = 0;
+    if (p_table.defined()) {
+        c.wants(p_table, "prefix_table", at::kInt, {-1, -1}, true);
+        groups = p_table.size(0);
+        p_pages = p_table.size(1);
+        c.wants(p_rows, "prefix_rows", at::kInt, {groups}, true);
+        c.wants(start, "group_start", at::kInt, {groups + 1}, true);
+    } else if (p_rows.defined() || start.defined()) {
+        refuse("chunk_attn: prefix_rows and group_start need prefix_table");
+    }
+    if (status.defined()) c.wants(status, "status", at::kInt, {1}, true);
+    if (table.size(1) > 0x7fffffff || groups > 0x7fffffff || p_pages > 0x7fffffff) refuse("chunk_attn: sizes out of range");
+    const float scale = (float)number(a[9]);
+    const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.dev);
+    const RowsOut o(c, q, a + 10, batch, kv.n_kv_heads);
+    if (o.rc != ADSA_OK) return PyLong_FromLong(o.rc);
+    const int rc = c_chunk_attn(&kv, q.data_ptr(), q.stride(0), q.stride(1), at_of<int32_t>(cu), (int)batch, q.size(0), (int)q.size(1),
+                                at_of<int32_t>(table), (int)table.size(1), at_of<int32_t>(n_rows), at_of<int32_t>(p_table), (int)p_pages,
+                                at_of<int32_t>(p_rows), at_of<int32_t>(start), (int)groups, scale, at_of<void>(o.out), at_of<float>(o.out_f32),
+                                at_of<float>(o.lse), at_of<void>(o.ws), o.ws_bytes(), (uint32_t *)at_of<int32_t>(status), stream_of(c.dev));
+    return o.result(rc, a + 10);
+}
+
 // the addresses of the C functions, in the order of the declarations above
 PyObject *bind(PyObject *const *a, Py_ssize_t n)
 {
-    need(n, 5, "bind");
-    void *p[5];
-    for (int i = 0; i < 5; ++i) {
+    constexpr int kBound = 8;
+    need(n, kBound, "bind");
+    void *p[kBound];
+    for (int i = 0; i < kBound; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: a function is missing");
@@ -315,6 +424,9 @@ PyObject *bind(PyObject *const *a, Py_ssize_t n)
     c_workspace_bytes = (decltype(c_workspace_bytes))p[2];
     c_shared_prefix_attn = (decltype(c_shared_prefix_attn))p[3];
     c_norm_residual = (decltype(c_norm_residual))p[4];
+    c_prompt_workspace_bytes = (decltype(c_prompt_workspace_bytes))p[5];
+    c_packed_attn = (decltype(c_packed_attn))p[6];
+    c_chunk_attn = (decltype(c_chunk_attn))p[7];
     Py_RETURN_NONE;
 }
 
@@ -335,7 +447,8 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 #define ADSA_ENTRY(name) {#name, (PyCFunction)(void *)entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ADSA_ENTRY(bind),          ADSA_ENTRY(rope_axes),     ADSA_ENTRY(paged_append),
-                         ADSA_ENTRY(shared_prefix_attn), ADSA_ENTRY(norm_residual), {nullptr, nullptr, 0, nullptr}};
+                         ADSA_ENTRY(shared_prefix_attn), ADSA_ENTRY(norm_residual), ADSA_ENTRY(packed_attn),
+                         ADSA_ENTRY(chunk_attn),    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "adsa_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

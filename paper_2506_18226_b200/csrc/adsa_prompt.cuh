@@ -1,0 +1,158 @@
+// What the kernels of adsa_packed_attn and adsa_chunk_attn share: their arguments, sequences as the device finds them, and the
+// attention of one query row by a warp.
+#pragma once
+
+#include "adsa_prefix.cuh"
+
+namespace adsa {
+
+struct PromptArgs {
+    const void *q, *k, *v;                  // k, v: packed rows, or the pools
+    long long q_token, q_head, k_token, k_head, v_token, v_head;   // element strides (k, v: of packed rows)
+    const int32_t *cu_q, *cu_k;             // [batch + 1]; null: sequences of equal length
+    // a paged cache: table != null
+    const int32_t *table, *n_rows;          // [batch][max_pages], [batch]
+    const int32_t *p_table, *p_rows, *start;   // [groups][max_p_pages], [groups], [groups + 1]
+    uint32_t *status;
+    long long n_q, n_k;                     // tokens of q; of packed k and v
+    int batch, groups, kv_heads, per_kv;    // per_kv: query heads of a key head
+    int max_pages, max_p_pages, page_rows, n_pages;
+    int d, row_stride, causal;
+    float scale_log2e;
+    void *out;                              // 16-bit, or null
+    float *out_f32, *lse;                   // or null
+};
+
+// A sequence: its new tokens q0 .. q0 + m - 1, its own rows (k0 .. of packed ones), the prefix of its group.
+struct PromptSeq {
+    long long q0, k0;
+    int m, n, p, group;
+    // own rows that new token i attends
+    __device__ __forceinline__ int seen(int i, int causal) const { return causal ? max(min(n - m + i + 1, n), 0) : n; }
+};
+
+// boundaries as given, kept inside 0 .. most and ascending for this sequence
+__device__ __forceinline__ void prompt_range(const int32_t *cu, int b, int batch, long long most, long long &begin, int &count)
+{
+    long long lo, hi;
+    if (cu) {
+        lo = cu[b];
+        hi = cu[b + 1];
+    } else {
+        const long long each = most / batch;
+        lo = b * each;
+        hi = lo + each;
+    }
+    begin = min(max(lo, 0LL), most);
+    count = (int)(min(max(hi, begin), most) - begin);
+}
+__device__ __forceinline__ int prompt_group(const PromptArgs &a, int b)
+{
+    int lo = 0, hi = a.groups;              // start[lo] <= b < start[hi], where boundaries ascend
+    if (hi == 0 || b < a.start[0] || b >= a.start[hi]) return -1;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.start[mid] <= b) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b)
+{
+    PromptSeq s;
+    prompt_range(a.cu_q, b, a.batch, a.n_q, s.q0, s.m);
+    s.k0 = 0;
+    s.p = 0;
+    s.group = -1;
+    if (a.table) {
+        s.n = clamp_rows(a.n_rows[b], a.max_pages, a.page_rows);
+        s.group = prompt_group(a, b);
+        if (s.group >= 0) s.p = clamp_rows(a.p_rows[s.group], a.max_p_pages, a.page_rows);
+    } else {
+        prompt_range(a.cu_k, b, a.batch, a.n_k, s.k0, s.n);
+    }
+    return s;
+}
+// the page that holds a row; one outside the pool is reported, and read as page 0 (the result is then unspecified)
+__device__ __forceinline__ int prompt_page(const PromptArgs &a, const int32_t *pages, int row)
+{
+    const int page = pages[row / a.page_rows];
+    if (page >= 0 && page < a.n_pages) return page;
+    if (a.status) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
+    return 0;
+}
+// element offset of cached row j (prefix rows first) of a sequence, key head h, in k (v: their own strides when packed)
+__device__ __forceinline__ size_t prompt_row(const PromptArgs &a, const PromptSeq &s, int b, int h, int j, bool value)
+{
+    if (!a.table) return (size_t)((s.k0 + j) * (value ? a.v_token : a.k_token) + h * (value ? a.v_head : a.k_head));
+    const bool pre = j < s.p;
+    const int row = pre ? j : j - s.p;
+    const int32_t *pages = pre ? a.p_table + (size_t)s.group * a.max_p_pages : a.table + (size_t)b * a.max_pages;
+    const int page = prompt_page(a, pages, row);
+    return (((size_t)page * a.kv_heads + h) * a.page_rows + row % a.page_rows) * a.row_stride;
+}
+
+// One query row by one warp, as the formula has it: a cached row per lane for the scores, elements spread over the lanes for
+// the sums.  All in 32 bits.  row: the row's index in out.
+template <typename T>
+__device__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int b, int i, int head, int lane)
+{
+    constexpr int PER = ADSA_MAX_HEAD_DIM / 64;              // pairs of elements a lane
+    const int h = head / a.per_kv, n = s.p + s.seen(i, a.causal);
+    const T *q = (const T *)a.q + (s.q0 + i) * a.q_token + head * a.q_head;
+    float m = -INFINITY, l = 0.f;
+    float2 o[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = make_float2(0.f, 0.f);
+    for (int j0 = 0; j0 < n; j0 += 32) {
+        const int j = j0 + lane;
+        float x = -INFINITY;
+        size_t v_at = 0;
+        if (j < n) {
+            const T *k = (const T *)a.k + prompt_row(a, s, b, h, j, false);
+            v_at = prompt_row(a, s, b, h, j, true);
+            x = 0.f;
+            for (int e = 0; e < a.d; ++e) x = fmaf(to_f32(q[e]), to_f32(k[e]), x);
+            x *= a.scale_log2e;
+        }
+        // (a NaN score has to reach the result: max would drop it)
+        const bool nan = __any_sync(0xffffffffu, isnan(x));
+        float mx = x;
+#pragma unroll
+        for (int k = 16; k; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
+        const float m_new = nan ? NAN : fmaxf(m, mx);
+        const float base = m_new == -INFINITY ? 0.f : m_new, corr = pa_exp2(m - base), w = j < n ? pa_exp2(x - base) : 0.f;
+        m = m_new;
+        float sum = w;
+#pragma unroll
+        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        l = l * corr + sum;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) { o[e].x *= corr; o[e].y *= corr; }
+        const int rows = min(n - j0, 32);
+        for (int r = 0; r < rows; ++r) {
+            const float p = __shfl_sync(0xffffffffu, w, r);
+            const T *v = (const T *)a.v + __shfl_sync(0xffffffffu, v_at, r);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                const int at = 2 * (lane + 32 * e);
+                if (at < a.d) {
+                    o[e].x = fmaf(p, to_f32(v[at]), o[e].x);
+                    o[e].y = fmaf(p, to_f32(v[at + 1]), o[e].y);
+                }
+            }
+        }
+    }
+    const size_t row = (size_t)(s.q0 + i) * a.kv_heads * a.per_kv + head;
+    const float inv = n > 0 ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int at = 2 * (lane + 32 * e);
+        if (at >= a.d) continue;
+        if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(o[e].x * inv, o[e].y * inv);
+        if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = make_float2(o[e].x * inv, o[e].y * inv);
+    }
+    if (a.lse && lane == 0) a.lse[row] = n > 0 ? (m + log2f(l)) * 0.693147180559945309f : -INFINITY;
+}
+
+}  // namespace adsa

@@ -1,0 +1,126 @@
+// Attention of many query rows per sequence: whole prompts laid end to end (adsa_packed_attn), and a chunk of new tokens over a
+// paged cache with a prefix that sequences share (adsa_chunk_attn).
+#include <math.h>
+
+#include "adsa_prompt.cuh"
+
+namespace adsa {
+
+constexpr int kPromptMaxBatch = 4096;
+constexpr long long kPromptMaxRows = 0x7fffff00LL;   // rows a table has room for, packed rows of a call: row numbers stay in 32 bits past the last tile
+constexpr int kPromptMaxPerKv = 64;
+
+// a warp per query row
+template <typename T>
+__global__ void __launch_bounds__(128) prompt_rows_kernel(const __grid_constant__ PromptArgs a)
+{
+    const int lane = threadIdx.x & 31, heads = a.kv_heads * a.per_kv;
+    pdl_wait();
+    pdl_launch();
+    for (long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); w < a.n_q * heads; w += (long long)gridDim.x * 4) {
+        const long long t = w / heads;
+        for (int b = 0; b < a.batch; ++b) {
+            const PromptSeq s = prompt_seq(a, b);
+            if (t < s.q0 || t >= s.q0 + s.m) continue;
+            prompt_row_by_warp<T>(a, s, b, (int)(t - s.q0), (int)(w - t * heads), lane);
+            break;
+        }
+    }
+}
+
+namespace {
+
+cudaError_t launch_prompt(int dtype, const PromptArgs &a, cudaStream_t st)
+{
+    const long long rows = a.n_q * a.kv_heads * a.per_kv, blocks = (rows + 3) / 4;
+    const unsigned grid = (unsigned)(blocks < 148 * 64 ? blocks : 148 * 64);
+    return dtype == ADSA_BF16 ? launch_pdl(prompt_rows_kernel<__nv_bfloat16>, dim3(grid), 128, 0, st, a)
+                              : launch_pdl(prompt_rows_kernel<__half>, dim3(grid), 128, 0, st, a);
+}
+
+bool heads_ok(int n_heads, int n_kv_heads, int head_dim)
+{
+    return n_kv_heads >= 1 && n_heads >= n_kv_heads && n_heads % n_kv_heads == 0 && n_heads / n_kv_heads <= kPromptMaxPerKv && head_dim >= 2 &&
+           head_dim % 2 == 0 && head_dim <= ADSA_MAX_HEAD_DIM;
+}
+
+// what both calls ask of q, the outputs and the workspace
+bool rows_ok(const void *q, long long q_token, long long q_head, int batch, long long n_q, int n_heads, float softmax_scale, const void *out,
+             const float *out_f32, const float *lse, const int32_t *cu_q, const void *workspace)
+{
+    if (!q || batch < 1 || batch > kPromptMaxBatch || n_q > kPromptMaxRows || n_q * n_heads > 0x7fffffffLL || (!cu_q && n_q % batch)) return false;
+    if ((!out && !out_f32) || !(softmax_scale >= 0.f) || !workspace) return false;
+    if (((uintptr_t)q & 3) || q_token % 2 || q_head % 2 || ((uintptr_t)workspace & 255) || ((uintptr_t)out & 3) || ((uintptr_t)out_f32 & 7)) return false;
+    return (((uintptr_t)lse | (uintptr_t)cu_q) & 3) == 0;
+}
+
+}  // namespace
+}  // namespace adsa
+
+using namespace adsa;
+
+extern "C" {
+
+int adsa_prompt_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes)
+{
+    if (!out_bytes || batch < 1 || batch > kPromptMaxBatch || !heads_ok(n_heads, n_kv_heads, head_dim)) return ADSA_EINVAL;
+    *out_bytes = 256;
+    return ADSA_OK;
+}
+
+int adsa_packed_attn(int dtype, const void *q, long long q_token, long long q_head, const void *k, long long k_token, long long k_head,
+                     const void *v, long long v_token, long long v_head, const int32_t *cu_q, const int32_t *cu_k, int batch, long long n_q,
+                     long long n_k, int n_heads, int n_kv_heads, int head_dim, int causal, float softmax_scale, void *out, float *out_f32,
+                     float *lse, void *workspace, size_t workspace_bytes, adsa_stream_t stream)
+{
+    size_t bytes = 0;
+    if ((dtype != ADSA_BF16 && dtype != ADSA_F16) || !heads_ok(n_heads, n_kv_heads, head_dim) || n_q < 0 || n_k < 0) return ADSA_EINVAL;
+    if (n_q == 0) return ADSA_OK;
+    if (!rows_ok(q, q_token, q_head, batch, n_q, n_heads, softmax_scale, out, out_f32, lse, cu_q, workspace)) return ADSA_EINVAL;
+    if ((n_k && (!k || !v)) || n_k > kPromptMaxRows || (!cu_k && n_k % batch)) return ADSA_EINVAL;
+    if (((uintptr_t)k & 3) || k_token % 2 || k_head % 2 || ((uintptr_t)v & 3) || v_token % 2 || v_head % 2 || ((uintptr_t)cu_k & 3)) return ADSA_EINVAL;
+    if (adsa_prompt_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, &bytes) != ADSA_OK) return ADSA_EINVAL;
+    if (workspace_bytes < bytes) return ADSA_ENOMEM;
+    PromptArgs a = {};
+    a.q = q; a.q_token = q_token; a.q_head = q_head;
+    a.k = k; a.k_token = k_token; a.k_head = k_head;
+    a.v = v; a.v_token = v_token; a.v_head = v_head;
+    a.cu_q = cu_q; a.cu_k = cu_k; a.batch = batch; a.n_q = n_q; a.n_k = n_k;
+    a.kv_heads = n_kv_heads; a.per_kv = n_heads / n_kv_heads; a.d = head_dim; a.causal = causal != 0;
+    a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : softmax_scale) * 1.44269504088896341f;
+    a.out = out; a.out_f32 = out_f32; a.lse = lse;
+    return launch_prompt(dtype, a, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
+}
+
+int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, long long q_head, const int32_t *cu_tokens, int batch,
+                    long long n_tokens, int n_heads, const int32_t *page_table, int max_pages, const int32_t *n_rows,
+                    const int32_t *prefix_table, int max_prefix_pages, const int32_t *prefix_rows, const int32_t *group_start, int n_groups,
+                    float softmax_scale, void *out, float *out_f32, float *lse, void *workspace, size_t workspace_bytes, uint32_t *status,
+                    adsa_stream_t stream)
+{
+    size_t bytes = 0;
+    if (!paged_kv_ok(kv) || !heads_ok(n_heads, kv->n_kv_heads, kv->head_dim) || n_tokens < 0 || n_groups < 0 || max_pages < 1) return ADSA_EINVAL;
+    if (n_tokens == 0) return ADSA_OK;
+    if (!rows_ok(q, q_token, q_head, batch, n_tokens, n_heads, softmax_scale, out, out_f32, lse, cu_tokens, workspace)) return ADSA_EINVAL;
+    if (!page_table || !n_rows || n_groups > kPromptMaxBatch) return ADSA_EINVAL;
+    if (n_groups && (!prefix_table || !prefix_rows || !group_start || max_prefix_pages < 1)) return ADSA_EINVAL;
+    if (((uintptr_t)page_table | (uintptr_t)n_rows | (uintptr_t)prefix_table | (uintptr_t)prefix_rows | (uintptr_t)group_start | (uintptr_t)status) & 3)
+        return ADSA_EINVAL;
+    if ((long long)max_pages * kv->page_rows > kPromptMaxRows || (n_groups && (long long)max_prefix_pages * kv->page_rows > kPromptMaxRows))
+        return ADSA_EINVAL;
+    if (adsa_prompt_workspace_bytes(batch, n_heads, kv->n_kv_heads, kv->head_dim, &bytes) != ADSA_OK) return ADSA_EINVAL;
+    if (workspace_bytes < bytes) return ADSA_ENOMEM;
+    PromptArgs a = {};
+    a.q = q; a.q_token = q_token; a.q_head = q_head;
+    a.k = kv->k_pool; a.v = kv->v_pool;
+    a.cu_q = cu_tokens; a.batch = batch; a.n_q = n_tokens;
+    a.table = page_table; a.max_pages = max_pages; a.n_rows = n_rows;
+    a.p_table = prefix_table; a.max_p_pages = max_prefix_pages; a.p_rows = prefix_rows; a.start = group_start; a.groups = n_groups;
+    a.page_rows = kv->page_rows; a.n_pages = kv->n_pages; a.row_stride = kv->row_stride; a.status = status;
+    a.kv_heads = kv->n_kv_heads; a.per_kv = n_heads / kv->n_kv_heads; a.d = kv->head_dim; a.causal = 1;
+    a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale) * 1.44269504088896341f;
+    a.out = out; a.out_f32 = out_f32; a.lse = lse;
+    return launch_prompt(kv->dtype, a, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
+}
+
+}  // extern "C"
