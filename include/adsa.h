@@ -525,7 +525,7 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
  * that this arithmetic leaves infinite or NaN is made again in 32 bits throughout, from the rows it attends alone: what lies in
  * rows that a query does not attend has no effect, infinities and NaN included.
  *
- * batch <= 4096 sequences; cu_q, cu_k, cu_tokens: int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 are sequence b (of no
+ * batch <= 4000 sequences; cu_q, cu_k, cu_tokens: int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 are sequence b (of no
  * tokens, maybe); tokens before cu[0] and from cu[batch] on are padding, whose output rows are left as they were; boundaries are
  * clamped to the tokens there are.  NULL: all sequences are equally long.  n_heads = g * n_kv_heads with g <= 64: query head h reads
  * key head h / g.  head_dim even, 2 .. 256.  q, k, v 4-byte aligned, even strides (quickest: 16 bytes, multiples of 8).

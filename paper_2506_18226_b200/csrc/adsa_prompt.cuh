@@ -1,5 +1,5 @@
-// What the kernels of adsa_packed_attn and adsa_chunk_attn share: their arguments, sequences as the device finds them, and the
-// attention of one query row by a warp.
+// What the kernels of adsa_packed_attn and adsa_chunk_attn share: their arguments, sequences as the device finds them, how the
+// work is cut, and the attention of one query row by a warp.
 #pragma once
 
 #include "adsa_prefix.cuh"
@@ -21,6 +21,12 @@ struct PromptArgs {
     float scale_log2e;
     void *out;                              // 16-bit, or null
     float *out_f32, *lse;                   // or null
+    // workspace: what each run leaves for the merge, partial states [2 runs][256 rows][64 or 128] and their (m, l)
+    int4 *run_desc;
+    float *state, *state_ml;
+    int box_rows;                           // rows of a copy's box in a page; 0: K and V are copied row by row
+    int q_boxes, tokens_first;              // q, and packed k and v, by boxes; their maps' order: bit 0 q, 1 k, 2 v: tokens before heads
+    int split;                              // items may be cut (into partial states)
 };
 
 // A sequence: its new tokens q0 .. q0 + m - 1, its own rows (k0 .. of packed ones), the prefix of its group.
@@ -73,6 +79,38 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b)
     }
     return s;
 }
+constexpr int kTileRows = 128;               // query rows of a half item, cached rows of a tile
+constexpr int kTileOver = 2;                // what an item costs beside its tiles, in units
+
+// An item: the query rows of `per` tokens (all query heads of one key head), in one half of up to 128 rows or in two.
+template <bool WIDE>
+struct TileItem {
+    int first, count, tiles;                // tokens; tiles of 128 cached rows (prefix, then own rows)
+    bool pair;                              // two halves
+    unsigned cost_tile;
+    __device__ __forceinline__ TileItem(const PromptArgs &a, const PromptSeq &s, int q);
+    __device__ __forceinline__ unsigned cost() const { return kTileOver + cost_tile * (unsigned)tiles; }
+};
+__device__ __forceinline__ int half_tokens(const PromptArgs &a) { return kTileRows / a.per_kv; }
+template <bool WIDE>
+__device__ __forceinline__ int item_tokens(const PromptArgs &a) { return WIDE ? half_tokens(a) : 2 * half_tokens(a); }
+template <bool WIDE>
+__device__ __forceinline__ int items_of(const PromptArgs &a, int m) { return (m + item_tokens<WIDE>(a) - 1) / item_tokens<WIDE>(a); }
+// tiles that the tokens up to i attend
+__device__ __forceinline__ int tiles_until(const PromptArgs &a, const PromptSeq &s, int i)
+{
+    return (s.p + kTileRows - 1) / kTileRows + (s.seen(i, a.causal) + kTileRows - 1) / kTileRows;
+}
+template <bool WIDE>
+__device__ __forceinline__ TileItem<WIDE>::TileItem(const PromptArgs &a, const PromptSeq &s, int q)
+{
+    first = q * item_tokens<WIDE>(a);
+    count = min(s.m - first, item_tokens<WIDE>(a));
+    tiles = tiles_until(a, s, first + count - 1);
+    pair = !WIDE && count > half_tokens(a);
+    cost_tile = WIDE || pair ? 2u : 1u;
+}
+
 // the page that holds a row; one outside the pool is reported, and read as page 0 (the result is then unspecified)
 __device__ __forceinline__ int prompt_page(const PromptArgs &a, const int32_t *pages, int row)
 {
@@ -93,11 +131,11 @@ __device__ __forceinline__ size_t prompt_row(const PromptArgs &a, const PromptSe
 }
 
 // One query row by one warp, as the formula has it: a cached row per lane for the scores, elements spread over the lanes for
-// the sums.  All in 32 bits.  row: the row's index in out.
+// the sums.  All in 32 bits.  Elements c0 .. c1 - 1 of the output, at most 128 of them.
 template <typename T>
-__device__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int b, int i, int head, int lane)
+__device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int b, int i, int head, int lane, int c0, int c1)
 {
-    constexpr int PER = ADSA_MAX_HEAD_DIM / 64;              // pairs of elements a lane
+    constexpr int PER = 2;                                   // pairs of elements a lane
     const int h = head / a.per_kv, n = s.p + s.seen(i, a.causal);
     const T *q = (const T *)a.q + (s.q0 + i) * a.q_token + head * a.q_head;
     float m = -INFINITY, l = 0.f;
@@ -135,8 +173,8 @@ __device__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int 
             const T *v = (const T *)a.v + __shfl_sync(0xffffffffu, v_at, r);
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
-                const int at = 2 * (lane + 32 * e);
-                if (at < a.d) {
+                const int at = c0 + 2 * (lane + 32 * e);
+                if (at < c1) {
                     o[e].x = fmaf(p, to_f32(v[at]), o[e].x);
                     o[e].y = fmaf(p, to_f32(v[at + 1]), o[e].y);
                 }
@@ -147,12 +185,15 @@ __device__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int 
     const float inv = n > 0 ? 1.f / l : 0.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-        const int at = 2 * (lane + 32 * e);
-        if (at >= a.d) continue;
+        const int at = c0 + 2 * (lane + 32 * e);
+        if (at >= c1) continue;
         if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(o[e].x * inv, o[e].y * inv);
         if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = make_float2(o[e].x * inv, o[e].y * inv);
     }
-    if (a.lse && lane == 0) a.lse[row] = n > 0 ? (m + log2f(l)) * 0.693147180559945309f : -INFINITY;
+    if (a.lse && lane == 0 && c0 == 0) a.lse[row] = n > 0 ? (m + log2f(l)) * 0.693147180559945309f : -INFINITY;
 }
+
+size_t prompt_workspace(int head_dim, int sms, PromptArgs *a, void *workspace);   // lays the workspace out; its size
+cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &a, int sms, cudaStream_t st);
 
 }  // namespace adsa

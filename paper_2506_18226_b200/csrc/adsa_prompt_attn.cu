@@ -6,36 +6,20 @@
 
 namespace adsa {
 
-constexpr int kPromptMaxBatch = 4096;
+constexpr int kPromptMaxBatch = 4000;        // the list of their work lies in shared memory, beside the tiles
 constexpr long long kPromptMaxRows = 0x7fffff00LL;   // rows a table has room for, packed rows of a call: row numbers stay in 32 bits past the last tile
 constexpr int kPromptMaxPerKv = 64;
 
-// a warp per query row
-template <typename T>
-__global__ void __launch_bounds__(128) prompt_rows_kernel(const __grid_constant__ PromptArgs a)
-{
-    const int lane = threadIdx.x & 31, heads = a.kv_heads * a.per_kv;
-    pdl_wait();
-    pdl_launch();
-    for (long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); w < a.n_q * heads; w += (long long)gridDim.x * 4) {
-        const long long t = w / heads;
-        for (int b = 0; b < a.batch; ++b) {
-            const PromptSeq s = prompt_seq(a, b);
-            if (t < s.q0 || t >= s.q0 + s.m) continue;
-            prompt_row_by_warp<T>(a, s, b, (int)(t - s.q0), (int)(w - t * heads), lane);
-            break;
-        }
-    }
-}
-
 namespace {
 
-cudaError_t launch_prompt(int dtype, const PromptArgs &a, cudaStream_t st)
+int sm_count()
 {
-    const long long rows = a.n_q * a.kv_heads * a.per_kv, blocks = (rows + 3) / 4;
-    const unsigned grid = (unsigned)(blocks < 148 * 64 ? blocks : 148 * 64);
-    return dtype == ADSA_BF16 ? launch_pdl(prompt_rows_kernel<__nv_bfloat16>, dim3(grid), 128, 0, st, a)
-                              : launch_pdl(prompt_rows_kernel<__half>, dim3(grid), 128, 0, st, a);
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return 148;
+    }
+    return n;
 }
 
 bool heads_ok(int n_heads, int n_kv_heads, int head_dim)
@@ -64,7 +48,7 @@ extern "C" {
 int adsa_prompt_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes)
 {
     if (!out_bytes || batch < 1 || batch > kPromptMaxBatch || !heads_ok(n_heads, n_kv_heads, head_dim)) return ADSA_EINVAL;
-    *out_bytes = 256;
+    *out_bytes = prompt_workspace(head_dim, sm_count(), nullptr, nullptr);
     return ADSA_OK;
 }
 
@@ -89,7 +73,10 @@ int adsa_packed_attn(int dtype, const void *q, long long q_token, long long q_he
     a.kv_heads = n_kv_heads; a.per_kv = n_heads / n_kv_heads; a.d = head_dim; a.causal = causal != 0;
     a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : softmax_scale) * 1.44269504088896341f;
     a.out = out; a.out_f32 = out_f32; a.lse = lse;
-    return launch_prompt(dtype, a, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
+    a.split = n_k > 4 * kTileRows;
+    const int sms = sm_count();
+    prompt_workspace(head_dim, sms, &a, workspace);
+    return launch_prompt_tiles(dtype, a, sms, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 
 int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, long long q_head, const int32_t *cu_tokens, int batch,
@@ -120,7 +107,10 @@ int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, l
     a.kv_heads = kv->n_kv_heads; a.per_kv = n_heads / kv->n_kv_heads; a.d = kv->head_dim; a.causal = 1;
     a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale) * 1.44269504088896341f;
     a.out = out; a.out_f32 = out_f32; a.lse = lse;
-    return launch_prompt(kv->dtype, a, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
+    a.split = ((long long)max_pages + max_prefix_pages) * kv->page_rows > 4 * kTileRows;
+    const int sms = sm_count();
+    prompt_workspace(kv->head_dim, sms, &a, workspace);
+    return launch_prompt_tiles(kv->dtype, a, sms, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
 }
 
 }  // extern "C"

@@ -1,0 +1,930 @@
+// Attention of many query rows per sequence on the fifth-generation tensor cores, for packed prompts and for chunks of new
+// tokens over a paged cache.
+//
+// A block (one per SM) has two groups of four warps, a query row per thread, with a 128-row tile of Q, 128 tensor-memory columns
+// of scores and up to 128 of O each.  Per tile of 128 cached rows and group: S = Q K^T (operands in shared memory), softmax weights
+// by the group's threads (row maxima and sums need no exchange between threads), P written back over S in tensor memory as 16-bit
+// values, O += P V (P from tensor memory, V as it lies: rows of K, elements contiguous).  One warp copies K and V, one Q, one issues
+// all products, one walks the list of items ahead of the others, so that one group's products run under the other's softmax and
+// the next item's copies and first scores under the last one's outputs.
+//
+// An item is the query rows of a run of tokens for all query heads of one key head (row = token * heads + head): with more than 128 rows,
+// both groups take every tile, each with its own half; up to 128, the groups take the tiles in turns, and join their states through
+// tensor memory at the end.  Heads of more than 128 elements (WIDE): items of up to 128 rows, both groups make the same scores and
+// weights, and each has 128 elements of O.
+//
+// The list of items in units (a tile of a half; two for what an item costs beside them) is cut into one run per block.  A cut near the
+// end of an item moves there; else the item's states go to the workspace, and a second kernel joins them.
+//
+// The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units): until then weights up to 2^8
+// are allowed, sums and products stay exact multiples, and O is rarely rescaled.  Weights are rounded once to the 16-bit type.
+// Rows of V behind the end are cleared in shared memory before they are used.  A weight of zero does not silence an infinity or NaN of a
+// later token's V in the same tile: a row that comes out infinite or NaN is made again by one warp from the rows it attends.
+#include <float.h>
+
+#include "adsa_prompt.cuh"
+#include "adsa_tc.cuh"
+
+namespace adsa {
+
+constexpr int kTileThreads = 384;           // warps 0 .. 3, 4 .. 7: the groups; 8 copies K and V; 9 issues the products; 10 copies Q; 11 walks
+constexpr int kTileColumns = 512;           // all of tensor memory: S (and P) of the groups at 0 and 128, O at 256 and 384
+constexpr float kTileSlack = 8.f;
+constexpr int kTileRing = 4;                // items ahead
+constexpr unsigned kTileMinRun = 6;         // units of a run, at least, where items may be cut
+
+struct TileDesc {                           // an item of a run, as the walking warp finds it
+    PromptSeq s;
+    int b, head, q;
+    int t0, t1;                             // tiles of this run; t1 < 0: no more items
+    int slot;                               // of the partial state; -1: the whole item
+};
+struct TilePos {
+    int b, head, q, tile;
+    __device__ __forceinline__ bool before(const TilePos &o) const
+    {
+        if (b != o.b) return b < o.b;
+        if (head != o.head) return head < o.head;
+        return q != o.q ? q < o.q : tile < o.tile;
+    }
+};
+struct TileControl {
+    uint64_t bars[48];
+    uint32_t tmem;
+    TileDesc ring[kTileRing];
+    float2 ml[kTileRows];                   // (m, l) of group 1 where the groups take turns
+};
+
+__device__ __forceinline__ void tile_tma3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tile_copy(uint32_t dst, const void *src, int bytes)
+{
+    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+// where byte x of a row lies in a tile of 128-byte columns in the 128-byte swizzle
+__device__ __forceinline__ uint32_t tile_at(int row, int x, uint32_t sub)
+{
+    return (uint32_t)(x >> 7) * sub + (uint32_t)row * 128u + (uint32_t)((((x >> 4) & 7) ^ (row & 7)) << 4) + (uint32_t)(x & 15);
+}
+// largest of 16, 8, 4 bytes that divides all of these
+__device__ __forceinline__ int piece_of(const void *p, long long token, long long head, int d)
+{
+    const unsigned long long x = (unsigned long long)(uintptr_t)p | (unsigned long long)(token * 2) | (unsigned long long)(head * 2) | (unsigned)(d * 2);
+    return x & 7 ? 4 : x & 15 ? 8 : 16;
+}
+
+// The item that unit u of the list lies in, and the tile that a run beginning there takes first; by a whole warp.
+template <bool WIDE>
+__device__ TilePos tile_locate(const PromptArgs &a, const unsigned long long *plan, unsigned long long u, unsigned long long tol, int lane)
+{
+    if (u >= plan[a.batch]) return {a.batch, 0, 0, 0};
+    int b = 0;
+    for (int b0 = 0;; b0 += 32) {
+        const int done = __popc(__ballot_sync(0xffffffffu, b0 + lane < a.batch && plan[b0 + lane + 1] <= u));
+        b = b0 + done;
+        if (done < 32) break;
+    }
+    const PromptSeq s = prompt_seq(a, b);
+    const unsigned long long per_head = (plan[b + 1] - plan[b]) / (unsigned)a.kv_heads;
+    unsigned long long rem = u - plan[b];
+    const int head = (int)(rem / per_head);
+    rem -= head * per_head;
+    const int nq = items_of<WIDE>(a, s.m);
+    for (int q0 = 0;; q0 += 32) {
+        const bool in = q0 + lane < nq;
+        const TileItem<WIDE> mine(a, s, in ? q0 + lane : 0);
+        const unsigned long long cost = in ? mine.cost() : 0u;
+        unsigned long long incl = cost;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+        const unsigned past = __ballot_sync(0xffffffffu, incl > rem);
+        if (!past && q0 + 32 < nq) {
+            rem -= __shfl_sync(0xffffffffu, incl, 31);
+            continue;
+        }
+        const int at = past ? __ffs(past) - 1 : 31;         // (past is never empty: the plan counted the same items)
+        const unsigned long long item_cost = __shfl_sync(0xffffffffu, cost, at), off = rem - (__shfl_sync(0xffffffffu, incl, at) - item_cost);
+        const int tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
+        const unsigned ct = __shfl_sync(0xffffffffu, mine.cost_tile, at);
+        const unsigned long long left = item_cost - off;
+        const bool near = min(off, left) <= tol;
+        int q = q0 + at, tile = near || off <= kTileOver ? 0 : (int)((off - kTileOver + ct - 1u) / ct);
+        if (near ? off <= left : tile < tiles || tiles == 0) return {b, head, q, tile};
+        if (++q < nq) return {b, head, q, 0};
+        return head + 1 < a.kv_heads ? TilePos{b, head + 1, 0, 0} : TilePos{b + 1, 0, 0, 0};
+    }
+}
+
+template <typename T, int NSUB, int SLOTS>
+__global__ void __launch_bounds__(kTileThreads, 1)
+prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                   const __grid_constant__ CUtensorMap v_map)
+{
+    constexpr bool WIDE = NSUB > 2;
+    constexpr int PARTS = WIDE ? 2 : 1, PSUB = NSUB / PARTS;   // a tile of K or V lies in PARTS slots of PSUB columns of 64 elements
+    constexpr int DO = 64 * PSUB;                             // elements of O of a group
+    constexpr uint32_t kSub = kTileRows * 128, kSlot = PSUB * kSub, kQ = (WIDE ? 1 : 2) * NSUB * kSub;
+    constexpr float kBias = WideBias<T>::value;
+    extern __shared__ unsigned char tile_smem[];
+    const uint32_t base = (smem_u32(tile_smem) + 1023u) & ~1023u;
+    const uint32_t q_at = base, ring = base + kQ;
+    unsigned char *const ctl = tile_smem + (base - smem_u32(tile_smem)) + kQ + (size_t)SLOTS * kSlot;
+    TileControl &c = *reinterpret_cast<TileControl *>(ctl);
+    unsigned long long *const plan = reinterpret_cast<unsigned long long *>(ctl + sizeof(TileControl));
+    const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 16, s_full = q_empty + 16,
+                   p_full = s_full + 16, o_full = p_full + 32, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8,
+                   d_empty = d_full + 8 * kTileRing;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
+
+    if (tid == 0) {
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        for (int g = 0; g < 2; ++g) {
+            mbar_init(q_full + 8 * g, 1); mbar_init(q_empty + 8 * g, 1); mbar_init(s_full + 8 * g, 1); mbar_init(o_full + 8 * g, 1);
+            mbar_init(p_full + 16 * g, 4); mbar_init(p_full + 16 * g + 8, 4);
+        }
+        mbar_init(m_full, 4);
+        mbar_init(m_empty, 4);
+        for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 11); }
+        mbar_init_fence();
+        if (a.q_boxes) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+        if (a.box_rows) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+        }
+    }
+    // what row copies leave of a row's last 16 elements is zero from the start
+    if ((!a.q_boxes || !a.box_rows) && a.d % 16) {
+        for (uint32_t i = tid; i < (kQ + SLOTS * kSlot) / 16; i += kTileThreads)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(base + 16 * i), "r"(0u) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 9) tc_alloc(smem_u32(&c.tmem), kTileColumns);
+    pdl_wait();
+    pdl_launch();
+    // units of every sequence: short ones by a lane each, long ones by their warp; then their running sum
+    for (int b0 = warp * 32; b0 < a.batch; b0 += kTileThreads) {
+        const int b = b0 + lane;
+        PromptSeq s = {};
+        if (b < a.batch) s = prompt_seq(a, b);
+        const int nq = items_of<WIDE>(a, s.m);
+        unsigned long long units = 0;
+        if (nq <= 4) {
+            for (int q = 0; q < nq; ++q) units += TileItem<WIDE>(a, s, q).cost();
+        }
+        for (unsigned todo = __ballot_sync(0xffffffffu, nq > 4); todo; todo &= todo - 1) {
+            const int src = __ffs(todo) - 1;
+            PromptSeq t = {};
+            t.m = __shfl_sync(0xffffffffu, s.m, src);
+            t.n = __shfl_sync(0xffffffffu, s.n, src);
+            t.p = __shfl_sync(0xffffffffu, s.p, src);
+            const int many = items_of<WIDE>(a, t.m);
+            unsigned long long sum = 0;
+            for (int q = lane; q < many; q += 32) sum += TileItem<WIDE>(a, t, q).cost();
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == src) units = sum;
+        }
+        if (b < a.batch) plan[b + 1] = units * (unsigned)a.kv_heads;
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, c.tmem, 0);
+
+    int limit = kCopySpinLimit;
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (!mbar_wait_bounded(bar, parity, limit)) {
+            limit = kCopySpinAfterTimeout;
+            if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+        }
+    };
+    int at = 0;                                                    // the next item of the ring
+    uint32_t d_phase = 0;
+    const auto next_item = [&]() {                                 // leaves the one before to be written over
+        __syncwarp();
+        if (lane == 0) mbar_arrive(d_empty + 8 * at);
+        if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
+    };
+    const auto have_item = [&]() {                                 // c.ring[at] is one
+        wait(d_full + 8 * at, d_phase);
+        return c.ring[at].t1 >= 0;
+    };
+    // cached rows of tile t, from its first row on
+    const auto rows_of = [&](const PromptSeq &s, int t) {
+        const int before = (s.p + kTileRows - 1) / kTileRows;
+        return t < before ? s.p - t * kTileRows : s.n - (t - before) * kTileRows;
+    };
+
+    // 168 registers a thread at the launch: the groups take what the other four warps leave
+    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 11) {                                              // ---- the list of items ----
+        if (lane == 0) plan[0] = 0;
+        __syncwarp();
+        unsigned long long before = 0;
+        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+            unsigned long long incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+            if (b0 + lane < a.batch) plan[b0 + lane + 1] = before + incl;
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        __syncwarp();
+        const unsigned run = blockIdx.x;
+        const unsigned long long most = max(a.split ? before / kTileMinRun : before, 1ULL), runs = min(most, (unsigned long long)gridDim.x);
+        int4 left = make_int4(-1, 0, 0, 0);                         // {sequence of the item that the last run to begin an item leaves
+                                                                   // unfinished, key head, item; whether an item cut before ends here}
+        if (run < runs) {
+            const unsigned long long tol = a.split ? before / runs / 32 : ~0ULL;
+            const TilePos end = tile_locate<WIDE>(a, plan, before * (run + 1) / runs, tol, lane);
+            TilePos pos = tile_locate<WIDE>(a, plan, before * run / runs, tol, lane);
+            int have = -1;
+            PromptSeq s = {};
+            while (pos.before(end)) {
+                if (pos.b != have) { s = prompt_seq(a, pos.b); have = pos.b; }
+                if (s.m == 0) { pos = {pos.b + 1, 0, 0, 0}; continue; }
+                const TileItem<WIDE> item(a, s, pos.q);
+                const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
+                const int t1 = last ? end.tile : item.tiles;
+                const bool whole = pos.tile == 0 && t1 == item.tiles;
+                if (!whole) {
+                    if (pos.tile > 0) left.w = t1 == item.tiles;
+                    else left = make_int4(pos.b, pos.head, pos.q, left.w);
+                }
+                wait(d_empty + 8 * at, d_phase ^ 1u);
+                if (lane == 0) {
+                    c.ring[at] = {s, pos.b, pos.head, pos.q, pos.tile, t1, whole ? -1 : (int)(2 * run) + (pos.tile > 0 ? 0 : 1)};
+                    mbar_arrive(d_full + 8 * at);
+                }
+                if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
+                if (last) break;
+                if (++pos.q >= items_of<WIDE>(a, s.m)) {
+                    pos.q = 0;
+                    if (++pos.head >= a.kv_heads) { pos.head = 0; ++pos.b; }
+                }
+                pos.tile = 0;
+            }
+        }
+        wait(d_empty + 8 * at, d_phase ^ 1u);
+        if (lane == 0) {
+            c.ring[at].t1 = -1;
+            mbar_arrive(d_full + 8 * at);
+            if (a.split) a.run_desc[run] = left;
+        }
+    } else if (warp == 8) {                                        // ---- copies of K and V ----
+        int slot = 0, waiting = 0;                                 // waiting: row copies in flight that nobody knows of yet
+        uint32_t phase = 0;
+        const int k_piece = piece_of(a.k, a.table ? a.row_stride : a.k_token, a.table ? 0 : a.k_head, a.d),
+                  v_piece = piece_of(a.v, a.table ? a.row_stride : a.v_token, a.table ? 0 : a.v_head, a.d);
+        const auto flush = [&]() {                                 // tell of all row copies
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0)
+                for (int i = waiting; i > 0; --i) mbar_arrive(full + 8 * (slot >= i ? slot - i : slot - i + SLOTS));
+            waiting = 0;
+        };
+        const auto copy = [&](const TileDesc &it, int t, bool value, int part) {   // a part of K or V of tile t into the next slot
+            const int before = (it.s.p + kTileRows - 1) / kTileRows, valid = min(rows_of(it.s, t), kTileRows);
+            const bool pre = t < before;
+            const int row0 = (pre ? t : t - before) * kTileRows, x0 = part * PSUB * 64;
+            const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
+            if (waiting && !mbar_try_wait(empty + 8 * slot, phase ^ 1u)) flush();
+            wait(empty + 8 * slot, phase ^ 1u);
+            const int32_t *pages = pre ? a.p_table + (size_t)it.s.group * a.max_p_pages : a.table + (size_t)it.b * a.max_pages;
+            if (a.box_rows && a.table) {
+                const int boxes = (valid + a.box_rows - 1) / a.box_rows;
+                if (lane == 0) mbar_expect_tx(bar, (uint32_t)(boxes * a.box_rows) * 128u * PSUB);
+                __syncwarp();
+                for (int i = lane; i < boxes; i += 32) {
+                    const int row = row0 + i * a.box_rows, page = prompt_page(a, pages, row);
+                    const int y = (page * a.kv_heads + it.head) * a.page_rows + row % a.page_rows;
+#pragma unroll
+                    for (int s = 0; s < PSUB; ++s)
+                        pa_tma(dst + (uint32_t)(i * a.box_rows) * 128u + s * kSub, value ? &v_map : &k_map, x0 + s * 64, y, bar);
+                }
+            } else if (a.box_rows) {
+                if (lane == 0) {
+                    mbar_expect_tx(bar, kSlot);
+                    const int tok = (int)it.s.k0 + row0;
+                    const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
+#pragma unroll
+                    for (int s = 0; s < PSUB; ++s)
+                        tile_tma3(dst + s * kSub, value ? &v_map : &k_map, x0 + s * 64, tf ? tok : it.head, tf ? it.head : tok, bar);
+                }
+                __syncwarp();
+            } else {
+                // row by row: a lane knows four rows, eight lanes copy one
+                const unsigned char *src = (const unsigned char *)(value ? a.v : a.k);
+                const int piece = value ? v_piece : k_piece, bytes = min(2 * a.d - 2 * x0, PSUB * 128);
+                unsigned long long off[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = lane + 32 * k;
+                    off[k] = r < valid ? 2ULL * prompt_row(a, it.s, it.b, it.head, (pre ? 0 : it.s.p) + row0 + r, value) + 2ULL * x0 : 0ULL;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    for (int i = 0; i < 8 && 32 * k + 4 * i < valid; ++i) {
+                        const int r = 32 * k + 4 * i + (lane >> 3);
+                        const unsigned long long o = __shfl_sync(0xffffffffu, off[k], r & 31);
+                        if (r < valid)
+                            for (int x = (lane & 7) * piece; x < bytes; x += 8 * piece) tile_copy(dst + tile_at(r, x, kSub), src + o + x, piece);
+                    }
+                }
+                ++waiting;
+            }
+            if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+        };
+        // in the order the products take them: K0 V0 K1 V1 .. where both groups share a tile, else K0 K1 V0 K2 V1 K3 ..
+        for (;;) {
+            if (waiting && !mbar_try_wait(d_full + 8 * at, d_phase)) flush();
+            if (!have_item()) break;
+            const TileDesc &it = c.ring[at];
+            const bool turns = !WIDE && min(it.s.m - it.q * item_tokens<WIDE>(a), item_tokens<WIDE>(a)) <= half_tokens(a);
+            const int ahead = turns ? 2 : 1;
+            for (int t = it.t0; t < min(it.t0 + ahead, it.t1); ++t) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) copy(it, t, false, p);
+            }
+            for (int t = it.t0; t < it.t1; ++t) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) copy(it, t, true, p);
+                if (t + ahead < it.t1) {
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) copy(it, t + ahead, false, p);
+                }
+            }
+            next_item();
+        }
+        if (waiting) flush();
+    } else if (warp == 10) {                                       // ---- copies of Q ----
+        uint32_t phase[2] = {0, 0};
+        const int piece = piece_of(a.q, a.q_token, a.q_head, a.d), per_row = 2 * a.d / piece, tph = half_tokens(a);
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            if (it.t1 == it.t0) continue;
+            const TileItem<WIDE> item(a, it.s, it.q);
+#pragma unroll
+            for (int h = 0; h < (WIDE ? 1 : 2); ++h) {
+                if (h == 1 && !item.pair) continue;
+                const int tok = item.first + h * tph, tokens = min(item.count - h * tph, tph);
+                const uint32_t dst = q_at + (uint32_t)h * NSUB * kSub, bar = q_full + 8 * h;
+                wait(q_empty + 8 * h, phase[h] ^ 1u);
+                phase[h] ^= 1u;
+                if (a.q_boxes) {
+                    if (lane == 0) {
+                        const int boxes = (a.d + 63) / 64, y = it.head * a.per_kv, z = (int)it.s.q0 + tok;
+                        mbar_expect_tx(bar, (uint32_t)(boxes * tph * a.per_kv) * 128u);
+                        for (int s = 0; s < boxes; ++s)
+                            tile_tma3(dst + s * kSub, &q_map, s * 64, y, z, bar);
+                    }
+                    __syncwarp();
+                } else {
+                    const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + tok) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
+                    for (int i = lane; i < tokens * a.per_kv * per_row; i += 32) {
+                        const int r = i / per_row, x = (i - r * per_row) * piece, t = r / a.per_kv;
+                        tile_copy(dst + tile_at(r, x, kSub), src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head) + x, piece);
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar);
+                }
+            }
+        }
+    } else if (warp == 9) {                                        // ---- products ----
+        const int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;
+        const uint32_t s_shape = tc_shape<T>(kTileRows, false);
+        int slot = 0;
+        uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+        const auto take = [&]() {                                  // the next slot, once its tile is there
+            wait(full + 8 * slot, phase);
+            const int taken = slot;
+            if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+            return taken;
+        };
+        const auto score = [&](int g, const int (&k_slot)[PARTS], uint32_t q) {   // S = Q K^T
+            const uint64_t qd = tc_operand(q, 16), kd0 = tc_operand(ring + (uint32_t)k_slot[0] * kSlot, 16),
+                           kd1 = tc_operand(ring + (uint32_t)k_slot[PARTS - 1] * kSlot, 16);
+            if (tc_elect()) {
+#pragma unroll
+                for (int ks = 0; ks < 4 * NSUB; ++ks) {
+                    const uint64_t q_off = ((uint32_t)(ks >> 2) * kSub + (uint32_t)(ks & 3) * 32u) >> 4;
+                    const uint64_t k_off = ((uint32_t)((ks >> 2) % PSUB) * kSub + (uint32_t)(ks & 3) * 32u) >> 4;
+                    if (ks < k_steps) tc_mma_ss(tmem + g * 128, qd + q_off, (ks < 4 * PSUB ? kd0 : kd1) + k_off, s_shape, ks > 0);
+                }
+            }
+        };
+        const auto take_v = [&](const TileDesc &it, int t) {                           // V of tile t, or a part of it
+            const int taken = take(), valid = rows_of(it.s, t);
+            if (valid < kTileRows) {
+                // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN
+                const uint32_t v_at = ring + (uint32_t)taken * kSlot;
+                for (int i = lane; i < (kTileRows - valid) * 8 * PSUB; i += 32) {
+                    const int r = valid + i / (8 * PSUB), ch = i % (8 * PSUB);
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v_at + (ch >> 3) * kSub + r * 128 + (ch & 7) * 16), "r"(0u) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            return taken;
+        };
+        const auto weigh = [&](int g, int v_slot, bool first) {    // O += P V, once the group has left P
+            const uint64_t vd = tc_operand(ring + (uint32_t)v_slot * kSlot, kSub);
+            const uint32_t o_shape = tc_shape<T>(WIDE ? min(d_cols - g * DO, DO) : d_cols, true);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {                 // P comes in two halves: the first is used while the second is made
+                wait(p_full + 16 * g + 8 * half, p_phase[g]);
+                tc_after();
+                if (tc_elect()) {
+#pragma unroll
+                    for (int k = 0; k < kTileRows / 32; ++k) {
+                        const int ks = half * (kTileRows / 32) + k;
+                        tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, !first || ks > 0);
+                    }
+                }
+                __syncwarp();
+            }
+            p_phase[g] ^= 1u;
+        };
+        const auto done = [&](uint32_t bar) {                      // counted when everything issued so far is complete
+            if (tc_elect()) tc_commit(bar);
+            __syncwarp();
+        };
+        const auto queries = [&](int h) {
+            wait(q_full + 8 * h, q_phase[h]);
+            q_phase[h] ^= 1u;
+        };
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            const int n = it.t1 - it.t0;
+            if (n == 0) continue;
+            const TileItem<WIDE> item(a, it.s, it.q);
+            int k[PARTS], v[PARTS];
+            const auto take_k = [&]() {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) k[p] = take();
+            };
+            const auto free_k = [&]() {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) done(empty + 8 * k[p]);
+            };
+            queries(0);
+            if (WIDE || item.pair) {
+                // the first half's tokens attend no more tiles than the second's
+                const int n0 = WIDE ? n : min(max(tiles_until(a, it.s, item.first + half_tokens(a) - 1) - it.t0, 0), n);
+                const uint32_t q1 = WIDE ? q_at : q_at + NSUB * kSub;
+                if (!WIDE) queries(1);
+                tc_after();
+                take_k();
+                if (n0 > 0) { score(0, k, q_at); done(s_full); }
+                if (!WIDE && n0 <= 1) done(q_empty);
+                score(1, k, q1);
+                free_k();
+                done(s_full + 8);
+                for (int i = 0; i < n; ++i) {
+                    const bool more = i + 1 < n;
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) v[p] = take_v(it, it.t0 + i);
+                    if (i < n0) weigh(0, v[0], i == 0);
+                    if (i == n0 - 1) done(o_full);
+                    if (more) {
+                        take_k();
+                        if (i + 1 < n0) {
+                            score(0, k, q_at);
+                            done(s_full);
+                            if (!WIDE && i + 2 == n0) done(q_empty);
+                        }
+                    }
+                    if (WIDE) done(empty + 8 * v[0]);
+                    weigh(1, v[PARTS - 1], i == 0);
+                    done(empty + 8 * v[PARTS - 1]);
+                    if (more) {
+                        score(1, k, q1);
+                        free_k();
+                        done(s_full + 8);
+                    }
+                    if (i + 2 == n || n == 1) done(q_empty + (WIDE ? 0 : 8));   // the last scores are issued
+                    if (!more) done(o_full + 8);
+                }
+            } else {
+                tc_after();
+                for (int g = 0; g < min(2, n); ++g) {
+                    take_k();
+                    score(g, k, q_at);
+                    free_k();
+                    done(s_full + 8 * g);
+                }
+                if (n <= 2) done(q_empty);
+                for (int i = 0; i < n; ++i) {
+                    const int g = i & 1;
+                    v[0] = take_v(it, it.t0 + i);
+                    weigh(g, v[0], i < 2);
+                    done(empty + 8 * v[0]);
+                    if (i + 2 < n) {
+                        take_k();
+                        score(g, k, q_at);
+                        free_k();
+                        done(s_full + 8 * g);
+                        if (i + 3 == n) done(q_empty);
+                    } else {
+                        done(o_full + 8 * g);
+                    }
+                }
+            }
+        }
+    } else {                                                       // ---- a query row per thread ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int g = warp >> 2, row = tid & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
+        const uint32_t my_s = s_full + 8 * g, my_p = p_full + 16 * g, my_o = o_full + 8 * g;
+        const int tph = half_tokens(a), heads = a.kv_heads * a.per_kv;
+        uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            const TileItem<WIDE> item(a, it.s, it.q);
+            const bool turns = !WIDE && !item.pair;                // the groups take the tiles in turns
+            const int half = item.pair ? g : 0, in = row / a.per_kv, tok = item.first + half * tph + in, head = it.head * a.per_kv + row - in * a.per_kv;
+            const bool there = in < tph && in + half * tph < item.count;
+            const int own = it.s.seen(min(tok, it.s.m - 1), a.causal), before = (it.s.p + kTileRows - 1) / kTileRows;
+            const bool warp_there = __any_sync(0xffffffffu, there);
+            int tiles = it.t1 - it.t0;
+            if (turns) tiles = (tiles + 1 - g) / 2;
+            else if (item.pair && g == 0) tiles = min(max(tiles_until(a, it.s, item.first + tph - 1) - it.t0, 0), tiles);
+            float m = -INFINITY;                                   // raw units; the row's weights are relative to it
+            float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            for (int i = 0; i < tiles; ++i) {
+                const int t = it.t0 + (turns ? 2 * i + g : i);
+                const int valid = t < before ? it.s.p - t * kTileRows : own - (t - before) * kTileRows;   // rows of the tile that this row attends
+                wait(my_s, s_phase);
+                s_phase ^= 1u;
+                tc_after();
+                if (!warp_there) {
+                    tc_before();
+                    if (lane == 0) { mbar_arrive(my_p); mbar_arrive(my_p + 8); }
+                    continue;
+                }
+                float v[kTileRows];
+#pragma unroll
+                for (int x = 0; x < kTileRows; x += 32) tc_load32(s_col + x, *reinterpret_cast<float (*)[32]>(v + x));
+                tc_load_wait();
+                if (__any_sync(0xffffffffu, valid < kTileRows)) {
+#pragma unroll
+                    for (int x = 0; x < kTileRows; ++x) v[x] = x < valid ? v[x] : -INFINITY;
+                }
+                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int x = 0; x < kTileRows; ++x) mx4[x & 3] = fmaxf(mx4[x & 3], v[x]);
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+                const bool move = (mx - m) * a.scale_log2e > kTileSlack || m == -INFINITY;
+                if (__any_sync(0xffffffffu, move)) {
+                    const float m_new = move ? fmaxf(m, mx) : m;
+                    const float corr = m_new == -INFINITY || m == -INFINITY ? (m == m_new ? 1.f : 0.f) : pa_exp2((m - m_new) * a.scale_log2e);
+                    m = m_new;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) { l2[k].x *= corr; l2[k].y *= corr; }
+                    if (i > 0) {                                   // the products before this tile's are complete: their S is
+#pragma unroll 1
+                        for (int x = 0; x < DO; x += 16) {
+                            float o[16];
+                            tc_load16(o_col + x, o);
+                            tc_load_wait();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] *= corr;
+                            tc_store16f(o_col + x, o);
+                        }
+                    }
+                }
+                const float shift = kBias - (m == -INFINITY ? 0.f : m) * a.scale_log2e;
+                const float2 scale2 = make_float2(a.scale_log2e, a.scale_log2e), shift2 = make_float2(shift, shift);
+#pragma unroll
+                for (int x = 0; x < kTileRows; x += 32) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float2 w = fma2(make_float2(v[x + 2 * k], v[x + 2 * k + 1]), scale2, shift2);
+                        w.x = pa_exp2(w.x);
+                        w.y = pa_exp2(w.y);
+                        l2[k & 1] = add2(l2[k & 1], w);            // the sum takes the weights before they are rounded
+                        p[k] = pack2<T>(w.x, w.y);
+                    }
+                    tc_store16(s_col + x / 2, p);                  // over scores that are in registers by now
+                    if (x % 64 == 32) {
+                        tc_store_wait();
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(my_p + 8 * (x / 64));
+                    }
+                }
+            }
+            if (tiles > 0) {
+                wait(my_o, o_phase);
+                o_phase ^= 1u;
+                tc_after();
+            }
+            // the row's state: O (in tensor memory) and l relative to 2^m2
+            float m2 = m == -INFINITY ? -INFINITY : m * a.scale_log2e - kBias, l = l2[0].x + l2[0].y + l2[1].x + l2[1].y, w0 = 1.f, w1 = 0.f;
+            bool both = false;
+            if (turns) {
+                if (g == 1) {
+                    c.ml[row] = make_float2(m2, l);
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(m_full);
+                    wait(m_empty, m_phase);                        // (group 0 has read this group's O)
+                    m_phase ^= 1u;
+                    tc_after();
+                    continue;
+                }
+                wait(m_full, m_phase);
+                m_phase ^= 1u;
+                tc_after();
+                both = it.t1 - it.t0 > 1;
+                if (both) {
+                    const float2 other = c.ml[row];
+                    const float M = fmaxf(m2, other.x);
+                    w0 = m2 == -INFINITY ? 0.f : pa_exp2(m2 - M);
+                    w1 = other.x == -INFINITY ? 0.f : pa_exp2(other.x - M);
+                    l = l * w0 + other.y * w1;
+                    m2 = M;
+                }
+            }
+            const int c0 = WIDE ? g * DO : 0, c1 = min(a.d, c0 + DO);   // elements of the output
+            const bool none = it.s.p + own == 0, partial = it.slot >= 0;
+            const float inv = 1.f / l;
+            if (!partial && none) w0 = w1 = 0.f;
+            else if (!partial) { w0 *= inv; w1 *= inv; }
+            const size_t at_row = ((size_t)it.s.q0 + tok) * heads + head, at_slot = (size_t)it.slot * 256 + (WIDE ? g * 128 : half * 128) + row;
+            float2 bad = make_float2(0.f, 0.f);
+            if (warp_there) {
+#pragma unroll 1
+                for (int x = 0; x < DO; x += 16) {
+                    if (c0 + x >= c1 && !partial) break;
+                    float o[16];
+                    if (tiles > 0) {
+                        tc_load16(o_col + x, o);
+                        tc_load_wait();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] *= w0;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = 0.f;
+                    }
+                    if (both) {
+                        float o1[16];
+                        tc_load16(tmem + 384 + lanes + x, o1);
+                        tc_load_wait();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = fmaf(o1[k], w1, o[k]);
+                    }
+                    if (there && partial) {
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4)
+                            *reinterpret_cast<float4 *>(a.state + at_slot * DO + x + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                    } else if (there) {
+                        const int cols = min(16, c1 - c0 - x);
+                        if (none) {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] = 0.f;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 16; k += 2)
+                            if (k < cols) bad = fma2(make_float2(o[k], o[k + 1]), make_float2(0.f, 0.f), bad);
+                        if (a.out) {
+                            T *dst = (T *)a.out + at_row * a.d + c0 + x;
+                            if (cols == 16 && ((uintptr_t)dst & 15) == 0) {
+#pragma unroll
+                                for (int k = 0; k < 16; k += 8)
+                                    *reinterpret_cast<uint4 *>(dst + k) =
+                                        make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 16; k += 2)
+                                    if (k < cols) *reinterpret_cast<uint32_t *>(dst + k) = pack2<T>(o[k], o[k + 1]);
+                            }
+                        }
+                        if (a.out_f32) {
+#pragma unroll
+                            for (int k = 0; k < 16; k += 2)
+                                if (k < cols) *reinterpret_cast<float2 *>(a.out_f32 + at_row * a.d + c0 + x + k) = make_float2(o[k], o[k + 1]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (there && partial) *reinterpret_cast<float2 *>(a.state_ml + 2 * at_slot) = make_float2(m2, l);
+                if (there && !partial && a.lse && c0 == 0) a.lse[at_row] = none ? -INFINITY : (m2 + log2f(l)) * 0.693147180559945309f;
+            }
+            tc_before();                                           // read before the next item's products write O
+            if (turns) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(m_empty);
+            }
+            // rows that came out infinite or NaN, from what they attend alone
+            unsigned again = __ballot_sync(0xffffffffu, there && !partial && bad.x + bad.y != 0.f);
+            for (; again; again &= again - 1) {
+                const int src = __ffs(again) - 1;
+                prompt_row_by_warp<T>(a, it.s, it.b, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), lane, c0, c1);
+            }
+        }
+    }
+    tc_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_after();
+        tc_dealloc(tmem, kTileColumns);
+    }
+}
+
+// Joins the states of items that runs have cut: a warp per row, blocks (cut, eight rows).  The run that began such an item
+// names it; the runs behind it have one state each, up to the one that ended the item.
+constexpr int kTileMergeThreads = 256;
+template <typename T, int NSUB>
+__global__ void __launch_bounds__(kTileMergeThreads)
+prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
+{
+    constexpr bool WIDE = NSUB > 2;
+    constexpr int DO = WIDE ? 128 : 64 * NSUB, PER = DO / 32, AHEAD = 4;
+    const int lane = threadIdx.x & 31, r = (int)blockIdx.y * (kTileMergeThreads / 32) + (threadIdx.x >> 5);
+    pdl_wait();
+    pdl_launch();
+    const int lead = blockIdx.x;
+    const int4 d = a.run_desc[lead];
+    if (d.x < 0) return;
+    const PromptSeq s = prompt_seq(a, d.x);
+    const TileItem<WIDE> item(a, s, d.z);
+    const int half = r >> 7, tph = half_tokens(a), in = (r & 127) / a.per_kv, in_item = in + (WIDE ? 0 : half * tph);
+    if (in >= tph || in_item >= item.count || (half && !WIDE && !item.pair)) return;
+    int pieces = 2;
+    while (lead + pieces < runs && !a.run_desc[lead + pieces - 1].w) ++pieces;
+    const int tok = item.first + in_item, head = d.y * a.per_kv + (r & 127) - in * a.per_kv;
+    float m = -INFINITY, l = 0.f, o[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = 0.f;
+    for (int i0 = 0; i0 < pieces; i0 += AHEAD) {
+        float2 ml[AHEAD];
+        float x[AHEAD][PER];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k;
+            ml[k] = make_float2(-INFINITY, 0.f);
+            if (i < pieces) {
+                const size_t slot = ((size_t)2 * (lead + i) + (i == 0 ? 1 : 0)) * 256 + r;
+                ml[k] = *reinterpret_cast<const float2 *>(a.state_ml + 2 * slot);
+#pragma unroll
+                for (int e = 0; e < PER; e += 2) *reinterpret_cast<float2 *>(&x[k][e]) = *reinterpret_cast<const float2 *>(a.state + slot * DO + e * 32 + 2 * lane);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (ml[k].y == 0.f && ml[k].x == -INFINITY) continue;   // an empty state
+            const float M = fmaxf(m, ml[k].x), w1 = m == -INFINITY ? 0.f : pa_exp2(m - M), w2 = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
+            l = l * w1 + ml[k].y * w2;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) o[e] = o[e] * w1 + x[k][e] * w2;
+            m = M;
+        }
+    }
+    const bool none = s.p + s.seen(tok, a.causal) == 0;
+    const float inv = none ? 0.f : 1.f / l;
+    const int c0 = WIDE ? half * DO : 0, c1 = min(a.d, c0 + DO);
+    const size_t row = ((size_t)s.q0 + tok) * a.kv_heads * a.per_kv + head;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < PER; e += 2) {
+        const int at = c0 + e * 32 + 2 * lane;
+        if (at >= c1) continue;
+        const float2 x = none ? make_float2(0.f, 0.f) : make_float2(o[e] * inv, o[e + 1] * inv);
+        bad = bad || !(fabsf(x.x) <= FLT_MAX) || !(fabsf(x.y) <= FLT_MAX);
+        if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(x.x, x.y);
+        if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = x;
+    }
+    if (a.lse && lane == 0 && c0 == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+    if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, s, d.x, tok, head, lane, c0, c1);
+}
+
+size_t prompt_workspace(int head_dim, int sms, PromptArgs *a, void *workspace)
+{
+    const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    const size_t rows = (size_t)2 * sms * 256, desc = up((size_t)sms * sizeof(int4)), state = up(rows * (head_dim <= 64 ? 64 : 128) * 4);
+    if (a) {
+        unsigned char *const w = (unsigned char *)workspace;
+        a->run_desc = (int4 *)w;
+        a->state = (float *)(w + desc);
+        a->state_ml = (float *)(w + desc + state);
+    }
+    return desc + state + up(rows * 8);
+}
+
+namespace {
+
+typedef CUresult (*encode_t)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                             const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                             CUtensorMapFloatOOBfill);
+encode_t encoder()
+{
+    static encode_t fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return (encode_t)f;
+    }();
+    return fn;
+}
+bool encode(CUtensorMap *m, int dtype, int rank, const void *at, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box)
+{
+    const encode_t fn = encoder();
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn && fn(m, dtype == ADSA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void *>(at), dims,
+                    strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Rows of heads and tokens as boxes of heads x tokens rows of 64 elements; heads before tokens, or (one head to a box) the other way
+// round, where that makes strides ascend.  False: not aligned as a box has to be.
+bool rows_map(CUtensorMap *m, int dtype, const void *at, int d, long long n_heads, long long head, long long n_tokens, long long token, int box_heads,
+              int box_tokens, bool *tokens_first)
+{
+    if (((uintptr_t)at & 15) || head % 8 || token % 8 || head <= 0 || token <= 0 || n_tokens < 1) return false;
+    const bool tf = box_heads == 1 && token < head;
+    const cuuint64_t h = (cuuint64_t)n_heads, t = (cuuint64_t)n_tokens, hs = (cuuint64_t)head * 2, ts = (cuuint64_t)token * 2;
+    const cuuint64_t dims[3] = {(cuuint64_t)d, tf ? t : h, tf ? h : t}, strides[2] = {tf ? ts : hs, tf ? hs : ts};
+    const cuuint32_t box[3] = {64, (cuuint32_t)(tf ? box_tokens : box_heads), (cuuint32_t)(tf ? box_heads : box_tokens)};
+    *tokens_first = tf;
+    return encode(m, dtype, 3, at, dims, strides, box);
+}
+bool page_map(CUtensorMap *m, int dtype, const PromptArgs &a, const void *pool, int box_rows)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)a.d, (cuuint64_t)a.n_pages * a.kv_heads * a.page_rows}, strides[1] = {(cuuint64_t)a.row_stride * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return encode(m, dtype, 2, pool, dims, strides, box);
+}
+
+template <typename T, int NSUB, int SLOTS>
+cudaError_t launch_tiles(const PromptArgs &a, unsigned runs, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+{
+    constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
+    constexpr size_t most = 227 * 1024;
+    static_assert(sizeof(TileControl) % 8 == 0 && 2 * SLOTS + 28 <= 48, "control block");
+    static_assert(1024 + q + SLOTS * slot + sizeof(TileControl) <= most, "shared memory");
+    const size_t smem = 1024 + q + SLOTS * slot + sizeof(TileControl) + (size_t)(a.batch + 1) * 8;
+    if (smem > most) {                                             // the list of a large batch takes the room of a slot
+        if constexpr (SLOTS == 5) return launch_tiles<T, NSUB, SLOTS - 1>(a, runs, qm, km, vm, st);
+        return cudaErrorInvalidValue;
+    }
+    const auto kern = prompt_tile_kernel<T, NSUB, SLOTS>;
+    static int told[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool known = dev >= 0 && dev < 64;
+    if (!known || !__atomic_load_n(&told[dev], __ATOMIC_ACQUIRE)) {
+        e = cudaFuncSetAttribute((const void *)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+        if (e != cudaSuccess) return e;
+        if (known) __atomic_store_n(&told[dev], 1, __ATOMIC_RELEASE);
+    }
+    e = launch_pdl(kern, dim3(runs), kTileThreads, smem, st, a, qm, km, vm);
+    if (e != cudaSuccess || !a.split || runs < 2) return e;
+    return launch_pdl(prompt_tile_merge_kernel<T, NSUB>, dim3(runs - 1, 256 / (kTileMergeThreads / 32)), kTileMergeThreads, 0, st, a, (int)runs);
+}
+template <typename T>
+cudaError_t launch_tiles_type(const PromptArgs &a, unsigned runs, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+{
+    if (a.d <= 64) return launch_tiles<T, 1, 10>(a, runs, qm, km, vm, st);
+    if (a.d <= 128) return launch_tiles<T, 2, 5>(a, runs, qm, km, vm, st);
+    return launch_tiles<T, 4, 5>(a, runs, qm, km, vm, st);
+}
+
+}  // namespace
+
+cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cudaStream_t st)
+{
+    PromptArgs a = args;
+    CUtensorMap qm = {}, km = {}, vm = {};
+    const int heads = a.kv_heads * a.per_kv;
+    bool tf = false;
+    a.q_boxes = rows_map(&qm, dtype, a.q, a.d, heads, a.q_head, a.n_q, a.q_token, a.per_kv, kTileRows / a.per_kv, &tf) && !tf;
+    a.tokens_first = 0;
+    a.box_rows = 0;
+    if (a.table) {
+        int box = kTileRows;
+        while (a.page_rows % box) box /= 2;                        // boxes that never straddle two pages; eight rows are one block of the swizzle
+        if (box >= 8 && page_map(&km, dtype, a, a.k, box) && page_map(&vm, dtype, a, a.v, box)) a.box_rows = box;
+    } else {
+        bool kt = false, vt = false;
+        if (rows_map(&km, dtype, a.k, a.d, a.kv_heads, a.k_head, a.n_k, a.k_token, 1, kTileRows, &kt) &&
+            rows_map(&vm, dtype, a.v, a.d, a.kv_heads, a.v_head, a.n_k, a.v_token, 1, kTileRows, &vt)) {
+            a.box_rows = kTileRows;
+            a.tokens_first = (kt ? 2 : 0) | (vt ? 4 : 0);
+        }
+    }
+    return dtype == ADSA_BF16 ? launch_tiles_type<__nv_bfloat16>(a, (unsigned)sms, qm, km, vm, st) : launch_tiles_type<__half>(a, (unsigned)sms, qm, km, vm, st);
+}
+
+}  // namespace adsa
