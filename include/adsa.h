@@ -557,6 +557,35 @@ ADSA_API int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q
                              int n_groups, float softmax_scale, void *out, float *out_f32, float *lse, void *workspace,
                              size_t workspace_bytes, uint32_t *status, adsa_stream_t stream);
 
+/* ---- the next token ----------------------------------------------------------------------------------------------
+ * Drawn per row of logits from given uniform numbers, with settings per row or for all.  With x the row's logits (or mixed ones, see
+ * below), M the largest and w_i = exp((x_i - M) / temperature), the ids in the order (x descending, id ascending) are kept
+ *   - up to the top_k-th (top_k < 1: all of them),
+ *   - of these up to the first at which the running sum of w reaches top_p of their sum (top_p >= 1: all; one id at least),
+ *   - of these while w_i >= min_p (min_p <= 0: all; > 1: as 1),
+ * and the token is the first kept id, in ascending order of id, at which the running sum of w reaches u * (sum of w).
+ * temperature <= 0: the largest logit, the lowest id of these.  Ids with logits of -infinity or NaN are never drawn; a row
+ * of nothing else gets token -1, logprob -infinity.  Of infinite logits the +infinite alone have weight.  Weights are made in 64 bits and
+ * summed in steps of 2^-42 of the largest, independent of the order: ids are kept and drawn as the real numbers say, and a call is reproducible.
+ *   logits   bf16, f16 or float [rows][vocab], rows `row` elements apart; 1 <= vocab <= 2^20
+ *   uncond   the same, or NULL; then x = uncond + guidance * (logits - uncond), each of the three operations rounded to 32 bits
+ *            (adsa_cfg_sample's mix, which rounds twice)
+ *   uniforms float [rows] in [0, 1) (others are clamped to 0 .. 1);  tokens int32 [rows]
+ *   logprobs float [rows]: ln of the drawn id's share of the kept weights, or NULL
+ * NaN among the settings on the host and a guidance that is not finite are ADSA_EINVAL; per row (on the device) NaN leaves top_p and min_p
+ * out and takes the largest logit for a temperature. */
+typedef struct {
+    float temperature;                /* for all rows, unless the array is given: [device] [rows], each may be NULL */
+    int32_t top_k;
+    float top_p, min_p;
+    const float *temperatures;
+    const int32_t *top_ks;
+    const float *top_ps, *min_ps;
+    float guidance;                   /* of uncond */
+} adsa_sampling;
+ADSA_API int adsa_sample(const adsa_sampling *how, int dtype, const void *logits, long long row, const void *uncond, long long uncond_row,
+                         int rows, int vocab, const float *uniforms, int32_t *tokens, float *logprobs, adsa_stream_t stream);
+
 ADSA_API const char *adsa_strerror(int status);
 
 #ifdef __cplusplus

@@ -29,7 +29,7 @@ EXPORTS = [
     "adsa_rmsnorm", "adsa_swiglu", "adsa_cfg_sample",
     "adsa_rotary_init", "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn",
     "adsa_norm_residual",
-    "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn",
+    "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn", "adsa_sample",
 ]
 
 
@@ -54,6 +54,11 @@ class AdsaPagedKv(C.Structure):
 class AdsaRotary(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("head_dim", "n_axes", "n_pairs", "halves")] + \
         [("turns", C.c_double * 128), ("axis", C.c_uint8 * 128)]
+
+
+class AdsaSampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float), ("temperatures", C.c_void_p),
+                ("top_ks", C.c_void_p), ("top_ps", C.c_void_p), ("min_ps", C.c_void_p), ("guidance", C.c_float)]
 
 
 class AdsaError(RuntimeError):
@@ -113,6 +118,7 @@ def load(rebuild: bool = False) -> C.CDLL:
             "adsa_norm_residual": [i32, i32, vp, vp, vp, vp, ll, vp, vp, vp, ll, i32, C.c_float, C.c_float, vp],
             "adsa_prompt_workspace_bytes": [i32, i32, i32, i32, C.POINTER(sz)],
             "adsa_packed_attn": [i32, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, i32, ll, ll, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp, sz, vp],
+            "adsa_sample": [C.POINTER(AdsaSampling), i32, vp, ll, vp, ll, i32, i32, vp, vp, vp, vp],
             "adsa_chunk_attn": [vp, vp, ll, ll, vp, i32, ll, i32, vp, i32, vp, vp, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, sz, vp, vp],
         }
         for name, args in sig.items():
@@ -216,7 +222,7 @@ def _marshal():
         loader.exec_module(module)
         module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value for name in (
             "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn", "adsa_norm_residual",
-            "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn")))
+            "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn", "adsa_sample")))
         _marshal_module = module
     return _marshal_module
 
@@ -348,6 +354,19 @@ def chunk_attn(q, k_pool, v_pool, page_table, n_rows, cu_tokens=None, prefix_tab
                                                    scale, out, out_f32, lse, workspace, status)
     if r.__class__ is int:
         raise AdsaError(r, "adsa_chunk_attn")
+    return r
+
+
+def sample(logits, uniforms, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, uncond=None, guidance=1.0, tokens=None, logprobs=None):
+    """adsa_sample: the next token of every row of logits [rows, vocab] (bfloat16, float16 or float32, any row stride) from
+    uniforms, float32 [rows] in [0, 1); returns int32 [rows].
+
+    temperature (0: the largest logit), top_k (0: all), top_p (1: all), min_p (0: all): a number for all rows, or a tensor of one per
+    row (float32; top_k int32).  uncond [rows, vocab]: logits are mixed as uncond + guidance * (logits - uncond) first.  logprobs:
+    float32 [rows] for the logarithm of the drawn token's share of what was kept."""
+    r = (_marshal_module or _marshal()).sample(logits, uniforms, temperature, top_k, top_p, min_p, uncond, guidance, tokens, logprobs)
+    if r.__class__ is int:
+        raise AdsaError(r, "adsa_sample")
     return r
 
 

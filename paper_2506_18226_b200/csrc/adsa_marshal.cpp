@@ -27,6 +27,7 @@ decltype(&adsa_norm_residual) c_norm_residual;
 decltype(&adsa_prompt_workspace_bytes) c_prompt_workspace_bytes;
 decltype(&adsa_packed_attn) c_packed_attn;
 decltype(&adsa_chunk_attn) c_chunk_attn;
+decltype(&adsa_sample) c_sample;
 
 struct Raised {};                            // a Python exception is set
 
@@ -406,10 +407,58 @@ PyObject *chunk_attn(PyObject *const *a, Py_ssize_t n)
     return o.result(rc, a + 10);
 }
 
+// logits, uniforms, temperature, top_k, top_p, min_p, uncond, guidance, tokens, logprobs
+PyObject *sample(PyObject *const *a, Py_ssize_t n)
+{
+    Check c{"sample"};
+    need(n, 10, c.call);
+    const at::Tensor &logits = tensor(a[0], c.call, "logits"), &uniforms = tensor(a[1], c.call, "uniforms"), &uncond = tensor(a[6], c.call, "uncond"),
+                     &logprobs = tensor(a[9], c.call, "logprobs");
+    c.device_of(logits, "logits");
+    const at::ScalarType type = logits.scalar_type();
+    const int code = type == at::kFloat && logits.dim() == 2 ? ADSA_F32 : c.code(logits, "logits", 2);
+    c.wants(logits, "logits", type, {-1, -1}, false);
+    const int64_t rows = logits.size(0), vocab = logits.size(1);
+    c.wants(uniforms, "uniforms", at::kFloat, {rows}, true);
+    if (uncond.defined()) c.wants(uncond, "uncond", type, {rows, vocab}, false);
+    if (logprobs.defined()) c.wants(logprobs, "logprobs", at::kFloat, {rows}, true);
+    at::Tensor tokens = tensor(a[8], c.call, "tokens");
+    if (tokens.defined()) c.wants(tokens, "tokens", at::kInt, {rows}, true);
+    adsa_sampling how = {1.f, 0, 1.f, 0.f, nullptr, nullptr, nullptr, nullptr, (float)number(a[7])};
+    const auto setting = [&](PyObject *o, const char *name, float &all, const float *&each) {   // a number, or one per row
+        if (!THPVariable_Check(o)) {
+            all = (float)number(o);
+            return;
+        }
+        const at::Tensor &t = THPVariable_Unpack(o);
+        c.wants(t, name, at::kFloat, {rows}, true);
+        each = at_of<float>(t);
+    };
+    setting(a[2], "temperature", how.temperature, how.temperatures);
+    setting(a[4], "top_p", how.top_p, how.top_ps);
+    setting(a[5], "min_p", how.min_p, how.min_ps);
+    if (THPVariable_Check(a[3])) {
+        const at::Tensor &t = THPVariable_Unpack(a[3]);
+        c.wants(t, "top_k", at::kInt, {rows}, true);
+        how.top_ks = at_of<int32_t>(t);
+    } else {
+        const long k = PyLong_AsLong(a[3]);
+        if (k == -1 && PyErr_Occurred()) throw Raised();
+        if (k > 0x7fffffff || k < -0x7fffffff) refuse("sample: top_k is out of range");
+        how.top_k = (int32_t)k;
+    }
+    if (rows > 0x7fffffff || vocab > 0x7fffffff) refuse("sample: sizes out of range");
+    const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.dev);
+    if (!tokens.defined()) tokens = at::empty({rows}, logits.options().dtype(at::kInt));
+    const int rc = c_sample(&how, code, logits.data_ptr(), logits.stride(0), at_of<void>(uncond), uncond.defined() ? uncond.stride(0) : 0, (int)rows,
+                            (int)vocab, at_of<float>(uniforms), at_of<int32_t>(tokens), at_of<float>(logprobs), stream_of(c.dev));
+    return answer(rc, wrap(tokens, a[8]));
+}
+
 // the addresses of the C functions, in the order of the declarations above
 PyObject *bind(PyObject *const *a, Py_ssize_t n)
 {
-    constexpr int kBound = 8;
+    constexpr int kBound = 9;
     need(n, kBound, "bind");
     void *p[kBound];
     for (int i = 0; i < kBound; ++i) {
@@ -427,6 +476,7 @@ PyObject *bind(PyObject *const *a, Py_ssize_t n)
     c_prompt_workspace_bytes = (decltype(c_prompt_workspace_bytes))p[5];
     c_packed_attn = (decltype(c_packed_attn))p[6];
     c_chunk_attn = (decltype(c_chunk_attn))p[7];
+    c_sample = (decltype(c_sample))p[8];
     Py_RETURN_NONE;
 }
 
@@ -448,7 +498,7 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define ADSA_ENTRY(name) {#name, (PyCFunction)(void *)entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ADSA_ENTRY(bind),          ADSA_ENTRY(rope_axes),     ADSA_ENTRY(paged_append),
                          ADSA_ENTRY(shared_prefix_attn), ADSA_ENTRY(norm_residual), ADSA_ENTRY(packed_attn),
-                         ADSA_ENTRY(chunk_attn),    {nullptr, nullptr, 0, nullptr}};
+                         ADSA_ENTRY(chunk_attn),    ADSA_ENTRY(sample),        {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "adsa_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
