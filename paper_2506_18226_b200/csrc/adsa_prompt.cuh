@@ -6,6 +6,19 @@
 
 namespace adsa {
 
+// Division of numbers below 2^31 by a divisor that the host knows.
+struct FastDiv {
+    uint32_t mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t d)
+    {
+        shift = 0;
+        while ((1ULL << shift) < d) ++shift;
+        mul = (uint32_t)(((1ULL << 32) * ((1ULL << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift); }
+};
+
 struct PromptArgs {
     const void *q, *k, *v;                  // k, v: packed rows, or the pools
     long long q_token, q_head, k_token, k_head, v_token, v_head;   // element strides (k, v: of packed rows)
@@ -21,7 +34,9 @@ struct PromptArgs {
     float scale_log2e;
     void *out;                              // 16-bit, or null
     float *out_f32, *lse;                   // or null
-    // workspace: what each run leaves for the merge, partial states [2 runs][256 rows][64 or 128] and their (m, l)
+    int half_tokens;                        // of an item's half: 128 / per_kv
+    FastDiv by_per_kv, by_page;
+    // workspace: what each run leaves for the merge, partial states [2 runs][16 or 32][256 rows][4 elements] and their (m, l)
     int4 *run_desc;
     float *state, *state_ml;
     int box_rows;                           // rows of a copy's box in a page; 0: K and V are copied row by row
@@ -80,41 +95,33 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b)
     return s;
 }
 constexpr int kTileRows = 128;               // query rows of a half item, cached rows of a tile
-constexpr int kTileOver = 2;                // what an item costs beside its tiles, in units
+constexpr unsigned kTileOver = 2;           // what an item costs beside its tiles, in units
 
-// An item: the query rows of `per` tokens (all query heads of one key head), in one half of up to 128 rows or in two.
-template <bool WIDE>
-struct TileItem {
-    int first, count, tiles;                // tokens; tiles of 128 cached rows (prefix, then own rows)
-    bool pair;                              // two halves
-    unsigned cost_tile;
-    __device__ __forceinline__ TileItem(const PromptArgs &a, const PromptSeq &s, int q);
-    __device__ __forceinline__ unsigned cost() const { return kTileOver + cost_tile * (unsigned)tiles; }
-};
-__device__ __forceinline__ int half_tokens(const PromptArgs &a) { return kTileRows / a.per_kv; }
-template <bool WIDE>
-__device__ __forceinline__ int item_tokens(const PromptArgs &a) { return WIDE ? half_tokens(a) : 2 * half_tokens(a); }
-template <bool WIDE>
-__device__ __forceinline__ int items_of(const PromptArgs &a, int m) { return (m + item_tokens<WIDE>(a) - 1) / item_tokens<WIDE>(a); }
-// tiles that the tokens up to i attend
+// An item: the query rows of a run of tokens (all query heads of one key head), in one half of up to 128 rows or in two.
+template <bool WIDE> __device__ __forceinline__ int item_tokens(const PromptArgs &a) { return WIDE ? a.half_tokens : 2 * a.half_tokens; }
+// tiles of 128 rows (prefix, then own rows) that the tokens up to i attend
 __device__ __forceinline__ int tiles_until(const PromptArgs &a, const PromptSeq &s, int i)
 {
     return (s.p + kTileRows - 1) / kTileRows + (s.seen(i, a.causal) + kTileRows - 1) / kTileRows;
 }
 template <bool WIDE>
-__device__ __forceinline__ TileItem<WIDE>::TileItem(const PromptArgs &a, const PromptSeq &s, int q)
-{
-    first = q * item_tokens<WIDE>(a);
-    count = min(s.m - first, item_tokens<WIDE>(a));
-    tiles = tiles_until(a, s, first + count - 1);
-    pair = !WIDE && count > half_tokens(a);
-    cost_tile = WIDE || pair ? 2u : 1u;
-}
+struct TileItem {
+    int first, count, tiles;                // tokens; tiles
+    bool pair;                              // two halves
+    __device__ __forceinline__ TileItem(const PromptArgs &a, const PromptSeq &s, int q) : first(q * item_tokens<WIDE>(a))
+    {
+        count = min(s.m - first, item_tokens<WIDE>(a));
+        tiles = tiles_until(a, s, first + count - 1);
+        pair = !WIDE && count > a.half_tokens;
+    }
+    __device__ __forceinline__ unsigned tile_cost() const { return WIDE || pair ? 2u : 1u; }
+    __device__ __forceinline__ unsigned cost() const { return kTileOver + tile_cost() * (unsigned)tiles; }
+};
 
 // the page that holds a row; one outside the pool is reported, and read as page 0 (the result is then unspecified)
 __device__ __forceinline__ int prompt_page(const PromptArgs &a, const int32_t *pages, int row)
 {
-    const int page = pages[row / a.page_rows];
+    const int page = pages[a.by_page(row)];
     if (page >= 0 && page < a.n_pages) return page;
     if (a.status) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
     return 0;
@@ -127,7 +134,7 @@ __device__ __forceinline__ size_t prompt_row(const PromptArgs &a, const PromptSe
     const int row = pre ? j : j - s.p;
     const int32_t *pages = pre ? a.p_table + (size_t)s.group * a.max_p_pages : a.table + (size_t)b * a.max_pages;
     const int page = prompt_page(a, pages, row);
-    return (((size_t)page * a.kv_heads + h) * a.page_rows + row % a.page_rows) * a.row_stride;
+    return (((size_t)page * a.kv_heads + h) * a.page_rows + row - a.by_page(row) * a.page_rows) * a.row_stride;
 }
 
 // One query row by one warp, as the formula has it: a cached row per lane for the scores, elements spread over the lanes for
@@ -136,7 +143,7 @@ template <typename T>
 __device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int b, int i, int head, int lane, int c0, int c1)
 {
     constexpr int PER = 2;                                   // pairs of elements a lane
-    const int h = head / a.per_kv, n = s.p + s.seen(i, a.causal);
+    const int h = a.by_per_kv(head), n = s.p + s.seen(i, a.causal);
     const T *q = (const T *)a.q + (s.q0 + i) * a.q_token + head * a.q_head;
     float m = -INFINITY, l = 0.f;
     float2 o[PER];

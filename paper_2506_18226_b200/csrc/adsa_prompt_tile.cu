@@ -49,10 +49,11 @@ struct TilePos {
     }
 };
 struct TileControl {
-    uint64_t bars[48];
-    uint32_t tmem;
+    uint64_t bars[40];
     TileDesc ring[kTileRing];
-    float2 ml[kTileRows];                   // (m, l) of group 1 where the groups take turns
+    TilePos begin, end;                     // of this block's run
+    uint32_t tmem;
+    int limit;                              // polls of a wait before it gives up
 };
 
 __device__ __forceinline__ void tile_tma3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
@@ -60,11 +61,11 @@ __device__ __forceinline__ void tile_tma3(uint32_t dst, const CUtensorMap *map, 
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tile_copy(uint32_t dst, const void *src, int bytes)
+template <int BYTES>
+__device__ __forceinline__ void tile_copy(uint32_t dst, const void *src)
 {
-    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 // where byte x of a row lies in a tile of 128-byte columns in the 128-byte swizzle
 __device__ __forceinline__ uint32_t tile_at(int row, int x, uint32_t sub)
@@ -80,7 +81,7 @@ __device__ __forceinline__ int piece_of(const void *p, long long token, long lon
 
 // The item that unit u of the list lies in, and the tile that a run beginning there takes first; by a whole warp.
 template <bool WIDE>
-__device__ TilePos tile_locate(const PromptArgs &a, const unsigned long long *plan, unsigned long long u, unsigned long long tol, int lane)
+__device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, unsigned u, unsigned tol, int lane)
 {
     if (u >= plan[a.batch]) return {a.batch, 0, 0, 0};
     int b = 0;
@@ -90,37 +91,37 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned long long *pl
         if (done < 32) break;
     }
     const PromptSeq s = prompt_seq(a, b);
-    const unsigned long long per_head = (plan[b + 1] - plan[b]) / (unsigned)a.kv_heads;
-    unsigned long long rem = u - plan[b];
+    const unsigned per_head = (plan[b + 1] - plan[b]) / (unsigned)a.kv_heads;
+    unsigned rem = u - plan[b];
     const int head = (int)(rem / per_head);
     rem -= head * per_head;
-    const int nq = items_of<WIDE>(a, s.m);
     for (int q0 = 0;; q0 += 32) {
-        const bool in = q0 + lane < nq;
+        const bool in = (q0 + lane) * item_tokens<WIDE>(a) < s.m;
         const TileItem<WIDE> mine(a, s, in ? q0 + lane : 0);
-        const unsigned long long cost = in ? mine.cost() : 0u;
-        unsigned long long incl = cost;
+        const unsigned cost = in ? mine.cost() : 0u;
+        unsigned incl = cost;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+        for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
         const unsigned past = __ballot_sync(0xffffffffu, incl > rem);
-        if (!past && q0 + 32 < nq) {
+        if (!past && (q0 + 32) * item_tokens<WIDE>(a) < s.m) {
             rem -= __shfl_sync(0xffffffffu, incl, 31);
             continue;
         }
-        const int at = past ? __ffs(past) - 1 : 31;         // (past is never empty: the plan counted the same items)
-        const unsigned long long item_cost = __shfl_sync(0xffffffffu, cost, at), off = rem - (__shfl_sync(0xffffffffu, incl, at) - item_cost);
+        const int at = past ? __ffs(past) - 1 : 31;         // (past is never empty here: the plan counted the same items)
+        const unsigned item_cost = __shfl_sync(0xffffffffu, cost, at), off = rem - (__shfl_sync(0xffffffffu, incl, at) - item_cost);
         const int tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
-        const unsigned ct = __shfl_sync(0xffffffffu, mine.cost_tile, at);
-        const unsigned long long left = item_cost - off;
+        const bool two = __shfl_sync(0xffffffffu, mine.tile_cost(), at) == 2u;
+        const unsigned left = item_cost - off;
         const bool near = min(off, left) <= tol;
-        int q = q0 + at, tile = near || off <= kTileOver ? 0 : (int)((off - kTileOver + ct - 1u) / ct);
+        int q = q0 + at, tile = near || off <= kTileOver ? 0 : (int)(two ? (off - kTileOver + 1u) / 2u : off - kTileOver);
         if (near ? off <= left : tile < tiles || tiles == 0) return {b, head, q, tile};
-        if (++q < nq) return {b, head, q, 0};
+        if (++q * item_tokens<WIDE>(a) < s.m) return {b, head, q, 0};
         return head + 1 < a.kv_heads ? TilePos{b, head + 1, 0, 0} : TilePos{b + 1, 0, 0, 0};
     }
 }
 
-template <typename T, int NSUB, int SLOTS>
+// STAGE: elements of an output row that a warp turns over in shared memory at a time
+template <typename T, int NSUB, int SLOTS, int STAGE>
 __global__ void __launch_bounds__(kTileThreads, 1)
 prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                    const __grid_constant__ CUtensorMap v_map)
@@ -128,14 +129,14 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     constexpr bool WIDE = NSUB > 2;
     constexpr int PARTS = WIDE ? 2 : 1, PSUB = NSUB / PARTS;   // a tile of K or V lies in PARTS slots of PSUB columns of 64 elements
     constexpr int DO = 64 * PSUB;                             // elements of O of a group
-    constexpr uint32_t kSub = kTileRows * 128, kSlot = PSUB * kSub, kQ = (WIDE ? 1 : 2) * NSUB * kSub;
+    constexpr uint32_t kSub = kTileRows * 128, kSlot = PSUB * kSub, kQ = (WIDE ? 1 : 2) * NSUB * kSub, kStage = 32 * STAGE * 2;
     constexpr float kBias = WideBias<T>::value;
     extern __shared__ unsigned char tile_smem[];
     const uint32_t base = (smem_u32(tile_smem) + 1023u) & ~1023u;
     const uint32_t q_at = base, ring = base + kQ;
-    unsigned char *const ctl = tile_smem + (base - smem_u32(tile_smem)) + kQ + (size_t)SLOTS * kSlot;
+    unsigned char *const stages = tile_smem + (base - smem_u32(tile_smem)) + kQ + (size_t)SLOTS * kSlot, *const ctl = stages + 8 * kStage;
     TileControl &c = *reinterpret_cast<TileControl *>(ctl);
-    unsigned long long *const plan = reinterpret_cast<unsigned long long *>(ctl + sizeof(TileControl));
+    unsigned *const plan = reinterpret_cast<unsigned *>(ctl + sizeof(TileControl));
     const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 16, s_full = q_empty + 16,
                    p_full = s_full + 16, o_full = p_full + 32, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8,
                    d_empty = d_full + 8 * kTileRing;
@@ -147,6 +148,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             mbar_init(q_full + 8 * g, 1); mbar_init(q_empty + 8 * g, 1); mbar_init(s_full + 8 * g, 1); mbar_init(o_full + 8 * g, 1);
             mbar_init(p_full + 16 * g, 4); mbar_init(p_full + 16 * g + 8, 4);
         }
+        c.limit = kCopySpinLimit;
         mbar_init(m_full, 4);
         mbar_init(m_empty, 4);
         for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 11); }
@@ -171,36 +173,55 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const int b = b0 + lane;
         PromptSeq s = {};
         if (b < a.batch) s = prompt_seq(a, b);
-        const int nq = items_of<WIDE>(a, s.m);
-        unsigned long long units = 0;
-        if (nq <= 4) {
-            for (int q = 0; q < nq; ++q) units += TileItem<WIDE>(a, s, q).cost();
+        const bool many = s.m > 32 * item_tokens<WIDE>(a);
+        unsigned units = 0;
+        if (!many) {
+            for (int q = 0; q * item_tokens<WIDE>(a) < s.m; ++q) units += TileItem<WIDE>(a, s, q).cost();
         }
-        for (unsigned todo = __ballot_sync(0xffffffffu, nq > 4); todo; todo &= todo - 1) {
+        for (unsigned todo = __ballot_sync(0xffffffffu, many); todo; todo &= todo - 1) {
             const int src = __ffs(todo) - 1;
             PromptSeq t = {};
             t.m = __shfl_sync(0xffffffffu, s.m, src);
             t.n = __shfl_sync(0xffffffffu, s.n, src);
             t.p = __shfl_sync(0xffffffffu, s.p, src);
-            const int many = items_of<WIDE>(a, t.m);
-            unsigned long long sum = 0;
-            for (int q = lane; q < many; q += 32) sum += TileItem<WIDE>(a, t, q).cost();
-#pragma unroll
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            unsigned sum = 0;
+            for (int q = lane; q * item_tokens<WIDE>(a) < t.m; q += 32) sum += TileItem<WIDE>(a, t, q).cost();
+            sum = __reduce_add_sync(0xffffffffu, sum);
             if (lane == src) units = sum;
         }
         if (b < a.batch) plan[b + 1] = units * (unsigned)a.kv_heads;
+    }
+    __syncthreads();
+    if (warp == 11) {
+        if (lane == 0) plan[0] = 0;
+        unsigned before = 0;
+        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+            unsigned incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+            if (b0 + lane < a.batch) plan[b0 + lane + 1] = before + incl;
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    __syncthreads();
+    const unsigned total = plan[a.batch], runs = min(max(a.split ? total / kTileMinRun : total, 1u), gridDim.x);
+    if (warp >= 10) {                                              // where this block's run begins and ends
+        const unsigned run = blockIdx.x + (warp - 10);
+        const unsigned u = run > runs ? total : (unsigned)((unsigned long long)run * total / runs);
+        const TilePos at = tile_locate<WIDE>(a, plan, u, a.split ? total / runs / 32u : 0xffffffffu, lane);
+        if (lane == 0) (warp == 10 ? c.begin : c.end) = at;
     }
     tc_before();
     __syncthreads();
     tc_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, c.tmem, 0);
 
-    int limit = kCopySpinLimit;
     const auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (!mbar_wait_bounded(bar, parity, limit)) {
-            limit = kCopySpinAfterTimeout;
-            if (a.status && lane == 0) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+        for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
+            if (polls < *(volatile int *)&c.limit) continue;
+            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short)
+            if (a.status) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+            break;
         }
     };
     int at = 0;                                                    // the next item of the ring
@@ -223,51 +244,36 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     // 168 registers a thread at the launch: the groups take what the other four warps leave
     if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 11) {                                              // ---- the list of items ----
-        if (lane == 0) plan[0] = 0;
-        __syncwarp();
-        unsigned long long before = 0;
-        for (int b0 = 0; b0 < a.batch; b0 += 32) {
-            unsigned long long incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
-            if (b0 + lane < a.batch) plan[b0 + lane + 1] = before + incl;
-            before += __shfl_sync(0xffffffffu, incl, 31);
-        }
-        __syncwarp();
         const unsigned run = blockIdx.x;
-        const unsigned long long most = max(a.split ? before / kTileMinRun : before, 1ULL), runs = min(most, (unsigned long long)gridDim.x);
-        int4 left = make_int4(-1, 0, 0, 0);                         // {sequence of the item that the last run to begin an item leaves
-                                                                   // unfinished, key head, item; whether an item cut before ends here}
-        if (run < runs) {
-            const unsigned long long tol = a.split ? before / runs / 32 : ~0ULL;
-            const TilePos end = tile_locate<WIDE>(a, plan, before * (run + 1) / runs, tol, lane);
-            TilePos pos = tile_locate<WIDE>(a, plan, before * run / runs, tol, lane);
-            int have = -1;
-            PromptSeq s = {};
-            while (pos.before(end)) {
-                if (pos.b != have) { s = prompt_seq(a, pos.b); have = pos.b; }
-                if (s.m == 0) { pos = {pos.b + 1, 0, 0, 0}; continue; }
-                const TileItem<WIDE> item(a, s, pos.q);
-                const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
-                const int t1 = last ? end.tile : item.tiles;
-                const bool whole = pos.tile == 0 && t1 == item.tiles;
-                if (!whole) {
-                    if (pos.tile > 0) left.w = t1 == item.tiles;
-                    else left = make_int4(pos.b, pos.head, pos.q, left.w);
-                }
-                wait(d_empty + 8 * at, d_phase ^ 1u);
-                if (lane == 0) {
-                    c.ring[at] = {s, pos.b, pos.head, pos.q, pos.tile, t1, whole ? -1 : (int)(2 * run) + (pos.tile > 0 ? 0 : 1)};
-                    mbar_arrive(d_full + 8 * at);
-                }
-                if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
-                if (last) break;
-                if (++pos.q >= items_of<WIDE>(a, s.m)) {
-                    pos.q = 0;
-                    if (++pos.head >= a.kv_heads) { pos.head = 0; ++pos.b; }
-                }
-                pos.tile = 0;
+        int4 left = make_int4(-1, 0, 0, 0);                         // {sequence of the item that this run begins and leaves unfinished, key
+                                                                   // head, item; whether an item cut before ends here}
+        const TilePos end = c.end;
+        TilePos pos = c.begin;
+        int have = -1;
+        PromptSeq s = {};
+        while (pos.before(end)) {
+            if (pos.b != have) { s = prompt_seq(a, pos.b); have = pos.b; }
+            if (s.m == 0) { pos = {pos.b + 1, 0, 0, 0}; continue; }
+            const TileItem<WIDE> item(a, s, pos.q);
+            const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
+            const int t1 = last ? end.tile : item.tiles;
+            const bool whole = pos.tile == 0 && t1 == item.tiles;
+            if (!whole) {
+                if (pos.tile > 0) left.w = t1 == item.tiles;
+                else left = make_int4(pos.b, pos.head, pos.q, left.w);
             }
+            wait(d_empty + 8 * at, d_phase ^ 1u);
+            if (lane == 0) {
+                c.ring[at] = {s, pos.b, pos.head, pos.q, pos.tile, t1, whole ? -1 : (int)(2 * run) + (pos.tile > 0 ? 0 : 1)};
+                mbar_arrive(d_full + 8 * at);
+            }
+            if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
+            if (last) break;
+            if (++pos.q * item_tokens<WIDE>(a) >= s.m) {
+                pos.q = 0;
+                if (++pos.head >= a.kv_heads) { pos.head = 0; ++pos.b; }
+            }
+            pos.tile = 0;
         }
         wait(d_empty + 8 * at, d_phase ^ 1u);
         if (lane == 0) {
@@ -288,6 +294,26 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 for (int i = waiting; i > 0; --i) mbar_arrive(full + 8 * (slot >= i ? slot - i : slot - i + SLOTS));
             waiting = 0;
         };
+        // row by row: a lane knows one row of 32, eight lanes copy one
+        const auto by_rows = [&](auto piece_, const TileDesc &it, bool pre, int row0, int x0, int valid, uint32_t dst, bool value) {
+            constexpr int piece = decltype(piece_)::value;
+            const unsigned char *src = (const unsigned char *)(value ? a.v : a.k);
+            const int bytes = min(2 * a.d - 2 * x0, PSUB * 128);
+#pragma unroll 1
+            for (int r0 = 0; r0 < valid; r0 += 32) {
+                unsigned long long off = 0;
+                if (r0 + lane < valid) off = 2ULL * prompt_row(a, it.s, it.b, it.head, (pre ? 0 : it.s.p) + row0 + r0 + lane, value) + 2ULL * x0;
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const int r = r0 + i + (lane >> 3);
+                    const unsigned char *from = src + __shfl_sync(0xffffffffu, off, i + (lane >> 3));
+                    if (r < valid) {
+#pragma unroll 1
+                        for (int x = (lane & 7) * piece; x < bytes; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x, kSub), from + x);
+                    }
+                }
+            }
+        };
         const auto copy = [&](const TileDesc &it, int t, bool value, int part) {   // a part of K or V of tile t into the next slot
             const int before = (it.s.p + kTileRows - 1) / kTileRows, valid = min(rows_of(it.s, t), kTileRows);
             const bool pre = t < before;
@@ -302,7 +328,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 __syncwarp();
                 for (int i = lane; i < boxes; i += 32) {
                     const int row = row0 + i * a.box_rows, page = prompt_page(a, pages, row);
-                    const int y = (page * a.kv_heads + it.head) * a.page_rows + row % a.page_rows;
+                    const int y = (page * a.kv_heads + it.head) * a.page_rows + row - a.by_page(row) * a.page_rows;
 #pragma unroll
                     for (int s = 0; s < PSUB; ++s)
                         pa_tma(dst + (uint32_t)(i * a.box_rows) * 128u + s * kSub, value ? &v_map : &k_map, x0 + s * 64, y, bar);
@@ -318,24 +344,10 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 }
                 __syncwarp();
             } else {
-                // row by row: a lane knows four rows, eight lanes copy one
-                const unsigned char *src = (const unsigned char *)(value ? a.v : a.k);
-                const int piece = value ? v_piece : k_piece, bytes = min(2 * a.d - 2 * x0, PSUB * 128);
-                unsigned long long off[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = lane + 32 * k;
-                    off[k] = r < valid ? 2ULL * prompt_row(a, it.s, it.b, it.head, (pre ? 0 : it.s.p) + row0 + r, value) + 2ULL * x0 : 0ULL;
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    for (int i = 0; i < 8 && 32 * k + 4 * i < valid; ++i) {
-                        const int r = 32 * k + 4 * i + (lane >> 3);
-                        const unsigned long long o = __shfl_sync(0xffffffffu, off[k], r & 31);
-                        if (r < valid)
-                            for (int x = (lane & 7) * piece; x < bytes; x += 8 * piece) tile_copy(dst + tile_at(r, x, kSub), src + o + x, piece);
-                    }
-                }
+                const int piece = value ? v_piece : k_piece;
+                if (piece == 16) by_rows(std::integral_constant<int, 16>(), it, pre, row0, x0, valid, dst, value);
+                else if (piece == 8) by_rows(std::integral_constant<int, 8>(), it, pre, row0, x0, valid, dst, value);
+                else by_rows(std::integral_constant<int, 4>(), it, pre, row0, x0, valid, dst, value);
                 ++waiting;
             }
             if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
@@ -345,37 +357,31 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (waiting && !mbar_try_wait(d_full + 8 * at, d_phase)) flush();
             if (!have_item()) break;
             const TileDesc &it = c.ring[at];
-            const bool turns = !WIDE && min(it.s.m - it.q * item_tokens<WIDE>(a), item_tokens<WIDE>(a)) <= half_tokens(a);
-            const int ahead = turns ? 2 : 1;
-            for (int t = it.t0; t < min(it.t0 + ahead, it.t1); ++t) {
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) copy(it, t, false, p);
-            }
-            for (int t = it.t0; t < it.t1; ++t) {
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) copy(it, t, true, p);
-                if (t + ahead < it.t1) {
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p) copy(it, t + ahead, false, p);
-                }
+            const bool turns = !WIDE && it.s.m - it.q * item_tokens<WIDE>(a) <= a.half_tokens;
+            const int ahead = turns ? 2 : 1, n = it.t1 - it.t0;
+#pragma unroll 1
+            for (int i = 0; i < 2 * n * PARTS; ++i) {
+                const int j = i / PARTS;                           // K of the first tiles; V and K in turn; V of the last
+                const bool value = j >= min(ahead, n) && (j >= 2 * n - ahead || ((j - ahead) & 1) == 0);
+                const int tile = !value ? (j < ahead ? j : (j - ahead) / 2 + ahead) : j >= 2 * n - ahead ? j - n : (j - ahead) / 2;
+                copy(it, it.t0 + tile, value, i % PARTS);
             }
             next_item();
         }
         if (waiting) flush();
     } else if (warp == 10) {                                       // ---- copies of Q ----
-        uint32_t phase[2] = {0, 0};
-        const int piece = piece_of(a.q, a.q_token, a.q_head, a.d), per_row = 2 * a.d / piece, tph = half_tokens(a);
+        uint32_t phase = 0;                                        // bit h: of half h
+        const int piece = piece_of(a.q, a.q_token, a.q_head, a.d), tph = a.half_tokens;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             if (it.t1 == it.t0) continue;
             const TileItem<WIDE> item(a, it.s, it.q);
-#pragma unroll
-            for (int h = 0; h < (WIDE ? 1 : 2); ++h) {
-                if (h == 1 && !item.pair) continue;
+#pragma unroll 1
+            for (int h = 0; h < (item.pair ? 2 : 1); ++h) {
                 const int tok = item.first + h * tph, tokens = min(item.count - h * tph, tph);
                 const uint32_t dst = q_at + (uint32_t)h * NSUB * kSub, bar = q_full + 8 * h;
-                wait(q_empty + 8 * h, phase[h] ^ 1u);
-                phase[h] ^= 1u;
+                wait(q_empty + 8 * h, (phase >> h & 1u) ^ 1u);
+                phase ^= 1u << h;
                 if (a.q_boxes) {
                     if (lane == 0) {
                         const int boxes = (a.d + 63) / 64, y = it.head * a.per_kv, z = (int)it.s.q0 + tok;
@@ -386,10 +392,19 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     __syncwarp();
                 } else {
                     const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + tok) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
-                    for (int i = lane; i < tokens * a.per_kv * per_row; i += 32) {
-                        const int r = i / per_row, x = (i - r * per_row) * piece, t = r / a.per_kv;
-                        tile_copy(dst + tile_at(r, x, kSub), src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head) + x, piece);
-                    }
+                    const auto by_rows = [&](auto piece_) {
+                        constexpr int piece = decltype(piece_)::value;
+#pragma unroll 1
+                        for (int r0 = 0; r0 < tokens * a.per_kv; r0 += 4) {
+                            const int r = r0 + (lane >> 3), t = a.by_per_kv(r);
+                            const unsigned char *from = src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head);
+                            if (r < tokens * a.per_kv)
+                                for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x, kSub), from + x);
+                        }
+                    };
+                    if (piece == 16) by_rows(std::integral_constant<int, 16>());
+                    else if (piece == 8) by_rows(std::integral_constant<int, 8>());
+                    else by_rows(std::integral_constant<int, 4>());
                     asm volatile("cp.async.wait_all;" ::: "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -401,7 +416,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;
         const uint32_t s_shape = tc_shape<T>(kTileRows, false);
         int slot = 0;
-        uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+        uint32_t phase = 0, q_phase = 0, p_phase = 0;               // (bit g: of group or half g)
         const auto take = [&]() {                                  // the next slot, once its tile is there
             wait(full + 8 * slot, phase);
             const int taken = slot;
@@ -421,7 +436,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             }
         };
         const auto take_v = [&](const TileDesc &it, int t) {                           // V of tile t, or a part of it
-            const int taken = take(), valid = rows_of(it.s, t);
+            const int taken = take(), valid = __shfl_sync(0xffffffffu, rows_of(it.s, t), 0);
             if (valid < kTileRows) {
                 // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN
                 const uint32_t v_at = ring + (uint32_t)taken * kSlot;
@@ -437,9 +452,9 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const auto weigh = [&](int g, int v_slot, bool first) {    // O += P V, once the group has left P
             const uint64_t vd = tc_operand(ring + (uint32_t)v_slot * kSlot, kSub);
             const uint32_t o_shape = tc_shape<T>(WIDE ? min(d_cols - g * DO, DO) : d_cols, true);
-#pragma unroll
+#pragma unroll 1
             for (int half = 0; half < 2; ++half) {                 // P comes in two halves: the first is used while the second is made
-                wait(p_full + 16 * g + 8 * half, p_phase[g]);
+                wait(p_full + 16 * g + 8 * half, p_phase >> g & 1u);
                 tc_after();
                 if (tc_elect()) {
 #pragma unroll
@@ -450,90 +465,64 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 }
                 __syncwarp();
             }
-            p_phase[g] ^= 1u;
+            p_phase ^= 1u << g;
         };
         const auto done = [&](uint32_t bar) {                      // counted when everything issued so far is complete
             if (tc_elect()) tc_commit(bar);
             __syncwarp();
         };
         const auto queries = [&](int h) {
-            wait(q_full + 8 * h, q_phase[h]);
-            q_phase[h] ^= 1u;
+            wait(q_full + 8 * h, q_phase >> h & 1u);
+            q_phase ^= 1u << h;
         };
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
-            const int n = it.t1 - it.t0;
+            // (shuffled, so that the compiler knows them to be uniform)
+            const int t0 = __shfl_sync(0xffffffffu, it.t0, 0), n = __shfl_sync(0xffffffffu, it.t1, 0) - t0;
             if (n == 0) continue;
             const TileItem<WIDE> item(a, it.s, it.q);
-            int k[PARTS], v[PARTS];
-            const auto take_k = [&]() {
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) k[p] = take();
-            };
-            const auto free_k = [&]() {
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) done(empty + 8 * k[p]);
-            };
+            const bool pair = __shfl_sync(0xffffffffu, (int)item.pair, 0);
             queries(0);
-            if (WIDE || item.pair) {
-                // the first half's tokens attend no more tiles than the second's
-                const int n0 = WIDE ? n : min(max(tiles_until(a, it.s, item.first + half_tokens(a) - 1) - it.t0, 0), n);
-                const uint32_t q1 = WIDE ? q_at : q_at + NSUB * kSub;
-                if (!WIDE) queries(1);
-                tc_after();
-                take_k();
-                if (n0 > 0) { score(0, k, q_at); done(s_full); }
-                if (!WIDE && n0 <= 1) done(q_empty);
-                score(1, k, q1);
-                free_k();
-                done(s_full + 8);
-                for (int i = 0; i < n; ++i) {
-                    const bool more = i + 1 < n;
+            if (pair) queries(1);
+            tc_after();
+            // Steps of the two groups in turn.  Each: O of a tile, for the group whose weights are due, then the scores of its next tile.  Where
+            // both groups take every tile, group 0 takes it and group 1 leaves it; else the group of the step does both.
+            const bool turns = !WIDE && !pair;
+            const int ahead = turns ? 2 : 1, steps = turns ? n + 2 : 2 * n + 2;
+            // the first half's tokens attend no more tiles than the second's
+            const int n0 = pair ? __shfl_sync(0xffffffffu, min(max(tiles_until(a, it.s, item.first + a.half_tokens - 1) - t0, 0), n), 0) : n;
+            int k[PARTS], v[PARTS];
+            if (n0 == 0) done(q_empty);
+#pragma unroll 1
+            for (int step = 0; step < steps; ++step) {
+                const int g = step & 1, i = turns ? step : step >> 1, mine = g == 0 ? n0 : n, j = i - ahead;   // scores of tile i, O of tile j
+                const bool takes = turns || g == 0, leaves = turns || g == 1;
+                if (j >= 0) {
+                    if (takes) {
 #pragma unroll
-                    for (int p = 0; p < PARTS; ++p) v[p] = take_v(it, it.t0 + i);
-                    if (i < n0) weigh(0, v[0], i == 0);
-                    if (i == n0 - 1) done(o_full);
-                    if (more) {
-                        take_k();
-                        if (i + 1 < n0) {
-                            score(0, k, q_at);
-                            done(s_full);
-                            if (!WIDE && i + 2 == n0) done(q_empty);
-                        }
+                        for (int p = 0; p < PARTS; ++p) v[p] = take_v(it, t0 + j);
                     }
-                    if (WIDE) done(empty + 8 * v[0]);
-                    weigh(1, v[PARTS - 1], i == 0);
-                    done(empty + 8 * v[PARTS - 1]);
-                    if (more) {
-                        score(1, k, q1);
-                        free_k();
-                        done(s_full + 8);
+                    if (j < mine) {
+                        weigh(g, WIDE && g == 1 ? v[PARTS - 1] : v[0], j < ahead);
+                        if (j + ahead >= mine) done(o_full + 8 * g);           // that was the group's last
                     }
-                    if (i + 2 == n || n == 1) done(q_empty + (WIDE ? 0 : 8));   // the last scores are issued
-                    if (!more) done(o_full + 8);
+                    if (WIDE) done(empty + 8 * (g == 1 ? v[PARTS - 1] : v[0]));
+                    else if (leaves) done(empty + 8 * v[0]);
                 }
-            } else {
-                tc_after();
-                for (int g = 0; g < min(2, n); ++g) {
-                    take_k();
-                    score(g, k, q_at);
-                    free_k();
-                    done(s_full + 8 * g);
-                }
-                if (n <= 2) done(q_empty);
-                for (int i = 0; i < n; ++i) {
-                    const int g = i & 1;
-                    v[0] = take_v(it, it.t0 + i);
-                    weigh(g, v[0], i < 2);
-                    done(empty + 8 * v[0]);
-                    if (i + 2 < n) {
-                        take_k();
-                        score(g, k, q_at);
-                        free_k();
+                if (i < n) {
+                    if (takes) {
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) k[p] = take();
+                    }
+                    if (i < mine) {
+                        score(g, k, pair && g == 1 ? q_at + NSUB * kSub : q_at);
                         done(s_full + 8 * g);
-                        if (i + 3 == n) done(q_empty);
-                    } else {
-                        done(o_full + 8 * g);
+                        // the last scores that read this half of Q
+                        if (pair ? i + 1 == mine : i + 1 == n && leaves) done(q_empty + (pair ? 8 * g : 0));
+                    }
+                    if (leaves) {
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) done(empty + 8 * k[p]);
                     }
                 }
             }
@@ -543,13 +532,13 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const int g = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
         const uint32_t my_s = s_full + 8 * g, my_p = p_full + 16 * g, my_o = o_full + 8 * g;
-        const int tph = half_tokens(a), heads = a.kv_heads * a.per_kv;
+        const int tph = a.half_tokens, heads = a.kv_heads * a.per_kv;
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<WIDE> item(a, it.s, it.q);
             const bool turns = !WIDE && !item.pair;                // the groups take the tiles in turns
-            const int half = item.pair ? g : 0, in = row / a.per_kv, tok = item.first + half * tph + in, head = it.head * a.per_kv + row - in * a.per_kv;
+            const int half = item.pair ? g : 0, in = a.by_per_kv(row), tok = item.first + half * tph + in, head = it.head * a.per_kv + row - in * a.per_kv;
             const bool there = in < tph && in + half * tph < item.count;
             const int own = it.s.seen(min(tok, it.s.m - 1), a.causal), before = (it.s.p + kTileRows - 1) / kTileRows;
             const bool warp_there = __any_sync(0xffffffffu, there);
@@ -632,7 +621,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             bool both = false;
             if (turns) {
                 if (g == 1) {
-                    c.ml[row] = make_float2(m2, l);
+                    reinterpret_cast<float2 *>(stages + warp * kStage)[lane] = make_float2(m2, l);
                     tc_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(m_full);
@@ -646,7 +635,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 tc_after();
                 both = it.t1 - it.t0 > 1;
                 if (both) {
-                    const float2 other = c.ml[row];
+                    const float2 other = reinterpret_cast<const float2 *>(stages + (warp + 4) * kStage)[lane];
                     const float M = fmaxf(m2, other.x);
                     w0 = m2 == -INFINITY ? 0.f : pa_exp2(m2 - M);
                     w1 = other.x == -INFINITY ? 0.f : pa_exp2(other.x - M);
@@ -659,65 +648,101 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const float inv = 1.f / l;
             if (!partial && none) w0 = w1 = 0.f;
             else if (!partial) { w0 *= inv; w1 *= inv; }
-            const size_t at_row = ((size_t)it.s.q0 + tok) * heads + head, at_slot = (size_t)it.slot * 256 + (WIDE ? g * 128 : half * 128) + row;
+            const int at_row = there ? (int)((it.s.q0 + tok) * heads + head) : -1;   // (rows of a call are below 2^31)
+            const size_t at_slot = (size_t)it.slot * 256 + (WIDE ? g * 128 : half * 128) + row;
             float2 bad = make_float2(0.f, 0.f);
             if (warp_there) {
-#pragma unroll 1
-                for (int x = 0; x < DO; x += 16) {
-                    if (c0 + x >= c1 && !partial) break;
-                    float o[16];
+                const auto load = [&](int x, float (&o)[32]) {     // 32 elements of the row's output, or of its state
                     if (tiles > 0) {
-                        tc_load16(o_col + x, o);
+                        tc_load32(o_col + x, o);
                         tc_load_wait();
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] *= w0;
+                        for (int k = 0; k < 32; ++k) o[k] *= w0;
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = 0.f;
+                        for (int k = 0; k < 32; ++k) o[k] = 0.f;
                     }
                     if (both) {
-                        float o1[16];
-                        tc_load16(tmem + 384 + lanes + x, o1);
+                        float o1[32];
+                        tc_load32(tmem + 384 + lanes + x, o1);
                         tc_load_wait();
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = fmaf(o1[k], w1, o[k]);
+                        for (int k = 0; k < 32; ++k) o[k] = fmaf(o1[k], w1, o[k]);
                     }
-                    if (there && partial) {
+                };
+                if (partial) {
+#pragma unroll 1
+                    for (int x = 0; x < DO; x += 32) {
+                        float o[32];
+                        load(x, o);
+                        if (there) {
 #pragma unroll
-                        for (int k = 0; k < 16; k += 4)
-                            *reinterpret_cast<float4 *>(a.state + at_slot * DO + x + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-                    } else if (there) {
-                        const int cols = min(16, c1 - c0 - x);
-                        if (none) {
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = 0.f;
+                            for (int k = 0; k < 32; k += 4)        // neighbouring rows lie next to each other
+                                *reinterpret_cast<float4 *>(a.state + ((at_slot >> 8) * (DO / 4) + (x + k) / 4) * 1024 + (at_slot & 255) * 4) =
+                                    make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                         }
+                        __syncwarp();
+                    }
+                    if (there) *reinterpret_cast<float2 *>(a.state_ml + 2 * at_slot) = make_float2(m2, l);
+                } else {
+                    const uint32_t stage = smem_u32(stages) + warp * kStage;
+                    const bool wide_out = a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0;
+#pragma unroll 1
+                    for (int x0 = 0; x0 < c1 - c0; x0 += STAGE) {
+#pragma unroll 1
+                        for (int x = 0; x < STAGE && x0 + x < c1 - c0; x += 32) {
+                            float o[32];
+                            load(x0 + x, o);
+                            if (none) {
 #pragma unroll
-                        for (int k = 0; k < 16; k += 2)
-                            if (k < cols) bad = fma2(make_float2(o[k], o[k + 1]), make_float2(0.f, 0.f), bad);
-                        if (a.out) {
-                            T *dst = (T *)a.out + at_row * a.d + c0 + x;
-                            if (cols == 16 && ((uintptr_t)dst & 15) == 0) {
+                                for (int k = 0; k < 32; ++k) o[k] = 0.f;
+                            }
+                            const int cols = c1 - c0 - x0 - x;
 #pragma unroll
-                                for (int k = 0; k < 16; k += 8)
-                                    *reinterpret_cast<uint4 *>(dst + k) =
-                                        make_uint4(pack2<T>(o[k], o[k + 1]), pack2<T>(o[k + 2], o[k + 3]), pack2<T>(o[k + 4], o[k + 5]), pack2<T>(o[k + 6], o[k + 7]));
-                            } else {
+                            for (int k = 0; k < 32; k += 2)
+                                if (k < cols) bad = fma2(make_float2(o[k], o[k + 1]), make_float2(0.f, 0.f), bad);
+                            if (a.out_f32 && there) {
 #pragma unroll
-                                for (int k = 0; k < 16; k += 2)
-                                    if (k < cols) *reinterpret_cast<uint32_t *>(dst + k) = pack2<T>(o[k], o[k + 1]);
+                                for (int k = 0; k < 32; k += 2)
+                                    if (k < cols) *reinterpret_cast<float2 *>(a.out_f32 + (size_t)at_row * a.d + c0 + x0 + x + k) = make_float2(o[k], o[k + 1]);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; k += 8)
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
+                                             ::"r"(stage + (uint32_t)(lane * STAGE * 2) + (uint32_t)((((x + k) / 8) ^ (lane & (STAGE / 8 - 1))) << 4)),
+                                             "r"(pack2<T>(o[k], o[k + 1])), "r"(pack2<T>(o[k + 2], o[k + 3])), "r"(pack2<T>(o[k + 4], o[k + 5])),
+                                             "r"(pack2<T>(o[k + 6], o[k + 7])) : "memory");
+                        }
+                        __syncwarp();
+                        if (a.out && wide_out) {                   // 16 bytes a lane, STAGE / 8 lanes a row
+                            constexpr int LANES = STAGE / 8;
+#pragma unroll 4
+                            for (int i = 0; i < 32; i += 32 / LANES) {
+                                const int r = i + lane / LANES, ch = lane % LANES, to = __shfl_sync(0xffffffffu, at_row, r);
+                                if (to >= 0 && c0 + x0 + ch * 8 < c1) {
+                                    uint4 w;
+                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                                                 : "r"(stage + (uint32_t)(r * STAGE * 2) + (uint32_t)((ch ^ (r & (LANES - 1))) << 4)) : "memory");
+                                    *reinterpret_cast<uint4 *>((T *)a.out + (size_t)to * a.d + c0 + x0 + ch * 8) = w;
+                                }
+                            }
+                        } else if (a.out) {                        // 4 bytes a lane, STAGE / 2 lanes a row
+                            constexpr int LANES = STAGE / 2;
+#pragma unroll 2
+                            for (int i = 0; i < 32; i += 32 / LANES) {
+                                const int r = i + lane / LANES, e = 2 * (lane % LANES), to = __shfl_sync(0xffffffffu, at_row, r);
+                                if (to >= 0 && c0 + x0 + e < c1) {
+                                    uint32_t w;
+                                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w)
+                                                 : "r"(stage + (uint32_t)(r * STAGE * 2) + (uint32_t)(((e / 8) ^ (r & (STAGE / 8 - 1))) << 4) + (uint32_t)(e % 8) * 2u) : "memory");
+                                    *reinterpret_cast<uint32_t *>((T *)a.out + (size_t)to * a.d + c0 + x0 + e) = w;
+                                }
                             }
                         }
-                        if (a.out_f32) {
-#pragma unroll
-                            for (int k = 0; k < 16; k += 2)
-                                if (k < cols) *reinterpret_cast<float2 *>(a.out_f32 + at_row * a.d + c0 + x + k) = make_float2(o[k], o[k + 1]);
-                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    if (there && a.lse && c0 == 0) a.lse[at_row] = none ? -INFINITY : (m2 + log2f(l)) * 0.693147180559945309f;
                 }
-                if (there && partial) *reinterpret_cast<float2 *>(a.state_ml + 2 * at_slot) = make_float2(m2, l);
-                if (there && !partial && a.lse && c0 == 0) a.lse[at_row] = none ? -INFINITY : (m2 + log2f(l)) * 0.693147180559945309f;
             }
             tc_before();                                           // read before the next item's products write O
             if (turns) {
@@ -757,7 +782,7 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     if (d.x < 0) return;
     const PromptSeq s = prompt_seq(a, d.x);
     const TileItem<WIDE> item(a, s, d.z);
-    const int half = r >> 7, tph = half_tokens(a), in = (r & 127) / a.per_kv, in_item = in + (WIDE ? 0 : half * tph);
+    const int half = r >> 7, tph = a.half_tokens, in = a.by_per_kv(r & 127), in_item = in + (WIDE ? 0 : half * tph);
     if (in >= tph || in_item >= item.count || (half && !WIDE && !item.pair)) return;
     int pieces = 2;
     while (lead + pieces < runs && !a.run_desc[lead + pieces - 1].w) ++pieces;
@@ -773,10 +798,12 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
             const int i = i0 + k;
             ml[k] = make_float2(-INFINITY, 0.f);
             if (i < pieces) {
-                const size_t slot = ((size_t)2 * (lead + i) + (i == 0 ? 1 : 0)) * 256 + r;
-                ml[k] = *reinterpret_cast<const float2 *>(a.state_ml + 2 * slot);
-#pragma unroll
-                for (int e = 0; e < PER; e += 2) *reinterpret_cast<float2 *>(&x[k][e]) = *reinterpret_cast<const float2 *>(a.state + slot * DO + e * 32 + 2 * lane);
+                const size_t slot = (size_t)2 * (lead + i) + (i == 0 ? 1 : 0);
+                ml[k] = *reinterpret_cast<const float2 *>(a.state_ml + 2 * (slot * 256 + r));
+                // a lane has PER neighbouring elements
+                const float *from = a.state + (slot * (DO / 4) + lane * PER / 4) * 1024 + r * 4 + lane * PER % 4;
+                if constexpr (PER == 4) *reinterpret_cast<float4 *>(x[k]) = *reinterpret_cast<const float4 *>(from);
+                else *reinterpret_cast<float2 *>(x[k]) = *reinterpret_cast<const float2 *>(from);
             }
         }
 #pragma unroll
@@ -796,7 +823,7 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     bool bad = false;
 #pragma unroll
     for (int e = 0; e < PER; e += 2) {
-        const int at = c0 + e * 32 + 2 * lane;
+        const int at = c0 + lane * PER + e;
         if (at >= c1) continue;
         const float2 x = none ? make_float2(0.f, 0.f) : make_float2(o[e] * inv, o[e + 1] * inv);
         bad = bad || !(fabsf(x.x) <= FLT_MAX) || !(fabsf(x.y) <= FLT_MAX);
@@ -866,19 +893,18 @@ bool page_map(CUtensorMap *m, int dtype, const PromptArgs &a, const void *pool, 
     return encode(m, dtype, 2, pool, dims, strides, box);
 }
 
-template <typename T, int NSUB, int SLOTS>
-cudaError_t launch_tiles(const PromptArgs &a, unsigned runs, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+template <typename T, int NSUB, int SLOTS, int STAGE>
+cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
     constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
-    constexpr size_t most = 227 * 1024;
-    static_assert(sizeof(TileControl) % 8 == 0 && 2 * SLOTS + 28 <= 48, "control block");
-    static_assert(1024 + q + SLOTS * slot + sizeof(TileControl) <= most, "shared memory");
-    const size_t smem = 1024 + q + SLOTS * slot + sizeof(TileControl) + (size_t)(a.batch + 1) * 8;
-    if (smem > most) {                                             // the list of a large batch takes the room of a slot
-        if constexpr (SLOTS == 5) return launch_tiles<T, NSUB, SLOTS - 1>(a, runs, qm, km, vm, st);
+    constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * STAGE * 2 + sizeof(TileControl), most = 227 * 1024;
+    static_assert(2 * SLOTS + 22 <= 40, "barriers");
+    const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
+    if (smem > most) {                                             // the list of a large batch takes half the room of the outputs
+        if constexpr (STAGE == 64) return launch_tiles<T, NSUB, SLOTS, 32>(a, blocks, qm, km, vm, st);
         return cudaErrorInvalidValue;
     }
-    const auto kern = prompt_tile_kernel<T, NSUB, SLOTS>;
+    const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, STAGE>;
     static int told[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -889,16 +915,16 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned runs, const CUtensorMap &
         if (e != cudaSuccess) return e;
         if (known) __atomic_store_n(&told[dev], 1, __ATOMIC_RELEASE);
     }
-    e = launch_pdl(kern, dim3(runs), kTileThreads, smem, st, a, qm, km, vm);
-    if (e != cudaSuccess || !a.split || runs < 2) return e;
-    return launch_pdl(prompt_tile_merge_kernel<T, NSUB>, dim3(runs - 1, 256 / (kTileMergeThreads / 32)), kTileMergeThreads, 0, st, a, (int)runs);
+    e = launch_pdl(kern, dim3(blocks), kTileThreads, smem, st, a, qm, km, vm);
+    if (e != cudaSuccess || !a.split || blocks < 2) return e;
+    return launch_pdl(prompt_tile_merge_kernel<T, NSUB>, dim3(blocks - 1, 256 / (kTileMergeThreads / 32)), kTileMergeThreads, 0, st, a, (int)blocks);
 }
 template <typename T>
-cudaError_t launch_tiles_type(const PromptArgs &a, unsigned runs, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+cudaError_t launch_tiles_type(const PromptArgs &a, unsigned blocks, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
-    if (a.d <= 64) return launch_tiles<T, 1, 10>(a, runs, qm, km, vm, st);
-    if (a.d <= 128) return launch_tiles<T, 2, 5>(a, runs, qm, km, vm, st);
-    return launch_tiles<T, 4, 5>(a, runs, qm, km, vm, st);
+    if (a.d <= 64) return launch_tiles<T, 1, 8, 64>(a, blocks, qm, km, vm, st);
+    if (a.d <= 128) return launch_tiles<T, 2, 4, 64>(a, blocks, qm, km, vm, st);
+    return launch_tiles<T, 4, 4, 64>(a, blocks, qm, km, vm, st);
 }
 
 }  // namespace
@@ -906,6 +932,9 @@ cudaError_t launch_tiles_type(const PromptArgs &a, unsigned runs, const CUtensor
 cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cudaStream_t st)
 {
     PromptArgs a = args;
+    a.half_tokens = kTileRows / a.per_kv;
+    a.by_per_kv = FastDiv((uint32_t)a.per_kv);
+    a.by_page = FastDiv((uint32_t)max(a.page_rows, 1));
     CUtensorMap qm = {}, km = {}, vm = {};
     const int heads = a.kv_heads * a.per_kv;
     bool tf = false;
