@@ -40,7 +40,8 @@ struct PromptArgs {
     int4 *run_desc;
     float *state, *state_ml;
     int box_rows;                           // rows of a copy's box in a page; 0: K and V are copied row by row
-    int q_boxes, tokens_first;              // q, and packed k and v, by boxes; their maps' order: bit 0 q, 1 k, 2 v: tokens before heads
+    int q_boxes, tokens_first;              // q by boxes; the order in the maps of packed k (bit 1) and v (bit 2): tokens before heads
+    int shifted;                            // packed k and v by boxes that begin up to 7 elements before a head's row
     int split;                              // items may be cut (into partial states)
 };
 

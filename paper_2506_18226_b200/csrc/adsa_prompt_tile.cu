@@ -49,7 +49,7 @@ struct TilePos {
     }
 };
 struct TileControl {
-    uint64_t bars[40];
+    uint64_t bars[42];
     TileDesc ring[kTileRing];
     TilePos begin, end;                     // of this block's run
     uint32_t tmem;
@@ -71,6 +71,12 @@ __device__ __forceinline__ void tile_copy(uint32_t dst, const void *src)
 __device__ __forceinline__ uint32_t tile_at(int row, int x, uint32_t sub)
 {
     return (uint32_t)(x >> 7) * sub + (uint32_t)row * 128u + (uint32_t)((((x >> 4) & 7) ^ (row & 7)) << 4) + (uint32_t)(x & 15);
+}
+__device__ __forceinline__ float tile_max3(float x, float y, float z)
+{
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+    return m;
 }
 // largest of 16, 8, 4 bytes that divides all of these
 __device__ __forceinline__ int piece_of(const void *p, long long token, long long head, int d)
@@ -138,7 +144,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     TileControl &c = *reinterpret_cast<TileControl *>(ctl);
     unsigned *const plan = reinterpret_cast<unsigned *>(ctl + sizeof(TileControl));
     const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 16, s_full = q_empty + 16,
-                   p_full = s_full + 16, o_full = p_full + 32, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8,
+                   p_full = s_full + 16, o_full = p_full + 64, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8,
                    d_empty = d_full + 8 * kTileRing;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
 
@@ -146,7 +152,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         for (int i = 0; i < SLOTS; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int g = 0; g < 2; ++g) {
             mbar_init(q_full + 8 * g, 1); mbar_init(q_empty + 8 * g, 1); mbar_init(s_full + 8 * g, 1); mbar_init(o_full + 8 * g, 1);
-            mbar_init(p_full + 16 * g, 4); mbar_init(p_full + 16 * g + 8, 4);
+            for (int i = 0; i < 4; ++i) mbar_init(p_full + 32 * g + 8 * i, 4);
         }
         c.limit = kCopySpinLimit;
         mbar_init(m_full, 4);
@@ -235,6 +241,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         wait(d_full + 8 * at, d_phase);
         return c.ring[at].t1 >= 0;
     };
+    // where the elements of a head's row begin in a tile of K or V
+    const auto shift_of = [&](int head, bool value) { return a.shifted ? (int)(head * (value ? a.v_head : a.k_head)) & 7 : 0; };
     // cached rows of tile t, from its first row on
     const auto rows_of = [&](const PromptSeq &s, int t) {
         const int before = (s.p + kTileRows - 1) / kTileRows;
@@ -242,7 +250,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     };
 
     // 168 registers a thread at the launch: the groups take what the other four warps leave
-    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {                                              // ---- the list of items ----
         const unsigned run = blockIdx.x;
         int4 left = make_int4(-1, 0, 0, 0);                         // {sequence of the item that this run begins and leaves unfinished, key
@@ -336,11 +344,13 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             } else if (a.box_rows) {
                 if (lane == 0) {
                     mbar_expect_tx(bar, kSlot);
-                    const int tok = (int)it.s.k0 + row0;
+                    const int tok = (int)it.s.k0 + row0, shift = shift_of(it.head, value);
                     const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
 #pragma unroll
-                    for (int s = 0; s < PSUB; ++s)
-                        tile_tma3(dst + s * kSub, value ? &v_map : &k_map, x0 + s * 64, tf ? tok : it.head, tf ? it.head : tok, bar);
+                    for (int s = 0; s < PSUB; ++s) {
+                        if (a.shifted) pa_tma(dst + s * kSub, value ? &v_map : &k_map, (int)(it.head * (value ? a.v_head : a.k_head)) - shift + s * 64, tok, bar);
+                        else tile_tma3(dst + s * kSub, value ? &v_map : &k_map, x0 + s * 64, tf ? tok : it.head, tf ? it.head : tok, bar);
+                    }
                 }
                 __syncwarp();
             } else {
@@ -371,7 +381,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         if (waiting) flush();
     } else if (warp == 10) {                                       // ---- copies of Q ----
         uint32_t phase = 0;                                        // bit h: of half h
-        const int piece = piece_of(a.q, a.q_token, a.q_head, a.d), tph = a.half_tokens;
+        const int q_piece = piece_of(a.q, a.q_token, a.q_head, a.d), tph = a.half_tokens;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             if (it.t1 == it.t0) continue;
@@ -392,6 +402,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     __syncwarp();
                 } else {
                     const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + tok) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
+                    const int shift = shift_of(it.head, false), piece = shift ? min(q_piece, (2 * shift) & -(2 * shift)) : q_piece;
                     const auto by_rows = [&](auto piece_) {
                         constexpr int piece = decltype(piece_)::value;
 #pragma unroll 1
@@ -399,9 +410,16 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                             const int r = r0 + (lane >> 3), t = a.by_per_kv(r);
                             const unsigned char *from = src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head);
                             if (r < tokens * a.per_kv)
-                                for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x, kSub), from + x);
+                                for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x + 2 * shift, kSub), from + x);
                         }
                     };
+                    if (a.shifted) {                               // what K has beside the head's elements meets zeros
+                        const int end = (a.d + shift + 15) / 16 * 16;
+                        for (int r = lane; r < kTileRows; r += 32) {
+                            for (int x = shift > 0 ? 0 : a.d; x < end; x = x + 2 == shift ? shift + a.d : x + 2)
+                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + tile_at(r, 2 * x, kSub)), "r"(0u) : "memory");
+                        }
+                    }
                     if (piece == 16) by_rows(std::integral_constant<int, 16>());
                     else if (piece == 8) by_rows(std::integral_constant<int, 8>());
                     else by_rows(std::integral_constant<int, 4>());
@@ -413,7 +431,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             }
         }
     } else if (warp == 9) {                                        // ---- products ----
-        const int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;
+        int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;       // (of this head's place in K; in V)
         const uint32_t s_shape = tc_shape<T>(kTileRows, false);
         int slot = 0;
         uint32_t phase = 0, q_phase = 0, p_phase = 0;               // (bit g: of group or half g)
@@ -453,13 +471,13 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const uint64_t vd = tc_operand(ring + (uint32_t)v_slot * kSlot, kSub);
             const uint32_t o_shape = tc_shape<T>(WIDE ? min(d_cols - g * DO, DO) : d_cols, true);
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {                 // P comes in two halves: the first is used while the second is made
-                wait(p_full + 16 * g + 8 * half, p_phase >> g & 1u);
+            for (int part = 0; part < 4; ++part) {                 // P comes in quarters: one is used while the next is made
+                wait(p_full + 32 * g + 8 * part, p_phase >> g & 1u);
                 tc_after();
                 if (tc_elect()) {
 #pragma unroll
-                    for (int k = 0; k < kTileRows / 32; ++k) {
-                        const int ks = half * (kTileRows / 32) + k;
+                    for (int k = 0; k < kTileRows / 64; ++k) {
+                        const int ks = part * (kTileRows / 64) + k;
                         tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, !first || ks > 0);
                     }
                 }
@@ -482,6 +500,10 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (n == 0) continue;
             const TileItem<WIDE> item(a, it.s, it.q);
             const bool pair = __shfl_sync(0xffffffffu, (int)item.pair, 0);
+            if (a.shifted) {
+                k_steps = __shfl_sync(0xffffffffu, (a.d + shift_of(it.head, false) + 15) / 16, 0);
+                d_cols = __shfl_sync(0xffffffffu, (a.d + shift_of(it.head, true) + 15) / 16, 0) * 16;
+            }
             queries(0);
             if (pair) queries(1);
             tc_after();
@@ -528,10 +550,10 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             }
         }
     } else {                                                       // ---- a query row per thread ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int g = warp >> 2, row = tid & 127;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
-        const uint32_t my_s = s_full + 8 * g, my_p = p_full + 16 * g, my_o = o_full + 8 * g;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col0 = tmem + 256 + g * 128 + lanes;
+        const uint32_t my_s = s_full + 8 * g, my_p = p_full + 32 * g, my_o = o_full + 8 * g;
         const int tph = a.half_tokens, heads = a.kv_heads * a.per_kv;
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
         for (; have_item(); next_item()) {
@@ -555,10 +577,10 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 tc_after();
                 if (!warp_there) {
                     tc_before();
-                    if (lane == 0) { mbar_arrive(my_p); mbar_arrive(my_p + 8); }
+                    if (lane < 4) mbar_arrive(my_p + 8 * lane);
                     continue;
                 }
-                float v[kTileRows];
+                alignas(8) float v[kTileRows];
 #pragma unroll
                 for (int x = 0; x < kTileRows; x += 32) tc_load32(s_col + x, *reinterpret_cast<float (*)[32]>(v + x));
                 tc_load_wait();
@@ -568,8 +590,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 }
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int x = 0; x < kTileRows; ++x) mx4[x & 3] = fmaxf(mx4[x & 3], v[x]);
-                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+                for (int x = 0; x < kTileRows; x += 2) mx4[x / 2 & 3] = tile_max3(mx4[x / 2 & 3], v[x], v[x + 1]);
+                const float mx = fmaxf(tile_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
                 const bool move = (mx - m) * a.scale_log2e > kTileSlack || m == -INFINITY;
                 if (__any_sync(0xffffffffu, move)) {
                     const float m_new = move ? fmaxf(m, mx) : m;
@@ -581,11 +603,11 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 #pragma unroll 1
                         for (int x = 0; x < DO; x += 16) {
                             float o[16];
-                            tc_load16(o_col + x, o);
+                            tc_load16(o_col0 + x, o);
                             tc_load_wait();
 #pragma unroll
                             for (int k = 0; k < 16; ++k) o[k] *= corr;
-                            tc_store16f(o_col + x, o);
+                            tc_store16f(o_col0 + x, o);
                         }
                     }
                 }
@@ -603,12 +625,10 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                         p[k] = pack2<T>(w.x, w.y);
                     }
                     tc_store16(s_col + x / 2, p);                  // over scores that are in registers by now
-                    if (x % 64 == 32) {
-                        tc_store_wait();
-                        tc_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(my_p + 8 * (x / 64));
-                    }
+                    tc_store_wait();
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(my_p + 8 * (x / 32));
                 }
             }
             if (tiles > 0) {
@@ -652,28 +672,35 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const size_t at_slot = (size_t)it.slot * 256 + (WIDE ? g * 128 : half * 128) + row;
             float2 bad = make_float2(0.f, 0.f);
             if (warp_there) {
-                const auto load = [&](int x, float (&o)[32]) {     // 32 elements of the row's output, or of its state
+                const uint32_t shift = (uint32_t)shift_of(it.head, true), o_col = o_col0 + shift;
+                // 32 elements of the row's output, or of its state; zeros where the 16 columns lie past the head's elements
+                const auto load = [&](int x, float (&o)[32]) {
+                    const bool second = x + 16 < c1 - c0;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = 0.f;
                     if (tiles > 0) {
-                        tc_load32(o_col + x, o);
+                        tc_load16(o_col + x, *reinterpret_cast<float (*)[16]>(o));
+                        if (second) tc_load16(o_col + x + 16, *reinterpret_cast<float (*)[16]>(o + 16));
                         tc_load_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] *= w0;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = 0.f;
+                        for (int k = 0; k < 32; k += 2) *reinterpret_cast<float2 *>(o + k) = mul2(*reinterpret_cast<float2 *>(o + k), make_float2(w0, w0));
                     }
                     if (both) {
-                        float o1[32];
-                        tc_load32(tmem + 384 + lanes + x, o1);
+                        alignas(8) float o1[32];
+#pragma unroll
+                        for (int k = 16; k < 32; ++k) o1[k] = 0.f;
+                        tc_load16(tmem + 384 + lanes + shift + x, *reinterpret_cast<float (*)[16]>(o1));
+                        if (second) tc_load16(tmem + 384 + lanes + shift + x + 16, *reinterpret_cast<float (*)[16]>(o1 + 16));
                         tc_load_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = fmaf(o1[k], w1, o[k]);
+                        for (int k = 0; k < 32; k += 2)
+                            *reinterpret_cast<float2 *>(o + k) = fma2(*reinterpret_cast<float2 *>(o1 + k), make_float2(w1, w1), *reinterpret_cast<float2 *>(o + k));
                     }
                 };
                 if (partial) {
 #pragma unroll 1
-                    for (int x = 0; x < DO; x += 32) {
-                        float o[32];
+                    for (int x = 0; x < c1 - c0; x += 32) {
+                        alignas(8) float o[32];
                         load(x, o);
                         if (there) {
 #pragma unroll
@@ -691,16 +718,19 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     for (int x0 = 0; x0 < c1 - c0; x0 += STAGE) {
 #pragma unroll 1
                         for (int x = 0; x < STAGE && x0 + x < c1 - c0; x += 32) {
-                            float o[32];
+                            alignas(8) float o[32];
                             load(x0 + x, o);
-                            if (none) {
+                            if (__any_sync(0xffffffffu, none)) {
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] = 0.f;
+                                for (int k = 0; k < 32; ++k) o[k] = none ? 0.f : o[k];
                             }
                             const int cols = c1 - c0 - x0 - x;
+                            if (cols < 32) {                       // (no products were made past the head's elements)
 #pragma unroll
-                            for (int k = 0; k < 32; k += 2)
-                                if (k < cols) bad = fma2(make_float2(o[k], o[k + 1]), make_float2(0.f, 0.f), bad);
+                                for (int k = 0; k < 32; ++k) o[k] = k < cols ? o[k] : 0.f;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; k += 2) bad = fma2(*reinterpret_cast<float2 *>(o + k), make_float2(0.f, 0.f), bad);
                             if (a.out_f32 && there) {
 #pragma unroll
                                 for (int k = 0; k < 32; k += 2)
@@ -716,15 +746,16 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                         __syncwarp();
                         if (a.out && wide_out) {                   // 16 bytes a lane, STAGE / 8 lanes a row
                             constexpr int LANES = STAGE / 8;
-#pragma unroll 4
-                            for (int i = 0; i < 32; i += 32 / LANES) {
-                                const int r = i + lane / LANES, ch = lane % LANES, to = __shfl_sync(0xffffffffu, at_row, r);
-                                if (to >= 0 && c0 + x0 + ch * 8 < c1) {
-                                    uint4 w;
-                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                                                 : "r"(stage + (uint32_t)(r * STAGE * 2) + (uint32_t)((ch ^ (r & (LANES - 1))) << 4)) : "memory");
-                                    *reinterpret_cast<uint4 *>((T *)a.out + (size_t)to * a.d + c0 + x0 + ch * 8) = w;
-                                }
+                            uint4 w[LANES];
+#pragma unroll
+                            for (int i = 0; i < LANES; ++i) {
+                                const int r = i * (32 / LANES) + lane / LANES;
+                                w[i] = *reinterpret_cast<const uint4 *>(stages + warp * kStage + r * STAGE * 2 + ((lane % LANES ^ (r & (LANES - 1))) << 4));
+                            }
+#pragma unroll
+                            for (int i = 0; i < LANES; ++i) {
+                                const int to = __shfl_sync(0xffffffffu, at_row, i * (32 / LANES) + lane / LANES);
+                                if (to >= 0 && c0 + x0 + lane % LANES * 8 < c1) *reinterpret_cast<uint4 *>((T *)a.out + (size_t)to * a.d + c0 + x0 + lane % LANES * 8) = w[i];
                             }
                         } else if (a.out) {                        // 4 bytes a lane, STAGE / 2 lanes a row
                             constexpr int LANES = STAGE / 2;
@@ -886,6 +917,14 @@ bool rows_map(CUtensorMap *m, int dtype, const void *at, int d, long long n_head
     *tokens_first = tf;
     return encode(m, dtype, 3, at, dims, strides, box);
 }
+// Rows whose heads begin at any even element, out of 16-byte aligned tokens: boxes of 64 elements x 128 tokens of the whole row.
+bool shifted_map(CUtensorMap *m, int dtype, const void *at, int d, long long n_heads, long long head, long long n_tokens, long long token)
+{
+    if (((uintptr_t)at & 15) || token % 8 || token > 0x7fffffff || head <= 0 || (n_heads - 1) * head + d > token || n_tokens < 1) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)((n_heads - 1) * head + d), (cuuint64_t)n_tokens}, strides[1] = {(cuuint64_t)token * 2};
+    const cuuint32_t box[2] = {64, kTileRows};
+    return encode(m, dtype, 2, at, dims, strides, box);
+}
 bool page_map(CUtensorMap *m, int dtype, const PromptArgs &a, const void *pool, int box_rows)
 {
     const cuuint64_t dims[2] = {(cuuint64_t)a.d, (cuuint64_t)a.n_pages * a.kv_heads * a.page_rows}, strides[1] = {(cuuint64_t)a.row_stride * 2};
@@ -898,7 +937,7 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap
 {
     constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
     constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * STAGE * 2 + sizeof(TileControl), most = 227 * 1024;
-    static_assert(2 * SLOTS + 22 <= 40, "barriers");
+    static_assert(2 * SLOTS + 26 <= 42, "barriers");
     const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
     if (smem > most) {                                             // the list of a large batch takes half the room of the outputs
         if constexpr (STAGE == 64) return launch_tiles<T, NSUB, SLOTS, 32>(a, blocks, qm, km, vm, st);
@@ -943,14 +982,19 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
     a.box_rows = 0;
     if (a.table) {
         int box = kTileRows;
-        while (a.page_rows % box) box /= 2;                        // boxes that never straddle two pages; eight rows are one block of the swizzle
-        if (box >= 8 && page_map(&km, dtype, a, a.k, box) && page_map(&vm, dtype, a, a.v, box)) a.box_rows = box;
+        while (a.page_rows % box) box /= 2;                        // the largest power of two that divides a page: boxes never straddle two
+        if (page_map(&km, dtype, a, a.k, box) && page_map(&vm, dtype, a, a.v, box)) a.box_rows = box;
     } else {
         bool kt = false, vt = false;
         if (rows_map(&km, dtype, a.k, a.d, a.kv_heads, a.k_head, a.n_k, a.k_token, 1, kTileRows, &kt) &&
             rows_map(&vm, dtype, a.v, a.d, a.kv_heads, a.v_head, a.n_k, a.v_token, 1, kTileRows, &vt)) {
             a.box_rows = kTileRows;
             a.tokens_first = (kt ? 2 : 0) | (vt ? 4 : 0);
+        } else if ((a.d <= 58 || (a.d > 64 && a.d <= 112)) && shifted_map(&km, dtype, a.k, a.d, a.kv_heads, a.k_head, a.n_k, a.k_token) &&
+                   shifted_map(&vm, dtype, a.v, a.d, a.kv_heads, a.v_head, a.n_k, a.v_token)) {
+            a.box_rows = kTileRows;                                // (elements of a head and the 6 before it fit its columns, in steps of 16)
+            a.shifted = 1;
+            a.q_boxes = 0;                                         // (q has to lie where the head's elements do, between zeros)
         }
     }
     return dtype == ADSA_BF16 ? launch_tiles_type<__nv_bfloat16>(a, (unsigned)sms, qm, km, vm, st) : launch_tiles_type<__half>(a, (unsigned)sms, qm, km, vm, st);
