@@ -31,6 +31,7 @@ constexpr int kTileThreads = 384;           // warps 0 .. 3, 4 .. 7: the groups;
 constexpr int kTileColumns = 512;           // all of tensor memory: S (and P) of the groups at 0 and 128, O at 256 and 384
 constexpr float kTileSlack = 8.f;
 constexpr int kTileRing = 4;                // items ahead
+constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time
 constexpr unsigned kTileMinRun = 6;         // units of a run, at least, where items may be cut
 
 struct TileDesc {                           // an item of a run, as the walking warp finds it
@@ -48,6 +49,15 @@ struct TilePos {
         return q != o.q ? q < o.q : tile < o.tile;
     }
 };
+template <bool WIDE>
+__device__ __forceinline__ TilePos next_pos(const PromptArgs &a, const PromptSeq &s, TilePos pos)
+{
+    pos.tile = 0;
+    if (++pos.q * item_tokens<WIDE>(a) < s.m) return pos;
+    pos.q = 0;
+    if (s.m == 0 || ++pos.head >= a.kv_heads) { pos.head = 0; ++pos.b; }
+    return pos;
+}
 struct TileControl {
     uint64_t bars[42];
     TileDesc ring[kTileRing];
@@ -126,8 +136,9 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, unsign
     }
 }
 
-// STAGE: elements of an output row that a warp turns over in shared memory at a time
-template <typename T, int NSUB, int SLOTS, int STAGE>
+// PLAIN: what calls as a rule are: everything copied by boxes, outputs of 16 bits in 16-byte pieces.  What is left (row copies, other
+// outputs) has a kernel of its own for its code's sake: it slowed this one by 10 to 15%, without being run.
+template <typename T, int NSUB, int SLOTS, bool PLAIN>
 __global__ void __launch_bounds__(kTileThreads, 1)
 prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                    const __grid_constant__ CUtensorMap v_map)
@@ -135,7 +146,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     constexpr bool WIDE = NSUB > 2;
     constexpr int PARTS = WIDE ? 2 : 1, PSUB = NSUB / PARTS;   // a tile of K or V lies in PARTS slots of PSUB columns of 64 elements
     constexpr int DO = 64 * PSUB;                             // elements of O of a group
-    constexpr uint32_t kSub = kTileRows * 128, kSlot = PSUB * kSub, kQ = (WIDE ? 1 : 2) * NSUB * kSub, kStage = 32 * STAGE * 2;
+    constexpr uint32_t kSub = kTileRows * 128, kSlot = PSUB * kSub, kQ = (WIDE ? 1 : 2) * NSUB * kSub, kStage = 32 * kTileStage * 2;
     constexpr float kBias = WideBias<T>::value;
     extern __shared__ unsigned char tile_smem[];
     const uint32_t base = (smem_u32(tile_smem) + 1023u) & ~1023u;
@@ -166,7 +177,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         }
     }
     // what row copies leave of a row's last 16 elements is zero from the start
-    if ((!a.q_boxes || !a.box_rows) && a.d % 16) {
+    if (!PLAIN && (!a.q_boxes || !a.box_rows) && a.d % 16) {
         for (uint32_t i = tid; i < (kQ + SLOTS * kSlot) / 16; i += kTileThreads)
             asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(base + 16 * i), "r"(0u) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -242,7 +253,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         return c.ring[at].t1 >= 0;
     };
     // where the elements of a head's row begin in a tile of K or V
-    const auto shift_of = [&](int head, bool value) { return a.shifted ? (int)(head * (value ? a.v_head : a.k_head)) & 7 : 0; };
+    const auto shift_of = [&](int head, bool value) { return !PLAIN && a.shifted ? (int)(head * (value ? a.v_head : a.k_head)) & 7 : 0; };
     // cached rows of tile t, from its first row on
     const auto rows_of = [&](const PromptSeq &s, int t) {
         const int before = (s.p + kTileRows - 1) / kTileRows;
@@ -261,7 +272,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         PromptSeq s = {};
         while (pos.before(end)) {
             if (pos.b != have) { s = prompt_seq(a, pos.b); have = pos.b; }
-            if (s.m == 0) { pos = {pos.b + 1, 0, 0, 0}; continue; }
+            if (s.m == 0) { pos = next_pos<WIDE>(a, s, pos); continue; }
             const TileItem<WIDE> item(a, s, pos.q);
             const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
             const int t1 = last ? end.tile : item.tiles;
@@ -277,11 +288,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             }
             if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
             if (last) break;
-            if (++pos.q * item_tokens<WIDE>(a) >= s.m) {
-                pos.q = 0;
-                if (++pos.head >= a.kv_heads) { pos.head = 0; ++pos.b; }
-            }
-            pos.tile = 0;
+            pos = next_pos<WIDE>(a, s, pos);
         }
         wait(d_empty + 8 * at, d_phase ^ 1u);
         if (lane == 0) {
@@ -327,10 +334,10 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const bool pre = t < before;
             const int row0 = (pre ? t : t - before) * kTileRows, x0 = part * PSUB * 64;
             const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
-            if (waiting && !mbar_try_wait(empty + 8 * slot, phase ^ 1u)) flush();
+            if (!PLAIN && waiting && !mbar_try_wait(empty + 8 * slot, phase ^ 1u)) flush();
             wait(empty + 8 * slot, phase ^ 1u);
             const int32_t *pages = pre ? a.p_table + (size_t)it.s.group * a.max_p_pages : a.table + (size_t)it.b * a.max_pages;
-            if (a.box_rows && a.table) {
+            if ((PLAIN || a.box_rows) && a.table) {
                 const int boxes = (valid + a.box_rows - 1) / a.box_rows;
                 if (lane == 0) mbar_expect_tx(bar, (uint32_t)(boxes * a.box_rows) * 128u * PSUB);
                 __syncwarp();
@@ -341,19 +348,19 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     for (int s = 0; s < PSUB; ++s)
                         pa_tma(dst + (uint32_t)(i * a.box_rows) * 128u + s * kSub, value ? &v_map : &k_map, x0 + s * 64, y, bar);
                 }
-            } else if (a.box_rows) {
+            } else if (PLAIN || a.box_rows) {
                 if (lane == 0) {
                     mbar_expect_tx(bar, kSlot);
                     const int tok = (int)it.s.k0 + row0, shift = shift_of(it.head, value);
                     const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
 #pragma unroll
                     for (int s = 0; s < PSUB; ++s) {
-                        if (a.shifted) pa_tma(dst + s * kSub, value ? &v_map : &k_map, (int)(it.head * (value ? a.v_head : a.k_head)) - shift + s * 64, tok, bar);
+                        if (!PLAIN && a.shifted) pa_tma(dst + s * kSub, value ? &v_map : &k_map, (int)(it.head * (value ? a.v_head : a.k_head)) - shift + s * 64, tok, bar);
                         else tile_tma3(dst + s * kSub, value ? &v_map : &k_map, x0 + s * 64, tf ? tok : it.head, tf ? it.head : tok, bar);
                     }
                 }
                 __syncwarp();
-            } else {
+            } else if constexpr (!PLAIN) {
                 const int piece = value ? v_piece : k_piece;
                 if (piece == 16) by_rows(std::integral_constant<int, 16>(), it, pre, row0, x0, valid, dst, value);
                 else if (piece == 8) by_rows(std::integral_constant<int, 8>(), it, pre, row0, x0, valid, dst, value);
@@ -364,7 +371,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         };
         // in the order the products take them: K0 V0 K1 V1 .. where both groups share a tile, else K0 K1 V0 K2 V1 K3 ..
         for (;;) {
-            if (waiting && !mbar_try_wait(d_full + 8 * at, d_phase)) flush();
+            if (!PLAIN && waiting && !mbar_try_wait(d_full + 8 * at, d_phase)) flush();
             if (!have_item()) break;
             const TileDesc &it = c.ring[at];
             const bool turns = !WIDE && it.s.m - it.q * item_tokens<WIDE>(a) <= a.half_tokens;
@@ -378,7 +385,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             }
             next_item();
         }
-        if (waiting) flush();
+        if (!PLAIN && waiting) flush();
     } else if (warp == 10) {                                       // ---- copies of Q ----
         uint32_t phase = 0;                                        // bit h: of half h
         const int q_piece = piece_of(a.q, a.q_token, a.q_head, a.d), tph = a.half_tokens;
@@ -392,7 +399,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 const uint32_t dst = q_at + (uint32_t)h * NSUB * kSub, bar = q_full + 8 * h;
                 wait(q_empty + 8 * h, (phase >> h & 1u) ^ 1u);
                 phase ^= 1u << h;
-                if (a.q_boxes) {
+                if (PLAIN || a.q_boxes) {
                     if (lane == 0) {
                         const int boxes = (a.d + 63) / 64, y = it.head * a.per_kv, z = (int)it.s.q0 + tok;
                         mbar_expect_tx(bar, (uint32_t)(boxes * tph * a.per_kv) * 128u);
@@ -400,7 +407,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                             tile_tma3(dst + s * kSub, &q_map, s * 64, y, z, bar);
                     }
                     __syncwarp();
-                } else {
+                } else if constexpr (!PLAIN) {
                     const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + tok) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
                     const int shift = shift_of(it.head, false), piece = shift ? min(q_piece, (2 * shift) & -(2 * shift)) : q_piece;
                     const auto by_rows = [&](auto piece_) {
@@ -500,7 +507,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (n == 0) continue;
             const TileItem<WIDE> item(a, it.s, it.q);
             const bool pair = __shfl_sync(0xffffffffu, (int)item.pair, 0);
-            if (a.shifted) {
+            if (!PLAIN && a.shifted) {
                 k_steps = __shfl_sync(0xffffffffu, (a.d + shift_of(it.head, false) + 15) / 16, 0);
                 d_cols = __shfl_sync(0xffffffffu, (a.d + shift_of(it.head, true) + 15) / 16, 0) * 16;
             }
@@ -556,6 +563,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const uint32_t my_s = s_full + 8 * g, my_p = p_full + 32 * g, my_o = o_full + 8 * g;
         const int tph = a.half_tokens, heads = a.kv_heads * a.per_kv;
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
+        bool again = false;                                        // a row of this lane came out infinite or NaN
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<WIDE> item(a, it.s, it.q);
@@ -713,11 +721,11 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     if (there) *reinterpret_cast<float2 *>(a.state_ml + 2 * at_slot) = make_float2(m2, l);
                 } else {
                     const uint32_t stage = smem_u32(stages) + warp * kStage;
-                    const bool wide_out = a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0;
+                    const bool wide_out = PLAIN || (a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0), half_out = a.d % 4 == 0 && ((uintptr_t)a.out & 7) == 0;
 #pragma unroll 1
-                    for (int x0 = 0; x0 < c1 - c0; x0 += STAGE) {
+                    for (int x0 = 0; x0 < c1 - c0; x0 += kTileStage) {
 #pragma unroll 1
-                        for (int x = 0; x < STAGE && x0 + x < c1 - c0; x += 32) {
+                        for (int x = 0; x < kTileStage && x0 + x < c1 - c0; x += 32) {
                             alignas(8) float o[32];
                             load(x0 + x, o);
                             if (__any_sync(0xffffffffu, none)) {
@@ -731,7 +739,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                             }
 #pragma unroll
                             for (int k = 0; k < 32; k += 2) bad = fma2(*reinterpret_cast<float2 *>(o + k), make_float2(0.f, 0.f), bad);
-                            if (a.out_f32 && there) {
+                            if (!PLAIN && a.out_f32 && there) {
 #pragma unroll
                                 for (int k = 0; k < 32; k += 2)
                                     if (k < cols) *reinterpret_cast<float2 *>(a.out_f32 + (size_t)at_row * a.d + c0 + x0 + x + k) = make_float2(o[k], o[k + 1]);
@@ -739,36 +747,41 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 #pragma unroll
                             for (int k = 0; k < 32; k += 8)
                                 asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
-                                             ::"r"(stage + (uint32_t)(lane * STAGE * 2) + (uint32_t)((((x + k) / 8) ^ (lane & (STAGE / 8 - 1))) << 4)),
+                                             ::"r"(stage + (uint32_t)(lane * kTileStage * 2) + (uint32_t)((((x + k) / 8) ^ (lane & (kTileStage / 8 - 1))) << 4)),
                                              "r"(pack2<T>(o[k], o[k + 1])), "r"(pack2<T>(o[k + 2], o[k + 3])), "r"(pack2<T>(o[k + 4], o[k + 5])),
                                              "r"(pack2<T>(o[k + 6], o[k + 7])) : "memory");
                         }
                         __syncwarp();
-                        if (a.out && wide_out) {                   // 16 bytes a lane, STAGE / 8 lanes a row
-                            constexpr int LANES = STAGE / 8;
+                        if ((PLAIN || a.out) && wide_out) {                   // 16 bytes a lane, kTileStage / 8 lanes a row
+                            constexpr int LANES = kTileStage / 8;
                             uint4 w[LANES];
 #pragma unroll
                             for (int i = 0; i < LANES; ++i) {
                                 const int r = i * (32 / LANES) + lane / LANES;
-                                w[i] = *reinterpret_cast<const uint4 *>(stages + warp * kStage + r * STAGE * 2 + ((lane % LANES ^ (r & (LANES - 1))) << 4));
+                                w[i] = *reinterpret_cast<const uint4 *>(stages + warp * kStage + r * kTileStage * 2 + ((lane % LANES ^ (r & (LANES - 1))) << 4));
                             }
 #pragma unroll
                             for (int i = 0; i < LANES; ++i) {
                                 const int to = __shfl_sync(0xffffffffu, at_row, i * (32 / LANES) + lane / LANES);
                                 if (to >= 0 && c0 + x0 + lane % LANES * 8 < c1) *reinterpret_cast<uint4 *>((T *)a.out + (size_t)to * a.d + c0 + x0 + lane % LANES * 8) = w[i];
                             }
-                        } else if (a.out) {                        // 4 bytes a lane, STAGE / 2 lanes a row
-                            constexpr int LANES = STAGE / 2;
-#pragma unroll 2
-                            for (int i = 0; i < 32; i += 32 / LANES) {
-                                const int r = i + lane / LANES, e = 2 * (lane % LANES), to = __shfl_sync(0xffffffffu, at_row, r);
-                                if (to >= 0 && c0 + x0 + e < c1) {
-                                    uint32_t w;
-                                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w)
-                                                 : "r"(stage + (uint32_t)(r * STAGE * 2) + (uint32_t)(((e / 8) ^ (r & (STAGE / 8 - 1))) << 4) + (uint32_t)(e % 8) * 2u) : "memory");
-                                    *reinterpret_cast<uint32_t *>((T *)a.out + (size_t)to * a.d + c0 + x0 + e) = w;
+                        } else if (!PLAIN && a.out) {              // 8 or 4 bytes a lane
+                            const auto pieces = [&](auto words_) {
+                                constexpr int WORDS = decltype(words_)::value, LANES = kTileStage / 2 / WORDS;
+#pragma unroll 4
+                                for (int i = 0; i < 32; i += 32 / LANES) {
+                                    const int r = i + lane / LANES, e = 2 * WORDS * (lane % LANES), to = __shfl_sync(0xffffffffu, at_row, r);
+                                    const uint32_t *from = reinterpret_cast<const uint32_t *>(
+                                        stages + warp * kStage + r * kTileStage * 2 + (((e / 8) ^ (r & (kTileStage / 8 - 1))) << 4) + e % 8 * 2);
+                                    uint32_t *out = reinterpret_cast<uint32_t *>((T *)a.out + (size_t)max(to, 0) * a.d + c0 + x0 + e);
+                                    if (to >= 0 && c0 + x0 + e < c1) {
+                                        if constexpr (WORDS == 2) *reinterpret_cast<uint2 *>(out) = *reinterpret_cast<const uint2 *>(from);
+                                        else *out = *from;
+                                    }
                                 }
-                            }
+                            };
+                            if (half_out) pieces(std::integral_constant<int, 2>());
+                            else pieces(std::integral_constant<int, 1>());
                         }
                         __syncwarp();
                     }
@@ -780,11 +793,32 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 __syncwarp();
                 if (lane == 0) mbar_arrive(m_empty);
             }
-            // rows that came out infinite or NaN, from what they attend alone
-            unsigned again = __ballot_sync(0xffffffffu, there && !partial && bad.x + bad.y != 0.f);
-            for (; again; again &= again - 1) {
-                const int src = __ffs(again) - 1;
-                prompt_row_by_warp<T>(a, it.s, it.b, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), lane, c0, c1);
+            again = again || (there && !partial && bad.x + bad.y != 0.f);
+        }
+        // Rows that came out infinite or NaN, from what they attend alone: the run once more, in whole items.  (A call in the loop above
+        // cost it 8%.)
+        if (__any_sync(0xffffffffu, again)) {
+            const TilePos end = c.end;
+            for (TilePos pos = c.begin; pos.before(end); pos.tile = 0) {
+                const PromptSeq s = prompt_seq(a, pos.b);
+                if (s.m > 0) {
+                    const TileItem<WIDE> item(a, s, pos.q);
+                    const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
+                    if (pos.tile == 0 && (!last || end.tile == item.tiles) && (WIDE || item.pair || g == 0)) {
+                        const int in = a.by_per_kv(row), at = in + (item.pair ? g * tph : 0), c0 = WIDE ? g * DO : 0, c1 = min(a.d, c0 + DO);
+                        const int tok = item.first + at, head = pos.head * a.per_kv + row - in * a.per_kv;
+                        bool bad = false;
+                        if (in < tph && at < item.count) {
+                            const size_t first = ((size_t)(s.q0 + tok) * heads + head) * a.d;
+                            for (int e = c0; e < c1; ++e) bad = bad || !(fabsf(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]) <= FLT_MAX);
+                        }
+                        for (unsigned todo = __ballot_sync(0xffffffffu, bad); todo; todo &= todo - 1) {
+                            const int src = __ffs(todo) - 1;
+                            prompt_row_by_warp<T>(a, s, pos.b, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), lane, c0, c1);
+                        }
+                    }
+                }
+                pos = next_pos<WIDE>(a, s, pos);
             }
         }
     }
@@ -932,18 +966,15 @@ bool page_map(CUtensorMap *m, int dtype, const PromptArgs &a, const void *pool, 
     return encode(m, dtype, 2, pool, dims, strides, box);
 }
 
-template <typename T, int NSUB, int SLOTS, int STAGE>
+template <typename T, int NSUB, int SLOTS, bool PLAIN>
 cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
     constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
-    constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * STAGE * 2 + sizeof(TileControl), most = 227 * 1024;
+    constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * kTileStage * 2 + sizeof(TileControl), most = 227 * 1024;
     static_assert(2 * SLOTS + 26 <= 42, "barriers");
     const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
-    if (smem > most) {                                             // the list of a large batch takes half the room of the outputs
-        if constexpr (STAGE == 64) return launch_tiles<T, NSUB, SLOTS, 32>(a, blocks, qm, km, vm, st);
-        return cudaErrorInvalidValue;
-    }
-    const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, STAGE>;
+    if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
+    const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, PLAIN>;
     static int told[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -958,12 +989,12 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap
     if (e != cudaSuccess || !a.split || blocks < 2) return e;
     return launch_pdl(prompt_tile_merge_kernel<T, NSUB>, dim3(blocks - 1, 256 / (kTileMergeThreads / 32)), kTileMergeThreads, 0, st, a, (int)blocks);
 }
-template <typename T>
+template <typename T, bool PLAIN>
 cudaError_t launch_tiles_type(const PromptArgs &a, unsigned blocks, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
-    if (a.d <= 64) return launch_tiles<T, 1, 8, 64>(a, blocks, qm, km, vm, st);
-    if (a.d <= 128) return launch_tiles<T, 2, 4, 64>(a, blocks, qm, km, vm, st);
-    return launch_tiles<T, 4, 4, 64>(a, blocks, qm, km, vm, st);
+    if (a.d <= 64) return launch_tiles<T, 1, 8, PLAIN>(a, blocks, qm, km, vm, st);
+    if (a.d <= 128) return launch_tiles<T, 2, 4, PLAIN>(a, blocks, qm, km, vm, st);
+    return launch_tiles<T, 4, 4, PLAIN>(a, blocks, qm, km, vm, st);
 }
 
 }  // namespace
@@ -997,7 +1028,10 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
             a.q_boxes = 0;                                         // (q has to lie where the head's elements do, between zeros)
         }
     }
-    return dtype == ADSA_BF16 ? launch_tiles_type<__nv_bfloat16>(a, (unsigned)sms, qm, km, vm, st) : launch_tiles_type<__half>(a, (unsigned)sms, qm, km, vm, st);
+    const bool plain = a.q_boxes && a.box_rows && !a.shifted && a.out && !a.out_f32 && a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0;
+    const unsigned blocks = (unsigned)sms;
+    if (dtype == ADSA_BF16) return plain ? launch_tiles_type<__nv_bfloat16, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__nv_bfloat16, false>(a, blocks, qm, km, vm, st);
+    return plain ? launch_tiles_type<__half, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__half, false>(a, blocks, qm, km, vm, st);
 }
 
 }  // namespace adsa
