@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libadsa.so")
 SOURCES = ["adsa_api.cu", "adsa_pool.cu", "adsa_score_select.cu", "adsa_attn.cu", "adsa_step.cu", "adsa_pstep.cu", "adsa_wstep.cu", "adsa_prefill.cu", "adsa_attn_static.cu", "adsa_shell.cu",
-           "adsa_rotary.cu", "adsa_residual.cu", "adsa_prefix_attn.cu", "adsa_prefix_wide.cu", "adsa_prompt_attn.cu", "adsa_prompt_tile.cu", "adsa_sample.cu"]
+           "adsa_rotary.cu", "adsa_residual.cu", "adsa_prefix_attn.cu", "adsa_prefix_wide.cu", "adsa_prompt_attn.cu", "adsa_prompt_tile.cu", "adsa_prompt_few.cu", "adsa_sample.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 

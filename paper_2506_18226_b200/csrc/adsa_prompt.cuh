@@ -39,7 +39,7 @@ struct PromptArgs {
     // workspace: what each run leaves for the merge, partial states [2 runs][16 or 32][256 rows][4 elements] and their (m, l)
     int4 *run_desc;
     float *state, *state_ml;
-    int box_rows;                           // rows of a copy's box in a page; 0: K and V are copied row by row
+    int box_rows, box_shift;                // rows of a copy's box (a power of two, its logarithm); 0: K and V are copied row by row
     int q_boxes, tokens_first;              // q by boxes; the order in the maps of packed k (bit 1) and v (bit 2): tokens before heads
     int shifted;                            // packed k and v by boxes that begin up to 7 elements before a head's row
     int split;                              // items may be cut (into partial states)
@@ -119,10 +119,9 @@ struct TileItem {
     __device__ __forceinline__ unsigned cost() const { return kTileOver + tile_cost() * (unsigned)tiles; }
 };
 
-// the page that holds a row; one outside the pool is reported, and read as page 0 (the result is then unspecified)
-__device__ __forceinline__ int prompt_page(const PromptArgs &a, const int32_t *pages, int row)
+// a page as a table names it; one outside the pool is reported, and read as page 0 (the result is then unspecified)
+__device__ __forceinline__ int prompt_page(const PromptArgs &a, int page)
 {
-    const int page = pages[a.by_page(row)];
     if (page >= 0 && page < a.n_pages) return page;
     if (a.status) atomicOr(a.status, ADSA_DEV_BAD_PAGE);
     return 0;
@@ -134,7 +133,7 @@ __device__ __forceinline__ size_t prompt_row(const PromptArgs &a, const PromptSe
     const bool pre = j < s.p;
     const int row = pre ? j : j - s.p;
     const int32_t *pages = pre ? a.p_table + (size_t)s.group * a.max_p_pages : a.table + (size_t)b * a.max_pages;
-    const int page = prompt_page(a, pages, row);
+    const int page = prompt_page(a, pages[a.by_page(row)]);
     return (((size_t)page * a.kv_heads + h) * a.page_rows + row - a.by_page(row) * a.page_rows) * a.row_stride;
 }
 

@@ -1,0 +1,491 @@
+// Attention of few query rows per sequence (single tokens, guesses to be checked, a row of a grid) over packed rows or a paged
+// cache: what the tile kernel does, laid out for calls whose time is that of reading the cache.
+//
+// An item has up to 64 query rows of a key head.  They are spread over a 128-row tile of Q so that each of a group's four warps has
+// 8 of them (16 of more than 32), and a warp takes its scores from tensor memory four lanes to a row: 32 or 64 exponentials a thread and
+// tile for all 128 cached rows, on all four parts of an SM, where a row per thread takes 128 on as many parts as have rows.  The two groups
+// take the tiles in turns, so that one's products run under the other's softmax, and join their states at the end.  Q takes half of what
+// two halves take and outputs go straight to memory: the ring of tiles has the rest, 160 to 192 KB.
+//
+// 32 sequences of one token over 1144 rows of 20 heads of 64 (187 MB): 74 us by the tile kernel.
+#include <float.h>
+
+#include "adsa_prompt_tile.cuh"
+
+namespace adsa {
+
+struct FewControl {
+    uint64_t bars[48];
+    TileDesc ring[kTileRing];
+    TilePos ends[2];                        // of this block's run
+    float2 ml[kFewRows];                    // (m, l) of group 1
+    uint32_t tmem;
+    int limit;                              // polls of a wait before it gives up
+};
+
+// 16 rows of the warp's part of tensor memory x 8 N columns, four lanes to a row: register 4 i + 2 h + e of lane t has row t / 4 + 8 h,
+// column 8 i + 2 (t % 4) + e
+__device__ __forceinline__ void few_load4(uint32_t at, float (&v)[16])
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at) : "memory");
+}
+__device__ __forceinline__ void few_store4(uint32_t at, const float (&v)[16])
+{
+    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// the same with 4 N columns of two 16-bit values: register 2 i + h of lane t has row t / 4 + 8 h, values 8 i + 2 (t % 4) and the next
+__device__ __forceinline__ void few_store_pairs(uint32_t at, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+template <typename T, int NSUB, int SLOTS>
+__global__ void __launch_bounds__(kTileThreads, 1)
+prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
+{
+    constexpr int DO = 64 * NSUB;
+    constexpr uint32_t kSub = kTileRows * 128, kSlot = NSUB * kSub;
+    constexpr float kBias = WideBias<T>::value;
+    extern __shared__ unsigned char few_smem[];
+    const uint32_t base = (smem_u32(few_smem) + 1023u) & ~1023u;
+    const uint32_t q_at = base, ring = base + kSlot;
+    unsigned char *const ctl = few_smem + (base - smem_u32(few_smem)) + (size_t)(SLOTS + 1) * kSlot;
+    FewControl &c = *reinterpret_cast<FewControl *>(ctl);
+    unsigned *const plan = reinterpret_cast<unsigned *>(ctl + sizeof(FewControl));
+    const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 8, s_full = q_empty + 8, p_full = s_full + 16,
+                   o_full = p_full + 16, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8, d_empty = d_full + 8 * kTileRing;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
+
+    if (tid == 0) {
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        for (int g = 0; g < 2; ++g) { mbar_init(s_full + 8 * g, 1); mbar_init(p_full + 8 * g, 4); mbar_init(o_full + 8 * g, 1); }
+        mbar_init(m_full, 4);
+        mbar_init(m_empty, 4);
+        for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 11); }
+        c.limit = kCopySpinLimit;
+        mbar_init_fence();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    }
+    // what the copies of Q leave of a row's last 16 elements is zero from the start
+    if (a.d % 16) {
+        for (uint32_t i = tid; i < kSlot / 16; i += kTileThreads)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(q_at + 16 * i), "r"(0u) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 9) tc_alloc(smem_u32(&c.tmem), kTileColumns);
+    pdl_wait();
+    pdl_launch();
+    tile_plan<true>(a, plan, c.ends, warp, lane);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, c.tmem, 0);
+
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+        for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
+            if (polls < *(volatile int *)&c.limit) continue;
+            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short)
+            if (a.status) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+            break;
+        }
+    };
+    int at = 0;                                                    // the next item of the ring
+    uint32_t d_phase = 0;
+    const auto next_item = [&]() {                                 // leaves the one before to be written over
+        __syncwarp();
+        if (lane == 0) mbar_arrive(d_empty + 8 * at);
+        if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
+    };
+    const auto have_item = [&]() {                                 // c.ring[at] is one
+        wait(d_full + 8 * at, d_phase);
+        return c.ring[at].t1 >= 0;
+    };
+    // where query row r of an item of `rows` lies: 8 or 16 to a warp
+    const auto per_warp = [](int rows) { return rows <= 32 ? 8 : 16; };
+
+    if (warp == 11) {                                              // ---- the list of items ----
+        tile_walk<true>(a, c.ends, c.ring, d_full, d_empty, lane, wait);
+    } else if (warp == 8) {                                        // ---- copies of K and V ----
+        int slot = 0;
+        uint32_t phase = 0;
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            const TileSource src(a, it);
+            const int t0 = it.t0, n = it.t1 - t0;
+            const auto copy = [&](const CUtensorMap *map, int t, int y, bool value) {
+                const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
+                wait(empty + 8 * slot, phase ^ 1u);
+                if (lane == 0) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
+                __syncwarp();
+                if (a.table) {
+                    for (int i = lane; y >= 0; i += 32, y = i << a.box_shift < kTileRows ? src.pool_row(a, t, i) : -1) {
+#pragma unroll
+                        for (int s = 0; s < NSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, s * 64, y, bar);
+                    }
+                } else if (lane == 0) {
+                    const int tok = src.tok + src.row0(t);
+                    const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
+#pragma unroll
+                    for (int s = 0; s < NSUB; ++s) tile_tma3(dst + s * kSub, map, s * 64, tf ? tok : src.head, tf ? src.head : tok, bar);
+                }
+                if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+            };
+            // K0 K1 V0 K2 V1 K3 .., in the order the products take them; V lies where K does
+            int y0 = n > 0 ? src.pool_row(a, t0, lane) : -1, y1 = n > 1 ? src.pool_row(a, t0 + 1, lane) : -1;
+            if (n > 0) copy(&k_map, t0, y0, false);
+            if (n > 1) copy(&k_map, t0 + 1, y1, false);
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                const int y2 = i + 2 < n ? src.pool_row(a, t0 + i + 2, lane) : -1;
+                copy(&v_map, t0 + i, y0, true);
+                if (i + 2 < n) copy(&k_map, t0 + i + 2, y2, false);
+                y0 = y1;
+                y1 = y2;
+            }
+        }
+    } else if (warp == 10) {                                       // ---- copies of Q ----
+        uint32_t phase = 0;
+        const int piece = piece_of(a.q, a.q_token, a.q_head, a.d);
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            if (it.t1 == it.t0) continue;
+            const TileItem<true> item(a, it.s, it.q);
+            const int rows = item.count * a.per_kv, pw = per_warp(rows);
+            const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + item.first) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
+            wait(q_empty, phase ^ 1u);
+            phase ^= 1u;
+            const auto by_rows = [&](auto piece_) {
+                constexpr int piece = decltype(piece_)::value;
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += 4) {
+                    const int r = r0 + (lane >> 3), t = a.by_per_kv(r), m = r / pw * 32 + r % pw;
+                    const unsigned char *from = src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head);
+                    if (r < rows)
+                        for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(q_at + tile_at(m, x, kSub), from + x);
+                }
+            };
+            if (piece == 16) by_rows(std::integral_constant<int, 16>());
+            else if (piece == 8) by_rows(std::integral_constant<int, 8>());
+            else by_rows(std::integral_constant<int, 4>());
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+        }
+    } else if (warp == 9) {                                        // ---- products ----
+        const int k_steps = (a.d + 15) / 16;
+        const uint32_t s_shape = tc_shape<T>(kTileRows, false), o_shape = tc_shape<T>(k_steps * 16, true);
+        int slot = 0;
+        uint32_t phase = 0, q_phase = 0, p_phase = 0;               // (p_phase: bit g of group g)
+        const auto take = [&]() {                                  // the next slot, once its tile is there
+            wait(full + 8 * slot, phase);
+            const int taken = slot;
+            if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+            return taken;
+        };
+        const auto done = [&](uint32_t bar) {                      // counted when everything issued so far is complete
+            if (tc_elect()) tc_commit(bar);
+            __syncwarp();
+        };
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            // (shuffled, so that the compiler knows them to be uniform)
+            const int t0 = __shfl_sync(0xffffffffu, it.t0, 0), n = __shfl_sync(0xffffffffu, it.t1, 0) - t0, p_rows = __shfl_sync(0xffffffffu, it.s.p, 0),
+                      own_rows = __shfl_sync(0xffffffffu, it.s.n, 0), before = (p_rows + kTileRows - 1) / kTileRows;
+            if (n == 0) continue;
+            wait(q_full, q_phase);
+            q_phase ^= 1u;
+            tc_after();
+#pragma unroll 1
+            for (int step = 0; step < n + 2; ++step) {
+                const int g = step & 1, j = step - 2;              // O of tile j, then the scores of tile `step`, for the same group
+                if (j >= 0) {
+                    const int v = take(), t = t0 + j, valid = t < before ? p_rows - t * kTileRows : own_rows - (t - before) * kTileRows;
+                    if (valid < kTileRows) {
+                        // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN
+                        const uint32_t v_at = ring + (uint32_t)v * kSlot;
+                        for (int i = lane; i < (kTileRows - valid) * 8 * NSUB; i += 32) {
+                            const int r = valid + i / (8 * NSUB), ch = i % (8 * NSUB);
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v_at + (ch >> 3) * kSub + r * 128 + (ch & 7) * 16), "r"(0u) : "memory");
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    wait(p_full + 8 * g, p_phase >> g & 1u);
+                    p_phase ^= 1u << g;
+                    tc_after();
+                    const uint64_t vd = tc_operand(ring + (uint32_t)v * kSlot, kSub);
+                    if (tc_elect()) {
+#pragma unroll
+                        for (int ks = 0; ks < kTileRows / 16; ++ks)
+                            tc_mma_ts(tmem + 256 + g * 128, tmem + g * 128 + ks * 8, vd + (uint64_t)(ks * 128), o_shape, j >= 2 || ks > 0);
+                    }
+                    __syncwarp();
+                    done(empty + 8 * v);
+                    if (j + 2 >= n) done(o_full + 8 * g);          // that was the group's last
+                }
+                if (step < n) {
+                    const int k = take();
+                    const uint64_t qd = tc_operand(q_at, 16), kd = tc_operand(ring + (uint32_t)k * kSlot, 16);
+                    if (tc_elect()) {
+#pragma unroll
+                        for (int ks = 0; ks < 4 * NSUB; ++ks) {
+                            const uint64_t off = ((uint32_t)(ks >> 2) * kSub + (uint32_t)(ks & 3) * 32u) >> 4;
+                            if (ks < k_steps) tc_mma_ss(tmem + g * 128, qd + off, kd + off, s_shape, ks > 0);
+                        }
+                    }
+                    __syncwarp();
+                    done(s_full + 8 * g);
+                    done(empty + 8 * k);
+                    if (step + 1 == n) done(q_empty);
+                }
+            }
+        }
+    } else if (warp < 8) {                                         // ---- four lanes to a query row ----
+        const int g = warp >> 2, in_row = lane >> 2, col = 2 * (lane & 3);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
+        const int heads = a.kv_heads * a.per_kv;
+        uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
+        bool again = false;                                        // a row came out infinite or NaN
+        for (; have_item(); next_item()) {
+            const TileDesc &it = c.ring[at];
+            const TileItem<true> item(a, it.s, it.q);
+            const int rows = item.count * a.per_kv, pw = per_warp(rows), row0 = (warp & 3) * pw;
+            const bool both = pw == 16, warp_there = row0 < rows;  // both: rows t / 4 and t / 4 + 8 of the warp
+            int row[2], own[2];
+            bool there[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                row[h] = row0 + in_row + 8 * h;
+                there[h] = row[h] < rows && (h == 0 || both);
+                own[h] = it.s.seen(min(item.first + a.by_per_kv(row[h]), it.s.m - 1), a.causal);
+            }
+            const int p_rows = it.s.p, before = (p_rows + kTileRows - 1) / kTileRows, t0 = it.t0, n = it.t1 - t0, tiles = (n + 1 - g) / 2;
+            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // (l: this lane's part of the row's sum)
+            for (int i = 0; i < tiles; ++i) {
+                const int t = t0 + 2 * i + g;
+                wait(s_full + 8 * g, s_phase);
+                s_phase ^= 1u;
+                tc_after();
+                if (!warp_there) {
+                    tc_before();
+                    if (lane == 0) mbar_arrive(p_full + 8 * g);
+                    continue;
+                }
+                alignas(8) float v[4][16];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) few_load4(s_col + 32 * x, v[x]);
+                tc_load_wait();
+                uint32_t p[2][16];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1 && !both) break;
+                    const int valid = (t < before ? p_rows - t * kTileRows : own[h] - (t - before) * kTileRows) - col;   // from this lane's first column on
+                    if (__any_sync(0xffffffffu, valid < kTileRows)) {
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            float *w = &v[x / 4][4 * (x % 4) + 2 * h];
+                            w[0] = 8 * x < valid ? w[0] : -INFINITY;
+                            w[1] = 8 * x + 1 < valid ? w[1] : -INFINITY;
+                        }
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) mx = tile_max3(mx, v[x / 4][4 * (x % 4) + 2 * h], v[x / 4][4 * (x % 4) + 2 * h + 1]);
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    const bool move = (mx - m[h]) * a.scale_log2e > kTileSlack || m[h] == -INFINITY;
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float m_new = move ? fmaxf(m[h], mx) : m[h];
+                        const float corr = m_new == -INFINITY || m[h] == -INFINITY ? (m[h] == m_new ? 1.f : 0.f) : pa_exp2((m[h] - m_new) * a.scale_log2e);
+                        m[h] = m_new;
+                        l[h] *= corr;
+                        if (i > 0) {                               // the products before this tile's are complete: their S is
+#pragma unroll 1
+                            for (int x = 0; x < DO; x += 32) {
+                                float o[16];
+                                few_load4(o_col + x, o);
+                                tc_load_wait();
+#pragma unroll
+                                for (int k = 0; k < 16; ++k)
+                                    if ((k >> 1 & 1) == h) o[k] *= corr;
+                                few_store4(o_col + x, o);
+                            }
+                        }
+                    }
+                    const float shift = kBias - (m[h] == -INFINITY ? 0.f : m[h]) * a.scale_log2e;
+                    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        float2 w = fma2(make_float2(v[x / 4][4 * (x % 4) + 2 * h], v[x / 4][4 * (x % 4) + 2 * h + 1]), make_float2(a.scale_log2e, a.scale_log2e),
+                                        make_float2(shift, shift));
+                        w.x = pa_exp2(w.x);
+                        w.y = pa_exp2(w.y);
+                        sum = add2(sum, w);                        // the sum takes the weights before they are rounded
+                        p[x / 8][2 * (x % 8) + h] = pack2<T>(w.x, w.y);
+                    }
+                    l[h] += sum.x + sum.y;
+                }
+                if (!both) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) p[x / 8][2 * (x % 8) + 1] = 0u;
+                }
+                few_store_pairs(s_col, p[0]);                      // over scores that are in registers by now
+                few_store_pairs(s_col + 32, p[1]);
+                tc_store_wait();
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 8 * g);
+            }
+            if (tiles > 0) {
+                wait(o_full + 8 * g, o_phase);
+                o_phase ^= 1u;
+                tc_after();
+            }
+            // each row's state: O (in tensor memory) and l relative to 2^m2
+            float m2[2], w0[2], w1[2];
+            const bool partial = it.slot >= 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+                m2[h] = m[h] == -INFINITY ? -INFINITY : m[h] * a.scale_log2e - kBias;
+                if (g == 1 && there[h] && (lane & 3) == 0) c.ml[row[h]] = make_float2(m2[h], l[h]);
+            }
+            if (g == 1) {
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(m_full);
+                wait(m_empty, m_phase);                            // (group 0 has read this group's O)
+                m_phase ^= 1u;
+                tc_after();
+                continue;
+            }
+            wait(m_full, m_phase);
+            m_phase ^= 1u;
+            tc_after();
+            int to[2];                                             // row of the output, or -1
+            bool none[2], bad = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                w0[h] = 1.f;
+                w1[h] = 0.f;
+                if (n > 1 && there[h]) {
+                    const float2 other = c.ml[row[h]];
+                    const float M = fmaxf(m2[h], other.x);
+                    w0[h] = m2[h] == -INFINITY ? 0.f : pa_exp2(m2[h] - M);
+                    w1[h] = other.x == -INFINITY ? 0.f : pa_exp2(other.x - M);
+                    l[h] = l[h] * w0[h] + other.y * w1[h];
+                    m2[h] = M;
+                }
+                none[h] = it.s.p + own[h] == 0;
+                if (!partial) { w0[h] *= 1.f / l[h]; w1[h] *= 1.f / l[h]; }
+                const int tok = a.by_per_kv(row[h]);
+                to[h] = there[h] ? (int)((it.s.q0 + item.first + tok) * heads + it.head * a.per_kv + row[h] - tok * a.per_kv) : -1;
+                if (there[h] && (lane & 3) == 0) {
+                    if (partial) *reinterpret_cast<float2 *>(a.state_ml + 2 * ((size_t)it.slot * 256 + row[h])) = make_float2(m2[h], l[h]);
+                    else if (a.lse) a.lse[to[h]] = none[h] ? -INFINITY : (m2[h] + log2f(l[h])) * 0.693147180559945309f;
+                }
+            }
+            if (warp_there) {
+#pragma unroll 1
+                for (int x0 = 0; x0 < a.d; x0 += 32) {
+                    float o[16], o1[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = o1[k] = 0.f;
+                    if (tiles > 0) few_load4(o_col + x0, o);
+                    if (n > 1) few_load4(o_col + 128 + x0, o1);
+                    tc_load_wait();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int x = x0 + 8 * i + col;
+                            if (to[h] < 0 || x >= a.d) continue;
+                            float2 y = make_float2(o[4 * i + 2 * h] * w0[h], o[4 * i + 2 * h + 1] * w0[h]);
+                            if (n > 1) y = make_float2(fmaf(o1[4 * i + 2 * h], w1[h], y.x), fmaf(o1[4 * i + 2 * h + 1], w1[h], y.y));
+                            if (partial) {
+                                *reinterpret_cast<float2 *>(a.state + ((size_t)it.slot * (DO / 4) + x / 4) * 1024 + row[h] * 4 + x % 4) = y;
+                                continue;
+                            }
+                            if (none[h]) y = make_float2(0.f, 0.f);
+                            bad = bad || !(fabsf(y.x) <= FLT_MAX) || !(fabsf(y.y) <= FLT_MAX);
+                            if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + (size_t)to[h] * a.d + x) = pack2<T>(y.x, y.y);
+                            if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + (size_t)to[h] * a.d + x) = y;
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            again = again || bad;
+            tc_before();                                           // read before the next item's products write O
+            __syncwarp();
+            if (lane == 0) mbar_arrive(m_empty);
+        }
+        // rows that came out infinite or NaN, from what they attend alone: the run once more, in whole items
+        if (__any_sync(0xffffffffu, again)) {
+            const TilePos end = c.ends[1];
+            for (TilePos pos = c.ends[0]; pos.before(end);) {
+                const PromptSeq s = prompt_seq(a, pos.b);
+                if (s.m > 0) {
+                    const TileItem<true> item(a, s, pos.q);
+                    const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
+                    const int rows = item.count * a.per_kv, pw = per_warp(rows);
+                    if (pos.tile == 0 && (!last || end.tile == item.tiles)) {
+                        for (int r = warp * pw; r < min((warp + 1) * pw, rows); ++r) {
+                            const int i = a.by_per_kv(r), tok = item.first + i, head = pos.head * a.per_kv + r - i * a.per_kv;
+                            const size_t first = ((size_t)(s.q0 + tok) * heads + head) * a.d;
+                            bool bad = false;
+                            for (int e = lane; e < a.d; e += 32) bad = bad || !(fabsf(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]) <= FLT_MAX);
+                            if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, s, pos.b, tok, head, lane, 0, a.d);
+                        }
+                    }
+                }
+                pos = next_pos<true>(a, s, pos);
+            }
+        }
+    }
+    tc_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_after();
+        tc_dealloc(tmem, kTileColumns);
+    }
+}
+
+namespace {
+
+template <typename T, int NSUB, int SLOTS>
+cudaError_t launch_few(const PromptArgs &a, unsigned blocks, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+{
+    constexpr size_t most = 227 * 1024, fixed = 1024 + (size_t)(SLOTS + 1) * NSUB * kTileRows * 128 + sizeof(FewControl);
+    static_assert(2 * SLOTS + 18 <= 48, "barriers");
+    const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
+    if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
+    const auto kern = prompt_few_kernel<T, NSUB, SLOTS>;
+    static int told[64];
+    const cudaError_t e = tile_allow_smem((const void *)kern, told, most);
+    return e != cudaSuccess ? e : launch_pdl(kern, dim3(blocks), kTileThreads, smem, st, a, km, vm);
+}
+
+}  // namespace
+
+cudaError_t launch_prompt_few(int dtype, const PromptArgs &a, unsigned blocks, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
+{
+    if (dtype == ADSA_BF16) return a.d <= 64 ? launch_few<__nv_bfloat16, 1, 11>(a, blocks, km, vm, st) : launch_few<__nv_bfloat16, 2, 5>(a, blocks, km, vm, st);
+    return a.d <= 64 ? launch_few<__half, 1, 11>(a, blocks, km, vm, st) : launch_few<__half, 2, 5>(a, blocks, km, vm, st);
+}
+
+}  // namespace adsa

@@ -22,119 +22,19 @@
 // later token's V in the same tile: a row that comes out infinite or NaN is made again by one warp from the rows it attends.
 #include <float.h>
 
-#include "adsa_prompt.cuh"
-#include "adsa_tc.cuh"
+#include "adsa_prompt_tile.cuh"
 
 namespace adsa {
 
-constexpr int kTileThreads = 384;           // warps 0 .. 3, 4 .. 7: the groups; 8 copies K and V; 9 issues the products; 10 copies Q; 11 walks
-constexpr int kTileColumns = 512;           // all of tensor memory: S (and P) of the groups at 0 and 128, O at 256 and 384
-constexpr float kTileSlack = 8.f;
-constexpr int kTileRing = 4;                // items ahead
 constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time
-constexpr unsigned kTileMinRun = 6;         // units of a run, at least, where items may be cut
-
-struct TileDesc {                           // an item of a run, as the walking warp finds it
-    PromptSeq s;
-    int b, head, q;
-    int t0, t1;                             // tiles of this run; t1 < 0: no more items
-    int slot;                               // of the partial state; -1: the whole item
-};
-struct TilePos {
-    int b, head, q, tile;
-    __device__ __forceinline__ bool before(const TilePos &o) const
-    {
-        if (b != o.b) return b < o.b;
-        if (head != o.head) return head < o.head;
-        return q != o.q ? q < o.q : tile < o.tile;
-    }
-};
-template <bool WIDE>
-__device__ __forceinline__ TilePos next_pos(const PromptArgs &a, const PromptSeq &s, TilePos pos)
-{
-    pos.tile = 0;
-    if (++pos.q * item_tokens<WIDE>(a) < s.m) return pos;
-    pos.q = 0;
-    if (s.m == 0 || ++pos.head >= a.kv_heads) { pos.head = 0; ++pos.b; }
-    return pos;
-}
+constexpr int kFewMean = 64;                 // query rows per sequence and key head, on the mean, up to which the kernel for few rows runs
 struct TileControl {
     uint64_t bars[42];
     TileDesc ring[kTileRing];
-    TilePos begin, end;                     // of this block's run
+    TilePos ends[2];                        // of this block's run
     uint32_t tmem;
     int limit;                              // polls of a wait before it gives up
 };
-
-__device__ __forceinline__ void tile_tma3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-}
-template <int BYTES>
-__device__ __forceinline__ void tile_copy(uint32_t dst, const void *src)
-{
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
-}
-// where byte x of a row lies in a tile of 128-byte columns in the 128-byte swizzle
-__device__ __forceinline__ uint32_t tile_at(int row, int x, uint32_t sub)
-{
-    return (uint32_t)(x >> 7) * sub + (uint32_t)row * 128u + (uint32_t)((((x >> 4) & 7) ^ (row & 7)) << 4) + (uint32_t)(x & 15);
-}
-__device__ __forceinline__ float tile_max3(float x, float y, float z)
-{
-    float m;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
-    return m;
-}
-// largest of 16, 8, 4 bytes that divides all of these
-__device__ __forceinline__ int piece_of(const void *p, long long token, long long head, int d)
-{
-    const unsigned long long x = (unsigned long long)(uintptr_t)p | (unsigned long long)(token * 2) | (unsigned long long)(head * 2) | (unsigned)(d * 2);
-    return x & 7 ? 4 : x & 15 ? 8 : 16;
-}
-
-// The item that unit u of the list lies in, and the tile that a run beginning there takes first; by a whole warp.
-template <bool WIDE>
-__device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, unsigned u, unsigned tol, int lane)
-{
-    if (u >= plan[a.batch]) return {a.batch, 0, 0, 0};
-    int b = 0;
-    for (int b0 = 0;; b0 += 32) {
-        const int done = __popc(__ballot_sync(0xffffffffu, b0 + lane < a.batch && plan[b0 + lane + 1] <= u));
-        b = b0 + done;
-        if (done < 32) break;
-    }
-    const PromptSeq s = prompt_seq(a, b);
-    const unsigned per_head = (plan[b + 1] - plan[b]) / (unsigned)a.kv_heads;
-    unsigned rem = u - plan[b];
-    const int head = (int)(rem / per_head);
-    rem -= head * per_head;
-    for (int q0 = 0;; q0 += 32) {
-        const bool in = (q0 + lane) * item_tokens<WIDE>(a) < s.m;
-        const TileItem<WIDE> mine(a, s, in ? q0 + lane : 0);
-        const unsigned cost = in ? mine.cost() : 0u;
-        unsigned incl = cost;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
-        const unsigned past = __ballot_sync(0xffffffffu, incl > rem);
-        if (!past && (q0 + 32) * item_tokens<WIDE>(a) < s.m) {
-            rem -= __shfl_sync(0xffffffffu, incl, 31);
-            continue;
-        }
-        const int at = past ? __ffs(past) - 1 : 31;         // (past is never empty here: the plan counted the same items)
-        const unsigned item_cost = __shfl_sync(0xffffffffu, cost, at), off = rem - (__shfl_sync(0xffffffffu, incl, at) - item_cost);
-        const int tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
-        const bool two = __shfl_sync(0xffffffffu, mine.tile_cost(), at) == 2u;
-        const unsigned left = item_cost - off;
-        const bool near = min(off, left) <= tol;
-        int q = q0 + at, tile = near || off <= kTileOver ? 0 : (int)(two ? (off - kTileOver + 1u) / 2u : off - kTileOver);
-        if (near ? off <= left : tile < tiles || tiles == 0) return {b, head, q, tile};
-        if (++q * item_tokens<WIDE>(a) < s.m) return {b, head, q, 0};
-        return head + 1 < a.kv_heads ? TilePos{b, head + 1, 0, 0} : TilePos{b + 1, 0, 0, 0};
-    }
-}
 
 // PLAIN: what calls as a rule are: everything copied by boxes, outputs of 16 bits in 16-byte pieces.  What is left (row copies, other
 // outputs) has a kernel of its own for its code's sake: it slowed this one by 10 to 15%, without being run.
@@ -185,49 +85,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     if (warp == 9) tc_alloc(smem_u32(&c.tmem), kTileColumns);
     pdl_wait();
     pdl_launch();
-    // units of every sequence: short ones by a lane each, long ones by their warp; then their running sum
-    for (int b0 = warp * 32; b0 < a.batch; b0 += kTileThreads) {
-        const int b = b0 + lane;
-        PromptSeq s = {};
-        if (b < a.batch) s = prompt_seq(a, b);
-        const bool many = s.m > 32 * item_tokens<WIDE>(a);
-        unsigned units = 0;
-        if (!many) {
-            for (int q = 0; q * item_tokens<WIDE>(a) < s.m; ++q) units += TileItem<WIDE>(a, s, q).cost();
-        }
-        for (unsigned todo = __ballot_sync(0xffffffffu, many); todo; todo &= todo - 1) {
-            const int src = __ffs(todo) - 1;
-            PromptSeq t = {};
-            t.m = __shfl_sync(0xffffffffu, s.m, src);
-            t.n = __shfl_sync(0xffffffffu, s.n, src);
-            t.p = __shfl_sync(0xffffffffu, s.p, src);
-            unsigned sum = 0;
-            for (int q = lane; q * item_tokens<WIDE>(a) < t.m; q += 32) sum += TileItem<WIDE>(a, t, q).cost();
-            sum = __reduce_add_sync(0xffffffffu, sum);
-            if (lane == src) units = sum;
-        }
-        if (b < a.batch) plan[b + 1] = units * (unsigned)a.kv_heads;
-    }
-    __syncthreads();
-    if (warp == 11) {
-        if (lane == 0) plan[0] = 0;
-        unsigned before = 0;
-        for (int b0 = 0; b0 < a.batch; b0 += 32) {
-            unsigned incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
-            if (b0 + lane < a.batch) plan[b0 + lane + 1] = before + incl;
-            before += __shfl_sync(0xffffffffu, incl, 31);
-        }
-    }
-    __syncthreads();
-    const unsigned total = plan[a.batch], runs = min(max(a.split ? total / kTileMinRun : total, 1u), gridDim.x);
-    if (warp >= 10) {                                              // where this block's run begins and ends
-        const unsigned run = blockIdx.x + (warp - 10);
-        const unsigned u = run > runs ? total : (unsigned)((unsigned long long)run * total / runs);
-        const TilePos at = tile_locate<WIDE>(a, plan, u, a.split ? total / runs / 32u : 0xffffffffu, lane);
-        if (lane == 0) (warp == 10 ? c.begin : c.end) = at;
-    }
+    tile_plan<WIDE>(a, plan, c.ends, warp, lane);
     tc_before();
     __syncthreads();
     tc_after();
@@ -254,48 +112,11 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     };
     // where the elements of a head's row begin in a tile of K or V
     const auto shift_of = [&](int head, bool value) { return !PLAIN && a.shifted ? (int)(head * (value ? a.v_head : a.k_head)) & 7 : 0; };
-    // cached rows of tile t, from its first row on
-    const auto rows_of = [&](const PromptSeq &s, int t) {
-        const int before = (s.p + kTileRows - 1) / kTileRows;
-        return t < before ? s.p - t * kTileRows : s.n - (t - before) * kTileRows;
-    };
 
     // 168 registers a thread at the launch: the groups take what the other four warps leave
     if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {                                              // ---- the list of items ----
-        const unsigned run = blockIdx.x;
-        int4 left = make_int4(-1, 0, 0, 0);                         // {sequence of the item that this run begins and leaves unfinished, key
-                                                                   // head, item; whether an item cut before ends here}
-        const TilePos end = c.end;
-        TilePos pos = c.begin;
-        int have = -1;
-        PromptSeq s = {};
-        while (pos.before(end)) {
-            if (pos.b != have) { s = prompt_seq(a, pos.b); have = pos.b; }
-            if (s.m == 0) { pos = next_pos<WIDE>(a, s, pos); continue; }
-            const TileItem<WIDE> item(a, s, pos.q);
-            const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
-            const int t1 = last ? end.tile : item.tiles;
-            const bool whole = pos.tile == 0 && t1 == item.tiles;
-            if (!whole) {
-                if (pos.tile > 0) left.w = t1 == item.tiles;
-                else left = make_int4(pos.b, pos.head, pos.q, left.w);
-            }
-            wait(d_empty + 8 * at, d_phase ^ 1u);
-            if (lane == 0) {
-                c.ring[at] = {s, pos.b, pos.head, pos.q, pos.tile, t1, whole ? -1 : (int)(2 * run) + (pos.tile > 0 ? 0 : 1)};
-                mbar_arrive(d_full + 8 * at);
-            }
-            if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
-            if (last) break;
-            pos = next_pos<WIDE>(a, s, pos);
-        }
-        wait(d_empty + 8 * at, d_phase ^ 1u);
-        if (lane == 0) {
-            c.ring[at].t1 = -1;
-            mbar_arrive(d_full + 8 * at);
-            if (a.split) a.run_desc[run] = left;
-        }
+        tile_walk<WIDE>(a, c.ends, c.ring, d_full, d_empty, lane, wait);
     } else if (warp == 8) {                                        // ---- copies of K and V ----
         int slot = 0, waiting = 0;                                 // waiting: row copies in flight that nobody knows of yet
         uint32_t phase = 0;
@@ -329,39 +150,33 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 }
             }
         };
-        const auto copy = [&](const TileDesc &it, int t, bool value, int part) {   // a part of K or V of tile t into the next slot
-            const int before = (it.s.p + kTileRows - 1) / kTileRows, valid = min(rows_of(it.s, t), kTileRows);
-            const bool pre = t < before;
-            const int row0 = (pre ? t : t - before) * kTileRows, x0 = part * PSUB * 64;
+        // a part of K or V of tile t into the next slot; y: where the lane's box lies in the pool
+        const auto copy = [&](const TileDesc &it, const TileSource &src, int t, int y, bool value, int part) {
+            const int x0 = part * PSUB * 64;
             const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
+            const CUtensorMap *map = value ? &v_map : &k_map;
             if (!PLAIN && waiting && !mbar_try_wait(empty + 8 * slot, phase ^ 1u)) flush();
             wait(empty + 8 * slot, phase ^ 1u);
-            const int32_t *pages = pre ? a.p_table + (size_t)it.s.group * a.max_p_pages : a.table + (size_t)it.b * a.max_pages;
-            if ((PLAIN || a.box_rows) && a.table) {
-                const int boxes = (valid + a.box_rows - 1) / a.box_rows;
-                if (lane == 0) mbar_expect_tx(bar, (uint32_t)(boxes * a.box_rows) * 128u * PSUB);
+            if (PLAIN || a.box_rows) {
+                if (lane == 0) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
                 __syncwarp();
-                for (int i = lane; i < boxes; i += 32) {
-                    const int row = row0 + i * a.box_rows, page = prompt_page(a, pages, row);
-                    const int y = (page * a.kv_heads + it.head) * a.page_rows + row - a.by_page(row) * a.page_rows;
+                if (a.table) {
+                    for (int i = lane; y >= 0; i += 32, y = i << a.box_shift < kTileRows ? src.pool_row(a, t, i) : -1) {
 #pragma unroll
-                    for (int s = 0; s < PSUB; ++s)
-                        pa_tma(dst + (uint32_t)(i * a.box_rows) * 128u + s * kSub, value ? &v_map : &k_map, x0 + s * 64, y, bar);
-                }
-            } else if (PLAIN || a.box_rows) {
-                if (lane == 0) {
-                    mbar_expect_tx(bar, kSlot);
-                    const int tok = (int)it.s.k0 + row0, shift = shift_of(it.head, value);
+                        for (int s = 0; s < PSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, x0 + s * 64, y, bar);
+                    }
+                } else if (lane == 0) {
+                    const int tok = src.tok + src.row0(t);
                     const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
 #pragma unroll
                     for (int s = 0; s < PSUB; ++s) {
-                        if (!PLAIN && a.shifted) pa_tma(dst + s * kSub, value ? &v_map : &k_map, (int)(it.head * (value ? a.v_head : a.k_head)) - shift + s * 64, tok, bar);
-                        else tile_tma3(dst + s * kSub, value ? &v_map : &k_map, x0 + s * 64, tf ? tok : it.head, tf ? it.head : tok, bar);
+                        if (!PLAIN && a.shifted) pa_tma(dst + s * kSub, map, (int)(src.head * (value ? a.v_head : a.k_head)) - shift_of(src.head, value) + s * 64, tok, bar);
+                        else tile_tma3(dst + s * kSub, map, x0 + s * 64, tf ? tok : src.head, tf ? src.head : tok, bar);
                     }
                 }
-                __syncwarp();
             } else if constexpr (!PLAIN) {
-                const int piece = value ? v_piece : k_piece;
+                const int piece = value ? v_piece : k_piece, valid = src.valid(t), row0 = src.row0(t);
+                const bool pre = t < src.before;
                 if (piece == 16) by_rows(std::integral_constant<int, 16>(), it, pre, row0, x0, valid, dst, value);
                 else if (piece == 8) by_rows(std::integral_constant<int, 8>(), it, pre, row0, x0, valid, dst, value);
                 else by_rows(std::integral_constant<int, 4>(), it, pre, row0, x0, valid, dst, value);
@@ -375,13 +190,23 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (!have_item()) break;
             const TileDesc &it = c.ring[at];
             const bool turns = !WIDE && it.s.m - it.q * item_tokens<WIDE>(a) <= a.half_tokens;
-            const int ahead = turns ? 2 : 1, n = it.t1 - it.t0;
+            const TileSource src(a, it);
+            const int ahead = turns ? 2 : 1, t0 = it.t0, n = it.t1 - t0;
+            const auto copy_tile = [&](int t, int y, bool value) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) copy(it, src, t0 + t, y, value, p);
+            };
+            // V lies where K does: y0 of tile i, y1 of the next (where the groups take turns, y2 of the one after it)
+            int y0 = n > 0 ? src.pool_row(a, t0, lane) : -1, y1 = n > 1 ? src.pool_row(a, t0 + 1, lane) : -1;
 #pragma unroll 1
-            for (int i = 0; i < 2 * n * PARTS; ++i) {
-                const int j = i / PARTS;                           // K of the first tiles; V and K in turn; V of the last
-                const bool value = j >= min(ahead, n) && (j >= 2 * n - ahead || ((j - ahead) & 1) == 0);
-                const int tile = !value ? (j < ahead ? j : (j - ahead) / 2 + ahead) : j >= 2 * n - ahead ? j - n : (j - ahead) / 2;
-                copy(it, it.t0 + tile, value, i % PARTS);
+            for (int i = -ahead; i < n; ++i) {
+                const int next = i + ahead, y2 = turns && i >= 0 && next < n ? src.pool_row(a, t0 + next, lane) : -1;
+                if (i >= 0) copy_tile(i, y0, true);
+                if (next < n) copy_tile(next, i < 0 ? (next == 0 ? y0 : y1) : turns ? y2 : y1, false);
+                if (i >= 0) {
+                    y0 = y1;
+                    y1 = turns ? y2 : next + 1 < n ? src.pool_row(a, t0 + next + 1, lane) : -1;
+                }
             }
             next_item();
         }
@@ -460,8 +285,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 }
             }
         };
-        const auto take_v = [&](const TileDesc &it, int t) {                           // V of tile t, or a part of it
-            const int taken = take(), valid = __shfl_sync(0xffffffffu, rows_of(it.s, t), 0);
+        const auto take_v = [&](int valid) {                           // V of tile t, or a part of it
+            const int taken = take();
             if (valid < kTileRows) {
                 // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN
                 const uint32_t v_at = ring + (uint32_t)taken * kSlot;
@@ -503,7 +328,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             // (shuffled, so that the compiler knows them to be uniform)
-            const int t0 = __shfl_sync(0xffffffffu, it.t0, 0), n = __shfl_sync(0xffffffffu, it.t1, 0) - t0;
+            const int t0 = __shfl_sync(0xffffffffu, it.t0, 0), n = __shfl_sync(0xffffffffu, it.t1, 0) - t0, p_rows = __shfl_sync(0xffffffffu, it.s.p, 0),
+                      own_rows = __shfl_sync(0xffffffffu, it.s.n, 0), before = (p_rows + kTileRows - 1) / kTileRows;
             if (n == 0) continue;
             const TileItem<WIDE> item(a, it.s, it.q);
             const bool pair = __shfl_sync(0xffffffffu, (int)item.pair, 0);
@@ -528,8 +354,9 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 const bool takes = turns || g == 0, leaves = turns || g == 1;
                 if (j >= 0) {
                     if (takes) {
+                        const int t = t0 + j, valid = t < before ? p_rows - t * kTileRows : own_rows - (t - before) * kTileRows;
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) v[p] = take_v(it, t0 + j);
+                        for (int p = 0; p < PARTS; ++p) v[p] = take_v(valid);
                     }
                     if (j < mine) {
                         weigh(g, WIDE && g == 1 ? v[PARTS - 1] : v[0], j < ahead);
@@ -572,14 +399,15 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const bool there = in < tph && in + half * tph < item.count;
             const int own = it.s.seen(min(tok, it.s.m - 1), a.causal), before = (it.s.p + kTileRows - 1) / kTileRows;
             const bool warp_there = __any_sync(0xffffffffu, there);
-            int tiles = it.t1 - it.t0;
+            const int p_rows = it.s.p, t0 = it.t0;
+            int tiles = it.t1 - t0;
             if (turns) tiles = (tiles + 1 - g) / 2;
             else if (item.pair && g == 0) tiles = min(max(tiles_until(a, it.s, item.first + tph - 1) - it.t0, 0), tiles);
             float m = -INFINITY;                                   // raw units; the row's weights are relative to it
             float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             for (int i = 0; i < tiles; ++i) {
-                const int t = it.t0 + (turns ? 2 * i + g : i);
-                const int valid = t < before ? it.s.p - t * kTileRows : own - (t - before) * kTileRows;   // rows of the tile that this row attends
+                const int t = t0 + (turns ? 2 * i + g : i);
+                const int valid = t < before ? p_rows - t * kTileRows : own - (t - before) * kTileRows;   // rows of the tile that this row attends
                 wait(my_s, s_phase);
                 s_phase ^= 1u;
                 tc_after();
@@ -798,8 +626,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         // Rows that came out infinite or NaN, from what they attend alone: the run once more, in whole items.  (A call in the loop above
         // cost it 8%.)
         if (__any_sync(0xffffffffu, again)) {
-            const TilePos end = c.end;
-            for (TilePos pos = c.begin; pos.before(end); pos.tile = 0) {
+            const TilePos end = c.ends[1];
+            for (TilePos pos = c.ends[0]; pos.before(end); pos.tile = 0) {
                 const PromptSeq s = prompt_seq(a, pos.b);
                 if (s.m > 0) {
                     const TileItem<WIDE> item(a, s, pos.q);
@@ -833,11 +661,11 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
 // Joins the states of items that runs have cut: a warp per row, blocks (cut, eight rows).  The run that began such an item
 // names it; the runs behind it have one state each, up to the one that ended the item.
 constexpr int kTileMergeThreads = 256;
-template <typename T, int NSUB>
+template <typename T, int NSUB, bool FEW>
 __global__ void __launch_bounds__(kTileMergeThreads)
 prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
 {
-    constexpr bool WIDE = NSUB > 2;
+    constexpr bool WIDE = NSUB > 2;                                // (the kernel for few rows: items of one half of up to 64 rows)
     constexpr int DO = WIDE ? 128 : 64 * NSUB, PER = DO / 32, AHEAD = 4;
     const int lane = threadIdx.x & 31, r = (int)blockIdx.y * (kTileMergeThreads / 32) + (threadIdx.x >> 5);
     pdl_wait();
@@ -846,7 +674,7 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     const int4 d = a.run_desc[lead];
     if (d.x < 0) return;
     const PromptSeq s = prompt_seq(a, d.x);
-    const TileItem<WIDE> item(a, s, d.z);
+    const TileItem<WIDE || FEW> item(a, s, d.z);
     const int half = r >> 7, tph = a.half_tokens, in = a.by_per_kv(r & 127), in_item = in + (WIDE ? 0 : half * tph);
     if (in >= tph || in_item >= item.count || (half && !WIDE && !item.pair)) return;
     int pieces = 2;
@@ -966,6 +794,12 @@ bool page_map(CUtensorMap *m, int dtype, const PromptArgs &a, const void *pool, 
     return encode(m, dtype, 2, pool, dims, strides, box);
 }
 
+template <typename T, int NSUB, bool FEW>
+cudaError_t launch_merge(const PromptArgs &a, unsigned blocks, cudaStream_t st)
+{
+    return launch_pdl(prompt_tile_merge_kernel<T, NSUB, FEW>, dim3(blocks - 1, (FEW ? kFewRows : 256) / (kTileMergeThreads / 32)), kTileMergeThreads, 0, st, a, (int)blocks);
+}
+
 template <typename T, int NSUB, int SLOTS, bool PLAIN>
 cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
@@ -976,18 +810,11 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap
     if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
     const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, PLAIN>;
     static int told[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    cudaError_t e = tile_allow_smem((const void *)kern, told, most);
     if (e != cudaSuccess) return e;
-    const bool known = dev >= 0 && dev < 64;
-    if (!known || !__atomic_load_n(&told[dev], __ATOMIC_ACQUIRE)) {
-        e = cudaFuncSetAttribute((const void *)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
-        if (e != cudaSuccess) return e;
-        if (known) __atomic_store_n(&told[dev], 1, __ATOMIC_RELEASE);
-    }
     e = launch_pdl(kern, dim3(blocks), kTileThreads, smem, st, a, qm, km, vm);
     if (e != cudaSuccess || !a.split || blocks < 2) return e;
-    return launch_pdl(prompt_tile_merge_kernel<T, NSUB>, dim3(blocks - 1, 256 / (kTileMergeThreads / 32)), kTileMergeThreads, 0, st, a, (int)blocks);
+    return launch_merge<T, NSUB, false>(a, blocks, st);
 }
 template <typename T, bool PLAIN>
 cudaError_t launch_tiles_type(const PromptArgs &a, unsigned blocks, const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
@@ -1015,11 +842,12 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
         int box = kTileRows;
         while (a.page_rows % box) box /= 2;                        // the largest power of two that divides a page: boxes never straddle two
         if (page_map(&km, dtype, a, a.k, box) && page_map(&vm, dtype, a, a.v, box)) a.box_rows = box;
+        while (1 << a.box_shift < box) ++a.box_shift;
     } else {
         bool kt = false, vt = false;
         if (rows_map(&km, dtype, a.k, a.d, a.kv_heads, a.k_head, a.n_k, a.k_token, 1, kTileRows, &kt) &&
             rows_map(&vm, dtype, a.v, a.d, a.kv_heads, a.v_head, a.n_k, a.v_token, 1, kTileRows, &vt)) {
-            a.box_rows = kTileRows;
+            a.box_rows = kTileRows;                                // (the shift is a pool's)
             a.tokens_first = (kt ? 2 : 0) | (vt ? 4 : 0);
         } else if ((a.d <= 58 || (a.d > 64 && a.d <= 112)) && shifted_map(&km, dtype, a.k, a.d, a.kv_heads, a.k_head, a.n_k, a.k_token) &&
                    shifted_map(&vm, dtype, a.v, a.d, a.kv_heads, a.v_head, a.n_k, a.v_token)) {
@@ -1028,8 +856,16 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
             a.q_boxes = 0;                                         // (q has to lie where the head's elements do, between zeros)
         }
     }
-    const bool plain = a.q_boxes && a.box_rows && !a.shifted && a.out && !a.out_f32 && a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0;
     const unsigned blocks = (unsigned)sms;
+    // Few rows a sequence on the mean: {rows measured}
+    if (a.box_rows && !a.shifted && a.d <= 128 && a.n_q * a.per_kv <= (long long)kFewMean * a.batch) {
+        a.half_tokens = kFewRows / a.per_kv;
+        const cudaError_t e = launch_prompt_few(dtype, a, blocks, km, vm, st);
+        if (e != cudaSuccess || !a.split || blocks < 2) return e;
+        if (dtype == ADSA_BF16) return a.d <= 64 ? launch_merge<__nv_bfloat16, 1, true>(a, blocks, st) : launch_merge<__nv_bfloat16, 2, true>(a, blocks, st);
+        return a.d <= 64 ? launch_merge<__half, 1, true>(a, blocks, st) : launch_merge<__half, 2, true>(a, blocks, st);
+    }
+    const bool plain = a.q_boxes && a.box_rows && !a.shifted && a.out && !a.out_f32 && a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0;
     if (dtype == ADSA_BF16) return plain ? launch_tiles_type<__nv_bfloat16, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__nv_bfloat16, false>(a, blocks, qm, km, vm, st);
     return plain ? launch_tiles_type<__half, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__half, false>(a, blocks, qm, km, vm, st);
 }
