@@ -1,9 +1,9 @@
 // Attention of few query rows per sequence (single tokens, guesses to be checked, a row of a grid) over packed rows or a paged
 // cache: what the tile kernel does, laid out for calls whose time is that of reading the cache.
 //
-// An item has up to 64 query rows of a key head.  They are spread over a 128-row tile of Q so that each of a group's four warps has
-// 8 of them (16 of more than 32), and a warp takes its scores from tensor memory four lanes to a row: 32 or 64 exponentials a thread and
-// tile for all 128 cached rows, on all four parts of an SM, where a row per thread takes 128 on as many parts as have rows.  The two groups
+// An item has up to 32 query rows of a key head.  They are spread over a 128-row tile of Q so that each of a group's four warps has
+// 8 of them, and a warp takes its scores from tensor memory four lanes to a row: 32 exponentials a thread and tile for all 128 cached
+// rows, on all four parts of an SM, where a row per thread takes 128 on as many parts as have rows.  The two groups
 // take the tiles in turns, so that one's products run under the other's softmax, and join their states at the end.  Q takes half of what
 // two halves take and outputs go straight to memory: the ring of tiles has the rest, 160 to 192 KB.
 //
@@ -96,8 +96,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     const auto wait = [&](uint32_t bar, uint32_t parity) {
         for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
             if (polls < *(volatile int *)&c.limit) continue;
-            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short)
-            if (a.status) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short; reported at the end)
             break;
         }
     };
@@ -112,9 +111,6 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         wait(d_full + 8 * at, d_phase);
         return c.ring[at].t1 >= 0;
     };
-    // where query row r of an item of `rows` lies: 8 or 16 to a warp
-    const auto per_warp = [](int rows) { return rows <= 32 ? 8 : 16; };
-
     if (warp == 11) {                                              // ---- the list of items ----
         tile_walk<true>(a, c.ends, c.ring, d_full, d_empty, lane, wait);
     } else if (warp == 8) {                                        // ---- copies of K and V ----
@@ -124,35 +120,43 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             const TileDesc &it = c.ring[at];
             const TileSource src(a, it);
             const int t0 = it.t0, n = it.t1 - t0;
-            const auto copy = [&](const CUtensorMap *map, int t, int y, bool value) {
+            // K0 K1 V0 K2 V1 K3 .., in the order the products take them; V lies where K does
+            int k_next = 0, v_next = 0, y_last = -1, y_before = -1;   // pool rows of this lane's box in the last K and the one before it
+#pragma unroll 1
+            for (int j = 0; j < 2 * n; ++j) {
+                const bool value = k_next == n || k_next - v_next == 2;
+                const int t = t0 + (value ? v_next : k_next);
+                int y = k_next - v_next == 2 ? y_before : y_last;
+                if (!value) {
+                    y = src.pool_row(a, t, lane);
+                    y_before = y_last;
+                    y_last = y;
+                }
+                (value ? v_next : k_next) += 1;
                 const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
+                const CUtensorMap *map = value ? &v_map : &k_map;
                 wait(empty + 8 * slot, phase ^ 1u);
-                if (lane == 0) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
+                if (tc_elect()) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
                 __syncwarp();
                 if (a.table) {
-                    for (int i = lane; y >= 0; i += 32, y = i << a.box_shift < kTileRows ? src.pool_row(a, t, i) : -1) {
+                    // one lane issues for all: a copy by several lanes at a time is issued lane by lane too, with more ado
+#pragma unroll 1
+                    for (int i = 0; i << a.box_shift < src.valid(t); ++i) {
+                        if (i && (i & 31) == 0) y = src.pool_row(a, t, i + lane);
+                        const int row = __shfl_sync(0xffffffffu, y, i & 31);
+                        if (tc_elect()) {
 #pragma unroll
-                        for (int s = 0; s < NSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, s * 64, y, bar);
+                            for (int s = 0; s < NSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, s * 64, row, bar);
+                        }
                     }
-                } else if (lane == 0) {
+                } else if (tc_elect()) {
                     const int tok = src.tok + src.row0(t);
                     const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
 #pragma unroll
                     for (int s = 0; s < NSUB; ++s) tile_tma3(dst + s * kSub, map, s * 64, tf ? tok : src.head, tf ? src.head : tok, bar);
                 }
+                __syncwarp();
                 if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
-            };
-            // K0 K1 V0 K2 V1 K3 .., in the order the products take them; V lies where K does
-            int y0 = n > 0 ? src.pool_row(a, t0, lane) : -1, y1 = n > 1 ? src.pool_row(a, t0 + 1, lane) : -1;
-            if (n > 0) copy(&k_map, t0, y0, false);
-            if (n > 1) copy(&k_map, t0 + 1, y1, false);
-#pragma unroll 1
-            for (int i = 0; i < n; ++i) {
-                const int y2 = i + 2 < n ? src.pool_row(a, t0 + i + 2, lane) : -1;
-                copy(&v_map, t0 + i, y0, true);
-                if (i + 2 < n) copy(&k_map, t0 + i + 2, y2, false);
-                y0 = y1;
-                y1 = y2;
             }
         }
     } else if (warp == 10) {                                       // ---- copies of Q ----
@@ -162,23 +166,24 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             const TileDesc &it = c.ring[at];
             if (it.t1 == it.t0) continue;
             const TileItem<true> item(a, it.s, it.q);
-            const int rows = item.count * a.per_kv, pw = per_warp(rows);
+            const int rows = item.count * a.per_kv;
             const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + item.first) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
             wait(q_empty, phase ^ 1u);
             phase ^= 1u;
-            const auto by_rows = [&](auto piece_) {
-                constexpr int piece = decltype(piece_)::value;
 #pragma unroll 1
-                for (int r0 = 0; r0 < rows; r0 += 4) {
-                    const int r = r0 + (lane >> 3), t = a.by_per_kv(r), m = r / pw * 32 + r % pw;
-                    const unsigned char *from = src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head);
-                    if (r < rows)
-                        for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(q_at + tile_at(m, x, kSub), from + x);
+            for (int r0 = 0; r0 < rows; r0 += 4) {
+                const int r = r0 + (lane >> 3), t = a.by_per_kv(r), m = (r >> 3) * 32 + (r & 7);
+                const unsigned char *from = src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head);
+                if (r < rows) {
+#pragma unroll 1
+                    for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) {
+                        const uint32_t to = q_at + tile_at(m, x, kSub);
+                        if (piece == 16) tile_copy<16>(to, from + x);
+                        else if (piece == 8) tile_copy<8>(to, from + x);
+                        else tile_copy<4>(to, from + x);
+                    }
                 }
-            };
-            if (piece == 16) by_rows(std::integral_constant<int, 16>());
-            else if (piece == 8) by_rows(std::integral_constant<int, 8>());
-            else by_rows(std::integral_constant<int, 4>());
+            }
             asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -254,64 +259,50 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             }
         }
     } else if (warp < 8) {                                         // ---- four lanes to a query row ----
-        const int g = warp >> 2, in_row = lane >> 2, col = 2 * (lane & 3);
+        const int g = warp >> 2, col = 2 * (lane & 3), row = (warp & 3) * 8 + (lane >> 2);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
-        const int heads = a.kv_heads * a.per_kv;
+        const int in = a.by_per_kv(row), in_head = row - in * a.per_kv;   // token in the item, head in the key head's
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
         bool again = false;                                        // a row came out infinite or NaN
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<true> item(a, it.s, it.q);
-            const int rows = item.count * a.per_kv, pw = per_warp(rows), row0 = (warp & 3) * pw;
-            const bool both = pw == 16, warp_there = row0 < rows;  // both: rows t / 4 and t / 4 + 8 of the warp
-            int row[2], own[2];
-            bool there[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                row[h] = row0 + in_row + 8 * h;
-                there[h] = row[h] < rows && (h == 0 || both);
-                own[h] = it.s.seen(min(item.first + a.by_per_kv(row[h]), it.s.m - 1), a.causal);
-            }
+            const bool there = row < item.count * a.per_kv, warp_there = (warp & 3) * 8 < item.count * a.per_kv;
+            const int own = it.s.seen(min(item.first + in, it.s.m - 1), a.causal);
             const int p_rows = it.s.p, before = (p_rows + kTileRows - 1) / kTileRows, t0 = it.t0, n = it.t1 - t0, tiles = (n + 1 - g) / 2;
-            float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // (l: this lane's part of the row's sum)
+            float m = -INFINITY, l = 0.f;                          // (l: this lane's part of the row's sum)
+#pragma unroll 1
             for (int i = 0; i < tiles; ++i) {
                 const int t = t0 + 2 * i + g;
                 wait(s_full + 8 * g, s_phase);
                 s_phase ^= 1u;
                 tc_after();
-                if (!warp_there) {
-                    tc_before();
-                    if (lane == 0) mbar_arrive(p_full + 8 * g);
-                    continue;
-                }
-                alignas(8) float v[4][16];
+                if (warp_there) {
+                    float v[4][16];                                // (of 16 rows, 8 of them the item's: v[.][4 x], v[.][4 x + 1])
 #pragma unroll
-                for (int x = 0; x < 4; ++x) few_load4(s_col + 32 * x, v[x]);
-                tc_load_wait();
-                uint32_t p[2][16];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1 && !both) break;
-                    const int valid = (t < before ? p_rows - t * kTileRows : own[h] - (t - before) * kTileRows) - col;   // from this lane's first column on
+                    for (int x = 0; x < 4; ++x) few_load4(s_col + 32 * x, v[x]);
+                    tc_load_wait();
+                    const int valid = (t < before ? p_rows - t * kTileRows : own - (t - before) * kTileRows) - col;   // from this lane's first column on
                     if (__any_sync(0xffffffffu, valid < kTileRows)) {
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
-                            float *w = &v[x / 4][4 * (x % 4) + 2 * h];
+                            float *w = &v[x / 4][4 * (x % 4)];
                             w[0] = 8 * x < valid ? w[0] : -INFINITY;
                             w[1] = 8 * x + 1 < valid ? w[1] : -INFINITY;
                         }
                     }
-                    float mx = -INFINITY;
+                    float mx2[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) mx = tile_max3(mx, v[x / 4][4 * (x % 4) + 2 * h], v[x / 4][4 * (x % 4) + 2 * h + 1]);
+                    for (int x = 0; x < 16; ++x) mx2[x & 1] = tile_max3(mx2[x & 1], v[x / 4][4 * (x % 4)], v[x / 4][4 * (x % 4) + 1]);
+                    float mx = fmaxf(mx2[0], mx2[1]);
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    const bool move = (mx - m[h]) * a.scale_log2e > kTileSlack || m[h] == -INFINITY;
+                    const bool move = (mx - m) * a.scale_log2e > kTileSlack || m == -INFINITY;
                     if (__any_sync(0xffffffffu, move)) {
-                        const float m_new = move ? fmaxf(m[h], mx) : m[h];
-                        const float corr = m_new == -INFINITY || m[h] == -INFINITY ? (m[h] == m_new ? 1.f : 0.f) : pa_exp2((m[h] - m_new) * a.scale_log2e);
-                        m[h] = m_new;
-                        l[h] *= corr;
+                        const float m_new = move ? fmaxf(m, mx) : m;
+                        const float corr = m_new == -INFINITY || m == -INFINITY ? (m == m_new ? 1.f : 0.f) : pa_exp2((m - m_new) * a.scale_log2e);
+                        m = m_new;
+                        l *= corr;
                         if (i > 0) {                               // the products before this tile's are complete: their S is
 #pragma unroll 1
                             for (int x = 0; x < DO; x += 32) {
@@ -319,32 +310,29 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                                 few_load4(o_col + x, o);
                                 tc_load_wait();
 #pragma unroll
-                                for (int k = 0; k < 16; ++k)
-                                    if ((k >> 1 & 1) == h) o[k] *= corr;
+                                for (int k = 0; k < 16; k += 4) { o[k] *= corr; o[k + 1] *= corr; }
                                 few_store4(o_col + x, o);
                             }
                         }
                     }
-                    const float shift = kBias - (m[h] == -INFINITY ? 0.f : m[h]) * a.scale_log2e;
-                    float2 sum = make_float2(0.f, 0.f);
+                    const float shift = kBias - (m == -INFINITY ? 0.f : m) * a.scale_log2e;
+                    const float2 scale2 = make_float2(a.scale_log2e, a.scale_log2e), shift2 = make_float2(shift, shift);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    uint32_t p[2][16];
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
-                        float2 w = fma2(make_float2(v[x / 4][4 * (x % 4) + 2 * h], v[x / 4][4 * (x % 4) + 2 * h + 1]), make_float2(a.scale_log2e, a.scale_log2e),
-                                        make_float2(shift, shift));
+                        float2 w = fma2(make_float2(v[x / 4][4 * (x % 4)], v[x / 4][4 * (x % 4) + 1]), scale2, shift2);
                         w.x = pa_exp2(w.x);
                         w.y = pa_exp2(w.y);
-                        sum = add2(sum, w);                        // the sum takes the weights before they are rounded
-                        p[x / 8][2 * (x % 8) + h] = pack2<T>(w.x, w.y);
+                        sum[x & 1] = add2(sum[x & 1], w);          // the sum takes the weights before they are rounded
+                        p[x / 8][2 * (x % 8)] = pack2<T>(w.x, w.y);
+                        p[x / 8][2 * (x % 8) + 1] = 0u;
                     }
-                    l[h] += sum.x + sum.y;
+                    l += sum[0].x + sum[0].y + sum[1].x + sum[1].y;
+                    few_store_pairs(s_col, p[0]);                  // over scores that are in registers by now
+                    few_store_pairs(s_col + 32, p[1]);
+                    tc_store_wait();
                 }
-                if (!both) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) p[x / 8][2 * (x % 8) + 1] = 0u;
-                }
-                few_store_pairs(s_col, p[0]);                      // over scores that are in registers by now
-                few_store_pairs(s_col + 32, p[1]);
-                tc_store_wait();
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + 8 * g);
@@ -354,17 +342,12 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 o_phase ^= 1u;
                 tc_after();
             }
-            // each row's state: O (in tensor memory) and l relative to 2^m2
-            float m2[2], w0[2], w1[2];
-            const bool partial = it.slot >= 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-                m2[h] = m[h] == -INFINITY ? -INFINITY : m[h] * a.scale_log2e - kBias;
-                if (g == 1 && there[h] && (lane & 3) == 0) c.ml[row[h]] = make_float2(m2[h], l[h]);
-            }
+            // the row's state: O (in tensor memory) and l relative to 2^m2
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
+            float m2 = m == -INFINITY ? -INFINITY : m * a.scale_log2e - kBias;
             if (g == 1) {
+                if ((lane & 3) == 0) c.ml[row] = make_float2(m2, l);
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(m_full);
@@ -376,28 +359,25 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             wait(m_full, m_phase);
             m_phase ^= 1u;
             tc_after();
-            int to[2];                                             // row of the output, or -1
-            bool none[2], bad = false;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                w0[h] = 1.f;
-                w1[h] = 0.f;
-                if (n > 1 && there[h]) {
-                    const float2 other = c.ml[row[h]];
-                    const float M = fmaxf(m2[h], other.x);
-                    w0[h] = m2[h] == -INFINITY ? 0.f : pa_exp2(m2[h] - M);
-                    w1[h] = other.x == -INFINITY ? 0.f : pa_exp2(other.x - M);
-                    l[h] = l[h] * w0[h] + other.y * w1[h];
-                    m2[h] = M;
-                }
-                none[h] = it.s.p + own[h] == 0;
-                if (!partial) { w0[h] *= 1.f / l[h]; w1[h] *= 1.f / l[h]; }
-                const int tok = a.by_per_kv(row[h]);
-                to[h] = there[h] ? (int)((it.s.q0 + item.first + tok) * heads + it.head * a.per_kv + row[h] - tok * a.per_kv) : -1;
-                if (there[h] && (lane & 3) == 0) {
-                    if (partial) *reinterpret_cast<float2 *>(a.state_ml + 2 * ((size_t)it.slot * 256 + row[h])) = make_float2(m2[h], l[h]);
-                    else if (a.lse) a.lse[to[h]] = none[h] ? -INFINITY : (m2[h] + log2f(l[h])) * 0.693147180559945309f;
-                }
+            const bool partial = it.slot >= 0, none = p_rows + own == 0, two = n > 1;
+            float w0 = 1.f, w1 = 0.f;
+            if (two) {
+                const float2 other = c.ml[row];
+                const float M = fmaxf(m2, other.x);
+                w0 = m2 == -INFINITY ? 0.f : pa_exp2(m2 - M);
+                w1 = other.x == -INFINITY ? 0.f : pa_exp2(other.x - M);
+                l = l * w0 + other.y * w1;
+                m2 = M;
+            }
+            if (!partial) {
+                const float inv = 1.f / l;
+                w0 *= inv;
+                w1 *= inv;
+            }
+            const size_t to = (size_t)(it.s.q0 + item.first + in) * (a.kv_heads * a.per_kv) + it.head * a.per_kv + in_head;
+            if (there && (lane & 3) == 0) {
+                if (partial) *reinterpret_cast<float2 *>(a.state_ml + 2 * ((size_t)it.slot * 256 + row)) = make_float2(m2, l);
+                else if (a.lse) a.lse[to] = none ? -INFINITY : (m2 + log2f(l)) * 0.693147180559945309f;
             }
             if (warp_there) {
 #pragma unroll 1
@@ -406,30 +386,27 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
 #pragma unroll
                     for (int k = 0; k < 16; ++k) o[k] = o1[k] = 0.f;
                     if (tiles > 0) few_load4(o_col + x0, o);
-                    if (n > 1) few_load4(o_col + 128 + x0, o1);
+                    if (two) few_load4(o_col + 128 + x0, o1);
                     tc_load_wait();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int x = x0 + 8 * i + col;
-                            if (to[h] < 0 || x >= a.d) continue;
-                            float2 y = make_float2(o[4 * i + 2 * h] * w0[h], o[4 * i + 2 * h + 1] * w0[h]);
-                            if (n > 1) y = make_float2(fmaf(o1[4 * i + 2 * h], w1[h], y.x), fmaf(o1[4 * i + 2 * h + 1], w1[h], y.y));
+                        const int x = x0 + 8 * i + col;
+                        float2 y = make_float2(o[4 * i] * w0, o[4 * i + 1] * w0);
+                        if (two) y = make_float2(fmaf(o1[4 * i], w1, y.x), fmaf(o1[4 * i + 1], w1, y.y));
+                        if (none) y = make_float2(0.f, 0.f);
+                        if (there && x < a.d) {
                             if (partial) {
-                                *reinterpret_cast<float2 *>(a.state + ((size_t)it.slot * (DO / 4) + x / 4) * 1024 + row[h] * 4 + x % 4) = y;
-                                continue;
+                                *reinterpret_cast<float2 *>(a.state + ((size_t)it.slot * (DO / 4) + x / 4) * 1024 + row * 4 + x % 4) = y;
+                            } else {
+                                again = again || !(fabsf(y.x) + fabsf(y.y) <= FLT_MAX);
+                                if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + to * a.d + x) = pack2<T>(y.x, y.y);
+                                if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + to * a.d + x) = y;
                             }
-                            if (none[h]) y = make_float2(0.f, 0.f);
-                            bad = bad || !(fabsf(y.x) <= FLT_MAX) || !(fabsf(y.y) <= FLT_MAX);
-                            if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + (size_t)to[h] * a.d + x) = pack2<T>(y.x, y.y);
-                            if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + (size_t)to[h] * a.d + x) = y;
                         }
                     }
                     __syncwarp();
                 }
             }
-            again = again || bad;
             tc_before();                                           // read before the next item's products write O
             __syncwarp();
             if (lane == 0) mbar_arrive(m_empty);
@@ -442,11 +419,11 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 if (s.m > 0) {
                     const TileItem<true> item(a, s, pos.q);
                     const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
-                    const int rows = item.count * a.per_kv, pw = per_warp(rows);
+                    const int rows = item.count * a.per_kv;
                     if (pos.tile == 0 && (!last || end.tile == item.tiles)) {
-                        for (int r = warp * pw; r < min((warp + 1) * pw, rows); ++r) {
+                        for (int r = warp * 8; r < min((warp + 1) * 8, rows); ++r) {
                             const int i = a.by_per_kv(r), tok = item.first + i, head = pos.head * a.per_kv + r - i * a.per_kv;
-                            const size_t first = ((size_t)(s.q0 + tok) * heads + head) * a.d;
+                            const size_t first = ((size_t)(s.q0 + tok) * (a.kv_heads * a.per_kv) + head) * a.d;
                             bool bad = false;
                             for (int e = lane; e < a.d; e += 32) bad = bad || !(fabsf(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]) <= FLT_MAX);
                             if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, s, pos.b, tok, head, lane, 0, a.d);
@@ -459,6 +436,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     }
     tc_before();
     __syncthreads();
+    if (tid == 0 && a.status && c.limit != kCopySpinLimit) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
     if (warp == 9) {
         tc_after();
         tc_dealloc(tmem, kTileColumns);

@@ -27,7 +27,7 @@
 namespace adsa {
 
 constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time
-constexpr int kFewMean = 64;                 // query rows per sequence and key head, on the mean, up to which the kernel for few rows runs
+constexpr int kFewMean = 32;                 // query rows per sequence and key head, on the mean, up to which the kernel for few rows runs
 struct TileControl {
     uint64_t bars[42];
     TileDesc ring[kTileRing];
@@ -94,8 +94,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     const auto wait = [&](uint32_t bar, uint32_t parity) {
         for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
             if (polls < *(volatile int *)&c.limit) continue;
-            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short)
-            if (a.status) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short; reported at the end)
             break;
         }
     };
@@ -158,14 +157,19 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             if (!PLAIN && waiting && !mbar_try_wait(empty + 8 * slot, phase ^ 1u)) flush();
             wait(empty + 8 * slot, phase ^ 1u);
             if (PLAIN || a.box_rows) {
-                if (lane == 0) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
+                if (tc_elect()) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
                 __syncwarp();
                 if (a.table) {
-                    for (int i = lane; y >= 0; i += 32, y = i << a.box_shift < kTileRows ? src.pool_row(a, t, i) : -1) {
+                    // one lane issues for all: a copy by several lanes at a time is issued lane by lane too, with more ado
+                    for (int i = 0; i << a.box_shift < src.valid(t); ++i) {
+                        if (i && (i & 31) == 0) y = src.pool_row(a, t, i + lane);
+                        const int row = __shfl_sync(0xffffffffu, y, i & 31);
+                        if (tc_elect()) {
 #pragma unroll
-                        for (int s = 0; s < PSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, x0 + s * 64, y, bar);
+                            for (int s = 0; s < PSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, x0 + s * 64, row, bar);
+                        }
                     }
-                } else if (lane == 0) {
+                } else if (tc_elect()) {
                     const int tok = src.tok + src.row0(t);
                     const bool tf = a.tokens_first >> (value ? 2 : 1) & 1;
 #pragma unroll
@@ -174,6 +178,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                         else tile_tma3(dst + s * kSub, map, x0 + s * 64, tf ? tok : src.head, tf ? src.head : tok, bar);
                     }
                 }
+                __syncwarp();
             } else if constexpr (!PLAIN) {
                 const int piece = value ? v_piece : k_piece, valid = src.valid(t), row0 = src.row0(t);
                 const bool pre = t < src.before;
@@ -192,21 +197,20 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const bool turns = !WIDE && it.s.m - it.q * item_tokens<WIDE>(a) <= a.half_tokens;
             const TileSource src(a, it);
             const int ahead = turns ? 2 : 1, t0 = it.t0, n = it.t1 - t0;
-            const auto copy_tile = [&](int t, int y, bool value) {
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) copy(it, src, t0 + t, y, value, p);
-            };
-            // V lies where K does: y0 of tile i, y1 of the next (where the groups take turns, y2 of the one after it)
-            int y0 = n > 0 ? src.pool_row(a, t0, lane) : -1, y1 = n > 1 ? src.pool_row(a, t0 + 1, lane) : -1;
+            int k_next = 0, v_next = 0, y_last = -1, y_before = -1;   // pool rows of this lane's box in the last K and the one before it
 #pragma unroll 1
-            for (int i = -ahead; i < n; ++i) {
-                const int next = i + ahead, y2 = turns && i >= 0 && next < n ? src.pool_row(a, t0 + next, lane) : -1;
-                if (i >= 0) copy_tile(i, y0, true);
-                if (next < n) copy_tile(next, i < 0 ? (next == 0 ? y0 : y1) : turns ? y2 : y1, false);
-                if (i >= 0) {
-                    y0 = y1;
-                    y1 = turns ? y2 : next + 1 < n ? src.pool_row(a, t0 + next + 1, lane) : -1;
+            for (int j = 0; j < 2 * n; ++j) {
+                const bool value = k_next == n || k_next - v_next == ahead;
+                const int t = t0 + (value ? v_next : k_next);
+                int y = k_next - v_next == 2 ? y_before : y_last;  // V lies where K does
+                if (!value) {
+                    y = src.pool_row(a, t, lane);
+                    y_before = y_last;
+                    y_last = y;
                 }
+                (value ? v_next : k_next) += 1;
+#pragma unroll 1
+                for (int p = 0; p < PARTS; ++p) copy(it, src, t, y, value, p);
             }
             next_item();
         }
@@ -652,6 +656,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     }
     tc_before();
     __syncthreads();
+    if (tid == 0 && a.status && c.limit != kCopySpinLimit) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
     if (warp == 9) {
         tc_after();
         tc_dealloc(tmem, kTileColumns);
@@ -858,7 +863,7 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
     }
     const unsigned blocks = (unsigned)sms;
     // Few rows a sequence on the mean: {rows measured}
-    if (a.box_rows && !a.shifted && a.d <= 128 && a.n_q * a.per_kv <= (long long)kFewMean * a.batch) {
+    if (a.box_rows && !a.shifted && a.d <= 128 && a.per_kv <= kFewRows && a.n_q * a.per_kv <= (long long)kFewMean * a.batch) {
         a.half_tokens = kFewRows / a.per_kv;
         const cudaError_t e = launch_prompt_few(dtype, a, blocks, km, vm, st);
         if (e != cudaSuccess || !a.split || blocks < 2) return e;

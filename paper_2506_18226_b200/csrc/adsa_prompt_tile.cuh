@@ -11,7 +11,7 @@ constexpr int kTileThreads = 384;           // warps 0 .. 3, 4 .. 7: two groups;
 constexpr int kTileColumns = 512;           // all of tensor memory: S (and P) of the groups at 0 and 128, O at 256 and 384
 constexpr float kTileSlack = 8.f;
 constexpr int kTileRing = 4;                // items ahead
-constexpr int kFewRows = 64;                // query rows of an item of the kernel for few rows
+constexpr int kFewRows = 32;                // query rows of an item of the kernel for few rows
 constexpr unsigned kTileMinRun = 6;         // units of a run, at least, where items may be cut
 
 struct TileDesc {                           // an item of a run, as the walking warp finds it
