@@ -55,19 +55,49 @@ __device__ __forceinline__ uint32_t draw_load(const DrawArgs &a, int r, int i)
 }
 
 struct DrawShared {
-    unsigned long long mass[kDrawBins];     // of the steps; of sorted entries
+    unsigned long long mass[kDrawBins];     // of the steps
     unsigned long long list[kDrawList];
     unsigned count[kDrawBins];
+    double power[64];                       // 2^(j / 64)
     unsigned long long warp_mass[kDrawWarps];
     unsigned warp_count[kDrawWarps];
     uint32_t warp_key[kDrawWarps], warp_low[kDrawWarps];
-    unsigned long long before, at;
+    double largest, per_64th;               // the largest logit; 64 log2(e) / temperature
+    unsigned long long before;
+    uint32_t top, min_key;
     unsigned bin, n, bin_count;
     int pick;
 };
 
-// Sums over the block, for all threads: x, and the sum of what threads before this one have.
-__device__ __forceinline__ unsigned long long draw_scan(unsigned long long x, unsigned long long &before, DrawShared &s)
+// Functions that are not inlined: every phase runs once, and what bounds a small call is fetching its code.
+
+// exp((x - largest) / temperature) in 64 bits, off by about 2^-51: the 64ths of the power of two from a table, the rest (up to 1/128 of a
+// doubling) by the exponential series (table-driven, after Tang 1989).  Below 2^-1000: 0.
+__device__ __forceinline__ double draw_share(uint32_t key, const DrawShared &s)
+{
+    const double x = (draw_logit(key) - s.largest) * s.per_64th, magic = 6755399441055744.0;
+    if (key == s.top) return 1.0;
+    if (!(x > -64000.0)) return 0.0;
+    const double k = x + magic, r = (x - (k - magic)) * 0.010830424696249145;   // ln 2 / 64
+    double p = fma(r, 1.0 / 120, 1.0 / 24);
+    p = fma(p, r, 1.0 / 6);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    const int n = __double2loint(k);                               // (two's complement in the low bits of the sum)
+    const double y = p * s.power[n & 63];
+    return __hiloint2double(__double2hiint(y) + ((n >> 6) << 20), __double2loint(y));
+}
+// ... as a whole multiple of 2^-42
+__device__ __forceinline__ unsigned long long draw_weight(uint32_t key, const DrawShared &s)
+{
+    return (unsigned long long)__double_as_longlong(fma(draw_share(key, s), kDrawOne, 4503599627370496.0)) & 0xfffffffffffffULL;   // 2^52 + the multiple
+}
+__device__ __noinline__ unsigned long long draw_weight_of(uint32_t key, const DrawShared &s) { return draw_weight(key, s); }
+__device__ __noinline__ bool draw_enough(uint32_t key, double min_p, const DrawShared &s) { return draw_share(key, s) >= min_p; }
+
+// Sum of x over the block, for all threads; before: what threads before this one have of it.
+__device__ __noinline__ unsigned long long draw_scan(unsigned long long x, unsigned long long *before, DrawShared &s)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned long long incl = x;
@@ -79,11 +109,12 @@ __device__ __forceinline__ unsigned long long draw_scan(unsigned long long x, un
     unsigned long long w = s.warp_mass[lane];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const unsigned long long t = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += t; }
-    before = incl - x + (warp ? __shfl_sync(0xffffffffu, w, (warp + 31) & 31) : 0);
+    const unsigned long long own = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+    *before = incl - x + (warp ? own : 0);
     return __shfl_sync(0xffffffffu, w, 31);
 }
 // The list's n entries, largest first (room for a power of two).
-__device__ __forceinline__ void draw_sort(DrawShared &s, unsigned n)
+__device__ __noinline__ void draw_sort(DrawShared &s, unsigned n)
 {
     unsigned size = 2;
     while (size < n) size *= 2;
@@ -91,10 +122,10 @@ __device__ __forceinline__ void draw_sort(DrawShared &s, unsigned n)
     for (unsigned k = 2; k <= size; k *= 2) {
         for (unsigned j = k / 2; j; j /= 2) {
             // pairs within a warp's 64 entries need the warp alone
-            if (j >= 32 || j == k / 2) __syncthreads();
+            if (j >= 32 || k == 2) __syncthreads();
             else __syncwarp();
-            for (unsigned t = threadIdx.x; t < size / 2; t += kDrawThreads) {
-                const unsigned i = 2 * t - (t & (j - 1)), o = i + j;
+            const unsigned t = threadIdx.x, i = 2 * t - (t & (j - 1)), o = i + j;
+            if (t < size / 2) {
                 const unsigned long long x = s.list[i], y = s.list[o];
                 if ((x < y) == ((i & k) == 0)) { s.list[i] = y; s.list[o] = x; }
             }
@@ -102,29 +133,118 @@ __device__ __forceinline__ void draw_sort(DrawShared &s, unsigned n)
     }
     __syncthreads();
 }
+// Largest and lowest of the block's keys.
+__device__ __noinline__ uint2 draw_ends(uint32_t most, uint32_t fewest, DrawShared &s)
+{
+    most = __reduce_max_sync(0xffffffffu, most);
+    fewest = __reduce_min_sync(0xffffffffu, fewest);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) { s.warp_key[threadIdx.x >> 5] = most; s.warp_low[threadIdx.x >> 5] = fewest; }
+    __syncthreads();
+    return make_uint2(__reduce_max_sync(0xffffffffu, s.warp_key[threadIdx.x & 31]), __reduce_min_sync(0xffffffffu, s.warp_low[threadIdx.x & 31]));
+}
 
 // The row's keys: shared memory up to `stashed`, the rest read again.
 template <typename T>
 struct DrawRow {
-    const DrawArgs &a;
     const uint32_t *stash;
     int r, stashed;
-    __device__ __forceinline__ uint32_t operator[](int i) const { return i < stashed ? stash[i] : draw_load<T>(a, r, i); }
+    __device__ __forceinline__ uint32_t at(const DrawArgs &a, int i) const { return i < stashed ? stash[i] : draw_load<T>(a, r, i); }
 };
 
-// Steps between the logits of two keys, the larger one's first.
+// Steps between the logits of two keys.
 struct DrawSteps {
+    uint32_t top, low;
     float high, scale;
-    __device__ __forceinline__ DrawSteps(uint32_t top, uint32_t low) : high(0.5f * draw_logit(top))
+    __device__ __forceinline__ DrawSteps(uint32_t top_, uint32_t low_) : top(top_), low(low_), high(0.5f * draw_logit(top_))
     {
-        scale = (kDrawBins - 1) / (high - 0.5f * draw_logit(low));   // (halves: their difference is finite; infinite for neighbours, see below)
+        scale = (kDrawBins - 1) / (high - 0.5f * draw_logit(low));   // (halves: their difference is finite; it may round to 0)
     }
     // descending in x; 0 for the larger end, the last for the lower (0 x infinity is NaN, which converts to 0)
     __device__ __forceinline__ unsigned operator()(uint32_t key) const
     {
         return min((unsigned)max((int)((high - 0.5f * draw_logit(key)) * scale), 0), (unsigned)kDrawBins - 1u);
     }
+    __device__ __forceinline__ bool has(uint32_t key) const { return key <= top && key >= low; }
 };
+
+// How many of the row's keys lie in each step, and with `masses` their weights.
+template <typename T>
+__device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, bool masses, DrawShared &s)
+{
+    __syncthreads();
+    for (int i = threadIdx.x; i < kDrawBins; i += kDrawThreads) { s.count[i] = 0; s.mass[i] = 0; }
+    __syncthreads();
+#pragma unroll 2
+    for (int i = threadIdx.x; i < a.vocab; i += kDrawThreads) {
+        const uint32_t k = row.at(a, i);
+        if (!steps.has(k)) continue;
+        const unsigned b = steps(k);
+        atomicAdd(&s.count[b], 1u);
+        if (masses) atomicAdd(&s.mass[b], draw_weight(k, s));
+    }
+    __syncthreads();
+}
+// The ids with keys in the steps from `first` to `last` into the list, as key and id, sorted: larger keys first, of equal ones lower ids.
+template <typename T>
+__device__ __noinline__ void draw_gather(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned first, unsigned last, DrawShared &s)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+#pragma unroll 2
+    for (int i = threadIdx.x; i < a.vocab; i += kDrawThreads) {
+        const uint32_t k = row.at(a, i);
+        if (!steps.has(k)) continue;
+        const unsigned b = steps(k);
+        if (b >= first && b <= last) s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k << 32 | (0xffffffffu - (unsigned)i);
+    }
+    __syncthreads();
+    draw_sort(s, s.n);
+}
+// Largest and lowest key of a step.
+template <typename T>
+__device__ __noinline__ uint2 draw_step_ends(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned bin, DrawShared &s)
+{
+    uint32_t most = 0, fewest = 0xffffffffu;
+    for (int i = threadIdx.x; i < a.vocab; i += kDrawThreads) {
+        const uint32_t k = row.at(a, i);
+        if (steps.has(k) && steps(k) == bin) { most = max(most, k); fewest = min(fewest, k); }
+    }
+    return draw_ends(most, fewest, s);
+}
+// The last step with ids in it of which the count (masses: the mass) before is below the goal, or else the first: s.bin, s.bin_count, s.before.
+// start: what is before the first step.
+__device__ __noinline__ void draw_find(bool masses, double goal, unsigned long long start, DrawShared &s)
+{
+    const int tid = threadIdx.x;
+    if (tid == 0) s.pick = -1;
+    unsigned long long before;
+    const unsigned long long c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1], m0 = masses ? s.mass[2 * tid] : c0, m1 = masses ? s.mass[2 * tid + 1] : c1;
+    draw_scan(m0 + m1, &before, s);
+    before += start;
+    const bool g0 = c0 && ((double)before < goal || before == start), g1 = c1 && ((double)(before + m0) < goal || before + m0 == start);
+    if (g0 || g1) atomicMax(&s.pick, 2 * tid + (g1 ? 1 : 0));
+    __syncthreads();
+    if (s.pick >> 1 == tid) {
+        s.bin = (unsigned)s.pick;
+        s.before = s.pick & 1 ? before + m0 : before;
+        s.bin_count = (unsigned)(s.pick & 1 ? c1 : c0);
+    }
+    __syncthreads();
+}
+// Of the sorted list: the first entry with the same key as entry `at`.
+__device__ __noinline__ unsigned draw_first_equal(const DrawShared &s, unsigned at)
+{
+    const uint32_t key = (uint32_t)(s.list[at] >> 32);
+    unsigned first = 0;
+    while (first < at) {
+        const unsigned mid = (first + at) / 2;
+        if ((uint32_t)(s.list[mid] >> 32) == key) at = mid;
+        else first = mid + 1;
+    }
+    return first;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kDrawThreads)
@@ -133,26 +253,26 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     __shared__ DrawShared s;
     extern __shared__ uint32_t draw_stash[];
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.vocab;
-    const DrawRow<T> row{a, draw_stash, r, stashed};
+    const DrawRow<T> row{draw_stash, r, stashed};
+    if (tid < 64) s.power[tid] = exp2(tid / 64.0);
     pdl_wait();
     pdl_launch();
     // the largest and the lowest
     uint32_t top = 0, low = 0xffffffffu;
     unsigned able = 0;                                             // ids that can be drawn
+#pragma unroll 4
     for (int i = tid; i < V; i += kDrawThreads) {
         const uint32_t k = draw_load<T>(a, r, i);
         if (i < stashed) draw_stash[i] = k;
         top = max(top, k);
-        if (k) { low = min(low, k); ++able; }
+        low = min(low, k - 1u);                                    // (a key of 0 becomes the largest number)
+        able += k != 0u;
     }
-    top = __reduce_max_sync(0xffffffffu, top);
-    low = __reduce_min_sync(0xffffffffu, low);
-    able = __reduce_add_sync(0xffffffffu, able);
-    if (lane == 0) { s.warp_key[warp] = top; s.warp_low[warp] = low; s.warp_count[warp] = able; }
-    __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, s.warp_key[lane]);
-    low = __reduce_min_sync(0xffffffffu, s.warp_low[lane]);
-    able = __reduce_add_sync(0xffffffffu, s.warp_count[lane]);
+    const uint2 ends = draw_ends(top, low, s);
+    top = ends.x;
+    low = ends.y + 1u;
+    unsigned long long unused;
+    able = (unsigned)draw_scan(able, &unused, s);
     if (top == 0) {                                                // nothing to draw
         if (tid == 0) {
             a.tokens[r] = -1;
@@ -164,226 +284,193 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
     const float top_p = a.top_ps ? a.top_ps[r] : a.top_p;
     const float least = a.min_ps ? a.min_ps[r] : a.min_p;
-    const double largest = draw_logit(top), t = temperature;
+    const double largest = draw_logit(top);
     const double min_p = largest == INFINITY ? 1.0 : least > 0.f ? fmin((double)least, 1.0) : 0.0;   // (infinite ones alone, where there are any)
     const double goal_u = fmin(fmax((double)a.uniforms[r], 0.0), 1.0);
     if (!(temperature > 0.f)) top_k = 1;
     const bool by_count = top_k > 0 && (unsigned)top_k < able, by_mass = top_p < 1.f && top_k != 1;
     if (!by_count) top_k = (int)able;
-    const auto share_of = [&](uint32_t key) { return key == top ? 1.0 : exp((draw_logit(key) - largest) / t); };
-    const auto weight_of = [&](uint32_t key) { return (unsigned long long)(share_of(key) * kDrawOne + 0.5); };
-    const auto enough = [&](uint32_t key) { return key == top || !(min_p > 0.0) || share_of(key) >= min_p; };
-    const auto answer = [&](int id, uint32_t key, unsigned long long total) {
-        a.tokens[r] = id;
-        if (a.logprobs) a.logprobs[r] = (float)((key == top ? 0.0 : (draw_logit(key) - largest) / t) - log((double)total / kDrawOne));
-    };
-
-    // Histogram of the keys between high and low (both among them) above `above`: of counts, or of the masses of those that count.
-    const auto histogram = [&](uint32_t high, uint32_t lowest, const DrawSteps &steps, bool masses) {
-        for (int i = tid; i < kDrawBins; i += kDrawThreads) { s.count[i] = 0; s.mass[i] = 0; }
-        __syncthreads();
-        for (int i = tid; i < V; i += kDrawThreads) {
-            const uint32_t k = row[i];
-            if (k > high || k < lowest || k == 0) continue;
-            const unsigned b = steps(k);
-            atomicAdd(&s.count[b], 1u);
-            if (masses) atomicAdd(&s.mass[b], weight_of(k));
+    if (tid == 0) {
+        s.largest = largest;
+        s.per_64th = 92.33248261893469 / (double)temperature;      // 64 / ln 2
+        s.top = top;
+    }
+    __syncthreads();
+    // the lowest key with a weight of min_p at least: 32 borders at a time
+    if (warp == 0) {
+        uint32_t lo = low, hi = top;                               // hi has it; what is below lo does not
+        while (min_p > 0.0 && lo < hi) {
+            const uint32_t step = (hi - lo) / 32u + 1u, at = min(hi - lo, step * lane) + lo;
+            const unsigned has = __ballot_sync(0xffffffffu, draw_enough(at, min_p, s));
+            const int first = has ? __ffs(has) - 1 : 32;           // (weights rise with keys)
+            const uint32_t base = lo;
+            if (first < 32) hi = min(hi, base + min(hi - base, step * first));
+            if (first > 0) lo = min(hi, base + min(hi - base, step * (first - 1)) + 1u);
         }
-        __syncthreads();
-    };
-    // The ids with keys from high to lowest in steps up to `last` (from `first` on) into the list, as key and id, so that larger ones come first.
-    const auto gather = [&](uint32_t high, uint32_t lowest, const DrawSteps &steps, unsigned first, unsigned last) {
-        if (tid == 0) s.n = 0;
-        __syncthreads();
-        for (int i = tid; i < V; i += kDrawThreads) {
-            const uint32_t k = row[i];
-            if (k > high || k < lowest || k == 0) continue;
-            const unsigned b = steps(k);
-            if (b < first || b > last) continue;
-            s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k << 32 | (0xffffffffu - (unsigned)i);
-        }
-        __syncthreads();
-        draw_sort(s, s.n);
-    };
-    // The step in which the running count passes need - 1, or the last whose masses before it are below the goal: s.bin, s.bin_count, s.before
-    const auto find_step = [&](bool masses, unsigned long long need, double goal, unsigned long long start) {
-        if (tid == 0) s.pick = -1;
-        __syncthreads();
-        unsigned long long before;
-        const unsigned long long c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1], m0 = masses ? s.mass[2 * tid] : c0, m1 = masses ? s.mass[2 * tid + 1] : c1;
-        draw_scan(m0 + m1, before, s);
-        before += start;
-        const auto good = [&](unsigned long long c, unsigned long long at) { return c && (masses ? (double)at < goal || at == start : at < need); };
-        const bool g0 = good(c0, before), g1 = good(c1, before + m0);
-        if (g0 || g1) atomicMax(&s.pick, 2 * tid + (g1 ? 1 : 0));
-        __syncthreads();
-        if (s.pick >> 1 == tid) {
-            s.bin = (unsigned)s.pick;
-            s.before = s.pick & 1 ? before + m0 : before;
-            s.bin_count = (unsigned)(s.pick & 1 ? c1 : c0);
-        }
-        __syncthreads();
-    };
+        if (lane == 0) s.min_key = min_p > 0.0 ? hi : low;
+    }
+    __syncthreads();
+    const uint32_t min_key = s.min_key;
 
     uint32_t thr = low;                                            // the border: keys above thr, and the first `ties` ids with just that key
-    unsigned ties = 0xffffffffu;
-    bool listed = able <= kDrawList;                               // all that can be kept is in the list, sorted
+    unsigned ties = 0xffffffffu, n = 0;
+    bool listed = able <= kDrawList, cut = false;                  // all that can be kept is in the list, sorted; what is in the list's first n is kept
     if (listed) {
-        gather(top, low, DrawSteps(top, low), 0u, kDrawBins - 1u);
+        draw_gather(a, row, DrawSteps(top, low), 0u, kDrawBins - 1u, s);
     } else if (by_count) {
-        uint32_t high = top, lowest = low;
+        DrawSteps steps(top, low);
         unsigned long long start = 0;
-        for (int level = 0;; ++level) {
-            const DrawSteps steps(high, lowest);
-            histogram(high, lowest, steps, false);
-            find_step(false, (unsigned)top_k, 0.0, start);
+        for (bool first = true;; first = false) {
+            draw_histogram(a, row, steps, false, s);
+            draw_find(false, (double)top_k, start, s);
             const unsigned bin = s.bin, in_bin = s.bin_count;
             const unsigned long long before = s.before;
-            if (level == 0 && before + in_bin <= kDrawList) {
-                gather(high, lowest, steps, 0u, bin);
-                listed = true;
-                break;
-            }
-            if (in_bin <= kDrawList) {
-                gather(high, lowest, steps, bin, bin);
-                const unsigned at = (unsigned)(top_k - before) - 1u;   // the last that is kept
-                thr = (uint32_t)(s.list[at] >> 32);
-                unsigned first = 0, last = at;                     // its first equal
-                while (first < last) {
-                    const unsigned mid = (first + last) / 2;
-                    if ((uint32_t)(s.list[mid] >> 32) == thr) last = mid;
-                    else first = mid + 1;
+            listed = first && before + in_bin <= kDrawList;
+            if (listed || in_bin <= kDrawList) {
+                draw_gather(a, row, steps, listed ? 0u : bin, bin, s);
+                if (!listed) {
+                    const unsigned last = (unsigned)(top_k - before) - 1u;   // that is kept
+                    thr = (uint32_t)(s.list[last] >> 32);
+                    ties = last + 1u - draw_first_equal(s, last);
                 }
-                ties = at - first + 1u;
                 break;
             }
             // too many in one step: between its own largest and lowest
-            uint32_t most = 0, fewest = 0xffffffffu;
-            for (int i = tid; i < V; i += kDrawThreads) {
-                const uint32_t k = row[i];
-                if (k <= high && k >= lowest && k && steps(k) == bin) { most = max(most, k); fewest = min(fewest, k); }
+            const uint2 e = draw_step_ends(a, row, steps, bin, s);
+            if (e.x == e.y) {
+                thr = e.x;
+                ties = (unsigned)(top_k - before);
+                break;
             }
-            most = __reduce_max_sync(0xffffffffu, most);
-            fewest = __reduce_min_sync(0xffffffffu, fewest);
-            if (lane == 0) { s.warp_key[warp] = most; s.warp_low[warp] = fewest; }
-            __syncthreads();
-            high = __reduce_max_sync(0xffffffffu, s.warp_key[lane]);
-            lowest = __reduce_min_sync(0xffffffffu, s.warp_low[lane]);
-            __syncthreads();
+            steps = DrawSteps(e.x, e.y);
             start = before;
-            if (high == lowest) { thr = high; ties = (unsigned)(top_k - before); break; }
         }
     }
-    if (listed) {
-        unsigned n = min((unsigned)top_k, s.n);
+    if (!listed && min_key > thr && min_p > 0.0) {
+        // few by min_p, whose mass is below top_p of all: then top_p cuts nothing more
+        unsigned long long sum = 0, few = 0;
+        unsigned many = 0, equal = 0;
+#pragma unroll 2
+        for (int i = tid; i < V; i += kDrawThreads) {
+            const uint32_t k = row.at(a, i);
+            if (k < thr) continue;
+            const unsigned long long w = by_mass && k > thr ? draw_weight(k, s) : 0;
+            sum += w;
+            equal += k == thr;
+            if (k >= min_key) { few += w; ++many; }
+        }
+        many = (unsigned)draw_scan(many, &unused, s);
+        bool first = !by_mass;
+        if (by_mass) {
+            const unsigned long long border = min(draw_scan(equal, &unused, s), (unsigned long long)ties) * draw_weight_of(thr, s);
+            const double goal = fmax((double)top_p, 0.0) * (double)(draw_scan(sum, &unused, s) + border);
+            first = (double)draw_scan(few, &unused, s) < goal;
+        }
+        if (first) {
+            thr = min_key;
+            ties = 0xffffffffu;
+            if (many <= kDrawList) {
+                draw_gather(a, row, DrawSteps(top, min_key), 0u, kDrawBins - 1u, s);
+                listed = cut = true;
+                n = many;
+            }
+        }
+        if (first && !listed) cut = true;
+    }
+    if (listed && !cut) {
+        n = min((unsigned)top_k, s.n);
         // two entries a thread: their weights, the mass before them
-        const auto key_at = [&](unsigned i) { return (uint32_t)(s.list[i] >> 32); };
-        const unsigned long long w0 = 2u * tid < n ? weight_of(key_at(2 * tid)) : 0, w1 = 2u * tid + 1u < n ? weight_of(key_at(2 * tid + 1)) : 0;
+        const uint32_t k0 = (uint32_t)(s.list[2 * tid] >> 32), k1 = (uint32_t)(s.list[2 * tid + 1] >> 32);
+        const unsigned long long w0 = 2u * tid < n ? draw_weight_of(k0, s) : 0, w1 = 2u * tid + 1u < n ? draw_weight_of(k1, s) : 0;
         unsigned long long before;
-        unsigned long long total = draw_scan(w0 + w1, before, s);
+        const unsigned long long total = draw_scan(w0 + w1, &before, s);
         const double goal = by_mass ? fmax((double)top_p, 0.0) * (double)total : INFINITY;
-        const bool in0 = 2u * tid < n && (tid == 0 || ((double)before < goal && enough(key_at(2 * tid)))),
-                   in1 = 2u * tid + 1u < n && (double)(before + w0) < goal && enough(key_at(2 * tid + 1));
-        unsigned long long none;
-        n = (unsigned)draw_scan((unsigned)in0 + (unsigned)in1, none, s);   // (a head of the list)
+        const unsigned in0 = 2u * tid < n && (tid == 0 || ((double)before < goal && k0 >= min_key)),
+                       in1 = 2u * tid + 1u < n && (double)(before + w0) < goal && k1 >= min_key;
+        n = (unsigned)draw_scan(in0 + in1, &unused, s);            // (a head of the list)
+    }
+    if (listed) {
         // by id
-        unsigned long long e0 = 0, e1 = 0;
-        if (in0) e0 = (s.list[2 * tid] << 32) | (s.list[2 * tid] >> 32);
-        if (in1) e1 = (s.list[2 * tid + 1] << 32) | (s.list[2 * tid + 1] >> 32);
+        unsigned long long e0 = s.list[2 * tid], e1 = s.list[2 * tid + 1], before;
         __syncthreads();
-        s.list[2 * tid] = e0;
-        s.list[2 * tid + 1] = e1;
+        s.list[2 * tid] = e0 << 32 | e0 >> 32;
+        s.list[2 * tid + 1] = e1 << 32 | e1 >> 32;
+        if (tid == 0) s.pick = (int)n - 1;
         __syncthreads();
         draw_sort(s, n);
-        const auto low_key = [&](unsigned i) { return (uint32_t)s.list[i]; };
-        const unsigned long long v0 = 2u * tid < n ? weight_of(low_key(2 * tid)) : 0, v1 = 2u * tid + 1u < n ? weight_of(low_key(2 * tid + 1)) : 0;
-        if (tid == 0) s.pick = (int)n - 1;
-        total = draw_scan(v0 + v1, before, s);
+        const unsigned long long v0 = 2u * tid < n ? draw_weight_of((uint32_t)s.list[2 * tid], s) : 0,
+                                 v1 = 2u * tid + 1u < n ? draw_weight_of((uint32_t)s.list[2 * tid + 1], s) : 0;
+        const unsigned long long total = draw_scan(v0 + v1, &before, s);
         const double at = goal_u * (double)total;
         if (2u * tid < n && (double)(before + v0) >= at) atomicMin(&s.pick, 2 * tid);
         else if (2u * tid + 1u < n && (double)(before + v0 + v1) >= at) atomicMin(&s.pick, 2 * tid + 1);
         __syncthreads();
-        if (tid == 0) answer((int)(0xffffffffu - (uint32_t)(s.list[s.pick] >> 32)), low_key(s.pick), total);
+        if (tid == 0) {
+            const uint32_t key = (uint32_t)s.list[s.pick];
+            a.tokens[r] = (int)(0xffffffffu - (uint32_t)(s.list[s.pick] >> 32));
+            if (a.logprobs) a.logprobs[r] = (float)((key == top ? 0.0 : (draw_logit(key) - largest) / (double)temperature) - log((double)total / kDrawOne));
+        }
         return;
     }
-    if (by_mass) {
-        // mass of what top_k keeps: of the ids at its border, the first `ties`
-        unsigned long long sum = 0, none;
-        unsigned equal = 0;
-        uint32_t high = top, lowest = thr;
-        DrawSteps steps(high, lowest);
-        histogram(high, lowest, steps, true);
-        for (int i = tid; i < V; i += kDrawThreads) equal += row[i] == thr;
-        const unsigned n_equal = (unsigned)draw_scan(equal, none, s), drop = n_equal - min(n_equal, ties);
-        if (tid == 0 && drop) {                                    // (they are in the last step that holds any)
-            s.mass[steps(thr)] -= drop * weight_of(thr);
-            s.count[steps(thr)] -= drop;
-        }
-        __syncthreads();
-        sum = s.mass[2 * tid] + s.mass[2 * tid + 1];
-        const double goal = fmax((double)top_p, 0.0) * (double)draw_scan(sum, none, s);
-        unsigned long long start = 0;
+    if (by_mass && !cut) {
+        // of the ids at top_k's border, the first `ties` count
         const uint32_t k_thr = thr;
+        unsigned equal = 0;
+        if (ties != 0xffffffffu) {
+            for (int i = tid; i < V; i += kDrawThreads) equal += row.at(a, i) == thr;
+            equal = (unsigned)draw_scan(equal, &unused, s);
+        }
+        const unsigned drop = equal - min(equal, ties);
+        DrawSteps steps(top, thr);
+        unsigned long long start = 0;
+        double goal = -1.0;
         for (;;) {
-            find_step(true, 0, goal, start);
-            const unsigned bin = s.bin, in_bin = s.bin_count + (bin == steps(k_thr) && lowest == k_thr ? drop : 0u);
-            const unsigned long long before = s.before;
-            uint32_t most = 0, fewest = 0xffffffffu;
-            if (in_bin <= kDrawList) {
-                gather(high, lowest, steps, bin, bin);
-                const unsigned n = s.n - (bin == steps(k_thr) && lowest == k_thr ? drop : 0u);
-                const unsigned long long w0 = 2u * tid < n ? weight_of((uint32_t)(s.list[2 * tid] >> 32)) : 0,
-                                         w1 = 2u * tid + 1u < n ? weight_of((uint32_t)(s.list[2 * tid + 1] >> 32)) : 0;
-                unsigned long long at;
-                draw_scan(w0 + w1, at, s);
-                at += before;
-                const unsigned kept = (unsigned)draw_scan((unsigned)(2u * tid < n && ((double)at < goal || tid == 0)) + (unsigned)(2u * tid + 1u < n && (double)(at + w0) < goal), none, s);
-                thr = (uint32_t)(s.list[kept - 1u] >> 32);
-                unsigned first = 0, last = kept - 1u;
-                while (first < last) {
-                    const unsigned mid = (first + last) / 2;
-                    if ((uint32_t)(s.list[mid] >> 32) == thr) last = mid;
-                    else first = mid + 1;
-                }
-                ties = kept - first;
-                break;
-            }
-            for (int i = tid; i < V; i += kDrawThreads) {
-                const uint32_t k = row[i];
-                if (k <= high && k >= lowest && k && steps(k) == bin) { most = max(most, k); fewest = min(fewest, k); }
-            }
-            most = __reduce_max_sync(0xffffffffu, most);
-            fewest = __reduce_min_sync(0xffffffffu, fewest);
-            if (lane == 0) { s.warp_key[warp] = most; s.warp_low[warp] = fewest; }
-            __syncthreads();
-            high = __reduce_max_sync(0xffffffffu, s.warp_key[lane]);
-            lowest = __reduce_min_sync(0xffffffffu, s.warp_low[lane]);
-            __syncthreads();
-            start = before;
-            if (high == lowest) {
-                // equal keys: those with less than the goal before them, one at least
-                const unsigned long long w = weight_of(high);
-                unsigned n = in_bin - (high == k_thr ? drop : 0u), at = 1;
-                while (at < n) {
-                    const unsigned mid = (at + n + 1) / 2;         // is the mid-th kept?
-                    if ((double)(before + (mid - 1) * w) < goal) at = mid;
-                    else n = mid - 1;
-                }
-                thr = high;
-                ties = at;
-                break;
-            }
-            steps = DrawSteps(high, lowest);
-            histogram(high, lowest, steps, true);
-            if (tid == 0 && drop && lowest == k_thr) {
-                s.mass[steps(k_thr)] -= drop * weight_of(k_thr);
+            draw_histogram(a, row, steps, true, s);
+            if (tid == 0 && drop && steps.low == k_thr) {          // (they are the last of the last step that holds any)
+                s.mass[steps(k_thr)] -= drop * draw_weight_of(k_thr, s);
                 s.count[steps(k_thr)] -= drop;
             }
             __syncthreads();
+            if (goal < 0.0) goal = fmax((double)top_p, 0.0) * (double)draw_scan(s.mass[2 * tid] + s.mass[2 * tid + 1], &unused, s);
+            draw_find(true, goal, start, s);
+            const unsigned bin = s.bin, less = steps.low == k_thr && bin == steps(k_thr) ? drop : 0u, in_bin = s.bin_count;
+            const unsigned long long before = s.before;
+            if (in_bin + less <= kDrawList) {
+                draw_gather(a, row, steps, bin, bin, s);
+                const unsigned long long w0 = 2u * tid < in_bin ? draw_weight_of((uint32_t)(s.list[2 * tid] >> 32), s) : 0,
+                                         w1 = 2u * tid + 1u < in_bin ? draw_weight_of((uint32_t)(s.list[2 * tid + 1] >> 32), s) : 0;
+                unsigned long long at;
+                draw_scan(w0 + w1, &at, s);
+                at += before;
+                const unsigned in0 = 2u * tid < in_bin && (tid == 0 || (double)at < goal), in1 = 2u * tid + 1u < in_bin && (double)(at + w0) < goal;
+                const unsigned kept = (unsigned)draw_scan(in0 + in1, &unused, s);
+                thr = (uint32_t)(s.list[kept - 1u] >> 32);
+                ties = kept - draw_first_equal(s, kept - 1u);
+                break;
+            }
+            const uint2 e = draw_step_ends(a, row, steps, bin, s);
+            if (e.x == e.y) {
+                // equal keys: those with less than the goal before them, one at least
+                const unsigned long long w = draw_weight_of(e.x, s);
+                unsigned high = in_bin, at = 1;
+                while (at < high) {
+                    const unsigned mid = (at + high + 1) / 2;      // is the mid-th kept?
+                    if ((double)(before + (mid - 1) * w) < goal) at = mid;
+                    else high = mid - 1;
+                }
+                thr = e.x;
+                ties = at;
+                break;
+            }
+            steps = DrawSteps(e.x, e.y);
+            start = before;
         }
         __syncthreads();
     }
-    const auto kept_key = [&](uint32_t k) { return k >= thr && k && enough(k); };   // (min_p is a border of keys too)
+    if (min_key > thr) {
+        thr = min_key;
+        ties = 0xffffffffu;
+    }
     // Mass of what is kept, by segments of ids in order, one per warp; then the segment in which the running sum reaches its goal is cut
     // into one per warp again.  (Ids at the border count in order.)
     unsigned long long total = 0, before = 0;
@@ -395,10 +482,10 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         unsigned long long sum = 0;
         unsigned equal = 0, kept = 0;
         for (int i = i0 + lane; i < i1; i += 32) {
-            const uint32_t k = row[i];
-            if (!kept_key(k)) continue;
+            const uint32_t k = row.at(a, i);
+            if (k < thr) continue;
             if (k == thr) ++equal;
-            else { sum += weight_of(k); ++kept; }
+            else { sum += draw_weight(k, s); ++kept; }
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
@@ -409,7 +496,7 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         __syncthreads();
         if (lane == 0) { s.warp_mass[warp] = sum; s.warp_count[warp] = equal; s.warp_key[warp] = kept; }
         __syncthreads();
-        const unsigned long long w = weight_of(thr);
+        const unsigned long long w = draw_weight_of(thr, s);
         if (level == 0) {
             unsigned e = 0;
             for (int x = 0; x < kDrawWarps; ++x) { total += s.warp_mass[x]; e += s.warp_count[x]; }
@@ -445,17 +532,18 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     // up to 32 ids: a lane each
     if (warp == 0) {
         const int i = begin + lane;
-        const uint32_t k = i < end ? row[i] : 0u;
-        bool kept = i < end && kept_key(k);
+        const uint32_t k = i < end ? row.at(a, i) : 0u;
+        bool kept = i < end && k >= thr;
         const unsigned equal = __ballot_sync(0xffffffffu, kept && k == thr);
         if (kept && k == thr) kept = equal_before + __popc(equal & ((1u << lane) - 1u)) < ties;
-        unsigned long long run = kept ? weight_of(k) : 0;
+        unsigned long long run = kept ? draw_weight_of(k, s) : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const unsigned long long x = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += x; }
         const unsigned all = __ballot_sync(0xffffffffu, kept), reached = __ballot_sync(0xffffffffu, kept && (double)(before + run) >= goal);
         const int pick = reached ? __ffs(reached) - 1 : 31 - __clz(all);
         if (lane == pick) {
-            answer(i, k, total);
+            a.tokens[r] = i;
+            if (a.logprobs) a.logprobs[r] = (float)((k == top ? 0.0 : (draw_logit(k) - largest) / (double)temperature) - log((double)total / kDrawOne));
         }
     }
 }
