@@ -6,10 +6,11 @@
 // most significant first, from counts (top_k) or masses (top_p) per byte.  Weights are made in 64 bits and added up as whole
 // multiples of 2^-42 of the largest: sums do not depend on their order, and an id is kept or drawn as the real numbers say.
 //
-// A block per row; keys lie in shared memory, as many as fit.  Where up to 2048 ids can be kept (by top_k, or the vocabulary has no more),
-// these are sorted, cut, sorted again by id and summed: three passes over the row and two sorts.  Else the borders are found by histograms
-// of 2048 steps between the largest and the lowest logit, of counts or of masses, and a sort of the step that holds the border (or again, where
-// one step holds too many), and the sum is followed over the row itself.
+// A block per row; keys lie in shared memory, as many as fit.  A border is found by a histogram of 2048 steps between the largest and the
+// lowest logit, of counts or of masses, and a sort of the step that holds it (where one step holds over 2048 ids: by steps between its own
+// ends).  Where up to 2048 ids can be kept, they are listed in order of their ids once, and the rest works on the list; else over the row.
+// (Sorting such a list, by logit and then by id, took 30000 clocks each time: 46 us for one row of 16384.)
+#include <float.h>
 #include <math.h>
 
 #include "adsa_half.cuh"
@@ -17,6 +18,7 @@
 namespace adsa {
 
 constexpr int kDrawThreads = 1024, kDrawWarps = kDrawThreads / 32;
+constexpr unsigned kDrawSorted = 256;        // entries that are sorted by id rather than listed in order
 constexpr int kDrawBins = 2048, kDrawList = 2048;   // steps of a histogram; entries that are sorted
 constexpr int kDrawMaxVocab = 1 << 20;       // so that 2^20 weights of 2^42 fit 63 bits
 constexpr double kDrawOne = 4398046511104.0;   // 2^42
@@ -24,7 +26,7 @@ constexpr double kDrawOne = 4398046511104.0;   // 2^42
 struct DrawArgs {
     const void *logits, *uncond;
     long long row, uncond_row;              // element strides
-    int rows, vocab;
+    int rows, vocab, wide;                  // wide: rows begin on 16 bytes
     float guidance, temperature, top_p, min_p;
     int top_k;
     const float *temperatures, *top_ps, *min_ps;   // per row, or null
@@ -43,21 +45,45 @@ __device__ __forceinline__ uint32_t draw_key(float x)
 }
 __device__ __forceinline__ float draw_logit(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
+// Eight neighbouring logits from id i on, a multiple of 8; 0 past the end.
 template <typename T>
-__device__ __forceinline__ uint32_t draw_load(const DrawArgs &a, int r, int i)
+__device__ __forceinline__ void draw_load8(const T *row, int i, int vocab, bool wide, float (&x)[8])
 {
-    float x = to_f32(((const T *)a.logits)[(size_t)r * a.row + i]);
-    if (a.uncond) {
-        const float u = to_f32(((const T *)a.uncond)[(size_t)r * a.uncond_row + i]);
-        x = __fadd_rn(u, __fmul_rn(a.guidance, __fsub_rn(x, u)));
+    if (wide && i + 8 <= vocab) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4 *>(x + j) = __ldg(reinterpret_cast<const float4 *>(row + i + j));
+        } else {
+            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(row + i));
+            const uint32_t p[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<float2 *>(x + 2 * j) = unpack2<T>(p[j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = i + j < vocab ? to_f32(row[i + j]) : 0.f;
     }
-    return draw_key(x);
+}
+// ... as keys, mixed with the other row's if there is one; 0 past the end
+template <typename T>
+__device__ __forceinline__ void draw_keys(const DrawArgs &a, int r, int i, uint32_t (&k)[8])
+{
+    alignas(16) float x[8], u[8];
+    draw_load8((const T *)a.logits + (size_t)r * a.row, i, a.vocab, a.wide, x);
+    if (a.uncond) {
+        draw_load8((const T *)a.uncond + (size_t)r * a.uncond_row, i, a.vocab, a.wide, u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __fadd_rn(u[j], __fmul_rn(a.guidance, __fsub_rn(x[j], u[j])));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = i + j < a.vocab ? draw_key(x[j]) : 0u;
 }
 
 struct DrawShared {
     unsigned long long mass[kDrawBins];     // of the steps
     unsigned long long list[kDrawList];
     unsigned count[kDrawBins];
+    uint32_t key[kDrawList], id[kDrawList]; // what can be kept, in order of ids
     double power[64];                       // 2^(j / 64)
     unsigned long long warp_mass[kDrawWarps];
     unsigned warp_count[kDrawWarps];
@@ -144,26 +170,40 @@ __device__ __noinline__ uint2 draw_ends(uint32_t most, uint32_t fewest, DrawShar
     return make_uint2(__reduce_max_sync(0xffffffffu, s.warp_key[threadIdx.x & 31]), __reduce_min_sync(0xffffffffu, s.warp_low[threadIdx.x & 31]));
 }
 
-// The row's keys: shared memory up to `stashed`, the rest read again.
+// The row's keys, eight at a time: shared memory up to `stashed` (a multiple of 8), the rest read again.
 template <typename T>
 struct DrawRow {
     const uint32_t *stash;
     int r, stashed;
-    __device__ __forceinline__ uint32_t at(const DrawArgs &a, int i) const { return i < stashed ? stash[i] : draw_load<T>(a, r, i); }
+    __device__ __forceinline__ void at(const DrawArgs &a, int i, uint32_t (&k)[8]) const
+    {
+        if (i < stashed) {
+            *reinterpret_cast<uint4 *>(k) = *reinterpret_cast<const uint4 *>(stash + i);
+            *reinterpret_cast<uint4 *>(k + 4) = *reinterpret_cast<const uint4 *>(stash + i + 4);
+        } else {
+            draw_keys<T>(a, r, i, k);
+        }
+    }
 };
+constexpr int kDrawStride = 8 * kDrawThreads;
 
-// Steps between the logits of two keys.
+// Steps between the logits of two keys, even in the logits; or, where their distance is none or infinite, in the keys.  The two
+// ends are in different steps.
 struct DrawSteps {
     uint32_t top, low;
     float high, scale;
+    bool by_key;
     __device__ __forceinline__ DrawSteps(uint32_t top_, uint32_t low_) : top(top_), low(low_), high(0.5f * draw_logit(top_))
     {
-        scale = (kDrawBins - 1) / (high - 0.5f * draw_logit(low));   // (halves: their difference is finite; it may round to 0)
+        scale = (kDrawBins - 1) / (high - 0.5f * draw_logit(low));   // (halves: the distance of finite logits is finite)
+        by_key = !(scale > 0.f && scale <= FLT_MAX);
+        if (by_key) scale = (float)(kDrawBins - 1) / (float)max(top - low, 1u);
     }
-    // descending in x; 0 for the larger end, the last for the lower (0 x infinity is NaN, which converts to 0)
+    // descending: 0 for the larger end
     __device__ __forceinline__ unsigned operator()(uint32_t key) const
     {
-        return min((unsigned)max((int)((high - 0.5f * draw_logit(key)) * scale), 0), (unsigned)kDrawBins - 1u);
+        const float x = by_key ? (float)(top - key) : high - 0.5f * draw_logit(key);
+        return min((unsigned)max((int)(x * scale), 0), (unsigned)kDrawBins - 1u);
     }
     __device__ __forceinline__ bool has(uint32_t key) const { return key <= top && key >= low; }
 };
@@ -175,41 +215,105 @@ __device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, D
     __syncthreads();
     for (int i = threadIdx.x; i < kDrawBins; i += kDrawThreads) { s.count[i] = 0; s.mass[i] = 0; }
     __syncthreads();
-#pragma unroll 2
-    for (int i = threadIdx.x; i < a.vocab; i += kDrawThreads) {
-        const uint32_t k = row.at(a, i);
-        if (!steps.has(k)) continue;
-        const unsigned b = steps(k);
-        atomicAdd(&s.count[b], 1u);
-        if (masses) atomicAdd(&s.mass[b], draw_weight(k, s));
+    for (int i = 8 * threadIdx.x; i < a.vocab; i += kDrawStride) {
+        alignas(16) uint32_t k[8];
+        row.at(a, i, k);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!steps.has(k[j])) continue;
+            const unsigned b = steps(k[j]);
+            atomicAdd(&s.count[b], 1u);
+            if (masses) atomicAdd(&s.mass[b], draw_weight(k[j], s));
+        }
     }
     __syncthreads();
 }
-// The ids with keys in the steps from `first` to `last` into the list, as key and id, sorted: larger keys first, of equal ones lower ids.
+// The ids with keys of the steps from `first` to `last` into the list, as key and id, sorted: larger keys first, of equal ones lower ids.
 template <typename T>
 __device__ __noinline__ void draw_gather(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned first, unsigned last, DrawShared &s)
 {
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-#pragma unroll 2
-    for (int i = threadIdx.x; i < a.vocab; i += kDrawThreads) {
-        const uint32_t k = row.at(a, i);
-        if (!steps.has(k)) continue;
-        const unsigned b = steps(k);
-        if (b >= first && b <= last) s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k << 32 | (0xffffffffu - (unsigned)i);
+    for (int i = 8 * threadIdx.x; i < a.vocab; i += kDrawStride) {
+        alignas(16) uint32_t k[8];
+        row.at(a, i, k);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!steps.has(k[j])) continue;
+            const unsigned b = steps(k[j]);
+            if (b >= first && b <= last) s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k[j] << 32 | (0xffffffffu - (unsigned)(i + j));
+        }
     }
     __syncthreads();
     draw_sort(s, s.n);
+}
+// The ids that can be kept into s.key and s.id in their order: keys above thr, and the first `ties` with just that key; a warp per segment of ids,
+// 256 at a time.
+template <typename T>
+__device__ __noinline__ unsigned draw_list(const DrawArgs &a, DrawRow<T> row, uint32_t thr, unsigned ties, DrawShared &s)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = ((a.vocab + kDrawWarps - 1) / kDrawWarps + 255) & ~255, i0 = warp * per, i1 = min(i0 + per, a.vocab);
+    unsigned both = 0;                                             // keys above thr, 2^16 times keys of thr (ids of a lane: below 2^16)
+    for (int i = i0 + 8 * lane; i < i1; i += 256) {
+        alignas(16) uint32_t k[8];
+        row.at(a, i, k);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) both += (k[j] > thr ? 1u : 0u) + (k[j] == thr ? 0x10000u : 0u);
+    }
+    const unsigned above = __reduce_add_sync(0xffffffffu, both & 0xffffu), equal = __reduce_add_sync(0xffffffffu, both >> 16);
+    __syncthreads();
+    if (lane == 0) { s.warp_count[warp] = above; s.warp_key[warp] = equal; }
+    __syncthreads();
+    // entries and equals of the warps before this one
+    const unsigned c = s.warp_count[lane], e = s.warp_key[lane];
+    unsigned eq = __reduce_add_sync(0xffffffffu, lane < warp ? e : 0u), at = __reduce_add_sync(0xffffffffu, lane < warp ? c : 0u) + min(eq, ties);
+    const unsigned n = __reduce_add_sync(0xffffffffu, c) + min(__reduce_add_sync(0xffffffffu, e), ties);
+    if (above + equal) {
+        for (int i = i0 + 8 * lane; i - 8 * lane < i1; i += 256) {
+            alignas(16) uint32_t k[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (i < i1) row.at(a, i, k);
+            unsigned mine = 0, same = 0;                           // bits: kept for sure; of the border
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { mine |= (k[j] > thr) << j; same |= (k[j] == thr) << j; }
+            if (!__any_sync(0xffffffffu, mine | same)) continue;
+            unsigned before = __popc(same) << 16, all = before;    // (sums of both counts)
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, before, o); if (lane >= o) before += t; }
+            all = __shfl_sync(0xffffffffu, before, 31) >> 16;
+            unsigned rank = eq + (before >> 16) - __popc(same);    // of this lane's first at the border
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (same >> j & 1u) mine |= (rank++ < ties) << j;
+            before = __popc(mine);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, before, o); if (lane >= o) before += t; }
+            unsigned to = at + before - __popc(mine);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (mine >> j & 1u) {
+                    s.key[to] = k[j];
+                    s.id[to++] = (uint32_t)(i + j);
+                }
+            }
+            at += __shfl_sync(0xffffffffu, before, 31);
+            eq += all;
+        }
+    }
+    __syncthreads();
+    return n;
 }
 // Largest and lowest key of a step.
 template <typename T>
 __device__ __noinline__ uint2 draw_step_ends(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned bin, DrawShared &s)
 {
     uint32_t most = 0, fewest = 0xffffffffu;
-    for (int i = threadIdx.x; i < a.vocab; i += kDrawThreads) {
-        const uint32_t k = row.at(a, i);
-        if (steps.has(k) && steps(k) == bin) { most = max(most, k); fewest = min(fewest, k); }
+    for (int i = 8 * threadIdx.x; i < a.vocab; i += kDrawStride) {
+        alignas(16) uint32_t k[8];
+        row.at(a, i, k);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (steps.has(k[j]) && steps(k[j]) == bin) { most = max(most, k[j]); fewest = min(fewest, k[j]); }
     }
     return draw_ends(most, fewest, s);
 }
@@ -250,8 +354,9 @@ template <typename T>
 __global__ void __launch_bounds__(kDrawThreads)
 draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
 {
-    __shared__ DrawShared s;
-    extern __shared__ uint32_t draw_stash[];
+    extern __shared__ __align__(16) unsigned char draw_smem[];
+    DrawShared &s = *reinterpret_cast<DrawShared *>(draw_smem);
+    uint32_t *const draw_stash = reinterpret_cast<uint32_t *>(draw_smem + sizeof(DrawShared));
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.vocab;
     const DrawRow<T> row{draw_stash, r, stashed};
     if (tid < 64) s.power[tid] = exp2(tid / 64.0);
@@ -260,13 +365,20 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     // the largest and the lowest
     uint32_t top = 0, low = 0xffffffffu;
     unsigned able = 0;                                             // ids that can be drawn
-#pragma unroll 4
-    for (int i = tid; i < V; i += kDrawThreads) {
-        const uint32_t k = draw_load<T>(a, r, i);
-        if (i < stashed) draw_stash[i] = k;
-        top = max(top, k);
-        low = min(low, k - 1u);                                    // (a key of 0 becomes the largest number)
-        able += k != 0u;
+#pragma unroll 2
+    for (int i = 8 * tid; i < V; i += kDrawStride) {
+        alignas(16) uint32_t k[8];
+        draw_keys<T>(a, r, i, k);
+        if (i < stashed) {
+            *reinterpret_cast<uint4 *>(draw_stash + i) = *reinterpret_cast<const uint4 *>(k);
+            *reinterpret_cast<uint4 *>(draw_stash + i + 4) = *reinterpret_cast<const uint4 *>(k + 4);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            top = max(top, k[j]);
+            low = min(low, k[j] - 1u);                             // (a key of 0 becomes the largest number)
+            able += k[j] != 0u;
+        }
     }
     const uint2 ends = draw_ends(top, low, s);
     top = ends.x;
@@ -313,26 +425,24 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     const uint32_t min_key = s.min_key;
 
     uint32_t thr = low;                                            // the border: keys above thr, and the first `ties` ids with just that key
-    unsigned ties = 0xffffffffu, n = 0;
-    bool listed = able <= kDrawList, cut = false;                  // all that can be kept is in the list, sorted; what is in the list's first n is kept
-    if (listed) {
-        draw_gather(a, row, DrawSteps(top, low), 0u, kDrawBins - 1u, s);
-    } else if (by_count) {
+    unsigned ties = 0xffffffffu;
+    bool few = able <= kDrawList, cut = false;                     // at most 2048 ids can be kept; top_p cuts nothing more
+    unsigned keys = able;                                          // with keys of thr and above
+    if (by_count) {
+        few = few || top_k <= kDrawList;
         DrawSteps steps(top, low);
         unsigned long long start = 0;
-        for (bool first = true;; first = false) {
+        for (;;) {
             draw_histogram(a, row, steps, false, s);
             draw_find(false, (double)top_k, start, s);
             const unsigned bin = s.bin, in_bin = s.bin_count;
             const unsigned long long before = s.before;
-            listed = first && before + in_bin <= kDrawList;
-            if (listed || in_bin <= kDrawList) {
-                draw_gather(a, row, steps, listed ? 0u : bin, bin, s);
-                if (!listed) {
-                    const unsigned last = (unsigned)(top_k - before) - 1u;   // that is kept
-                    thr = (uint32_t)(s.list[last] >> 32);
-                    ties = last + 1u - draw_first_equal(s, last);
-                }
+            if (in_bin <= kDrawList) {
+                draw_gather(a, row, steps, bin, bin, s);
+                const unsigned last = (unsigned)(top_k - before) - 1u;   // that is kept
+                thr = (uint32_t)(s.list[last] >> 32);
+                ties = last + 1u - draw_first_equal(s, last);
+                keys = last + 1u < in_bin && (uint32_t)(s.list[last + 1u] >> 32) == thr ? 0xffffffffu : (unsigned)top_k;   // (more ids with just the border's key)
                 break;
             }
             // too many in one step: between its own largest and lowest
@@ -340,74 +450,119 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
             if (e.x == e.y) {
                 thr = e.x;
                 ties = (unsigned)(top_k - before);
+                keys = 0xffffffffu;
                 break;
             }
             steps = DrawSteps(e.x, e.y);
             start = before;
         }
     }
-    if (!listed && min_key > thr && min_p > 0.0) {
+    if (!few && min_key > thr) {
         // few by min_p, whose mass is below top_p of all: then top_p cuts nothing more
-        unsigned long long sum = 0, few = 0;
+        unsigned long long sum = 0, part = 0;
         unsigned many = 0, equal = 0;
-#pragma unroll 2
-        for (int i = tid; i < V; i += kDrawThreads) {
-            const uint32_t k = row.at(a, i);
-            if (k < thr) continue;
-            const unsigned long long w = by_mass && k > thr ? draw_weight(k, s) : 0;
-            sum += w;
-            equal += k == thr;
-            if (k >= min_key) { few += w; ++many; }
+        for (int i = 8 * tid; i < V; i += kDrawStride) {
+            alignas(16) uint32_t k[8];
+            row.at(a, i, k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (k[j] < thr) continue;
+                const unsigned long long w = by_mass && k[j] > thr ? draw_weight(k[j], s) : 0;
+                sum += w;
+                equal += k[j] == thr;
+                if (k[j] >= min_key) { part += w; ++many; }
+            }
         }
         many = (unsigned)draw_scan(many, &unused, s);
-        bool first = !by_mass;
+        cut = !by_mass;
         if (by_mass) {
             const unsigned long long border = min(draw_scan(equal, &unused, s), (unsigned long long)ties) * draw_weight_of(thr, s);
             const double goal = fmax((double)top_p, 0.0) * (double)(draw_scan(sum, &unused, s) + border);
-            first = (double)draw_scan(few, &unused, s) < goal;
+            cut = (double)draw_scan(part, &unused, s) < goal;
         }
-        if (first) {
+        if (cut) {
             thr = min_key;
             ties = 0xffffffffu;
-            if (many <= kDrawList) {
-                draw_gather(a, row, DrawSteps(top, min_key), 0u, kDrawBins - 1u, s);
-                listed = cut = true;
-                n = many;
-            }
+            keys = many;
+            few = many <= kDrawList;
         }
-        if (first && !listed) cut = true;
     }
-    if (listed && !cut) {
-        n = min((unsigned)top_k, s.n);
-        // two entries a thread: their weights, the mass before them
-        const uint32_t k0 = (uint32_t)(s.list[2 * tid] >> 32), k1 = (uint32_t)(s.list[2 * tid + 1] >> 32);
-        const unsigned long long w0 = 2u * tid < n ? draw_weight_of(k0, s) : 0, w1 = 2u * tid + 1u < n ? draw_weight_of(k1, s) : 0;
+    if (few) {
+        unsigned n = keys;
+        if (keys <= kDrawSorted) {                                 // in any order, and then sorted, takes half the time
+            draw_gather(a, row, DrawSteps(top, thr), 0u, kDrawBins - 1u, s);
+            const unsigned long long e = s.list[min((unsigned)tid, kDrawList - 1u)];
+            __syncthreads();
+            if (tid < n) s.list[tid] = e << 32 | e >> 32;
+            draw_sort(s, n);
+            if (tid < n) {
+                s.key[tid] = (uint32_t)s.list[tid];
+                s.id[tid] = 0xffffffffu - (uint32_t)(s.list[tid] >> 32);
+            }
+            __syncthreads();
+        } else {
+            n = draw_list(a, row, thr, ties, s);
+        }
+        // two entries a thread
+        const uint32_t k0 = s.key[2 * tid], k1 = s.key[2 * tid + 1];
+        const bool has0 = 2u * tid < n, has1 = 2u * tid + 1u < n;
+        const unsigned long long w0 = has0 ? draw_weight_of(k0, s) : 0, w1 = has1 ? draw_weight_of(k1, s) : 0;
         unsigned long long before;
-        const unsigned long long total = draw_scan(w0 + w1, &before, s);
-        const double goal = by_mass ? fmax((double)top_p, 0.0) * (double)total : INFINITY;
-        const unsigned in0 = 2u * tid < n && (tid == 0 || ((double)before < goal && k0 >= min_key)),
-                       in1 = 2u * tid + 1u < n && (double)(before + w0) < goal && k1 >= min_key;
-        n = (unsigned)draw_scan(in0 + in1, &unused, s);            // (a head of the list)
-    }
-    if (listed) {
-        // by id
-        unsigned long long e0 = s.list[2 * tid], e1 = s.list[2 * tid + 1], before;
+        unsigned long long total = draw_scan(w0 + w1, &before, s);
+        bool in0 = has0 && k0 >= min_key, in1 = has1 && k1 >= min_key;
+        if (by_mass && !cut) {
+            // the border by mass among them
+            const double goal = fmax((double)top_p, 0.0) * (double)total;
+            DrawSteps steps(top, thr);
+            unsigned long long start = 0;
+            for (;;) {
+                for (int i = tid; i < kDrawBins; i += kDrawThreads) { s.count[i] = 0; s.mass[i] = 0; }
+                if (tid == 0) s.n = 0;
+                __syncthreads();
+                const unsigned b0 = has0 && steps.has(k0) ? steps(k0) : kDrawBins, b1 = has1 && steps.has(k1) ? steps(k1) : kDrawBins;
+                if (b0 < kDrawBins) { atomicAdd(&s.count[b0], 1u); atomicAdd(&s.mass[b0], w0); }
+                if (b1 < kDrawBins) { atomicAdd(&s.count[b1], 1u); atomicAdd(&s.mass[b1], w1); }
+                __syncthreads();
+                draw_find(true, goal, start, s);
+                const unsigned bin = s.bin;
+                start = s.before;
+                if (s.bin_count <= 64u) break;
+                const uint2 e = draw_ends(max(b0 == bin ? k0 : 0u, b1 == bin ? k1 : 0u), min(b0 == bin ? k0 : 0xffffffffu, b1 == bin ? k1 : 0xffffffffu), s);
+                if (e.x == e.y) break;
+                steps = DrawSteps(e.x, e.y);
+            }
+            // (of one step; or of equal keys, more than are sorted quickly)
+            const unsigned bin = s.bin;
+            if (has0 && steps.has(k0) && steps(k0) == bin) s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k0 << 32 | (0xffffffffu - 2u * tid);
+            if (has1 && steps.has(k1) && steps(k1) == bin) s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k1 << 32 | (0xfffffffeu - 2u * tid);
+            __syncthreads();
+            const unsigned in_bin = s.n;
+            draw_sort(s, in_bin);
+            const unsigned long long x0 = 2u * tid < in_bin ? draw_weight_of((uint32_t)(s.list[2 * tid] >> 32), s) : 0,
+                                     x1 = 2u * tid + 1u < in_bin ? draw_weight_of((uint32_t)(s.list[2 * tid + 1] >> 32), s) : 0;
+            unsigned long long at;
+            draw_scan(x0 + x1, &at, s);
+            at += start;
+            const unsigned kept = (unsigned)draw_scan((2u * tid < in_bin && (tid == 0 || (double)at < goal)) + (2u * tid + 1u < in_bin && (double)(at + x0) < goal), &unused, s);
+            const unsigned long long last = s.list[kept - 1u];     // as key and place in the list
+            in0 = in0 && ((unsigned long long)k0 << 32 | (0xffffffffu - 2u * tid)) >= last;
+            in1 = in1 && ((unsigned long long)k1 << 32 | (0xfffffffeu - 2u * tid)) >= last;
+        }
+        if (tid == 0) s.pick = 0x7fffffff;
+        total = draw_scan((in0 ? w0 : 0) + (in1 ? w1 : 0), &before, s);
+        if (in0) before += w0;
+        const double goal = goal_u * (double)total;
+        if (in0 && (double)before >= goal) atomicMin(&s.pick, 2 * tid);
+        else if (in1 && (double)(before + w1) >= goal) atomicMin(&s.pick, 2 * tid + 1);
         __syncthreads();
-        s.list[2 * tid] = e0 << 32 | e0 >> 32;
-        s.list[2 * tid + 1] = e1 << 32 | e1 >> 32;
-        if (tid == 0) s.pick = (int)n - 1;
-        __syncthreads();
-        draw_sort(s, n);
-        const unsigned long long v0 = 2u * tid < n ? draw_weight_of((uint32_t)s.list[2 * tid], s) : 0,
-                                 v1 = 2u * tid + 1u < n ? draw_weight_of((uint32_t)s.list[2 * tid + 1], s) : 0;
-        const unsigned long long total = draw_scan(v0 + v1, &before, s);
-        const double at = goal_u * (double)total;
-        if (2u * tid < n && (double)(before + v0) >= at) atomicMin(&s.pick, 2 * tid);
-        else if (2u * tid + 1u < n && (double)(before + v0 + v1) >= at) atomicMin(&s.pick, 2 * tid + 1);
-        __syncthreads();
+        if (s.pick == 0x7fffffff) {                                // (rounding, u = 1: the last that is kept)
+            const uint2 e = draw_ends(in1 ? 2u * tid + 2u : in0 ? 2u * tid + 1u : 0u, 0u, s);
+            if (tid == 0) s.pick = (int)e.x - 1;
+            __syncthreads();
+        }
         if (tid == 0) {
-            const uint32_t key = (uint32_t)s.list[s.pick];
-            a.tokens[r] = (int)(0xffffffffu - (uint32_t)(s.list[s.pick] >> 32));
+            const uint32_t key = s.key[s.pick];
+            a.tokens[r] = (int)s.id[s.pick];
             if (a.logprobs) a.logprobs[r] = (float)((key == top ? 0.0 : (draw_logit(key) - largest) / (double)temperature) - log((double)total / kDrawOne));
         }
         return;
@@ -417,7 +572,12 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         const uint32_t k_thr = thr;
         unsigned equal = 0;
         if (ties != 0xffffffffu) {
-            for (int i = tid; i < V; i += kDrawThreads) equal += row.at(a, i) == thr;
+            for (int i = 8 * tid; i < V; i += kDrawStride) {
+                alignas(16) uint32_t k[8];
+                row.at(a, i, k);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) equal += k[j] == thr;
+            }
             equal = (unsigned)draw_scan(equal, &unused, s);
         }
         const unsigned drop = equal - min(equal, ties);
@@ -467,7 +627,7 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         }
         __syncthreads();
     }
-    if (min_key > thr) {
+    if (!cut && min_key > thr) {
         thr = min_key;
         ties = 0xffffffffu;
     }
@@ -478,14 +638,18 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     int begin = 0, end = V;
     double goal = 0.0;
     for (int level = 0;; ++level) {
-        const int per = ((end - begin) + kDrawWarps - 1) / kDrawWarps, i0 = begin + warp * per, i1 = min(i0 + per, end);
+        const int per = ((end - begin + kDrawWarps - 1) / kDrawWarps + 7) & ~7, i0 = begin + warp * per, i1 = min(i0 + per, end);   // (begin: a multiple of 8)
         unsigned long long sum = 0;
         unsigned equal = 0, kept = 0;
-        for (int i = i0 + lane; i < i1; i += 32) {
-            const uint32_t k = row.at(a, i);
-            if (k < thr) continue;
-            if (k == thr) ++equal;
-            else { sum += draw_weight(k, s); ++kept; }
+        for (int i = i0 + 8 * lane; i < i1; i += 256) {
+            alignas(16) uint32_t k[8];
+            row.at(a, i, k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (k[j] < thr || i + j >= i1) continue;
+                if (k[j] == thr) ++equal;
+                else { sum += draw_weight(k[j], s); ++kept; }
+            }
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
@@ -499,6 +663,7 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         const unsigned long long w = draw_weight_of(thr, s);
         if (level == 0) {
             unsigned e = 0;
+#pragma unroll 1
             for (int x = 0; x < kDrawWarps; ++x) { total += s.warp_mass[x]; e += s.warp_count[x]; }
             total += min(e, ties) * w;
             goal = goal_u * (double)total;
@@ -510,6 +675,7 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         {
             unsigned long long run = before;
             unsigned eq = equal_before;
+#pragma unroll 1
             for (int x = 0; x < kDrawWarps; ++x) {
                 const unsigned e = min(eq + s.warp_count[x], ties) - min(eq, ties);
                 const unsigned long long after = run + s.warp_mass[x] + e * w;
@@ -532,7 +698,12 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     // up to 32 ids: a lane each
     if (warp == 0) {
         const int i = begin + lane;
-        const uint32_t k = i < end ? row.at(a, i) : 0u;
+        alignas(16) uint32_t k8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if ((i & ~7) < end) row.at(a, i & ~7, k8);
+        uint32_t k = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((i & 7) == j && i < end) k = k8[j];
         bool kept = i < end && k >= thr;
         const unsigned equal = __ballot_sync(0xffffffffu, kept && k == thr);
         if (kept && k == thr) kept = equal_before + __popc(equal & ((1u << lane) - 1u)) < ties;
@@ -553,19 +724,20 @@ namespace {
 template <typename T>
 cudaError_t launch_draw(const DrawArgs &a, dim3 grid, cudaStream_t st)
 {
-    constexpr int most = (227 * 1024 - (int)sizeof(DrawShared) - 1024) / 4;
+    constexpr int most = (227 * 1024 - (int)sizeof(DrawShared)) / 4;   // keys that fit
+    static_assert(sizeof(DrawShared) % 16 == 0, "keys behind it");
     static int told[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const bool known = dev >= 0 && dev < 64;
     if (!known || !__atomic_load_n(&told[dev], __ATOMIC_ACQUIRE)) {
-        e = cudaFuncSetAttribute((const void *)draw_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, most * 4);
+        e = cudaFuncSetAttribute((const void *)draw_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
         if (e != cudaSuccess) return e;
         if (known) __atomic_store_n(&told[dev], 1, __ATOMIC_RELEASE);
     }
-    const int stashed = a.vocab < most ? a.vocab : most;
-    return launch_pdl(draw_kernel<T>, grid, kDrawThreads, (size_t)stashed * 4, st, a, stashed);
+    const int stashed = a.vocab <= (most & ~7) ? (a.vocab + 7) & ~7 : most & ~7;
+    return launch_pdl(draw_kernel<T>, grid, kDrawThreads, sizeof(DrawShared) + (size_t)stashed * 4, st, a, stashed);
 }
 
 }  // namespace
@@ -589,6 +761,8 @@ extern "C" int adsa_sample(const adsa_sampling *how, int dtype, const void *logi
     DrawArgs a = {};
     a.logits = logits; a.uncond = uncond; a.row = row; a.uncond_row = uncond_row;
     a.rows = rows; a.vocab = vocab;
+    const long long pitch = dtype == ADSA_F32 ? 4 : 8;             // elements of 16 bytes
+    a.wide = (((uintptr_t)logits | (uintptr_t)uncond) & 15) == 0 && row % pitch == 0 && (!uncond || uncond_row % pitch == 0);
     a.guidance = how->guidance; a.temperature = how->temperature; a.top_p = how->top_p; a.min_p = how->min_p; a.top_k = how->top_k;
     a.temperatures = how->temperatures; a.top_ps = how->top_ps; a.min_ps = how->min_ps; a.top_ks = how->top_ks;
     a.uniforms = uniforms; a.tokens = tokens; a.logprobs = logprobs;
