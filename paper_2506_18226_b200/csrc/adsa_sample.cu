@@ -59,6 +59,29 @@ __device__ __forceinline__ void draw_load8(const T *row, int i, int vocab, bool 
 #pragma unroll
             for (int j = 0; j < 4; ++j) *reinterpret_cast<float2 *>(x + 2 * j) = unpack2<T>(p[j]);
         }
+    } else if (i >= 8 && i + 16 <= vocab) {
+        // from the 16-byte pieces around them, shifted by what the row is off (a multiple of the type's size)
+        constexpr int WORDS = sizeof(T) == 4 ? 12 : 8;
+        const uintptr_t at = (uintptr_t)(row + i);
+        const uint4 *p = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
+        uint32_t w[WORDS];
+#pragma unroll
+        for (int j = 0; j < WORDS; j += 4) {
+            const uint4 v = __ldg(p + j / 4);
+            w[j] = v.x; w[j + 1] = v.y; w[j + 2] = v.z; w[j + 3] = v.w;
+        }
+        const unsigned off = (unsigned)(at & 15);
+#pragma unroll
+        for (int j = 0; j + 2 < WORDS; ++j) w[j] = off & 8 ? w[j + 2] : w[j];
+#pragma unroll
+        for (int j = 0; j + 1 < WORDS; ++j) w[j] = off & 4 ? w[j + 1] : w[j];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<float2 *>(x + 2 * j) = unpack2<T>(off & 2 ? __funnelshift_r(w[j], w[j + 1], 16) : w[j]);
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = i + j < vocab ? to_f32(row[i + j]) : 0.f;
@@ -457,28 +480,28 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
             start = before;
         }
     }
-    if (!few && min_key > thr) {
-        // few by min_p, whose mass is below top_p of all: then top_p cuts nothing more
-        unsigned long long sum = 0, part = 0;
-        unsigned many = 0, equal = 0;
+    if (!few && min_key > thr && largest != INFINITY) {
+        // Few by min_p, whose mass is well below top_p of all, by weights in 32 bits (sums of a thread's ids, off by 2^-12 at most): then top_p
+        // cuts nothing more.
+        float sum = 0.f, part = 0.f;
+        unsigned many = 0;
+        const float high = draw_logit(top), scale = 1.44269504f / temperature;
         for (int i = 8 * tid; i < V; i += kDrawStride) {
             alignas(16) uint32_t k[8];
             row.at(a, i, k);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (k[j] < thr) continue;
-                const unsigned long long w = by_mass && k[j] > thr ? draw_weight(k[j], s) : 0;
-                sum += w;
-                equal += k[j] == thr;
-                if (k[j] >= min_key) { part += w; ++many; }
+                const float w = k[j] >= thr && by_mass ? exp2f((draw_logit(k[j]) - high) * scale) : 0.f;   // (with ties that top_k leaves out: more)
+                sum += k[j] > thr ? w : 0.f;
+                part += k[j] >= min_key ? w : 0.f;
+                many += k[j] >= min_key;
             }
         }
         many = (unsigned)draw_scan(many, &unused, s);
         cut = !by_mass;
         if (by_mass) {
-            const unsigned long long border = min(draw_scan(equal, &unused, s), (unsigned long long)ties) * draw_weight_of(thr, s);
-            const double goal = fmax((double)top_p, 0.0) * (double)(draw_scan(sum, &unused, s) + border);
-            cut = (double)draw_scan(part, &unused, s) < goal;
+            const unsigned long long all = draw_scan((unsigned long long)(sum * 1048576.f), &unused, s), kept = draw_scan((unsigned long long)(part * 1048576.f) + 1u, &unused, s);
+            cut = (double)kept * 1.001 < (double)top_p * (double)all * 0.999;
         }
         if (cut) {
             thr = min_key;
