@@ -15,7 +15,8 @@ halves are fed the same sampled ids.
 SharedPromptShell is the same decoder for several images of ONE prompt, nothing evicted: the condition's rows are kept
 once per guidance half in a paged cache and every decode step sweeps them once for all images, the new rows are rotated
 on their way into the cache, the residual additions and normalisations are one call each, and a whole decode step is one
-CUDA graph (every length and position it needs lies on the device).
+CUDA graph (every length and position it needs lies on the device).  Conditions of different lengths are prefilled end to end
+(packed attention), and tokens that are given, the upper part of an image say, enter several cells at a time (chunk attention).
 """
 from __future__ import annotations
 
@@ -43,6 +44,8 @@ class ShellConfig:
     temperature: float = 1.0
     norm_eps: float = 1e-5
     sandwich_norm: bool = False         # SharedPromptShell: a normalisation after each block too, before its residual addition
+    top_p: float = 1.0                  # with top_k: the smallest head of the most likely ids that holds top_p of their mass,
+    min_p: float = 0.0                  # and of these the ids at least min_p times as likely as the first
 
     @property
     def head_dim(self) -> int:
@@ -106,6 +109,15 @@ class _Decoder:
     wq = property(lambda self: self.wqkv_t[:, 0].transpose(1, 2))
     wk = property(lambda self: self.wqkv_t[:, 1].transpose(1, 2))
     wv = property(lambda self: self.wqkv_t[:, 2].transpose(1, 2))
+
+    def _draw(self, logits, u):
+        """The next token of every image from the logits of both halves, with guidance."""
+        c, n = self.cfg, self.cfg.n_images
+        if c.top_p < 1 or c.min_p > 0:
+            B.sample(logits[:n], u, temperature=c.temperature, top_k=min(c.top_k, c.vocab), top_p=c.top_p, min_p=c.min_p, uncond=logits[n:],
+                     guidance=c.cfg_scale, tokens=self.tokens)
+        else:
+            B.cfg_sample(logits, c.cfg_scale, min(c.top_k, c.vocab), c.temperature, u, tokens=self.tokens)
 
     def generate(self, text_emb, n_cells=None):
         """Prefill and decode `n_cells` grid cells (default: the whole grid); returns the ids on the host, [cells, n_images]."""
@@ -194,7 +206,7 @@ class LlamaGenShell(_Decoder):
         c = self.cfg
         B.rmsnorm(self.x, self.norm_f, out=self.h, eps=c.norm_eps)
         torch.mm(self.h, self.head.t(), out=self.logits)
-        B.cfg_sample(self.logits, c.cfg_scale, min(c.top_k, c.vocab), c.temperature, self.u, tokens=self.tokens)
+        self._draw(self.logits, self.u)
 
     def _segments(self):
         L = self.cfg.n_layers
@@ -258,7 +270,7 @@ class LlamaGenShell(_Decoder):
         c = self.cfg
         h = B.rmsnorm(x_last, self.norm_f, eps=c.norm_eps)
         torch.mm(h, self.head.t(), out=self.logits)
-        B.cfg_sample(self.logits, c.cfg_scale, min(c.top_k, c.vocab), c.temperature, self.uniforms[cell], tokens=self.tokens)
+        self._draw(self.logits, self.uniforms[cell])
         self.ids_host[cell].copy_(self.tokens, non_blocking=True)          # ids leave the GPU as they are drawn
         self.kernel_calls += 2
         return self.tokens
@@ -316,10 +328,13 @@ class SharedPromptShell(_Decoder):
 
     def prefill(self, text_emb):
         """The condition, text_emb [2, n_text, dim] bf16 (conditional, unconditional), enters the shared pages; row i of it
-        attends rows 0 .. i, as so many queries over the same pages with lengths 1, 2, ..  Draws the first tokens."""
+        attends rows 0 .. i, as so many queries over the same pages with lengths 1, 2, ..  Draws the first tokens.  Or two
+        tensors [rows, dim] of 1 to n_text rows each: both enter end to end."""
         self.next_cell = None                                              # (until the condition is whole)
         with torch.cuda.device(self.dev):                                  # (calls go to the current device's stream)
-            return self._prefill(text_emb)
+            if torch.is_tensor(text_emb):
+                return self._prefill(text_emb)
+            return self._prefill_pair(*text_emb)
 
     def _prefill(self, text_emb):
         c, T, H, d = self.cfg, self.cfg.n_text, self.cfg.n_heads, self.cfg.head_dim
@@ -343,13 +358,82 @@ class SharedPromptShell(_Decoder):
         for layer in range(c.n_layers):
             self._block(layer, x, h, y, attend)
         self.kernel_calls += 1 + (5 + len(range(0, 2 * T, self.ATTN_ROWS))) * c.n_layers + 1
+        self.prefix_rows.fill_(T)
+        return self._first_tokens(h.view(2, T, c.dim)[:, -1])
+
+    def _prefill_pair(self, cond, uncond):
+        c, H, d = self.cfg, self.cfg.n_heads, self.cfg.head_dim
+        i32 = dict(dtype=torch.int32, device=self.dev)
+        lens = [cond.shape[0], uncond.shape[0]]
+        if min(lens) < 1 or max(lens) > c.n_text or cond.shape[1] != c.dim or uncond.shape[1] != c.dim:
+            raise ValueError(f"prefill: conditions of 1 to {c.n_text} rows of {c.dim}, got {list(cond.shape)} and {list(uncond.shape)}")
+        n = sum(lens)
+        x = torch.cat([cond, uncond]).to(device=self.dev, dtype=torch.bfloat16)
+        h, y = B.rmsnorm(x, self.norm1[0], eps=c.norm_eps), torch.empty_like(x)
+        cu = torch.tensor([0, lens[0], n], **i32)
+        none = torch.zeros(2, **i32)
+        out = torch.empty(n, H, d, dtype=torch.bfloat16, device=self.dev)
+        ws = B.prompt_workspace(out, H, 2)
+
+        def attend(layer, h):                                              # (the condition is not rotated)
+            q, k, v = torch.matmul(h.unsqueeze(0), self.wqkv_t[layer]).view(3, n, H, d)
+            B.paged_append(k, v, self.k_pool[layer], self.v_pool[layer], self.prefix_table, none, cu_tokens=cu, status=self.status)
+            return B.packed_attn(q, k, v, cu, out=out, workspace=ws).view(n, c.dim)
+
+        for layer in range(c.n_layers):
+            self._block(layer, x, h, y, attend)
+        self.kernel_calls += 1 + 5 * c.n_layers + 1
+        self.prefix_rows.copy_(cu[1:] - cu[:-1])
+        return self._first_tokens(h[(cu[1:] - 1).long()])
+
+    def _first_tokens(self, last):
+        """From the conditions' last rows, [2, dim]."""
         self.n_before.zero_()
         self.n_after.fill_(1)
         self.cell.fill_(0)
-        self.h.copy_(h.view(2, T, c.dim)[:, -1].repeat_interleave(c.n_images, 0))   # every image starts from the same row
+        self.h.copy_(last.repeat_interleave(self.cfg.n_images, 0))          # every image starts from the same row
         self._sample()
         self.ids_host[0].copy_(self.tokens, non_blocking=True)
         self.next_cell = 1
+        return self.tokens
+
+    def given(self, ids):
+        """Tokens that are given rather than drawn: ids [cells, n_images] are those of the cells from the last drawn one on (after
+        prefill: of the first cells), in its place; all enter the cache in one pass, each attending the condition and the cells
+        up to itself.  Draws the cell behind them, which decode_step then follows."""
+        c, n, m, H, d = self.cfg, self.cfg.n_images, ids.shape[0], self.cfg.n_heads, self.cfg.head_dim
+        cells = c.grid_h * c.grid_w
+        if self.next_cell is None or m < 1 or ids.shape[1:] != (n,) or self.next_cell - 1 + m >= cells:
+            raise ValueError(f"given: {list(ids.shape)} ids cannot follow, the next cell is {self.next_cell} of {cells} (None: prefill first)")
+        first = self.next_cell - 1
+        self.next_cell = None
+        with torch.cuda.device(self.dev):
+            ids = ids.to(device=self.dev, dtype=torch.int32)
+            x = self.tok_emb[ids.t().repeat(2, 1).reshape(-1).long()]       # batch rows outermost: conditional, then unconditional
+            h, y = B.rmsnorm(x, self.norm1[0], eps=c.norm_eps), torch.empty_like(x)
+            pos = self.positions[first:first + m].repeat(c.batch, 1)
+            after = self.n_before + m
+            out = torch.empty(c.batch * m, H, d, dtype=torch.bfloat16, device=self.dev)
+            ws = B.prompt_workspace(out, H, c.batch)
+
+            def attend(layer, h):
+                q, k, v = torch.matmul(h.unsqueeze(0), self.wqkv_t[layer]).view(3, c.batch * m, H, d)
+                B.paged_append(k, v, self.k_pool[layer], self.v_pool[layer], self.page_table, self.n_before, rotary=self.rotary, pos=pos, q=q, q_out=q,
+                               status=self.status)
+                B.chunk_attn(q, self.k_pool[layer], self.v_pool[layer], self.page_table, after, None, self.prefix_table, self.prefix_rows, self.group_start,
+                             out=out, workspace=ws, status=self.status)
+                return out.view(c.batch * m, c.dim)
+
+            for layer in range(c.n_layers):
+                self._block(layer, x, h, y, attend)
+            for t in (self.n_before, self.n_after, self.cell):
+                t.add_(m)
+            self.h.copy_(h.view(c.batch, m, c.dim)[:, -1])
+            self._sample()
+            self.ids_host[first:first + m].copy_(ids, non_blocking=True)
+            self.ids_host[first + m].copy_(self.tokens, non_blocking=True)
+        self.kernel_calls += 1 + 5 * c.n_layers + 1
+        self.next_cell = first + m + 1
         return self.tokens
 
     def _sample(self):
@@ -357,7 +441,7 @@ class SharedPromptShell(_Decoder):
         c = self.cfg
         torch.mm(self.h, self.head.t(), out=self.logits)
         torch.index_select(self.uniforms, 0, self.cell, out=self.u.view(1, -1))
-        B.cfg_sample(self.logits, c.cfg_scale, min(c.top_k, c.vocab), c.temperature, self.u, tokens=self.tokens)
+        self._draw(self.logits, self.u)
 
     def _attend(self, layer, h):
         c = self.cfg
