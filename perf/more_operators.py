@@ -182,8 +182,9 @@ def run(s):
             A.chunk_attn(s["q"], s["k_pool"], s["v_pool"], s["table"], s["n_rows"], s["cu"], s["p_table"], s["p_rows"], s["start"],
                          out=s["out"], lse=s["lse"], workspace=s["workspace"])
             return s["out"], s["lse"]
-        return A.sample(s["logits"], s["u"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"], min_p=s["min_p"],
-                        uncond=s["uncond"], guidance=4.0, tokens=s["tokens"], logprobs=s["logprobs"])
+        A.sample(s["logits"], s["u"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"], min_p=s["min_p"],
+                 uncond=s["uncond"], guidance=4.0, tokens=s["tokens"], logprobs=s["logprobs"])
+        return s["tokens"], s["logprobs"]
     if op == "packed":
         return _plain_packed(s)
     if op == "chunk":
