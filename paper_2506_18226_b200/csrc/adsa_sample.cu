@@ -9,7 +9,8 @@
 // A block per row; keys lie in shared memory, as many as fit.  A border is found by a histogram of 2048 steps between the largest and the
 // lowest logit, of counts or of masses, and a sort of the step that holds it (where one step holds over 2048 ids: by steps between its own
 // ends).  Where up to 2048 ids can be kept, they are listed in order of their ids once, and the rest works on the list; else over the row.
-// (Sorting such a list, by logit and then by id, took 30000 clocks each time: 46 us for one row of 16384.)
+// (Sorting 2048 of them, by logit and then by id, took 30000 clocks each time: 46 us for one row of 16384.)  Up to 1024, or up to 256 by top_k,
+// are gathered in one pass and sorted both ways.
 #include <float.h>
 #include <math.h>
 
@@ -18,7 +19,7 @@
 namespace adsa {
 
 constexpr int kDrawThreads = 1024, kDrawWarps = kDrawThreads / 32;
-constexpr unsigned kDrawSorted = 256;        // entries that are sorted by id rather than listed in order
+constexpr int kDrawShort = 256;              // top_k up to which the threads' largest keys show where it lies
 constexpr int kDrawBins = 2048, kDrawList = 2048;   // steps of a histogram; entries that are sorted
 constexpr int kDrawMaxVocab = 1 << 20;       // so that 2^20 weights of 2^42 fit 63 bits
 constexpr double kDrawOne = 4398046511104.0;   // 2^42
@@ -137,6 +138,12 @@ __device__ __forceinline__ double draw_share(uint32_t key, const DrawShared &s)
     const double y = p * s.power[n & 63];
     return __hiloint2double(__double2hiint(y) + ((n >> 6) << 20), __double2loint(y));
 }
+__device__ __forceinline__ float draw_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // ... as a whole multiple of 2^-42
 __device__ __forceinline__ unsigned long long draw_weight(uint32_t key, const DrawShared &s)
 {
@@ -165,7 +172,28 @@ __device__ __noinline__ unsigned long long draw_scan(unsigned long long x, unsig
 // The list's n entries, largest first (room for a power of two).
 __device__ __noinline__ void draw_sort(DrawShared &s, unsigned n)
 {
-    unsigned size = 2;
+    if (n <= 64) {                                                 // a warp's registers hold them: entries lane, lane + 32
+        if (threadIdx.x < 32) {
+            const unsigned lane = threadIdx.x;
+            unsigned long long x[2] = {lane < n ? s.list[lane] : 0, lane + 32 < n ? s.list[lane + 32] : 0};
+#pragma unroll 1
+            for (unsigned k = 2; k <= 64; k *= 2) {
+#pragma unroll 1
+                for (unsigned j = k / 2; j; j /= 2) {
+                    const unsigned long long y0 = j == 32 ? x[1] : __shfl_xor_sync(0xffffffffu, x[0], j & 31), y1 = j == 32 ? x[0] : __shfl_xor_sync(0xffffffffu, x[1], j & 31);
+                    // the lower of a pair keeps the larger, where larger ones come first
+                    const bool low0 = j == 32 || !(lane & j), low1 = j != 32 && !(lane & j);
+                    x[0] = (x[0] > y0) == (low0 == ((lane & k) == 0)) ? x[0] : y0;
+                    x[1] = (x[1] > y1) == (low1 == (((lane + 32) & k) == 0)) ? x[1] : y1;
+                }
+            }
+            s.list[lane] = x[0];
+            s.list[lane + 32] = x[1];
+        }
+        __syncthreads();
+        return;
+    }
+    unsigned size = 128;
     while (size < n) size *= 2;
     for (unsigned i = n + threadIdx.x; i < size; i += kDrawThreads) s.list[i] = 0;
     for (unsigned k = 2; k <= size; k *= 2) {
@@ -251,7 +279,8 @@ __device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, D
     }
     __syncthreads();
 }
-// The ids with keys of the steps from `first` to `last` into the list, as key and id, sorted: larger keys first, of equal ones lower ids.
+// The ids with keys of the steps from `first` to `last` into the list, as key and id, sorted: larger keys first, of equal ones lower ids.  s.n: how
+// many there are; more than the list holds are not sorted.
 template <typename T>
 __device__ __noinline__ void draw_gather(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned first, unsigned last, DrawShared &s)
 {
@@ -265,11 +294,13 @@ __device__ __noinline__ void draw_gather(const DrawArgs &a, DrawRow<T> row, Draw
         for (int j = 0; j < 8; ++j) {
             if (!steps.has(k[j])) continue;
             const unsigned b = steps(k[j]);
-            if (b >= first && b <= last) s.list[atomicAdd(&s.n, 1u)] = (unsigned long long)k[j] << 32 | (0xffffffffu - (unsigned)(i + j));
+            if (b < first || b > last) continue;
+            const unsigned at = atomicAdd(&s.n, 1u);
+            if (at < kDrawList) s.list[at] = (unsigned long long)k[j] << 32 | (0xffffffffu - (unsigned)(i + j));
         }
     }
     __syncthreads();
-    draw_sort(s, s.n);
+    if (s.n <= kDrawList) draw_sort(s, s.n);
 }
 // The ids that can be kept into s.key and s.id in their order: keys above thr, and the first `ties` with just that key; a warp per segment of ids,
 // 256 at a time.
@@ -403,6 +434,7 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
             able += k[j] != 0u;
         }
     }
+    const uint32_t mine = top;
     const uint2 ends = draw_ends(top, low, s);
     top = ends.x;
     low = ends.y + 1u;
@@ -450,8 +482,29 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
     uint32_t thr = low;                                            // the border: keys above thr, and the first `ties` ids with just that key
     unsigned ties = 0xffffffffu;
     bool few = able <= kDrawList, cut = false;                     // at most 2048 ids can be kept; top_p cuts nothing more
-    unsigned keys = able;                                          // with keys of thr and above
-    if (by_count) {
+    // The short way: what can be kept lies in the list, sorted, `n` of it by top_k.
+    bool listed = false;
+    unsigned n = 0;
+    if (able <= kDrawThreads) {
+        draw_gather(a, row, DrawSteps(top, low), 0u, kDrawBins - 1u, s);
+        listed = true;
+        n = (unsigned)top_k;
+    } else if (by_count && top_k <= kDrawShort) {
+        // The threads' largest keys: the top_k-th of them is not above the top_k-th of all, and few others are above it.
+        for (int i = tid; i < kDrawBins; i += kDrawThreads) s.count[i] = 0;
+        __syncthreads();
+        const DrawSteps steps(top, low);
+        if (mine) atomicAdd(&s.count[steps(mine)], 1u);
+        __syncthreads();
+        draw_find(false, (double)top_k, 0, s);
+        const unsigned bin = s.bin;
+        if (s.before + s.bin_count >= (unsigned)top_k) {           // (else fewer threads than that have a key)
+            draw_gather(a, row, steps, 0u, bin, s);
+            listed = s.n <= kDrawThreads;
+            n = (unsigned)top_k;
+        }
+    }
+    if (!listed && by_count) {
         few = few || top_k <= kDrawList;
         DrawSteps steps(top, low);
         unsigned long long start = 0;
@@ -465,7 +518,6 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
                 const unsigned last = (unsigned)(top_k - before) - 1u;   // that is kept
                 thr = (uint32_t)(s.list[last] >> 32);
                 ties = last + 1u - draw_first_equal(s, last);
-                keys = last + 1u < in_bin && (uint32_t)(s.list[last + 1u] >> 32) == thr ? 0xffffffffu : (unsigned)top_k;   // (more ids with just the border's key)
                 break;
             }
             // too many in one step: between its own largest and lowest
@@ -473,14 +525,13 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
             if (e.x == e.y) {
                 thr = e.x;
                 ties = (unsigned)(top_k - before);
-                keys = 0xffffffffu;
                 break;
             }
             steps = DrawSteps(e.x, e.y);
             start = before;
         }
     }
-    if (!few && min_key > thr && largest != INFINITY) {
+    if (!listed && !few && min_key > thr && largest != INFINITY) {
         // Few by min_p, whose mass is well below top_p of all, by weights in 32 bits (sums of a thread's ids, off by 2^-12 at most): then top_p
         // cuts nothing more.
         float sum = 0.f, part = 0.f;
@@ -491,7 +542,7 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
             row.at(a, i, k);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float w = k[j] >= thr && by_mass ? exp2f((draw_logit(k[j]) - high) * scale) : 0.f;   // (with ties that top_k leaves out: more)
+                const float w = k[j] >= thr && by_mass ? draw_exp2((draw_logit(k[j]) - high) * scale) : 0.f;   // (with ties that top_k leaves out: more)
                 sum += k[j] > thr ? w : 0.f;
                 part += k[j] >= min_key ? w : 0.f;
                 many += k[j] >= min_key;
@@ -506,26 +557,40 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
         if (cut) {
             thr = min_key;
             ties = 0xffffffffu;
-            keys = many;
             few = many <= kDrawList;
+            // (a pass and a sort by logit and one by id, against two passes)
+            if (many <= 256u || (many <= kDrawThreads && V >= 65536)) {
+                draw_gather(a, row, DrawSteps(top, thr), 0u, kDrawBins - 1u, s);
+                listed = true;
+                n = many;
+            }
         }
     }
-    if (few) {
-        unsigned n = keys;
-        if (keys <= kDrawSorted) {                                 // in any order, and then sorted, takes half the time
-            draw_gather(a, row, DrawSteps(top, thr), 0u, kDrawBins - 1u, s);
-            const unsigned long long e = s.list[min((unsigned)tid, kDrawList - 1u)];
-            __syncthreads();
-            if (tid < n) s.list[tid] = e << 32 | e >> 32;
-            draw_sort(s, n);
-            if (tid < n) {
-                s.key[tid] = (uint32_t)s.list[tid];
-                s.id[tid] = 0xffffffffu - (uint32_t)(s.list[tid] >> 32);
-            }
-            __syncthreads();
-        } else {
-            n = draw_list(a, row, thr, ties, s);
+    if (listed) {
+        // an entry a thread
+        unsigned long long e = s.list[tid], before;
+        uint32_t key = (uint32_t)(e >> 32);
+        unsigned long long w = tid < n ? draw_weight_of(key, s) : 0, total = draw_scan(w, &before, s);
+        const double goal = by_mass && !cut ? fmax((double)top_p, 0.0) * (double)total : INFINITY;
+        n = (unsigned)draw_scan(tid < n && (tid == 0 || ((double)before < goal && key >= min_key)) ? 1u : 0u, &before, s);   // (a head of the list)
+        if (tid < n) s.list[tid] = e << 32 | e >> 32;              // by id
+        if (tid == 0) s.pick = (int)n - 1;
+        __syncthreads();
+        draw_sort(s, n);
+        e = s.list[tid];
+        key = (uint32_t)e;
+        w = tid < n ? draw_weight_of(key, s) : 0;
+        total = draw_scan(w, &before, s);
+        if (tid < n && (double)(before + w) >= goal_u * (double)total) atomicMin(&s.pick, tid);
+        __syncthreads();
+        if (tid == s.pick) {
+            a.tokens[r] = (int)(0xffffffffu - (uint32_t)(e >> 32));
+            if (a.logprobs) a.logprobs[r] = (float)((key == top ? 0.0 : (draw_logit(key) - largest) / (double)temperature) - log((double)total / kDrawOne));
         }
+        return;
+    }
+    if (few) {
+        n = draw_list(a, row, thr, ties, s);
         // two entries a thread
         const uint32_t k0 = s.key[2 * tid], k1 = s.key[2 * tid + 1];
         const bool has0 = 2u * tid < n, has1 = 2u * tid + 1u < n;
