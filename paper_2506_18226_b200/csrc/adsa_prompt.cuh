@@ -41,7 +41,7 @@ struct PromptArgs {
     float *state, *state_ml;
     int box_rows, box_shift;                // rows of a copy's box (a power of two, its logarithm); 0: K and V are copied row by row
     int q_boxes, tokens_first;              // q by boxes; the order in the maps of packed k (bit 1) and v (bit 2): tokens before heads
-    int shifted;                            // packed k and v by boxes that begin up to 7 elements before a head's row
+    int shifted, q_shifted;                 // packed k and v (q) by boxes that begin up to 7 elements before a head's row
     int split;                              // items may be cut (into partial states)
 };
 

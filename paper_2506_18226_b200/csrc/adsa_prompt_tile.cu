@@ -29,7 +29,7 @@ namespace adsa {
 constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time
 constexpr int kFewMean = 32;                 // query rows per sequence and key head, on the mean, up to which the kernel for few rows runs
 struct TileControl {
-    uint64_t bars[42];
+    uint64_t bars[43];
     TileDesc ring[kTileRing];
     TilePos ends[2];                        // of this block's run
     uint32_t tmem;
@@ -56,7 +56,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     unsigned *const plan = reinterpret_cast<unsigned *>(ctl + sizeof(TileControl));
     const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 16, s_full = q_empty + 16,
                    p_full = s_full + 16, o_full = p_full + 64, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8,
-                   d_empty = d_full + 8 * kTileRing;
+                   d_empty = d_full + 8 * kTileRing, q_come = d_empty + 8 * kTileRing;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
 
     if (tid == 0) {
@@ -65,12 +65,13 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             mbar_init(q_full + 8 * g, 1); mbar_init(q_empty + 8 * g, 1); mbar_init(s_full + 8 * g, 1); mbar_init(o_full + 8 * g, 1);
             for (int i = 0; i < 4; ++i) mbar_init(p_full + 32 * g + 8 * i, 4);
         }
+        mbar_init(q_come, 1);
         c.limit = kCopySpinLimit;
         mbar_init(m_full, 4);
         mbar_init(m_empty, 4);
         for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 11); }
         mbar_init_fence();
-        if (a.q_boxes) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+        if (a.q_boxes || a.q_shifted) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
         if (a.box_rows) {
             asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
@@ -216,7 +217,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         }
         if (!PLAIN && waiting) flush();
     } else if (warp == 10) {                                       // ---- copies of Q ----
-        uint32_t phase = 0;                                        // bit h: of half h
+        uint32_t phase = 0, come = 0;                              // (phase: bit h of half h)
         const int q_piece = piece_of(a.q, a.q_token, a.q_head, a.d), tph = a.half_tokens;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
@@ -249,6 +250,16 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                                 for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x + 2 * shift, kSub), from + x);
                         }
                     };
+                    if (a.q_shifted) {                             // q's rows lie as K's do
+                        if (lane == 0) {
+                            const int boxes = (a.d + 63) / 64;
+                            mbar_expect_tx(q_come, (uint32_t)boxes * kSub);
+                            for (int s = 0; s < boxes; ++s) pa_tma(dst + s * kSub, &q_map, (int)(it.head * a.q_head) - shift + s * 64, (int)it.s.q0 + tok, q_come);
+                        }
+                        __syncwarp();
+                        wait(q_come, come);
+                        come ^= 1u;
+                    }
                     if (a.shifted) {                               // what K has beside the head's elements meets zeros
                         const int end = (a.d + shift + 15) / 16 * 16;
                         for (int r = lane; r < kTileRows; r += 32) {
@@ -256,9 +267,11 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                                 asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + tile_at(r, 2 * x, kSub)), "r"(0u) : "memory");
                         }
                     }
-                    if (piece == 16) by_rows(std::integral_constant<int, 16>());
-                    else if (piece == 8) by_rows(std::integral_constant<int, 8>());
-                    else by_rows(std::integral_constant<int, 4>());
+                    if (!a.q_shifted) {
+                        if (piece == 16) by_rows(std::integral_constant<int, 16>());
+                        else if (piece == 8) by_rows(std::integral_constant<int, 8>());
+                        else by_rows(std::integral_constant<int, 4>());
+                    }
                     asm volatile("cp.async.wait_all;" ::: "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -810,7 +823,7 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap
 {
     constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
     constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * kTileStage * 2 + sizeof(TileControl), most = 227 * 1024;
-    static_assert(2 * SLOTS + 26 <= 42, "barriers");
+    static_assert(2 * SLOTS + 27 <= 43, "barriers");
     const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
     if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
     const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, PLAIN>;
@@ -859,6 +872,7 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
             a.box_rows = kTileRows;                                // (elements of a head and the 6 before it fit its columns, in steps of 16)
             a.shifted = 1;
             a.q_boxes = 0;                                         // (q has to lie where the head's elements do, between zeros)
+            a.q_shifted = a.per_kv == 1 && (a.q_head - a.k_head) % 8 == 0 && shifted_map(&qm, dtype, a.q, a.d, heads, a.q_head, a.n_q, a.q_token);
         }
     }
     const unsigned blocks = (unsigned)sms;

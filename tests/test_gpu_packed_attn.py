@@ -111,6 +111,25 @@ def test_strides_and_alignment(d, offset, layout):
     assert torch.equal(flat, before)
 
 
+@pytest.mark.parametrize("d,H,KV", [(100, 6, 6), (100, 6, 3), (36, 4, 4), (50, 8, 8), (112, 5, 5), (66, 16, 16), (30, 8, 4)])
+@pytest.mark.parametrize("bad", [False, True])
+def test_heads_that_begin_between_16_byte_pieces(d, H, KV, bad):
+    """Dense rows whose tokens are 16-byte aligned and whose heads are not (they are read with what lies before them): the neighbours'
+    infinities and NaN have no effect."""
+    import paper_2506_18226_b200 as A
+    lens, g, pad = [300, 7, 129, 260], gen(d), -KV * d % 8
+    T = sum(lens)
+    q = randn(g, T, H * d + (-H * d % 8), scale=1.5)[:, :H * d].unflatten(1, (H, d))
+    k, v = (randn(g, T, KV * d + pad)[:, :KV * d].unflatten(1, (KV, d)) for _ in range(2))
+    if bad:
+        k[:, 1], v[:, 1], q[:, H // KV] = math.nan, math.inf, math.inf
+    out, lse = torch.empty(T, H, d, dtype=torch.bfloat16, device=DEV), torch.empty(T, H, device=DEV)
+    A.packed_attn(q, k, v, starts(lens), out=out, lse=lse)
+    g_ = H // KV
+    heads = [h for h in range(H) if not bad or h // g_ != 1]
+    verify(q[:, heads], k[:, [h // g_ for h in heads]], v[:, [h // g_ for h in heads]], lens, lens, True, out[:, heads].contiguous(), lse[:, heads].contiguous())
+
+
 def test_a_head_dimension_shared_by_all_key_heads():
     """k and v expanded over heads (a stride of zero)."""
     import paper_2506_18226_b200 as A
