@@ -87,7 +87,8 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     if (warp == 9) tc_alloc(smem_u32(&c.tmem), kTileColumns);
     pdl_wait();
     pdl_launch();
-    tile_plan<true>(a, plan, c.ends, warp, lane);
+    PromptSeq *const seqs = a.batch <= kTileSeqs ? reinterpret_cast<PromptSeq *>(plan + ((a.batch + 2) & ~1)) : nullptr;
+    tile_plan<true>(a, plan, seqs, c.ends, warp, lane);
     tc_before();
     __syncthreads();
     tc_after();
@@ -112,7 +113,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         return c.ring[at].t1 >= 0;
     };
     if (warp == 11) {                                              // ---- the list of items ----
-        tile_walk<true>(a, c.ends, c.ring, d_full, d_empty, lane, wait);
+        tile_walk<true>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, wait);
     } else if (warp == 8) {                                        // ---- copies of K and V ----
         int slot = 0;
         uint32_t phase = 0;
@@ -450,7 +451,7 @@ cudaError_t launch_few(const PromptArgs &a, unsigned blocks, const CUtensorMap &
 {
     constexpr size_t most = 227 * 1024, fixed = 1024 + (size_t)(SLOTS + 1) * NSUB * kTileRows * 128 + sizeof(FewControl);
     static_assert(2 * SLOTS + 18 <= 48, "barriers");
-    const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
+    const size_t smem = fixed + tile_list_bytes(a.batch);
     if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
     const auto kern = prompt_few_kernel<T, NSUB, SLOTS>;
     static int told[64];

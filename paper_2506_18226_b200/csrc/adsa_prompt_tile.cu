@@ -86,7 +86,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     if (warp == 9) tc_alloc(smem_u32(&c.tmem), kTileColumns);
     pdl_wait();
     pdl_launch();
-    tile_plan<WIDE>(a, plan, c.ends, warp, lane);
+    PromptSeq *const seqs = a.batch <= kTileSeqs ? reinterpret_cast<PromptSeq *>(plan + ((a.batch + 2) & ~1)) : nullptr;
+    tile_plan<WIDE>(a, plan, seqs, c.ends, warp, lane);
     tc_before();
     __syncthreads();
     tc_after();
@@ -116,7 +117,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     // 168 registers a thread at the launch: the groups take what the other four warps leave
     if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {                                              // ---- the list of items ----
-        tile_walk<WIDE>(a, c.ends, c.ring, d_full, d_empty, lane, wait);
+        tile_walk<WIDE>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, wait);
     } else if (warp == 8) {                                        // ---- copies of K and V ----
         int slot = 0, waiting = 0;                                 // waiting: row copies in flight that nobody knows of yet
         uint32_t phase = 0;
@@ -144,7 +145,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     const int r = r0 + i + (lane >> 3);
                     const unsigned char *from = src + __shfl_sync(0xffffffffu, off, i + (lane >> 3));
                     if (r < valid) {
-#pragma unroll 1
+#pragma unroll 4
                         for (int x = (lane & 7) * piece; x < bytes; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x, kSub), from + x);
                     }
                 }
@@ -242,11 +243,12 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     const int shift = shift_of(it.head, false), piece = shift ? min(q_piece, (2 * shift) & -(2 * shift)) : q_piece;
                     const auto by_rows = [&](auto piece_) {
                         constexpr int piece = decltype(piece_)::value;
-#pragma unroll 1
+#pragma unroll 2
                         for (int r0 = 0; r0 < tokens * a.per_kv; r0 += 4) {
                             const int r = r0 + (lane >> 3), t = a.by_per_kv(r);
                             const unsigned char *from = src + 2 * (t * a.q_token + (r - t * a.per_kv) * a.q_head);
                             if (r < tokens * a.per_kv)
+#pragma unroll 4
                                 for (int x = (lane & 7) * piece; x < 2 * a.d; x += 8 * piece) tile_copy<piece>(dst + tile_at(r, x + 2 * shift, kSub), from + x);
                         }
                     };
@@ -824,7 +826,7 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap
     constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
     constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * kTileStage * 2 + sizeof(TileControl), most = 227 * 1024;
     static_assert(2 * SLOTS + 27 <= 43, "barriers");
-    const size_t smem = fixed + (size_t)(a.batch + 1) * 4;
+    const size_t smem = fixed + tile_list_bytes(a.batch);
     if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
     const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, PLAIN>;
     static int told[64];

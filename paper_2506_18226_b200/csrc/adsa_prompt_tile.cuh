@@ -11,6 +11,7 @@ constexpr int kTileThreads = 384;           // warps 0 .. 3, 4 .. 7: two groups;
 constexpr int kTileColumns = 512;           // all of tensor memory: S (and P) of the groups at 0 and 128, O at 256 and 384
 constexpr float kTileSlack = 8.f;
 constexpr int kTileRing = 4;                // items ahead
+constexpr int kTileSeqs = 64;                // sequences that are kept in shared memory, read once
 constexpr int kFewRows = 32;                // query rows of an item of the kernel for few rows
 constexpr unsigned kTileMinRun = 6;         // units of a run, at least, where items may be cut
 
@@ -69,7 +70,7 @@ __device__ __forceinline__ int piece_of(const void *p, long long token, long lon
 
 // The item that unit u of the list lies in, and the tile that a run beginning there takes first; by a whole warp.
 template <bool WIDE>
-__device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, unsigned u, unsigned tol, int lane)
+__device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const PromptSeq *seqs, unsigned u, unsigned tol, int lane)
 {
     if (u >= plan[a.batch]) return {a.batch, 0, 0, 0};
     int b = 0;
@@ -78,7 +79,7 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, unsign
         b = b0 + done;
         if (done < 32) break;
     }
-    const PromptSeq s = prompt_seq(a, b);
+    const PromptSeq s = seqs ? seqs[b] : prompt_seq(a, b);
     const unsigned per_head = (plan[b + 1] - plan[b]) / (unsigned)a.kv_heads;
     unsigned rem = u - plan[b];
     const int head = (int)(rem / per_head);
@@ -110,13 +111,16 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, unsign
 
 // The list of the call's work, plan[b] units before sequence b, and where this block's run begins and ends; by all threads.
 template <bool WIDE>
-__device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, TilePos *ends, int warp, int lane)
+__device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, PromptSeq *seqs, TilePos *ends, int warp, int lane)
 {
     // units of every sequence: short ones by a lane each, long ones by their warp; then their running sum
     for (int b0 = warp * 32; b0 < a.batch; b0 += kTileThreads) {
         const int b = b0 + lane;
         PromptSeq s = {};
-        if (b < a.batch) s = prompt_seq(a, b);
+        if (b < a.batch) {
+            s = prompt_seq(a, b);
+            if (seqs) seqs[b] = s;
+        }
         const bool many = s.m > 32 * item_tokens<WIDE>(a);
         unsigned units = 0;
         if (!many) {
@@ -152,14 +156,14 @@ __device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, T
     if (warp >= 10) {                                              // where this block's run begins and ends
         const unsigned run = blockIdx.x + (warp - 10);
         const unsigned u = run > runs ? total : (unsigned)((unsigned long long)run * total / runs);
-        const TilePos at = tile_locate<WIDE>(a, plan, u, a.split ? total / runs / 32u : 0xffffffffu, lane);
+        const TilePos at = tile_locate<WIDE>(a, plan, seqs, u, a.split ? total / runs / 32u : 0xffffffffu, lane);
         if (lane == 0) ends[warp - 10] = at;
     }
 }
 
 // The warp that walks a block's run and names its items to the others, a few ahead of them.
 template <bool WIDE, typename Wait>
-__device__ __forceinline__ void tile_walk(const PromptArgs &a, const TilePos *ends, TileDesc *ring, uint32_t d_full, uint32_t d_empty, int lane, Wait &&wait)
+__device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *seqs, const TilePos *ends, TileDesc *ring, uint32_t d_full, uint32_t d_empty, int lane, Wait &&wait)
 {
     int at = 0;
     uint32_t d_phase = 0;
@@ -171,7 +175,7 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const TilePos *en
     int have = -1;
     PromptSeq s = {};
     while (pos.before(end)) {
-        if (pos.b != have) { s = prompt_seq(a, pos.b); have = pos.b; }
+        if (pos.b != have) { s = seqs ? seqs[pos.b] : prompt_seq(a, pos.b); have = pos.b; }
         if (s.m == 0) { pos = next_pos<WIDE>(a, s, pos); continue; }
         const TileItem<WIDE> item(a, s, pos.q);
         const bool last = pos.b == end.b && pos.head == end.head && pos.q == end.q;
@@ -219,6 +223,8 @@ struct TileSource {
         return a.table ? (uint32_t)((valid(t) + a.box_rows - 1) >> a.box_shift << a.box_shift) * (full / kTileRows) : full;
     }
 };
+// the list of the call's work: units before each sequence; the sequences, of few
+inline size_t tile_list_bytes(int batch) { return (size_t)((batch + 2) & ~1) * 4 + (batch <= kTileSeqs ? (size_t)batch * sizeof(PromptSeq) : 0); }
 // lets a kernel use `most` bytes of an SM's shared memory on the current device; asks the driver once per device
 inline cudaError_t tile_allow_smem(const void *kernel, int (&told)[64], size_t most)
 {
