@@ -26,7 +26,7 @@
 
 namespace adsa {
 
-constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time
+constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time: those of one load
 constexpr int kFewMean = 32;                 // query rows per sequence and key head, on the mean, up to which the kernel for few rows runs
 struct TileControl {
     uint64_t bars[43];
@@ -567,70 +567,88 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     }
                     if (there) *reinterpret_cast<float2 *>(a.state_ml + 2 * at_slot) = make_float2(m2, l);
                 } else {
-                    const uint32_t stage = smem_u32(stages) + warp * kStage;
-                    const bool wide_out = PLAIN || (a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0), half_out = a.d % 4 == 0 && ((uintptr_t)a.out & 7) == 0;
+                    const auto outputs = [&](int x, float (&o)[32]) {   // 32 elements of the output
+                        load(x, o);
+                        if (__any_sync(0xffffffffu, none)) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = none ? 0.f : o[k];
+                        }
+                        if (!PLAIN && c1 - c0 - x < 32) {          // (what lies past the head's elements is not of its products)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = k < c1 - c0 - x ? o[k] : 0.f;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) bad = fma2(*reinterpret_cast<float2 *>(o + k), make_float2(0.f, 0.f), bad);
+                    };
+                    if constexpr (PLAIN) {
+                        // a row per lane, in whole sectors of 32 bytes (through shared memory, so that lanes shared rows: 7% slower for
+                        // items of three tiles)
 #pragma unroll 1
-                    for (int x0 = 0; x0 < c1 - c0; x0 += kTileStage) {
-#pragma unroll 1
-                        for (int x = 0; x < kTileStage && x0 + x < c1 - c0; x += 32) {
+                        for (int x = 0; x < c1 - c0; x += 32) {
                             alignas(8) float o[32];
-                            load(x0 + x, o);
-                            if (__any_sync(0xffffffffu, none)) {
+                            outputs(x, o);
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] = none ? 0.f : o[k];
-                            }
-                            const int cols = c1 - c0 - x0 - x;
-                            if (cols < 32) {                       // (no products were made past the head's elements)
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] = k < cols ? o[k] : 0.f;
-                            }
-#pragma unroll
-                            for (int k = 0; k < 32; k += 2) bad = fma2(*reinterpret_cast<float2 *>(o + k), make_float2(0.f, 0.f), bad);
-                            if (!PLAIN && a.out_f32 && there) {
+                            for (int k = 0; k < 32; k += 16)
+                                if (there && x + k < c1 - c0)
+                                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                                                 ::"l"((T *)a.out + (size_t)at_row * a.d + c0 + x + k), "r"(pack2<T>(o[k], o[k + 1])), "r"(pack2<T>(o[k + 2], o[k + 3])),
+                                                 "r"(pack2<T>(o[k + 4], o[k + 5])), "r"(pack2<T>(o[k + 6], o[k + 7])), "r"(pack2<T>(o[k + 8], o[k + 9])),
+                                                 "r"(pack2<T>(o[k + 10], o[k + 11])), "r"(pack2<T>(o[k + 12], o[k + 13])), "r"(pack2<T>(o[k + 14], o[k + 15]))
+                                                 : "memory");
+                            __syncwarp();
+                        }
+                    } else {
+                        const uint32_t stage = smem_u32(stages) + warp * kStage;
+                        const bool wide_out = a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0, half_out = a.d % 4 == 0 && ((uintptr_t)a.out & 7) == 0;
+#pragma unroll 1
+                        for (int x0 = 0; x0 < c1 - c0; x0 += kTileStage) {
+                            alignas(8) float o[32];
+                            outputs(x0, o);
+                            if (a.out_f32 && there) {
 #pragma unroll
                                 for (int k = 0; k < 32; k += 2)
-                                    if (k < cols) *reinterpret_cast<float2 *>(a.out_f32 + (size_t)at_row * a.d + c0 + x0 + x + k) = make_float2(o[k], o[k + 1]);
+                                    if (k < c1 - c0 - x0) *reinterpret_cast<float2 *>(a.out_f32 + (size_t)at_row * a.d + c0 + x0 + k) = make_float2(o[k], o[k + 1]);
                             }
 #pragma unroll
                             for (int k = 0; k < 32; k += 8)
                                 asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};"
-                                             ::"r"(stage + (uint32_t)(lane * kTileStage * 2) + (uint32_t)((((x + k) / 8) ^ (lane & (kTileStage / 8 - 1))) << 4)),
+                                             ::"r"(stage + (uint32_t)(lane * kTileStage * 2) + (uint32_t)(((k / 8) ^ (lane & (kTileStage / 8 - 1))) << 4)),
                                              "r"(pack2<T>(o[k], o[k + 1])), "r"(pack2<T>(o[k + 2], o[k + 3])), "r"(pack2<T>(o[k + 4], o[k + 5])),
                                              "r"(pack2<T>(o[k + 6], o[k + 7])) : "memory");
-                        }
-                        __syncwarp();
-                        if ((PLAIN || a.out) && wide_out) {                   // 16 bytes a lane, kTileStage / 8 lanes a row
-                            constexpr int LANES = kTileStage / 8;
-                            uint4 w[LANES];
+                            __syncwarp();
+                            if (a.out && wide_out) {                   // 16 bytes a lane, kTileStage / 8 lanes a row
+                                constexpr int LANES = kTileStage / 8;
+                                uint4 w[LANES];
 #pragma unroll
-                            for (int i = 0; i < LANES; ++i) {
-                                const int r = i * (32 / LANES) + lane / LANES;
-                                w[i] = *reinterpret_cast<const uint4 *>(stages + warp * kStage + r * kTileStage * 2 + ((lane % LANES ^ (r & (LANES - 1))) << 4));
-                            }
-#pragma unroll
-                            for (int i = 0; i < LANES; ++i) {
-                                const int to = __shfl_sync(0xffffffffu, at_row, i * (32 / LANES) + lane / LANES);
-                                if (to >= 0 && c0 + x0 + lane % LANES * 8 < c1) *reinterpret_cast<uint4 *>((T *)a.out + (size_t)to * a.d + c0 + x0 + lane % LANES * 8) = w[i];
-                            }
-                        } else if (!PLAIN && a.out) {              // 8 or 4 bytes a lane
-                            const auto pieces = [&](auto words_) {
-                                constexpr int WORDS = decltype(words_)::value, LANES = kTileStage / 2 / WORDS;
-#pragma unroll 4
-                                for (int i = 0; i < 32; i += 32 / LANES) {
-                                    const int r = i + lane / LANES, e = 2 * WORDS * (lane % LANES), to = __shfl_sync(0xffffffffu, at_row, r);
-                                    const uint32_t *from = reinterpret_cast<const uint32_t *>(
-                                        stages + warp * kStage + r * kTileStage * 2 + (((e / 8) ^ (r & (kTileStage / 8 - 1))) << 4) + e % 8 * 2);
-                                    uint32_t *out = reinterpret_cast<uint32_t *>((T *)a.out + (size_t)max(to, 0) * a.d + c0 + x0 + e);
-                                    if (to >= 0 && c0 + x0 + e < c1) {
-                                        if constexpr (WORDS == 2) *reinterpret_cast<uint2 *>(out) = *reinterpret_cast<const uint2 *>(from);
-                                        else *out = *from;
-                                    }
+                                for (int i = 0; i < LANES; ++i) {
+                                    const int r = i * (32 / LANES) + lane / LANES;
+                                    w[i] = *reinterpret_cast<const uint4 *>(stages + warp * kStage + r * kTileStage * 2 + ((lane % LANES ^ (r & (LANES - 1))) << 4));
                                 }
-                            };
-                            if (half_out) pieces(std::integral_constant<int, 2>());
-                            else pieces(std::integral_constant<int, 1>());
+#pragma unroll
+                                for (int i = 0; i < LANES; ++i) {
+                                    const int to = __shfl_sync(0xffffffffu, at_row, i * (32 / LANES) + lane / LANES);
+                                    if (to >= 0 && c0 + x0 + lane % LANES * 8 < c1) *reinterpret_cast<uint4 *>((T *)a.out + (size_t)to * a.d + c0 + x0 + lane % LANES * 8) = w[i];
+                                }
+                            } else if (a.out) {                        // 8 or 4 bytes a lane
+                                const auto pieces = [&](auto words_) {
+                                    constexpr int WORDS = decltype(words_)::value, LANES = kTileStage / 2 / WORDS;
+#pragma unroll 4
+                                    for (int i = 0; i < 32; i += 32 / LANES) {
+                                        const int r = i + lane / LANES, e = 2 * WORDS * (lane % LANES), to = __shfl_sync(0xffffffffu, at_row, r);
+                                        const uint32_t *from = reinterpret_cast<const uint32_t *>(
+                                            stages + warp * kStage + r * kTileStage * 2 + (((e / 8) ^ (r & (kTileStage / 8 - 1))) << 4) + e % 8 * 2);
+                                        uint32_t *out = reinterpret_cast<uint32_t *>((T *)a.out + (size_t)max(to, 0) * a.d + c0 + x0 + e);
+                                        if (to >= 0 && c0 + x0 + e < c1) {
+                                            if constexpr (WORDS == 2) *reinterpret_cast<uint2 *>(out) = *reinterpret_cast<const uint2 *>(from);
+                                            else *out = *from;
+                                        }
+                                    }
+                                };
+                                if (half_out) pieces(std::integral_constant<int, 2>());
+                                else pieces(std::integral_constant<int, 1>());
+                            }
+                            __syncwarp();
                         }
-                        __syncwarp();
                     }
                     if (there && a.lse && c0 == 0) a.lse[at_row] = none ? -INFINITY : (m2 + log2f(l)) * 0.693147180559945309f;
                 }
@@ -886,7 +904,7 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
         if (dtype == ADSA_BF16) return a.d <= 64 ? launch_merge<__nv_bfloat16, 1, true>(a, blocks, st) : launch_merge<__nv_bfloat16, 2, true>(a, blocks, st);
         return a.d <= 64 ? launch_merge<__half, 1, true>(a, blocks, st) : launch_merge<__half, 2, true>(a, blocks, st);
     }
-    const bool plain = a.q_boxes && a.box_rows && !a.shifted && a.out && !a.out_f32 && a.d % 8 == 0 && ((uintptr_t)a.out & 15) == 0;
+    const bool plain = a.q_boxes && a.box_rows && !a.shifted && a.out && !a.out_f32 && a.d % 16 == 0 && ((uintptr_t)a.out & 31) == 0;
     if (dtype == ADSA_BF16) return plain ? launch_tiles_type<__nv_bfloat16, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__nv_bfloat16, false>(a, blocks, qm, km, vm, st);
     return plain ? launch_tiles_type<__half, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__half, false>(a, blocks, qm, km, vm, st);
 }
