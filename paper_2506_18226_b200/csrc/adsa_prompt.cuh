@@ -96,7 +96,7 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b)
     return s;
 }
 constexpr int kTileRows = 128;               // query rows of a half item, cached rows of a tile
-constexpr unsigned kTileOver = 2;           // what an item costs beside its tiles, in units
+constexpr unsigned kTileOver = 8;           // what an item costs beside its tiles, in units (half a tile's time for both halves)
 
 // An item: the query rows of a run of tokens (all query heads of one key head), in one half of up to 128 rows or in two.
 template <bool WIDE> __device__ __forceinline__ int item_tokens(const PromptArgs &a) { return WIDE ? a.half_tokens : 2 * a.half_tokens; }

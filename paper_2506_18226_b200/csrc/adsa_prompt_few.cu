@@ -14,6 +14,8 @@
 
 namespace adsa {
 
+constexpr int kFewThreads = kTileThreads + 32;   // warp 8 copies K, warp 12 V: one warp for both, at 700 clocks a copy, was what bounded
+
 struct FewControl {
     uint64_t bars[48];
     TileDesc ring[kTileRing];
@@ -49,7 +51,7 @@ __device__ __forceinline__ void few_store_pairs(uint32_t at, const uint32_t (&r)
 }
 
 template <typename T, int NSUB, int SLOTS>
-__global__ void __launch_bounds__(kTileThreads, 1)
+__global__ void __launch_bounds__(kFewThreads, 1)
 prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
     constexpr int DO = 64 * NSUB;
@@ -72,7 +74,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         for (int g = 0; g < 2; ++g) { mbar_init(s_full + 8 * g, 1); mbar_init(p_full + 8 * g, 4); mbar_init(o_full + 8 * g, 1); }
         mbar_init(m_full, 4);
         mbar_init(m_empty, 4);
-        for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 11); }
+        for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 12); }
         c.limit = kCopySpinLimit;
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
@@ -80,7 +82,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     }
     // what the copies of Q leave of a row's last 16 elements is zero from the start
     if (a.d % 16) {
-        for (uint32_t i = tid; i < kSlot / 16; i += kTileThreads)
+        for (uint32_t i = tid; i < kSlot / 16; i += kFewThreads)
             asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(q_at + 16 * i), "r"(0u) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -114,40 +116,33 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     };
     if (warp == 11) {                                              // ---- the list of items ----
         tile_walk<true>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, wait);
-    } else if (warp == 8) {                                        // ---- copies of K and V ----
-        int slot = 0;
-        uint32_t phase = 0;
+    } else if (warp == 8 || warp == 12) {                          // ---- copies of K, of V ----
+        const bool value = warp == 12;
+        const CUtensorMap *map = value ? &v_map : &k_map;
+        uint32_t base = 0;                                         // copies of both before this item
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileSource src(a, it);
             const int t0 = it.t0, n = it.t1 - t0;
-            // K0 K1 V0 K2 V1 K3 .., in the order the products take them; V lies where K does
-            int k_next = 0, v_next = 0, y_last = -1, y_before = -1;   // pool rows of this lane's box in the last K and the one before it
 #pragma unroll 1
-            for (int j = 0; j < 2 * n; ++j) {
-                const bool value = k_next == n || k_next - v_next == 2;
-                const int t = t0 + (value ? v_next : k_next);
-                int y = k_next - v_next == 2 ? y_before : y_last;
-                if (!value) {
-                    y = src.pool_row(a, t, lane);
-                    y_before = y_last;
-                    y_last = y;
-                }
-                (value ? v_next : k_next) += 1;
-                const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
-                const CUtensorMap *map = value ? &v_map : &k_map;
-                wait(empty + 8 * slot, phase ^ 1u);
+            for (int i = 0; i < n; ++i) {
+                // K0 K1 V0 K2 V1 K3 .., in the order the products take them
+                const uint32_t place = base + (uint32_t)(value ? min(2 * i + 2, 2 * n - 1) : max(2 * i - 1, 0)), turn = place / SLOTS, slot = place - turn * SLOTS;
+                const uint32_t dst = ring + slot * kSlot, bar = full + 8 * slot;
+                const int t = t0 + i;
+                int y = src.pool_row(a, t, lane);
+                wait(empty + 8 * slot, (turn & 1u) ^ 1u);
                 if (tc_elect()) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
                 __syncwarp();
                 if (a.table) {
                     // one lane issues for all: a copy by several lanes at a time is issued lane by lane too, with more ado
 #pragma unroll 1
-                    for (int i = 0; i << a.box_shift < src.valid(t); ++i) {
-                        if (i && (i & 31) == 0) y = src.pool_row(a, t, i + lane);
-                        const int row = __shfl_sync(0xffffffffu, y, i & 31);
+                    for (int b = 0; b << a.box_shift < src.valid(t); ++b) {
+                        if (b && (b & 31) == 0) y = src.pool_row(a, t, b + lane);
+                        const int row = __shfl_sync(0xffffffffu, y, b & 31);
                         if (tc_elect()) {
 #pragma unroll
-                            for (int s = 0; s < NSUB; ++s) pa_tma(dst + (uint32_t)(i << a.box_shift) * 128u + s * kSub, map, s * 64, row, bar);
+                            for (int s = 0; s < NSUB; ++s) pa_tma(dst + (uint32_t)(b << a.box_shift) * 128u + s * kSub, map, s * 64, row, bar);
                         }
                     }
                 } else if (tc_elect()) {
@@ -157,8 +152,8 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                     for (int s = 0; s < NSUB; ++s) tile_tma3(dst + s * kSub, map, s * 64, tf ? tok : src.head, tf ? src.head : tok, bar);
                 }
                 __syncwarp();
-                if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
             }
+            base += 2u * (uint32_t)n;
         }
     } else if (warp == 10) {                                       // ---- copies of Q ----
         uint32_t phase = 0;
@@ -456,7 +451,7 @@ cudaError_t launch_few(const PromptArgs &a, unsigned blocks, const CUtensorMap &
     const auto kern = prompt_few_kernel<T, NSUB, SLOTS>;
     static int told[64];
     const cudaError_t e = tile_allow_smem((const void *)kern, told, most);
-    return e != cudaSuccess ? e : launch_pdl(kern, dim3(blocks), kTileThreads, smem, st, a, km, vm);
+    return e != cudaSuccess ? e : launch_pdl(kern, dim3(blocks), kFewThreads, smem, st, a, km, vm);
 }
 
 }  // namespace

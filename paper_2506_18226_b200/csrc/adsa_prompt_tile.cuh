@@ -13,7 +13,7 @@ constexpr float kTileSlack = 8.f;
 constexpr int kTileRing = 4;                // items ahead
 constexpr int kTileSeqs = 64;                // sequences that are kept in shared memory, read once
 constexpr int kFewRows = 32;                // query rows of an item of the kernel for few rows
-constexpr unsigned kTileMinRun = 6;         // units of a run, at least, where items may be cut
+constexpr unsigned kTileMinRun = 12;        // units of a run, at least, where items may be cut
 
 struct TileDesc {                           // an item of a run, as the walking warp finds it
     PromptSeq s;
@@ -153,7 +153,7 @@ __device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, P
     }
     __syncthreads();
     const unsigned total = plan[a.batch], runs = min(max(a.split ? total / kTileMinRun : total, 1u), gridDim.x);
-    if (warp >= 10) {                                              // where this block's run begins and ends
+    if (warp == 10 || warp == 11) {                                // where this block's run begins and ends
         const unsigned run = blockIdx.x + (warp - 10);
         const unsigned u = run > runs ? total : (unsigned)((unsigned long long)run * total / runs);
         const TilePos at = tile_locate<WIDE>(a, plan, seqs, u, a.split ? total / runs / 32u : 0xffffffffu, lane);
