@@ -81,7 +81,6 @@ int adsa_packed_attn(int dtype, const void *q, long long q_token, long long q_he
     a.kv_heads = n_kv_heads; a.per_kv = n_heads / n_kv_heads; a.d = head_dim; a.causal = causal != 0;
     a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : softmax_scale) * 1.44269504088896341f;
     a.out = out; a.out_f32 = out_f32; a.lse = lse;
-    a.split = n_k > 4 * kTileRows;
     const int sms = sm_count();
     prompt_workspace(head_dim, sms, &a, workspace);
     return launch_prompt_tiles(dtype, a, sms, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
@@ -116,7 +115,6 @@ int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, l
     a.kv_heads = kv->n_kv_heads; a.per_kv = n_heads / kv->n_kv_heads; a.d = kv->head_dim; a.causal = 1;
     a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale) * 1.44269504088896341f;
     a.out = out; a.out_f32 = out_f32; a.lse = lse;
-    a.split = ((long long)max_pages + max_prefix_pages) * kv->page_rows > 4 * kTileRows;
     const int sms = sm_count();
     prompt_workspace(kv->head_dim, sms, &a, workspace);
     return launch_prompt_tiles(kv->dtype, a, sms, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;

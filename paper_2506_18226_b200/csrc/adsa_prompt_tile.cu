@@ -21,6 +21,7 @@
 // Rows of V behind the end are cleared in shared memory before they are used.  A weight of zero does not silence an infinity or NaN of a
 // later token's V in the same tile: a row that comes out infinite or NaN is made again by one warp from the rows it attends.
 #include <float.h>
+#include <math.h>
 
 #include "adsa_prompt_tile.cuh"
 
@@ -709,14 +710,19 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     pdl_wait();
     pdl_launch();
     const int lead = blockIdx.x;
-    const int4 d = a.run_desc[lead];
+    const int4 d = a.run_desc[2 * lead];
     if (d.x < 0) return;
-    const PromptSeq s = prompt_seq(a, d.x);
+    const int4 d2 = a.run_desc[2 * lead + 1];
+    PromptSeq s = {};
+    s.q0 = d2.x;
+    s.m = d2.y;
+    s.n = d2.z;
+    s.p = d2.w;
     const TileItem<WIDE || FEW> item(a, s, d.z);
     const int half = r >> 7, tph = a.half_tokens, in = a.by_per_kv(r & 127), in_item = in + (WIDE ? 0 : half * tph);
     if (in >= tph || in_item >= item.count || (half && !WIDE && !item.pair)) return;
     int pieces = 2;
-    while (lead + pieces < runs && !a.run_desc[lead + pieces - 1].w) ++pieces;
+    while (lead + pieces < runs && !a.run_desc[2 * (lead + pieces - 1)].w) ++pieces;
     const int tok = item.first + in_item, head = d.y * a.per_kv + (r & 127) - in * a.per_kv;
     float m = -INFINITY, l = 0.f, o[PER];
 #pragma unroll
@@ -762,13 +768,13 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
         if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = x;
     }
     if (a.lse && lane == 0 && c0 == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
-    if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, s, d.x, tok, head, lane, c0, c1);
+    if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, prompt_seq(a, d.x), d.x, tok, head, lane, c0, c1);
 }
 
 size_t prompt_workspace(int head_dim, int sms, PromptArgs *a, void *workspace)
 {
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-    const size_t rows = (size_t)2 * sms * 256, desc = up((size_t)sms * sizeof(int4)), state = up(rows * (head_dim <= 64 ? 64 : 128) * 4);
+    const size_t rows = (size_t)2 * sms * 256, desc = up((size_t)sms * 2 * sizeof(int4)), state = up(rows * (head_dim <= 64 ? 64 : 128) * 4);
     if (a) {
         unsigned char *const w = (unsigned char *)workspace;
         a->run_desc = (int4 *)w;
@@ -864,6 +870,19 @@ cudaError_t launch_tiles_type(const PromptArgs &a, unsigned blocks, const CUtens
 
 }  // namespace
 
+// Whether items are cut for an even share of each block.  Uncut, the blocks that have an item less than others wait for up to one item (half
+// of one, where they have many); cut, a second kernel and the states take some 9 us.  By the items there are, sequences of mean length, and the
+// tiles that tables (or the mean sequence) have room for, us a tile each.  Measured, uncut / cut in us: one token x 2 x 12 heads of 64 over 128
+// rows 7.0 / 9.9, 1024 10.6 / 12.4, 2048 14.9 / 13.0; x 32 x 20 over 1144 42.9 / 49.0, 2048 60.6 / 61.8; 5 tokens x 8 x 8 key heads of 128 over up
+// to 16384 94.7 / 59.5; prompts of 2 x 128 x 12 heads of 64 7.7 / 15.3, of 16 x 512 x 8 key heads of 128 62 / 69, of 16384 x 4 1036 / 948.
+static bool cuts_pay(const PromptArgs &a, unsigned blocks, int item_tokens, double us_a_tile)
+{
+    const double mean = (double)a.n_q / a.batch, rows = a.table ? ((double)a.max_pages + (a.groups ? a.max_p_pages : 0)) * a.page_rows : (double)a.n_k / a.batch;
+    const double share = a.batch * fmax(1.0, ceil(mean / item_tokens)) * a.kv_heads / blocks;   // items a block
+    const double item = ceil(rows / kTileRows) * us_a_tile + 3.0;
+    return item * (share <= 1.0 ? 1.0 - share : fmin(ceil(share) - share, 0.5)) > 9.0;
+}
+
 cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cudaStream_t st)
 {
     PromptArgs a = args;
@@ -896,14 +915,18 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
         }
     }
     const unsigned blocks = (unsigned)sms;
-    // Few rows a sequence on the mean: {rows measured}
+    // Few rows a sequence, on the mean.  Measured, this kernel / the other in us: 32 sequences x 20 heads of 64 over 600 rows, 8 rows each 30.1 /
+    // 42.4, 32 rows 32.3 / 42.3, 48 rows (by two items) 44.4 / 43.1; 8 x 8 key heads of 128 over 8000 rows, 8 rows 50.8 / 55.2, 32 rows 52.1 /
+    // 57.0, 48 rows 68.3 / 58.1.
     if (a.box_rows && !a.shifted && a.d <= 128 && a.per_kv <= kFewRows && a.n_q * a.per_kv <= (long long)kFewMean * a.batch) {
         a.half_tokens = kFewRows / a.per_kv;
+        a.split = cuts_pay(a, blocks, kFewRows / a.per_kv, a.d <= 64 ? 0.6 : 1.2);
         const cudaError_t e = launch_prompt_few(dtype, a, blocks, km, vm, st);
         if (e != cudaSuccess || !a.split || blocks < 2) return e;
         if (dtype == ADSA_BF16) return a.d <= 64 ? launch_merge<__nv_bfloat16, 1, true>(a, blocks, st) : launch_merge<__nv_bfloat16, 2, true>(a, blocks, st);
         return a.d <= 64 ? launch_merge<__half, 1, true>(a, blocks, st) : launch_merge<__half, 2, true>(a, blocks, st);
     }
+    a.split = cuts_pay(a, blocks, (a.d > 128 ? 1 : 2) * a.half_tokens, a.d <= 64 ? 1.4 : 1.9);
     const bool plain = a.q_boxes && a.box_rows && !a.shifted && a.out && !a.out_f32 && a.d % 16 == 0 && ((uintptr_t)a.out & 31) == 0;
     if (dtype == ADSA_BF16) return plain ? launch_tiles_type<__nv_bfloat16, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__nv_bfloat16, false>(a, blocks, qm, km, vm, st);
     return plain ? launch_tiles_type<__half, true>(a, blocks, qm, km, vm, st) : launch_tiles_type<__half, false>(a, blocks, qm, km, vm, st);

@@ -170,6 +170,7 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *
     const unsigned run = blockIdx.x;
     int4 left = make_int4(-1, 0, 0, 0);                         // {sequence of the item that this run begins and leaves unfinished, key
                                                                // head, item; whether an item cut before ends here}
+    int4 of = left;                                            // that sequence's first token, tokens, own rows, rows of the prefix
     const TilePos end = ends[1];
     TilePos pos = ends[0];
     int have = -1;
@@ -183,7 +184,10 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *
         const bool whole = pos.tile == 0 && t1 == item.tiles;
         if (!whole) {
             if (pos.tile > 0) left.w = t1 == item.tiles;
-            else left = make_int4(pos.b, pos.head, pos.q, left.w);
+            else {
+                left = make_int4(pos.b, pos.head, pos.q, left.w);
+                of = make_int4((int)s.q0, s.m, s.n, s.p);
+            }
         }
         wait(d_empty + 8 * at, d_phase ^ 1u);
         if (lane == 0) {
@@ -198,7 +202,10 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *
     if (lane == 0) {
         ring[at].t1 = -1;
         mbar_arrive(d_full + 8 * at);
-        if (a.split) a.run_desc[run] = left;
+        if (a.split) {
+            a.run_desc[2 * run] = left;
+            a.run_desc[2 * run + 1] = of;
+        }
     }
 }
 
