@@ -80,9 +80,9 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const 
         if (done < 32) break;
     }
     const PromptSeq s = seqs ? seqs[b] : prompt_seq(a, b);
-    const unsigned per_head = (plan[b + 1] - plan[b]) / (unsigned)a.kv_heads;
+    const unsigned per_head = max((plan[b + 1] - plan[b]) / (unsigned)a.kv_heads, 1u);
     unsigned rem = u - plan[b];
-    const int head = (int)(rem / per_head);
+    const int head = (int)min(rem / per_head, (unsigned)a.kv_heads - 1u);   // (a head that there is, also where boundaries do not ascend)
     rem -= head * per_head;
     for (int q0 = 0;; q0 += 32) {
         const bool in = (q0 + lane) * item_tokens<WIDE>(a) < s.m;
