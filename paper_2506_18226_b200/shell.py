@@ -332,9 +332,9 @@ class SharedPromptShell(_Decoder):
         tensors [rows, dim] of 1 to n_text rows each: both enter end to end."""
         self.next_cell = None                                              # (until the condition is whole)
         with torch.cuda.device(self.dev):                                  # (calls go to the current device's stream)
-            if torch.is_tensor(text_emb):
-                return self._prefill(text_emb)
-            return self._prefill_pair(*text_emb)
+            if isinstance(text_emb, (tuple, list)):
+                return self._prefill_pair(*text_emb)
+            return self._prefill(text_emb)
 
     def _prefill(self, text_emb):
         c, T, H, d = self.cfg, self.cfg.n_text, self.cfg.n_heads, self.cfg.head_dim
