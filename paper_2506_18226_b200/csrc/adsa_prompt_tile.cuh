@@ -80,10 +80,11 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const 
         if (done < 32) break;
     }
     const PromptSeq s = seqs ? seqs[b] : prompt_seq(a, b);
+    // (bounded: where boundaries do not ascend, sums may stop inside this sequence, at the largest number)
     const unsigned per_head = max((plan[b + 1] - plan[b]) / (unsigned)a.kv_heads, 1u);
     unsigned rem = u - plan[b];
-    const int head = (int)min(rem / per_head, (unsigned)a.kv_heads - 1u);   // (a head that there is, also where boundaries do not ascend)
-    rem -= head * per_head;
+    const int head = (int)min(rem / per_head, (unsigned)a.kv_heads - 1u);
+    rem = min(rem - head * per_head, per_head - 1u);
     for (int q0 = 0;; q0 += 32) {
         const bool in = (q0 + lane) * item_tokens<WIDE>(a) < s.m;
         const TileItem<WIDE> mine(a, s, in ? q0 + lane : 0);
@@ -108,6 +109,9 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const 
         return head + 1 < a.kv_heads ? TilePos{b, head + 1, 0, 0} : TilePos{b + 1, 0, 0, 0};
     }
 }
+
+// x + y, or the largest number: sequences whose boundaries do not ascend overlap, and count more units than the host allowed for
+__device__ __forceinline__ unsigned tile_sum(unsigned x, unsigned y) { return x > ~y ? 0xffffffffu : x + y; }
 
 // The list of the call's work, plan[b] units before sequence b, and where this block's run begins and ends; by all threads.
 template <bool WIDE>
@@ -146,9 +150,9 @@ __device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, P
         for (int b0 = 0; b0 < a.batch; b0 += 32) {
             unsigned incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
-            if (b0 + lane < a.batch) plan[b0 + lane + 1] = before + incl;
-            before += __shfl_sync(0xffffffffu, incl, 31);
+            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl = tile_sum(incl, t); }
+            if (b0 + lane < a.batch) plan[b0 + lane + 1] = tile_sum(before, incl);
+            before = tile_sum(before, __shfl_sync(0xffffffffu, incl, 31));
         }
     }
     __syncthreads();
