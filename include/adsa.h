@@ -531,6 +531,8 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
  * key head h / g.  head_dim even, 2 .. 256.  q, k, v 4-byte aligned, even strides (quickest: 16 bytes, multiples of 8).
  *   out, out_f32  16-bit / float [tokens][n_heads][head_dim], 4- / 8-byte aligned; either may be NULL, not both
  *   lse           float [tokens][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
+ * Outputs and workspace overlap neither q, k, v, the pools nor one another.  Where boundaries do not ascend, which output rows are
+ * written is not specified; none outside the tensors is.
  * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).  workspace: [device] 256-byte
  * aligned, adsa_prompt_workspace_bytes of them, nothing kept in it from call to call: calls that may overlap on the GPU need one
  * each, and a captured call's must outlive its graph. */
@@ -550,7 +552,7 @@ ADSA_API int adsa_packed_attn(int dtype, const void *q, long long q_token, long 
  * tokens (cu_tokens) and n = n_rows[b] rows, clamped to what the table holds, token i attends the prefix_rows[g] rows of its
  * group's prefix and rows 0 .. n - m + i of page_table[b] (i < m - n: the prefix alone).  page tables, prefixes and groups as
  * adsa_shared_prefix_attn has them; m = 1 is its step for one token, without the sweep of a long prefix for all rows of a group at once.
- * A page outside the pool sets ADSA_DEV_BAD_PAGE and is not read. */
+ * A page outside the pool sets ADSA_DEV_BAD_PAGE; page 0 is read in its place, and what attends it is not specified. */
 ADSA_API int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, long long q_head, const int32_t *cu_tokens,
                              int batch, long long n_tokens, int n_heads, const int32_t *page_table, int max_pages, const int32_t *n_rows,
                              const int32_t *prefix_table, int max_prefix_pages, const int32_t *prefix_rows, const int32_t *group_start,

@@ -302,13 +302,25 @@ PyObject *norm_residual(PyObject *const *a, Py_ssize_t n)
     return answer(rc, both);
 }
 
+// whether two tensors (no negative strides) have bytes in common, by their first and last
+bool touch(const at::Tensor &x, const at::Tensor &y)
+{
+    if (!x.defined() || !y.defined() || x.numel() == 0 || y.numel() == 0) return false;
+    const auto end = [](const at::Tensor &t) {
+        int64_t last = 0;
+        for (int64_t i = 0; i < t.dim(); ++i) last += (t.size(i) - 1) * t.stride(i);
+        return (uintptr_t)t.data_ptr() + (uintptr_t)(last + 1) * t.element_size();
+    };
+    return (uintptr_t)x.data_ptr() < end(y) && (uintptr_t)y.data_ptr() < end(x);
+}
+
 // outputs and workspace of the two calls with many query rows per sequence
 struct RowsOut {
     at::Tensor out, ws;
     const at::Tensor &out_f32, &lse;
     int rc = ADSA_OK;
     // o: out, out_f32, lse, workspace
-    RowsOut(const Check &c, const at::Tensor &q, PyObject *const *o, int64_t batch, int64_t kv_heads)
+    RowsOut(const Check &c, const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, PyObject *const *o, int64_t batch, int64_t kv_heads)
         : out(tensor(o[0], c.call, "out")), ws(tensor(o[3], c.call, "workspace")), out_f32(tensor(o[1], c.call, "out_f32")), lse(tensor(o[2], c.call, "lse"))
     {
         const int64_t tokens = q.size(0), heads = q.size(1), d = q.size(2);
@@ -316,14 +328,21 @@ struct RowsOut {
         if (out_f32.defined()) c.wants(out_f32, "out_f32", at::kFloat, {tokens, heads, d}, true);
         if (lse.defined()) c.wants(lse, "lse", at::kFloat, {tokens, heads}, true);
         if (batch > 0x7fffffff || heads > 0x7fffffff || kv_heads > 0x7fffffff || d > 0x7fffffff) refuse(std::string(c.call) + ": sizes out of range");
-        if (!out.defined() && !out_f32.defined()) out = at::empty(q.sizes(), q.options());
+        const at::Tensor *written[4] = {&out, &out_f32, &lse, &lse};    // (rows are read again after others are written)
         if (ws.defined()) {
             if (!ws.is_contiguous() || !ws.is_cuda() || ws.get_device() != c.dev) refuse(std::string(c.call) + ": workspace must be dense, on the device of q");
+            written[3] = &ws;
         } else if (tokens > 0) {
             size_t bytes = 0;
             rc = c_prompt_workspace_bytes((int)batch, (int)heads, (int)kv_heads, (int)d, &bytes);
             if (rc == ADSA_OK) ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
         }
+        for (int i = 0; i < 4; ++i) {
+            bool bad = touch(*written[i], q) || touch(*written[i], k) || touch(*written[i], v);
+            for (int j = 0; j < i; ++j) bad = bad || (written[i] != written[j] && touch(*written[i], *written[j]));
+            if (bad) refuse(std::string(c.call) + ": outputs and workspace must not overlap q, the cached rows or one another");
+        }
+        if (!out.defined() && !out_f32.defined()) out = at::empty(q.sizes(), q.options());
     }
     size_t ws_bytes() const { return ws.defined() ? ws.nbytes() : 0; }
     PyObject *result(int status, PyObject *const *o) const { return answer(status, out.defined() ? wrap(out, o[0]) : wrap(out_f32, o[1])); }
@@ -358,7 +377,7 @@ PyObject *packed_attn(PyObject *const *a, Py_ssize_t n)
     if (causal < 0) throw Raised();
     const float scale = (float)number(a[6]);
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.dev);
-    const RowsOut o(c, q, a + 7, batch, k.size(1));
+    const RowsOut o(c, q, k, v, a + 7, batch, k.size(1));
     if (o.rc != ADSA_OK) return PyLong_FromLong(o.rc);
     const int rc = c_packed_attn(code, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
                                  v.stride(1), at_of<int32_t>(cu_q), at_of<int32_t>(cu_k), (int)batch, q.size(0), k.size(0), (int)q.size(1),
@@ -398,7 +417,7 @@ PyObject *chunk_attn(PyObject *const *a, Py_ssize_t n)
     if (table.size(1) > 0x7fffffff || groups > 0x7fffffff || p_pages > 0x7fffffff) refuse("chunk_attn: sizes out of range");
     const float scale = (float)number(a[9]);
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.dev);
-    const RowsOut o(c, q, a + 10, batch, kv.n_kv_heads);
+    const RowsOut o(c, q, tensor(a[1], c.call, "k_pool"), tensor(a[2], c.call, "v_pool"), a + 10, batch, kv.n_kv_heads);
     if (o.rc != ADSA_OK) return PyLong_FromLong(o.rc);
     const int rc = c_chunk_attn(&kv, q.data_ptr(), q.stride(0), q.stride(1), at_of<int32_t>(cu), (int)batch, q.size(0), (int)q.size(1),
                                 at_of<int32_t>(table), (int)table.size(1), at_of<int32_t>(n_rows), at_of<int32_t>(p_table), (int)p_pages,

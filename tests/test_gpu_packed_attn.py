@@ -250,3 +250,38 @@ def test_boundaries_past_the_tokens_are_clamped():
     out = torch.full_like(q, 7.0)
     A.packed_attn(q, k, v, torch.tensor([-50, 60, 2000, 3000], dtype=torch.int32, device=DEV), out=out)
     verify(q, k, v, [60, 40], [60, 40], True, out, None)
+
+
+def test_boundaries_that_do_not_ascend_write_no_row_outside():
+    """The sequences overlap; rows around the outputs stay as they were."""
+    import paper_2506_18226_b200 as A
+    g = gen(77)
+    q, k, v = inputs(g, [90], [90], 4, 2, 64, torch.bfloat16)
+    around = torch.full((90 + 64, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    cu = torch.tensor([0, 90, 20, 200, -5, 90, 0, 90], dtype=torch.int32, device=DEV)
+    A.packed_attn(q, k, v, cu, out=around[32:122])
+    assert (around[:32] == 7).all() and (around[122:] == 7).all()
+    assert torch.isfinite(around.float()).all()
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "half of q", "lse", "workspace"])
+def test_outputs_on_top_of_inputs_are_refused(which):
+    import paper_2506_18226_b200 as A
+    g = gen(78)
+    q, k, v = inputs(g, [40], [40], 2, 2, 64, torch.bfloat16)
+    both = torch.zeros(60, 2, 64, dtype=torch.bfloat16, device=DEV)
+    out = {"q": q, "k": k, "v": v}.get(which, torch.empty_like(q))
+    kw = {}
+    if which == "half of q":
+        both[:40] = q
+        q, out = both[:40], both[20:]
+    if which == "lse":
+        kw["lse"] = out.view(torch.float32).view(-1)[:80].view(40, 2)
+    if which == "workspace":
+        kw["workspace"] = A.prompt_workspace(q, 2, 1)
+        out = kw["workspace"][:q.numel() * 2].view(torch.bfloat16).view(q.shape)
+    with pytest.raises(ValueError, match="overlap"):
+        A.packed_attn(q, k, v, out=out, **kw)
+    # beside one another they are taken: three parts of one projection
+    qkv = randn(g, 40, 6, 64)
+    A.packed_attn(qkv[:, :2], qkv[:, 2:4], qkv[:, 4:], out=torch.empty_like(v))
