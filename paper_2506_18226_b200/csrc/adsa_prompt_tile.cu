@@ -24,7 +24,7 @@
 // 16384 tokens x 16 heads on 4 of 128, causal (1.1 TFLOP): 0.96 ms, 1.15 PFLOP/s of 1.68 measured.  128 cached rows for both groups take 3200
 // clocks at 1.7 GHz; the products alone are 2048, the exponentials too (both units 64% busy, issue slots 38%).  What bounds is a group's chain:
 // scores out of tensor memory, their maximum, 128 exponentials a thread, the last quarter's product, the next scores.  Weights come in quarters, so
-// that three of four products run under the softmax (in halves: 3% more).  A third of the exponentials by polynomial on the multiply-add pipe:
+// that three of four products run under the softmax.  A third of the exponentials by polynomial on the multiply-add pipe:
 // 1020 us where 960 went without, by the length of the code.  Code that does not run counts: with row copies, 32-bit outputs and the call that makes
 // rows again in one loop, 144 KB of it, 48 prompts of 640 tokens took 277 us, 242 without.  An item's fixed part is 5000 clocks (its last product,
 // outputs, next scores), which is what short prompts see: 48 of 143 to 1144 tokens, 26 items of three tiles a block, 280 us.
