@@ -155,6 +155,15 @@ __device__ __forceinline__ unsigned long long draw_weight(uint32_t key, const Dr
 __device__ __noinline__ unsigned long long draw_weight_of(uint32_t key, const DrawShared &s) { return draw_weight(key, s); }
 __device__ __noinline__ bool draw_enough(uint32_t key, double min_p, const DrawShared &s) { return draw_share(key, s) >= min_p; }
 
+// *sum += x in shared memory, by its two words: the low one's overflow is carried by whoever makes it.
+__device__ __forceinline__ void draw_add(unsigned long long *sum, unsigned long long x)
+{
+    unsigned *const word = reinterpret_cast<unsigned *>(sum);
+    const unsigned low = (unsigned)x;
+    unsigned high = (unsigned)(x >> 32);
+    if (low) high += atomicAdd(word, low) > ~low;
+    if (high) atomicAdd(word + 1, high);
+}
 // Sum of x over the block, for all threads; before: what threads before this one have of it.
 __device__ __noinline__ unsigned long long draw_scan(unsigned long long x, unsigned long long *before, DrawShared &s)
 {
@@ -277,7 +286,7 @@ __device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, D
             if (!steps.has(k[j])) continue;
             const unsigned b = steps(k[j]);
             atomicAdd(&s.count[b], 1u);
-            if (masses) atomicAdd(&s.mass[b], draw_weight(k[j], s));
+            if (masses) draw_add(&s.mass[b], draw_weight(k[j], s));
         }
     }
     __syncthreads();
@@ -611,8 +620,8 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
                 if (tid == 0) s.n = 0;
                 __syncthreads();
                 const unsigned b0 = has0 && steps.has(k0) ? steps(k0) : kDrawBins, b1 = has1 && steps.has(k1) ? steps(k1) : kDrawBins;
-                if (b0 < kDrawBins) { atomicAdd(&s.count[b0], 1u); atomicAdd(&s.mass[b0], w0); }
-                if (b1 < kDrawBins) { atomicAdd(&s.count[b1], 1u); atomicAdd(&s.mass[b1], w1); }
+                if (b0 < kDrawBins) { atomicAdd(&s.count[b0], 1u); draw_add(&s.mass[b0], w0); }
+                if (b1 < kDrawBins) { atomicAdd(&s.count[b1], 1u); draw_add(&s.mass[b1], w1); }
                 __syncthreads();
                 draw_find(true, goal, start, s);
                 const unsigned bin = s.bin;
