@@ -271,6 +271,22 @@ struct DrawSteps {
     __device__ __forceinline__ bool has(uint32_t key) const { return key <= top && key >= low; }
 };
 
+// A range of keys around those of the steps first .. last, a step or more too wide at both ends: from .. from + more.  What lies outside
+// needs no step of its own.  (The slack is well above what rounding moves: 2^-24 of the distance, and of the larger end.)
+__device__ __forceinline__ uint2 draw_range(const DrawSteps &t, unsigned first, unsigned last)
+{
+    const float wide = 1.f / t.scale, down = (float)(last + 2u) * wide, up = first > 1u ? (float)(first - 1u) * wide : 0.f, slack = fabsf(t.high) * 4e-7f;
+    uint32_t from, to;
+    if (t.by_key) {
+        from = down + 1.f < (float)(t.top - t.low) ? t.top - (uint32_t)(down + 1.f) : t.low;
+        to = up > 1.f ? t.top - (uint32_t)(up - 1.f) : t.top;
+    } else {
+        from = max(draw_key(2.f * (t.high - down - slack)), t.low);
+        to = first > 1u ? min(draw_key(2.f * (t.high - up + slack)), t.top) : t.top;
+    }
+    return make_uint2(from, max(to, from) - from);
+}
+
 // How many of the row's keys lie in each step, and with `masses` their weights.
 template <typename T>
 __device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, bool masses, DrawShared &s)
@@ -296,6 +312,7 @@ __device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, D
 template <typename T>
 __device__ __noinline__ void draw_gather(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned first, unsigned last, DrawShared &s)
 {
+    const uint2 range = draw_range(steps, first, last);            // (a step for every id: 8 us of a pass over 131072)
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
@@ -304,7 +321,7 @@ __device__ __noinline__ void draw_gather(const DrawArgs &a, DrawRow<T> row, Draw
         row.at(a, i, k);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (!steps.has(k[j])) continue;
+            if (k[j] - range.x > range.y) continue;
             const unsigned b = steps(k[j]);
             if (b < first || b > last) continue;
             const unsigned at = atomicAdd(&s.n, 1u);
@@ -373,13 +390,14 @@ __device__ __noinline__ unsigned draw_list(const DrawArgs &a, DrawRow<T> row, ui
 template <typename T>
 __device__ __noinline__ uint2 draw_step_ends(const DrawArgs &a, DrawRow<T> row, DrawSteps steps, unsigned bin, DrawShared &s)
 {
+    const uint2 range = draw_range(steps, bin, bin);
     uint32_t most = 0, fewest = 0xffffffffu;
     for (int i = 8 * threadIdx.x; i < a.vocab; i += kDrawStride) {
         alignas(16) uint32_t k[8];
         row.at(a, i, k);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (steps.has(k[j]) && steps(k[j]) == bin) { most = max(most, k[j]); fewest = min(fewest, k[j]); }
+            if (k[j] - range.x <= range.y && steps(k[j]) == bin) { most = max(most, k[j]); fewest = min(fewest, k[j]); }
     }
     return draw_ends(most, fewest, s);
 }
