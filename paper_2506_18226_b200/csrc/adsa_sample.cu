@@ -129,8 +129,6 @@ struct DrawShared {
 __device__ __forceinline__ double draw_share(uint32_t key, const DrawShared &s)
 {
     const double x = (draw_logit(key) - s.largest) * s.per_64th, magic = 6755399441055744.0;
-    if (key == s.top) return 1.0;
-    if (!(x > -64000.0)) return 0.0;
     const double k = x + magic, r = (x - (k - magic)) * 0.010830424696249145;   // ln 2 / 64
     double p = fma(r, 1.0 / 120, 1.0 / 24);
     p = fma(p, r, 1.0 / 6);
@@ -139,7 +137,8 @@ __device__ __forceinline__ double draw_share(uint32_t key, const DrawShared &s)
     p = fma(p, r, 1.0);
     const int n = __double2loint(k);                               // (two's complement in the low bits of the sum)
     const double y = p * s.power[n & 63];
-    return __hiloint2double(__double2hiint(y) + ((n >> 6) << 20), __double2loint(y));
+    const double w = __hiloint2double(__double2hiint(y) + ((n >> 6) << 20), __double2loint(y));
+    return key == s.top ? 1.0 : x > -64000.0 ? w : 0.0;            // (chosen, not branched over: neighbours' chains run side by side)
 }
 __device__ __forceinline__ float draw_exp2(float x)
 {
@@ -298,11 +297,17 @@ __device__ __noinline__ void draw_histogram(const DrawArgs &a, DrawRow<T> row, D
         alignas(16) uint32_t k[8];
         row.at(a, i, k);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (!steps.has(k[j])) continue;
-            const unsigned b = steps(k[j]);
-            atomicAdd(&s.count[b], 1u);
-            if (masses) draw_add(&s.mass[b], draw_weight(k[j], s));
+        for (int j = 0; j < 8; j += 2) {
+            const bool in0 = steps.has(k[j]), in1 = steps.has(k[j + 1]);
+            if (!in0 && !in1) continue;
+            const unsigned b0 = steps(k[j]), b1 = steps(k[j + 1]);
+            if (in0) atomicAdd(&s.count[b0], 1u);
+            if (in1) atomicAdd(&s.count[b1], 1u);
+            if (masses) {
+                const unsigned long long w0 = draw_weight(k[j], s), w1 = draw_weight(k[j + 1], s);
+                if (in0) draw_add(&s.mass[b0], w0);
+                if (in1) draw_add(&s.mass[b1], w1);
+            }
         }
     }
     __syncthreads();
@@ -763,10 +768,13 @@ draw_kernel(const __grid_constant__ DrawArgs a, int stashed)
             alignas(16) uint32_t k[8];
             row.at(a, i, k);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (k[j] < thr || i + j >= i1) continue;
-                if (k[j] == thr) ++equal;
-                else { sum += draw_weight(k[j], s); ++kept; }
+            for (int j = 0; j < 8; j += 2) {                       // (segments end at multiples of 8, or with the row)
+                const bool in0 = k[j] > thr, in1 = k[j + 1] > thr;
+                equal += (k[j] == thr) + (k[j + 1] == thr);
+                kept += in0 + in1;
+                if (!in0 && !in1) continue;
+                const unsigned long long w0 = draw_weight(k[j], s), w1 = draw_weight(k[j + 1], s);
+                sum += (in0 ? w0 : 0) + (in1 ? w1 : 0);
             }
         }
 #pragma unroll
