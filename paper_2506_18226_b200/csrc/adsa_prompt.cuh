@@ -137,8 +137,16 @@ __device__ __forceinline__ size_t prompt_row(const PromptArgs &a, const PromptSe
     return (((size_t)page * a.kv_heads + h) * a.page_rows + row - a.by_page(row) * a.page_rows) * a.row_stride;
 }
 
+// Magnitudes from here on are infinite in the 16-bit type (halfway from its largest value to the next power of two).  An output is a mean of
+// values of that type and never as large, but weights that are rounded and a sum that is not can make it so: such a row, like one that
+// came out infinite or NaN, is made again.
+template <typename T> struct TooLarge { static constexpr float value = 255.5f * 1.329227995784916e36f; };   // (2 - 2^-8) 2^127
+template <> struct TooLarge<__half> { static constexpr float value = 65520.f; };
+template <typename T> __device__ __forceinline__ bool prompt_fits(float x) { return fabsf(x) < TooLarge<T>::value; }   // (not NaN)
+
 // One query row by one warp, as the formula has it: a cached row per lane for the scores, elements spread over the lanes for
-// the sums.  All in 32 bits.  Elements c0 .. c1 - 1 of the output, at most 128 of them.
+// the sums.  All in 32 bits.  The running output is the mean so far, moved on by shares of the sum so far: it stays within the values' range,
+// where a sum that is divided at the end passes 32 bits.  Elements c0 .. c1 - 1 of the output, at most 128 of them.
 template <typename T>
 __device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const PromptSeq &s, int b, int i, int head, int lane, int c0, int c1)
 {
@@ -166,17 +174,18 @@ __device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const Promp
 #pragma unroll
         for (int k = 16; k; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
         const float m_new = nan ? NAN : fmaxf(m, mx);
-        const float base = m_new == -INFINITY ? 0.f : m_new, corr = pa_exp2(m - base), w = j < n ? pa_exp2(x - base) : 0.f;
+        const float base = m_new == -INFINITY ? 0.f : m_new, before = l * pa_exp2(m - base), w = j < n ? pa_exp2(x - base) : 0.f;
         m = m_new;
         float sum = w;
 #pragma unroll
         for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        l = l * corr + sum;
+        l = before + sum;
+        const float inv = l == 0.f ? 0.f : 1.f / l, old = before * inv, share = w * inv;   // (no weight yet: as if nothing had come)
 #pragma unroll
-        for (int e = 0; e < PER; ++e) { o[e].x *= corr; o[e].y *= corr; }
+        for (int e = 0; e < PER; ++e) { o[e].x *= old; o[e].y *= old; }
         const int rows = min(n - j0, 32);
         for (int r = 0; r < rows; ++r) {
-            const float p = __shfl_sync(0xffffffffu, w, r);
+            const float p = __shfl_sync(0xffffffffu, share, r);
             const T *v = (const T *)a.v + __shfl_sync(0xffffffffu, v_at, r);
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
@@ -189,13 +198,13 @@ __device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const Promp
         }
     }
     const size_t row = (size_t)(s.q0 + i) * a.kv_heads * a.per_kv + head;
-    const float inv = n > 0 ? 1.f / l : 0.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         const int at = c0 + 2 * (lane + 32 * e);
         if (at >= c1) continue;
-        if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(o[e].x * inv, o[e].y * inv);
-        if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = make_float2(o[e].x * inv, o[e].y * inv);
+        if (n > 0 && l == 0.f) o[e] = make_float2(NAN, NAN);   // (scores of -infinity alone)
+        if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(o[e].x, o[e].y);
+        if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = o[e];
     }
     if (a.lse && lane == 0 && c0 == 0) a.lse[row] = n > 0 ? (m + log2f(l)) * 0.693147180559945309f : -INFINITY;
 }

@@ -10,7 +10,6 @@
 // 32 sequences of one token over 1144 rows of 20 heads of 64 (188 MB): 41 us, 4.6 TB/s of 6.5 measured; 8 x 5 tokens over up to 16384 rows of 8 key heads of
 // 128 (302 MB): 58 us, 5.2 TB/s.  What bounds: for long rows the memory; for short ones an item's fixed part, some 5000 clocks of first copies,
 // joining and outputs, most of them waiting for instructions that run once per item (so this code is kept short).
-#include <float.h>
 
 #include "adsa_prompt_tile.cuh"
 
@@ -261,7 +260,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
         const int in = a.by_per_kv(row), in_head = row - in * a.per_kv;   // token in the item, head in the key head's
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
-        bool again = false;                                        // a row came out infinite or NaN
+        bool again = false;                                        // a row came out too large for its type, or NaN
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<true> item(a, it.s, it.q);
@@ -396,7 +395,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                             if (partial) {
                                 *reinterpret_cast<float2 *>(a.state + ((size_t)it.slot * (DO / 4) + x / 4) * 1024 + row * 4 + x % 4) = y;
                             } else {
-                                again = again || !(fabsf(y.x) + fabsf(y.y) <= FLT_MAX);
+                                again = again || !prompt_fits<T>(y.x) || !prompt_fits<T>(y.y);
                                 if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + to * a.d + x) = pack2<T>(y.x, y.y);
                                 if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + to * a.d + x) = y;
                             }
@@ -409,7 +408,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             __syncwarp();
             if (lane == 0) mbar_arrive(m_empty);
         }
-        // rows that came out infinite or NaN, from what they attend alone: the run once more, in whole items
+        // rows that came out too large or NaN, from what they attend alone: the run once more, in whole items
         if (__any_sync(0xffffffffu, again)) {
             const TilePos end = c.ends[1];
             for (TilePos pos = c.ends[0]; pos.before(end);) {
@@ -423,7 +422,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                             const int i = a.by_per_kv(r), tok = item.first + i, head = pos.head * a.per_kv + r - i * a.per_kv;
                             const size_t first = ((size_t)(s.q0 + tok) * (a.kv_heads * a.per_kv) + head) * a.d;
                             bool bad = false;
-                            for (int e = lane; e < a.d; e += 32) bad = bad || !(fabsf(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]) <= FLT_MAX);
+                            for (int e = lane; e < a.d; e += 32) bad = bad || !prompt_fits<T>(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]);
                             if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, s, pos.b, tok, head, lane, 0, a.d);
                         }
                     }

@@ -19,7 +19,7 @@
 // The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units): until then weights up to 2^8
 // are allowed, sums and products stay exact multiples, and O is rarely rescaled.  Weights are rounded once to the 16-bit type.
 // Rows of V behind the end are cleared in shared memory before they are used.  A weight of zero does not silence an infinity or NaN of a
-// later token's V in the same tile: a row that comes out infinite or NaN is made again by one warp from the rows it attends.
+// later token's V in the same tile: a row that comes out NaN or too large for its type is made again by one warp from the rows it attends.
 //
 // 16384 tokens x 16 heads on 4 of 128, causal (1.1 TFLOP): 0.96 ms, 1.15 PFLOP/s of 1.68 measured.  128 cached rows for both groups take 3200
 // clocks at 1.7 GHz; the products alone are 2048, the exponentials too (both units 64% busy, issue slots 38%).  What bounds is a group's chain:
@@ -28,7 +28,6 @@
 // 1020 us where 960 went without, by the length of the code.  Code that does not run counts: with row copies, 32-bit outputs and the call that makes
 // rows again in one loop, 144 KB of it, 48 prompts of 640 tokens took 277 us, 242 without.  An item's fixed part is 5000 clocks (its last product,
 // outputs, next scores), which is what short prompts see: 48 of 143 to 1144 tokens, 26 items of three tiles a block, 280 us.
-#include <float.h>
 #include <math.h>
 
 #include "adsa_prompt_tile.cuh"
@@ -418,7 +417,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const uint32_t my_s = s_full + 8 * g, my_p = p_full + 32 * g, my_o = o_full + 8 * g;
         const int tph = a.half_tokens, heads = a.kv_heads * a.per_kv;
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
-        bool again = false;                                        // a row of this lane came out infinite or NaN
+        bool again = false;                                        // a row of this lane came out too large for its type, or NaN
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<WIDE> item(a, it.s, it.q);
@@ -534,7 +533,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             else if (!partial) { w0 *= inv; w1 *= inv; }
             const int at_row = there ? (int)((it.s.q0 + tok) * heads + head) : -1;   // (rows of a call are below 2^31)
             const size_t at_slot = (size_t)it.slot * 256 + (WIDE ? g * 128 : half * 128) + row;
-            float2 bad = make_float2(0.f, 0.f);
+            float most = 0.f;                                      // of the row's outputs
             if (warp_there) {
                 const uint32_t shift = (uint32_t)shift_of(it.head, true), o_col = o_col0 + shift;
                 // 32 elements of the row's output, or of its state; zeros where the 16 columns lie past the head's elements
@@ -587,7 +586,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                             for (int k = 0; k < 32; ++k) o[k] = k < c1 - c0 - x ? o[k] : 0.f;
                         }
 #pragma unroll
-                        for (int k = 0; k < 32; k += 2) bad = fma2(*reinterpret_cast<float2 *>(o + k), make_float2(0.f, 0.f), bad);
+                        for (int k = 0; k < 32; k += 2) most = tile_magnitude(most, o[k], o[k + 1]);
                     };
                     if constexpr (PLAIN) {
                         // a row per lane, in whole sectors of 32 bytes (through shared memory, so that lanes shared rows: 7% slower for
@@ -667,9 +666,9 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 __syncwarp();
                 if (lane == 0) mbar_arrive(m_empty);
             }
-            again = again || (there && !partial && bad.x + bad.y != 0.f);
+            again = again || (there && !partial && !prompt_fits<T>(most));
         }
-        // Rows that came out infinite or NaN, from what they attend alone: the run once more, in whole items.  (A call in the loop above
+        // Rows that came out too large or NaN, from what they attend alone: the run once more, in whole items.  (A call in the loop above
         // cost it 8%.)
         if (__any_sync(0xffffffffu, again)) {
             const TilePos end = c.ends[1];
@@ -684,7 +683,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                         bool bad = false;
                         if (in < tph && at < item.count) {
                             const size_t first = ((size_t)(s.q0 + tok) * heads + head) * a.d;
-                            for (int e = c0; e < c1; ++e) bad = bad || !(fabsf(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]) <= FLT_MAX);
+                            for (int e = c0; e < c1; ++e) bad = bad || !prompt_fits<T>(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]);
                         }
                         for (unsigned todo = __ballot_sync(0xffffffffu, bad); todo; todo &= todo - 1) {
                             const int src = __ffs(todo) - 1;
@@ -771,7 +770,7 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
         const int at = c0 + lane * PER + e;
         if (at >= c1) continue;
         const float2 x = none ? make_float2(0.f, 0.f) : make_float2(o[e] * inv, o[e + 1] * inv);
-        bad = bad || !(fabsf(x.x) <= FLT_MAX) || !(fabsf(x.y) <= FLT_MAX);
+        bad = bad || !prompt_fits<T>(x.x) || !prompt_fits<T>(x.y);
         if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(x.x, x.y);
         if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = x;
     }

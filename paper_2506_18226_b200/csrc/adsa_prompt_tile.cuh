@@ -61,6 +61,13 @@ __device__ __forceinline__ float tile_max3(float x, float y, float z)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
     return m;
 }
+// largest magnitude, or NaN if one of them is
+__device__ __forceinline__ float tile_magnitude(float x, float y, float z)
+{
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+    return m;
+}
 // largest of 16, 8, 4 bytes that divides all of these
 __device__ __forceinline__ int piece_of(const void *p, long long token, long long head, int d)
 {
