@@ -529,7 +529,8 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
  * batch <= 4000 sequences; cu_q, cu_k, cu_tokens: int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 are sequence b (of no
  * tokens, maybe); tokens before cu[0] and from cu[batch] on are padding, whose output rows are left as they were; boundaries are
  * clamped to the tokens there are.  NULL: all sequences are equally long.  n_heads = g * n_kv_heads with g <= 64: query head h reads
- * key head h / g.  head_dim even, 2 .. 256.  q, k, v 4-byte aligned, even strides (quickest: 16 bytes, multiples of 8).
+ * key head h / g.  head_dim even, 2 .. 256.  q, k, v 4-byte aligned, even strides (quickest: 16 bytes, multiples of 8).  Up to
+ * 2^31 - 8449 tokens of q, rows of k, and rows that a table and a prefix's have room for together; tokens of q times n_heads below 2^31.
  *   out, out_f32  16-bit / float [tokens][n_heads][head_dim], 4- / 8-byte aligned; either may be NULL, not both
  *   lse           float [tokens][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
  * Outputs and workspace overlap neither q, k, v, the pools nor one another.  Where boundaries do not ascend, which output rows are

@@ -7,7 +7,9 @@
 namespace adsa {
 
 constexpr int kPromptMaxBatch = 4000;        // the list of their work lies in shared memory, beside the tiles
-constexpr long long kPromptMaxRows = 0x7fffff00LL;   // rows a table has room for, packed rows of a call: row numbers stay in 32 bits past the last tile
+// Tokens of a call, packed rows of a call, rows a table and a prefix's have room for: numbers of tokens and rows stay in 32 bits past the last tile, and past the
+// last item too, where a warp looks at 32 items of up to 256 tokens at a time.
+constexpr long long kPromptMaxRows = 0x7fffffffLL - 32 * 256 - 256;
 constexpr int kPromptMaxPerKv = 64;
 
 namespace {
@@ -100,8 +102,7 @@ int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, l
     if (n_groups && (!prefix_table || !prefix_rows || !group_start || max_prefix_pages < 1)) return ADSA_EINVAL;
     if (((uintptr_t)page_table | (uintptr_t)n_rows | (uintptr_t)prefix_table | (uintptr_t)prefix_rows | (uintptr_t)group_start | (uintptr_t)status) & 3)
         return ADSA_EINVAL;
-    if ((long long)max_pages * kv->page_rows > kPromptMaxRows || (n_groups && (long long)max_prefix_pages * kv->page_rows > kPromptMaxRows))
-        return ADSA_EINVAL;
+    if (((long long)max_pages + (n_groups ? max_prefix_pages : 0)) * kv->page_rows > kPromptMaxRows) return ADSA_EINVAL;   // (rows of both are added up)
     if (!units_ok(n_tokens, batch, kv->n_kv_heads, n_heads / kv->n_kv_heads, ((double)max_pages + max_prefix_pages) * kv->page_rows)) return ADSA_EINVAL;
     if (adsa_prompt_workspace_bytes(batch, n_heads, kv->n_kv_heads, kv->head_dim, &bytes) != ADSA_OK) return ADSA_EINVAL;
     if (workspace_bytes < bytes) return ADSA_ENOMEM;
