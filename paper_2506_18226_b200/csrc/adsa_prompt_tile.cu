@@ -131,6 +131,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         uint32_t phase = 0;
         const int k_piece = piece_of(a.k, a.table ? a.row_stride : a.k_token, a.table ? 0 : a.k_head, a.d),
                   v_piece = piece_of(a.v, a.table ? a.row_stride : a.v_token, a.table ? 0 : a.v_head, a.d);
+        // (by all lanes or none: a lane that flushed alone would not have waited for the others' copies, nor counted them)
+        const auto ready = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) != 0; };
         const auto flush = [&]() {                                 // tell of all row copies
             asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -164,7 +166,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const int x0 = part * PSUB * 64;
             const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
             const CUtensorMap *map = value ? &v_map : &k_map;
-            if (!PLAIN && waiting && !mbar_try_wait(empty + 8 * slot, phase ^ 1u)) flush();
+            if (!PLAIN && waiting && !ready(empty + 8 * slot, phase ^ 1u)) flush();
             wait(empty + 8 * slot, phase ^ 1u);
             if (PLAIN || a.box_rows) {
                 if (tc_elect()) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
@@ -201,7 +203,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         };
         // in the order the products take them: K0 V0 K1 V1 .. where both groups share a tile, else K0 K1 V0 K2 V1 K3 ..
         for (;;) {
-            if (!PLAIN && waiting && !mbar_try_wait(d_full + 8 * at, d_phase)) flush();
+            if (!PLAIN && waiting && !ready(d_full + 8 * at, d_phase)) flush();
             if (!have_item()) break;
             const TileDesc &it = c.ring[at];
             const bool turns = !WIDE && it.s.m - it.q * item_tokens<WIDE>(a) <= a.half_tokens;
