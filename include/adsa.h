@@ -535,9 +535,14 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
  *   lse           float [tokens][n_heads]: ln sum_j exp(q.k_j * scale), or NULL
  * Outputs and workspace overlap neither q, k, v, the pools nor one another.  Where boundaries do not ascend, which output rows are
  * written is not specified; none outside the tensors is.
+ * Waits inside the kernels are bounded (adsa_prompt_wait_polls).  One that runs out, which none does on a sound GPU, sets
+ * ADSA_DEV_COPY_TIMEOUT where the call has a status: some output rows of the call are then as they were before it, all others right.
  * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).  workspace: [device] 256-byte
  * aligned, adsa_prompt_workspace_bytes of them, nothing kept in it from call to call: calls that may overlap on the GPU need one
  * each, and a captured call's must outlive its graph. */
+/* How often a wait polls (4 microseconds each) before its block gives up, in the calls that are made or captured from now on; below 0, as it is
+ * at first: 2^18, and 64 more for every 128 rows that a sequence of the call can have.  Returns what it was.  So that the report can be tested: with 0, a wait that is not over within one poll has run out. */
+ADSA_API int adsa_prompt_wait_polls(int polls);
 ADSA_API int adsa_prompt_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes);
 
 /* Attention over whole prompts laid end to end.  q [n_q][n_heads][head_dim], k, v [n_k][n_kv_heads][head_dim] with the given
@@ -549,6 +554,12 @@ ADSA_API int adsa_packed_attn(int dtype, const void *q, long long q_token, long 
                               const int32_t *cu_k, int batch, long long n_q, long long n_k, int n_heads, int n_kv_heads, int head_dim,
                               int causal, float softmax_scale, void *out, float *out_f32, float *lse, void *workspace,
                               size_t workspace_bytes, adsa_stream_t stream);
+/* The same, and device-side errors are ORed into status (uint32 [device], or NULL). */
+ADSA_API int adsa_packed_attn_status(int dtype, const void *q, long long q_token, long long q_head, const void *k, long long k_token, long long k_head,
+                                     const void *v, long long v_token, long long v_head, const int32_t *cu_q, const int32_t *cu_k, int batch,
+                                     long long n_q, long long n_k, int n_heads, int n_kv_heads, int head_dim, int causal, float softmax_scale,
+                                     void *out, float *out_f32, float *lse, void *workspace, size_t workspace_bytes, uint32_t *status,
+                                     adsa_stream_t stream);
 
 /* Attention of a chunk of new tokens per sequence over a paged cache that holds them already (adsa_paged_append first): with m
  * tokens (cu_tokens) and n = n_rows[b] rows, clamped to what the table holds, token i attends the prefix_rows[g] rows of its

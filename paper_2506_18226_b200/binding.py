@@ -29,7 +29,7 @@ EXPORTS = [
     "adsa_rmsnorm", "adsa_swiglu", "adsa_cfg_sample",
     "adsa_rotary_init", "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn",
     "adsa_norm_residual",
-    "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn", "adsa_sample",
+    "adsa_prompt_workspace_bytes", "adsa_prompt_wait_polls", "adsa_packed_attn", "adsa_packed_attn_status", "adsa_chunk_attn", "adsa_sample",
 ]
 
 
@@ -118,6 +118,8 @@ def load(rebuild: bool = False) -> C.CDLL:
             "adsa_norm_residual": [i32, i32, vp, vp, vp, vp, ll, vp, vp, vp, ll, i32, C.c_float, C.c_float, vp],
             "adsa_prompt_workspace_bytes": [i32, i32, i32, i32, C.POINTER(sz)],
             "adsa_packed_attn": [i32, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, i32, ll, ll, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp, sz, vp],
+            "adsa_prompt_wait_polls": [i32],
+            "adsa_packed_attn_status": [i32, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, i32, ll, ll, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp, sz, vp, vp],
             "adsa_sample": [C.POINTER(AdsaSampling), i32, vp, ll, vp, ll, i32, i32, vp, vp, vp, vp],
             "adsa_chunk_attn": [vp, vp, ll, ll, vp, i32, ll, i32, vp, i32, vp, vp, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, sz, vp, vp],
         }
@@ -222,7 +224,7 @@ def _marshal():
         loader.exec_module(module)
         module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value for name in (
             "adsa_rope_axes", "adsa_paged_append", "adsa_shared_prefix_workspace_bytes", "adsa_shared_prefix_attn", "adsa_norm_residual",
-            "adsa_prompt_workspace_bytes", "adsa_packed_attn", "adsa_chunk_attn", "adsa_sample")))
+            "adsa_prompt_workspace_bytes", "adsa_packed_attn_status", "adsa_chunk_attn", "adsa_sample")))
         _marshal_module = module
     return _marshal_module
 
@@ -327,16 +329,16 @@ def prompt_workspace(q, n_kv_heads, batch):
     return torch.empty(out.value, dtype=torch.uint8, device=q.device)
 
 
-def packed_attn(q, k, v, cu_q=None, cu_k=None, *, causal=True, scale=0.0, out=None, out_f32=None, lse=None, workspace=None):
+def packed_attn(q, k, v, cu_q=None, cu_k=None, *, causal=True, scale=0.0, out=None, out_f32=None, lse=None, workspace=None, status=None):
     """adsa_packed_attn: attention over whole prompts laid end to end; q [n_q, n_heads, head_dim], k and v
     [n_k, n_kv_heads, head_dim] (any token and head stride), query head h on key head h / (n_heads / n_kv_heads).
 
     cu_q, cu_k: int32 [batch + 1], where the sequences of q and of k begin and end (cu_k None: as cu_q; both None: one
     sequence).  causal: the last token of a sequence's q sees all its rows, each token before it one row less.  out 16-bit or
     out_f32 float [n_q, n_heads, head_dim] (default: a new tensor; its rows of no sequence are left as they are), lse float
-    [n_q, n_heads].  workspace: from prompt_workspace; None takes one from torch's allocator for this call.  Returns out, or out_f32
-    without one."""
-    r = (_marshal_module or _marshal()).packed_attn(q, k, v, cu_q, cu_k, causal, scale, out, out_f32, lse, workspace)
+    [n_q, n_heads].  workspace: from prompt_workspace; None takes one from torch's allocator for this call.  status: int32 [1] that
+    device-side errors are ORed into.  Returns out, or out_f32 without one."""
+    r = (_marshal_module or _marshal()).packed_attn(q, k, v, cu_q, cu_k, causal, scale, out, out_f32, lse, workspace, status)
     if r.__class__ is int:
         raise AdsaError(r, "adsa_packed_attn")
     return r
@@ -349,7 +351,7 @@ def chunk_attn(q, k_pool, v_pool, page_table, n_rows, cu_tokens=None, prefix_tab
 
     page_table int32 [batch, max_pages], n_rows int32 [batch]; cu_tokens int32 [batch + 1] or None (the same number of tokens for
     every sequence); prefix_table, prefix_rows, group_start as in shared_prefix_attn (all three None: no prefix); the rest
-    as in packed_attn.  status: int32 [1] that device-side errors are ORed into."""
+    as in packed_attn."""
     r = (_marshal_module or _marshal()).chunk_attn(q, k_pool, v_pool, page_table, n_rows, cu_tokens, prefix_table, prefix_rows, group_start,
                                                    scale, out, out_f32, lse, workspace, status)
     if r.__class__ is int:

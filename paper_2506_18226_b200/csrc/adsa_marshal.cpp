@@ -25,7 +25,7 @@ decltype(&adsa_shared_prefix_workspace_bytes) c_workspace_bytes;
 decltype(&adsa_shared_prefix_attn) c_shared_prefix_attn;
 decltype(&adsa_norm_residual) c_norm_residual;
 decltype(&adsa_prompt_workspace_bytes) c_prompt_workspace_bytes;
-decltype(&adsa_packed_attn) c_packed_attn;
+decltype(&adsa_packed_attn_status) c_packed_attn;
 decltype(&adsa_chunk_attn) c_chunk_attn;
 decltype(&adsa_sample) c_sample;
 
@@ -348,12 +348,13 @@ struct RowsOut {
     PyObject *result(int status, PyObject *const *o) const { return answer(status, out.defined() ? wrap(out, o[0]) : wrap(out_f32, o[1])); }
 };
 
-// q, k, v, cu_q, cu_k, causal, scale, out, out_f32, lse, workspace
+// q, k, v, cu_q, cu_k, causal, scale, out, out_f32, lse, workspace, status
 PyObject *packed_attn(PyObject *const *a, Py_ssize_t n)
 {
     Check c{"packed_attn"};
-    need(n, 11, c.call);
-    const at::Tensor &q = tensor(a[0], c.call, "q"), &k = tensor(a[1], c.call, "k"), &v = tensor(a[2], c.call, "v"), &cu_q = tensor(a[3], c.call, "cu_q");
+    need(n, 12, c.call);
+    const at::Tensor &q = tensor(a[0], c.call, "q"), &k = tensor(a[1], c.call, "k"), &v = tensor(a[2], c.call, "v"), &cu_q = tensor(a[3], c.call, "cu_q"),
+                     &status = tensor(a[11], c.call, "status");
     at::Tensor cu_k = tensor(a[4], c.call, "cu_k");
     c.device_of(q, "q");
     const int code = c.code(q, "q", 3);
@@ -373,6 +374,7 @@ PyObject *packed_attn(PyObject *const *a, Py_ssize_t n)
         c.wants(cu_k, "cu_k", at::kInt, {cu_q.defined() ? batch + 1 : -1}, true);
         if (!cu_q.defined()) refuse("packed_attn: cu_k needs cu_q");
     }
+    if (status.defined()) c.wants(status, "status", at::kInt, {1}, true);
     const int causal = PyObject_IsTrue(a[5]);
     if (causal < 0) throw Raised();
     const float scale = (float)number(a[6]);
@@ -382,7 +384,7 @@ PyObject *packed_attn(PyObject *const *a, Py_ssize_t n)
     const int rc = c_packed_attn(code, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
                                  v.stride(1), at_of<int32_t>(cu_q), at_of<int32_t>(cu_k), (int)batch, q.size(0), k.size(0), (int)q.size(1),
                                  (int)k.size(1), (int)d, causal, scale, at_of<void>(o.out), at_of<float>(o.out_f32), at_of<float>(o.lse),
-                                 at_of<void>(o.ws), o.ws_bytes(), stream_of(c.dev));
+                                 at_of<void>(o.ws), o.ws_bytes(), (uint32_t *)at_of<int32_t>(status), stream_of(c.dev));
     return o.result(rc, a + 7);
 }
 

@@ -36,13 +36,15 @@ struct PromptArgs {
     float *out_f32, *lse;                   // or null
     int half_tokens;                        // of an item's half: 128 / per_kv
     FastDiv by_per_kv, by_page;
-    // workspace: what each run leaves for the merge, partial states [2 runs][16 or 32][256 rows][4 elements] and their (m, l)
+    // workspace: what each run leaves for the merge ({sequence of the item that it begins and leaves unfinished, or -1, key head, item, bit 0: an
+    // item cut before ends here, bit 1: its block gave up a wait}, {that sequence's first token, tokens, own rows, rows of the prefix}), partial states [2 runs][16 or 32][256 rows][4 elements] and their (m, l)
     int4 *run_desc;
     float *state, *state_ml;
     int box_rows, box_shift;                // rows of a copy's box (a power of two, its logarithm); 0: K and V are copied row by row
     int q_boxes, tokens_first;              // q by boxes; the order in the maps of packed k (bit 1) and v (bit 2): tokens before heads
     int shifted, q_shifted;                 // packed k and v (q) by boxes that begin up to 7 elements before a head's row
     int split;                              // items may be cut (into partial states)
+    int polls;                              // of a wait inside a kernel, before it gives up
 };
 
 // A sequence: its new tokens q0 .. q0 + m - 1, its own rows (k0 .. of packed ones), the prefix of its group.

@@ -14,6 +14,15 @@ constexpr int kPromptMaxPerKv = 64;
 
 namespace {
 
+int g_polls = -1;                            // of a wait inside the kernels; below 0: by the rows a sequence can have
+
+// A poll waits for 4 us itself.  A second, and 50 us a tile for what waits while the five items before it run (2 us a tile, 20 by row copies).
+int polls_for(long long rows)
+{
+    const int polls = __atomic_load_n(&g_polls, __ATOMIC_RELAXED);
+    return polls >= 0 ? polls : (1 << 18) + 64 * (int)(rows / kTileRows + 2);
+}
+
 int sm_count()
 {
     int dev = 0, n = 0;
@@ -61,17 +70,29 @@ int adsa_prompt_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head
     return ADSA_OK;
 }
 
+int adsa_prompt_wait_polls(int polls) { return __atomic_exchange_n(&g_polls, polls < 0 ? -1 : polls, __ATOMIC_RELAXED); }
+
 int adsa_packed_attn(int dtype, const void *q, long long q_token, long long q_head, const void *k, long long k_token, long long k_head,
                      const void *v, long long v_token, long long v_head, const int32_t *cu_q, const int32_t *cu_k, int batch, long long n_q,
                      long long n_k, int n_heads, int n_kv_heads, int head_dim, int causal, float softmax_scale, void *out, float *out_f32,
                      float *lse, void *workspace, size_t workspace_bytes, adsa_stream_t stream)
+{
+    return adsa_packed_attn_status(dtype, q, q_token, q_head, k, k_token, k_head, v, v_token, v_head, cu_q, cu_k, batch, n_q, n_k, n_heads, n_kv_heads, head_dim,
+                                   causal, softmax_scale, out, out_f32, lse, workspace, workspace_bytes, nullptr, stream);
+}
+
+int adsa_packed_attn_status(int dtype, const void *q, long long q_token, long long q_head, const void *k, long long k_token, long long k_head,
+                            const void *v, long long v_token, long long v_head, const int32_t *cu_q, const int32_t *cu_k, int batch, long long n_q,
+                            long long n_k, int n_heads, int n_kv_heads, int head_dim, int causal, float softmax_scale, void *out, float *out_f32,
+                            float *lse, void *workspace, size_t workspace_bytes, uint32_t *status, adsa_stream_t stream)
 {
     size_t bytes = 0;
     if ((dtype != ADSA_BF16 && dtype != ADSA_F16) || !heads_ok(n_heads, n_kv_heads, head_dim) || n_q < 0 || n_k < 0) return ADSA_EINVAL;
     if (n_q == 0) return ADSA_OK;
     if (!rows_ok(q, q_token, q_head, batch, n_q, n_heads, softmax_scale, out, out_f32, lse, cu_q, workspace)) return ADSA_EINVAL;
     if ((n_k && (!k || !v)) || n_k > kPromptMaxRows || (!cu_k && n_k % batch)) return ADSA_EINVAL;
-    if (((uintptr_t)k & 3) || k_token % 2 || k_head % 2 || ((uintptr_t)v & 3) || v_token % 2 || v_head % 2 || ((uintptr_t)cu_k & 3)) return ADSA_EINVAL;
+    if (((uintptr_t)k & 3) || k_token % 2 || k_head % 2 || ((uintptr_t)v & 3) || v_token % 2 || v_head % 2 || (((uintptr_t)cu_k | (uintptr_t)status) & 3))
+        return ADSA_EINVAL;
     if (!units_ok(n_q, batch, n_kv_heads, n_heads / n_kv_heads, (double)n_k)) return ADSA_EINVAL;
     if (adsa_prompt_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, &bytes) != ADSA_OK) return ADSA_EINVAL;
     if (workspace_bytes < bytes) return ADSA_ENOMEM;
@@ -82,7 +103,8 @@ int adsa_packed_attn(int dtype, const void *q, long long q_token, long long q_he
     a.cu_q = cu_q; a.cu_k = cu_k; a.batch = batch; a.n_q = n_q; a.n_k = n_k;
     a.kv_heads = n_kv_heads; a.per_kv = n_heads / n_kv_heads; a.d = head_dim; a.causal = causal != 0;
     a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : softmax_scale) * 1.44269504088896341f;
-    a.out = out; a.out_f32 = out_f32; a.lse = lse;
+    a.out = out; a.out_f32 = out_f32; a.lse = lse; a.status = status;
+    a.polls = polls_for(n_k);
     const int sms = sm_count();
     prompt_workspace(head_dim, sms, &a, workspace);
     return launch_prompt_tiles(dtype, a, sms, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;
@@ -116,6 +138,7 @@ int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, l
     a.kv_heads = kv->n_kv_heads; a.per_kv = n_heads / kv->n_kv_heads; a.d = kv->head_dim; a.causal = 1;
     a.scale_log2e = (softmax_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : softmax_scale) * 1.44269504088896341f;
     a.out = out; a.out_f32 = out_f32; a.lse = lse;
+    a.polls = polls_for(((long long)max_pages + (n_groups ? max_prefix_pages : 0)) * kv->page_rows);
     const int sms = sm_count();
     prompt_workspace(kv->head_dim, sms, &a, workspace);
     return launch_prompt_tiles(kv->dtype, a, sms, (cudaStream_t)stream) == cudaSuccess ? ADSA_OK : ADSA_ECUDA;

@@ -21,9 +21,11 @@ struct FewControl {
     uint64_t bars[48];
     TileDesc ring[kTileRing];
     TilePos ends[2];                        // of this block's run
+    int4 desc[2];                           // what it leaves for the merge
     float2 ml[kFewRows];                    // (m, l) of group 1
+    TileWaits waits;
+    uint32_t turn[16];                      // of the last copy into each slot, K's or V's: what is in flight, when the block gives up
     uint32_t tmem;
-    int limit;                              // polls of a wait before it gives up
 };
 
 // 16 rows of the warp's part of tensor memory x 8 N columns, four lanes to a row: register 4 i + 2 h + e of lane t has row t / 4 + 8 h,
@@ -65,7 +67,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     FewControl &c = *reinterpret_cast<FewControl *>(ctl);
     unsigned *const plan = reinterpret_cast<unsigned *>(ctl + sizeof(FewControl));
     const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 8, s_full = q_empty + 8, p_full = s_full + 16,
-                   o_full = p_full + 16, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8, d_empty = d_full + 8 * kTileRing;
+                   o_full = p_full + 16, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8, d_empty = d_full + 8 * kTileRing, last = d_empty + 8 * kTileRing;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
 
     if (tid == 0) {
@@ -76,7 +78,9 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         mbar_init(m_full, 4);
         mbar_init(m_empty, 4);
         for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 12); }
-        c.limit = kCopySpinLimit;
+        mbar_init(last, 1);
+        c.waits = {a.polls, 0};
+        for (int i = 0; i < SLOTS; ++i) c.turn[i] = 1u;            // (none: as if a phase before the first)
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
@@ -97,13 +101,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     tc_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, c.tmem, 0);
 
-    const auto wait = [&](uint32_t bar, uint32_t parity) {
-        for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
-            if (polls < *(volatile int *)&c.limit) continue;
-            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short; reported at the end)
-            break;
-        }
-    };
+    const auto wait = [&](uint32_t bar, uint32_t parity) { tile_wait(c.waits, bar, parity); };
     int at = 0;                                                    // the next item of the ring
     uint32_t d_phase = 0;
     const auto next_item = [&]() {                                 // leaves the one before to be written over
@@ -111,29 +109,32 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         if (lane == 0) mbar_arrive(d_empty + 8 * at);
         if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
     };
-    const auto have_item = [&]() {                                 // c.ring[at] is one
-        wait(d_full + 8 * at, d_phase);
-        return c.ring[at].t1 >= 0;
-    };
+    const auto go_on = [&](uint32_t bar, uint32_t parity) { return tile_wait_warp(c.waits, bar, parity); };   // for a whole warp
+    const auto have_item = [&]() { return go_on(d_full + 8 * at, d_phase) && c.ring[at].t1 >= 0; };   // c.ring[at] is one
     if (warp == 11) {                                              // ---- the list of items ----
-        tile_walk<true>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, wait);
+        tile_walk<true>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, c.waits, c.desc);
     } else if (warp == 8 || warp == 12) {                          // ---- copies of K, of V ----
         const bool value = warp == 12;
         const CUtensorMap *map = value ? &v_map : &k_map;
         uint32_t base = 0;                                         // copies of both before this item
+        bool going = true;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileSource src(a, it);
             const int t0 = it.t0, n = it.t1 - t0;
 #pragma unroll 1
-            for (int i = 0; i < n; ++i) {
+            for (int i = 0; going && i < n; ++i) {
                 // K0 K1 V0 K2 V1 K3 .., in the order the products take them
                 const uint32_t place = base + (uint32_t)(value ? min(2 * i + 2, 2 * n - 1) : max(2 * i - 1, 0)), turn = place / SLOTS, slot = place - turn * SLOTS;
                 const uint32_t dst = ring + slot * kSlot, bar = full + 8 * slot;
                 const int t = t0 + i;
                 int y = src.pool_row(a, t, lane);
-                wait(empty + 8 * slot, (turn & 1u) ^ 1u);
-                if (tc_elect()) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
+                going = go_on(empty + 8 * slot, (turn & 1u) ^ 1u);
+                if (!going) break;
+                if (tc_elect()) {
+                    c.turn[slot] = turn;
+                    mbar_expect_tx(bar, src.bytes(a, t, kSlot));
+                }
                 __syncwarp();
                 if (a.table) {
                     // one lane issues for all: a copy by several lanes at a time is issued lane by lane too, with more ado
@@ -154,6 +155,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 }
                 __syncwarp();
             }
+            if (!going) break;
             base += 2u * (uint32_t)n;
         }
     } else if (warp == 10) {                                       // ---- copies of Q ----
@@ -165,7 +167,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             const TileItem<true> item(a, it.s, it.q);
             const int rows = item.count * a.per_kv;
             const unsigned char *src = (const unsigned char *)a.q + 2 * ((it.s.q0 + item.first) * a.q_token + (long long)it.head * a.per_kv * a.q_head);
-            wait(q_empty, phase ^ 1u);
+            if (!go_on(q_empty, phase ^ 1u)) break;
             phase ^= 1u;
 #pragma unroll 1
             for (int r0 = 0; r0 < rows; r0 += 4) {
@@ -191,8 +193,9 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         const uint32_t s_shape = tc_shape<T>(kTileRows, false), o_shape = tc_shape<T>(k_steps * 16, true);
         int slot = 0;
         uint32_t phase = 0, q_phase = 0, p_phase = 0;               // (p_phase: bit g of group g)
+        bool going = true;                                         // what did not come is neither used nor told to be free
         const auto take = [&]() {                                  // the next slot, once its tile is there
-            wait(full + 8 * slot, phase);
+            going = go_on(full + 8 * slot, phase);
             const int taken = slot;
             if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
             return taken;
@@ -207,7 +210,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             const int t0 = __shfl_sync(0xffffffffu, it.t0, 0), n = __shfl_sync(0xffffffffu, it.t1, 0) - t0, p_rows = __shfl_sync(0xffffffffu, it.s.p, 0),
                       own_rows = __shfl_sync(0xffffffffu, it.s.n, 0), before = (p_rows + kTileRows - 1) / kTileRows;
             if (n == 0) continue;
-            wait(q_full, q_phase);
+            if (!go_on(q_full, q_phase)) break;
             q_phase ^= 1u;
             tc_after();
 #pragma unroll 1
@@ -215,6 +218,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 const int g = step & 1, j = step - 2;              // O of tile j, then the scores of tile `step`, for the same group
                 if (j >= 0) {
                     const int v = take(), t = t0 + j, valid = t < before ? p_rows - t * kTileRows : own_rows - (t - before) * kTileRows;
+                    if (!going) break;
                     if (valid < kTileRows) {
                         // rows behind the end hold anything, and a weight of zero does not silence an infinity or a NaN
                         const uint32_t v_at = ring + (uint32_t)v * kSlot;
@@ -240,6 +244,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 }
                 if (step < n) {
                     const int k = take();
+                    if (!going) break;
                     const uint64_t qd = tc_operand(q_at, 16), kd = tc_operand(ring + (uint32_t)k * kSlot, 16);
                     if (tc_elect()) {
 #pragma unroll
@@ -254,6 +259,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                     if (step + 1 == n) done(q_empty);
                 }
             }
+            if (!going) break;
         }
     } else if (warp < 8) {                                         // ---- four lanes to a query row ----
         const int g = warp >> 2, col = 2 * (lane & 3), row = (warp & 3) * 8 + (lane >> 2);
@@ -264,7 +270,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<true> item(a, it.s, it.q);
-            const bool there = row < item.count * a.per_kv, warp_there = (warp & 3) * 8 < item.count * a.per_kv;
+            const bool warp_there = (warp & 3) * 8 < item.count * a.per_kv;
             const int own = it.s.seen(min(item.first + in, it.s.m - 1), a.causal);
             const int p_rows = it.s.p, before = (p_rows + kTileRows - 1) / kTileRows, t0 = it.t0, n = it.t1 - t0, tiles = (n + 1 - g) / 2;
             float m = -INFINITY, l = 0.f;                          // (l: this lane's part of the row's sum)
@@ -357,6 +363,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             m_phase ^= 1u;
             tc_after();
             const bool partial = it.slot >= 0, none = p_rows + own == 0, two = n > 1;
+            const bool there = row < item.count * a.per_kv && !tile_gave_up(c.waits);   // (what a block makes after it gave up is not written)
             float w0 = 1.f, w1 = 0.f;
             if (two) {
                 const float2 other = c.ml[row];
@@ -433,10 +440,24 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     }
     tc_before();
     __syncthreads();
-    if (tid == 0 && a.status && c.limit != kCopySpinLimit) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+    const bool gave_up = tile_gave_up(c.waits);
     if (warp == 9) {
+        if (gave_up) tile_land(last, 1, 0u, true);
         tc_after();
         tc_dealloc(tmem, kTileColumns);
+    }
+    if (tid == 0 && a.split) {
+        const int4 d = c.desc[0];
+        a.run_desc[2 * blockIdx.x] = make_int4(d.x, d.y, d.z, d.w | (gave_up ? 2 : 0));
+        a.run_desc[2 * blockIdx.x + 1] = c.desc[1];
+    }
+    if (gave_up) {
+        if (tid == 0 && a.status) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+        if (warp == 8) {
+            uint32_t flight = 0;
+            for (int i = 0; i < SLOTS; ++i) flight |= (c.turn[i] & 1u) << i;
+            tile_land(full, SLOTS, flight, false);
+        }
     }
 }
 
@@ -446,7 +467,7 @@ template <typename T, int NSUB, int SLOTS>
 cudaError_t launch_few(const PromptArgs &a, unsigned blocks, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t st)
 {
     constexpr size_t most = 227 * 1024, fixed = 1024 + (size_t)(SLOTS + 1) * NSUB * kTileRows * 128 + sizeof(FewControl);
-    static_assert(2 * SLOTS + 18 <= 48, "barriers");
+    static_assert(2 * SLOTS + 19 <= 48 && SLOTS <= 16, "barriers, turns");
     const size_t smem = fixed + tile_list_bytes(a.batch);
     if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
     const auto kern = prompt_few_kernel<T, NSUB, SLOTS>;

@@ -37,11 +37,12 @@ namespace adsa {
 constexpr int kTileStage = 32;              // elements of an output row that a warp turns over in shared memory at a time: those of one load
 constexpr int kFewMean = 32;                 // query rows per sequence and key head, on the mean, up to which the kernel for few rows runs
 struct TileControl {
-    uint64_t bars[43];
+    uint64_t bars[44];
     TileDesc ring[kTileRing];
     TilePos ends[2];                        // of this block's run
+    int4 desc[2];                           // what it leaves for the merge
+    TileWaits waits;
     uint32_t tmem;
-    int limit;                              // polls of a wait before it gives up
 };
 
 // PLAIN: what calls as a rule are: everything copied by boxes, outputs of 16 bits in 16-byte pieces.  What is left (row copies, other
@@ -64,7 +65,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     unsigned *const plan = reinterpret_cast<unsigned *>(ctl + sizeof(TileControl));
     const uint32_t full = smem_u32(c.bars), empty = full + 8 * SLOTS, q_full = empty + 8 * SLOTS, q_empty = q_full + 16, s_full = q_empty + 16,
                    p_full = s_full + 16, o_full = p_full + 64, m_full = o_full + 16, m_empty = m_full + 8, d_full = m_empty + 8,
-                   d_empty = d_full + 8 * kTileRing, q_come = d_empty + 8 * kTileRing;
+                   d_empty = d_full + 8 * kTileRing, q_come = d_empty + 8 * kTileRing, last = q_come + 8;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // (known to be uniform)
 
     if (tid == 0) {
@@ -74,7 +75,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             for (int i = 0; i < 4; ++i) mbar_init(p_full + 32 * g + 8 * i, 4);
         }
         mbar_init(q_come, 1);
-        c.limit = kCopySpinLimit;
+        mbar_init(last, 1);
+        c.waits = {a.polls, 0};
         mbar_init(m_full, 4);
         mbar_init(m_empty, 4);
         for (int i = 0; i < kTileRing; ++i) { mbar_init(d_full + 8 * i, 1); mbar_init(d_empty + 8 * i, 11); }
@@ -101,13 +103,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     tc_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, c.tmem, 0);
 
-    const auto wait = [&](uint32_t bar, uint32_t parity) {
-        for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
-            if (polls < *(volatile int *)&c.limit) continue;
-            *(volatile int *)&c.limit = kCopySpinAfterTimeout;     // (the block's later waits are short; reported at the end)
-            break;
-        }
-    };
+    const auto wait = [&](uint32_t bar, uint32_t parity) { tile_wait(c.waits, bar, parity); };
+    uint32_t flight = 0xffffffffu;                                 // bit i: the parity that this warp's last copy to its barrier i completes
     int at = 0;                                                    // the next item of the ring
     uint32_t d_phase = 0;
     const auto next_item = [&]() {                                 // leaves the one before to be written over
@@ -115,17 +112,15 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         if (lane == 0) mbar_arrive(d_empty + 8 * at);
         if (++at == kTileRing) { at = 0; d_phase ^= 1u; }
     };
-    const auto have_item = [&]() {                                 // c.ring[at] is one
-        wait(d_full + 8 * at, d_phase);
-        return c.ring[at].t1 >= 0;
-    };
+    const auto go_on = [&](uint32_t bar, uint32_t parity) { return tile_wait_warp(c.waits, bar, parity); };   // for a whole warp
+    const auto have_item = [&]() { return go_on(d_full + 8 * at, d_phase) && c.ring[at].t1 >= 0; };   // c.ring[at] is one
     // where the elements of a head's row begin in a tile of K or V
     const auto shift_of = [&](int head, bool value) { return !PLAIN && a.shifted ? (int)(head * (value ? a.v_head : a.k_head)) & 7 : 0; };
 
     // 168 registers a thread at the launch: the groups take what the other four warps leave
     if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {                                              // ---- the list of items ----
-        tile_walk<WIDE>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, wait);
+        tile_walk<WIDE>(a, seqs, c.ends, c.ring, d_full, d_empty, lane, c.waits, c.desc);
     } else if (warp == 8) {                                        // ---- copies of K and V ----
         int slot = 0, waiting = 0;                                 // waiting: row copies in flight that nobody knows of yet
         uint32_t phase = 0;
@@ -167,7 +162,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const uint32_t dst = ring + (uint32_t)slot * kSlot, bar = full + 8 * slot;
             const CUtensorMap *map = value ? &v_map : &k_map;
             if (!PLAIN && waiting && !ready(empty + 8 * slot, phase ^ 1u)) flush();
-            wait(empty + 8 * slot, phase ^ 1u);
+            if (!go_on(empty + 8 * slot, phase ^ 1u)) return false;
             if (PLAIN || a.box_rows) {
                 if (tc_elect()) mbar_expect_tx(bar, src.bytes(a, t, kSlot));
                 __syncwarp();
@@ -200,7 +195,9 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 ++waiting;
             }
             if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+            return true;
         };
+        bool going = true;
         // in the order the products take them: K0 V0 K1 V1 .. where both groups share a tile, else K0 K1 V0 K2 V1 K3 ..
         for (;;) {
             if (!PLAIN && waiting && !ready(d_full + 8 * at, d_phase)) flush();
@@ -211,7 +208,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const int ahead = turns ? 2 : 1, t0 = it.t0, n = it.t1 - t0;
             int k_next = 0, v_next = 0, y_last = -1, y_before = -1;   // pool rows of this lane's box in the last K and the one before it
 #pragma unroll 1
-            for (int j = 0; j < 2 * n; ++j) {
+            for (int j = 0; going && j < 2 * n; ++j) {
                 const bool value = k_next == n || k_next - v_next == ahead;
                 const int t = t0 + (value ? v_next : k_next);
                 int y = k_next - v_next == 2 ? y_before : y_last;  // V lies where K does
@@ -222,23 +219,27 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 }
                 (value ? v_next : k_next) += 1;
 #pragma unroll 1
-                for (int p = 0; p < PARTS; ++p) copy(it, src, t, y, value, p);
+                for (int p = 0; going && p < PARTS; ++p) going = copy(it, src, t, y, value, p);
             }
+            if (!going) break;
             next_item();
         }
         if (!PLAIN && waiting) flush();
+        flight = (phase ? 0u : 0xffffffffu << slot) | (phase ? (1u << slot) - 1u : 0u);   // below `slot` this round's, above it the last one's
     } else if (warp == 10) {                                       // ---- copies of Q ----
         uint32_t phase = 0, come = 0;                              // (phase: bit h of half h)
+        bool going = true;
         const int q_piece = piece_of(a.q, a.q_token, a.q_head, a.d), tph = a.half_tokens;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             if (it.t1 == it.t0) continue;
             const TileItem<WIDE> item(a, it.s, it.q);
 #pragma unroll 1
-            for (int h = 0; h < (item.pair ? 2 : 1); ++h) {
+            for (int h = 0; going && h < (item.pair ? 2 : 1); ++h) {
                 const int tok = item.first + h * tph, tokens = min(item.count - h * tph, tph);
                 const uint32_t dst = q_at + (uint32_t)h * NSUB * kSub, bar = q_full + 8 * h;
-                wait(q_empty + 8 * h, (phase >> h & 1u) ^ 1u);
+                going = go_on(q_empty + 8 * h, (phase >> h & 1u) ^ 1u);
+                if (!going) break;
                 phase ^= 1u << h;
                 if (PLAIN || a.q_boxes) {
                     if (lane == 0) {
@@ -269,8 +270,9 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                             for (int s = 0; s < boxes; ++s) pa_tma(dst + s * kSub, &q_map, (int)(it.head * a.q_head) - shift + s * 64, (int)it.s.q0 + tok, q_come);
                         }
                         __syncwarp();
-                        wait(q_come, come);
                         come ^= 1u;
+                        going = go_on(q_come, come ^ 1u);
+                        if (!going) break;
                     }
                     if (a.shifted) {                               // what K has beside the head's elements meets zeros
                         const int end = (a.d + shift + 15) / 16 * 16;
@@ -290,14 +292,17 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     if (lane == 0) mbar_arrive(bar);
                 }
             }
+            if (!going) break;
         }
+        flight = (phase ^ 3u) | (come ^ 1u) << 2;                  // (0, 1: the halves'; 2: q_come)
     } else if (warp == 9) {                                        // ---- products ----
         int k_steps = (a.d + 15) / 16, d_cols = k_steps * 16;       // (of this head's place in K; in V)
         const uint32_t s_shape = tc_shape<T>(kTileRows, false);
         int slot = 0;
         uint32_t phase = 0, q_phase = 0, p_phase = 0;               // (bit g: of group or half g)
+        bool going = true;                                         // what did not come is neither used nor told to be free
         const auto take = [&]() {                                  // the next slot, once its tile is there
-            wait(full + 8 * slot, phase);
+            going = go_on(full + 8 * slot, phase);
             const int taken = slot;
             if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
             return taken;
@@ -351,7 +356,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             __syncwarp();
         };
         const auto queries = [&](int h) {
-            wait(q_full + 8 * h, q_phase >> h & 1u);
+            going = go_on(q_full + 8 * h, q_phase >> h & 1u) && going;
             q_phase ^= 1u << h;
         };
         for (; have_item(); next_item()) {
@@ -368,6 +373,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             }
             queries(0);
             if (pair) queries(1);
+            if (!going) break;
             tc_after();
             // Steps of the two groups in turn.  Each: O of a tile, for the group whose weights are due, then the scores of its next tile.  Where
             // both groups take every tile, group 0 takes it and group 1 leaves it; else the group of the step does both.
@@ -385,7 +391,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     if (takes) {
                         const int t = t0 + j, valid = t < before ? p_rows - t * kTileRows : own_rows - (t - before) * kTileRows;
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) v[p] = take_v(valid);
+                        for (int p = 0; p < PARTS; ++p) { v[p] = take_v(valid); if (!going) break; }
+                        if (!going) break;
                     }
                     if (j < mine) {
                         weigh(g, WIDE && g == 1 ? v[PARTS - 1] : v[0], j < ahead);
@@ -397,7 +404,8 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 if (i < n) {
                     if (takes) {
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) k[p] = take();
+                        for (int p = 0; p < PARTS; ++p) { k[p] = take(); if (!going) break; }
+                        if (!going) break;
                     }
                     if (i < mine) {
                         score(g, k, pair && g == 1 ? q_at + NSUB * kSub : q_at);
@@ -411,6 +419,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                     }
                 }
             }
+            if (!going) break;
         }
     } else {                                                       // ---- a query row per thread ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -425,7 +434,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const TileItem<WIDE> item(a, it.s, it.q);
             const bool turns = !WIDE && !item.pair;                // the groups take the tiles in turns
             const int half = item.pair ? g : 0, in = a.by_per_kv(row), tok = item.first + half * tph + in, head = it.head * a.per_kv + row - in * a.per_kv;
-            const bool there = in < tph && in + half * tph < item.count;
+            bool there = in < tph && in + half * tph < item.count;
             const int own = it.s.seen(min(tok, it.s.m - 1), a.causal), before = (it.s.p + kTileRows - 1) / kTileRows;
             const bool warp_there = __any_sync(0xffffffffu, there);
             const int p_rows = it.s.p, t0 = it.t0;
@@ -533,6 +542,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const float inv = 1.f / l;
             if (!partial && none) w0 = w1 = 0.f;
             else if (!partial) { w0 *= inv; w1 *= inv; }
+            there = there && !tile_gave_up(c.waits);               // (what a block makes after it gave up is not written)
             const int at_row = there ? (int)((it.s.q0 + tok) * heads + head) : -1;   // (rows of a call are below 2^31)
             const size_t at_slot = (size_t)it.slot * 256 + (WIDE ? g * 128 : half * 128) + row;
             float most = 0.f;                                      // of the row's outputs
@@ -699,10 +709,22 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     }
     tc_before();
     __syncthreads();
-    if (tid == 0 && a.status && c.limit != kCopySpinLimit) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+    const bool gave_up = tile_gave_up(c.waits);
     if (warp == 9) {
+        if (gave_up) tile_land(last, 1, 0u, true);
         tc_after();
         tc_dealloc(tmem, kTileColumns);
+    }
+    if (tid == 0 && a.split) {
+        const int4 d = c.desc[0];
+        a.run_desc[2 * blockIdx.x] = make_int4(d.x, d.y, d.z, d.w | (gave_up ? 2 : 0));
+        a.run_desc[2 * blockIdx.x + 1] = c.desc[1];
+    }
+    if (gave_up) {
+        if (tid == 0 && a.status) atomicOr(a.status, ADSA_DEV_COPY_TIMEOUT);
+        if (warp == 8) tile_land(full, SLOTS, flight, false);
+        if (warp == 10 && (PLAIN || a.q_boxes)) tile_land(q_full, 2, flight, false);
+        if (!PLAIN && warp == 10 && a.q_shifted) tile_land(q_come, 1, flight >> 2, false);
     }
 }
 
@@ -720,7 +742,7 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     pdl_launch();
     const int lead = blockIdx.x;
     const int4 d = a.run_desc[2 * lead];
-    if (d.x < 0) return;
+    if (d.x < 0 || d.w & 2) return;
     const int4 d2 = a.run_desc[2 * lead + 1];
     PromptSeq s = {};
     s.q0 = d2.x;
@@ -730,8 +752,11 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     const TileItem<WIDE || FEW> item(a, s, d.z);
     const int half = r >> 7, tph = a.half_tokens, in = a.by_per_kv(r & 127), in_item = in + (WIDE ? 0 : half * tph);
     if (in >= tph || in_item >= item.count || (half && !WIDE && !item.pair)) return;
-    int pieces = 2;
-    while (lead + pieces < runs && !a.run_desc[2 * (lead + pieces - 1)].w) ++pieces;
+    int pieces = 1;
+    for (int w = 0; lead + pieces < runs && !w; ++pieces) {
+        w = a.run_desc[2 * (lead + pieces)].w;
+        if (w & 2) return;                                         // a block that gave up has left no state
+    }
     const int tok = item.first + in_item, head = d.y * a.per_kv + (r & 127) - in * a.per_kv;
     float m = -INFINITY, l = 0.f, o[PER];
 #pragma unroll
@@ -858,7 +883,7 @@ cudaError_t launch_tiles(const PromptArgs &a, unsigned blocks, const CUtensorMap
 {
     constexpr size_t tile = (size_t)kTileRows * 128, q = (NSUB > 2 ? 1 : 2) * NSUB * tile, slot = (NSUB > 2 ? 2 : NSUB) * tile;
     constexpr size_t fixed = 1024 + q + SLOTS * slot + 8 * 32 * kTileStage * 2 + sizeof(TileControl), most = 227 * 1024;
-    static_assert(2 * SLOTS + 27 <= 43, "barriers");
+    static_assert(2 * SLOTS + 28 <= 44, "barriers");
     const size_t smem = fixed + tile_list_bytes(a.batch);
     if (smem > most) return cudaErrorInvalidValue;                 // (not with the batches that the calls take)
     const auto kern = prompt_tile_kernel<T, NSUB, SLOTS, PLAIN>;

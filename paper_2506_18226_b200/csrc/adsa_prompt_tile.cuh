@@ -44,6 +44,47 @@ __device__ __forceinline__ void tile_tma3(uint32_t dst, const CUtensorMap *map, 
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+
+// Bounded waits of a block.  One that runs out says so in gave_up, and the block's later ones run out at their first poll.  What the block does from then on
+// stays inside its buffers, but works on what happens to be there: no copy begins without its slot, no item is taken, nothing is written to the outputs or
+// the states, the merge leaves out items with a part of this block, and the status says so.
+struct TileWaits {
+    int limit, gave_up;                     // polls; 0 or 1
+};
+__device__ __forceinline__ bool tile_wait(TileWaits &w, uint32_t bar, uint32_t parity)
+{
+    for (int polls = 0; !mbar_try_wait(bar, parity); ++polls) {
+        if (polls < *(volatile int *)&w.limit) continue;
+        *(volatile int *)&w.gave_up = 1;
+        *(volatile int *)&w.limit = 0;
+        return false;
+    }
+    return true;
+}
+// the same for a whole warp, which goes on as one
+__device__ __forceinline__ bool tile_wait_warp(TileWaits &w, uint32_t bar, uint32_t parity)
+{
+    for (int polls = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++polls) {
+        if (__all_sync(0xffffffffu, polls < *(volatile int *)&w.limit)) continue;
+        *(volatile int *)&w.gave_up = 1;
+        *(volatile int *)&w.limit = 0;
+        return false;
+    }
+    return true;
+}
+__device__ __forceinline__ bool tile_gave_up(const TileWaits &w) { return *(const volatile int *)&w.gave_up != 0; }
+// What is in flight when a block gives up has to land before it ends: n barriers, bit i of `flight` the parity that the last copy to barrier i
+// completes; products: those of this warp, by barrier `bar`.  (Not inlined: no sound block runs it.)
+static __device__ __noinline__ void tile_land(uint32_t bar, int n, uint32_t flight, bool products)
+{
+    if (products) {
+        if (tc_elect()) tc_commit(bar);
+        __syncwarp();
+    }
+    for (int i = 0; i < n; ++i) mbar_wait_bounded(bar + 8 * i, flight >> i & 1u, 1 << 12);   // (16 ms)
+    __syncwarp();
+}
+
 template <int BYTES>
 __device__ __forceinline__ void tile_copy(uint32_t dst, const void *src)
 {
@@ -172,9 +213,11 @@ __device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, P
     }
 }
 
-// The warp that walks a block's run and names its items to the others, a few ahead of them.
-template <bool WIDE, typename Wait>
-__device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *seqs, const TilePos *ends, TileDesc *ring, uint32_t d_full, uint32_t d_empty, int lane, Wait &&wait)
+// The warp that walks a block's run and names its items to the others, a few ahead of them, unless the block has given up; desc: what the run leaves for the
+// merge.
+template <bool WIDE>
+__device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *seqs, const TilePos *ends, TileDesc *ring, uint32_t d_full, uint32_t d_empty, int lane, TileWaits &waits,
+                                          int4 *desc)
 {
     int at = 0;
     uint32_t d_phase = 0;
@@ -185,7 +228,9 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *
     const TilePos end = ends[1];
     TilePos pos = ends[0];
     int have = -1;
+    bool going = true;
     PromptSeq s = {};
+    const auto go_on = [&](uint32_t bar, uint32_t parity) { return tile_wait_warp(waits, bar, parity) && __all_sync(0xffffffffu, !tile_gave_up(waits)); };
     while (pos.before(end)) {
         if (pos.b != have) { s = seqs ? seqs[pos.b] : prompt_seq(a, pos.b); have = pos.b; }
         if (s.m == 0) { pos = next_pos<WIDE>(a, s, pos); continue; }
@@ -200,7 +245,8 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *
                 of = make_int4((int)s.q0, s.m, s.n, s.p);
             }
         }
-        wait(d_empty + 8 * at, d_phase ^ 1u);
+        going = go_on(d_empty + 8 * at, d_phase ^ 1u);
+        if (!going) break;
         if (lane == 0) {
             ring[at] = {s, pos.b, pos.head, pos.q, pos.tile, t1, whole ? -1 : (int)(2 * run) + (pos.tile > 0 ? 0 : 1)};
             mbar_arrive(d_full + 8 * at);
@@ -209,14 +255,13 @@ __device__ __forceinline__ void tile_walk(const PromptArgs &a, const PromptSeq *
         if (last) break;
         pos = next_pos<WIDE>(a, s, pos);
     }
-    wait(d_empty + 8 * at, d_phase ^ 1u);
-    if (lane == 0) {
+    if (going && go_on(d_empty + 8 * at, d_phase ^ 1u) && lane == 0) {
         ring[at].t1 = -1;
         mbar_arrive(d_full + 8 * at);
-        if (a.split) {
-            a.run_desc[2 * run] = left;
-            a.run_desc[2 * run + 1] = of;
-        }
+    }
+    if (lane == 0) {
+        desc[0] = left;
+        desc[1] = of;
     }
 }
 

@@ -378,7 +378,7 @@ class SharedPromptShell(_Decoder):
         def attend(layer, h):                                              # (the condition is not rotated)
             q, k, v = torch.matmul(h.unsqueeze(0), self.wqkv_t[layer]).view(3, n, H, d)
             B.paged_append(k, v, self.k_pool[layer], self.v_pool[layer], self.prefix_table, none, cu_tokens=cu, status=self.status)
-            return B.packed_attn(q, k, v, cu, out=out, workspace=ws).view(n, c.dim)
+            return B.packed_attn(q, k, v, cu, out=out, workspace=ws, status=self.status).view(n, c.dim)
 
         for layer in range(c.n_layers):
             self._block(layer, x, h, y, attend)
