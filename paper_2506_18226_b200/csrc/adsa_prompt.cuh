@@ -118,7 +118,7 @@ struct TileItem {
         pair = !WIDE && count > a.half_tokens;
     }
     __device__ __forceinline__ unsigned tile_cost() const { return WIDE || pair ? 2u : 1u; }
-    __device__ __forceinline__ unsigned cost() const { return kTileOver + tile_cost() * (unsigned)tiles; }
+    __device__ __forceinline__ unsigned cost(int shift) const { return max((kTileOver + tile_cost() * (unsigned)tiles) >> shift, 1u); }   // in units of 2^shift
 };
 
 // a page as a table names it; one outside the pool is reported, and read as page 0 (the result is then unspecified)

@@ -33,13 +33,6 @@ int sm_count()
     return n;
 }
 
-// the units of a call are counted in 32 bits; rows: the most that one sequence can have
-bool units_ok(long long n_q, int batch, int kv_heads, int per_kv, double rows)
-{
-    const double items = ((double)n_q * per_kv / kTileRows * 2 + batch) * kv_heads;
-    return items * (kTileOver + 2 * (rows / kTileRows + 2)) < 4e9;
-}
-
 bool heads_ok(int n_heads, int n_kv_heads, int head_dim)
 {
     return n_kv_heads >= 1 && n_heads >= n_kv_heads && n_heads % n_kv_heads == 0 && n_heads / n_kv_heads <= kPromptMaxPerKv && head_dim >= 2 &&
@@ -93,7 +86,6 @@ int adsa_packed_attn_status(int dtype, const void *q, long long q_token, long lo
     if ((n_k && (!k || !v)) || n_k > kPromptMaxRows || (!cu_k && n_k % batch)) return ADSA_EINVAL;
     if (((uintptr_t)k & 3) || k_token % 2 || k_head % 2 || ((uintptr_t)v & 3) || v_token % 2 || v_head % 2 || (((uintptr_t)cu_k | (uintptr_t)status) & 3))
         return ADSA_EINVAL;
-    if (!units_ok(n_q, batch, n_kv_heads, n_heads / n_kv_heads, (double)n_k)) return ADSA_EINVAL;
     if (adsa_prompt_workspace_bytes(batch, n_heads, n_kv_heads, head_dim, &bytes) != ADSA_OK) return ADSA_EINVAL;
     if (workspace_bytes < bytes) return ADSA_ENOMEM;
     PromptArgs a = {};
@@ -125,7 +117,6 @@ int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q_token, l
     if (((uintptr_t)page_table | (uintptr_t)n_rows | (uintptr_t)prefix_table | (uintptr_t)prefix_rows | (uintptr_t)group_start | (uintptr_t)status) & 3)
         return ADSA_EINVAL;
     if (((long long)max_pages + (n_groups ? max_prefix_pages : 0)) * kv->page_rows > kPromptMaxRows) return ADSA_EINVAL;   // (rows of both are added up)
-    if (!units_ok(n_tokens, batch, kv->n_kv_heads, n_heads / kv->n_kv_heads, ((double)max_pages + max_prefix_pages) * kv->page_rows)) return ADSA_EINVAL;
     if (adsa_prompt_workspace_bytes(batch, n_heads, kv->n_kv_heads, kv->head_dim, &bytes) != ADSA_OK) return ADSA_EINVAL;
     if (workspace_bytes < bytes) return ADSA_ENOMEM;
     PromptArgs a = {};

@@ -116,7 +116,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
     } else if (warp == 8 || warp == 12) {                          // ---- copies of K, of V ----
         const bool value = warp == 12;
         const CUtensorMap *map = value ? &v_map : &k_map;
-        uint32_t base = 0;                                         // copies of both before this item
+        uint32_t base = 0;                                         // copies of both before this item (but for whole pairs of turns)
         bool going = true;
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
@@ -156,7 +156,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 __syncwarp();
             }
             if (!going) break;
-            base += 2u * (uint32_t)n;
+            base = (base + 2u * (uint32_t)n) % (2u * SLOTS);
         }
     } else if (warp == 10) {                                       // ---- copies of Q ----
         uint32_t phase = 0;

@@ -116,9 +116,9 @@ __device__ __forceinline__ int piece_of(const void *p, long long token, long lon
     return x & 7 ? 4 : x & 15 ? 8 : 16;
 }
 
-// The item that unit u of the list lies in, and the tile that a run beginning there takes first; by a whole warp.
+// The item that unit u of the list (of 2^shift units each) lies in, and the tile that a run beginning there takes first; by a whole warp.
 template <bool WIDE>
-__device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const PromptSeq *seqs, unsigned u, unsigned tol, int lane)
+__device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const PromptSeq *seqs, unsigned u, int shift, unsigned tol, int lane)
 {
     if (u >= plan[a.batch]) return {a.batch, 0, 0, 0};
     int b = 0;
@@ -136,7 +136,7 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const 
     for (int q0 = 0;; q0 += 32) {
         const bool in = (q0 + lane) * item_tokens<WIDE>(a) < s.m;
         const TileItem<WIDE> mine(a, s, in ? q0 + lane : 0);
-        const unsigned cost = in ? mine.cost() : 0u;
+        const unsigned cost = in ? mine.cost(shift) : 0u;
         unsigned incl = cost;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
@@ -151,64 +151,75 @@ __device__ TilePos tile_locate(const PromptArgs &a, const unsigned *plan, const 
         const bool two = __shfl_sync(0xffffffffu, mine.tile_cost(), at) == 2u;
         const unsigned left = item_cost - off;
         const bool near = min(off, left) <= tol;
-        int q = q0 + at, tile = near || off <= kTileOver ? 0 : (int)(two ? (off - kTileOver + 1u) / 2u : off - kTileOver);
+        const unsigned inside = off << shift;
+        int q = q0 + at, tile = near || inside <= kTileOver ? 0 : (int)(two ? (inside - kTileOver + 1u) / 2u : inside - kTileOver);
         if (near ? off <= left : tile < tiles || tiles == 0) return {b, head, q, tile};
         if (++q * item_tokens<WIDE>(a) < s.m) return {b, head, q, 0};
         return head + 1 < a.kv_heads ? TilePos{b, head + 1, 0, 0} : TilePos{b + 1, 0, 0, 0};
     }
 }
 
-// x + y, or the largest number: sequences whose boundaries do not ascend overlap, and count more units than the host allowed for
+// x + y, or the largest number
 __device__ __forceinline__ unsigned tile_sum(unsigned x, unsigned y) { return x > ~y ? 0xffffffffu : x + y; }
 
-// The list of the call's work, plan[b] units before sequence b, and where this block's run begins and ends; by all threads.
+// The list of the call's work, plan[b] units before sequence b, and where this block's run begins and ends; by all threads.  Units are counted in 32
+// bits (the list lies in shared memory beside the tiles); a call of more, some half a minute's work, is counted again in units of 2^9, 2^18, 2^27, in
+// which an item has one at least: a call has fewer than 2^31 items, but for sequences whose boundaries do not ascend and overlap (sums then stop at
+// the largest number, and which rows are made is not specified).
 template <bool WIDE>
 __device__ __forceinline__ void tile_plan(const PromptArgs &a, unsigned *plan, PromptSeq *seqs, TilePos *ends, int warp, int lane)
 {
-    // units of every sequence: short ones by a lane each, long ones by their warp; then their running sum
-    for (int b0 = warp * 32; b0 < a.batch; b0 += kTileThreads) {
-        const int b = b0 + lane;
-        PromptSeq s = {};
-        if (b < a.batch) {
-            s = prompt_seq(a, b);
-            if (seqs) seqs[b] = s;
+    int shift = 0;
+#pragma unroll 1
+    for (;; shift += 9) {
+        // units of every sequence: short ones by a lane each, long ones by their warp; then their running sum
+        for (int b0 = warp * 32; b0 < a.batch; b0 += kTileThreads) {
+            const int b = b0 + lane;
+            PromptSeq s = {};
+            if (b < a.batch) {
+                s = prompt_seq(a, b);
+                if (seqs) seqs[b] = s;
+            }
+            const bool many = s.m > 32 * item_tokens<WIDE>(a);
+            unsigned units = 0;
+            if (!many) {
+                for (int q = 0; q * item_tokens<WIDE>(a) < s.m; ++q) units = tile_sum(units, TileItem<WIDE>(a, s, q).cost(shift));
+            }
+            for (unsigned todo = __ballot_sync(0xffffffffu, many); todo; todo &= todo - 1) {
+                const int src = __ffs(todo) - 1;
+                PromptSeq t = {};
+                t.m = __shfl_sync(0xffffffffu, s.m, src);
+                t.n = __shfl_sync(0xffffffffu, s.n, src);
+                t.p = __shfl_sync(0xffffffffu, s.p, src);
+                unsigned sum = 0;
+                for (int q = lane; q * item_tokens<WIDE>(a) < t.m; q += 32) sum = tile_sum(sum, TileItem<WIDE>(a, t, q).cost(shift));
+                const unsigned high = __reduce_add_sync(0xffffffffu, sum >> 16), low = __reduce_add_sync(0xffffffffu, sum & 0xffffu);
+                sum = high > 0xffffu ? 0xffffffffu : tile_sum(high << 16, low);
+                if (lane == src) units = sum;
+            }
+            if (b < a.batch) plan[b + 1] = __umulhi(units, (unsigned)a.kv_heads) ? 0xffffffffu : units * (unsigned)a.kv_heads;
         }
-        const bool many = s.m > 32 * item_tokens<WIDE>(a);
-        unsigned units = 0;
-        if (!many) {
-            for (int q = 0; q * item_tokens<WIDE>(a) < s.m; ++q) units += TileItem<WIDE>(a, s, q).cost();
-        }
-        for (unsigned todo = __ballot_sync(0xffffffffu, many); todo; todo &= todo - 1) {
-            const int src = __ffs(todo) - 1;
-            PromptSeq t = {};
-            t.m = __shfl_sync(0xffffffffu, s.m, src);
-            t.n = __shfl_sync(0xffffffffu, s.n, src);
-            t.p = __shfl_sync(0xffffffffu, s.p, src);
-            unsigned sum = 0;
-            for (int q = lane; q * item_tokens<WIDE>(a) < t.m; q += 32) sum += TileItem<WIDE>(a, t, q).cost();
-            sum = __reduce_add_sync(0xffffffffu, sum);
-            if (lane == src) units = sum;
-        }
-        if (b < a.batch) plan[b + 1] = units * (unsigned)a.kv_heads;
-    }
-    __syncthreads();
-    if (warp == 11) {
-        if (lane == 0) plan[0] = 0;
-        unsigned before = 0;
-        for (int b0 = 0; b0 < a.batch; b0 += 32) {
-            unsigned incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
+        __syncthreads();
+        if (warp == 11) {
+            if (lane == 0) plan[0] = 0;
+            unsigned before = 0;
+            for (int b0 = 0; b0 < a.batch; b0 += 32) {
+                unsigned incl = b0 + lane < a.batch ? plan[b0 + lane + 1] : 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl = tile_sum(incl, t); }
-            if (b0 + lane < a.batch) plan[b0 + lane + 1] = tile_sum(before, incl);
-            before = tile_sum(before, __shfl_sync(0xffffffffu, incl, 31));
+                for (int o = 1; o < 32; o <<= 1) { const unsigned t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl = tile_sum(incl, t); }
+                if (b0 + lane < a.batch) plan[b0 + lane + 1] = tile_sum(before, incl);
+                before = tile_sum(before, __shfl_sync(0xffffffffu, incl, 31));
+            }
         }
+        __syncthreads();
+        if (plan[a.batch] != 0xffffffffu || shift == 27) break;
+        __syncthreads();                                               // (all have read it)
     }
-    __syncthreads();
     const unsigned total = plan[a.batch], runs = min(max(a.split ? total / kTileMinRun : total, 1u), gridDim.x);
     if (warp == 10 || warp == 11) {                                // where this block's run begins and ends
         const unsigned run = blockIdx.x + (warp - 10);
         const unsigned u = run > runs ? total : (unsigned)((unsigned long long)run * total / runs);
-        const TilePos at = tile_locate<WIDE>(a, plan, seqs, u, a.split ? total / runs / 32u : 0xffffffffu, lane);
+        const TilePos at = tile_locate<WIDE>(a, plan, seqs, u, shift, a.split ? total / runs / 32u : 0xffffffffu, lane);
         if (lane == 0) ends[warp - 10] = at;
     }
 }

@@ -24,3 +24,11 @@ def test_rows_of_a_table_and_its_prefix_together():
         assert _chunk(kv=dict(page_rows=rows, n_kv_heads=1), batch=1, n=1, heads=1, max_pages=own, mpp=pre, wsb=0) == want
     # without a prefix the width of its table does not count
     assert _chunk(kv=dict(page_rows=rows, n_kv_heads=1), batch=1, n=1, heads=1, max_pages=most, mpp=10 ** 9, groups=0, wsb=0) == B.ENOMEM
+
+
+@pytest.mark.parametrize("heads,kv,batch,tokens", [(32, 8, 1024, 1024), (64, 64, 700, 1000), (8, 8, 4000, 32768), (32, 1, 2, 2 ** 24)])
+def test_many_tokens_of_many_sequences_are_taken(heads, kv, batch, tokens):
+    """(What a call's work is depends on the lengths, which lie on the device: tokens times rows of all sequences together say little.)"""
+    n = batch * tokens
+    assert _packed(heads=heads, kv=kv, batch=batch, n_q=n, n_k=n, d=16, qt=heads * 16, qh=16, kt=kv * 16, kh=16, vt=kv * 16, vh=16, wsb=0) == B.ENOMEM
+    assert _chunk(kv=dict(n_kv_heads=kv), heads=heads, batch=batch, n=n, max_pages=2 ** 20, mpp=1, wsb=0) == B.ENOMEM
