@@ -398,13 +398,20 @@ class SharedPromptShell(_Decoder):
         return self.tokens
 
     def given(self, ids):
-        """Tokens that are given rather than drawn: ids [cells, n_images] are those of the cells from the last drawn one on (after
-        prefill: of the first cells), in its place; all enter the cache in one pass, each attending the condition and the cells
-        up to itself.  Draws the cell behind them, which decode_step then follows."""
-        c, n, m, H, d = self.cfg, self.cfg.n_images, ids.shape[0], self.cfg.n_heads, self.cfg.head_dim
+        """Tokens that are given rather than drawn: whole numbers ids [cells, n_images], of the vocabulary, are those of the cells from the
+        last drawn one on (after prefill: of the first cells), in its place; all enter the cache in one pass, each attending the condition
+        and the cells up to itself.  Draws the cell behind them, which decode_step then follows.  (ids on the GPU are waited for: what they
+        index is read before anything else is.)"""
+        c, n, H, d = self.cfg, self.cfg.n_images, self.cfg.n_heads, self.cfg.head_dim
         cells = c.grid_h * c.grid_w
-        if self.next_cell is None or m < 1 or ids.shape[1:] != (n,) or self.next_cell - 1 + m >= cells:
+        if ids.dim() != 2 or ids.dtype not in (torch.uint8, torch.int8, torch.int16, torch.int32, torch.int64):
+            raise ValueError(f"given: ids must be whole numbers [cells, {n}], got {ids.dtype} {list(ids.shape)}")
+        m = ids.shape[0]
+        if self.next_cell is None or m < 1 or ids.shape[1] != n or self.next_cell - 1 + m >= cells:
             raise ValueError(f"given: {list(ids.shape)} ids cannot follow, the next cell is {self.next_cell} of {cells} (None: prefill first)")
+        least, most = (int(x) for x in ids.aminmax())
+        if least < 0 or most >= c.vocab:
+            raise ValueError(f"given: ids from {least} to {most}, the vocabulary has {c.vocab}")
         first = self.next_cell - 1
         self.next_cell = None
         with torch.cuda.device(self.dev):
