@@ -119,6 +119,12 @@ class _Decoder:
         else:
             B.cfg_sample(logits, c.cfg_scale, min(c.top_k, c.vocab), c.temperature, u, tokens=self.tokens)
 
+    def _fed(self):
+        """The ids that the next step embeds.  An image whose logits are NaN or -infinity throughout has nothing to draw, and adsa_sample says -1: it
+        goes on from id 0 (adsa_cfg_sample gives one of the vocabulary in any case)."""
+        c = self.cfg
+        return self.tokens.clamp(min=0) if c.top_p < 1 or c.min_p > 0 else self.tokens
+
     def generate(self, text_emb, n_cells=None):
         """Prefill and decode `n_cells` grid cells (default: the whole grid); returns the ids on the host, [cells, n_images]."""
         n = self.cfg.grid_h * self.cfg.grid_w if n_cells is None else n_cells
@@ -198,7 +204,7 @@ class LlamaGenShell(_Decoder):
 
     def _first(self):
         n = self.cfg.n_images
-        torch.index_select(self.tok_emb, 0, self.tokens, out=self.x[:n])
+        torch.index_select(self.tok_emb, 0, self._fed(), out=self.x[:n])
         self.x[n:].copy_(self.x[:n])                                       # conditional and unconditional rows
         self._pre(0)
 
@@ -251,7 +257,7 @@ class LlamaGenShell(_Decoder):
             self.ids_host[cell].copy_(self.tokens, non_blocking=True)
             self.kernel_calls += 5 * c.n_layers + 3
             return self.tokens
-        emb = self.tok_emb[self.tokens.long()]
+        emb = self.tok_emb[self._fed().long()]
         x = torch.cat([emb, emb], dim=0)                                   # conditional and unconditional rows
         self.pos.fill_(cur)
 
@@ -462,7 +468,7 @@ class SharedPromptShell(_Decoder):
     def _step(self):
         c, n = self.cfg, self.cfg.n_images
         self.pos.copy_(self.positions.index_select(0, self.cell).expand(c.batch, 2))
-        torch.index_select(self.tok_emb, 0, self.tokens, out=self.x[:n])
+        torch.index_select(self.tok_emb, 0, self._fed(), out=self.x[:n])
         self.x[n:].copy_(self.x[:n])                                       # conditional and unconditional rows
         B.rmsnorm(self.x, self.norm1[0], out=self.h, eps=c.norm_eps)
         for layer in range(c.n_layers):
