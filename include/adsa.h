@@ -587,6 +587,7 @@ ADSA_API int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q
  *            (adsa_cfg_sample's mix, which rounds twice)
  *   uniforms float [rows] in [0, 1) (others are clamped to 0 .. 1);  tokens int32 [rows]
  *   logprobs float [rows]: ln of the drawn id's share of the kept weights, or NULL
+ * tokens and logprobs overlap neither the inputs nor one another.
  * NaN among the settings on the host and a guidance that is not finite are ADSA_EINVAL; per row (on the device) NaN leaves top_p and min_p
  * out and takes the largest logit for a temperature. */
 typedef struct {

@@ -469,6 +469,12 @@ PyObject *sample(PyObject *const *a, Py_ssize_t n)
         how.top_k = (int32_t)k;
     }
     if (rows > 0x7fffffff || vocab > 0x7fffffff) refuse("sample: sizes out of range");
+    bool over = touch(tokens, logprobs);
+    for (const at::Tensor *x : std::initializer_list<const at::Tensor *>{&tokens, &logprobs}) {
+        over = over || touch(*x, logits) || touch(*x, uncond) || touch(*x, uniforms);
+        for (int i = 2; i < 6; ++i) over = over || (THPVariable_Check(a[i]) && touch(*x, THPVariable_Unpack(a[i])));
+    }
+    if (over) refuse("sample: tokens and logprobs must not overlap the inputs or one another");
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.dev);
     if (!tokens.defined()) tokens = at::empty({rows}, logits.options().dtype(at::kInt));
     const int rc = c_sample(&how, code, logits.data_ptr(), logits.stride(0), at_of<void>(uncond), uncond.defined() ? uncond.stride(0) : 0, (int)rows,
