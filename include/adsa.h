@@ -581,7 +581,9 @@ ADSA_API int adsa_chunk_attn(const adsa_paged_kv *kv, const void *q, long long q
  * and the token is the first kept id, in ascending order of id, at which the running sum of w reaches u * (sum of w).
  * temperature <= 0: the largest logit, the lowest id of these.  Ids with logits of -infinity or NaN are never drawn; a row
  * of nothing else gets token -1, logprob -infinity.  Of infinite logits the +infinite alone have weight.  Weights are made in 64 bits and
- * summed in steps of 2^-42 of the largest, independent of the order: ids are kept and drawn as the real numbers say, and a call is reproducible.
+ * summed as whole multiples of 2^-42 of the largest, independent of the order, so that a call is reproducible.  A sum of n weights is off by
+ * n 2^-43 of the largest at most (2^-29 for 16384 ids, 2^-23 for 2^20), and ids below 2^-43 of it have no weight: an id is kept or drawn as
+ * the real numbers say, but where a border lies that close to its edge.
  *   logits   bf16, f16 or float [rows][vocab], rows `row` elements apart; 1 <= vocab <= 2^20
  *   uncond   the same, or NULL; then x = uncond + guidance * (logits - uncond), each of the three operations rounded to 32 bits
  *            (adsa_cfg_sample's mix, which rounds twice)

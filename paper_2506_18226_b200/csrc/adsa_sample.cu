@@ -3,7 +3,9 @@
 //
 // All three rules keep a head of the ids in the order (logit descending, id ascending), so what is kept is one border: a key and how
 // many of the ids with just that logit.  Keys are the logits' bits in an order that integers have.  Weights are made in 64 bits and added up
-// as whole multiples of 2^-42 of the largest: sums do not depend on their order, and an id is kept or drawn as the real numbers say.
+// as whole multiples of 2^-42 of the largest (2^20 of them fit 63 bits): sums do not depend on their order.  One of n weights is off by n 2^-43
+// of the largest at most, where a sum of 32-bit weights would be by n 2^-24 of itself; within that of its edge an id may be kept or drawn otherwise
+// than the real numbers say.
 //
 // A block per row; keys lie in shared memory, as many as fit.  A border is found by a histogram of 2048 steps between the largest and the
 // lowest logit, of counts or of masses, and a sort of the step that holds it (where one step holds over 2048 ids: by steps between its own
