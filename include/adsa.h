@@ -522,9 +522,10 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
 /* ---- prompts and chunks: many query rows per sequence ------------------------------------------------------------
  * Rules as for the calls on a paged cache above, but that the softmax weights meet V rounded once to the 16-bit type (each off by
  * 2^-8 of itself at most for bfloat16, 2^-11 or 2^-31 of the largest for half; their sum is taken before).  An output row
- * that this arithmetic leaves NaN, infinite or too large for the 16-bit type (which no mean of its values is) is made again in 32
- * bits throughout, from the rows it attends alone: what lies in rows that a query does not attend, infinities and NaN included,
- * has no effect but that (an output is then exact to 32 bits, where its weights were rounded before).
+ * that this arithmetic leaves NaN, infinite or too large for the 16-bit type is mended by the rows it attends alone: an element with a
+ * NaN or infinities among its values is what they make it, one past half's largest value by its roundings becomes that, any other is
+ * made again in 32 bits throughout.  What lies in rows that a query does not attend, infinities and NaN included, has no effect but
+ * that (an output is then exact to 32 bits, where its weights were rounded before).
  *
  * batch <= 4000 sequences; cu_q, cu_k, cu_tokens: int32 [batch + 1], ascending: tokens cu[b] .. cu[b+1]-1 are sequence b (of no
  * tokens, maybe); tokens before cu[0] and from cu[batch] on are padding, whose output rows are left as they were; boundaries are

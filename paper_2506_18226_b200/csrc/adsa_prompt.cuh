@@ -140,11 +140,33 @@ __device__ __forceinline__ size_t prompt_row(const PromptArgs &a, const PromptSe
 }
 
 // Magnitudes from here on are infinite in the 16-bit type (halfway from its largest value to the next power of two).  An output is a mean of
-// values of that type and never as large, but weights that are rounded and a sum that is not can make it so: such a row, like one that
-// came out infinite or NaN, is made again.
+// values of that type and never as large, but weights that are rounded and a sum that is not can make it so.
 template <typename T> struct TooLarge { static constexpr float value = 255.5f * 1.329227995784916e36f; };   // (2 - 2^-8) 2^127
 template <> struct TooLarge<__half> { static constexpr float value = 65520.f; };
 template <typename T> __device__ __forceinline__ bool prompt_fits(float x) { return fabsf(x) < TooLarge<T>::value; }   // (not NaN)
+
+// bits that are all set in what is no finite number
+template <typename T> struct Infinite { static constexpr uint32_t bits = 0x7f80u; };
+template <> struct Infinite<__half> { static constexpr uint32_t bits = 0x7c00u; };
+// the output element at `at`, as it was written, is no finite number
+template <typename T>
+__device__ __forceinline__ bool prompt_odd(const PromptArgs &a, size_t at)
+{
+    if (a.out) return (reinterpret_cast<const uint16_t *>(a.out)[at] & Infinite<T>::bits) == Infinite<T>::bits;
+    return (reinterpret_cast<const uint32_t *>(a.out_f32)[at] & 0x7f800000u) == 0x7f800000u;
+}
+// A row whose scores or whose sum of weights are no numbers is NaN throughout, and rightly so: its first element is a NaN that no conversion makes, so
+// that it is not looked at again.  (Not where scores have zeros times what lies beside a head's elements.)
+__device__ __forceinline__ bool prompt_lost(const PromptArgs &a, float l) { return !a.shifted && !(l > 0.f && l < INFINITY); }
+__device__ __forceinline__ void prompt_mark_lost(const PromptArgs &a, size_t at)
+{
+    if (a.out) reinterpret_cast<uint16_t *>(a.out)[at] = 0x7ffe;
+    else reinterpret_cast<uint32_t *>(a.out_f32)[at] = 0x7ffffffeu;
+}
+__device__ __forceinline__ bool prompt_marked_lost(const PromptArgs &a, size_t at)
+{
+    return a.out ? reinterpret_cast<const uint16_t *>(a.out)[at] == 0x7ffe : reinterpret_cast<const uint32_t *>(a.out_f32)[at] == 0x7ffffffeu;
+}
 
 // One query row by one warp, as the formula has it: a cached row per lane for the scores, elements spread over the lanes for
 // the sums.  All in 32 bits.  The running output is the mean so far, moved on by shares of the sum so far: it stays within the values' range,
@@ -209,6 +231,183 @@ __device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const Promp
         if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = o[e];
     }
     if (a.lse && lane == 0 && c0 == 0) a.lse[row] = n > 0 ? (m + log2f(l)) * 0.693147180559945309f : -INFINITY;
+}
+
+// What V holds of infinities and NaN in the rows that were looked at, of one sequence and key head from row 0 on; a lane has the columns that it has in
+// prompt_row_by_warp.
+constexpr int kOddNone = 0x7fffffff;
+struct PromptOdd {
+    int b, head, rows, k_rows;              // looked at: rows of V, of K
+    int first[4][3], k_first;               // of a column of V: the row of the first NaN, infinity, -infinity; of K: the first that has one of them (a
+                                            // NaN, for heads that begin between 16-byte pieces)
+    __device__ __forceinline__ void reset(int b_, int head_)
+    {
+        b = b_;
+        head = head_;
+        rows = k_rows = 0;
+        k_first = kOddNone;
+#pragma unroll
+        for (int e = 0; e < 12; ++e) first[e / 3][e % 3] = kOddNone;
+    }
+};
+// Rows from .. to - 1 of V, until every column has a NaN; where it stopped.  (`first` in registers: through memory no load would pass a store.)
+template <typename T>
+__device__ __forceinline__ int prompt_look_v(const PromptArgs &a, const PromptSeq &s, int b, int h, int from, int to, int lane, int c0, int c1, int (&first)[4][3])
+{
+    constexpr uint32_t kInf = Infinite<T>::bits, kTop = 0x80008000u;
+    uint32_t known[2][3];                                          // of a pair of columns: the highest bit of a half whose column has had one
+#pragma unroll
+    for (int e = 0; e < 6; ++e) known[e / 3][e % 3] = (first[e / 3 * 2][e % 3] != kOddNone ? 0x8000u : 0u) | (first[e / 3 * 2 + 1][e % 3] != kOddNone ? 0x80000000u : 0u);
+    while (from < to) {
+        bool open = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) open = open || (c0 + 2 * (lane + 32 * (e / 2)) < c1 && first[e][0] == kOddNone);
+        if (!__any_sync(0xffffffffu, open)) break;
+        const size_t mine = from + lane < to ? prompt_row(a, s, b, h, from + lane, true) : 0;
+        const int rows = min(to - from, 32);
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            uint32_t w[8][2], odd = 0;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const T *v = (const T *)a.v + __shfl_sync(0xffffffffu, mine, r0 + r);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int col = c0 + 2 * (lane + 32 * e);
+                    w[r][e] = r0 + r < rows && col < c1 ? __ldg(reinterpret_cast<const uint32_t *>(v + col)) : 0u;
+                    odd |= (w[r][e] & 0x7fff7fffu) + (0x8000u - kInf) * 0x10001u;   // (the highest bit of a half whose exponent is full)
+                }
+            }
+            if (!(odd & kTop)) continue;
+            uint32_t any[2][3] = {};
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t x = w[e / 2][e & 1], t = x & 0x7fff7fffu, full = t + (0x8000u - kInf) * 0x10001u, nan = t + (0x7fffu - kInf) * 0x10001u;
+                any[e & 1][0] |= nan;
+                any[e & 1][1] |= full & ~nan & ~x;
+                any[e & 1][2] |= full & ~nan & x;
+            }
+            uint32_t more = 0;
+#pragma unroll
+            for (int e = 0; e < 6; ++e) more |= any[e / 3][e % 3] & ~known[e / 3][e % 3];
+            if (!(more & kTop)) continue;                          // (all of kinds that their columns have had)
+#pragma unroll
+            for (int e = 0; e < 6; ++e) known[e / 3][e % 3] |= any[e / 3][e % 3] & kTop;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t x = w[r][e / 2] >> (e & 1) * 16 & 0x7fffu;
+                    const bool minus = w[r][e / 2] >> (e & 1) * 16 & 0x8000u;
+                    const int at = from + r0 + r;
+                    if (x > kInf) first[e][0] = min(first[e][0], at);
+                    if (x == kInf && !minus) first[e][1] = min(first[e][1], at);
+                    if (x == kInf && minus) first[e][2] = min(first[e][2], at);
+                }
+            }
+        }
+        from += rows;
+    }
+    return from;
+}
+// Rows from .. to - 1 of K, until one has an infinity or a NaN (NAN_ALONE: a NaN): that one, or kOddNone.
+template <typename T, bool NAN_ALONE>
+__device__ __forceinline__ int prompt_look_k(const PromptArgs &a, const PromptSeq &s, int b, int h, int from, int to, int lane)
+{
+    constexpr uint32_t kInf = Infinite<T>::bits;
+    for (; from < to; from += 32) {
+        const size_t mine = from + lane < to ? prompt_row(a, s, b, h, from + lane, false) : 0;
+        const int rows = min(to - from, 32);
+        int first = kOddNone;
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            for (int e0 = 0; e0 < a.d; e0 += 64) {
+                const int e = e0 + 2 * lane;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const T *k = (const T *)a.k + __shfl_sync(0xffffffffu, mine, r0 + r);
+                    const uint32_t w = r0 + r < rows && e < a.d ? __ldg(reinterpret_cast<const uint32_t *>(k + e)) : 0u;
+                    if (((w & 0x7fff7fffu) + ((NAN_ALONE ? 0x7fffu : 0x8000u) - kInf) * 0x10001u) & 0x80008000u) first = min(first, from + r0 + r);
+                }
+            }
+        }
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (first != kOddNone) return first;
+    }
+    return kOddNone;
+}
+
+// An output row with elements that are no finite numbers, by a warp: each is what the values that the row attends make it, whatever stands beside them in a
+// tile.  A NaN among them makes NaN, an infinity that infinity, one of either sign NaN (weights are above zero, where no score is infinite); in half precision an
+// infinity without one is an output past the largest value by its roundings.  What is left (a row beside infinities or NaN that it does not attend, values of
+// bfloat16 near 2^127) is made again from the rows it attends.
+// Rows of V are looked at once for all rows of a key head: made again row by row, one NaN in a prompt of 16384 tokens took 537 ms of a call of 0.26.
+template <typename T>
+__device__ __noinline__ void prompt_mend_row(const PromptArgs &a, const PromptSeq &s, int b, int i, int head, int lane, int c0, int c1, PromptOdd &odd)
+{
+    const int h = a.by_per_kv(head), n = s.p + s.seen(i, a.causal);
+    if (odd.b != b || odd.head != h) odd.reset(b, h);
+    const T *q = (const T *)a.q + (s.q0 + i) * a.q_token + head * a.q_head;
+    if (a.shifted) {                                               // NaN by its own scores, or by what lies beside them
+        bool nan = false;
+        for (int e = lane; e < a.d; e += 32) nan = nan || isnan(to_f32(q[e]));
+        if (odd.k_rows < n && odd.k_first == kOddNone) {
+            odd.k_first = prompt_look_k<T, true>(a, s, b, h, odd.k_rows, n, lane);
+            odd.k_rows = n;
+        }
+        if (!__any_sync(0xffffffffu, nan) && odd.k_first >= n) prompt_row_by_warp<T>(a, s, b, i, head, lane, c0, c1);
+        return;
+    }
+    int first[4][3];
+#pragma unroll
+    for (int e = 0; e < 12; ++e) first[e / 3][e % 3] = odd.first[e / 3][e % 3];
+    if (odd.rows < n) {
+        odd.rows = prompt_look_v<T>(a, s, b, h, odd.rows, n, lane, c0, c1, first);
+#pragma unroll
+        for (int e = 0; e < 12; ++e) odd.first[e / 3][e % 3] = first[e / 3][e % 3];
+    }
+    const size_t row = ((size_t)(s.q0 + i) * a.kv_heads * a.per_kv + head) * a.d;
+    float y[4];
+    bool fix[4], made = false, infinite = false, only16[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int col = c0 + 2 * (lane + 32 * (e / 2)) + (e & 1);
+        fix[e] = only16[e] = false;
+        y[e] = 0.f;
+        if (col >= c1 || !prompt_odd<T>(a, row + col)) continue;
+        fix[e] = true;
+        const bool nan = first[e][0] < n, plus = first[e][1] < n, minus = first[e][2] < n;
+        const float x = a.out ? to_f32(((const T *)a.out)[row + col]) : a.out_f32[row + col];
+        if (nan || (plus && minus)) y[e] = NAN;
+        else if (plus || minus) {
+            y[e] = plus ? INFINITY : -INFINITY;
+            infinite = true;
+        } else if (std::is_same<T, __half>::value && a.out && !isnan(x)) {
+            y[e] = copysignf(65504.f, x);
+            only16[e] = true;
+        } else {
+            made = true;
+        }
+    }
+    made = __any_sync(0xffffffffu, made);
+    if (!made && __any_sync(0xffffffffu, infinite)) {              // a weight of zero, or none: an infinite score
+        bool bad = false;
+        for (int e = lane; e < a.d; e += 32) bad = bad || !(fabsf(to_f32(q[e])) < INFINITY);
+        if (odd.k_rows < n && odd.k_first == kOddNone) {
+            odd.k_first = prompt_look_k<T, false>(a, s, b, h, odd.k_rows, n, lane);
+            odd.k_rows = n;
+        }
+        made = odd.k_first < n || __any_sync(0xffffffffu, bad);
+    }
+    if (made) {
+        prompt_row_by_warp<T>(a, s, b, i, head, lane, c0, c1);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int col = c0 + 2 * (lane + 32 * (e / 2)) + (e & 1);
+        if (!fix[e]) continue;
+        if (a.out) reinterpret_cast<uint16_t *>(a.out)[row + col] = (uint16_t)pack2<T>(y[e], 0.f);
+        if (a.out_f32 && !only16[e]) a.out_f32[row + col] = y[e];
+    }
 }
 
 size_t prompt_workspace(int head_dim, int sms, PromptArgs *a, void *workspace);   // lays the workspace out; its size

@@ -266,7 +266,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_col = tmem + g * 128 + lanes, o_col = tmem + 256 + g * 128 + lanes;
         const int in = a.by_per_kv(row), in_head = row - in * a.per_kv;   // token in the item, head in the key head's
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
-        bool again = false;                                        // a row came out too large for its type, or NaN
+        bool again = false;                                        // a row came out too large for its type, or NaN where its weights are fine
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<true> item(a, it.s, it.q);
@@ -384,6 +384,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                 else if (a.lse) a.lse[to] = none ? -INFINITY : (m2 + log2f(l)) * 0.693147180559945309f;
             }
             if (warp_there) {
+                bool fits = true;
 #pragma unroll 1
                 for (int x0 = 0; x0 < a.d; x0 += 32) {
                     float o[16], o1[16];
@@ -402,7 +403,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                             if (partial) {
                                 *reinterpret_cast<float2 *>(a.state + ((size_t)it.slot * (DO / 4) + x / 4) * 1024 + row * 4 + x % 4) = y;
                             } else {
-                                again = again || !prompt_fits<T>(y.x) || !prompt_fits<T>(y.y);
+                                fits = fits && prompt_fits<T>(y.x) && prompt_fits<T>(y.y);
                                 if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + to * a.d + x) = pack2<T>(y.x, y.y);
                                 if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + to * a.d + x) = y;
                             }
@@ -410,14 +411,20 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                     }
                     __syncwarp();
                 }
+                if (!fits) {
+                    if (!prompt_lost(a, l)) again = true;
+                    else if ((lane & 3) == 0) prompt_mark_lost(a, to * a.d);
+                }
             }
             tc_before();                                           // read before the next item's products write O
             __syncwarp();
             if (lane == 0) mbar_arrive(m_empty);
         }
-        // rows that came out too large or NaN, from what they attend alone: the run once more, in whole items
+        // rows that came out too large or NaN, by what they attend alone: the run once more, in whole items
         if (__any_sync(0xffffffffu, again)) {
             const TilePos end = c.ends[1];
+            PromptOdd odd;
+            odd.reset(-1, 0);
             for (TilePos pos = c.ends[0]; pos.before(end);) {
                 const PromptSeq s = prompt_seq(a, pos.b);
                 if (s.m > 0) {
@@ -429,8 +436,9 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
                             const int i = a.by_per_kv(r), tok = item.first + i, head = pos.head * a.per_kv + r - i * a.per_kv;
                             const size_t first = ((size_t)(s.q0 + tok) * (a.kv_heads * a.per_kv) + head) * a.d;
                             bool bad = false;
-                            for (int e = lane; e < a.d; e += 32) bad = bad || !prompt_fits<T>(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]);
-                            if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, s, pos.b, tok, head, lane, 0, a.d);
+                            if (prompt_marked_lost(a, first)) continue;
+                            for (int e = lane; e < a.d; e += 32) bad = bad || prompt_odd<T>(a, first + e);
+                            if (__any_sync(0xffffffffu, bad)) prompt_mend_row<T>(a, s, pos.b, tok, head, lane, 0, a.d, odd);
                         }
                     }
                 }

@@ -19,7 +19,7 @@
 // The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units): until then weights up to 2^8
 // are allowed, sums and products stay exact multiples, and O is rarely rescaled.  Weights are rounded once to the 16-bit type.
 // Rows of V behind the end are cleared in shared memory before they are used.  A weight of zero does not silence an infinity or NaN of a
-// later token's V in the same tile: a row that comes out NaN or too large for its type is made again by one warp from the rows it attends.
+// later token's V in the same tile: a row that comes out NaN or too large for its type is mended by one warp from the rows it attends.
 //
 // 16384 tokens x 16 heads on 4 of 128, causal (1.1 TFLOP): 0.96 ms, 1.15 PFLOP/s of 1.68 measured.  128 cached rows for both groups take 3200
 // clocks at 1.7 GHz; the products alone are 2048, the exponentials too (both units 64% busy, issue slots 38%).  What bounds is a group's chain:
@@ -428,7 +428,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
         const uint32_t my_s = s_full + 8 * g, my_p = p_full + 32 * g, my_o = o_full + 8 * g;
         const int tph = a.half_tokens, heads = a.kv_heads * a.per_kv;
         uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
-        bool again = false;                                        // a row of this lane came out too large for its type, or NaN
+        bool again = false;                                        // a row of this lane came out too large for its type, or NaN where its weights are fine
         for (; have_item(); next_item()) {
             const TileDesc &it = c.ring[at];
             const TileItem<WIDE> item(a, it.s, it.q);
@@ -678,12 +678,17 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                 __syncwarp();
                 if (lane == 0) mbar_arrive(m_empty);
             }
-            again = again || (there && !partial && !prompt_fits<T>(most));
+            if (there && !partial && !prompt_fits<T>(most)) {
+                if (prompt_lost(a, l)) prompt_mark_lost(a, (size_t)at_row * a.d + c0);
+                else again = true;
+            }
         }
-        // Rows that came out too large or NaN, from what they attend alone: the run once more, in whole items.  (A call in the loop above
+        // Rows that came out too large or NaN, by what they attend alone: the run once more, in whole items.  (A call in the loop above
         // cost it 8%.)
         if (__any_sync(0xffffffffu, again)) {
             const TilePos end = c.ends[1];
+            PromptOdd odd;
+            odd.reset(-1, 0);
             for (TilePos pos = c.ends[0]; pos.before(end); pos.tile = 0) {
                 const PromptSeq s = prompt_seq(a, pos.b);
                 if (s.m > 0) {
@@ -695,11 +700,12 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
                         bool bad = false;
                         if (in < tph && at < item.count) {
                             const size_t first = ((size_t)(s.q0 + tok) * heads + head) * a.d;
-                            for (int e = c0; e < c1; ++e) bad = bad || !prompt_fits<T>(a.out ? to_f32(((const T *)a.out)[first + e]) : a.out_f32[first + e]);
+                            if (!prompt_marked_lost(a, first + c0))
+                                for (int e = c0; e < c1 && !bad; ++e) bad = prompt_odd<T>(a, first + e);
                         }
                         for (unsigned todo = __ballot_sync(0xffffffffu, bad); todo; todo &= todo - 1) {
                             const int src = __ffs(todo) - 1;
-                            prompt_row_by_warp<T>(a, s, pos.b, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), lane, c0, c1);
+                            prompt_mend_row<T>(a, s, pos.b, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), lane, c0, c1, odd);
                         }
                     }
                 }
@@ -728,16 +734,65 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
     }
 }
 
-// Joins the states of items that runs have cut: a warp per row, blocks (cut, eight rows).  The run that began such an item
-// names it; the runs behind it have one state each, up to the one that ended the item.
 constexpr int kTileMergeThreads = 256;
+// The rows `mend` (token, query head; token -1: none) of a cut item of sequence b and key head h, by a block: its warps look at a part of K and V each, and
+// one mends the rows.
+template <typename T>
+__device__ __noinline__ void prompt_mend_block(const PromptArgs &a, const int2 *mend, int (*firsts)[32], int b, int h, int lane, int warp, int c0, int c1)
+{
+    for (int i = threadIdx.x; i < 13 * 32; i += kTileMergeThreads) firsts[i / 32][i % 32] = kOddNone;
+    const PromptSeq whole = prompt_seq(a, b);
+    int last = -1;                                                 // of the tokens
+    for (int w = 0; w < kTileMergeThreads / 32; ++w) last = max(last, mend[w].x);
+    const int n = whole.p + whole.seen(last, a.causal), part = (n + kTileMergeThreads / 32 - 1) / (kTileMergeThreads / 32), from = min(warp * part, n), to = min(from + part, n);
+    PromptOdd odd;
+    odd.reset(b, h);
+    __syncthreads();
+    {
+        int first[4][3];
+#pragma unroll
+        for (int e = 0; e < 12; ++e) first[e / 3][e % 3] = kOddNone;
+        if (!a.shifted) {
+            prompt_look_v<T>(a, whole, b, h, 0, min(n, 32), lane, c0, c1, first);   // (every column may have its NaN there)
+            prompt_look_v<T>(a, whole, b, h, from, to, lane, c0, c1, first);
+        }
+#pragma unroll
+        for (int e = 0; e < 12; ++e)
+            if (first[e / 3][e % 3] != kOddNone) atomicMin(&firsts[e][lane], first[e / 3][e % 3]);
+    }
+    __syncthreads();
+    bool infinite = false;                                         // of a column: K decides
+#pragma unroll
+    for (int e = 0; e < 12; ++e) odd.first[e / 3][e % 3] = firsts[e][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) infinite = infinite || (odd.first[e][0] == kOddNone && min(odd.first[e][1], odd.first[e][2]) != kOddNone);
+    if (a.shifted || __any_sync(0xffffffffu, infinite)) {          // (the same for all warps)
+        const int k_first = a.shifted ? prompt_look_k<T, true>(a, whole, b, h, from, to, lane) : prompt_look_k<T, false>(a, whole, b, h, from, to, lane);
+        if (k_first != kOddNone) atomicMin(&firsts[12][lane], k_first);
+        __syncthreads();
+        odd.k_first = firsts[12][lane];
+        odd.k_rows = n;
+    }
+    if (warp) return;
+    odd.rows = n;
+    for (int w = 0; w < kTileMergeThreads / 32; ++w) {
+        const int2 which = mend[w];
+        if (which.x >= 0) prompt_mend_row<T>(a, whole, b, which.x, which.y, lane, c0, c1, odd);
+    }
+}
+
+// Joins the states of items that runs have cut: a warp per row, blocks (cut, eight rows).  The run that began such an item
+// names it; the runs behind it have one state each, up to the one that ended the item.  Rows of a block that are to be mended are so by one warp, after all
+// have looked at a part of K and V for them.
 template <typename T, int NSUB, bool FEW>
-__global__ void __launch_bounds__(kTileMergeThreads)
+__global__ void __launch_bounds__(kTileMergeThreads, 4)
 prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
 {
     constexpr bool WIDE = NSUB > 2;                                // (the kernel for few rows: items of one half of up to 64 rows)
     constexpr int DO = WIDE ? 128 : 64 * NSUB, PER = DO / 32, AHEAD = 4;
-    const int lane = threadIdx.x & 31, r = (int)blockIdx.y * (kTileMergeThreads / 32) + (threadIdx.x >> 5);
+    __shared__ int2 mend[kTileMergeThreads / 32];                  // token, query head; token -1: nothing to mend
+    __shared__ int firsts[13][32];                                 // (of prompt_mend_block)
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = (int)blockIdx.y * (kTileMergeThreads / 32) + warp;
     pdl_wait();
     pdl_launch();
     const int lead = blockIdx.x;
@@ -750,59 +805,66 @@ prompt_tile_merge_kernel(const __grid_constant__ PromptArgs a, int runs)
     s.n = d2.z;
     s.p = d2.w;
     const TileItem<WIDE || FEW> item(a, s, d.z);
-    const int half = r >> 7, tph = a.half_tokens, in = a.by_per_kv(r & 127), in_item = in + (WIDE ? 0 : half * tph);
-    if (in >= tph || in_item >= item.count || (half && !WIDE && !item.pair)) return;
+    const int half = r >> 7, tph = a.half_tokens, in = a.by_per_kv(r & 127), in_item = in + (WIDE ? 0 : half * tph);   // (half: the same for a block)
     int pieces = 1;
     for (int w = 0; lead + pieces < runs && !w; ++pieces) {
         w = a.run_desc[2 * (lead + pieces)].w;
         if (w & 2) return;                                         // a block that gave up has left no state
     }
-    const int tok = item.first + in_item, head = d.y * a.per_kv + (r & 127) - in * a.per_kv;
-    float m = -INFINITY, l = 0.f, o[PER];
+    const bool there = in < tph && in_item < item.count && !(half && !WIDE && !item.pair);
+    const int c0 = WIDE ? half * DO : 0, c1 = min(a.d, c0 + DO);
+    bool bad = false;
+    if (there) {
+        const int tok = item.first + in_item, head = d.y * a.per_kv + (r & 127) - in * a.per_kv;
+        float m = -INFINITY, l = 0.f, o[PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = 0.f;
-    for (int i0 = 0; i0 < pieces; i0 += AHEAD) {
-        float2 ml[AHEAD];
-        float x[AHEAD][PER];
+        for (int e = 0; e < PER; ++e) o[e] = 0.f;
+        for (int i0 = 0; i0 < pieces; i0 += AHEAD) {
+            float2 ml[AHEAD];
+            float x[AHEAD][PER];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int i = i0 + k;
-            ml[k] = make_float2(-INFINITY, 0.f);
-            if (i < pieces) {
-                const size_t slot = (size_t)2 * (lead + i) + (i == 0 ? 1 : 0);
-                ml[k] = *reinterpret_cast<const float2 *>(a.state_ml + 2 * (slot * 256 + r));
-                // a lane has PER neighbouring elements
-                const float *from = a.state + (slot * (DO / 4) + lane * PER / 4) * 1024 + r * 4 + lane * PER % 4;
-                if constexpr (PER == 4) *reinterpret_cast<float4 *>(x[k]) = *reinterpret_cast<const float4 *>(from);
-                else *reinterpret_cast<float2 *>(x[k]) = *reinterpret_cast<const float2 *>(from);
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = i0 + k;
+                ml[k] = make_float2(-INFINITY, 0.f);
+                if (i < pieces) {
+                    const size_t slot = (size_t)2 * (lead + i) + (i == 0 ? 1 : 0);
+                    ml[k] = *reinterpret_cast<const float2 *>(a.state_ml + 2 * (slot * 256 + r));
+                    // a lane has PER neighbouring elements
+                    const float *from = a.state + (slot * (DO / 4) + lane * PER / 4) * 1024 + r * 4 + lane * PER % 4;
+                    if constexpr (PER == 4) *reinterpret_cast<float4 *>(x[k]) = *reinterpret_cast<const float4 *>(from);
+                    else *reinterpret_cast<float2 *>(x[k]) = *reinterpret_cast<const float2 *>(from);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (i0 + k >= pieces) continue;
+                const float M = fmaxf(m, ml[k].x), w1 = m == -INFINITY ? 0.f : pa_exp2(m - M), w2 = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
+                l = l * w1 + ml[k].y * w2;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) o[e] = o[e] * w1 + x[k][e] * w2;
+                m = M;
             }
         }
+        const bool none = s.p + s.seen(tok, a.causal) == 0;
+        const float inv = none ? 0.f : 1.f / l;
+        const size_t row = ((size_t)s.q0 + tok) * a.kv_heads * a.per_kv + head;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (ml[k].y == 0.f && ml[k].x == -INFINITY) continue;   // an empty state
-            const float M = fmaxf(m, ml[k].x), w1 = m == -INFINITY ? 0.f : pa_exp2(m - M), w2 = ml[k].x == -INFINITY ? 0.f : pa_exp2(ml[k].x - M);
-            l = l * w1 + ml[k].y * w2;
-#pragma unroll
-            for (int e = 0; e < PER; ++e) o[e] = o[e] * w1 + x[k][e] * w2;
-            m = M;
+        for (int e = 0; e < PER; e += 2) {
+            const int at = c0 + lane * PER + e;
+            if (at >= c1) continue;
+            const float2 x = none ? make_float2(0.f, 0.f) : make_float2(o[e] * inv, o[e + 1] * inv);
+            bad = bad || !prompt_fits<T>(x.x) || !prompt_fits<T>(x.y);
+            if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(x.x, x.y);
+            if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = x;
         }
+        if (a.lse && lane == 0 && c0 == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+        bad = __any_sync(0xffffffffu, bad) && !prompt_lost(a, l);
+        if (lane == 0) mend[warp] = make_int2(bad ? tok : -1, head);
+    } else if (lane == 0) {
+        mend[warp] = make_int2(-1, 0);
     }
-    const bool none = s.p + s.seen(tok, a.causal) == 0;
-    const float inv = none ? 0.f : 1.f / l;
-    const int c0 = WIDE ? half * DO : 0, c1 = min(a.d, c0 + DO);
-    const size_t row = ((size_t)s.q0 + tok) * a.kv_heads * a.per_kv + head;
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < PER; e += 2) {
-        const int at = c0 + lane * PER + e;
-        if (at >= c1) continue;
-        const float2 x = none ? make_float2(0.f, 0.f) : make_float2(o[e] * inv, o[e + 1] * inv);
-        bad = bad || !prompt_fits<T>(x.x) || !prompt_fits<T>(x.y);
-        if (a.out) *reinterpret_cast<uint32_t *>((T *)a.out + row * a.d + at) = pack2<T>(x.x, x.y);
-        if (a.out_f32) *reinterpret_cast<float2 *>(a.out_f32 + row * a.d + at) = x;
-    }
-    if (a.lse && lane == 0 && c0 == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
-    if (__any_sync(0xffffffffu, bad)) prompt_row_by_warp<T>(a, prompt_seq(a, d.x), d.x, tok, head, lane, c0, c1);
+    // (lanes look at what others wrote)
+    if (__syncthreads_or(bad)) prompt_mend_block<T>(a, mend, firsts, d.x, d.y, lane, warp, c0, c1);
 }
 
 size_t prompt_workspace(int head_dim, int sms, PromptArgs *a, void *workspace)
