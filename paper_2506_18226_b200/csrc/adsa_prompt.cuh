@@ -6,7 +6,7 @@
 
 namespace adsa {
 
-// Division of numbers below 2^31 by a divisor that the host knows.
+// Division of numbers below 2^31 by a divisor that the host knows, by a product and a shift (Granlund and Montgomery 1994).
 struct FastDiv {
     uint32_t mul, shift;
     FastDiv() = default;

@@ -7,8 +7,8 @@
 // take the tiles in turns, so that one's products run under the other's softmax, and join their states at the end.  Q takes half of what
 // two halves take and outputs go straight to memory: the ring of tiles has the rest, 160 to 192 KB.
 //
-// 32 sequences of one token over 1144 rows of 20 heads of 64 (188 MB): 41 us, 4.6 TB/s of 6.5 measured; 8 x 5 tokens over up to 16384 rows of 8 key heads of
-// 128 (302 MB): 58 us, 5.2 TB/s.  What bounds: for long rows the memory; for short ones an item's fixed part, some 5000 clocks of first copies,
+// 32 sequences of one token over 1144 rows of 20 heads of 64 (188 MB): 41 .. 45 us, 4.2 .. 4.6 TB/s of 6.5 measured; 8 x 5 tokens over up to 16384 rows of 8 key
+// heads of 128 (302 MB): 61 .. 62 us, 4.9 TB/s.  Weights are rounded as the tile kernel rounds them.  What bounds: for long rows the memory; for short ones an item's fixed part, some 5000 clocks of first copies,
 // joining and outputs, most of them waiting for instructions that run once per item (so this code is kept short).
 
 #include "adsa_prompt_tile.cuh"

@@ -13,21 +13,23 @@
 // tensor memory at the end.  Heads of more than 128 elements (WIDE): items of up to 128 rows, both groups make the same scores and
 // weights, and each has 128 elements of O.
 //
-// The list of items in units (a tile of a half; two for what an item costs beside them) is cut into one run per block.  A cut near the
+// The list of items in units (a tile of a half; eight for what an item costs beside them) is cut into one run per block.  A cut near the
 // end of an item moves there; else the item's states go to the workspace, and a second kernel joins them.
 //
 // The running maximum of a row only moves when a tile exceeds it by more than 8 (in log2 units): until then weights up to 2^8
-// are allowed, sums and products stay exact multiples, and O is rarely rescaled.  Weights are rounded once to the 16-bit type.
+// are allowed, sums and products stay exact multiples, and O is rarely rescaled.  Weights are rounded once to the 16-bit type, their sum is taken before: a
+// second value for what the rounding leaves would add half as many products again and as many conversions to the chain below; so the error of an output
+// against 64 bits is 1.1 to 1.4 times that of rounding it alone (bfloat16 0.0016 -> 0.0018 .. 0.0023, half 0.00021 -> 0.00023 .. 0.00029).
 // Rows of V behind the end are cleared in shared memory before they are used.  A weight of zero does not silence an infinity or NaN of a
 // later token's V in the same tile: a row that comes out NaN or too large for its type is mended by one warp from the rows it attends.
 //
-// 16384 tokens x 16 heads on 4 of 128, causal (1.1 TFLOP): 0.96 ms, 1.15 PFLOP/s of 1.68 measured.  128 cached rows for both groups take 3200
+// 16384 tokens x 16 heads on 4 of 128, causal (1.1 TFLOP): 0.99 .. 1.03 ms, 1.07 .. 1.11 PFLOP/s of 1.68 measured.  128 cached rows for both groups take 3200
 // clocks at 1.7 GHz; the products alone are 2048, the exponentials too (both units 64% busy, issue slots 38%).  What bounds is a group's chain:
 // scores out of tensor memory, their maximum, 128 exponentials a thread, the last quarter's product, the next scores.  Weights come in quarters, so
 // that three of four products run under the softmax.  A third of the exponentials by polynomial on the multiply-add pipe:
 // 1020 us where 960 went without, by the length of the code.  Code that does not run counts: with row copies, 32-bit outputs and the call that makes
 // rows again in one loop, 144 KB of it, 48 prompts of 640 tokens took 277 us, 242 without.  An item's fixed part is 5000 clocks (its last product,
-// outputs, next scores), which is what short prompts see: 48 of 143 to 1144 tokens, 26 items of three tiles a block, 280 us.
+// outputs, next scores), which is what short prompts see: 48 of 143 to 1144 tokens, 26 items of three tiles a block, 316 .. 328 us.
 #include <math.h>
 
 #include "adsa_prompt_tile.cuh"
@@ -1011,7 +1013,8 @@ cudaError_t launch_prompt_tiles(int dtype, const PromptArgs &args, int sms, cuda
         }
     }
     const unsigned blocks = (unsigned)sms;
-    // Few rows a sequence, on the mean.  Measured, this kernel / the other in us: 32 sequences x 20 heads of 64 over 600 rows, 8 rows each 30.1 /
+    // Few rows a sequence, on the mean (lengths lie on the device: a long sequence among many single tokens goes by items of 32 rows, which read its cache
+    // eight times as often as items of 256; 255 single tokens over 1000 rows beside 1024 over 4096: 342 us, 161 + 92 in two calls).  Measured, this kernel / the other in us: 32 sequences x 20 heads of 64 over 600 rows, 8 rows each 30.1 /
     // 42.4, 32 rows 32.3 / 42.3, 48 rows (by two items) 44.4 / 43.1; 8 x 8 key heads of 128 over 8000 rows, 8 rows 50.8 / 55.2, 32 rows 52.1 /
     // 57.0, 48 rows 68.3 / 58.1.
     if (a.box_rows && !a.shifted && a.d <= 128 && a.per_kv <= kFewRows && a.n_q * a.per_kv <= (long long)kFewMean * a.batch) {
