@@ -238,6 +238,7 @@ __device__ __noinline__ void prompt_row_by_warp(const PromptArgs &a, const Promp
 constexpr int kOddNone = 0x7fffffff;
 struct PromptOdd {
     int b, head, rows, k_rows;              // looked at: rows of V, of K
+    bool whole;                             // rows are made again as a whole: a block that gave up may not have written them
     int first[4][3], k_first;               // of a column of V: the row of the first NaN, infinity, -infinity; of K: the first that has one of them (a
                                             // NaN, for heads that begin between 16-byte pieces)
     __device__ __forceinline__ void reset(int b_, int head_)
@@ -346,6 +347,10 @@ __device__ __noinline__ void prompt_mend_row(const PromptArgs &a, const PromptSe
     const int h = a.by_per_kv(head), n = s.p + s.seen(i, a.causal);
     if (odd.b != b || odd.head != h) odd.reset(b, h);
     const T *q = (const T *)a.q + (s.q0 + i) * a.q_token + head * a.q_head;
+    if (odd.whole) {
+        prompt_row_by_warp<T>(a, s, b, i, head, lane, c0, c1);
+        return;
+    }
     if (a.shifted) {                                               // NaN by its own scores, or by what lies beside them
         bool nan = false;
         for (int e = lane; e < a.d; e += 32) nan = nan || isnan(to_f32(q[e]));

@@ -425,6 +425,7 @@ prompt_few_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ 
             const TilePos end = c.ends[1];
             PromptOdd odd;
             odd.reset(-1, 0);
+            odd.whole = tile_gave_up(c.waits);
             for (TilePos pos = c.ends[0]; pos.before(end);) {
                 const PromptSeq s = prompt_seq(a, pos.b);
                 if (s.m > 0) {

@@ -691,6 +691,7 @@ prompt_tile_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__
             const TilePos end = c.ends[1];
             PromptOdd odd;
             odd.reset(-1, 0);
+            odd.whole = tile_gave_up(c.waits);
             for (TilePos pos = c.ends[0]; pos.before(end); pos.tile = 0) {
                 const PromptSeq s = prompt_seq(a, pos.b);
                 if (s.m > 0) {
@@ -749,6 +750,7 @@ __device__ __noinline__ void prompt_mend_block(const PromptArgs &a, const int2 *
     const int n = whole.p + whole.seen(last, a.causal), part = (n + kTileMergeThreads / 32 - 1) / (kTileMergeThreads / 32), from = min(warp * part, n), to = min(from + part, n);
     PromptOdd odd;
     odd.reset(b, h);
+    odd.whole = false;
     __syncthreads();
     {
         int first[4][3];

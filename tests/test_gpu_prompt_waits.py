@@ -1,6 +1,7 @@
 """Prompt attention whose waits run out: with no patience at all, kernels give up on copies that are under way.  The call ends, its status says so, what was
 written is right and nothing else was, and the next call is as any other.  No part of the GPU fails here: every copy lands."""
 import contextlib
+import math
 
 import pytest
 import torch
@@ -69,6 +70,28 @@ def test_chunks(batch, m, n, H, KV, d, page, long):
     q = randn(g, batch * m, H, d)
     ws = A.prompt_workspace(q, KV, batch)
     verify(lambda out, lse, status: A.chunk_attn(q, kp, vp, table, rows, out=out, lse=lse, workspace=ws, status=status), q.shape, q.dtype, long)
+
+
+@pytest.mark.parametrize("n,m,d", [(8192, 8192, 128), (6000, 400, 64), (30000, 2, 128)])
+def test_rows_that_held_infinities_before_are_left_or_right(n, m, d):
+    """Values of infinity make rows that are mended after the others; what was not written is not taken for one of them."""
+    import paper_2506_18226_b200 as A
+    g, H, KV, batch = gen(n), 4, 1, 40 if m < 10 else 1
+    q, k, v = randn(g, batch * m, H, d), randn(g, batch * n, KV, d), randn(g, batch * n, KV, d)
+    v[n // 2, :, 3] = math.inf
+    ws, cu = A.prompt_workspace(q, KV, batch), starts([m] * batch)
+    want = A.packed_attn(q, k, v, cu, starts([n] * batch), workspace=ws)
+    out, status = torch.full_like(want, math.inf), torch.zeros(1, dtype=torch.int32, device=DEV)
+    with patience(0):
+        A.packed_attn(q, k, v, cu, starts([n] * batch), out=out, workspace=ws, status=status)
+    torch.cuda.synchronize()
+    left = (out == math.inf).all(-1)
+    assert m == 400 or (int(status) == A.binding.DEV_COPY_TIMEOUT and bool(left.any()))   # (400 tokens: a part of an item a block, no wait of 4 us need be)
+    # (a row made again as a whole has its weights in 32 bits)
+    got, ref = out[~left].float(), want[~left].float()
+    odd = ~torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got), ~odd) and torch.equal(got[odd], ref[odd])
+    assert ((got - ref)[~odd].abs() <= 0.05).all()
 
 
 def test_a_call_without_a_status():
