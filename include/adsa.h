@@ -541,8 +541,9 @@ ADSA_API int adsa_norm_residual(int dtype, int x_dtype, const void *y, const voi
  * A row with nothing to attend gets out = 0 and lse = -inf.  softmax_scale 0 => 1/sqrt(head_dim).  workspace: [device] 256-byte
  * aligned, adsa_prompt_workspace_bytes of them, nothing kept in it from call to call: calls that may overlap on the GPU need one
  * each, and a captured call's must outlive its graph. */
-/* How often a wait polls (4 microseconds each) before its block gives up, in the calls that are made or captured from now on; below 0, as it is
- * at first: 2^18, and 64 more for every 128 rows that a sequence of the call can have.  Returns what it was.  So that the report can be tested: with 0, a wait that is not over within one poll has run out. */
+/* How often a wait polls (4 microseconds each) before its block gives up, in the calls that are made or captured from now on; below
+ * 0, as it is at first: 2^18, and 64 more for every 128 rows that a sequence of the call can have.  Returns what it was.  So that the
+ * report can be tested: with 0, a wait that is not over within one poll has run out. */
 ADSA_API int adsa_prompt_wait_polls(int polls);
 ADSA_API int adsa_prompt_workspace_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, size_t *out_bytes);
 
